@@ -19,6 +19,12 @@
  *   cure_resync_kv    Sec. 3.5, Alg. 1      write the path into the KV cache,
  *                                           realign the draft state
  *
+ * Around the step, for the target model's own attention layers:
+ *   cure_rope_qkv     Sec. 3.2, 3.4         head norms and rotary rotation of the tree's rows
+ *                                           at their positions, as cure_tree_attn takes them
+ *   cure_append_kv    Alg. 1 (input)        the same for prompt rows, K and V into the cache
+ *   cure_prompt_attn  Alg. 1 (input)        causal attention of prompt rows over the cache
+ *
  * Conventions shared by every call
  *  - Every pointer argument is a DEVICE pointer unless stated otherwise; the
  *    caller owns all memory (inputs, outputs, caches, workspace).  The library
@@ -322,6 +328,101 @@ cure_status cure_resync_kv(int32_t layers, void* const* k_caches, void* const* v
                            const int32_t* out_tokens, const int32_t* cache_len_in,
                            int32_t* cache_len_out, int32_t* draft_valid_len,
                            int32_t* replay_tokens, int32_t* n_replay, void* stream);
+
+/*
+ * The rotary rotation of a head (a HOST struct, made by cure_rope_init or
+ * cure_rope_init_freqs).  Of a head's first rot_dim values, pair i (0 <= i <
+ * rot_dim / 2) at position p turns by the angle p * f_i:
+ *   a' = A (a cos(p f_i) - b sin(p f_i)),  b' = A (b cos(p f_i) + a sin(p f_i))
+ * with A = amplitude and the pair (a, b) = values (i, i + rot_dim / 2) in style 0
+ * (half), values (2i, 2i + 1) in style 1 (interleaved); the other values pass
+ * through.
+ */
+typedef struct {
+  int32_t style;        /* 0: half, 1: interleaved */
+  int32_t rot_dim;      /* values of a head that are rotated: 0 (none) or a multiple of 16 up to 128 */
+  float amplitude;      /* A; 1 without scaling for long contexts that asks for another */
+  int32_t reserved;     /* 0 */
+  uint64_t turns[64];   /* f_i / (2 pi) modulo 1, in units of 2^-64 */
+} cure_rope;
+
+/* Frequencies scaled for longer contexts than a model was trained on. */
+typedef struct {
+  int32_t kind;         /* 0: none
+                           1 linear: f_i / factor
+                           2 base:   f_i of the base  base * factor^(r / (r - 2)), r = rot_dim
+                           3 bands:  with t_i = f_i original / (2 pi) turns within the original
+                                     context: f_i where t_i >= high, f_i / factor where t_i <= low,
+                                     between them g f_i + (1 - g) f_i / factor, g = (t_i - low) / (high - low)
+                           4 ramp:   (1 - g) f_i + g f_i / factor, g = clip((i - i_0) / (i_1 - i_0), 0, 1),
+                                     i_0 = max(floor(d(high)), 0), i_1 = min(ceil(d(low)), r - 1) (i_0 + 0.001 if
+                                     that is not above i_0), d(t) = r ln(original / (2 pi t)) / (2 ln base) */
+  int32_t reserved;     /* 0 */
+  double factor;        /* > 0 */
+  double low, high;     /* bands, ramp: turns, 0 < low < high */
+  double original;      /* bands, ramp: the original context length in tokens, > 0 */
+} cure_rope_scaling;
+
+/*
+ * Fills *out with the frequencies f_i = base^(-2i / rot_dim), scaled as `scaling`
+ * says (NULL: not at all), in 64-bit arithmetic on the host.  base > 1 and finite
+ * (CURE_ERR_INVALID_ARG otherwise, as for a rot_dim that is odd or outside
+ * 2..128); rot_dim a multiple of 16 (CURE_ERR_UNSUPPORTED otherwise).
+ */
+cure_status cure_rope_init(cure_rope* out, int32_t style, int32_t rot_dim, double base,
+                           const cure_rope_scaling* scaling, float amplitude);
+
+/* The same from the caller's own frequencies: `freqs` is a HOST array of rot_dim / 2
+ * finite values, in radians per position. */
+cure_status cure_rope_init_freqs(cure_rope* out, int32_t style, int32_t rot_dim, const double* freqs,
+                                 float amplitude);
+
+/*
+ * Per-head norms and the rotation, from the rows of a layer's Q/K/V projection
+ * to the rows that cure_tree_attn takes (Sec. 3.2, 3.4: the target scores the
+ * tree's nodes at their own positions).  For row r with pos[r] >= 0, every head
+ * x of q and k:
+ *   y = x * w / sqrt(mean(x^2) + eps)   (w = q_norm or k_norm, bf16 [D]; NULL: y = x)
+ * then y is rotated to position pos[r] by `rope` (a HOST pointer; NULL: not at
+ * all); heads of v are copied.  All in float32, rounded to bf16 once.  Rows with
+ * pos[r] < 0 (the padding of cure_build_tree's `pos`) are neither read nor written.
+ * q [rows][heads_q][D], k and v [rows][heads_kv][D], bf16; row r of a tensor
+ * starts ld values after row r - 1 (its heads lie end to end), so that the three
+ * may be parts of one projection's rows.  A tensor and its output may both be
+ * NULL (left out).  An output may be its input (same address and stride); any
+ * other overlap is not allowed.  head_dim = 128; all pointers 16-byte aligned,
+ * strides multiples of 8 values that hold a row's heads.  The angles are exact
+ * to 2^-32 of a turn at every position.  eps >= 0 and finite.
+ */
+cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                          int32_t rows, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const int32_t* pos,
+                          const cure_rope* rope, const void* q_norm, const void* k_norm, float eps, void* q_out,
+                          void* k_out, void* v_out, int64_t ld_q_out, int64_t ld_k_out, int64_t ld_v_out,
+                          void* stream);
+
+/*
+ * The same for packed rows whose K and V go into the cache (prompts, chunks of
+ * prompts, single new tokens).  Sequence b has the rows row_start[b] ..
+ * row_start[b+1] - 1 (device int32 [batch + 1], ascending; equal: none), and its
+ * i-th row's K and V are written to slot cache_len[b] + i of its cache (one
+ * layer, layout `kv`), behind the cache_len[b] tokens that it holds.  A row's
+ * position is its slot, or pos[row] when `pos` is given (device int32 [rows]);
+ * pos[row] < 0 leaves the row out.  With row_start = 0, n_max, 2 n_max, .. and
+ * the tree's `pos` that is the in-place layout of cure_tree_attn.
+ * q may be NULL (then q_out is not used); otherwise its rows go to q_out as in
+ * cure_rope_qkv.  cache_len is not advanced: every layer of a model is appended
+ * at the same lengths.  Rows outside row_start[0] .. row_start[batch] - 1 are
+ * left out.  A slot past the capacity (CURE_DEVERR_SLOT), a missing or bad page
+ * (CURE_DEVERR_PAGE) and a row_start that does not ascend (CURE_DEVERR_NODES)
+ * leave the rows concerned out.  q, k, v, the norms, strides and alignment as in
+ * cure_rope_qkv; caches 16-byte aligned; the inputs may not overlap the caches.
+ * No two rows of a call may have the same slot of the same page.
+ */
+cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                           int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
+                           const int32_t* cache_len, const int32_t* pos, const cure_kv_desc* kv, void* k_cache,
+                           void* v_cache, const cure_rope* rope, const void* q_norm, const void* k_norm, float eps,
+                           void* q_out, int64_t ld_q_out, void* stream);
 
 /* Reads and clears the device error word of the current device after
  * synchronising `stream`.  *bits receives the CURE_DEVERR_* bits (may be NULL).

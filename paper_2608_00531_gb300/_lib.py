@@ -21,7 +21,8 @@ DEVERR_PAGE, DEVERR_SLOT, DEVERR_NODES, DEVERR_TOKEN, DEVERR_TIMEOUT = 0x1, 0x2,
 EXPORTS = ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_tree_attn_workspace_size",
            "cure_accept", "cure_lm_head_argmax", "cure_lm_head_workspace_size", "cure_selftest_wait_timeout",
            "cure_selftest_lm_head_timeout", "cure_selftest_attn_route",
-           "cure_sample_target", "cure_resync_kv", "cure_device_error",
+           "cure_sample_target", "cure_resync_kv", "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv",
+           "cure_append_kv", "cure_device_error",
            "cure_status_string", "cure_abi_version")
 
 
@@ -39,6 +40,16 @@ class KVDesc(C.Structure):
                 ("block_table", C.c_void_p)]
 
 
+class Rope(C.Structure):
+    _fields_ = [("style", C.c_int32), ("rot_dim", C.c_int32), ("amplitude", C.c_float), ("reserved", C.c_int32),
+                ("turns", C.c_uint64 * 64)]
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("factor", C.c_double), ("low", C.c_double),
+                ("high", C.c_double), ("original", C.c_double)]
+
+
 class CureError(RuntimeError):
     def __init__(self, fn: str, code: int, detail: str = ""):
         super().__init__(f"{fn} returned {STATUS.get(code, code)}" + (f": {detail}" if detail else ""))
@@ -49,6 +60,7 @@ _lib = None
 
 P = C.c_void_p
 I32 = C.c_int32
+I64 = C.c_int64
 
 
 def load() -> C.CDLL:
@@ -80,12 +92,19 @@ def load() -> C.CDLL:
     lib.cure_resync_kv.argtypes = [I32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                    C.POINTER(KVDesc), P, P, I32, I32, I32, P, P, P, P, P, P, P,
                                    P, P, P]
+    lib.cure_rope_init.argtypes = [C.POINTER(Rope), I32, I32, C.c_double, C.POINTER(RopeScaling), C.c_float]
+    lib.cure_rope_init_freqs.argtypes = [C.POINTER(Rope), I32, I32, C.POINTER(C.c_double), C.c_float]
+    lib.cure_rope_qkv.argtypes = [P, P, P, I64, I64, I64, I32, I32, I32, I32, P, C.POINTER(Rope), P, P, C.c_float,
+                                  P, P, P, I64, I64, I64, P]
+    lib.cure_append_kv.argtypes = [P, P, P, I64, I64, I64, I32, I32, I32, P, P, P, C.POINTER(KVDesc), P, P,
+                                   C.POINTER(Rope), P, P, C.c_float, P, I64, P]
     lib.cure_device_error.argtypes = [P, C.POINTER(I32)]
     lib.cure_status_string.argtypes = [C.c_int]
     lib.cure_status_string.restype = C.c_char_p
     lib.cure_abi_version.restype = I32
     for name in ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_accept",
-                 "cure_resync_kv", "cure_device_error", "cure_sample_target", "cure_lm_head_argmax"):
+                 "cure_resync_kv", "cure_device_error", "cure_sample_target", "cure_lm_head_argmax",
+                 "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv", "cure_append_kv"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib

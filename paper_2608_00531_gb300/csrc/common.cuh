@@ -109,6 +109,24 @@ cudaError_t launch_resync(int layers, const LayerPtrs& caches, const cure_kv_des
                           int32_t* draft_valid_len, int32_t* replay_tokens, int32_t* n_replay,
                           int* err, cudaStream_t s);
 
+// Head norms and rotation (cure_rope_qkv), with K and V into the cache (cure_append_kv).
+struct RopeArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t *q_out, *k_out, *v_out;  // append: k_out, v_out are the caches
+  int64_t ld_q, ld_k, ld_v, ld_q_out, ld_k_out, ld_v_out;
+  int rows, heads_q, heads_kv;
+  const int32_t* pos;
+  int batch;  // append
+  const int32_t *row_start, *cache_len;
+  cure_kv_desc kv;
+  cure_rope rope;
+  const uint16_t *q_norm, *k_norm;
+  float eps;
+  int chunks, chunk_heads;  // set by the launcher: a row's heads in `chunks` parts, a warp each
+  int* err;
+};
+cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s);
+
 // Fused LM head + argmax: launch plan for a shape (persistent pairs of CTAs, one
 // tile of nt hidden rows each, the vocabulary's 256-id tiles split into `groups`
 // ranges).

@@ -2,6 +2,7 @@
 // Nothing here allocates device memory.
 #include <cuda.h>
 #include <float.h>
+#include <math.h>
 #include <nvtx3/nvToolsExt.h>
 
 #include <mutex>
@@ -354,6 +355,176 @@ cure_status cure_resync_kv(int32_t layers, void* const* k_caches, void* const* v
                                  path_nodes, accept_len, diverge_depth, out_tokens, cache_len_in,
                                  cache_len_out, draft_valid_len, replay_tokens, n_replay,
                                  device_error_word(), static_cast<cudaStream_t>(stream)));
+}
+
+// ---- rotary rotation
+
+static cure_status rope_shape_ok(const cure_rope* out, int32_t style, int32_t rot_dim, float amplitude) {
+  if (!out || (style != 0 && style != 1) || rot_dim < 2 || rot_dim > 128 || rot_dim % 2 != 0 ||
+      !(fabsf(amplitude) <= FLT_MAX))
+    return CURE_ERR_INVALID_ARG;
+  return rot_dim % 16 == 0 ? CURE_OK : CURE_ERR_UNSUPPORTED;
+}
+
+cure_status cure_rope_init_freqs(cure_rope* out, int32_t style, int32_t rot_dim, const double* freqs,
+                                 float amplitude) {
+  const cure_status st = rope_shape_ok(out, style, rot_dim, amplitude);
+  if (st != CURE_OK) return st;
+  if (!freqs) return CURE_ERR_INVALID_ARG;
+  for (int i = 0; i < rot_dim / 2; ++i)
+    if (!(fabs(freqs[i]) <= DBL_MAX)) return CURE_ERR_INVALID_ARG;
+  cure_rope r = {};
+  r.style = style;
+  r.rot_dim = rot_dim;
+  r.amplitude = amplitude;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    const double t = freqs[i] / 6.283185307179586476925286766559;
+    const double part = t - floor(t);  // [0, 1]: 1 where a tiny negative value rounds up
+    r.turns[i] = part < 1.0 ? (uint64_t)ldexp(part, 64) : 0;
+  }
+  *out = r;
+  return CURE_OK;
+}
+
+cure_status cure_rope_init(cure_rope* out, int32_t style, int32_t rot_dim, double base,
+                           const cure_rope_scaling* scaling, float amplitude) {
+  const cure_status st = rope_shape_ok(out, style, rot_dim, amplitude);
+  if (st == CURE_ERR_INVALID_ARG) return st;
+  if (!(base > 1.0 && base <= DBL_MAX)) return CURE_ERR_INVALID_ARG;
+  const int kind = scaling ? scaling->kind : 0;
+  if (kind < 0 || kind > 4) return CURE_ERR_INVALID_ARG;
+  if (kind > 0 && !(scaling->factor > 0.0 && scaling->factor <= DBL_MAX)) return CURE_ERR_INVALID_ARG;
+  if (kind >= 3 && !(scaling->low > 0.0 && scaling->low < scaling->high && scaling->high <= DBL_MAX &&
+                     scaling->original > 0.0 && scaling->original <= DBL_MAX))
+    return CURE_ERR_INVALID_ARG;
+  if (st != CURE_OK) return st;
+  const double two_pi = 6.283185307179586476925286766559, r = rot_dim;
+  if (kind == 2) base *= pow(scaling->factor, r / (r - 2.0));
+  double first = 0.0, last = 1.0;  // ramp: the pairs between which the slowing grows
+  if (kind == 4) {
+    auto pair = [&](double t) { return r * log(scaling->original / (two_pi * t)) / (2.0 * log(base)); };
+    first = fmax(floor(pair(scaling->high)), 0.0);
+    last = fmin(ceil(pair(scaling->low)), r - 1.0);
+    if (!(last > first)) last = first + 0.001;
+  }
+  double f[64];
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    f[i] = pow(base, -2.0 * i / r);
+    if (kind == 1) f[i] /= scaling->factor;
+    if (kind >= 3) {
+      const double slow = f[i] / scaling->factor;
+      double keep;  // the part of the frequency that stays
+      if (kind == 3) keep = (f[i] * scaling->original / two_pi - scaling->low) / (scaling->high - scaling->low);
+      else keep = 1.0 - (i - first) / (last - first);
+      keep = fmin(fmax(keep, 0.0), 1.0);
+      f[i] = keep * f[i] + (1.0 - keep) * slow;
+    }
+  }
+  return cure_rope_init_freqs(out, style, rot_dim, f, amplitude);
+}
+
+// What cure_rope_qkv and cure_append_kv check alike.
+static cure_status rope_args_ok(const RopeArgs& a, const cure_rope* rope) {
+  if (a.rows < 0 || a.heads_q < 0 || a.heads_kv < 0 || !(a.eps >= 0.f && a.eps <= FLT_MAX)) return CURE_ERR_INVALID_ARG;
+  if (a.heads_q > 4096 || a.heads_kv > 4096) return CURE_ERR_UNSUPPORTED;
+  if (rope && (rope->style < 0 || rope->style > 1 || rope->rot_dim < 0 || rope->rot_dim > 128 ||
+               rope->rot_dim % 16 != 0 || !(fabsf(rope->amplitude) <= FLT_MAX)))
+    return CURE_ERR_INVALID_ARG;
+  const struct { const uint16_t *in, *out; int64_t ld_in, ld_out; int heads; } t[3] = {
+      {a.q, a.q_out, a.ld_q, a.ld_q_out, a.heads_q},
+      {a.k, a.k_out, a.ld_k, a.ld_k_out, a.heads_kv},
+      {a.v, a.v_out, a.ld_v, a.ld_v_out, a.heads_kv}};
+  for (const auto& x : t) {
+    if (!x.in != !x.out) return CURE_ERR_INVALID_ARG;
+    if (!x.in) continue;
+    const int64_t row = (int64_t)x.heads * 128;
+    if (!aligned(x.in, 16) || !aligned(x.out, 16) || x.ld_in % 8 != 0 || x.ld_out % 8 != 0 || x.ld_in < row ||
+        x.ld_out < row)
+      return CURE_ERR_INVALID_ARG;
+  }
+  if (!aligned(a.q_norm, 16) || !aligned(a.k_norm, 16)) return CURE_ERR_INVALID_ARG;
+  return CURE_OK;
+}
+
+cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                          int32_t rows, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const int32_t* pos,
+                          const cure_rope* rope, const void* q_norm, const void* k_norm, float eps, void* q_out,
+                          void* k_out, void* v_out, int64_t ld_q_out, int64_t ld_k_out, int64_t ld_v_out,
+                          void* stream) {
+  ApiRange range("cure_rope_qkv");
+  RopeArgs a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.q_out = static_cast<uint16_t*>(q_out);
+  a.k_out = static_cast<uint16_t*>(k_out);
+  a.v_out = static_cast<uint16_t*>(v_out);
+  a.ld_q = ld_q;
+  a.ld_k = ld_k;
+  a.ld_v = ld_v;
+  a.ld_q_out = ld_q_out;
+  a.ld_k_out = ld_k_out;
+  a.ld_v_out = ld_v_out;
+  a.rows = rows;
+  a.heads_q = heads_q;
+  a.heads_kv = heads_kv;
+  a.pos = pos;
+  a.q_norm = static_cast<const uint16_t*>(q_norm);
+  a.k_norm = static_cast<const uint16_t*>(k_norm);
+  a.eps = eps;
+  const cure_status st = rope_args_ok(a, rope);
+  if (st != CURE_OK) return st;
+  if (head_dim != 128) return head_dim < 1 ? CURE_ERR_INVALID_ARG : CURE_ERR_UNSUPPORTED;
+  if (rows == 0 || (heads_q == 0 && heads_kv == 0) || (!q && !k && !v)) return CURE_OK;
+  if (!pos) return CURE_ERR_INVALID_ARG;
+  if (rope) a.rope = *rope;
+  a.err = device_error_word();
+  return from_cuda(launch_rope(a, false, static_cast<cudaStream_t>(stream)));
+}
+
+cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                           int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
+                           const int32_t* cache_len, const int32_t* pos, const cure_kv_desc* kv, void* k_cache,
+                           void* v_cache, const cure_rope* rope, const void* q_norm, const void* k_norm, float eps,
+                           void* q_out, int64_t ld_q_out, void* stream) {
+  ApiRange range("cure_append_kv");
+  cure_status why;
+  if (!kv_ok(kv, &why)) return why;
+  RopeArgs a = {};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.q_out = q ? static_cast<uint16_t*>(q_out) : nullptr;
+  a.k_out = static_cast<uint16_t*>(k_cache);
+  a.v_out = static_cast<uint16_t*>(v_cache);
+  a.ld_q = ld_q;
+  a.ld_k = ld_k;
+  a.ld_v = ld_v;
+  a.ld_q_out = ld_q_out;
+  a.ld_k_out = a.ld_v_out = (int64_t)kv->heads_kv * kv->head_dim;
+  a.rows = rows;
+  a.heads_q = q ? heads_q : 0;
+  a.heads_kv = kv->heads_kv;
+  a.pos = pos;
+  a.batch = batch;
+  a.row_start = row_start;
+  a.cache_len = cache_len;
+  a.kv = *kv;
+  a.q_norm = static_cast<const uint16_t*>(q_norm);
+  a.k_norm = static_cast<const uint16_t*>(k_norm);
+  a.eps = eps;
+  if (batch < 0 || (q && heads_q < 1)) return CURE_ERR_INVALID_ARG;
+  if (rows == 0 || batch == 0) {  // nothing to append, whatever the pointers
+    a.q = a.k = a.v = nullptr;
+    a.q_out = a.k_out = a.v_out = nullptr;
+  }
+  const cure_status st = rope_args_ok(a, rope);
+  if (st != CURE_OK) return st;
+  if (rows == 0 || batch == 0) return CURE_OK;
+  if (!k || !v || !row_start || !cache_len) return CURE_ERR_INVALID_ARG;
+  if (rope) a.rope = *rope;
+  a.err = device_error_word();
+  return from_cuda(launch_rope(a, true, static_cast<cudaStream_t>(stream)));
 }
 
 cure_status cure_device_error(void* stream, int32_t* bits) {

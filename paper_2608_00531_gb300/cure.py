@@ -13,7 +13,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import _lib
-from ._lib import KVDesc, TreeParams, check
+from ._lib import KVDesc, Rope, RopeScaling, TreeParams, check
 
 DEVERR_PAGE, DEVERR_SLOT, DEVERR_NODES = _lib.DEVERR_PAGE, _lib.DEVERR_SLOT, _lib.DEVERR_NODES
 
@@ -299,6 +299,179 @@ def cure_resync_kv(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Te
         _p(acc["out_tokens"]), _p(cache_len_in), _p(cache_len_out), _p(out["draft_valid_len"]),
         _p(out["replay_tokens"]), _p(out["n_replay"]), _stream(stream)))
     out["cache_len"] = cache_len_out
+    return out
+
+
+_SCALINGS = {"linear": 1, "base": 2, "bands": 3, "ramp": 4}
+
+
+def rope_desc(rot_dim: int = 128, base: float = 10000.0, *, style: str = "half", scaling: Optional[dict] = None,
+              amplitude: float = 1.0, freqs: Optional[Sequence[float]] = None) -> Rope:
+    """The rotation of a head's first ``rot_dim`` values, a host struct to keep with the model: pairs
+    (i, i + rot_dim / 2) with style "half", (2i, 2i + 1) with "interleaved".
+
+    The frequencies are base^(-2i / rot_dim), scaled by ``scaling``: dict(kind="linear" | "base", factor=) or
+    dict(kind="bands" | "ramp", factor=, low=, high=, original=) (the formulas are in include/cure.h; "ramp" also
+    takes its two numbers of turns as slow= and fast=).  Or they are ``freqs``, rot_dim / 2 values in radians per
+    position.  ``amplitude`` multiplies cosines and sines."""
+    if style not in ("half", "interleaved"):
+        raise ValueError(f"rope_desc: style must be 'half' or 'interleaved', got {style!r}")
+    st, r, lib = int(style == "interleaved"), Rope(), _lib.load()
+    if freqs is not None:
+        if scaling is not None:
+            raise ValueError("rope_desc: freqs are taken as they are; scaling goes with base")
+        f = [float(x) for x in freqs]
+        if len(f) != rot_dim // 2:
+            raise ValueError(f"rope_desc: {rot_dim // 2} frequencies expected, got {len(f)}")
+        check("cure_rope_init_freqs", lib.cure_rope_init_freqs(C.byref(r), st, rot_dim, (C.c_double * max(1, len(f)))(*f),
+                                                               float(amplitude)))
+        return r
+    sc = None
+    if scaling is not None:
+        d = dict(scaling)
+        kind = d.pop("kind", None)
+        if kind not in _SCALINGS:
+            raise ValueError(f"rope_desc: unknown scaling {kind!r}")
+        if kind == "ramp":
+            d = {dict(slow="low", fast="high").get(k, k): v for k, v in d.items()}
+        want = {"factor"} | ({"low", "high", "original"} if kind in ("bands", "ramp") else set())
+        if set(d) != want:
+            raise ValueError(f"rope_desc: scaling {kind!r} takes {sorted(want)}, got {sorted(d)}")
+        sc = C.byref(RopeScaling(kind=_SCALINGS[kind], **{k: float(v) for k, v in d.items()}))
+    check("cure_rope_init", lib.cure_rope_init(C.byref(r), st, rot_dim, float(base), sc, float(amplitude)))
+    return r
+
+
+def _here(t: Optional[torch.Tensor], name: str, dtype=None) -> Optional[int]:
+    """_p() of a tensor that must also be on the current device, and of a type where one is given."""
+    if t is None:
+        return None
+    if dtype is not None:
+        _need(t, dtype, name)
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    return _p(t)
+
+
+def _new(shape, dtype, stream) -> torch.Tensor:
+    """A tensor that the call fills on `stream`: allocated there, so that its memory is not in use on another."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    if stream.device_index != torch.cuda.current_device():
+        raise ValueError("stream must be on the current CUDA device")
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+
+
+def _head_rows(t: Optional[torch.Tensor], name: str):
+    """(address, values from row to row, rows, heads) of bf16 [...][heads][D]: heads end to end, the
+    leading dimensions one even step apart, as in a part of a fused projection's rows."""
+    if t is None:
+        return None, 0, 0, 0
+    _need(t, torch.bfloat16, name)
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+    sh, st = t.shape, t.stride()
+    if len(sh) < 2:
+        raise ValueError(f"{name} must be [...][heads][head_dim]")
+    H, D = sh[-2], sh[-1]
+    ld, rows, outer = H * D, 1, None
+    for n, step in zip(reversed(sh[:-2]), reversed(st[:-2])):
+        if n != 1:
+            if outer is None:
+                ld = step
+            elif step != outer:
+                raise ValueError(f"{name}: rows must lie one even step apart")
+            outer = step * n
+        rows *= n
+    if rows and H and D and ((D > 1 and st[-1] != 1) or (H > 1 and st[-2] != D)):
+        raise ValueError(f"{name}: a row's heads must lie end to end")
+    return t.data_ptr(), ld, rows, H
+
+
+def cure_rope_qkv(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor],
+                  pos: torch.Tensor, rope: Optional[Rope], *, q_norm: Optional[torch.Tensor] = None,
+                  k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, out=None, stream=None):
+    """Per-head norms and the rotation of q and k at the rows' positions, v copied: (q, k, v) as cure_tree_attn
+    takes them, from (parts of) the rows of a fused projection.
+
+    q bf16 [...][heads_q][D], k and v [...][heads_kv][D]; pos int32, one per row (the tree's ``pos``): rows with
+    pos < 0 are left out.  rope = None: no rotation.  Any of q, k, v may be None, and its output with it."""
+    ins = [_head_rows(t, nm) for t, nm in ((q, "q"), (k, "k"), (v, "v"))]
+    if out is None:
+        out = tuple(None if t is None else _new(t.shape, t.dtype, stream) for t in (q, k, v))
+    outs = [_head_rows(t, nm) for t, nm in zip(out, ("q's output", "k's output", "v's output"))]
+    rows = pos.numel()
+    for i, o, t, nm in zip(ins, outs, (q, k, v), "qkv"):
+        if i[2:] != o[2:] or (t is not None and i[2] != rows):
+            raise ValueError(f"cure_rope_qkv: {nm}, its output and pos must have the same rows and heads")
+    if k is not None and v is not None and ins[1][3] != ins[2][3]:
+        raise ValueError("cure_rope_qkv: k and v must have the same heads")
+    D = {t.shape[-1] for t in (q, k, v, *out) if t is not None}
+    if len(D) > 1:
+        raise ValueError("cure_rope_qkv: one head_dim")
+    check("cure_rope_qkv", _lib.load().cure_rope_qkv(
+        ins[0][0], ins[1][0], ins[2][0], ins[0][1], ins[1][1], ins[2][1], rows, ins[0][3], max(ins[1][3], ins[2][3]),
+        D.pop() if D else 128, _here(pos, "pos", torch.int32), None if rope is None else C.byref(rope),
+        _norm(q_norm, "q_norm"), _norm(k_norm, "k_norm"), float(eps), outs[0][0], outs[1][0], outs[2][0],
+        outs[0][1], outs[1][1], outs[2][1], _stream(stream)))
+    return out
+
+
+def _norm(w: Optional[torch.Tensor], name: str) -> Optional[int]:
+    if w is not None and w.numel() != 128:
+        raise ValueError(f"{name} must hold one weight for each of a head's 128 values")
+    return _here(w, name, torch.bfloat16)
+
+
+def _cache_fits(t: torch.Tensor, kv: KVDesc, batch: int, name: str) -> int:
+    """_here() of a cache that holds what its geometry says."""
+    rows = batch * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size
+    if t.numel() < rows * kv.heads_kv * kv.head_dim:
+        raise ValueError(f"{name} is smaller than its geometry")
+    return _here(t, name, torch.bfloat16)
+
+
+def _ragged(row_start: torch.Tensor, cache_len: torch.Tensor, kv: KVDesc) -> int:
+    """Sequences of a packed batch, whose tensors must agree on it."""
+    B = cache_len.numel()
+    if row_start.numel() != B + 1:
+        raise ValueError("row_start must hold one entry more than cache_len")
+    table = getattr(kv, "_keep", None)
+    if table is not None and table.numel() < B * kv.max_len:
+        raise ValueError("block_table has fewer rows than the batch has sequences")
+    return B
+
+
+def cure_append_kv(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv: KVDesc,
+                   row_start: torch.Tensor, cache_len: torch.Tensor, rope: Optional[Rope], *,
+                   q: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                   q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """cure_rope_qkv of packed rows whose K and V go into the cache, sequence b's rows row_start[b] ..
+    row_start[b+1] - 1 to slots cache_len[b], cache_len[b] + 1, ..; returns q's rows (None without q).
+
+    A row's position is its slot, or its entry of ``pos`` (int32; < 0 leaves the row out).  cache_len is not
+    advanced.  In-place tree rows: row_start = 0, n_max, 2 n_max, .., pos = the tree's ``pos``."""
+    B = _ragged(row_start, cache_len, kv)
+    (pq, lq, nq, hq), (pk, lk, nk, hk), (pv, lv, nv, hv) = (
+        _head_rows(t, nm) for t, nm in ((q, "q"), (k, "k"), (v, "v")))
+    if q is None:
+        out = None
+    elif out is None:
+        out = _new(q.shape, q.dtype, stream)
+    po, lo, no, ho = _head_rows(out, "out")
+    if nk != nv or hk != kv.heads_kv or hv != kv.heads_kv or (q is not None and (nq != nk or (no, ho) != (nq, hq))) or (
+            pos is not None and pos.numel() != nk):
+        raise ValueError("cure_append_kv: q, k, v, out and pos must have the same rows, k and v the cache's heads")
+    if any(t is not None and t.shape[-1] != kv.head_dim for t in (q, k, v, out)):
+        raise ValueError("cure_append_kv: heads must have the cache's head_dim")
+    check("cure_append_kv", _lib.load().cure_append_kv(
+        pq, pk, pv, lq, lk, lv, nk, hq, B, _here(row_start, "row_start", torch.int32),
+        _here(cache_len, "cache_len", torch.int32), _here(pos, "pos", torch.int32), C.byref(kv),
+        _cache_fits(k_cache, kv, B, "k_cache"), _cache_fits(v_cache, kv, B, "v_cache"),
+        None if rope is None else C.byref(rope), _norm(q_norm, "q_norm"), _norm(k_norm, "k_norm"), float(eps), po, lo,
+        _stream(stream)))
     return out
 
 
