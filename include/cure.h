@@ -424,6 +424,38 @@ cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t 
                            void* v_cache, const cure_rope* rope, const void* q_norm, const void* k_norm, float eps,
                            void* q_out, int64_t ld_q_out, void* stream);
 
+/*
+ * Causal attention of packed rows over the cache, one layer (Alg. 1's input: the
+ * target reads a prompt, a further chunk of one, or a single token, before the
+ * next step).  Sequence b has the rows row_start[b] .. row_start[b+1] - 1
+ * (device int32 [batch + 1], ascending; equal: none), which stand at positions
+ * cache_len[b], cache_len[b] + 1, .. and whose K and V are in the cache at these
+ * slots already (cure_append_kv).  For its i-th row r, head h (kv head
+ * h / (heads_q / heads_kv)):
+ *   out[r][h] = softmax(scale * q k^T) v over the cached keys 0 .. cache_len[b] + i
+ * q, out: bf16 [rows][heads_q][D], out not overlapping any input; k_cache,
+ * v_cache: one layer in the layout of `kv` (a HOST pointer).  Accumulation is
+ * float32; the probabilities are rounded to bf16 before the PV product.  What
+ * lies in the cache behind a sequence's last key does not matter; the V rows of
+ * the sequence's own keys must be finite (a key that a row does not see weighs 0
+ * in the product, not nothing).  Rows outside row_start[0] .. row_start[batch] - 1
+ * are left unwritten, and so are the rows of a sequence that does not fit its
+ * capacity (CURE_DEVERR_SLOT) or whose row_start does not ascend within
+ * 0 .. rows (CURE_DEVERR_NODES).  A missing or bad page counts as zeros
+ * (CURE_DEVERR_PAGE).  batch <= 256, D = 128, heads_q / heads_kv <= 128, scale > 0
+ * and finite; all base pointers 16-byte aligned.
+ * workspace: device scratch of at least cure_prompt_attn_workspace_size() bytes,
+ * 256-byte aligned; its contents on entry do not matter.  Calls that can overlap
+ * on the GPU must not share a workspace.
+ */
+cure_status cure_prompt_attn(const void* q, const void* k_cache, const void* v_cache, const cure_kv_desc* kv,
+                             const int32_t* row_start, const int32_t* cache_len, int32_t rows, int32_t batch,
+                             int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/* Bytes of workspace cure_prompt_attn needs for this shape on the current device (0 on a bad argument). */
+size_t cure_prompt_attn_workspace_size(int32_t rows, int32_t batch, int32_t heads_q, const cure_kv_desc* kv);
+
 /* Reads and clears the device error word of the current device after
  * synchronising `stream`.  *bits receives the CURE_DEVERR_* bits (may be NULL).
  * Returns CURE_ERR_DEVICE_FAULT when any bit was set, CURE_OK otherwise. */

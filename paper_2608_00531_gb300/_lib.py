@@ -22,7 +22,7 @@ EXPORTS = ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_tree_a
            "cure_accept", "cure_lm_head_argmax", "cure_lm_head_workspace_size", "cure_selftest_wait_timeout",
            "cure_selftest_lm_head_timeout", "cure_selftest_attn_route",
            "cure_sample_target", "cure_resync_kv", "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv",
-           "cure_append_kv", "cure_device_error",
+           "cure_append_kv", "cure_prompt_attn", "cure_prompt_attn_workspace_size", "cure_device_error",
            "cure_status_string", "cure_abi_version")
 
 
@@ -98,13 +98,16 @@ def load() -> C.CDLL:
                                   P, P, P, I64, I64, I64, P]
     lib.cure_append_kv.argtypes = [P, P, P, I64, I64, I64, I32, I32, I32, P, P, P, C.POINTER(KVDesc), P, P,
                                    C.POINTER(Rope), P, P, C.c_float, P, I64, P]
+    lib.cure_prompt_attn.argtypes = [P, P, P, C.POINTER(KVDesc), P, P, I32, I32, I32, C.c_float, P, P, C.c_size_t, P]
+    lib.cure_prompt_attn_workspace_size.argtypes = [I32, I32, I32, C.POINTER(KVDesc)]
+    lib.cure_prompt_attn_workspace_size.restype = C.c_size_t
     lib.cure_device_error.argtypes = [P, C.POINTER(I32)]
     lib.cure_status_string.argtypes = [C.c_int]
     lib.cure_status_string.restype = C.c_char_p
     lib.cure_abi_version.restype = I32
     for name in ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_accept",
                  "cure_resync_kv", "cure_device_error", "cure_sample_target", "cure_lm_head_argmax",
-                 "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv", "cure_append_kv"):
+                 "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv", "cure_append_kv", "cure_prompt_attn"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib

@@ -527,6 +527,41 @@ cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t 
   return from_cuda(launch_rope(a, true, static_cast<cudaStream_t>(stream)));
 }
 
+// The units of a call: row groups of two M tiles' rows, for each kv head.
+static cure_status prompt_shape_ok(int32_t rows, int32_t batch, int32_t heads_q, const cure_kv_desc* kv) {
+  cure_status why;
+  if (!kv_ok(kv, &why)) return why;
+  if (rows < 0 || batch < 0 || heads_q < 1 || heads_q % kv->heads_kv != 0) return CURE_ERR_INVALID_ARG;
+  const int G = heads_q / kv->heads_kv;
+  if (batch > kAttnBatchLimit || G > 128) return CURE_ERR_UNSUPPORTED;
+  const int64_t units = ((int64_t)rows / (2 * (128 / G)) + batch) * kv->heads_kv;
+  return units <= INT32_MAX / 2 ? CURE_OK : CURE_ERR_UNSUPPORTED;
+}
+
+size_t cure_prompt_attn_workspace_size(int32_t rows, int32_t batch, int32_t heads_q, const cure_kv_desc* kv) {
+  return prompt_shape_ok(rows, batch, heads_q, kv) == CURE_OK ? prompt_attn_workspace() : 0;
+}
+
+cure_status cure_prompt_attn(const void* q, const void* k_cache, const void* v_cache, const cure_kv_desc* kv,
+                             const int32_t* row_start, const int32_t* cache_len, int32_t rows, int32_t batch,
+                             int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  ApiRange range("cure_prompt_attn");
+  const cure_status st = prompt_shape_ok(rows, batch, heads_q, kv);
+  if (st != CURE_OK) return st;
+  if (!(scale > 0.f && scale <= FLT_MAX)) return CURE_ERR_INVALID_ARG;
+  if (rows == 0 || batch == 0) return CURE_OK;
+  if (!q || !k_cache || !v_cache || !row_start || !cache_len || !out || !workspace) return CURE_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) ||
+      !aligned(workspace, 256))
+    return CURE_ERR_INVALID_ARG;
+  if (workspace_bytes < prompt_attn_workspace()) return CURE_ERR_CAPACITY;
+  return from_cuda(launch_prompt_attn(static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_cache),
+                                      static_cast<const uint16_t*>(v_cache), *kv, row_start, cache_len, rows, batch,
+                                      heads_q, scale, static_cast<uint16_t*>(out), workspace, device_error_word(),
+                                      static_cast<cudaStream_t>(stream)));
+}
+
 cure_status cure_device_error(void* stream, int32_t* bits) {
   if (cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) != cudaSuccess) return CURE_ERR_CUDA;
   int v = 0;

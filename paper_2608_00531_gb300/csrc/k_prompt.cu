@@ -1,0 +1,491 @@
+// Causal grouped-head attention of packed prompt rows over the cache (the input
+// of Alg. 1: the target reads the prompt before the first step), on tcgen05
+// tensor cores.
+//
+//   out_i = sum_{j <= L + i} softmax_j(scale q_i k_j) v_j     (row i of a sequence
+//                                                             with L tokens before)
+//
+// Work.  A unit is (sequence, row group, kv head): 2 * npb rows' heads of one kv
+// head, packed (row, group head) into two M tiles of 128 (npb = 128 / G rows
+// each), against its keys 0 .. L + last row in 128-key tiles.  Two M tiles share
+// each K and V tile from shared memory, and one runs its softmax while the
+// other's products run.
+//
+// Roles (12 warps):
+//   warps 0-3 / 4-7   softmax of M tile 0 / 1, a thread a row: reads S from TMEM,
+//                     writes P (bf16) over it, keeps the row's running maximum
+//                     and sum, rescales O (only where the maximum has grown by
+//                     more than 2^8), writes the output
+//   warp 8            TMA producer: Q, and K and V tiles in turn through a ring
+//                     of 5 stages of 32 KiB
+//   warps 9 / 10      issue M tile 0 / 1's products: S = Q K^T (M128 N128 K128),
+//                     then, once P is published, O += P V (A from TMEM)
+// TMEM (512 columns): S[2] (128 each, P in the first 64 of them) | O[2] (128 each).
+// S of the next tile takes the place of P once the PV product that reads P is
+// done, so that every TMEM hand-over is by a barrier that was waited for.
+#include <algorithm>
+#include <atomic>
+
+#include "attn_tc.cuh"
+
+namespace cure {
+namespace {
+
+using namespace tc;
+
+constexpr int BM = kAttnRowsCta;  // 128 rows per M tile
+constexpr int BN = 128;           // keys per tile
+constexpr int D = kAttnD;
+constexpr int NS = 5;             // ring stages, a K or a V tile each
+constexpr int kThreads = 384;
+constexpr uint32_t kTmemCols = 512;
+
+constexpr int kQHalf = kAttnQHalf;      // 16 KiB: [128 rows][64 d]
+constexpr int kKHalf = BN * 64 * 2;     // 16 KiB: [128 keys][64 d]
+constexpr int kTile = 2 * kKHalf;       // 32 KiB
+constexpr int kVChunk = kAttnVChunk;    // 4 KiB: V keys 16c..16c+15, both d halves
+constexpr int kVHalf = kVChunk / 2;
+// from a paged cache: [8-key group][d half][8 keys][64 d], as in the tree attention
+constexpr int kPgGroup = 8 * D * 2;
+constexpr int kPgHalf = kPgGroup / 2;
+constexpr int kOffQ = 0;                       // Q[m][half]
+constexpr int kOffRing = kOffQ + 4 * kQHalf;   // K/V[stage]
+constexpr int kOffMisc = kOffRing + NS * kTile;
+enum {
+  B_QFULL = 0, B_QEMPTY = 1, B_FULL = 2, B_EMPTY = B_FULL + NS, B_SFULL = B_EMPTY + NS, B_PFULL = B_SFULL + 2,
+  B_PVDONE = B_PFULL + 2, B_DRAIN = B_PVDONE + 2, kNumBars = B_DRAIN + 2
+};
+constexpr int kOffTmemSlot = kOffMisc + 8 * kNumBars;
+constexpr int kOffAbort = kOffTmemSlot + 4;
+constexpr int kOffPrefix = (kOffAbort + 4 + 15) / 16 * 16;  // int units_start[B+1]
+constexpr int kSmemBytes = kOffPrefix + 4 * (kAttnMaxBatch + 1);
+static_assert(kSmemBytes <= 232448, "fits the 227 KiB opt-in");
+
+constexpr uint32_t kColS = 0;    // S[m]: columns m*128; P[m] in the first 64 of them
+constexpr uint32_t kColO = 256;  // O[m]: columns 256 + m*128
+
+struct PromptArgs {
+  cure_kv_desc kv;
+  const int32_t* row_start;
+  const int32_t* cache_len;
+  int rows, batch, heads_q, G, cap;
+  float scale_log2;
+  uint16_t* out;
+  int* err;
+};
+
+// A sequence's rows and the tokens before them; n = 0 where they do not make sense.
+struct Seq {
+  int r0, n, L;
+};
+__device__ __forceinline__ Seq sequence(const PromptArgs& A, int b, int* bad) {
+  Seq s;
+  s.r0 = A.row_start[b];
+  s.L = A.cache_len[b];
+  const int64_t n = (int64_t)A.row_start[b + 1] - s.r0;
+  s.n = (int)n;
+  *bad = 0;
+  if (s.r0 < 0 || n < 0 || s.r0 + n > A.rows) *bad = CURE_DEVERR_NODES;
+  else if (n > 0 && (s.L < 0 || s.L + n > A.cap)) *bad = CURE_DEVERR_SLOT;
+  if (*bad) s.n = 0;
+  return s;
+}
+
+struct Unit {
+  int b, h, rg;   // sequence, kv head, row group
+  int r0, n, L;   // its rows and the tokens before them
+  int keys, T;    // keys that any of the unit's rows sees, and their tiles
+};
+
+__device__ __forceinline__ Unit unit_at(const PromptArgs& A, const int* units_start, int npb, int u) {
+  int lo = 0, hi = A.batch;  // largest b with units_start[b] <= u
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (units_start[mid] <= u) lo = mid;
+    else hi = mid;
+  }
+  int bad;
+  const Seq s = sequence(A, lo, &bad);
+  Unit x;
+  x.b = lo;
+  x.r0 = s.r0;
+  x.n = s.n;
+  x.L = s.L;
+  const int k = u - units_start[lo];
+  x.rg = k / A.kv.heads_kv;
+  x.h = k % A.kv.heads_kv;
+  x.keys = s.L + min((x.rg + 1) * 2 * npb, s.n);
+  x.T = (x.keys + BN - 1) / BN;
+  return x;
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                   const __grid_constant__ CUtensorMap tm_q, const PromptArgs A) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t sb = smem_u32(smem);
+  if (sb & 1023u) {  // the swizzled tiles need a 1 KiB-aligned base
+    if (tid == 0) flag(A.err, CURE_DEVERR_ALIGN);
+    return;
+  }
+  const int G = A.G, npb = BM / G;
+  const Bar bar{sb + kOffMisc};
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
+  int* units_start = reinterpret_cast<int*>(smem + kOffPrefix);
+
+  // ---------------------------------------------------------------- set-up
+  if (tid == 0) {
+    mbar_init(bar(B_QFULL), 1);
+    mbar_init(bar(B_QEMPTY), 2);
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(bar(B_FULL + i), 1);
+      mbar_init(bar(B_EMPTY + i), 2);
+    }
+    for (int m = 0; m < 2; ++m) {
+      mbar_init(bar(B_SFULL + m), 1);
+      mbar_init(bar(B_PFULL + m), BM);
+      mbar_init(bar(B_PVDONE + m), 1);
+      mbar_init(bar(B_DRAIN + m), 1);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0) tmem_alloc(sb + kOffTmemSlot, kTmemCols);
+  if (warp == 8 && lane == 0) {
+    tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  // Q rows at or past npb * G are never written by the Q copies: zero them once
+  const int pad_rows = BM - npb * G;
+  for (int c = tid; c < 4 * pad_rows * 8; c += kThreads) {
+    const int q16 = c & 7, rr = npb * G + ((c >> 3) % pad_rows), mh = (c >> 3) / pad_rows;
+    st_shared_v4(sb + kOffQ + mh * kQHalf + rr * 128 + q16 * 16, 0u, 0u, 0u, 0u);
+  }
+  pdl_begin();
+  if (warp == 9) {  // units of each sequence and their prefix sums
+    int run = 0;
+    for (int base = 0; base < A.batch; base += 32) {
+      const int b = base + lane;
+      int ub = 0;
+      if (b < A.batch) {
+        int bad;
+        const Seq s = sequence(A, b, &bad);
+        if (bad && blockIdx.x == 0) flag(A.err, bad);
+        ub = (s.n + 2 * npb - 1) / (2 * npb) * A.kv.heads_kv;
+      }
+      int iu = ub;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, iu, off);
+        if (lane >= off) iu += y;
+      }
+      if (b < A.batch) units_start[b] = run + iu - ub;
+      run += __shfl_sync(0xffffffffu, iu, 31);
+    }
+    if (lane == 0) units_start[A.batch] = run;
+  }
+  fence_proxy_async_smem();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmemSlot);
+  const int units = units_start[A.batch];
+  // M tile 1 of a unit is active when its first row is one of the sequence's
+  auto active1 = [&](const Unit& x) { return (2 * x.rg + 1) * npb < x.n; };
+
+  if (warp == 8) {
+    // ================================================================ producer
+    const int ps = A.kv.page_size;
+    const int ppt = A.kv.layout == 1 ? BN / ps : 0;  // pages (boxes) of a tile: 2 .. 16
+    const uint32_t qbytes = (uint32_t)(npb * G * 128);
+    uint32_t qc = 0, issued = 0;  // units, ring tiles
+    bool ok = true;
+    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Unit x = unit_at(A, units_start, npb, u);
+      auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
+        const int tok = t * BN + lane * ps;
+        if (lane >= ppt || tok >= x.keys) return -1;
+        const int page = A.kv.block_table[(int64_t)x.b * A.kv.max_len + tok / ps];
+        if (page < 0 || page >= A.kv.num_pages) {
+          flag(A.err, CURE_DEVERR_PAGE);
+          return -1;
+        }
+        return page;
+      };
+      int page = ppt > 0 ? page_of(0) : -1;
+      for (int t = 0; ok && t < x.T; ++t) {
+        const int next = ppt > 0 && t + 1 < x.T ? page_of(t + 1) : -1;
+        for (int kv = 0; kv < 2; ++kv) {  // the K tile, then the V tile
+          const int st = (int)(issued % NS);
+          if (!wait_warp(bar(B_EMPTY + st), ((issued / NS) & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
+          const uint32_t full = bar(B_FULL + st), dst = sb + kOffRing + st * kTile;
+          if (lane == 0) mbar_arrive_expect_tx(full, kTile);
+          __syncwarp();
+          if (A.kv.layout == 1) {
+            if (lane < ppt) tma_load_5d(dst + lane * ps * 256, kv ? &tm_v : &tm_k, full, 0, 0, 2 * x.h, 0, page);
+          } else if (kv == 0) {
+            if (lane < 2) tma_load_3d(dst + lane * kKHalf, &tm_k, full, lane * 64, x.h, x.b * A.kv.max_len + t * BN);
+          } else if (lane < BN / 16) {
+            tma_load_4d(dst + lane * kVChunk, &tm_v, full, 0, x.b * A.kv.max_len + t * BN + 16 * lane, 0, x.h);
+          }
+          __syncwarp();
+          ++issued;
+          if (t == 0 && kv == 0) {  // Q of both M tiles once the previous unit's S products are done
+            if (!wait_warp(bar(B_QEMPTY), (qc & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
+            ++qc;
+            if (lane == 0) mbar_arrive_expect_tx(bar(B_QFULL), 4 * qbytes);
+            __syncwarp();
+            if (lane < 4)  // M tile lane / 2, d half lane % 2
+              tma_load_4d(sb + kOffQ + lane * kQHalf, &tm_q, bar(B_QFULL), (lane & 1) * 64, 0, x.h,
+                          x.r0 + (2 * x.rg + (lane >> 1)) * npb);
+            __syncwarp();
+          }
+        }
+        page = next;
+      }
+    }
+    if (*abort_flag) {  // let copies in flight land before the CTA's smem goes away
+      for (uint32_t i = (issued > NS ? issued - NS : 0); i < issued; ++i)
+        wait_bounded(bar(B_FULL + i % NS), (i / NS) & 1u, abort_flag, A.err, false);
+      if (qc > 0) wait_bounded(bar(B_QFULL), (qc - 1) & 1u, abort_flag, A.err, false);
+    }
+  } else if (warp == 9 || warp == 10) {
+    // ================================================================ products of M tile m
+    const int m = warp - 9;
+    constexpr uint32_t idS = idesc_bf16_f32(BM, BN, false), idO = idesc_bf16_f32(BM, D, true);
+    const bool paged = A.kv.layout == 1;
+    uint32_t qc = 0, r = 0, c = 0;  // units, ring tiles, tiles of this M tile
+    bool ok = true;
+    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Unit x = unit_at(A, units_start, npb, u);
+      const bool act = m == 0 || active1(x);
+      if (!wait_warp(bar(B_QFULL), qc & 1u, abort_flag, A.err)) break;
+      ++qc;
+      const uint64_t qd = sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024);
+      for (int t = 0; ok && t < x.T; ++t, r += 2) {
+        const uint32_t sk = r % NS, sv = (r + 1) % NS;
+        if (!wait_warp(bar(B_FULL + sk), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+        if (!act) {  // no rows in this M tile: the ring's tiles are passed on
+          if (lane == 0) mbar_arrive(bar(B_EMPTY + sk));
+          __syncwarp();
+          if (!wait_warp(bar(B_FULL + sv), ((r + 1) / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+          if (lane == 0) mbar_arrive(bar(B_EMPTY + sv));
+          __syncwarp();
+          continue;
+        }
+        // S takes P's place: the PV product of the tile before must be done
+        if (c > 0 && !wait_warp(bar(B_PVDONE + m), (c - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t ka = sb + kOffRing + sk * kTile;
+        const uint32_t sbo = paged ? kPgGroup : 1024u, kh = paged ? kPgHalf : kKHalf;
+        mma_s_group(tmem + kColS + m * BN, qd, sdesc_sw128(ka, 16, sbo), sdesc_sw128(ka + kh, 16, sbo), idS);
+        commit_elect(bar(B_SFULL + m));
+        commit_elect(bar(B_EMPTY + sk));
+        if (t == x.T - 1) commit_elect(bar(B_QEMPTY));  // the unit's last use of Q
+        if (!wait_warp(bar(B_FULL + sv), ((r + 1) / NS) & 1u, abort_flag, A.err) ||
+            !wait_warp(bar(B_PFULL + m), c & 1u, abort_flag, A.err)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
+        const uint64_t vd = sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
+        mma_pv_group(tmem + kColO + m * D, tmem + kColS + m * BN, vd, idO, t > 0 ? 1u : 0u);
+        mma_pv_group(tmem + kColO + m * D, tmem + kColS + m * BN + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
+        commit_elect(bar(B_PVDONE + m));
+        commit_elect(bar(B_EMPTY + sv));
+        ++c;
+      }
+      if (!act && ok) {
+        if (lane == 0) mbar_arrive(bar(B_QEMPTY));
+        __syncwarp();
+      }
+    }
+    __syncwarp();
+    commit_elect(bar(B_DRAIN + m));
+    wait_bounded(bar(B_DRAIN + m), 0, abort_flag, A.err, false);
+  } else if (warp < 8) {
+    // ================================================================ softmax
+    const int m = warp >> 2;
+    const int row = tid & 127;  // row within the M tile = TMEM lane
+    const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t tS = tl + kColS + m * BN, tO = tl + kColO + m * D;
+    const float c = A.scale_log2;
+    uint32_t sc = 0, r = 0;  // tiles of this M tile, ring tiles
+    bool ok = true;
+    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Unit x = unit_at(A, units_start, npb, u);
+      const uint32_t r_unit = r;
+      r += 2 * (uint32_t)x.T;
+      if (m == 1 && !active1(x)) continue;
+      const int i = (2 * x.rg + m) * npb + row / G;  // the row's place in its sequence
+      const int sees = x.L + i + 1;                  // keys that it sees
+      const int all_see = x.L + (2 * x.rg + m) * npb + 1;  // that every row of the M tile sees
+      float m_run = -INFINITY, l_run = 0.f;
+      for (int t = 0; t < x.T; ++t) {
+        if (!wait_warp(bar(B_SFULL + m), sc & 1u, abort_flag, A.err)) { ok = false; break; }
+        ++sc;
+        tc_fence_after();
+        uint32_t v[4][32];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(tS + 32 * q, v[q]);
+        tmem_wait_ld();
+        float x_[BN];
+#pragma unroll
+        for (int k = 0; k < BN; ++k) x_[k] = __uint_as_float(v[k >> 5][k & 31]);
+        if ((t + 1) * BN > all_see) {
+          const int lim = sees - t * BN;
+#pragma unroll
+          for (int k = 0; k < BN; ++k) x_[k] = k < lim ? x_[k] : -INFINITY;
+        }
+        float mx[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) mx[k] = fmaxf(x_[k], x_[8 + k]);
+#pragma unroll
+        for (int j = 16; j < BN; j += 16)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) mx[k] = fmax3(mx[k], x_[j + k], x_[j + 8 + k]);
+        const float mt = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * c;
+        const float m_new = fmaxf(m_run, mt);
+        const bool need = m_new > m_run + 8.0f;
+        const float alpha = need ? ex2(m_run - m_new) : 1.f;
+        if (need) m_run = m_new;
+        const float nbase = m_run == -INFINITY ? 0.f : -m_run;
+        const uint64_t c2 = f2_pack(c, c), nb2 = f2_pack(nbase, nbase);
+        uint64_t sm2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float a0, a1;
+            f2_unpack(f2_fma(f2_pack(x_[32 * q + 2 * k], x_[32 * q + 2 * k + 1]), c2, nb2), a0, a1);
+            const float p0 = ex2(a0), p1 = ex2(a1);
+            sm2[k & 1] = f2_add(sm2[k & 1], f2_pack(p0, p1));
+            pk[k] = pack_bf16(p0, p1);
+          }
+          tmem_st16(tS + 16 * q, pk);
+        }
+        float s4[4];
+        f2_unpack(sm2[0], s4[0], s4[1]);
+        f2_unpack(sm2[1], s4[2], s4[3]);
+        l_run = l_run * alpha + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
+        // O: the PV product of the tile before was done before this S was issued
+        if (t > 0 && __any_sync(0xffffffffu, need)) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint32_t o[32];
+            tmem_ld32(tO + q * 32, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+            tmem_st32(tO + q * 32, o);
+          }
+        }
+        // V rows past the unit's last key are zeroed (by both M tiles) so that what lies
+        // there cannot reach O through 0 * NaN
+        const int valid = x.keys - t * BN;
+        if (valid < BN) {
+          const uint32_t rv = r_unit + 2 * (uint32_t)t + 1;
+          if (!wait_warp(bar(B_FULL + rv % NS), (rv / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+          const uint32_t vb = sb + kOffRing + (rv % NS) * kTile;
+          const bool paged = A.kv.layout == 1;
+          for (int q = row; q < (BN - valid) * 16; q += BM) {
+            const int rr = valid + (q >> 4), hf = (q >> 3) & 1, cc = q & 7;
+            const uint32_t off = paged ? (rr >> 3) * kPgGroup + hf * kPgHalf + (rr & 7) * 128
+                                       : (rr >> 4) * kVChunk + hf * kVHalf + (rr & 15) * 128;
+            st_shared_v4(vb + off + cc * 16, 0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_smem();
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar(B_PFULL + m));
+      }
+      if (!ok || !wait_warp(bar(B_PVDONE + m), (sc - 1) & 1u, abort_flag, A.err)) break;
+      tc_fence_after();
+      // ---- the output rows
+      const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+      uint16_t* orow = A.out + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D;
+      const bool vrow = row < npb * G && i < x.n;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t o[32];
+        tmem_ld32(tO + q * 32, o);
+        tmem_wait_ld();
+        if (vrow) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 8) {
+            uint4 v;
+            v.x = pack_bf16(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
+            v.y = pack_bf16(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
+            v.z = pack_bf16(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
+            v.w = pack_bf16(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
+            *reinterpret_cast<uint4*>(orow + q * 32 + k) = v;
+          }
+        }
+      }
+      tc_fence_before();
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+}  // namespace
+
+size_t prompt_attn_workspace() { return 256; }  // none is needed
+
+cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
+                               const cure_kv_desc& kv, const int32_t* row_start, const int32_t* cache_len, int rows,
+                               int batch, int heads_q, float scale, uint16_t* out, void* workspace, int* err,
+                               cudaStream_t s) {
+  (void)workspace;
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(done.load() & bit)) {
+    e = cudaFuncSetAttribute(prompt_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e != cudaSuccess) return e;
+    done.fetch_or(bit);
+  }
+  const int Hkv = kv.heads_kv, G = heads_q / Hkv;
+  CUtensorMap mk, mv, mq;
+  bool ok;
+  if (kv.layout == 0) {
+    const uint64_t n = (uint64_t)batch * kv.max_len;
+    ok = make_kv_map(&mk, k_cache, n, Hkv, BN) && make_v_rows_map(&mv, v_cache, n, Hkv);
+  } else {
+    ok = make_page_map(&mk, k_cache, (uint64_t)kv.num_pages, kv.page_size, Hkv) &&
+         make_page_map(&mv, v_cache, (uint64_t)kv.num_pages, kv.page_size, Hkv);
+  }
+  ok = ok && make_q_map(&mq, q, (uint64_t)rows, Hkv, G, BM / G);
+  if (!ok) return cudaErrorInvalidValue;
+  PromptArgs A;
+  A.kv = kv;
+  A.row_start = row_start;
+  A.cache_len = cache_len;
+  A.rows = rows;
+  A.batch = batch;
+  A.heads_q = heads_q;
+  A.G = G;
+  A.cap = std::min(kv.layout == 0 ? kv.max_len : kv.max_len * kv.page_size, INT32_MAX - 2 * BN);
+  A.scale_log2 = scale * 1.4426950408889634f;
+  A.out = out;
+  A.err = err;
+  const int npb = BM / G;
+  const int64_t units = ((int64_t)rows / (2 * npb) + batch) * Hkv;  // at most
+  const int grid = (int)std::min<int64_t>(units, num_sms());
+  return launch_pdl(prompt_attn_kernel, dim3(grid), dim3(kThreads), kSmemBytes, s, mk, mv, mq, A);
+}
+
+}  // namespace cure

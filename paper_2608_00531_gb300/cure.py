@@ -475,6 +475,37 @@ def cure_append_kv(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
     return out
 
 
+def cure_prompt_attn_workspace_size(rows: int, batch: int, heads_q: int, kv: KVDesc) -> int:
+    return int(_lib.load().cure_prompt_attn_workspace_size(rows, batch, heads_q, C.byref(kv)))
+
+
+def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv: KVDesc,
+                     row_start: torch.Tensor, cache_len: torch.Tensor, scale: float, *,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """Causal attention of packed rows over the cache for one layer: whole prompts, further chunks, single tokens.
+
+    q bf16 [rows][heads_q][D]; sequence b's rows row_start[b] .. row_start[b+1] - 1 stand at positions cache_len[b],
+    cache_len[b] + 1, .., and their K and V are in the cache already (cure_append_kv at the same lengths)."""
+    _need(q, torch.bfloat16, "q")
+    B = _ragged(row_start, cache_len, kv)
+    if q.dim() != 3 or q.shape[2] != kv.head_dim:
+        raise ValueError("q must be [rows][heads_q][head_dim]")
+    rows, Hq, _ = q.shape
+    if out is None:
+        out = _new(q.shape, q.dtype, stream)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    if workspace is None:
+        workspace = _new((max(cure_prompt_attn_workspace_size(rows, B, Hq, kv), 256),), torch.uint8, stream)
+    check("cure_prompt_attn", _lib.load().cure_prompt_attn(
+        _here(q, "q"), _cache_fits(k_cache, kv, B, "k_cache"), _cache_fits(v_cache, kv, B, "v_cache"), C.byref(kv),
+        _here(row_start, "row_start", torch.int32), _here(cache_len, "cache_len", torch.int32), rows, B, Hq,
+        float(scale), _here(out, "out", torch.bfloat16), _here(workspace, "workspace"),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
 def cure_device_error(stream=None) -> int:
     """Synchronise and return (and clear) the device error word's bits."""
     bits = C.c_int32(0)

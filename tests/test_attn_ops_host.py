@@ -1,5 +1,5 @@
-"""The rotation's host side, without a GPU: the table of frequencies against decimal arithmetic, and the
-arguments that the entry points refuse before anything is launched."""
+"""The attention operators' host side, without a GPU: the rotation's table of frequencies against decimal arithmetic,
+and the arguments that the entry points refuse before anything is launched."""
 import ctypes as C
 import decimal
 import math
@@ -121,3 +121,27 @@ def test_refusals(lib):
     bad_kv = KVDesc(layout=1, heads_kv=2, head_dim=128, page_size=12, max_len=4, num_pages=4, block_table=1 << 20)
     assert append(kv=C.byref(bad_kv)) == 5
     assert append(rows=0, k=nul, v=nul) == 0 and append(batch=0, rs=nul, cl=nul) == 0
+
+
+def test_prompt_attn_refusals(lib):
+    from paper_2608_00531_gb300._lib import KVDesc
+    dev, nul, odd = C.c_void_p(1 << 20), None, C.c_void_p((1 << 20) + 8)
+    kv = KVDesc(layout=0, heads_kv=2, head_dim=128, page_size=16, max_len=100, num_pages=0, block_table=None)
+    need = lib.cure_prompt_attn_workspace_size(4, 1, 8, C.byref(kv))
+    assert need > 0 and need % 256 == 0
+    ok = dict(q=dev, kc=dev, vc=dev, kv=C.byref(kv), rs=dev, cl=dev, rows=4, batch=1, hq=8, scale=0.1, out=dev, ws=dev,
+              bytes=need)
+
+    def attn(**kw):
+        return lib.cure_prompt_attn(*dict(ok, **kw).values(), None)
+    for kw in (dict(rows=-1), dict(batch=-1), dict(hq=0), dict(hq=7), dict(scale=0.0), dict(scale=-1.0),
+               dict(scale=float("nan")), dict(scale=float("inf")), dict(q=nul), dict(kc=nul), dict(vc=nul), dict(rs=nul),
+               dict(cl=nul), dict(out=nul), dict(ws=nul), dict(q=odd), dict(kc=odd), dict(vc=odd), dict(out=odd),
+               dict(ws=C.c_void_p((1 << 20) + 128)), dict(kv=None)):
+        assert attn(**kw) == 1, kw
+    assert attn(batch=257) == 5 and attn(hq=258) == 5 and attn(bytes=need - 1) == 2
+    assert attn(rows=0, q=nul) == 0 and attn(batch=0, rs=nul) == 0
+    kv64 = KVDesc(layout=0, heads_kv=2, head_dim=64, page_size=16, max_len=100, num_pages=0, block_table=None)
+    assert attn(kv=C.byref(kv64)) == 5 and lib.cure_prompt_attn_workspace_size(4, 1, 8, C.byref(kv64)) == 0
+    many = KVDesc(layout=0, heads_kv=4096, head_dim=128, page_size=16, max_len=100, num_pages=0, block_table=None)
+    assert attn(kv=C.byref(many), rows=2 ** 31 - 1, hq=4096 * 128) == 5
