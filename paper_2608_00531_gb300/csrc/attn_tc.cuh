@@ -4,6 +4,7 @@
 
 #include <cuda_bf16.h>
 #include <cudaTypedefs.h>
+#include <float.h>
 
 #include <atomic>
 
@@ -118,6 +119,15 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
   return d;
 }
 
+// The base-2 log-sum-exp of a row of a piece.  A row that saw no key gets the lowest
+// finite value: its O is 0, so a merge over pieces that all saw none gives 0
+// (-inf would give NaN there).  A NaN stays one.
+__device__ __forceinline__ float row_lse(float m, float l) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(m + log2f(l)), "f"(-FLT_MAX));
+  return d;
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
@@ -128,6 +138,28 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c),
                "r"(d)
                : "memory");
+}
+
+// A unit's piece counter holds (launch tag << 9) | pieces arrived.  A word
+// whose tag is not this launch's (left by an aborted launch, or never
+// written) counts as zero, so the workspace needs no reset; a completed unit
+// leaves zero behind, so an old word can only match a later tag if its launch
+// was aborted exactly 2^23 - 1 launches earlier.
+constexpr int kCountBits = 9;
+constexpr int kCountMask = (1 << kCountBits) - 1;
+__device__ __forceinline__ int count_of(int v, uint32_t tag) {
+  return ((uint32_t)v >> kCountBits) == tag ? (v & kCountMask) : 0;
+}
+// This piece's arrival (after its release fence): the pieces arrived so far,
+// this one included.
+__device__ __forceinline__ int arrive(int* cnt, uint32_t tag) {
+  int old = *reinterpret_cast<volatile int*>(cnt);
+  while (true) {
+    const int nw = (int)((tag << kCountBits) | (uint32_t)(count_of(old, tag) + 1));
+    const int prev = atomicCAS(cnt, old, nw);
+    if (prev == old) return nw & kCountMask;
+    old = prev;
+  }
 }
 
 __device__ __forceinline__ int ld_acquire(const int* p) {

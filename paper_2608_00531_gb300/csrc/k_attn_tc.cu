@@ -101,37 +101,6 @@ constexpr uint32_t kColS = 0;    // S[m]:      columns m*64
 constexpr uint32_t kColP = 128;  // P[m][buf]: columns 128 + m*64 + buf*32
 constexpr uint32_t kColO = 256;  // O[m]:      columns 256 + m*128
 
-// The base-2 log-sum-exp of a row of a piece.  A row that saw no key gets the lowest
-// finite value: its O is 0, so a merge over pieces that all saw none gives 0
-// (-inf would give NaN there).  A NaN stays one.
-__device__ __forceinline__ float row_lse(float m, float l) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(m + log2f(l)), "f"(-FLT_MAX));
-  return d;
-}
-
-// A unit's piece counter holds (launch tag << 9) | pieces arrived.  A word
-// whose tag is not this launch's (left by an aborted launch, or never
-// written) counts as zero, so the workspace needs no reset; a completed unit
-// leaves zero behind, so an old word can only match a later tag if its launch
-// was aborted exactly 2^23 - 1 launches earlier.
-constexpr int kCountBits = 9;
-constexpr int kCountMask = (1 << kCountBits) - 1;
-__device__ __forceinline__ int count_of(int v, uint32_t tag) {
-  return ((uint32_t)v >> kCountBits) == tag ? (v & kCountMask) : 0;
-}
-// This piece's arrival (after its release fence): the pieces arrived so far,
-// this one included.
-__device__ __forceinline__ int arrive(int* cnt, uint32_t tag) {
-  int old = *reinterpret_cast<volatile int*>(cnt);
-  while (true) {
-    const int nw = (int)((tag << kCountBits) | (uint32_t)(count_of(old, tag) + 1));
-    const int prev = atomicCAS(cnt, old, nw);
-    if (prev == old) return nw & kCountMask;
-    old = prev;
-  }
-}
-
 __device__ __forceinline__ void named_sync_softmax() {  // warps 0-7
   asm volatile("bar.sync 1, 256;" ::: "memory");
 }

@@ -25,6 +25,7 @@
 // done, so that every TMEM hand-over is by a barrier that was waited for.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "attn_tc.cuh"
 
@@ -57,8 +58,10 @@ enum {
 };
 constexpr int kOffTmemSlot = kOffMisc + 8 * kNumBars;
 constexpr int kOffAbort = kOffTmemSlot + 4;
-constexpr int kOffPrefix = (kOffAbort + 4 + 15) / 16 * 16;  // int units_start[B+1]
-constexpr int kSmemBytes = kOffPrefix + 4 * (kAttnMaxBatch + 1);
+constexpr int kOffLast = kOffAbort + 4;
+constexpr int kOffSplit = kOffLast + 4;                          // 1: units are cut at range borders
+constexpr int kOffPrefix = (kOffSplit + 4 + 15) / 16 * 16;       // int64 first position of each sequence [B+1]
+constexpr int kSmemBytes = kOffPrefix + 8 * (kAttnMaxBatch + 1);
 static_assert(kSmemBytes <= 232448, "fits the 227 KiB opt-in");
 
 constexpr uint32_t kColS = 0;    // S[m]: columns m*128; P[m] in the first 64 of them
@@ -70,9 +73,21 @@ struct PromptArgs {
   const int32_t* cache_len;
   int rows, batch, heads_q, G, cap;
   float scale_log2;
+  int* cnt;       // [CTAs] (launch tag << 9) | pieces arrived of the unit whose first piece the CTA has
+  uint32_t tag;   // this launch's tag
+  float* ws_o;    // [2 * CTAs][32][256] float4 partial outputs
+  float* ws_lse;  // [2 * CTAs][256] their base-2 log-sum-exps
   uint16_t* out;
   int* err;
 };
+
+// Positions.  Every unit takes kUnitCost positions (what starting and ending a
+// piece costs, in key times) and then one for each key of the last row that its
+// row group could have; tile t of it stands at the position of its first key.
+constexpr int kUnitCost = 2 * BN;
+// What cutting units costs a call, and the fewest positions worth a CTA.
+constexpr int kMergeCost = 5 * BN;
+constexpr int kMinShare = 3 * BN;
 
 // A sequence's rows and the tokens before them; n = 0 where they do not make sense.
 struct Seq {
@@ -91,32 +106,109 @@ __device__ __forceinline__ Seq sequence(const PromptArgs& A, int b, int* bad) {
   return s;
 }
 
-struct Unit {
-  int b, h, rg;   // sequence, kv head, row group
-  int r0, n, L;   // its rows and the tokens before them
-  int keys, T;    // keys that any of the unit's rows sees, and their tiles
+// Tiles [t0, t1) of one unit.
+struct Piece {
+  int b, h, rg;    // sequence, kv head, row group
+  int r0, n, L;    // the sequence's rows and the tokens before them
+  int keys, T;     // keys that any of the unit's rows sees, and their tiles
+  int t0, t1;
+  int64_t first;   // position of tile 0
 };
 
-__device__ __forceinline__ Unit unit_at(const PromptArgs& A, const int* units_start, int npb, int u) {
-  int lo = 0, hi = A.batch;  // largest b with units_start[b] <= u
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (units_start[mid] <= u) lo = mid;
-    else hi = mid;
+// The pieces of one CTA.  Either units are cut (positions laid end to end and
+// split evenly over the CTAs) or they are dealt out whole, one position each.
+struct Walk {
+  const int64_t* start;  // first position of each sequence
+  int B, Hkv, R;         // R: rows of a row group
+  bool split;
+  int P;                 // CTAs that take part
+  int64_t total, g, g_end;
+  // the unit at position ustart
+  Seq s;
+  int b, rg, h, groups;
+  int64_t ustart, cost;
+
+  __device__ __forceinline__ int64_t before(int k) const {  // positions of a head's row groups 0 .. k - 1
+    return split ? k * (int64_t)(kUnitCost + s.L) + (int64_t)R * k * (k + 1) / 2 : k;
   }
-  int bad;
-  const Seq s = sequence(A, lo, &bad);
-  Unit x;
-  x.b = lo;
-  x.r0 = s.r0;
-  x.n = s.n;
-  x.L = s.L;
-  const int k = u - units_start[lo];
-  x.rg = k / A.kv.heads_kv;
-  x.h = k % A.kv.heads_kv;
-  x.keys = s.L + min((x.rg + 1) * 2 * npb, s.n);
-  x.T = (x.keys + BN - 1) / BN;
-  return x;
+  __device__ __forceinline__ int owner(int64_t p) const { return (int)(((p + 1) * P - 1) / total); }
+  __device__ __forceinline__ void load(const PromptArgs& A) {
+    int bad;
+    s = sequence(A, b, &bad);
+    groups = (s.n + R - 1) / R;
+  }
+  __device__ __forceinline__ void price() { cost = split ? kUnitCost + s.L + (int64_t)(rg + 1) * R : 1; }
+  __device__ void seek(const PromptArgs& A) {  // the unit that holds position g
+    int lo = 0, hi = B;  // largest b with start[b] <= g
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (start[mid] <= g) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    load(A);
+    const int64_t local = g - start[b];
+    lo = 0, hi = groups;  // largest row group that starts at or before it
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (Hkv * before(mid) <= local) lo = mid;
+      else hi = mid;
+    }
+    rg = lo;
+    price();
+    h = (int)((local - Hkv * before(rg)) / cost);
+    ustart = start[b] + Hkv * before(rg) + h * cost;
+  }
+  __device__ __forceinline__ void begin(const PromptArgs& A) {
+    const int c = (int)blockIdx.x;
+    g = !split ? c : c < P ? (int64_t)c * total / P : total;
+    g_end = !split ? total : c < P ? (int64_t)(c + 1) * total / P : total;
+    if (g < g_end) seek(A);
+  }
+  // The next piece; false when there is none.
+  __device__ bool next(const PromptArgs& A, Piece& x) {
+    while (g < g_end) {
+      x.b = b;
+      x.h = h;
+      x.rg = rg;
+      x.r0 = s.r0;
+      x.n = s.n;
+      x.L = s.L;
+      x.keys = s.L + min((rg + 1) * R, s.n);
+      x.T = (x.keys + BN - 1) / BN;
+      if (!split) {
+        x.t0 = 0;
+        x.t1 = x.T;
+        x.first = 0;
+        g += P;
+        if (g < g_end) seek(A);
+        return true;
+      }
+      x.first = ustart + kUnitCost;
+      x.t0 = g <= x.first ? 0 : (int)min((int64_t)x.T, (g - x.first + BN - 1) / BN);
+      x.t1 = g_end <= x.first ? 0 : (int)min((int64_t)x.T, (g_end - x.first + BN - 1) / BN);
+      g = ustart += cost;
+      if (g < g_end) {  // on to the next unit, in the same sequence or the next one that has rows
+        if (++h == Hkv) {
+          h = 0;
+          if (++rg == groups) {
+            rg = 0;
+            do {
+              ++b;
+              load(A);
+            } while (groups == 0);
+          }
+          price();
+        }
+      }
+      if (x.t0 < x.t1) return true;
+    }
+    return false;
+  }
+};
+
+__device__ __forceinline__ void sync_softmax() {  // warps 0-7
+  asm volatile("bar.sync 1, 256;" ::: "memory");
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -132,7 +224,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   const int G = A.G, npb = BM / G;
   const Bar bar{sb + kOffMisc};
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
-  int* units_start = reinterpret_cast<int*>(smem + kOffPrefix);
+  volatile int* last_flag = reinterpret_cast<volatile int*>(smem + kOffLast);
+  volatile int* split_flag = reinterpret_cast<volatile int*>(smem + kOffSplit);
+  int64_t* start = reinterpret_cast<int64_t*>(smem + kOffPrefix);
+  const int R = 2 * npb;
 
   // ---------------------------------------------------------------- set-up
   if (tid == 0) {
@@ -164,46 +259,79 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     st_shared_v4(sb + kOffQ + mh * kQHalf + rr * 128 + q16 * 16, 0u, 0u, 0u, 0u);
   }
   pdl_begin();
-  if (warp == 9) {  // units of each sequence and their prefix sums
-    int run = 0;
+  if (warp == 9) {
+    // Totals first: whether to cut units is chosen by them.  Whole units: as many
+    // rounds of the CTAs as it takes, of the longest unit's time; cut units: an even
+    // share and the merges.
+    auto positions = [&](int b, bool units, int* bad) -> int64_t {  // of sequence b
+      const Seq s = sequence(A, b, bad);
+      const int64_t k = (s.n + R - 1) / R;
+      return A.kv.heads_kv * (units ? k : k * (kUnitCost + s.L) + R * k * (k + 1) / 2);
+    };
+    int64_t units = 0, cost = 0;
+    int longest = 0;
+    for (int b = lane; b < A.batch; b += 32) {
+      int bad;
+      const Seq s = sequence(A, b, &bad);
+      if (bad && blockIdx.x == 0) flag(A.err, bad);
+      if (s.n > 0) longest = max(longest, s.L + s.n);
+      units += positions(b, true, &bad);
+      cost += positions(b, false, &bad);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+      units += __shfl_xor_sync(0xffffffffu, units, off);
+      cost += __shfl_xor_sync(0xffffffffu, cost, off);
+    }
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    const int64_t P = gridDim.x, rounds = (units + P - 1) / P;
+    const bool split = rounds * (longest + kUnitCost) > (cost + P - 1) / P + kMergeCost;
+    int64_t run = 0;
     for (int base = 0; base < A.batch; base += 32) {
       const int b = base + lane;
-      int ub = 0;
-      if (b < A.batch) {
-        int bad;
-        const Seq s = sequence(A, b, &bad);
-        if (bad && blockIdx.x == 0) flag(A.err, bad);
-        ub = (s.n + 2 * npb - 1) / (2 * npb) * A.kv.heads_kv;
-      }
-      int iu = ub;
+      int bad;
+      const int64_t own = b < A.batch ? positions(b, !split, &bad) : 0;
+      int64_t upto = own;
 #pragma unroll
       for (int off = 1; off < 32; off <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, iu, off);
-        if (lane >= off) iu += y;
+        const int64_t y = __shfl_up_sync(0xffffffffu, upto, off);
+        if (lane >= off) upto += y;
       }
-      if (b < A.batch) units_start[b] = run + iu - ub;
-      run += __shfl_sync(0xffffffffu, iu, 31);
+      if (b < A.batch) start[b] = run + upto - own;
+      run += __shfl_sync(0xffffffffu, upto, 31);
     }
-    if (lane == 0) units_start[A.batch] = run;
+    if (lane == 0) {
+      start[A.batch] = run;
+      *split_flag = split;
+    }
   }
   fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmemSlot);
-  const int units = units_start[A.batch];
-  // M tile 1 of a unit is active when its first row is one of the sequence's
-  auto active1 = [&](const Unit& x) { return (2 * x.rg + 1) * npb < x.n; };
+  Walk walk;
+  walk.start = start;
+  walk.B = A.batch;
+  walk.Hkv = A.kv.heads_kv;
+  walk.R = R;
+  walk.split = *split_flag;
+  walk.total = start[A.batch];
+  // every CTA that takes part in cut units has a tile of each unit that its range lies in
+  walk.P = walk.split ? (int)max((int64_t)1, min((int64_t)gridDim.x, walk.total / kMinShare)) : (int)gridDim.x;
+  walk.begin(A);
+  Piece x;
+  // M tile 1 of a piece is active when its first row is one of the sequence's
+  auto active1 = [&](const Piece& x) { return (2 * x.rg + 1) * npb < x.n; };
 
   if (warp == 8) {
     // ================================================================ producer
     const int ps = A.kv.page_size;
     const int ppt = A.kv.layout == 1 ? BN / ps : 0;  // pages (boxes) of a tile: 2 .. 16
     const uint32_t qbytes = (uint32_t)(npb * G * 128);
-    uint32_t qc = 0, issued = 0;  // units, ring tiles
+    uint32_t qc = 0, issued = 0;  // pieces, ring tiles
     bool ok = true;
-    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit x = unit_at(A, units_start, npb, u);
+    while (ok && walk.next(A, x)) {
       auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
         const int tok = t * BN + lane * ps;
         if (lane >= ppt || tok >= x.keys) return -1;
@@ -214,9 +342,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         }
         return page;
       };
-      int page = ppt > 0 ? page_of(0) : -1;
-      for (int t = 0; ok && t < x.T; ++t) {
-        const int next = ppt > 0 && t + 1 < x.T ? page_of(t + 1) : -1;
+      int page = ppt > 0 ? page_of(x.t0) : -1;
+      for (int t = x.t0; ok && t < x.t1; ++t) {
+        const int next = ppt > 0 && t + 1 < x.t1 ? page_of(t + 1) : -1;
         for (int kv = 0; kv < 2; ++kv) {  // the K tile, then the V tile
           const int st = (int)(issued % NS);
           if (!wait_warp(bar(B_EMPTY + st), ((issued / NS) & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
@@ -232,7 +360,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           }
           __syncwarp();
           ++issued;
-          if (t == 0 && kv == 0) {  // Q of both M tiles once the previous unit's S products are done
+          if (t == x.t0 && kv == 0) {  // Q of both M tiles once the previous piece's S products are done
             if (!wait_warp(bar(B_QEMPTY), (qc & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
             ++qc;
             if (lane == 0) mbar_arrive_expect_tx(bar(B_QFULL), 4 * qbytes);
@@ -256,15 +384,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const int m = warp - 9;
     constexpr uint32_t idS = idesc_bf16_f32(BM, BN, false), idO = idesc_bf16_f32(BM, D, true);
     const bool paged = A.kv.layout == 1;
-    uint32_t qc = 0, r = 0, c = 0;  // units, ring tiles, tiles of this M tile
+    uint32_t qc = 0, r = 0, c = 0;  // pieces, ring tiles, tiles of this M tile
     bool ok = true;
-    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit x = unit_at(A, units_start, npb, u);
+    while (ok && walk.next(A, x)) {
       const bool act = m == 0 || active1(x);
       if (!wait_warp(bar(B_QFULL), qc & 1u, abort_flag, A.err)) break;
       ++qc;
       const uint64_t qd = sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024);
-      for (int t = 0; ok && t < x.T; ++t, r += 2) {
+      for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
         const uint32_t sk = r % NS, sv = (r + 1) % NS;
         if (!wait_warp(bar(B_FULL + sk), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
         if (!act) {  // no rows in this M tile: the ring's tiles are passed on
@@ -283,7 +410,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         mma_s_group(tmem + kColS + m * BN, qd, sdesc_sw128(ka, 16, sbo), sdesc_sw128(ka + kh, 16, sbo), idS);
         commit_elect(bar(B_SFULL + m));
         commit_elect(bar(B_EMPTY + sk));
-        if (t == x.T - 1) commit_elect(bar(B_QEMPTY));  // the unit's last use of Q
+        if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
         if (!wait_warp(bar(B_FULL + sv), ((r + 1) / NS) & 1u, abort_flag, A.err) ||
             !wait_warp(bar(B_PFULL + m), c & 1u, abort_flag, A.err)) {
           ok = false;
@@ -292,7 +419,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         tc_fence_after();
         // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
         const uint64_t vd = sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
-        mma_pv_group(tmem + kColO + m * D, tmem + kColS + m * BN, vd, idO, t > 0 ? 1u : 0u);
+        mma_pv_group(tmem + kColO + m * D, tmem + kColS + m * BN, vd, idO, t > x.t0 ? 1u : 0u);
         mma_pv_group(tmem + kColO + m * D, tmem + kColS + m * BN + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
         commit_elect(bar(B_PVDONE + m));
         commit_elect(bar(B_EMPTY + sv));
@@ -315,16 +442,16 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const float c = A.scale_log2;
     uint32_t sc = 0, r = 0;  // tiles of this M tile, ring tiles
     bool ok = true;
-    for (int u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      const Unit x = unit_at(A, units_start, npb, u);
-      const uint32_t r_unit = r;
-      r += 2 * (uint32_t)x.T;
-      if (m == 1 && !active1(x)) continue;
+    while (walk.next(A, x)) {
+      const uint32_t r_piece = r;
+      r += 2 * (uint32_t)(x.t1 - x.t0);
+      const bool act = m == 0 || active1(x), whole = x.t1 - x.t0 == x.T;
+      if (whole && !act) continue;
       const int i = (2 * x.rg + m) * npb + row / G;  // the row's place in its sequence
       const int sees = x.L + i + 1;                  // keys that it sees
       const int all_see = x.L + (2 * x.rg + m) * npb + 1;  // that every row of the M tile sees
       float m_run = -INFINITY, l_run = 0.f;
-      for (int t = 0; t < x.T; ++t) {
+      for (int t = x.t0; act && ok && t < x.t1; ++t) {
         if (!wait_warp(bar(B_SFULL + m), sc & 1u, abort_flag, A.err)) { ok = false; break; }
         ++sc;
         tc_fence_after();
@@ -373,7 +500,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         f2_unpack(sm2[1], s4[2], s4[3]);
         l_run = l_run * alpha + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
         // O: the PV product of the tile before was done before this S was issued
-        if (t > 0 && __any_sync(0xffffffffu, need)) {
+        if (t > x.t0 && __any_sync(0xffffffffu, need)) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             uint32_t o[32];
@@ -388,7 +515,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         // there cannot reach O through 0 * NaN
         const int valid = x.keys - t * BN;
         if (valid < BN) {
-          const uint32_t rv = r_unit + 2 * (uint32_t)t + 1;
+          const uint32_t rv = r_piece + 2 * (uint32_t)(t - x.t0) + 1;
           if (!wait_warp(bar(B_FULL + rv % NS), (rv / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
           const uint32_t vb = sb + kOffRing + (rv % NS) * kTile;
           const bool paged = A.kv.layout == 1;
@@ -404,30 +531,139 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         tc_fence_before();
         mbar_arrive(bar(B_PFULL + m));
       }
-      if (!ok || !wait_warp(bar(B_PVDONE + m), (sc - 1) & 1u, abort_flag, A.err)) break;
+      if (act && ok && !wait_warp(bar(B_PVDONE + m), (sc - 1) & 1u, abort_flag, A.err)) ok = false;
       tc_fence_after();
-      // ---- the output rows
       const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-      uint16_t* orow = A.out + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D;
-      const bool vrow = row < npb * G && i < x.n;
+      const bool vrow = act && ok && row < npb * G && i < x.n;
+      if (whole) {
+        // ---- the output rows
+        uint16_t* orow = A.out + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D;
+        if (ok) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t o[32];
-        tmem_ld32(tO + q * 32, o);
-        tmem_wait_ld();
-        if (vrow) {
+          for (int q = 0; q < 4; ++q) {
+            uint32_t o[32];
+            tmem_ld32(tO + q * 32, o);
+            tmem_wait_ld();
+            if (vrow) {
 #pragma unroll
-          for (int k = 0; k < 32; k += 8) {
-            uint4 v;
-            v.x = pack_bf16(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
-            v.y = pack_bf16(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
-            v.z = pack_bf16(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
-            v.w = pack_bf16(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
-            *reinterpret_cast<uint4*>(orow + q * 32 + k) = v;
+              for (int k = 0; k < 32; k += 8) {
+                uint4 v;
+                v.x = pack_bf16(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
+                v.y = pack_bf16(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
+                v.z = pack_bf16(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
+                v.w = pack_bf16(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
+                *reinterpret_cast<uint4*>(orow + q * 32 + k) = v;
+              }
+            }
           }
         }
+        tc_fence_before();
+        continue;
+      }
+      // ---- a part of a unit: normalised O and log-sum-exp to the workspace, float4
+      // columns [32][256 rows]; the CTA whose piece arrives last joins all of them, in
+      // the order of the keys whichever that is
+      const int cta = (int)blockIdx.x;
+      const int64_t slot = 2 * (int64_t)cta + (x.t0 == 0);
+      const int prow = m * BM + row;
+      if (act && ok) {
+        float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + prow;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t o[32];
+          tmem_ld32(tO + q * 32, o);
+          tmem_wait_ld();
+          if (vrow) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              po[(q * 8 + k) * (2 * BM)] =
+                  make_float4(__uint_as_float(o[4 * k]) * inv, __uint_as_float(o[4 * k + 1]) * inv,
+                              __uint_as_float(o[4 * k + 2]) * inv, __uint_as_float(o[4 * k + 3]) * inv);
+          }
+        }
+        if (vrow) A.ws_lse[slot * (2 * BM) + prow] = row_lse(m_run, l_run);
       }
       tc_fence_before();
+      __threadfence();
+      sync_softmax();
+      const int o0 = walk.owner(x.first), parts = walk.owner(x.first + (int64_t)(x.T - 1) * BN) - o0 + 1;
+      if (tid == 0) {
+        int l = 0;
+        if (!*abort_flag) {
+          l = arrive(A.cnt + o0, A.tag) == parts;
+          if (l) A.cnt[o0] = 0;  // a completed unit leaves a zero word behind
+        }
+        *last_flag = l;
+      }
+      sync_softmax();
+      if (*last_flag) {
+        __threadfence();
+        // rows 0 .. v0 - 1 of M tile 0 and 0 .. v1 - 1 of M tile 1
+        const int v0 = min(npb, x.n - 2 * x.rg * npb) * G, v1 = max(0, min(npb, x.n - (2 * x.rg + 1) * npb)) * G;
+        const int rows8 = (v0 + v1 + 7) / 8;
+        // A warp takes 8 rows and 4 * C of the 32 float4 columns, N parts' loads in flight:
+        //   O = sum_p 2^(lse_p) O_p / sum_p 2^(lse_p), relative to the maximum so far
+        auto join = [&](auto ctag, auto ntag) {
+          constexpr int C = decltype(ctag)::value, N = decltype(ntag)::value;
+          for (int task = warp; task < rows8 * (8 / C); task += 8) {
+            const int k = task / (8 / C) * 8 + (lane >> 2), c0 = task % (8 / C) * 4 * C + (lane & 3);
+            if (k >= v0 + v1) continue;
+            const int mt = k >= v0, rr = mt ? k - v0 : k;
+            const int64_t at = mt * BM + rr;
+            float4 acc[C];
+#pragma unroll
+            for (int j = 0; j < C; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            float M = -INFINITY, wsum = 0.f;
+            for (int p0 = 0; p0 < parts; p0 += N) {
+              float w[N];
+              float4 o[N][C];
+#pragma unroll
+              for (int p = 0; p < N; ++p) {
+                if (p0 + p < parts) {
+                  const int64_t sl = 2 * (int64_t)(o0 + p0 + p) + (p0 + p == 0);
+                  w[p] = __ldcg(A.ws_lse + sl * (2 * BM) + at);
+#pragma unroll
+                  for (int j = 0; j < C; ++j)
+                    o[p][j] = __ldcg(reinterpret_cast<const float4*>(A.ws_o) + (sl * 32 + c0 + 4 * j) * (2 * BM) + at);
+                } else {
+                  w[p] = -INFINITY;
+#pragma unroll
+                  for (int j = 0; j < C; ++j) o[p][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+              }
+              float Mn = M;
+#pragma unroll
+              for (int p = 0; p < N; ++p) Mn = fmaxf(Mn, w[p]);
+              const float a = ex2(M - Mn);
+              M = Mn;
+              wsum *= a;
+#pragma unroll
+              for (int j = 0; j < C; ++j) acc[j] = make_float4(acc[j].x * a, acc[j].y * a, acc[j].z * a, acc[j].w * a);
+#pragma unroll
+              for (int p = 0; p < N; ++p) {
+                const float wp = ex2(w[p] - Mn);
+                wsum += wp;
+#pragma unroll
+                for (int j = 0; j < C; ++j) {
+                  acc[j].x += wp * o[p][j].x;
+                  acc[j].y += wp * o[p][j].y;
+                  acc[j].z += wp * o[p][j].z;
+                  acc[j].w += wp * o[p][j].w;
+                }
+              }
+            }
+            const float winv = 1.f / wsum;
+            uint16_t* orow =
+                A.out + ((int64_t)(x.r0 + (2 * x.rg + mt) * npb + rr / G) * A.heads_q + x.h * G + rr % G) * D;
+#pragma unroll
+            for (int j = 0; j < C; ++j)
+              *reinterpret_cast<uint2*>(orow + (c0 + 4 * j) * 4) =
+                  make_uint2(pack_bf16(acc[j].x * winv, acc[j].y * winv), pack_bf16(acc[j].z * winv, acc[j].w * winv));
+          }
+        };
+        if (rows8 >= 8) join(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
+        else join(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
+      }
     }
   }
 
@@ -441,13 +677,22 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 
 }  // namespace
 
-size_t prompt_attn_workspace() { return 256; }  // none is needed
+// Workspace: piece counters [CTAs] (256-byte rounded), partial outputs and their
+// log-sum-exps [2 * CTAs]: of a CTA's pieces at most its first and its last are
+// parts of a unit.
+namespace {
+size_t counter_bytes(int ctas) { return ((size_t)ctas * sizeof(int) + 255) / 256 * 256; }
+}  // namespace
+
+size_t prompt_attn_workspace() {
+  const int ctas = num_sms();
+  return counter_bytes(ctas) + (size_t)2 * ctas * 2 * BM * (D + 1) * sizeof(float);
+}
 
 cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
                                const cure_kv_desc& kv, const int32_t* row_start, const int32_t* cache_len, int rows,
                                int batch, int heads_q, float scale, uint16_t* out, void* workspace, int* err,
                                cudaStream_t s) {
-  (void)workspace;
   static std::atomic<uint64_t> done{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -482,10 +727,15 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
   A.scale_log2 = scale * 1.4426950408889634f;
   A.out = out;
   A.err = err;
-  const int npb = BM / G;
-  const int64_t units = ((int64_t)rows / (2 * npb) + batch) * Hkv;  // at most
-  const int grid = (int)std::min<int64_t>(units, num_sms());
-  return launch_pdl(prompt_attn_kernel, dim3(grid), dim3(kThreads), kSmemBytes, s, mk, mv, mq, A);
+  // a fresh tag per launch makes what the workspace's counters held count as zero
+  static std::atomic<uint32_t> launches{0};
+  A.tag = launches.fetch_add(1) % ((1u << (32 - kCountBits)) - 1) + 1;
+  const int ctas = num_sms();
+  char* ws = static_cast<char*>(workspace);
+  A.cnt = reinterpret_cast<int*>(ws);
+  A.ws_o = reinterpret_cast<float*>(ws + counter_bytes(ctas));
+  A.ws_lse = A.ws_o + (size_t)2 * ctas * 2 * BM * D;
+  return launch_pdl(prompt_attn_kernel, dim3(ctas), dim3(kThreads), kSmemBytes, s, mk, mv, mq, A);
 }
 
 }  // namespace cure
