@@ -13,16 +13,21 @@
 //
 // Roles (12 warps):
 //   warps 0-3 / 4-7   softmax of M tile 0 / 1, a thread a row: reads S from TMEM,
-//                     writes P (bf16) over it, keeps the row's running maximum
+//                     writes P (bf16) to TMEM, keeps the row's running maximum
 //                     and sum, rescales O (only where the maximum has grown by
 //                     more than 2^8), writes the output
 //   warp 8            TMA producer: Q, and K and V tiles in turn through a ring
 //                     of 5 stages of 32 KiB
-//   warps 9 / 10      issue M tile 0 / 1's products: S = Q K^T (M128 N128 K128),
-//                     then, once P is published, O += P V (A from TMEM)
-// TMEM (512 columns): S[2] (128 each, P in the first 64 of them) | O[2] (128 each).
-// S of the next tile takes the place of P once the PV product that reads P is
-// done, so that every TMEM hand-over is by a barrier that was waited for.
+//   warp 9            issues S = Q K^T (M128 N128 K128) of M tiles 0 and 1 in turn
+//   warp 10           issues O += P V (A = P from TMEM) once P is published
+// TMEM (512 columns): S (128) | P[2] (64 each) | O[2] (128 each).  There is one S
+// for both M tiles: a softmax frees it as soon as it has loaded its row (128
+// registers), long before its exponentials are done, and the other M tile's
+// product takes it.  That keeps the two M tiles half a tile apart, one in its
+// softmax while the tensor cores work for the other, and no product waits for
+// the PV product of its own M tile.  (With an S for each M tile and P over it, S
+// had to wait for PV to finish; both M tiles then ran in step, 1870 cycles of
+// softmax and 1940 of products a tile, one after the other.)
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -53,8 +58,8 @@ constexpr int kOffQ = 0;                       // Q[m][half]
 constexpr int kOffRing = kOffQ + 4 * kQHalf;   // K/V[stage]
 constexpr int kOffMisc = kOffRing + NS * kTile;
 enum {
-  B_QFULL = 0, B_QEMPTY = 1, B_FULL = 2, B_EMPTY = B_FULL + NS, B_SFULL = B_EMPTY + NS, B_PFULL = B_SFULL + 2,
-  B_PVDONE = B_PFULL + 2, B_DRAIN = B_PVDONE + 2, kNumBars = B_DRAIN + 2
+  B_QFULL = 0, B_QEMPTY = 1, B_SFREE = 2, B_FULL = 3, B_EMPTY = B_FULL + NS, B_SFULL = B_EMPTY + NS,
+  B_PFULL = B_SFULL + 2, B_PVDONE = B_PFULL + 2, B_DRAIN = B_PVDONE + 2, kNumBars = B_DRAIN + 2
 };
 constexpr int kOffTmemSlot = kOffMisc + 8 * kNumBars;
 constexpr int kOffAbort = kOffTmemSlot + 4;
@@ -64,7 +69,8 @@ constexpr int kOffPrefix = (kOffSplit + 4 + 15) / 16 * 16;       // int64 first 
 constexpr int kSmemBytes = kOffPrefix + 8 * (kAttnMaxBatch + 1);
 static_assert(kSmemBytes <= 232448, "fits the 227 KiB opt-in");
 
-constexpr uint32_t kColS = 0;    // S[m]: columns m*128; P[m] in the first 64 of them
+constexpr uint32_t kColS = 0;    // S:    columns 0 .. 127
+constexpr uint32_t kColP = 128;  // P[m]: columns 128 + m*64
 constexpr uint32_t kColO = 256;  // O[m]: columns 256 + m*128
 
 struct PromptArgs {
@@ -232,10 +238,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   // ---------------------------------------------------------------- set-up
   if (tid == 0) {
     mbar_init(bar(B_QFULL), 1);
-    mbar_init(bar(B_QEMPTY), 2);
+    mbar_init(bar(B_QEMPTY), 1);
+    mbar_init(bar(B_SFREE), BM);
     for (int i = 0; i < NS; ++i) {
       mbar_init(bar(B_FULL + i), 1);
-      mbar_init(bar(B_EMPTY + i), 2);
+      mbar_init(bar(B_EMPTY + i), 1);
     }
     for (int m = 0; m < 2; ++m) {
       mbar_init(bar(B_SFULL + m), 1);
@@ -379,66 +386,79 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         wait_bounded(bar(B_FULL + i % NS), (i / NS) & 1u, abort_flag, A.err, false);
       if (qc > 0) wait_bounded(bar(B_QFULL), (qc - 1) & 1u, abort_flag, A.err, false);
     }
-  } else if (warp == 9 || warp == 10) {
-    // ================================================================ products of M tile m
-    const int m = warp - 9;
-    constexpr uint32_t idS = idesc_bf16_f32(BM, BN, false), idO = idesc_bf16_f32(BM, D, true);
+  } else if (warp == 9) {
+    // ================================================================ S products
+    constexpr uint32_t idS = idesc_bf16_f32(BM, BN, false);
     const bool paged = A.kv.layout == 1;
-    uint32_t qc = 0, r = 0, c = 0;  // pieces, ring tiles, tiles of this M tile
+    uint32_t qc = 0, r = 0, c = 0;  // pieces, ring tiles, products
     bool ok = true;
     while (ok && walk.next(A, x)) {
-      const bool act = m == 0 || active1(x);
       if (!wait_warp(bar(B_QFULL), qc & 1u, abort_flag, A.err)) break;
       ++qc;
-      const uint64_t qd = sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024);
+      const int mts = active1(x) ? 2 : 1;
       for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
-        const uint32_t sk = r % NS, sv = (r + 1) % NS;
-        if (!wait_warp(bar(B_FULL + sk), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
-        if (!act) {  // no rows in this M tile: the ring's tiles are passed on
-          if (lane == 0) mbar_arrive(bar(B_EMPTY + sk));
-          __syncwarp();
-          if (!wait_warp(bar(B_FULL + sv), ((r + 1) / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
-          if (lane == 0) mbar_arrive(bar(B_EMPTY + sv));
-          __syncwarp();
-          continue;
-        }
-        // S takes P's place: the PV product of the tile before must be done
-        if (c > 0 && !wait_warp(bar(B_PVDONE + m), (c - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
-        tc_fence_after();
+        const uint32_t sk = r % NS;
         const uint32_t ka = sb + kOffRing + sk * kTile;
         const uint32_t sbo = paged ? kPgGroup : 1024u, kh = paged ? kPgHalf : kKHalf;
-        mma_s_group(tmem + kColS + m * BN, qd, sdesc_sw128(ka, 16, sbo), sdesc_sw128(ka + kh, 16, sbo), idS);
-        commit_elect(bar(B_SFULL + m));
+        for (int m = 0; m < mts; ++m) {
+          if (c > 0 && !wait_warp(bar(B_SFREE), (c - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
+          ++c;
+          // The K tile, after SFREE: a parity wait is sound from the phase before on and
+          // not later, and the stage's tile before this one, V of three tiles before, has
+          // landed when the softmax of M tile 0 has loaded S of the tile before (it then
+          // has seen the PV product of that V tile done).
+          if (m == 0 && !wait_warp(bar(B_FULL + sk), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+          tc_fence_after();
+          mma_s_group(tmem + kColS, sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024), sdesc_sw128(ka, 16, sbo),
+                      sdesc_sw128(ka + kh, 16, sbo), idS);
+          commit_elect(bar(B_SFULL + m));
+        }
+        if (!ok) break;
         commit_elect(bar(B_EMPTY + sk));
         if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
-        if (!wait_warp(bar(B_FULL + sv), ((r + 1) / NS) & 1u, abort_flag, A.err) ||
-            !wait_warp(bar(B_PFULL + m), c & 1u, abort_flag, A.err)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
-        const uint64_t vd = sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
-        mma_pv_group(tmem + kColO + m * D, tmem + kColS + m * BN, vd, idO, t > x.t0 ? 1u : 0u);
-        mma_pv_group(tmem + kColO + m * D, tmem + kColS + m * BN + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
-        commit_elect(bar(B_PVDONE + m));
-        commit_elect(bar(B_EMPTY + sv));
-        ++c;
-      }
-      if (!act && ok) {
-        if (lane == 0) mbar_arrive(bar(B_QEMPTY));
-        __syncwarp();
       }
     }
     __syncwarp();
-    commit_elect(bar(B_DRAIN + m));
-    wait_bounded(bar(B_DRAIN + m), 0, abort_flag, A.err, false);
+    commit_elect(bar(B_DRAIN));
+    wait_bounded(bar(B_DRAIN), 0, abort_flag, A.err, false);
+  } else if (warp == 10) {
+    // ================================================================ PV products
+    constexpr uint32_t idO = idesc_bf16_f32(BM, D, true);
+    const bool paged = A.kv.layout == 1;
+    uint32_t r = 1, c[2] = {0, 0};  // ring tiles, products of each M tile
+    bool ok = true;
+    while (ok && walk.next(A, x)) {
+      const int mts = active1(x) ? 2 : 1;
+      for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
+        const uint32_t sv = r % NS;
+        // (the stage's K tile of two tiles before has landed: its S became the P that this
+        // warp has waited for)
+        if (!wait_warp(bar(B_FULL + sv), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+        // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
+        const uint64_t vd = sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          if (m >= mts) break;
+          if (!wait_warp(bar(B_PFULL + m), c[m] & 1u, abort_flag, A.err)) { ok = false; break; }
+          ++c[m];
+          tc_fence_after();
+          mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0 ? 1u : 0u);
+          mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64 + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
+          commit_elect(bar(B_PVDONE + m));
+        }
+        if (!ok) break;
+        commit_elect(bar(B_EMPTY + sv));
+      }
+    }
+    __syncwarp();
+    commit_elect(bar(B_DRAIN + 1));
+    wait_bounded(bar(B_DRAIN + 1), 0, abort_flag, A.err, false);
   } else if (warp < 8) {
     // ================================================================ softmax
     const int m = warp >> 2;
     const int row = tid & 127;  // row within the M tile = TMEM lane
     const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t tS = tl + kColS + m * BN, tO = tl + kColO + m * D;
+    const uint32_t tS = tl + kColS, tP = tl + kColP + m * 64, tO = tl + kColO + m * D;
     const float c = A.scale_log2;
     uint32_t sc = 0, r = 0;  // tiles of this M tile, ring tiles
     bool ok = true;
@@ -459,6 +479,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 #pragma unroll
         for (int q = 0; q < 4; ++q) tmem_ld32(tS + 32 * q, v[q]);
         tmem_wait_ld();
+        tc_fence_before();
+        mbar_arrive(bar(B_SFREE));  // the next product may take S
         float x_[BN];
 #pragma unroll
         for (int k = 0; k < BN; ++k) x_[k] = __uint_as_float(v[k >> 5][k & 31]);
@@ -479,6 +501,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         const bool need = m_new > m_run + 8.0f;
         const float alpha = need ? ex2(m_run - m_new) : 1.f;
         if (need) m_run = m_new;
+        // P's place and O are free once this M tile's PV product before is done
+        if (sc > 1) {
+          if (!wait_warp(bar(B_PVDONE + m), (sc - 2) & 1u, abort_flag, A.err)) { ok = false; break; }
+          tc_fence_after();
+        }
         const float nbase = m_run == -INFINITY ? 0.f : -m_run;
         const uint64_t c2 = f2_pack(c, c), nb2 = f2_pack(nbase, nbase);
         uint64_t sm2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
@@ -493,13 +520,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             sm2[k & 1] = f2_add(sm2[k & 1], f2_pack(p0, p1));
             pk[k] = pack_bf16(p0, p1);
           }
-          tmem_st16(tS + 16 * q, pk);
+          tmem_st16(tP + 16 * q, pk);
         }
         float s4[4];
         f2_unpack(sm2[0], s4[0], s4[1]);
         f2_unpack(sm2[1], s4[2], s4[3]);
         l_run = l_run * alpha + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
-        // O: the PV product of the tile before was done before this S was issued
         if (t > x.t0 && __any_sync(0xffffffffu, need)) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
