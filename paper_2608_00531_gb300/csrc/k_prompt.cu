@@ -45,6 +45,8 @@ constexpr int D = kAttnD;
 constexpr int NS = 5;             // ring stages, a K or a V tile each
 constexpr int kThreads = 384;
 constexpr uint32_t kTmemCols = 512;
+constexpr int kPieces = 4;        // pieces that the scheduler may be ahead
+constexpr int kTakers = 11;       // warps that take pieces: 0 - 10
 
 constexpr int kQHalf = kAttnQHalf;      // 16 KiB: [128 rows][64 d]
 constexpr int kKHalf = BN * 64 * 2;     // 16 KiB: [128 keys][64 d]
@@ -59,13 +61,15 @@ constexpr int kOffRing = kOffQ + 4 * kQHalf;   // K/V[stage]
 constexpr int kOffMisc = kOffRing + NS * kTile;
 enum {
   B_QFULL = 0, B_QEMPTY = 1, B_SFREE = 2, B_FULL = 3, B_EMPTY = B_FULL + NS, B_SFULL = B_EMPTY + NS,
-  B_PFULL = B_SFULL + 2, B_PVDONE = B_PFULL + 2, B_DRAIN = B_PVDONE + 2, kNumBars = B_DRAIN + 2
+  B_PFULL = B_SFULL + 2, B_PVDONE = B_PFULL + 2, B_DRAIN = B_PVDONE + 2, B_JOIN = B_DRAIN + 2,
+  B_PIECE = B_JOIN + 1, B_TAKEN = B_PIECE + kPieces, kNumBars = B_TAKEN + kPieces
 };
 constexpr int kOffTmemSlot = kOffMisc + 8 * kNumBars;
 constexpr int kOffAbort = kOffTmemSlot + 4;
 constexpr int kOffLast = kOffAbort + 4;
-constexpr int kOffSplit = kOffLast + 4;                          // 1: units are cut at range borders
-constexpr int kOffPrefix = (kOffSplit + 4 + 15) / 16 * 16;       // int64 first position of each sequence [B+1]
+constexpr int kPieceInts = 12;
+constexpr int kOffPieces = (kOffLast + 4 + 15) / 16 * 16;             // int [kPieces][kPieceInts]
+constexpr int kOffPrefix = kOffPieces + kPieces * kPieceInts * 4;     // int64 first position of each sequence [B+1]
 constexpr int kSmemBytes = kOffPrefix + 8 * (kAttnMaxBatch + 1);
 static_assert(kSmemBytes <= 232448, "fits the 227 KiB opt-in");
 
@@ -113,22 +117,24 @@ __device__ __forceinline__ Seq sequence(const PromptArgs& A, int b, int* bad) {
 }
 
 // Tiles [t0, t1) of one unit.
-struct Piece {
+struct alignas(16) Piece {
   int b, h, rg;    // sequence, kv head, row group
   int r0, n, L;    // the sequence's rows and the tokens before them
   int keys, T;     // keys that any of the unit's rows sees, and their tiles
-  int t0, t1;
-  int64_t first;   // position of tile 0
+  int t0, t1;      // t0 == t1: no more pieces
+  int o0, parts;   // the unit's pieces: of CTAs o0 .. o0 + parts - 1
 };
+static_assert(sizeof(Piece) == 4 * kPieceInts, "as it lies in shared memory");
 
-// The pieces of one CTA.  Either units are cut (positions laid end to end and
-// split evenly over the CTAs) or they are dealt out whole, one position each.
+// The pieces of one CTA, laid out by the scheduler warp.  Either units are cut
+// (positions laid end to end and split evenly over the CTAs) or they are dealt
+// out whole, one position each.
 struct Walk {
   const int64_t* start;  // first position of each sequence
   int B, Hkv, R;         // R: rows of a row group
   bool split;
   int P;                 // CTAs that take part
-  int64_t total, g, g_end;
+  int64_t total;
   // the unit at position ustart
   Seq s;
   int b, rg, h, groups;
@@ -144,7 +150,7 @@ struct Walk {
     groups = (s.n + R - 1) / R;
   }
   __device__ __forceinline__ void price() { cost = split ? kUnitCost + s.L + (int64_t)(rg + 1) * R : 1; }
-  __device__ void seek(const PromptArgs& A) {  // the unit that holds position g
+  __device__ void seek(const PromptArgs& A, int64_t g) {  // the unit that holds position g
     int lo = 0, hi = B;  // largest b with start[b] <= g
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -165,56 +171,78 @@ struct Walk {
     h = (int)((local - Hkv * before(rg)) / cost);
     ustart = start[b] + Hkv * before(rg) + h * cost;
   }
-  __device__ __forceinline__ void begin(const PromptArgs& A) {
-    const int c = (int)blockIdx.x;
-    g = !split ? c : c < P ? (int64_t)c * total / P : total;
-    g_end = !split ? total : c < P ? (int64_t)(c + 1) * total / P : total;
-    if (g < g_end) seek(A);
-  }
-  // The next piece; false when there is none.
-  __device__ bool next(const PromptArgs& A, Piece& x) {
-    while (g < g_end) {
-      x.b = b;
-      x.h = h;
-      x.rg = rg;
-      x.r0 = s.r0;
-      x.n = s.n;
-      x.L = s.L;
-      x.keys = s.L + min((rg + 1) * R, s.n);
-      x.T = (x.keys + BN - 1) / BN;
-      if (!split) {
-        x.t0 = 0;
-        x.t1 = x.T;
-        x.first = 0;
-        g += P;
-        if (g < g_end) seek(A);
-        return true;
-      }
-      x.first = ustart + kUnitCost;
-      x.t0 = g <= x.first ? 0 : (int)min((int64_t)x.T, (g - x.first + BN - 1) / BN);
-      x.t1 = g_end <= x.first ? 0 : (int)min((int64_t)x.T, (g_end - x.first + BN - 1) / BN);
-      g = ustart += cost;
-      if (g < g_end) {  // on to the next unit, in the same sequence or the next one that has rows
-        if (++h == Hkv) {
-          h = 0;
-          if (++rg == groups) {
-            rg = 0;
-            do {
-              ++b;
-              load(A);
-            } while (groups == 0);
-          }
-          price();
-        }
-      }
-      if (x.t0 < x.t1) return true;
+  __device__ __forceinline__ void advance(const PromptArgs& A) {  // to the next unit (there is one)
+    ustart += cost;
+    if (++h < Hkv) return;
+    h = 0;
+    if (++rg == groups) {
+      rg = 0;
+      do {
+        ++b;
+        load(A);
+      } while (groups == 0);
     }
-    return false;
+    price();
+  }
+  __device__ __forceinline__ Piece whole() const {
+    Piece x;
+    x.b = b;
+    x.h = h;
+    x.rg = rg;
+    x.r0 = s.r0;
+    x.n = s.n;
+    x.L = s.L;
+    x.keys = s.L + min((rg + 1) * R, s.n);
+    x.T = (x.keys + BN - 1) / BN;
+    x.t0 = 0;
+    x.t1 = x.T;
+    x.o0 = (int)blockIdx.x;
+    x.parts = 1;
+    return x;
+  }
+  // The unit's tiles in the range [g, g_end).
+  __device__ __forceinline__ Piece within(int64_t g, int64_t g_end) const {
+    Piece x = whole();
+    const int64_t first = ustart + kUnitCost;  // tile 0's position
+    x.t0 = g <= first ? 0 : (int)min((int64_t)x.T, (g - first + BN - 1) / BN);
+    x.t1 = g_end <= first ? 0 : (int)min((int64_t)x.T, (g_end - first + BN - 1) / BN);
+    if (x.t1 - x.t0 < x.T && x.t0 < x.t1) {
+      x.o0 = owner(first);
+      x.parts = owner(first + (int64_t)(x.T - 1) * BN) - x.o0 + 1;
+    }
+    return x;
   }
 };
 
-__device__ __forceinline__ void sync_softmax() {  // warps 0-7
-  asm volatile("bar.sync 1, 256;" ::: "memory");
+// A role's place in the pieces that the scheduler has laid out.
+struct Pieces {
+  uint32_t k;
+  // The next one; false when there is none or the CTA has given up.  (All lanes of a warp.)
+  __device__ __forceinline__ bool next(const Bar& bar, const uint8_t* smem, volatile int* abort_flag, int* err, Piece& x) {
+    const uint32_t slot = k % kPieces;
+    if (!wait_warp(bar(B_PIECE + slot), (k / kPieces) & 1u, abort_flag, err)) return false;
+    const int4* p = reinterpret_cast<const int4*>(smem + kOffPieces + slot * (kPieceInts * 4));
+    int4* d = reinterpret_cast<int4*>(&x);
+#pragma unroll
+    for (int i = 0; i < kPieceInts / 4; ++i) d[i] = p[i];
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar(B_TAKEN + slot));
+    ++k;
+    return x.t0 < x.t1;
+  }
+};
+
+// 32 bytes of a row: one store where the output is aligned to it (whole sectors at
+// a time), else two.
+__device__ __forceinline__ void st_global_32(uint16_t* p, const uint32_t* v, bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+                 "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -231,9 +259,6 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   const Bar bar{sb + kOffMisc};
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
   volatile int* last_flag = reinterpret_cast<volatile int*>(smem + kOffLast);
-  volatile int* split_flag = reinterpret_cast<volatile int*>(smem + kOffSplit);
-  int64_t* start = reinterpret_cast<int64_t*>(smem + kOffPrefix);
-  const int R = 2 * npb;
 
   // ---------------------------------------------------------------- set-up
   if (tid == 0) {
@@ -249,6 +274,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       mbar_init(bar(B_PFULL + m), BM);
       mbar_init(bar(B_PVDONE + m), 1);
       mbar_init(bar(B_DRAIN + m), 1);
+    }
+    mbar_init(bar(B_JOIN), 2 * BM);
+    for (int i = 0; i < kPieces; ++i) {
+      mbar_init(bar(B_PIECE + i), 1);
+      mbar_init(bar(B_TAKEN + i), kTakers);
     }
     *abort_flag = 0;
     fence_mbar_init();
@@ -266,67 +296,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     st_shared_v4(sb + kOffQ + mh * kQHalf + rr * 128 + q16 * 16, 0u, 0u, 0u, 0u);
   }
   pdl_begin();
-  if (warp == 9) {
-    // Totals first: whether to cut units is chosen by them.  Whole units: as many
-    // rounds of the CTAs as it takes, of the longest unit's time; cut units: an even
-    // share and the merges.
-    auto positions = [&](int b, bool units, int* bad) -> int64_t {  // of sequence b
-      const Seq s = sequence(A, b, bad);
-      const int64_t k = (s.n + R - 1) / R;
-      return A.kv.heads_kv * (units ? k : k * (kUnitCost + s.L) + R * k * (k + 1) / 2);
-    };
-    int64_t units = 0, cost = 0;
-    int longest = 0;
-    for (int b = lane; b < A.batch; b += 32) {
-      int bad;
-      const Seq s = sequence(A, b, &bad);
-      if (bad && blockIdx.x == 0) flag(A.err, bad);
-      if (s.n > 0) longest = max(longest, s.L + s.n);
-      units += positions(b, true, &bad);
-      cost += positions(b, false, &bad);
-    }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-      units += __shfl_xor_sync(0xffffffffu, units, off);
-      cost += __shfl_xor_sync(0xffffffffu, cost, off);
-    }
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    const int64_t P = gridDim.x, rounds = (units + P - 1) / P;
-    const bool split = rounds * (longest + kUnitCost) > (cost + P - 1) / P + kMergeCost;
-    int64_t run = 0;
-    for (int base = 0; base < A.batch; base += 32) {
-      const int b = base + lane;
-      int bad;
-      const int64_t own = b < A.batch ? positions(b, !split, &bad) : 0;
-      int64_t upto = own;
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, upto, off);
-        if (lane >= off) upto += y;
-      }
-      if (b < A.batch) start[b] = run + upto - own;
-      run += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    if (lane == 0) {
-      start[A.batch] = run;
-      *split_flag = split;
-    }
-  }
   fence_proxy_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmemSlot);
-  Walk walk;
-  walk.start = start;
-  walk.B = A.batch;
-  walk.Hkv = A.kv.heads_kv;
-  walk.R = R;
-  walk.split = *split_flag;
-  walk.total = start[A.batch];
-  // every CTA that takes part in cut units has a tile of each unit that its range lies in
-  walk.P = walk.split ? (int)max((int64_t)1, min((int64_t)gridDim.x, walk.total / kMinShare)) : (int)gridDim.x;
-  walk.begin(A);
+  Pieces pieces{0};
   Piece x;
   // M tile 1 of a piece is active when its first row is one of the sequence's
   auto active1 = [&](const Piece& x) { return (2 * x.rg + 1) * npb < x.n; };
@@ -338,7 +313,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const uint32_t qbytes = (uint32_t)(npb * G * 128);
     uint32_t qc = 0, issued = 0;  // pieces, ring tiles
     bool ok = true;
-    while (ok && walk.next(A, x)) {
+    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
       auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
         const int tok = t * BN + lane * ps;
         if (lane >= ppt || tok >= x.keys) return -1;
@@ -392,7 +367,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const bool paged = A.kv.layout == 1;
     uint32_t qc = 0, r = 0, c = 0;  // pieces, ring tiles, products
     bool ok = true;
-    while (ok && walk.next(A, x)) {
+    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
       if (!wait_warp(bar(B_QFULL), qc & 1u, abort_flag, A.err)) break;
       ++qc;
       const int mts = active1(x) ? 2 : 1;
@@ -427,7 +402,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const bool paged = A.kv.layout == 1;
     uint32_t r = 1, c[2] = {0, 0};  // ring tiles, products of each M tile
     bool ok = true;
-    while (ok && walk.next(A, x)) {
+    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
       const int mts = active1(x) ? 2 : 1;
       for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
         const uint32_t sv = r % NS;
@@ -460,9 +435,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t tS = tl + kColS, tP = tl + kColP + m * 64, tO = tl + kColO + m * D;
     const float c = A.scale_log2;
+    const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
     uint32_t sc = 0, r = 0;  // tiles of this M tile, ring tiles
     bool ok = true;
-    while (walk.next(A, x)) {
+    // All softmax threads meet (an mbarrier, for a wait that ends when the CTA gives up).
+    uint32_t joins = 0;
+    auto join_softmax = [&]() -> bool {
+      mbar_arrive(bar(B_JOIN));
+      ok = wait_warp(bar(B_JOIN), joins++ & 1u, abort_flag, A.err) && ok;
+      return ok;
+    };
+    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
       const uint32_t r_piece = r;
       r += 2 * (uint32_t)(x.t1 - x.t0);
       const bool act = m == 0 || active1(x), whole = x.t1 - x.t0 == x.T;
@@ -557,30 +540,27 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         tc_fence_before();
         mbar_arrive(bar(B_PFULL + m));
       }
-      if (act && ok && !wait_warp(bar(B_PVDONE + m), (sc - 1) & 1u, abort_flag, A.err)) ok = false;
+      if (act && !(ok && wait_warp(bar(B_PVDONE + m), (sc - 1) & 1u, abort_flag, A.err))) {
+        ok = false;
+        break;
+      }
       tc_fence_after();
       const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-      const bool vrow = act && ok && row < npb * G && i < x.n;
+      const bool vrow = act && row < npb * G && i < x.n;
       if (whole) {
         // ---- the output rows
         uint16_t* orow = A.out + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D;
-        if (ok) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            uint32_t o[32];
-            tmem_ld32(tO + q * 32, o);
-            tmem_wait_ld();
-            if (vrow) {
+        for (int q = 0; q < 4; ++q) {
+          uint32_t o[32];
+          tmem_ld32(tO + q * 32, o);
+          tmem_wait_ld();
 #pragma unroll
-              for (int k = 0; k < 32; k += 8) {
-                uint4 v;
-                v.x = pack_bf16(__uint_as_float(o[k]) * inv, __uint_as_float(o[k + 1]) * inv);
-                v.y = pack_bf16(__uint_as_float(o[k + 2]) * inv, __uint_as_float(o[k + 3]) * inv);
-                v.z = pack_bf16(__uint_as_float(o[k + 4]) * inv, __uint_as_float(o[k + 5]) * inv);
-                v.w = pack_bf16(__uint_as_float(o[k + 6]) * inv, __uint_as_float(o[k + 7]) * inv);
-                *reinterpret_cast<uint4*>(orow + q * 32 + k) = v;
-              }
-            }
+          for (int k = 0; k < 16; ++k)
+            o[k] = pack_bf16(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
+          if (vrow) {
+            st_global_32(orow + q * 32, o, wide);
+            st_global_32(orow + q * 32 + 16, o + 8, wide);
           }
         }
         tc_fence_before();
@@ -592,7 +572,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const int cta = (int)blockIdx.x;
       const int64_t slot = 2 * (int64_t)cta + (x.t0 == 0);
       const int prow = m * BM + row;
-      if (act && ok) {
+      if (act) {
         float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + prow;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -611,17 +591,16 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       }
       tc_fence_before();
       __threadfence();
-      sync_softmax();
-      const int o0 = walk.owner(x.first), parts = walk.owner(x.first + (int64_t)(x.T - 1) * BN) - o0 + 1;
+      if (!join_softmax()) break;
       if (tid == 0) {
         int l = 0;
         if (!*abort_flag) {
-          l = arrive(A.cnt + o0, A.tag) == parts;
-          if (l) A.cnt[o0] = 0;  // a completed unit leaves a zero word behind
+          l = arrive(A.cnt + x.o0, A.tag) == x.parts;
+          if (l) A.cnt[x.o0] = 0;  // a completed unit leaves a zero word behind
         }
         *last_flag = l;
       }
-      sync_softmax();
+      if (!join_softmax()) break;
       if (*last_flag) {
         __threadfence();
         // rows 0 .. v0 - 1 of M tile 0 and 0 .. v1 - 1 of M tile 1
@@ -640,13 +619,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 #pragma unroll
             for (int j = 0; j < C; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
             float M = -INFINITY, wsum = 0.f;
-            for (int p0 = 0; p0 < parts; p0 += N) {
+            for (int p0 = 0; p0 < x.parts; p0 += N) {
               float w[N];
               float4 o[N][C];
 #pragma unroll
               for (int p = 0; p < N; ++p) {
-                if (p0 + p < parts) {
-                  const int64_t sl = 2 * (int64_t)(o0 + p0 + p) + (p0 + p == 0);
+                if (p0 + p < x.parts) {
+                  const int64_t sl = 2 * (int64_t)(x.o0 + p0 + p) + (p0 + p == 0);
                   w[p] = __ldcg(A.ws_lse + sl * (2 * BM) + at);
 #pragma unroll
                   for (int j = 0; j < C; ++j)
@@ -691,6 +670,92 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         else join(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
       }
     }
+  } else {
+    // ================================================================ scheduler
+    int64_t* start = reinterpret_cast<int64_t*>(smem + kOffPrefix);
+    Walk walk;
+    walk.start = start;
+    walk.B = A.batch;
+    walk.Hkv = A.kv.heads_kv;
+    walk.R = 2 * npb;
+    // Totals first: whether to cut units is chosen by them.  Whole units: as many
+    // rounds of the CTAs as it takes, of the longest unit's time; cut units: an even
+    // share and the merges.
+    auto positions = [&](int b, bool units, int* bad) -> int64_t {  // of sequence b
+      const Seq s = sequence(A, b, bad);
+      const int64_t k = (s.n + walk.R - 1) / walk.R;
+      return walk.Hkv * (units ? k : k * (kUnitCost + s.L) + walk.R * k * (k + 1) / 2);
+    };
+    int64_t units = 0, cost = 0;
+    int longest = 0;
+    for (int b = lane; b < A.batch; b += 32) {
+      int bad;
+      const Seq s = sequence(A, b, &bad);
+      if (bad && blockIdx.x == 0) flag(A.err, bad);
+      if (s.n > 0) longest = max(longest, s.L + s.n);
+      units += positions(b, true, &bad);
+      cost += positions(b, false, &bad);
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+      units += __shfl_xor_sync(0xffffffffu, units, off);
+      cost += __shfl_xor_sync(0xffffffffu, cost, off);
+    }
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    const int64_t rounds = (units + gridDim.x - 1) / gridDim.x;
+    walk.split = rounds * (longest + kUnitCost) > cost / gridDim.x + kMergeCost;
+    int64_t run = 0;
+    for (int base = 0; base < A.batch; base += 32) {
+      const int b = base + lane;
+      int bad;
+      const int64_t own = b < A.batch ? positions(b, !walk.split, &bad) : 0;
+      int64_t upto = own;
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, upto, off);
+        if (lane >= off) upto += y;
+      }
+      if (b < A.batch) start[b] = run + upto - own;
+      run += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    __syncwarp();
+    walk.total = run;
+    // every CTA that takes part in cut units has a tile of each unit that its range lies in
+    walk.P = walk.split ? (int)max((int64_t)1, min((int64_t)gridDim.x, run / kMinShare)) : (int)gridDim.x;
+    uint32_t k = 0;
+    auto put = [&](const Piece& p) -> bool {
+      const uint32_t slot = k % kPieces;
+      if (!wait_warp(bar(B_TAKEN + slot), ((k / kPieces) & 1u) ^ 1u, abort_flag, A.err)) return false;
+      ++k;
+      if (lane == 0) {
+        int4* d = reinterpret_cast<int4*>(smem + kOffPieces + slot * (kPieceInts * 4));
+        const int4* v = reinterpret_cast<const int4*>(&p);
+#pragma unroll
+        for (int i = 0; i < kPieceInts / 4; ++i) d[i] = v[i];
+        mbar_arrive(bar(B_PIECE + slot));
+      }
+      __syncwarp();
+      return true;
+    };
+    const int c = (int)blockIdx.x;
+    bool ok = true;
+    if (!walk.split) {
+      for (int64_t u = c; ok && u < run; u += walk.P) {
+        walk.seek(A, u);
+        ok = put(walk.whole());
+      }
+    } else if (c < walk.P) {
+      const int64_t g = (int64_t)c * run / walk.P, g_end = (int64_t)(c + 1) * run / walk.P;
+      walk.seek(A, g);
+      while (ok) {
+        x = walk.within(g, g_end);
+        if (x.t0 < x.t1) ok = put(x);
+        if (walk.ustart + walk.cost >= g_end) break;
+        walk.advance(A);
+      }
+    }
+    x = Piece{};
+    if (ok) put(x);
   }
 
   tc_fence_before();
