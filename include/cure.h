@@ -385,7 +385,7 @@ cure_status cure_rope_init_freqs(cure_rope* out, int32_t style, int32_t rot_dim,
  *   y = x * w / sqrt(mean(x^2) + eps)   (w = q_norm or k_norm, bf16 [D]; NULL: y = x)
  * then y is rotated to position pos[r] by `rope` (a HOST pointer; NULL: not at
  * all); heads of v are copied.  All in float32, rounded to bf16 once.  Rows with
- * pos[r] < 0 (the padding of cure_build_tree's `pos`) are neither read nor written.
+ * pos[r] < 0 (the padding of cure_build_tree's `pos`) are left out, their outputs unwritten.
  * q [rows][heads_q][D], k and v [rows][heads_kv][D], bf16; row r of a tensor
  * starts ld values after row r - 1 (its heads lie end to end), so that the three
  * may be parts of one projection's rows.  A tensor and its output may both be

@@ -13,13 +13,15 @@
 // (an error of p 2^-65 turns, below 2^-34 at every int32 position); its upper
 // 32 bits go to a float and through sincospif.
 //
-// Layout.  Half a warp holds a head, 8 values (16 bytes) a lane; a warp takes a
-// range of one row's heads, with the row's cosines and sines (times the norm
-// weights) in registers: they are the same for all heads.  In the half layout
-// the partner of a value lies rot_dim / 16 lanes away, in the interleaved
-// layout in the same lane.
+// Layout.  Half a warp holds a head, 8 values a lane, and a warp takes a range of
+// one row's heads with the row's cosines and sines (times the norm weights) in
+// registers: they are the same for all heads.  A lane's 8 values are four whole
+// pairs, so that no lane needs another's: in the half layout two runs of 4 values
+// rot_dim / 2 apart, two 8-byte loads; in the interleaved layout 8 values on end.
+// The arithmetic is on pairs of floats (f32x2).
 #include <cuda_bf16.h>
 
+#include "attn_tc.cuh"
 #include "common.cuh"
 
 namespace cure {
@@ -27,30 +29,54 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kD = 128;
-constexpr int kUnroll = 4;  // loads in flight a lane: heads of one pass of a warp = 2 * kUnroll
+constexpr int kUnroll = 4;  // heads of one step of a warp: 2 * kUnroll, their loads in flight together
 
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 __device__ __forceinline__ float lo_f(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float hi_f(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 
-struct Rows {  // bf16 rows of heads
-  const uint16_t* in;
-  uint16_t* out;
-  int64_t ld_in, ld_out;  // values from row to row
-  int heads;
+struct Raw {  // a lane's values of one head as they lie in memory
+  uint2 a, b;
 };
+// Its four pairs: first and second values, two pairs to a register pair.
+template <bool INTER>
+__device__ __forceinline__ void unpack(const Raw& x, uint64_t (&a)[2], uint64_t (&b)[2]) {
+  if (INTER) {
+    a[0] = tc::f2_pack(lo_f(x.a.x), lo_f(x.a.y));
+    b[0] = tc::f2_pack(hi_f(x.a.x), hi_f(x.a.y));
+    a[1] = tc::f2_pack(lo_f(x.b.x), lo_f(x.b.y));
+    b[1] = tc::f2_pack(hi_f(x.b.x), hi_f(x.b.y));
+  } else {
+    a[0] = tc::f2_pack(lo_f(x.a.x), hi_f(x.a.x));
+    a[1] = tc::f2_pack(lo_f(x.a.y), hi_f(x.a.y));
+    b[0] = tc::f2_pack(lo_f(x.b.x), hi_f(x.b.x));
+    b[1] = tc::f2_pack(lo_f(x.b.y), hi_f(x.b.y));
+  }
+}
+template <bool INTER>
+__device__ __forceinline__ Raw pack(const uint64_t (&a)[2], const uint64_t (&b)[2]) {
+  float a0, a1, a2, a3, b0, b1, b2, b3;
+  tc::f2_unpack(a[0], a0, a1);
+  tc::f2_unpack(a[1], a2, a3);
+  tc::f2_unpack(b[0], b0, b1);
+  tc::f2_unpack(b[1], b2, b3);
+  Raw y;
+  if (INTER) {
+    y.a = make_uint2(tc::pack_bf16(a0, b0), tc::pack_bf16(a1, b1));
+    y.b = make_uint2(tc::pack_bf16(a2, b2), tc::pack_bf16(a3, b3));
+  } else {
+    y.a = make_uint2(tc::pack_bf16(a0, a1), tc::pack_bf16(a2, a3));
+    y.b = make_uint2(tc::pack_bf16(b0, b1), tc::pack_bf16(b2, b3));
+  }
+  return y;
+}
 
-// A lane's 8 dims of a row's rotation: own = cos, other = -sin / +sin, with the
-// norm's weights of the value itself and of its partner.
-struct Turn {
-  float own[8], other[8];
-};
-
-template <bool APPEND>
-__global__ void __launch_bounds__(32 * kWarps)
+template <bool APPEND, bool INTER>
+__global__ void __launch_bounds__(32 * kWarps, 3)
 rope_kernel(const __grid_constant__ RopeArgs A) {
   __shared__ uint64_t turns[64];
   if (threadIdx.x < 64) turns[threadIdx.x] = A.rope.turns[threadIdx.x];
@@ -61,24 +87,61 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
   const int64_t row = item / A.chunks;
   const int chunk = (int)(item % A.chunks);
   if (row >= A.rows) return;
-  int h = chunk * A.chunk_heads;  // this warp's heads of Q, K, V end to end: [h, h_end)
-  const int h_end = min(h + A.chunk_heads, A.heads_q + 2 * A.heads_kv);
+  // this warp's heads of Q, K and V end to end: [h, h_end)
+  const int h = chunk * A.chunk_heads, k0 = A.heads_q, v0 = k0 + A.heads_kv;
+  const int h_end = min(h + A.chunk_heads, v0 + A.heads_kv);
+
+  // where the lane's values lie in a head: with rotated dims left, the pairs 4 l16
+  // .. 4 l16 + 3; the lanes behind them take the dims that are not rotated
+  const int r8 = A.rope.rot_dim >> 3;  // lanes that rotate
+  const bool rot = l16 < r8;
+  const int off_a = INTER ? 8 * l16 : rot ? 4 * l16 : 8 * l16;
+  const int off_b = INTER ? 8 * l16 + 4 : rot ? 4 * l16 + 4 * r8 : 8 * l16 + 4;
+
+  auto load = [&](const uint16_t* in, int a, int b, Raw (&x)[kUnroll]) {  // heads a .. b - 1, at most 2 * kUnroll
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int hh = a + 2 * u + half;
+      x[u].a = x[u].b = make_uint2(0u, 0u);
+      if (hh < b) {
+        x[u].a = *reinterpret_cast<const uint2*>(in + hh * kD + off_a);
+        x[u].b = *reinterpret_cast<const uint2*>(in + hh * kD + off_b);
+      }
+    }
+  };
+  const uint16_t* in_q = A.q ? A.q + row * A.ld_q : nullptr;
+  const uint16_t* in_k = A.k ? A.k + row * A.ld_k : nullptr;
+  const uint16_t* in_v = A.v ? A.v + row * A.ld_v : nullptr;
+  // the first step's loads go out before anything is looked up
+  Raw x[kUnroll];
+  if (h < k0) {
+    if (in_q) load(in_q, h, min(h_end, k0), x);
+  } else if (h < v0) {
+    if (in_k) load(in_k, h - k0, min(h_end, v0) - k0, x);
+  } else if (in_v) {
+    load(in_v, h - v0, h_end - v0, x);
+  }
 
   int p = A.pos ? A.pos[row] : 0;
   if (p < 0) return;  // a row that holds no token
-  int64_t crow = -1;  // APPEND: the row's place in the cache
+  int64_t crow = row;  // the row of K's and V's outputs
   if (APPEND) {
     // the row's sequence: as many of the ends row_start[1..B] are at or before it
     int seq = 0;
-    for (int base = 0; base < A.batch; base += 256) {
-      int e[8];
+    if (A.batch <= 32) {
+      const int e = lane < A.batch ? A.row_start[lane + 1] : INT32_MAX;
+      seq = __popc(__ballot_sync(0xffffffffu, e <= row));
+    } else {
+      for (int base = 0; base < A.batch; base += 256) {
+        int e[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int b = base + 32 * i + lane;
-        e[i] = b < A.batch ? A.row_start[b + 1] : INT32_MAX;
+        for (int i = 0; i < 8; ++i) {
+          const int b = base + 32 * i + lane;
+          e[i] = b < A.batch ? A.row_start[b + 1] : INT32_MAX;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) seq += __popc(__ballot_sync(0xffffffffu, e[i] <= row));
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) seq += __popc(__ballot_sync(0xffffffffu, e[i] <= row));
     }
     if (seq >= A.batch) return;  // behind the last sequence
     const int64_t i = row - A.row_start[seq];
@@ -96,113 +159,115 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
     if (A.kv.layout == 0) {
       crow = (int64_t)seq * A.kv.max_len + slot;
     } else {
-      const int page = A.kv.block_table[(int64_t)seq * A.kv.max_len + slot / A.kv.page_size];
+      const int ps = A.kv.page_size;
+      const int page = A.kv.block_table[(int64_t)seq * A.kv.max_len + (int)slot / ps];
       if (page < 0 || page >= A.kv.num_pages) {
         if (lane == 0) flag(A.err, CURE_DEVERR_PAGE);
         return;
       }
-      crow = (int64_t)page * A.kv.page_size + slot % A.kv.page_size;
+      crow = (int64_t)page * ps + (int)slot % ps;
     }
   }
 
-  // cosines and sines of the lane's dims
-  const int r16 = A.rope.rot_dim >> 4;  // lanes of one half of the rotated dims
-  const bool inter = A.rope.style == 1;
-  const bool rot = l16 < 2 * r16;
-  const bool first = l16 < r16;             // half layout: the lane holds the pairs' first values
-  const int partner = inter || !rot ? lane : first ? lane + r16 : lane - r16;
-  Turn t;
+  // cosines and sines of the lane's pairs: a' = a c + b ms, b' = b c + a s
+  float c[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+  if (rot && h < v0) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    t.own[e] = 1.f;
-    t.other[e] = 0.f;
-  }
-  if (rot && h < A.heads_q + A.heads_kv) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (inter && (e & 1)) {
-        t.own[e] = t.own[e - 1];
-        t.other[e] = -t.other[e - 1];
-        continue;
-      }
-      const int i = inter ? 4 * l16 + e / 2 : 8 * (first ? l16 : l16 - r16) + e;
+    for (int e = 0; e < 4; ++e) {
       // the fraction of a turn in 2^-32, as a signed number of half turns
-      const int32_t f = (int32_t)(uint32_t)(((uint64_t)(uint32_t)p * turns[i]) >> 32);
-      float s, c;
-      sincospif((float)f * 0x1p-31f, &s, &c);
-      t.own[e] = c * A.rope.amplitude;
-      t.other[e] = (inter || first ? -s : s) * A.rope.amplitude;
+      const int32_t f = (int32_t)(uint32_t)(((uint64_t)(uint32_t)p * turns[4 * l16 + e]) >> 32);
+      sincospif((float)f * 0x1p-31f, &sn[e], &c[e]);
+      c[e] *= A.rope.amplitude;
+      sn[e] *= A.rope.amplitude;
     }
   }
 
-  // heads [a, b) of one tensor
-  auto pass = [&](const Rows& R, int a, int b, const uint16_t* norm, bool turn) {
-    if (a >= b) return;
-    const uint16_t* src = R.in + row * R.ld_in + 8 * l16;
-    uint16_t* dst = R.out + row * R.ld_out + 8 * l16;
-    Turn w = t;
-    if (turn && norm) {
-      const uint4 v = *reinterpret_cast<const uint4*>(norm + 8 * l16);
-      const uint4 u = *reinterpret_cast<const uint4*>(norm + 8 * (partner & 15));
-      const uint32_t vv[4] = {v.x, v.y, v.z, v.w}, uu[4] = {u.x, u.y, u.z, u.w};
+  // heads [a, b) of one tensor; `have`: x holds the first step's values
+  auto pass = [&](const uint16_t* in, uint16_t* out, int a, int b, const uint16_t* norm, bool have) {
+    uint64_t ca[2], cb[2], sa[2], sb[2];  // factors of a and b: a' = ca a + sb b, b' = cb b + sa a
+    {
+      float wa[4] = {1.f, 1.f, 1.f, 1.f}, wb[4] = {1.f, 1.f, 1.f, 1.f};
+      if (norm) {
+        Raw w;
+        w.a = *reinterpret_cast<const uint2*>(norm + off_a);
+        w.b = *reinterpret_cast<const uint2*>(norm + off_b);
+        uint64_t pa[2], pb[2];
+        unpack<INTER>(w, pa, pb);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        w.own[2 * q] *= lo_f(vv[q]);
-        w.own[2 * q + 1] *= hi_f(vv[q]);
-        w.other[2 * q] *= inter ? hi_f(uu[q]) : lo_f(uu[q]);
-        w.other[2 * q + 1] *= inter ? lo_f(uu[q]) : hi_f(uu[q]);
+        for (int e = 0; e < 2; ++e) {
+          tc::f2_unpack(pa[e], wa[2 * e], wa[2 * e + 1]);
+          tc::f2_unpack(pb[e], wb[2 * e], wb[2 * e + 1]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        ca[e] = tc::f2_pack(c[2 * e] * wa[2 * e], c[2 * e + 1] * wa[2 * e + 1]);
+        cb[e] = tc::f2_pack(c[2 * e] * wb[2 * e], c[2 * e + 1] * wb[2 * e + 1]);
+        sa[e] = tc::f2_pack(sn[2 * e] * wa[2 * e], sn[2 * e + 1] * wa[2 * e + 1]);
+        sb[e] = tc::f2_pack(-sn[2 * e] * wb[2 * e], -sn[2 * e + 1] * wb[2 * e + 1]);
       }
     }
     for (int h0 = a; h0 < b; h0 += 2 * kUnroll) {
-      uint4 x[kUnroll];
+      if (!have) load(in, h0, b, x);
+      have = false;
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int hh = h0 + 2 * u + half;
-        x[u] = hh < b ? *reinterpret_cast<const uint4*>(src + (int64_t)hh * kD) : make_uint4(0, 0, 0, 0);
-      }
+        uint64_t va[2], vb[2], ya[2], yb[2];
+        unpack<INTER>(x[u], va, vb);
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        const int hh = h0 + 2 * u + half;
-        uint32_t v[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-        if (turn) {
-          float rs = 1.f;
-          if (norm) {
-            float ss = 0.f;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) ss += lo_f(v[q]) * lo_f(v[q]) + hi_f(v[q]) * hi_f(v[q]);
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            rs = rsqrtf(ss * (1.f / kD) + A.eps);
-          }
-          uint32_t g[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            g[q] = __shfl_sync(0xffffffffu, v[q], partner);
-            if (inter) g[q] = __byte_perm(g[q], 0, 0x1032);
-            if (!rot) g[q] = 0u;  // a value without a partner must not meet 0 * infinity
-          }
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const float lo = rs * (lo_f(v[q]) * w.own[2 * q] + lo_f(g[q]) * w.other[2 * q]);
-            const float hi = rs * (hi_f(v[q]) * w.own[2 * q + 1] + hi_f(g[q]) * w.other[2 * q + 1]);
-            v[q] = pack2(lo, hi);
+        for (int e = 0; e < 2; ++e) {
+          ya[e] = f2_mul(va[e], ca[e]);
+          yb[e] = f2_mul(vb[e], cb[e]);
+          if (rot) {  // a value that is not rotated must not meet 0 * infinity
+            ya[e] = tc::f2_fma(vb[e], sb[e], ya[e]);
+            yb[e] = tc::f2_fma(va[e], sa[e], yb[e]);
           }
         }
-        if (hh < b) *reinterpret_cast<uint4*>(dst + (int64_t)hh * kD) = make_uint4(v[0], v[1], v[2], v[3]);
+        if (norm) {
+          uint64_t ss = f2_mul(va[0], va[0]);
+          ss = tc::f2_fma(va[1], va[1], ss);
+          ss = tc::f2_fma(vb[0], vb[0], ss);
+          ss = tc::f2_fma(vb[1], vb[1], ss);
+          float s0, s1;
+          tc::f2_unpack(ss, s0, s1);
+          s0 += s1;
+#pragma unroll
+          for (int o = 8; o > 0; o >>= 1) s0 += __shfl_xor_sync(0xffffffffu, s0, o);
+          const float rs = rsqrtf(s0 * (1.f / kD) + A.eps);
+          const uint64_t rs2 = tc::f2_pack(rs, rs);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            ya[e] = f2_mul(ya[e], rs2);
+            yb[e] = f2_mul(yb[e], rs2);
+          }
+        }
+        if (hh < b) {
+          const Raw y = pack<INTER>(ya, yb);
+          *reinterpret_cast<uint2*>(out + hh * kD + off_a) = y.a;
+          *reinterpret_cast<uint2*>(out + hh * kD + off_b) = y.b;
+        }
       }
     }
   };
-  Rows Q{A.q, A.q_out, A.ld_q, A.ld_q_out, A.heads_q};
-  Rows K{A.k, A.k_out, A.ld_k, A.ld_k_out, A.heads_kv};
-  Rows V{A.v, A.v_out, A.ld_v, A.ld_v_out, A.heads_kv};
-  if (APPEND) {  // K and V rows go to the row's place in the cache
-    K.out += (crow - row) * K.ld_out;
-    V.out += (crow - row) * V.ld_out;
+  if (in_q && h < k0) pass(in_q, A.q_out + row * A.ld_q_out, h, min(h_end, k0), A.q_norm, true);
+  const int ka = max(h, k0) - k0, kb = min(h_end, v0) - k0;
+  if (in_k && ka < kb) pass(in_k, A.k_out + crow * A.ld_k_out, ka, kb, A.k_norm, h >= k0);
+  const int va = max(h, v0) - v0, vb = h_end - v0;
+  if (in_v && va < vb) {
+    uint16_t* out = A.v_out + crow * A.ld_v_out;
+    for (int h0 = va; h0 < vb; h0 += 2 * kUnroll) {
+      if (h0 > va || h < v0) load(in_v, h0, vb, x);
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int hh = h0 + 2 * u + half;
+        if (hh < vb) {
+          *reinterpret_cast<uint2*>(out + hh * kD + off_a) = x[u].a;
+          *reinterpret_cast<uint2*>(out + hh * kD + off_b) = x[u].b;
+        }
+      }
+    }
   }
-  const int k0 = A.heads_q, v0 = k0 + A.heads_kv;
-  if (A.q) pass(Q, h, min(h_end, k0), A.q_norm, true);
-  if (A.k) pass(K, max(h, k0) - k0, min(h_end, v0) - k0, A.k_norm, true);
-  if (A.v) pass(V, max(h, v0) - v0, h_end - v0, nullptr, false);
 }
 
 }  // namespace
@@ -210,10 +275,20 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
 cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s) {
   RopeArgs a = args;
   const int heads = a.heads_q + 2 * a.heads_kv;
+  // Few rows: a row's heads in parts of one step's heads, so that a row is over after
+  // one round of loads; many: a warp a row, so that its angles serve all heads.
+  const int64_t resident = (int64_t)num_sms() * 3 * kWarps;
   a.chunk_heads = heads;
-  a.chunks = 1;
+  for (int n = 2 * kUnroll; n < heads; n *= 2)
+    if (a.rows * (int64_t)((heads + n - 1) / n) <= resident) {
+      a.chunk_heads = n;
+      break;
+    }
+  a.chunks = (heads + a.chunk_heads - 1) / a.chunk_heads;
   const int64_t blocks = ((int64_t)a.rows * a.chunks + kWarps - 1) / kWarps;
-  return launch_pdl(append ? rope_kernel<true> : rope_kernel<false>, dim3((unsigned)blocks), dim3(32 * kWarps), 0, s, a);
+  auto kernel = a.rope.style == 1 ? (append ? rope_kernel<true, true> : rope_kernel<false, true>)
+                                  : (append ? rope_kernel<true, false> : rope_kernel<false, false>);
+  return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kWarps), 0, s, a);
 }
 
 }  // namespace cure

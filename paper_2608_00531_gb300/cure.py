@@ -342,51 +342,67 @@ def rope_desc(rot_dim: int = 128, base: float = 10000.0, *, style: str = "half",
     return r
 
 
-def _here(t: Optional[torch.Tensor], name: str, dtype=None) -> Optional[int]:
-    """_p() of a tensor that must also be on the current device, and of a type where one is given."""
+def _here(t: Optional[torch.Tensor], name: str, dtype, dev: int) -> Optional[int]:
+    """_p() of a tensor that must also be on device `dev` and of a type."""
     if t is None:
         return None
-    if dtype is not None:
-        _need(t, dtype, name)
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != dev:
         raise ValueError(f"{name} must be on the current CUDA device")
-    return _p(t)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _new(shape, dtype, stream) -> torch.Tensor:
     """A tensor that the call fills on `stream`: allocated there, so that its memory is not in use on another."""
     if stream is None:
         return torch.empty(shape, dtype=dtype, device="cuda")
-    if stream.device_index != torch.cuda.current_device():
-        raise ValueError("stream must be on the current CUDA device")
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device="cuda")
 
 
-def _head_rows(t: Optional[torch.Tensor], name: str):
-    """(address, values from row to row, rows, heads) of bf16 [...][heads][D]: heads end to end, the
+def _current(stream) -> tuple[int, int]:
+    """The current device, and the handle of `stream` (None: the current one), which must be on it."""
+    dev = torch.cuda.current_device()
+    if stream is None:
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
+    if stream.device_index != dev:
+        raise ValueError("stream must be on the current CUDA device")
+    return dev, stream.cuda_stream
+
+
+def _head_rows(t: torch.Tensor, name: str, dev: int):
+    """(address, values from row to row, (rows, heads, head_dim)) of bf16 [...][heads][D]: heads end to end, the
     leading dimensions one even step apart, as in a part of a fused projection's rows."""
-    if t is None:
-        return None, 0, 0, 0
-    _need(t, torch.bfloat16, name)
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
+    if t.get_device() != dev:
         raise ValueError(f"{name} must be on the current CUDA device")
-    sh, st = t.shape, t.stride()
-    if len(sh) < 2:
-        raise ValueError(f"{name} must be [...][heads][head_dim]")
-    H, D = sh[-2], sh[-1]
-    ld, rows, outer = H * D, 1, None
-    for n, step in zip(reversed(sh[:-2]), reversed(st[:-2])):
-        if n != 1:
-            if outer is None:
-                ld = step
-            elif step != outer:
-                raise ValueError(f"{name}: rows must lie one even step apart")
-            outer = step * n
-        rows *= n
-    if rows and H and D and ((D > 1 and st[-1] != 1) or (H > 1 and st[-2] != D)):
+    sh = t.shape
+    if len(sh) == 3:
+        rows, H, D = sh
+    elif len(sh) == 4:
+        outer, inner, H, D = sh
+        rows = outer * inner
+    else:
+        raise ValueError(f"{name} must be [rows][heads][head_dim] or [batch][rows][heads][head_dim]")
+    if rows <= 1 or t.is_contiguous():
+        ld = H * D
+        if rows == 0 or t.is_contiguous():
+            return t.data_ptr(), ld, (rows, H, D)
+    st = t.stride()
+    if rows > 1:
+        ld = st[-3] if len(sh) == 3 or inner > 1 else st[0]
+        if len(sh) == 4 and outer > 1 and inner > 1 and st[0] != inner * ld:
+            raise ValueError(f"{name}: rows must lie one even step apart")
+    if (D > 1 and st[-1] != 1) or (H > 1 and st[-2] != D):
         raise ValueError(f"{name}: a row's heads must lie end to end")
-    return t.data_ptr(), ld, rows, H
+    return t.data_ptr(), ld, (rows, H, D)
+
+
+_NO_ROWS = (None, 0, (0, 0, 0))
 
 
 def cure_rope_qkv(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor],
@@ -395,41 +411,50 @@ def cure_rope_qkv(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optio
     """Per-head norms and the rotation of q and k at the rows' positions, v copied: (q, k, v) as cure_tree_attn
     takes them, from (parts of) the rows of a fused projection.
 
-    q bf16 [...][heads_q][D], k and v [...][heads_kv][D]; pos int32, one per row (the tree's ``pos``): rows with
-    pos < 0 are left out.  rope = None: no rotation.  Any of q, k, v may be None, and its output with it."""
-    ins = [_head_rows(t, nm) for t, nm in ((q, "q"), (k, "k"), (v, "v"))]
+    q bf16 [rows][heads_q][D] or [batch][rows][heads_q][D], k and v the same with heads_kv; pos int32, one per row
+    (the tree's ``pos``): rows with pos < 0 are left out.  rope = None: no rotation.  Any of q, k, v may be None, and
+    its output with it."""
+    dev, s = _current(stream)
     if out is None:
         out = tuple(None if t is None else _new(t.shape, t.dtype, stream) for t in (q, k, v))
-    outs = [_head_rows(t, nm) for t, nm in zip(out, ("q's output", "k's output", "v's output"))]
     rows = pos.numel()
-    for i, o, t, nm in zip(ins, outs, (q, k, v), "qkv"):
-        if i[2:] != o[2:] or (t is not None and i[2] != rows):
+    heads, args, D = [0, 0, 0], [], 128
+    for i, (t, o, nm) in enumerate(zip((q, k, v), out, "qkv")):
+        if t is None or o is None:
+            if t is not o:
+                raise ValueError(f"cure_rope_qkv: {nm} without its output, or an output without {nm}")
+            args.append((None, 0, None, 0))
+            continue
+        pi, li, shape = _head_rows(t, nm, dev)
+        po, lo, shape_o = _head_rows(o, "an output", dev)
+        if shape != shape_o or shape[0] != rows:
             raise ValueError(f"cure_rope_qkv: {nm}, its output and pos must have the same rows and heads")
-    if k is not None and v is not None and ins[1][3] != ins[2][3]:
+        heads[i], D = shape[1], shape[2]
+        args.append((pi, li, po, lo))
+    (pq, lq, oq, loq), (pk, lk, ok, lok), (pv, lv, ov, lov) = args
+    if pk is not None and pv is not None and heads[1] != heads[2]:
         raise ValueError("cure_rope_qkv: k and v must have the same heads")
-    D = {t.shape[-1] for t in (q, k, v, *out) if t is not None}
-    if len(D) > 1:
-        raise ValueError("cure_rope_qkv: one head_dim")
+    if any(t is not None and t.shape[-1] != D for t in (q, k, v)):
+        raise ValueError("cure_rope_qkv: q, k and v must have one head_dim")
     check("cure_rope_qkv", _lib.load().cure_rope_qkv(
-        ins[0][0], ins[1][0], ins[2][0], ins[0][1], ins[1][1], ins[2][1], rows, ins[0][3], max(ins[1][3], ins[2][3]),
-        D.pop() if D else 128, _here(pos, "pos", torch.int32), None if rope is None else C.byref(rope),
-        _norm(q_norm, "q_norm"), _norm(k_norm, "k_norm"), float(eps), outs[0][0], outs[1][0], outs[2][0],
-        outs[0][1], outs[1][1], outs[2][1], _stream(stream)))
+        pq, pk, pv, lq, lk, lv, rows, heads[0], heads[1] or heads[2], D, _here(pos, "pos", torch.int32, dev),
+        None if rope is None else C.byref(rope), _norm(q_norm, "q_norm", dev), _norm(k_norm, "k_norm", dev), eps,
+        oq, ok, ov, loq, lok, lov, s))
     return out
 
 
-def _norm(w: Optional[torch.Tensor], name: str) -> Optional[int]:
+def _norm(w: Optional[torch.Tensor], name: str, dev: int) -> Optional[int]:
     if w is not None and w.numel() != 128:
         raise ValueError(f"{name} must hold one weight for each of a head's 128 values")
-    return _here(w, name, torch.bfloat16)
+    return _here(w, name, torch.bfloat16, dev)
 
 
-def _cache_fits(t: torch.Tensor, kv: KVDesc, batch: int, name: str) -> int:
+def _cache_fits(t: torch.Tensor, kv: KVDesc, batch: int, name: str, dev: int) -> int:
     """_here() of a cache that holds what its geometry says."""
     rows = batch * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size
     if t.numel() < rows * kv.heads_kv * kv.head_dim:
         raise ValueError(f"{name} is smaller than its geometry")
-    return _here(t, name, torch.bfloat16)
+    return _here(t, name, torch.bfloat16, dev)
 
 
 def _ragged(row_start: torch.Tensor, cache_len: torch.Tensor, kv: KVDesc) -> int:
@@ -453,25 +478,30 @@ def cure_append_kv(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
 
     A row's position is its slot, or its entry of ``pos`` (int32; < 0 leaves the row out).  cache_len is not
     advanced.  In-place tree rows: row_start = 0, n_max, 2 n_max, .., pos = the tree's ``pos``."""
+    dev, s = _current(stream)
     B = _ragged(row_start, cache_len, kv)
-    (pq, lq, nq, hq), (pk, lk, nk, hk), (pv, lv, nv, hv) = (
-        _head_rows(t, nm) for t, nm in ((q, "q"), (k, "k"), (v, "v")))
+    pk, lk, shape = _head_rows(k, "k", dev)
+    pv, lv, shape_v = _head_rows(v, "v", dev)
+    rows = shape[0]
+    if shape != shape_v or shape[1] != kv.heads_kv or shape[2] != kv.head_dim:
+        raise ValueError("cure_append_kv: k and v must have the same rows, the cache's heads and its head_dim")
     if q is None:
-        out = None
-    elif out is None:
-        out = _new(q.shape, q.dtype, stream)
-    po, lo, no, ho = _head_rows(out, "out")
-    if nk != nv or hk != kv.heads_kv or hv != kv.heads_kv or (q is not None and (nq != nk or (no, ho) != (nq, hq))) or (
-            pos is not None and pos.numel() != nk):
-        raise ValueError("cure_append_kv: q, k, v, out and pos must have the same rows, k and v the cache's heads")
-    if any(t is not None and t.shape[-1] != kv.head_dim for t in (q, k, v, out)):
-        raise ValueError("cure_append_kv: heads must have the cache's head_dim")
+        out, (pq, lq, shape_q), (po, lo, _) = None, _NO_ROWS, _NO_ROWS
+    else:
+        if out is None:
+            out = _new(q.shape, q.dtype, stream)
+        pq, lq, shape_q = _head_rows(q, "q", dev)
+        po, lo, shape_o = _head_rows(out, "out", dev)
+        if shape_q != shape_o or shape_q[0] != rows or shape_q[2] != kv.head_dim:
+            raise ValueError("cure_append_kv: q, its output and k must have the same rows and head_dim")
+    if pos is not None and pos.numel() != rows:
+        raise ValueError("cure_append_kv: pos must have an entry for every row")
     check("cure_append_kv", _lib.load().cure_append_kv(
-        pq, pk, pv, lq, lk, lv, nk, hq, B, _here(row_start, "row_start", torch.int32),
-        _here(cache_len, "cache_len", torch.int32), _here(pos, "pos", torch.int32), C.byref(kv),
-        _cache_fits(k_cache, kv, B, "k_cache"), _cache_fits(v_cache, kv, B, "v_cache"),
-        None if rope is None else C.byref(rope), _norm(q_norm, "q_norm"), _norm(k_norm, "k_norm"), float(eps), po, lo,
-        _stream(stream)))
+        pq, pk, pv, lq, lk, lv, rows, shape_q[1], B, _here(row_start, "row_start", torch.int32, dev),
+        _here(cache_len, "cache_len", torch.int32, dev), _here(pos, "pos", torch.int32, dev), C.byref(kv),
+        _cache_fits(k_cache, kv, B, "k_cache", dev), _cache_fits(v_cache, kv, B, "v_cache", dev),
+        None if rope is None else C.byref(rope), _norm(q_norm, "q_norm", dev), _norm(k_norm, "k_norm", dev), eps, po,
+        lo, s))
     return out
 
 
@@ -487,22 +517,23 @@ def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
 
     q bf16 [rows][heads_q][D]; sequence b's rows row_start[b] .. row_start[b+1] - 1 stand at positions cache_len[b],
     cache_len[b] + 1, .., and their K and V are in the cache already (cure_append_kv at the same lengths)."""
-    _need(q, torch.bfloat16, "q")
+    dev, s = _current(stream)
     B = _ragged(row_start, cache_len, kv)
-    if q.dim() != 3 or q.shape[2] != kv.head_dim:
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != kv.head_dim:
         raise ValueError("q must be [rows][heads_q][head_dim]")
-    rows, Hq, _ = q.shape
     if out is None:
-        out = _new(q.shape, q.dtype, stream)
-    elif out.shape != q.shape:
+        out = _new(shape, torch.bfloat16, stream)
+    elif out.shape != shape:
         raise ValueError("out must have q's shape")
     if workspace is None:
-        workspace = _new((max(cure_prompt_attn_workspace_size(rows, B, Hq, kv), 256),), torch.uint8, stream)
+        size = cure_prompt_attn_workspace_size(shape[0], B, shape[1], kv)
+        workspace = _new((max(size, 256),), torch.uint8, stream)
     check("cure_prompt_attn", _lib.load().cure_prompt_attn(
-        _here(q, "q"), _cache_fits(k_cache, kv, B, "k_cache"), _cache_fits(v_cache, kv, B, "v_cache"), C.byref(kv),
-        _here(row_start, "row_start", torch.int32), _here(cache_len, "cache_len", torch.int32), rows, B, Hq,
-        float(scale), _here(out, "out", torch.bfloat16), _here(workspace, "workspace"),
-        workspace.numel() * workspace.element_size(), _stream(stream)))
+        _here(q, "q", torch.bfloat16, dev), _cache_fits(k_cache, kv, B, "k_cache", dev),
+        _cache_fits(v_cache, kv, B, "v_cache", dev), C.byref(kv), _here(row_start, "row_start", torch.int32, dev),
+        _here(cache_len, "cache_len", torch.int32, dev), shape[0], B, shape[1], scale,
+        _here(out, "out", torch.bfloat16, dev), _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s))
     return out
 
 
