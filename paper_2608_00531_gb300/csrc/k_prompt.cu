@@ -306,129 +306,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   // M tile 1 of a piece is active when its first row is one of the sequence's
   auto active1 = [&](const Piece& x) { return (2 * x.rg + 1) * npb < x.n; };
 
-  if (warp == 8) {
-    // ================================================================ producer
-    const int ps = A.kv.page_size;
-    const int ppt = A.kv.layout == 1 ? BN / ps : 0;  // pages (boxes) of a tile: 2 .. 16
-    const uint32_t qbytes = (uint32_t)(npb * G * 128);
-    uint32_t qc = 0, issued = 0;  // pieces, ring tiles
-    bool ok = true;
-    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
-      auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
-        const int tok = t * BN + lane * ps;
-        if (lane >= ppt || tok >= x.keys) return -1;
-        const int page = A.kv.block_table[(int64_t)x.b * A.kv.max_len + tok / ps];
-        if (page < 0 || page >= A.kv.num_pages) {
-          flag(A.err, CURE_DEVERR_PAGE);
-          return -1;
-        }
-        return page;
-      };
-      int page = ppt > 0 ? page_of(x.t0) : -1;
-      for (int t = x.t0; ok && t < x.t1; ++t) {
-        const int next = ppt > 0 && t + 1 < x.t1 ? page_of(t + 1) : -1;
-        for (int kv = 0; kv < 2; ++kv) {  // the K tile, then the V tile
-          const int st = (int)(issued % NS);
-          if (!wait_warp(bar(B_EMPTY + st), ((issued / NS) & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
-          const uint32_t full = bar(B_FULL + st), dst = sb + kOffRing + st * kTile;
-          if (lane == 0) mbar_arrive_expect_tx(full, kTile);
-          __syncwarp();
-          if (A.kv.layout == 1) {
-            if (lane < ppt) tma_load_5d(dst + lane * ps * 256, kv ? &tm_v : &tm_k, full, 0, 0, 2 * x.h, 0, page);
-          } else if (kv == 0) {
-            if (lane < 2) tma_load_3d(dst + lane * kKHalf, &tm_k, full, lane * 64, x.h, x.b * A.kv.max_len + t * BN);
-          } else if (lane < BN / 16) {
-            tma_load_4d(dst + lane * kVChunk, &tm_v, full, 0, x.b * A.kv.max_len + t * BN + 16 * lane, 0, x.h);
-          }
-          __syncwarp();
-          ++issued;
-          if (t == x.t0 && kv == 0) {  // Q of both M tiles once the previous piece's S products are done
-            if (!wait_warp(bar(B_QEMPTY), (qc & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
-            ++qc;
-            if (lane == 0) mbar_arrive_expect_tx(bar(B_QFULL), 4 * qbytes);
-            __syncwarp();
-            if (lane < 4)  // M tile lane / 2, d half lane % 2
-              tma_load_4d(sb + kOffQ + lane * kQHalf, &tm_q, bar(B_QFULL), (lane & 1) * 64, 0, x.h,
-                          x.r0 + (2 * x.rg + (lane >> 1)) * npb);
-            __syncwarp();
-          }
-        }
-        page = next;
-      }
-    }
-    if (*abort_flag) {  // let copies in flight land before the CTA's smem goes away
-      for (uint32_t i = (issued > NS ? issued - NS : 0); i < issued; ++i)
-        wait_bounded(bar(B_FULL + i % NS), (i / NS) & 1u, abort_flag, A.err, false);
-      if (qc > 0) wait_bounded(bar(B_QFULL), (qc - 1) & 1u, abort_flag, A.err, false);
-    }
-  } else if (warp == 9) {
-    // ================================================================ S products
-    constexpr uint32_t idS = idesc_bf16_f32(BM, BN, false);
-    const bool paged = A.kv.layout == 1;
-    uint32_t qc = 0, r = 0, c = 0;  // pieces, ring tiles, products
-    bool ok = true;
-    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
-      if (!wait_warp(bar(B_QFULL), qc & 1u, abort_flag, A.err)) break;
-      ++qc;
-      const int mts = active1(x) ? 2 : 1;
-      for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
-        const uint32_t sk = r % NS;
-        const uint32_t ka = sb + kOffRing + sk * kTile;
-        const uint32_t sbo = paged ? kPgGroup : 1024u, kh = paged ? kPgHalf : kKHalf;
-        for (int m = 0; m < mts; ++m) {
-          if (c > 0 && !wait_warp(bar(B_SFREE), (c - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
-          ++c;
-          // The K tile, after SFREE: a parity wait is sound from the phase before on and
-          // not later, and the stage's tile before this one, V of three tiles before, has
-          // landed when the softmax of M tile 0 has loaded S of the tile before (it then
-          // has seen the PV product of that V tile done).
-          if (m == 0 && !wait_warp(bar(B_FULL + sk), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
-          tc_fence_after();
-          mma_s_group(tmem + kColS, sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024), sdesc_sw128(ka, 16, sbo),
-                      sdesc_sw128(ka + kh, 16, sbo), idS);
-          commit_elect(bar(B_SFULL + m));
-        }
-        if (!ok) break;
-        commit_elect(bar(B_EMPTY + sk));
-        if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
-      }
-    }
-    __syncwarp();
-    commit_elect(bar(B_DRAIN));
-    wait_bounded(bar(B_DRAIN), 0, abort_flag, A.err, false);
-  } else if (warp == 10) {
-    // ================================================================ PV products
-    constexpr uint32_t idO = idesc_bf16_f32(BM, D, true);
-    const bool paged = A.kv.layout == 1;
-    uint32_t r = 1, c[2] = {0, 0};  // ring tiles, products of each M tile
-    bool ok = true;
-    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
-      const int mts = active1(x) ? 2 : 1;
-      for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
-        const uint32_t sv = r % NS;
-        // (the stage's K tile of two tiles before has landed: its S became the P that this
-        // warp has waited for)
-        if (!wait_warp(bar(B_FULL + sv), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
-        // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
-        const uint64_t vd = sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-          if (m >= mts) break;
-          if (!wait_warp(bar(B_PFULL + m), c[m] & 1u, abort_flag, A.err)) { ok = false; break; }
-          ++c[m];
-          tc_fence_after();
-          mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0 ? 1u : 0u);
-          mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64 + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
-          commit_elect(bar(B_PVDONE + m));
-        }
-        if (!ok) break;
-        commit_elect(bar(B_EMPTY + sv));
-      }
-    }
-    __syncwarp();
-    commit_elect(bar(B_DRAIN + 1));
-    wait_bounded(bar(B_DRAIN + 1), 0, abort_flag, A.err, false);
-  } else if (warp < 8) {
+  // The softmax warps hold a row of S each: they get registers from the other four
+  // warps (2 * 128 * 208 + 128 * 88 = 384 * 168, what the block was launched with).
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ================================================================ softmax
     const int m = warp >> 2;
     const int row = tid & 127;  // row within the M tile = TMEM lane
@@ -671,91 +552,216 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       }
     }
   } else {
-    // ================================================================ scheduler
-    int64_t* start = reinterpret_cast<int64_t*>(smem + kOffPrefix);
-    Walk walk;
-    walk.start = start;
-    walk.B = A.batch;
-    walk.Hkv = A.kv.heads_kv;
-    walk.R = 2 * npb;
-    // Totals first: whether to cut units is chosen by them.  Whole units: as many
-    // rounds of the CTAs as it takes, of the longest unit's time; cut units: an even
-    // share and the merges.
-    auto positions = [&](int b, bool units, int* bad) -> int64_t {  // of sequence b
-      const Seq s = sequence(A, b, bad);
-      const int64_t k = (s.n + walk.R - 1) / walk.R;
-      return walk.Hkv * (units ? k : k * (kUnitCost + s.L) + walk.R * k * (k + 1) / 2);
-    };
-    int64_t units = 0, cost = 0;
-    int longest = 0;
-    for (int b = lane; b < A.batch; b += 32) {
-      int bad;
-      const Seq s = sequence(A, b, &bad);
-      if (bad && blockIdx.x == 0) flag(A.err, bad);
-      if (s.n > 0) longest = max(longest, s.L + s.n);
-      units += positions(b, true, &bad);
-      cost += positions(b, false, &bad);
-    }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-      units += __shfl_xor_sync(0xffffffffu, units, off);
-      cost += __shfl_xor_sync(0xffffffffu, cost, off);
-    }
-    longest = __reduce_max_sync(0xffffffffu, longest);
-    const int64_t rounds = (units + gridDim.x - 1) / gridDim.x;
-    walk.split = rounds * (longest + kUnitCost) > cost / gridDim.x + kMergeCost;
-    int64_t run = 0;
-    for (int base = 0; base < A.batch; base += 32) {
-      const int b = base + lane;
-      int bad;
-      const int64_t own = b < A.batch ? positions(b, !walk.split, &bad) : 0;
-      int64_t upto = own;
-#pragma unroll
-      for (int off = 1; off < 32; off <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, upto, off);
-        if (lane >= off) upto += y;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == 8) {
+      // ================================================================ producer
+      const int ps = A.kv.page_size;
+      const int ppt = A.kv.layout == 1 ? BN / ps : 0;  // pages (boxes) of a tile: 2 .. 16
+      const uint32_t qbytes = (uint32_t)(npb * G * 128);
+      uint32_t qc = 0, issued = 0;  // pieces, ring tiles
+      bool ok = true;
+      while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
+        auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
+          const int tok = t * BN + lane * ps;
+          if (lane >= ppt || tok >= x.keys) return -1;
+          const int page = A.kv.block_table[(int64_t)x.b * A.kv.max_len + tok / ps];
+          if (page < 0 || page >= A.kv.num_pages) {
+            flag(A.err, CURE_DEVERR_PAGE);
+            return -1;
+          }
+          return page;
+        };
+        int page = ppt > 0 ? page_of(x.t0) : -1;
+        for (int t = x.t0; ok && t < x.t1; ++t) {
+          const int next = ppt > 0 && t + 1 < x.t1 ? page_of(t + 1) : -1;
+          for (int kv = 0; kv < 2; ++kv) {  // the K tile, then the V tile
+            const int st = (int)(issued % NS);
+            if (!wait_warp(bar(B_EMPTY + st), ((issued / NS) & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
+            const uint32_t full = bar(B_FULL + st), dst = sb + kOffRing + st * kTile;
+            if (lane == 0) mbar_arrive_expect_tx(full, kTile);
+            __syncwarp();
+            if (A.kv.layout == 1) {
+              if (lane < ppt) tma_load_5d(dst + lane * ps * 256, kv ? &tm_v : &tm_k, full, 0, 0, 2 * x.h, 0, page);
+            } else if (kv == 0) {
+              if (lane < 2) tma_load_3d(dst + lane * kKHalf, &tm_k, full, lane * 64, x.h, x.b * A.kv.max_len + t * BN);
+            } else if (lane < BN / 16) {
+              tma_load_4d(dst + lane * kVChunk, &tm_v, full, 0, x.b * A.kv.max_len + t * BN + 16 * lane, 0, x.h);
+            }
+            __syncwarp();
+            ++issued;
+            if (t == x.t0 && kv == 0) {  // Q of both M tiles once the previous piece's S products are done
+              if (!wait_warp(bar(B_QEMPTY), (qc & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
+              ++qc;
+              if (lane == 0) mbar_arrive_expect_tx(bar(B_QFULL), 4 * qbytes);
+              __syncwarp();
+              if (lane < 4)  // M tile lane / 2, d half lane % 2
+                tma_load_4d(sb + kOffQ + lane * kQHalf, &tm_q, bar(B_QFULL), (lane & 1) * 64, 0, x.h,
+                            x.r0 + (2 * x.rg + (lane >> 1)) * npb);
+              __syncwarp();
+            }
+          }
+          page = next;
+        }
       }
-      if (b < A.batch) start[b] = run + upto - own;
-      run += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    __syncwarp();
-    walk.total = run;
-    // every CTA that takes part in cut units has a tile of each unit that its range lies in
-    walk.P = walk.split ? (int)max((int64_t)1, min((int64_t)gridDim.x, run / kMinShare)) : (int)gridDim.x;
-    uint32_t k = 0;
-    auto put = [&](const Piece& p) -> bool {
-      const uint32_t slot = k % kPieces;
-      if (!wait_warp(bar(B_TAKEN + slot), ((k / kPieces) & 1u) ^ 1u, abort_flag, A.err)) return false;
-      ++k;
-      if (lane == 0) {
-        int4* d = reinterpret_cast<int4*>(smem + kOffPieces + slot * (kPieceInts * 4));
-        const int4* v = reinterpret_cast<const int4*>(&p);
-#pragma unroll
-        for (int i = 0; i < kPieceInts / 4; ++i) d[i] = v[i];
-        mbar_arrive(bar(B_PIECE + slot));
+      if (*abort_flag) {  // let copies in flight land before the CTA's smem goes away
+        for (uint32_t i = (issued > NS ? issued - NS : 0); i < issued; ++i)
+          wait_bounded(bar(B_FULL + i % NS), (i / NS) & 1u, abort_flag, A.err, false);
+        if (qc > 0) wait_bounded(bar(B_QFULL), (qc - 1) & 1u, abort_flag, A.err, false);
+      }
+    } else if (warp == 9) {
+      // ================================================================ S products
+      constexpr uint32_t idS = idesc_bf16_f32(BM, BN, false);
+      const bool paged = A.kv.layout == 1;
+      uint32_t qc = 0, r = 0, c = 0;  // pieces, ring tiles, products
+      bool ok = true;
+      while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
+        if (!wait_warp(bar(B_QFULL), qc & 1u, abort_flag, A.err)) break;
+        ++qc;
+        const int mts = active1(x) ? 2 : 1;
+        for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
+          const uint32_t sk = r % NS;
+          const uint32_t ka = sb + kOffRing + sk * kTile;
+          const uint32_t sbo = paged ? kPgGroup : 1024u, kh = paged ? kPgHalf : kKHalf;
+          for (int m = 0; m < mts; ++m) {
+            if (c > 0 && !wait_warp(bar(B_SFREE), (c - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
+            ++c;
+            // The K tile, after SFREE: a parity wait is sound from the phase before on and
+            // not later, and the stage's tile before this one, V of three tiles before, has
+            // landed when the softmax of M tile 0 has loaded S of the tile before (it then
+            // has seen the PV product of that V tile done).
+            if (m == 0 && !wait_warp(bar(B_FULL + sk), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+            tc_fence_after();
+            mma_s_group(tmem + kColS, sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024), sdesc_sw128(ka, 16, sbo),
+                        sdesc_sw128(ka + kh, 16, sbo), idS);
+            commit_elect(bar(B_SFULL + m));
+          }
+          if (!ok) break;
+          commit_elect(bar(B_EMPTY + sk));
+          if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
+        }
       }
       __syncwarp();
-      return true;
-    };
-    const int c = (int)blockIdx.x;
-    bool ok = true;
-    if (!walk.split) {
-      for (int64_t u = c; ok && u < run; u += walk.P) {
-        walk.seek(A, u);
-        ok = put(walk.whole());
+      commit_elect(bar(B_DRAIN));
+      wait_bounded(bar(B_DRAIN), 0, abort_flag, A.err, false);
+    } else if (warp == 10) {
+      // ================================================================ PV products
+      constexpr uint32_t idO = idesc_bf16_f32(BM, D, true);
+      const bool paged = A.kv.layout == 1;
+      uint32_t r = 1, c[2] = {0, 0};  // ring tiles, products of each M tile
+      bool ok = true;
+      while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
+        const int mts = active1(x) ? 2 : 1;
+        for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
+          const uint32_t sv = r % NS;
+          // (the stage's K tile of two tiles before has landed: its S became the P that this
+          // warp has waited for)
+          if (!wait_warp(bar(B_FULL + sv), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+          // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
+          const uint64_t vd = sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            if (m >= mts) break;
+            if (!wait_warp(bar(B_PFULL + m), c[m] & 1u, abort_flag, A.err)) { ok = false; break; }
+            ++c[m];
+            tc_fence_after();
+            mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0 ? 1u : 0u);
+            mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64 + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
+            commit_elect(bar(B_PVDONE + m));
+          }
+          if (!ok) break;
+          commit_elect(bar(B_EMPTY + sv));
+        }
       }
-    } else if (c < walk.P) {
-      const int64_t g = (int64_t)c * run / walk.P, g_end = (int64_t)(c + 1) * run / walk.P;
-      walk.seek(A, g);
-      while (ok) {
-        x = walk.within(g, g_end);
-        if (x.t0 < x.t1) ok = put(x);
-        if (walk.ustart + walk.cost >= g_end) break;
-        walk.advance(A);
+      __syncwarp();
+      commit_elect(bar(B_DRAIN + 1));
+      wait_bounded(bar(B_DRAIN + 1), 0, abort_flag, A.err, false);
+    } else {
+      // ================================================================ scheduler
+      int64_t* start = reinterpret_cast<int64_t*>(smem + kOffPrefix);
+      Walk walk;
+      walk.start = start;
+      walk.B = A.batch;
+      walk.Hkv = A.kv.heads_kv;
+      walk.R = 2 * npb;
+      // Totals first: whether to cut units is chosen by them.  Whole units: as many
+      // rounds of the CTAs as it takes, of the longest unit's time; cut units: an even
+      // share and the merges.
+      auto positions = [&](int b, bool units, int* bad) -> int64_t {  // of sequence b
+        const Seq s = sequence(A, b, bad);
+        const int64_t k = (s.n + walk.R - 1) / walk.R;
+        return walk.Hkv * (units ? k : k * (kUnitCost + s.L) + walk.R * k * (k + 1) / 2);
+      };
+      int64_t units = 0, cost = 0;
+      int longest = 0;
+      for (int b = lane; b < A.batch; b += 32) {
+        int bad;
+        const Seq s = sequence(A, b, &bad);
+        if (bad && blockIdx.x == 0) flag(A.err, bad);
+        if (s.n > 0) longest = max(longest, s.L + s.n);
+        units += positions(b, true, &bad);
+        cost += positions(b, false, &bad);
       }
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) {
+        units += __shfl_xor_sync(0xffffffffu, units, off);
+        cost += __shfl_xor_sync(0xffffffffu, cost, off);
+      }
+      longest = __reduce_max_sync(0xffffffffu, longest);
+      const int64_t rounds = (units + gridDim.x - 1) / gridDim.x;
+      walk.split = rounds * (longest + kUnitCost) > cost / gridDim.x + kMergeCost;
+      int64_t run = 0;
+      for (int base = 0; base < A.batch; base += 32) {
+        const int b = base + lane;
+        int bad;
+        const int64_t own = b < A.batch ? positions(b, !walk.split, &bad) : 0;
+        int64_t upto = own;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int64_t y = __shfl_up_sync(0xffffffffu, upto, off);
+          if (lane >= off) upto += y;
+        }
+        if (b < A.batch) start[b] = run + upto - own;
+        run += __shfl_sync(0xffffffffu, upto, 31);
+      }
+      __syncwarp();
+      walk.total = run;
+      // every CTA that takes part in cut units has a tile of each unit that its range lies in
+      walk.P = walk.split ? (int)max((int64_t)1, min((int64_t)gridDim.x, run / kMinShare)) : (int)gridDim.x;
+      uint32_t k = 0;
+      auto put = [&](const Piece& p) -> bool {
+        const uint32_t slot = k % kPieces;
+        if (!wait_warp(bar(B_TAKEN + slot), ((k / kPieces) & 1u) ^ 1u, abort_flag, A.err)) return false;
+        ++k;
+        if (lane == 0) {
+          int4* d = reinterpret_cast<int4*>(smem + kOffPieces + slot * (kPieceInts * 4));
+          const int4* v = reinterpret_cast<const int4*>(&p);
+#pragma unroll
+          for (int i = 0; i < kPieceInts / 4; ++i) d[i] = v[i];
+          mbar_arrive(bar(B_PIECE + slot));
+        }
+        __syncwarp();
+        return true;
+      };
+      const int c = (int)blockIdx.x;
+      bool ok = true;
+      if (!walk.split) {
+        for (int64_t u = c; ok && u < run; u += walk.P) {
+          walk.seek(A, u);
+          ok = put(walk.whole());
+        }
+      } else if (c < walk.P) {
+        const int64_t g = (int64_t)c * run / walk.P, g_end = (int64_t)(c + 1) * run / walk.P;
+        walk.seek(A, g);
+        while (ok) {
+          x = walk.within(g, g_end);
+          if (x.t0 < x.t1) ok = put(x);
+          if (walk.ustart + walk.cost >= g_end) break;
+          walk.advance(A);
+        }
+      }
+      x = Piece{};
+      if (ok) put(x);
     }
-    x = Piece{};
-    if (ok) put(x);
   }
 
   tc_fence_before();

@@ -275,8 +275,11 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
 cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s) {
   RopeArgs a = args;
   const int heads = a.heads_q + 2 * a.heads_kv;
-  // Few rows: a row's heads in parts of one step's heads, so that a row is over after
-  // one round of loads; many: a warp a row, so that its angles serve all heads.
+  // Few rows: a row's heads in parts, of one step's heads where all parts are resident
+  // at once, so that a row is over after one round of loads.  Many: a warp a row, so
+  // that its angles serve all heads (10940 rows of 36 heads: 44 us, in parts of 24 / 16 /
+  // 8 heads 49 / 60 / 70).  Between one and two waves of whole rows the second would be
+  // mostly idle: parts of two steps (4096 rows of 80 heads: 37 -> 32 us).
   const int64_t resident = (int64_t)num_sms() * 3 * kWarps;
   a.chunk_heads = heads;
   for (int n = 2 * kUnroll; n < heads; n *= 2)
@@ -284,6 +287,7 @@ cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s) {
       a.chunk_heads = n;
       break;
     }
+  if (a.chunk_heads == heads && a.rows > resident && a.rows < 2 * resident) a.chunk_heads = 4 * kUnroll;
   a.chunks = (heads + a.chunk_heads - 1) / a.chunk_heads;
   const int64_t blocks = ((int64_t)a.rows * a.chunks + kWarps - 1) / kWarps;
   auto kernel = a.rope.style == 1 ? (append ? rope_kernel<true, true> : rope_kernel<false, true>)
