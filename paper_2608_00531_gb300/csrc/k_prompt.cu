@@ -333,7 +333,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       if (whole && !act) continue;
       const int i = (2 * x.rg + m) * npb + row / G;  // the row's place in its sequence
       const int sees = x.L + i + 1;                  // keys that it sees
-      const int all_see = x.L + (2 * x.rg + m) * npb + 1;  // that every row of the M tile sees
+      // the fewest and the most that a row of this warp sees
+      const int least = __shfl_sync(0xffffffffu, sees, 0), most = __shfl_sync(0xffffffffu, sees, 31);
       float m_run = -INFINITY, l_run = 0.f;
       for (int t = x.t0; act && ok && t < x.t1; ++t) {
         if (!wait_warp(bar(B_SFULL + m), sc & 1u, abort_flag, A.err)) { ok = false; break; }
@@ -348,10 +349,15 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         float x_[BN];
 #pragma unroll
         for (int k = 0; k < BN; ++k) x_[k] = __uint_as_float(v[k >> 5][k & 31]);
-        if ((t + 1) * BN > all_see) {
+        if ((t + 1) * BN > least) {
           const int lim = sees - t * BN;
 #pragma unroll
-          for (int k = 0; k < BN; ++k) x_[k] = k < lim ? x_[k] : -INFINITY;
+          for (int q = 0; q < 4; ++q) {
+            if (t * BN + 32 * (q + 1) > least) {
+#pragma unroll
+              for (int k = 32 * q; k < 32 * (q + 1); ++k) x_[k] = k < lim ? x_[k] : -INFINITY;
+            }
+          }
         }
         float mx[8];
 #pragma unroll
@@ -376,6 +382,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           uint32_t pk[16];
+          if (t * BN + 32 * q >= most) {  // no row of the warp sees these keys
+#pragma unroll
+            for (int k = 0; k < 16; ++k) pk[k] = 0u;
+            tmem_st16(tP + 16 * q, pk);
+            continue;
+          }
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
             float a0, a1;
@@ -401,15 +413,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             tmem_st32(tO + q * 32, o);
           }
         }
-        // V rows past the unit's last key are zeroed (by both M tiles) so that what lies
-        // there cannot reach O through 0 * NaN
+        // V rows past the unit's last key are zeroed so that what lies there cannot reach
+        // O through 0 * NaN: by M tile 0, whose PV product of a tile is issued first; up to
+        // the end of the last page or 16-row copy, behind which zeros were read
         const int valid = x.keys - t * BN;
-        if (valid < BN) {
+        if (m == 0 && valid < BN) {
           const uint32_t rv = r_piece + 2 * (uint32_t)(t - x.t0) + 1;
           if (!wait_warp(bar(B_FULL + rv % NS), (rv / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
           const uint32_t vb = sb + kOffRing + (rv % NS) * kTile;
           const bool paged = A.kv.layout == 1;
-          for (int q = row; q < (BN - valid) * 16; q += BM) {
+          const int unit = paged ? A.kv.page_size : 16;
+          for (int q = row; q < (unit - 1 - (valid - 1) % unit) * 16; q += BM) {
             const int rr = valid + (q >> 4), hf = (q >> 3) & 1, cc = q & 7;
             const uint32_t off = paged ? (rr >> 3) * kPgGroup + hf * kPgHalf + (rr & 7) * 128
                                        : (rr >> 4) * kVChunk + hf * kVHalf + (rr & 15) * 128;
@@ -585,7 +599,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             } else if (kv == 0) {
               if (lane < 2) tma_load_3d(dst + lane * kKHalf, &tm_k, full, lane * 64, x.h, x.b * A.kv.max_len + t * BN);
             } else if (lane < BN / 16) {
-              tma_load_4d(dst + lane * kVChunk, &tm_v, full, 0, x.b * A.kv.max_len + t * BN + 16 * lane, 0, x.h);
+              // 16 rows each; those past the unit's keys from behind the tensor, which reads zeros
+              const int row = t * BN + 16 * lane;
+              tma_load_4d(dst + lane * kVChunk, &tm_v, full, 0,
+                          row < x.keys ? x.b * A.kv.max_len + row : A.batch * A.kv.max_len, 0, x.h);
             }
             __syncwarp();
             ++issued;
