@@ -11,15 +11,17 @@
 // each K and V tile from shared memory, and one runs its softmax while the
 // other's products run.
 //
-// Roles (12 warps):
+// Roles (16 warps):
 //   warps 0-3 / 4-7   softmax of M tile 0 / 1, a thread a row: reads S from TMEM,
 //                     writes P (bf16) to TMEM, keeps the row's running maximum
 //                     and sum, rescales O (only where the maximum has grown by
-//                     more than 2^8), writes the output
+//                     more than 2^8)
 //   warp 8            TMA producer: Q, and K and V tiles in turn through a ring
 //                     of 5 stages of 32 KiB
 //   warp 9            issues S = Q K^T (M128 N128 K128) of M tiles 0 and 1 in turn
 //   warp 10           issues O += P V (A = P from TMEM) once P is published
+//   warp 11           lays out the CTA's pieces of work, a few ahead
+//   warps 12-15       epilogue: write O while the softmax warps are in the next piece
 // TMEM (512 columns): S (128) | P[2] (64 each) | O[2] (128 each).  There is one S
 // for both M tiles: a softmax frees it as soon as it has loaded its row (128
 // registers), long before its exponentials are done, and the other M tile's
@@ -43,10 +45,10 @@ constexpr int BM = kAttnRowsCta;  // 128 rows per M tile
 constexpr int BN = 128;           // keys per tile
 constexpr int D = kAttnD;
 constexpr int NS = 5;             // ring stages, a K or a V tile each
-constexpr int kThreads = 384;
+constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kPieces = 4;        // pieces that the scheduler may be ahead
-constexpr int kTakers = 11;       // warps that take pieces: 0 - 10
+constexpr int kTakers = 15;       // warps that take pieces: all but the scheduler
 
 constexpr int kQHalf = kAttnQHalf;      // 16 KiB: [128 rows][64 d]
 constexpr int kKHalf = BN * 64 * 2;     // 16 KiB: [128 keys][64 d]
@@ -61,15 +63,15 @@ constexpr int kOffRing = kOffQ + 4 * kQHalf;   // K/V[stage]
 constexpr int kOffMisc = kOffRing + NS * kTile;
 enum {
   B_QFULL = 0, B_QEMPTY = 1, B_SFREE = 2, B_FULL = 3, B_EMPTY = B_FULL + NS, B_SFULL = B_EMPTY + NS,
-  B_PFULL = B_SFULL + 2, B_PVDONE = B_PFULL + 2, B_DRAIN = B_PVDONE + 2, B_JOIN = B_DRAIN + 2,
-  B_PIECE = B_JOIN + 1, B_TAKEN = B_PIECE + kPieces, kNumBars = B_TAKEN + kPieces
+  B_PFULL = B_SFULL + 2, B_PVDONE = B_PFULL + 2, B_STAT = B_PVDONE + 2, B_OFREE = B_STAT + 2, B_DRAIN = B_OFREE + 2,
+  B_JOIN = B_DRAIN + 2, B_PIECE = B_JOIN + 1, B_TAKEN = B_PIECE + kPieces, kNumBars = B_TAKEN + kPieces
 };
 constexpr int kOffTmemSlot = kOffMisc + 8 * kNumBars;
 constexpr int kOffAbort = kOffTmemSlot + 4;
-constexpr int kOffLast = kOffAbort + 4;
+constexpr int kOffJoins = kOffAbort + 4;                              // units that this CTA joins at its end
 constexpr int kPieceInts = 12;
-constexpr int kOffPieces = (kOffLast + 4 + 15) / 16 * 16;             // int [kPieces][kPieceInts]
-constexpr int kOffPrefix = kOffPieces + kPieces * kPieceInts * 4;     // int64 first position of each sequence [B+1]
+constexpr int kOffPieces = (kOffJoins + 4 + 15) / 16 * 16;            // int [kPieces][kPieceInts], then [2] to join
+constexpr int kOffPrefix = kOffPieces + (kPieces + 2) * kPieceInts * 4;  // int64 first position of each sequence [B+1]
 constexpr int kSmemBytes = kOffPrefix + 8 * (kAttnMaxBatch + 1);
 static_assert(kSmemBytes <= 232448, "fits the 227 KiB opt-in");
 
@@ -87,6 +89,7 @@ struct PromptArgs {
   uint32_t tag;   // this launch's tag
   float* ws_o;    // [2 * CTAs][32][256] float4 partial outputs
   float* ws_lse;  // [2 * CTAs][256] their base-2 log-sum-exps
+  float* ws_inv;  // [CTAs][2 M tiles][128 rows] reciprocal row sums, softmax to epilogue
   uint16_t* out;
   int* err;
 };
@@ -95,9 +98,11 @@ struct PromptArgs {
 // piece costs, in key times) and then one for each key of the last row that its
 // row group could have; tile t of it stands at the position of its first key.
 constexpr int kUnitCost = 2 * BN;
-// What cutting units costs a call, and the fewest positions worth a CTA.
-constexpr int kMergeCost = 5 * BN;
+// What joining the parts of units costs a call, and the fewest positions worth a CTA.
+constexpr int kJoinCost = 8 * BN;
 constexpr int kMinShare = 3 * BN;
+// A share's border that lies nearer to a unit's border than this moves there.
+constexpr int kSnap = 4 * BN;
 
 // A sequence's rows and the tokens before them; n = 0 where they do not make sense.
 struct Seq {
@@ -126,15 +131,24 @@ struct alignas(16) Piece {
 };
 static_assert(sizeof(Piece) == 4 * kPieceInts, "as it lies in shared memory");
 
-// The pieces of one CTA, laid out by the scheduler warp.  Either units are cut
-// (positions laid end to end and split evenly over the CTAs) or they are dealt
-// out whole, one position each.
+// a / b of nonnegative numbers for a quotient that is at most `most` (some thousands).
+__device__ __forceinline__ int small_quotient(int64_t a, int64_t b, int most) {
+  int q = min(most, (int)((float)a / (float)b));  // off by one at most
+  if (q * b > a) --q;
+  if (q < most && (q + 1) * b <= a) ++q;
+  return q;
+}
+
+// The units of a call, laid end to end, as the scheduler warp walks them.  Either
+// they are cut (positions as above, an even share of them for every CTA) or they
+// are dealt out whole in turn, one position each.
 struct Walk {
   const int64_t* start;  // first position of each sequence
   int B, Hkv, R;         // R: rows of a row group
   bool split;
   int P;                 // CTAs that take part
-  int64_t total;
+  int64_t share;         // positions of one CTA (the last one takes the rest)
+  int64_t near;          // how far a share's border moves to a unit's border at most
   // the unit at position ustart
   Seq s;
   int b, rg, h, groups;
@@ -143,14 +157,14 @@ struct Walk {
   __device__ __forceinline__ int64_t before(int k) const {  // positions of a head's row groups 0 .. k - 1
     return split ? k * (int64_t)(kUnitCost + s.L) + (int64_t)R * k * (k + 1) / 2 : k;
   }
-  __device__ __forceinline__ int owner(int64_t p) const { return (int)(((p + 1) * P - 1) / total); }
+  __device__ __forceinline__ int owner(int64_t p) const { return small_quotient(p, share, P - 1); }
   __device__ __forceinline__ void load(const PromptArgs& A) {
     int bad;
     s = sequence(A, b, &bad);
     groups = (s.n + R - 1) / R;
   }
   __device__ __forceinline__ void price() { cost = split ? kUnitCost + s.L + (int64_t)(rg + 1) * R : 1; }
-  __device__ void seek(const PromptArgs& A, int64_t g) {  // the unit that holds position g
+  __device__ __forceinline__ void seek(const PromptArgs& A, int64_t g) {  // the unit that holds position g
     int lo = 0, hi = B;  // largest b with start[b] <= g
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
@@ -168,7 +182,7 @@ struct Walk {
     }
     rg = lo;
     price();
-    h = (int)((local - Hkv * before(rg)) / cost);
+    h = small_quotient(local - Hkv * before(rg), cost, Hkv - 1);
     ustart = start[b] + Hkv * before(rg) + h * cost;
   }
   __device__ __forceinline__ void advance(const PromptArgs& A) {  // to the next unit (there is one)
@@ -180,11 +194,22 @@ struct Walk {
       do {
         ++b;
         load(A);
-      } while (groups == 0);
+      } while (groups == 0 && b + 1 < B);
     }
     price();
   }
-  __device__ __forceinline__ Piece whole() const {
+  __device__ __forceinline__ int keys() const { return s.L + min((rg + 1) * R, s.n); }
+  __device__ __forceinline__ int tiles() const { return (keys() + BN - 1) / BN; }
+  // Where the border p of a share, which lies in this unit, is drawn: at one of the
+  // unit's borders if that is near (or if one side would be left without a tile).
+  __device__ __forceinline__ int64_t border(int64_t p) const {
+    const int64_t first = ustart + kUnitCost;
+    if (p < first + near) return ustart;
+    if (p > first + (int64_t)(tiles() - 1) * BN || ustart + cost - p < near) return ustart + cost;
+    return p;
+  }
+  // The unit's tiles in the range [g, g_end) between drawn borders.
+  __device__ __forceinline__ Piece within(int64_t g, int64_t g_end) const {
     Piece x;
     x.b = b;
     x.h = h;
@@ -192,23 +217,24 @@ struct Walk {
     x.r0 = s.r0;
     x.n = s.n;
     x.L = s.L;
-    x.keys = s.L + min((rg + 1) * R, s.n);
-    x.T = (x.keys + BN - 1) / BN;
+    x.keys = keys();
+    x.T = tiles();
     x.t0 = 0;
     x.t1 = x.T;
     x.o0 = (int)blockIdx.x;
     x.parts = 1;
-    return x;
-  }
-  // The unit's tiles in the range [g, g_end).
-  __device__ __forceinline__ Piece within(int64_t g, int64_t g_end) const {
-    Piece x = whole();
-    const int64_t first = ustart + kUnitCost;  // tile 0's position
-    x.t0 = g <= first ? 0 : (int)min((int64_t)x.T, (g - first + BN - 1) / BN);
-    x.t1 = g_end <= first ? 0 : (int)min((int64_t)x.T, (g_end - first + BN - 1) / BN);
-    if (x.t1 - x.t0 < x.T && x.t0 < x.t1) {
-      x.o0 = owner(first);
-      x.parts = owner(first + (int64_t)(x.T - 1) * BN) - x.o0 + 1;
+    if (split) {
+      const int64_t first = ustart + kUnitCost;  // tile 0's position
+      if (g > first) x.t0 = (int)min((int64_t)x.T, (g - first + BN - 1) / BN);
+      x.t1 = g_end <= first ? 0 : (int)min((int64_t)x.T, (g_end - first + BN - 1) / BN);
+      if (x.t0 < x.t1 && x.t1 - x.t0 < x.T) {
+        // the shares that the first and the last tile lie in, and theirs after the borders moved
+        int o1 = owner(first + (int64_t)(x.T - 1) * BN);
+        x.o0 = owner(first);
+        if (x.o0 < P - 1 && (x.o0 + 1) * share < first + near) ++x.o0;
+        if (o1 * share >= first + near && ustart + cost - o1 * share < near) --o1;
+        x.parts = o1 - x.o0 + 1;
+      }
     }
     return x;
   }
@@ -258,7 +284,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   const int G = A.G, npb = BM / G;
   const Bar bar{sb + kOffMisc};
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
-  volatile int* last_flag = reinterpret_cast<volatile int*>(smem + kOffLast);
+  volatile int* n_joins = reinterpret_cast<volatile int*>(smem + kOffJoins);
 
   // ---------------------------------------------------------------- set-up
   if (tid == 0) {
@@ -273,14 +299,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       mbar_init(bar(B_SFULL + m), 1);
       mbar_init(bar(B_PFULL + m), BM);
       mbar_init(bar(B_PVDONE + m), 1);
+      mbar_init(bar(B_STAT + m), BM);
+      mbar_init(bar(B_OFREE + m), BM);
       mbar_init(bar(B_DRAIN + m), 1);
     }
-    mbar_init(bar(B_JOIN), 2 * BM);
+    mbar_init(bar(B_JOIN), BM);
     for (int i = 0; i < kPieces; ++i) {
       mbar_init(bar(B_PIECE + i), 1);
       mbar_init(bar(B_TAKEN + i), kTakers);
     }
     *abort_flag = 0;
+    *n_joins = 0;
     fence_mbar_init();
   }
   if (warp == 0) tmem_alloc(sb + kOffTmemSlot, kTmemCols);
@@ -306,37 +335,29 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   // M tile 1 of a piece is active when its first row is one of the sequence's
   auto active1 = [&](const Piece& x) { return (2 * x.rg + 1) * npb < x.n; };
 
-  // The softmax warps hold a row of S each: they get registers from the other four
-  // warps (2 * 128 * 208 + 128 * 88 = 384 * 168, what the block was launched with).
+  // The softmax warps hold a row of S each: they get registers from the other
+  // warpgroups (128 * (2 * 168 + 96 + 80) = 512 * 128, what the block was launched with).
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     // ================================================================ softmax
     const int m = warp >> 2;
     const int row = tid & 127;  // row within the M tile = TMEM lane
     const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t tS = tl + kColS, tP = tl + kColP + m * 64, tO = tl + kColO + m * D;
     const float c = A.scale_log2;
-    const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
     uint32_t sc = 0, r = 0;  // tiles of this M tile, ring tiles
     bool ok = true;
-    // All softmax threads meet (an mbarrier, for a wait that ends when the CTA gives up).
-    uint32_t joins = 0;
-    auto join_softmax = [&]() -> bool {
-      mbar_arrive(bar(B_JOIN));
-      ok = wait_warp(bar(B_JOIN), joins++ & 1u, abort_flag, A.err) && ok;
-      return ok;
-    };
+    uint32_t done = 0;  // pieces of this M tile
     while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
       const uint32_t r_piece = r;
       r += 2 * (uint32_t)(x.t1 - x.t0);
-      const bool act = m == 0 || active1(x), whole = x.t1 - x.t0 == x.T;
-      if (whole && !act) continue;
+      if (m == 1 && !active1(x)) continue;
       const int i = (2 * x.rg + m) * npb + row / G;  // the row's place in its sequence
       const int sees = x.L + i + 1;                  // keys that it sees
       // the fewest and the most that a row of this warp sees
       const int least = __shfl_sync(0xffffffffu, sees, 0), most = __shfl_sync(0xffffffffu, sees, 31);
       float m_run = -INFINITY, l_run = 0.f;
-      for (int t = x.t0; act && ok && t < x.t1; ++t) {
+      for (int t = x.t0; t < x.t1; ++t) {
         if (!wait_warp(bar(B_SFULL + m), sc & 1u, abort_flag, A.err)) { ok = false; break; }
         ++sc;
         tc_fence_after();
@@ -379,15 +400,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         const float nbase = m_run == -INFINITY ? 0.f : -m_run;
         const uint64_t c2 = f2_pack(c, c), nb2 = f2_pack(nbase, nbase);
         uint64_t sm2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        auto exponentials = [&](int q) {  // of 32 keys
           uint32_t pk[16];
-          if (t * BN + 32 * q >= most) {  // no row of the warp sees these keys
-#pragma unroll
-            for (int k = 0; k < 16; ++k) pk[k] = 0u;
-            tmem_st16(tP + 16 * q, pk);
-            continue;
-          }
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
             float a0, a1;
@@ -397,13 +411,23 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             pk[k] = pack_bf16(p0, p1);
           }
           tmem_st16(tP + 16 * q, pk);
+        };
+        exponentials(0);
+        exponentials(1);
+        if (t * BN + BN / 2 < most) {
+          exponentials(2);
+          exponentials(3);
+        } else {  // keys that no row of the warp sees
+          const uint32_t zero[16] = {};
+          tmem_st16(tP + 32, zero);
+          tmem_st16(tP + 48, zero);
         }
         float s4[4];
         f2_unpack(sm2[0], s4[0], s4[1]);
         f2_unpack(sm2[1], s4[2], s4[3]);
         l_run = l_run * alpha + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
         if (t > x.t0 && __any_sync(0xffffffffu, need)) {
-#pragma unroll
+#pragma unroll 1
           for (int q = 0; q < 4; ++q) {
             uint32_t o[32];
             tmem_ld32(tO + q * 32, o);
@@ -435,46 +459,62 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         tc_fence_before();
         mbar_arrive(bar(B_PFULL + m));
       }
-      if (act && !(ok && wait_warp(bar(B_PVDONE + m), (sc - 1) & 1u, abort_flag, A.err))) {
-        ok = false;
-        break;
-      }
-      tc_fence_after();
-      const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-      const bool vrow = act && row < npb * G && i < x.n;
-      if (whole) {
-        // ---- the output rows
+      if (!ok) break;
+      // What the epilogue needs to know of the row, once it is done with the piece before
+      // (so that it also sees every phase of STAT).
+      if (done > 0 && !wait_warp(bar(B_OFREE + m), (done - 1) & 1u, abort_flag, A.err)) break;
+      __stcg(A.ws_inv + ((int64_t)blockIdx.x * 2 + m) * BM + row, l_run > 0.f ? 1.f / l_run : 0.f);
+      if (x.t1 - x.t0 < x.T)
+        __stcg(A.ws_lse + (2 * (int64_t)blockIdx.x + (x.t0 == 0)) * (2 * BM) + m * BM + row, row_lse(m_run, l_run));
+      mbar_arrive(bar(B_STAT + m));
+      ++done;
+    }
+  } else if (warp >= 12) {
+    // ================================================================ epilogue
+    // Writes a piece's rows while the softmax warps are in the next one.
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    const int row = tid & 127;  // row within an M tile = TMEM lane
+    const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColO;
+    const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
+    uint32_t done0 = 0, done1 = 0, tiles0 = 0, tiles1 = 0, joins = 0;
+    bool ok = true;
+    // The epilogue's threads meet (an mbarrier, for a wait that ends when the CTA gives up).
+    auto meet = [&]() -> bool {
+      mbar_arrive(bar(B_JOIN));
+      return ok = wait_warp(bar(B_JOIN), joins++ & 1u, abort_flag, A.err);
+    };
+    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
+      const bool whole = x.t1 - x.t0 == x.T;
+      const int64_t slot = 2 * (int64_t)blockIdx.x + (x.t0 == 0);
+#pragma unroll 1
+      for (int m = 0; m < 2; ++m) {
+        if (m == 1 && !active1(x)) break;
+        // STAT first: the softmax has then seen all PV products but the last
+        const uint32_t done = m ? done1++ : done0++;  // pieces before, and tiles with this one
+        const uint32_t tiles = m ? tiles1 += (uint32_t)(x.t1 - x.t0) : tiles0 += (uint32_t)(x.t1 - x.t0);
+        if (!wait_warp(bar(B_STAT + m), done & 1u, abort_flag, A.err)) { ok = false; break; }
+        const float inv = __ldcg(A.ws_inv + ((int64_t)blockIdx.x * 2 + m) * BM + row);
+        if (!wait_warp(bar(B_PVDONE + m), (tiles - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
+        tc_fence_after();
+        const int i = (2 * x.rg + m) * npb + row / G;
+        const bool vrow = row < npb * G && i < x.n;
         uint16_t* orow = A.out + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D;
-#pragma unroll
+        float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + m * BM + row;
+#pragma unroll 1
         for (int q = 0; q < 4; ++q) {
           uint32_t o[32];
-          tmem_ld32(tO + q * 32, o);
+          tmem_ld32(tO + m * D + q * 32, o);
           tmem_wait_ld();
+          if (whole) {
 #pragma unroll
-          for (int k = 0; k < 16; ++k)
-            o[k] = pack_bf16(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
-          if (vrow) {
-            st_global_32(orow + q * 32, o, wide);
-            st_global_32(orow + q * 32 + 16, o + 8, wide);
-          }
-        }
-        tc_fence_before();
-        continue;
-      }
-      // ---- a part of a unit: normalised O and log-sum-exp to the workspace, float4
-      // columns [32][256 rows]; the CTA whose piece arrives last joins all of them, in
-      // the order of the keys whichever that is
-      const int cta = (int)blockIdx.x;
-      const int64_t slot = 2 * (int64_t)cta + (x.t0 == 0);
-      const int prow = m * BM + row;
-      if (act) {
-        float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + prow;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t o[32];
-          tmem_ld32(tO + q * 32, o);
-          tmem_wait_ld();
-          if (vrow) {
+            for (int k = 0; k < 16; ++k)
+              o[k] = pack_bf16(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
+            if (vrow) {
+              st_global_32(orow + q * 32, o, wide);
+              st_global_32(orow + q * 32 + 16, o + 8, wide);
+            }
+          } else if (vrow) {
+            // a part of a unit: normalised O to the workspace, float4 columns [32][256 rows]
 #pragma unroll
             for (int k = 0; k < 8; ++k)
               po[(q * 8 + k) * (2 * BM)] =
@@ -482,91 +522,21 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
                               __uint_as_float(o[4 * k + 2]) * inv, __uint_as_float(o[4 * k + 3]) * inv);
           }
         }
-        if (vrow) A.ws_lse[slot * (2 * BM) + prow] = row_lse(m_run, l_run);
+        tc_fence_before();
+        mbar_arrive(bar(B_OFREE + m));
       }
-      tc_fence_before();
+      if (!ok || whole) continue;
+      // The CTA whose part arrives last joins the unit when its own pieces are done.
       __threadfence();
-      if (!join_softmax()) break;
-      if (tid == 0) {
-        int l = 0;
-        if (!*abort_flag) {
-          l = arrive(A.cnt + x.o0, A.tag) == x.parts;
-          if (l) A.cnt[x.o0] = 0;  // a completed unit leaves a zero word behind
-        }
-        *last_flag = l;
-      }
-      if (!join_softmax()) break;
-      if (*last_flag) {
-        __threadfence();
-        // rows 0 .. v0 - 1 of M tile 0 and 0 .. v1 - 1 of M tile 1
-        const int v0 = min(npb, x.n - 2 * x.rg * npb) * G, v1 = max(0, min(npb, x.n - (2 * x.rg + 1) * npb)) * G;
-        const int rows8 = (v0 + v1 + 7) / 8;
-        // A warp takes 8 rows and 4 * C of the 32 float4 columns, N parts' loads in flight:
-        //   O = sum_p 2^(lse_p) O_p / sum_p 2^(lse_p), relative to the maximum so far
-        auto join = [&](auto ctag, auto ntag) {
-          constexpr int C = decltype(ctag)::value, N = decltype(ntag)::value;
-          for (int task = warp; task < rows8 * (8 / C); task += 8) {
-            const int k = task / (8 / C) * 8 + (lane >> 2), c0 = task % (8 / C) * 4 * C + (lane & 3);
-            if (k >= v0 + v1) continue;
-            const int mt = k >= v0, rr = mt ? k - v0 : k;
-            const int64_t at = mt * BM + rr;
-            float4 acc[C];
-#pragma unroll
-            for (int j = 0; j < C; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-            float M = -INFINITY, wsum = 0.f;
-            for (int p0 = 0; p0 < x.parts; p0 += N) {
-              float w[N];
-              float4 o[N][C];
-#pragma unroll
-              for (int p = 0; p < N; ++p) {
-                if (p0 + p < x.parts) {
-                  const int64_t sl = 2 * (int64_t)(x.o0 + p0 + p) + (p0 + p == 0);
-                  w[p] = __ldcg(A.ws_lse + sl * (2 * BM) + at);
-#pragma unroll
-                  for (int j = 0; j < C; ++j)
-                    o[p][j] = __ldcg(reinterpret_cast<const float4*>(A.ws_o) + (sl * 32 + c0 + 4 * j) * (2 * BM) + at);
-                } else {
-                  w[p] = -INFINITY;
-#pragma unroll
-                  for (int j = 0; j < C; ++j) o[p][j] = make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-              }
-              float Mn = M;
-#pragma unroll
-              for (int p = 0; p < N; ++p) Mn = fmaxf(Mn, w[p]);
-              const float a = ex2(M - Mn);
-              M = Mn;
-              wsum *= a;
-#pragma unroll
-              for (int j = 0; j < C; ++j) acc[j] = make_float4(acc[j].x * a, acc[j].y * a, acc[j].z * a, acc[j].w * a);
-#pragma unroll
-              for (int p = 0; p < N; ++p) {
-                const float wp = ex2(w[p] - Mn);
-                wsum += wp;
-#pragma unroll
-                for (int j = 0; j < C; ++j) {
-                  acc[j].x += wp * o[p][j].x;
-                  acc[j].y += wp * o[p][j].y;
-                  acc[j].z += wp * o[p][j].z;
-                  acc[j].w += wp * o[p][j].w;
-                }
-              }
-            }
-            const float winv = 1.f / wsum;
-            uint16_t* orow =
-                A.out + ((int64_t)(x.r0 + (2 * x.rg + mt) * npb + rr / G) * A.heads_q + x.h * G + rr % G) * D;
-#pragma unroll
-            for (int j = 0; j < C; ++j)
-              *reinterpret_cast<uint2*>(orow + (c0 + 4 * j) * 4) =
-                  make_uint2(pack_bf16(acc[j].x * winv, acc[j].y * winv), pack_bf16(acc[j].z * winv, acc[j].w * winv));
-          }
-        };
-        if (rows8 >= 8) join(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
-        else join(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
+      if (!meet()) break;
+      if (tid == 12 * 32 && !*abort_flag && arrive(A.cnt + x.o0, A.tag) == x.parts) {
+        A.cnt[x.o0] = 0;  // a completed unit leaves a zero word behind
+        *reinterpret_cast<Piece*>(smem + kOffPieces + (kPieces + *n_joins) * (kPieceInts * 4)) = x;
+        *n_joins = *n_joins + 1;
       }
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == 8) {
       // ================================================================ producer
       const int ps = A.kv.page_size;
@@ -585,9 +555,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           }
           return page;
         };
-        int page = ppt > 0 ? page_of(x.t0) : -1;
+        int page = page_of(x.t0);
         for (int t = x.t0; ok && t < x.t1; ++t) {
-          const int next = ppt > 0 && t + 1 < x.t1 ? page_of(t + 1) : -1;
+          const int next = t + 1 < x.t1 ? page_of(t + 1) : -1;
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {  // the K tile, then the V tile
             const int st = (int)(issued % NS);
             if (!wait_warp(bar(B_EMPTY + st), ((issued / NS) & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
@@ -639,6 +610,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           const uint32_t sk = r % NS;
           const uint32_t ka = sb + kOffRing + sk * kTile;
           const uint32_t sbo = paged ? kPgGroup : 1024u, kh = paged ? kPgHalf : kKHalf;
+#pragma unroll 1
           for (int m = 0; m < mts; ++m) {
             if (c > 0 && !wait_warp(bar(B_SFREE), (c - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
             ++c;
@@ -664,7 +636,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       // ================================================================ PV products
       constexpr uint32_t idO = idesc_bf16_f32(BM, D, true);
       const bool paged = A.kv.layout == 1;
-      uint32_t r = 1, c[2] = {0, 0};  // ring tiles, products of each M tile
+      uint32_t r = 1, c0 = 0, c1 = 0, done0 = 0, done1 = 0;  // ring tiles; products and pieces of each M tile
       bool ok = true;
       while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
         const int mts = active1(x) ? 2 : 1;
@@ -674,12 +646,17 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           // warp has waited for)
           if (!wait_warp(bar(B_FULL + sv), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
           // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
-          const uint64_t vd = sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
-#pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            if (m >= mts) break;
-            if (!wait_warp(bar(B_PFULL + m), c[m] & 1u, abort_flag, A.err)) { ok = false; break; }
-            ++c[m];
+          const uint64_t vd =
+              sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
+#pragma unroll 1
+          for (int m = 0; m < mts; ++m) {
+            // the first product of a piece takes O over from the epilogue of the one before
+            const uint32_t c = m ? c1++ : c0++;
+            if (t == x.t0) {
+              const uint32_t done = m ? done1++ : done0++;
+              if (done > 0 && !wait_warp(bar(B_OFREE + m), (done - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
+            }
+            if (!wait_warp(bar(B_PFULL + m), c & 1u, abort_flag, A.err)) { ok = false; break; }
             tc_fence_after();
             mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0 ? 1u : 0u);
             mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64 + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
@@ -724,8 +701,12 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         cost += __shfl_xor_sync(0xffffffffu, cost, off);
       }
       longest = __reduce_max_sync(0xffffffffu, longest);
-      const int64_t rounds = (units + gridDim.x - 1) / gridDim.x;
-      walk.split = rounds * (longest + kUnitCost) > cost / gridDim.x + kMergeCost;
+      // Whole units: the longest one if every CTA has one at most, else an even share and,
+      // on average over the CTAs that end last, half of the longest.  Cut units: an even
+      // share, which the pieces' fixed costs upset by some 8 %, and the joins.
+      const float share = (float)cost / (float)gridDim.x;
+      const float whole = units <= gridDim.x ? (float)(longest + kUnitCost) : share + 0.5f * (float)(longest + kUnitCost);
+      walk.split = whole > 1.08f * share + kJoinCost;
       int64_t run = 0;
       for (int base = 0; base < A.batch; base += 32) {
         const int b = base + lane;
@@ -741,9 +722,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         run += __shfl_sync(0xffffffffu, upto, 31);
       }
       __syncwarp();
-      walk.total = run;
       // every CTA that takes part in cut units has a tile of each unit that its range lies in
-      walk.P = walk.split ? (int)max((int64_t)1, min((int64_t)gridDim.x, run / kMinShare)) : (int)gridDim.x;
+      walk.P = (int)gridDim.x;
+      if (walk.split) {
+        if (share < (float)kMinShare) walk.P = max(1, (int)((float)run / (float)kMinShare));
+        walk.share = (int64_t)((float)run / (float)walk.P * 0.999999f);
+        walk.near = min((int64_t)kSnap, max((int64_t)1, (walk.share - kUnitCost) / 2));
+      }
       uint32_t k = 0;
       auto put = [&](const Piece& p) -> bool {
         const uint32_t slot = k % kPieces;
@@ -759,30 +744,117 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         __syncwarp();
         return true;
       };
+      // Whole units: every P-th.  Cut ones: the first and the last piece of the range, which
+      // may be parts of units, come first, so that parts are joined while the CTAs are in
+      // later pieces; then the units between.
       const int c = (int)blockIdx.x;
-      bool ok = true;
-      if (!walk.split) {
-        for (int64_t u = c; ok && u < run; u += walk.P) {
-          walk.seek(A, u);
-          ok = put(walk.whole());
-        }
-      } else if (c < walk.P) {
-        const int64_t g = (int64_t)c * run / walk.P, g_end = (int64_t)(c + 1) * run / walk.P;
-        walk.seek(A, g);
-        while (ok) {
+      int64_t g = walk.split ? c * walk.share : c, g_end = run, last = run;
+      int64_t at = walk.split && c < walk.P - 1 ? g + walk.share : g;
+      Piece tail{};
+      for (int step = at > g ? 0 : 1;; ++step) {
+        bool end = c >= walk.P || at >= run;
+        if (!end && walk.split && step == 2) {
+          x = tail;
+          if (walk.ustart >= last) end = true;  // the range lies in one unit
+        } else if (!end) {
+          if (!walk.split || step < 2) walk.seek(A, at);
+          else if (walk.ustart + walk.cost >= last) end = true;
+          else walk.advance(A);
+          if (walk.split && step == 0) {  // the range's end: `last` is the unit that it lies in
+            g_end = walk.border(at);
+            last = walk.ustart;
+            tail = walk.within(last, g_end);
+            at = g;
+            continue;
+          }
+          if (walk.split && step == 1 && c > 0) g = walk.border(at);
           x = walk.within(g, g_end);
-          if (x.t0 < x.t1) ok = put(x);
-          if (walk.ustart + walk.cost >= g_end) break;
-          walk.advance(A);
         }
+        if (end) x = Piece{};
+        else if (x.t0 >= x.t1) continue;
+        if (!put(x) || end) break;
+        if (!walk.split) at += walk.P;
       }
-      x = Piece{};
-      if (ok) put(x);
     }
   }
 
+  // ---- the units that this CTA joins, by all warps and with equal registers again
+  __syncwarp();
+  if (warp < 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 128;");
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
   tc_fence_before();
   __syncthreads();
+  if (!*abort_flag) {
+    for (int d = 0; d < *n_joins; ++d) {
+      x = *reinterpret_cast<const Piece*>(smem + kOffPieces + (kPieces + d) * (kPieceInts * 4));
+      __threadfence();
+      // rows 0 .. v0 - 1 of M tile 0 and 0 .. v1 - 1 of M tile 1
+      const int v0 = min(npb, x.n - 2 * x.rg * npb) * G, v1 = max(0, min(npb, x.n - (2 * x.rg + 1) * npb)) * G;
+      const int rows8 = (v0 + v1 + 7) / 8;
+      // A warp takes 8 rows and 4 * C of the 32 float4 columns, N parts' loads in flight:
+      //   O = sum_p 2^(lse_p) O_p / sum_p 2^(lse_p), relative to the maximum so far
+      auto join = [&](auto ctag, auto ntag) {
+        constexpr int C = decltype(ctag)::value, N = decltype(ntag)::value;
+        for (int task = warp; task < rows8 * (8 / C); task += kThreads / 32) {
+          const int k = task / (8 / C) * 8 + (lane >> 2), c0 = task % (8 / C) * 4 * C + (lane & 3);
+          if (k >= v0 + v1) continue;
+          const int mt = k >= v0, rr = mt ? k - v0 : k;
+          const int64_t at = mt * BM + rr;
+          float4 acc[C];
+#pragma unroll
+          for (int j = 0; j < C; ++j) acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+          float M = -INFINITY, wsum = 0.f;
+          for (int p0 = 0; p0 < x.parts; p0 += N) {
+            float w[N];
+            float4 o[N][C];
+#pragma unroll
+            for (int p = 0; p < N; ++p) {
+              if (p0 + p < x.parts) {
+                const int64_t sl = 2 * (int64_t)(x.o0 + p0 + p) + (p0 + p == 0);
+                w[p] = __ldcg(A.ws_lse + sl * (2 * BM) + at);
+#pragma unroll
+                for (int j = 0; j < C; ++j)
+                  o[p][j] = __ldcg(reinterpret_cast<const float4*>(A.ws_o) + (sl * 32 + c0 + 4 * j) * (2 * BM) + at);
+              } else {
+                w[p] = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < C; ++j) o[p][j] = make_float4(0.f, 0.f, 0.f, 0.f);
+              }
+            }
+            float Mn = M;
+#pragma unroll
+            for (int p = 0; p < N; ++p) Mn = fmaxf(Mn, w[p]);
+            const float a = ex2(M - Mn);
+            M = Mn;
+            wsum *= a;
+#pragma unroll
+            for (int j = 0; j < C; ++j) acc[j] = make_float4(acc[j].x * a, acc[j].y * a, acc[j].z * a, acc[j].w * a);
+#pragma unroll
+            for (int p = 0; p < N; ++p) {
+              const float wp = ex2(w[p] - Mn);
+              wsum += wp;
+#pragma unroll
+              for (int j = 0; j < C; ++j) {
+                acc[j].x += wp * o[p][j].x;
+                acc[j].y += wp * o[p][j].y;
+                acc[j].z += wp * o[p][j].z;
+                acc[j].w += wp * o[p][j].w;
+              }
+            }
+          }
+          const float winv = 1.f / wsum;
+          uint16_t* orow =
+              A.out + ((int64_t)(x.r0 + (2 * x.rg + mt) * npb + rr / G) * A.heads_q + x.h * G + rr % G) * D;
+#pragma unroll
+          for (int j = 0; j < C; ++j)
+            *reinterpret_cast<uint2*>(orow + (c0 + 4 * j) * 4) =
+                make_uint2(pack_bf16(acc[j].x * winv, acc[j].y * winv), pack_bf16(acc[j].z * winv, acc[j].w * winv));
+        }
+      };
+      if (rows8 >= 8) join(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
+      else join(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
+    }
+  }
   if (warp == 0) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
@@ -793,14 +865,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 
 // Workspace: piece counters [CTAs] (256-byte rounded), partial outputs and their
 // log-sum-exps [2 * CTAs]: of a CTA's pieces at most its first and its last are
-// parts of a unit.
+// parts of a unit; and the row sums that softmax warps leave for the epilogue.
 namespace {
 size_t counter_bytes(int ctas) { return ((size_t)ctas * sizeof(int) + 255) / 256 * 256; }
 }  // namespace
 
 size_t prompt_attn_workspace() {
   const int ctas = num_sms();
-  return counter_bytes(ctas) + (size_t)2 * ctas * 2 * BM * (D + 1) * sizeof(float);
+  return counter_bytes(ctas) + (size_t)ctas * 2 * BM * (2 * (D + 1) + 1) * sizeof(float);
 }
 
 cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
@@ -849,6 +921,7 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
   A.cnt = reinterpret_cast<int*>(ws);
   A.ws_o = reinterpret_cast<float*>(ws + counter_bytes(ctas));
   A.ws_lse = A.ws_o + (size_t)2 * ctas * 2 * BM * D;
+  A.ws_inv = A.ws_lse + (size_t)2 * ctas * 2 * BM;
   return launch_pdl(prompt_attn_kernel, dim3(ctas), dim3(kThreads), kSmemBytes, s, mk, mv, mq, A);
 }
 
