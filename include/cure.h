@@ -442,11 +442,14 @@ cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t 
  * are left unwritten, and so are the rows of a sequence that does not fit its
  * capacity (CURE_DEVERR_SLOT) or whose row_start does not ascend within
  * 0 .. rows (CURE_DEVERR_NODES).  A missing or bad page counts as zeros
- * (CURE_DEVERR_PAGE).  batch <= 256, D = 128, heads_q / heads_kv <= 128, scale > 0
- * and finite; all base pointers 16-byte aligned.
+ * (CURE_DEVERR_PAGE).  batch <= 256, rows <= 2^22, D = 128, heads_q / heads_kv <=
+ * 128, scale > 0 and finite; all base pointers 16-byte aligned.
  * workspace: device scratch of at least cure_prompt_attn_workspace_size() bytes,
- * 256-byte aligned; its contents on entry do not matter.  Calls that can overlap
- * on the GPU must not share a workspace.
+ * 256-byte aligned (what parts of a long row group hand to the part that joins
+ * them); its contents on entry do not matter.  Calls that can overlap on the GPU
+ * must not share a workspace, captured ones included; after CURE_DEVERR_TIMEOUT zero
+ * it before a captured call is replayed on it.  The result does not depend on how a
+ * call's work was shared out: the same bits call after call.
  */
 cure_status cure_prompt_attn(const void* q, const void* k_cache, const void* v_cache, const cure_kv_desc* kv,
                              const int32_t* row_start, const int32_t* cache_len, int32_t rows, int32_t batch,

@@ -533,7 +533,7 @@ static cure_status prompt_shape_ok(int32_t rows, int32_t batch, int32_t heads_q,
   if (!kv_ok(kv, &why)) return why;
   if (rows < 0 || batch < 0 || heads_q < 1 || heads_q % kv->heads_kv != 0) return CURE_ERR_INVALID_ARG;
   const int G = heads_q / kv->heads_kv;
-  if (batch > kAttnBatchLimit || G > 128) return CURE_ERR_UNSUPPORTED;
+  if (batch > kAttnBatchLimit || G > 128 || rows > (1 << 22)) return CURE_ERR_UNSUPPORTED;
   const int64_t units = ((int64_t)rows / (2 * (128 / G)) + batch) * kv->heads_kv;
   return units <= INT32_MAX / 2 ? CURE_OK : CURE_ERR_UNSUPPORTED;
 }

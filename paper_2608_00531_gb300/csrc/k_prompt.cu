@@ -131,7 +131,7 @@ struct alignas(16) Piece {
 };
 static_assert(sizeof(Piece) == 4 * kPieceInts, "as it lies in shared memory");
 
-// a / b of nonnegative numbers for a quotient that is at most `most` (some thousands).
+// a / b of nonnegative numbers for a quotient of at most `most` (below 2^22 or so).
 __device__ __forceinline__ int small_quotient(int64_t a, int64_t b, int most) {
   int q = min(most, (int)((float)a / (float)b));  // off by one at most
   if (q * b > a) --q;
@@ -142,8 +142,15 @@ __device__ __forceinline__ int small_quotient(int64_t a, int64_t b, int most) {
 // The units of a call, laid end to end, as the scheduler warp walks them.  Either
 // they are cut (positions as above, an even share of them for every CTA) or they
 // are dealt out whole in turn, one position each.
+//
+// A batch of up to 32 sequences stays in the warp's registers, a sequence a lane;
+// of a larger one the first positions lie in shared memory and the rest is read
+// again.  (A call's first piece was 5,000 cycles away, most of it dependent loads.)
 struct Walk {
-  const int64_t* start;  // first position of each sequence
+  const int64_t* start;  // first position of each sequence (large batches)
+  bool few;
+  Seq mine;              // few: the lane's sequence and its first position
+  int64_t first_of_mine;
   int B, Hkv, R;         // R: rows of a row group
   bool split;
   int P;                 // CTAs that take part
@@ -159,31 +166,46 @@ struct Walk {
   }
   __device__ __forceinline__ int owner(int64_t p) const { return small_quotient(p, share, P - 1); }
   __device__ __forceinline__ void load(const PromptArgs& A) {
-    int bad;
-    s = sequence(A, b, &bad);
+    if (few) {
+      s.r0 = __shfl_sync(0xffffffffu, mine.r0, b);
+      s.n = __shfl_sync(0xffffffffu, mine.n, b);
+      s.L = __shfl_sync(0xffffffffu, mine.L, b);
+    } else {
+      int bad;
+      s = sequence(A, b, &bad);
+    }
     groups = (s.n + R - 1) / R;
   }
   __device__ __forceinline__ void price() { cost = split ? kUnitCost + s.L + (int64_t)(rg + 1) * R : 1; }
   __device__ __forceinline__ void seek(const PromptArgs& A, int64_t g) {  // the unit that holds position g
-    int lo = 0, hi = B;  // largest b with start[b] <= g
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (start[mid] <= g) lo = mid;
-      else hi = mid;
+    int64_t first;  // of the last sequence that starts at or before it
+    if (few) {
+      b = __popc(__ballot_sync(0xffffffffu, (int)(threadIdx.x & 31) < B && first_of_mine <= g)) - 1;
+      first = __shfl_sync(0xffffffffu, first_of_mine, b);
+    } else {
+      int lo = 0, hi = B;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= g) lo = mid;
+        else hi = mid;
+      }
+      b = lo;
+      first = start[b];
     }
-    b = lo;
     load(A);
-    const int64_t local = g - start[b];
-    lo = 0, hi = groups;  // largest row group that starts at or before it
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (Hkv * before(mid) <= local) lo = mid;
-      else hi = mid;
+    const int64_t local = g - first;
+    // the last row group that starts at or before it: local = Hkv before(rg)
+    if (split) {
+      const float each = (float)(kUnitCost + s.L) + 0.5f * (float)R, l = (float)local / (float)Hkv;
+      rg = min(groups - 1, (int)(2.f * l / (each + sqrtf(each * each + 2.f * (float)R * l))));  // off by one at most
+      if (rg > 0 && Hkv * before(rg) > local) --rg;
+      if (rg < groups - 1 && Hkv * before(rg + 1) <= local) ++rg;
+    } else {
+      rg = small_quotient(local, Hkv, groups - 1);
     }
-    rg = lo;
     price();
     h = small_quotient(local - Hkv * before(rg), cost, Hkv - 1);
-    ustart = start[b] + Hkv * before(rg) + h * cost;
+    ustart = first + Hkv * before(rg) + h * cost;
   }
   __device__ __forceinline__ void advance(const PromptArgs& A) {  // to the next unit (there is one)
     ustart += cost;
@@ -336,9 +358,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   auto active1 = [&](const Piece& x) { return (2 * x.rg + 1) * npb < x.n; };
 
   // The softmax warps hold a row of S each: they get registers from the other
-  // warpgroups (128 * (2 * 168 + 96 + 80) = 512 * 128, what the block was launched with).
+  // warpgroups (128 * (2 * 160 + 96 + 96) = 512 * 128, what the block was launched with).
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     // ================================================================ softmax
     const int m = warp >> 2;
     const int row = tid & 127;  // row within the M tile = TMEM lane
@@ -472,7 +494,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   } else if (warp >= 12) {
     // ================================================================ epilogue
     // Writes a piece's rows while the softmax warps are in the next one.
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     const int row = tid & 127;  // row within an M tile = TMEM lane
     const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColO;
     const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
@@ -501,25 +523,30 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         uint16_t* orow = A.out + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D;
         float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + m * BM + row;
 #pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-          uint32_t o[32];
-          tmem_ld32(tO + m * D + q * 32, o);
+        for (int q = 0; q < 2; ++q) {  // 64 columns
+          uint32_t o[2][32];
+          tmem_ld32(tO + m * D + q * 64, o[0]);
+          tmem_ld32(tO + m * D + q * 64 + 32, o[1]);
           tmem_wait_ld();
-          if (whole) {
 #pragma unroll
-            for (int k = 0; k < 16; ++k)
-              o[k] = pack_bf16(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
-            if (vrow) {
-              st_global_32(orow + q * 32, o, wide);
-              st_global_32(orow + q * 32 + 16, o + 8, wide);
+          for (int e = 0; e < 2; ++e) {
+            if (whole) {
+              uint32_t v[16];
+#pragma unroll
+              for (int k = 0; k < 16; ++k)
+                v[k] = pack_bf16(__uint_as_float(o[e][2 * k]) * inv, __uint_as_float(o[e][2 * k + 1]) * inv);
+              if (vrow) {
+                st_global_32(orow + q * 64 + e * 32, v, wide);
+                st_global_32(orow + q * 64 + e * 32 + 16, v + 8, wide);
+              }
+            } else if (vrow) {
+              // a part of a unit: normalised O to the workspace, float4 columns [32][256 rows]
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                po[(q * 16 + e * 8 + k) * (2 * BM)] =
+                    make_float4(__uint_as_float(o[e][4 * k]) * inv, __uint_as_float(o[e][4 * k + 1]) * inv,
+                                __uint_as_float(o[e][4 * k + 2]) * inv, __uint_as_float(o[e][4 * k + 3]) * inv);
             }
-          } else if (vrow) {
-            // a part of a unit: normalised O to the workspace, float4 columns [32][256 rows]
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              po[(q * 8 + k) * (2 * BM)] =
-                  make_float4(__uint_as_float(o[4 * k]) * inv, __uint_as_float(o[4 * k + 1]) * inv,
-                              __uint_as_float(o[4 * k + 2]) * inv, __uint_as_float(o[4 * k + 3]) * inv);
           }
         }
         tc_fence_before();
@@ -677,29 +704,43 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       walk.B = A.batch;
       walk.Hkv = A.kv.heads_kv;
       walk.R = 2 * npb;
-      // Totals first: whether to cut units is chosen by them.  Whole units: as many
-      // rounds of the CTAs as it takes, of the longest unit's time; cut units: an even
-      // share and the merges.
-      auto positions = [&](int b, bool units, int* bad) -> int64_t {  // of sequence b
-        const Seq s = sequence(A, b, bad);
+      // Totals first: whether to cut units is chosen by them.
+      struct Size {
+        int64_t units, cost;
+      };
+      auto size_of = [&](const Seq& s) -> Size {  // a sequence's positions of both kinds
         const int64_t k = (s.n + walk.R - 1) / walk.R;
-        return walk.Hkv * (units ? k : k * (kUnitCost + s.L) + walk.R * k * (k + 1) / 2);
+        return {walk.Hkv * k, walk.Hkv * (k * (kUnitCost + s.L) + walk.R * k * (k + 1) / 2)};
+      };
+      auto scan = [&](int64_t v) -> int64_t {  // sum over the lanes up to this one
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+          const int64_t y = __shfl_up_sync(0xffffffffu, v, off);
+          if (lane >= off) v += y;
+        }
+        return v;
       };
       int64_t units = 0, cost = 0;
       int longest = 0;
-      for (int b = lane; b < A.batch; b += 32) {
-        int bad;
-        const Seq s = sequence(A, b, &bad);
-        if (bad && blockIdx.x == 0) flag(A.err, bad);
+      walk.few = A.batch <= 32;
+      for (int base = 0; base < A.batch; base += 32) {
+        const int b = base + lane;
+        Seq s{0, 0, 0};
+        if (b < A.batch) {
+          int bad;
+          s = sequence(A, b, &bad);
+          if (bad && blockIdx.x == 0) flag(A.err, bad);
+        }
+        walk.mine = s;
         if (s.n > 0) longest = max(longest, s.L + s.n);
-        units += positions(b, true, &bad);
-        cost += positions(b, false, &bad);
+        units += size_of(s).units;
+        cost += size_of(s).cost;
       }
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) {
-        units += __shfl_xor_sync(0xffffffffu, units, off);
-        cost += __shfl_xor_sync(0xffffffffu, cost, off);
-      }
+      const int64_t units_upto = scan(units), cost_upto = scan(cost);
+      walk.first_of_mine = units_upto - units;  // few: as whole units; else not used
+      const int64_t cost_first = cost_upto - cost;
+      units = __shfl_sync(0xffffffffu, units_upto, 31);
+      cost = __shfl_sync(0xffffffffu, cost_upto, 31);
       longest = __reduce_max_sync(0xffffffffu, longest);
       // Whole units: the longest one if every CTA has one at most, else an even share and,
       // on average over the CTAs that end last, half of the longest.  Cut units: an even
@@ -707,21 +748,24 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const float share = (float)cost / (float)gridDim.x;
       const float whole = units <= gridDim.x ? (float)(longest + kUnitCost) : share + 0.5f * (float)(longest + kUnitCost);
       walk.split = whole > 1.08f * share + kJoinCost;
-      int64_t run = 0;
-      for (int base = 0; base < A.batch; base += 32) {
-        const int b = base + lane;
-        int bad;
-        const int64_t own = b < A.batch ? positions(b, !walk.split, &bad) : 0;
-        int64_t upto = own;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-          const int64_t y = __shfl_up_sync(0xffffffffu, upto, off);
-          if (lane >= off) upto += y;
+      const int64_t run = walk.split ? cost : units;
+      if (walk.split) walk.first_of_mine = cost_first;
+      if (!walk.few) {
+        int64_t upto = 0;
+        for (int base = 0; base < A.batch; base += 32) {
+          const int b = base + lane;
+          int64_t own = 0;
+          if (b < A.batch) {
+            int bad;
+            const Size z = size_of(sequence(A, b, &bad));
+            own = walk.split ? z.cost : z.units;
+          }
+          const int64_t to = scan(own);
+          if (b < A.batch) start[b] = upto + to - own;
+          upto += __shfl_sync(0xffffffffu, to, 31);
         }
-        if (b < A.batch) start[b] = run + upto - own;
-        run += __shfl_sync(0xffffffffu, upto, 31);
+        __syncwarp();
       }
-      __syncwarp();
       // every CTA that takes part in cut units has a tile of each unit that its range lies in
       walk.P = (int)gridDim.x;
       if (walk.split) {
