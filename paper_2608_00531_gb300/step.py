@@ -9,6 +9,11 @@ on one stream:
 Inputs of a step (``StepInputs``) are the draft logits, the tree's target
 Q/K/V per layer and the target logits; the KV caches are persistent state
 owned by the caller.  Nothing here computes: every stage is a libcure call.
+The Q/K/V may come as the rows of each layer's fused projection instead; the
+step then norms and rotates them itself (``rope``).
+
+``PromptPass`` fills the caches that a step starts from: the attention layers
+of the target over packed prompts, chunks of prompts or single tokens.
 
 ``run_from_host`` takes the same inputs in (pinned) host memory and streams
 them in on a copy stream in the order the stages consume them (draft logits,
@@ -18,6 +23,7 @@ them.
 """
 from __future__ import annotations
 
+import contextlib
 import dataclasses
 from typing import List, Optional
 
@@ -36,6 +42,57 @@ class StepInputs:
     tree_k: torch.Tensor            # bf16 [layers][B][n_max][Hkv][D]
     tree_v: torch.Tensor            # bf16 [layers][B][n_max][Hkv][D]
     target_logits: torch.Tensor     # bf16 [B][n_max][V]
+    # bf16 [layers][B][n_max][(Hq + 2 Hkv) D]: Q, K and V as the projections give them, before the head norms and the
+    # rotation; q, tree_k and tree_v are then None
+    qkv: Optional[torch.Tensor] = None
+
+
+def _parts(qkv: torch.Tensor, heads_q: int, heads_kv: int, head_dim: int):
+    """q, k and v [...][heads][D] within the rows of a fused projection."""
+    if qkv.shape[-1] != (heads_q + 2 * heads_kv) * head_dim:
+        raise ValueError("a projection's rows must hold (heads_q + 2 heads_kv) heads")
+    x = qkv.unflatten(-1, (-1, head_dim))
+    return (x[..., :heads_q, :], x[..., heads_q:heads_q + heads_kv, :], x[..., heads_q + heads_kv:, :])
+
+
+def _of_layer(norms, l: int):
+    return None if norms is None else norms[l]
+
+
+class PromptPass:
+    """The target's attention layers over packed rows (Alg. 1's input): per layer the head norms and the rotation,
+    K and V behind what the cache holds, and causal attention over the cache.
+
+    Sequence b's rows row_start[b] .. row_start[b+1] - 1 stand at positions cache_len[b], cache_len[b] + 1, ..; all
+    layers run at the same lengths, and ``advance`` gives the lengths after the pass.  q_norm, k_norm: a weight
+    (bf16 [D]) per layer, or None."""
+
+    def __init__(self, rows: int, batch: int, heads_q: int, kv: cure.KVDesc, rope: Optional[cure.Rope],
+                 device: torch.device, q_norm=None, k_norm=None, eps: float = 1e-6):
+        self.rows, self.B, self.Hq, self.kv, self.rope = rows, batch, heads_q, kv, rope
+        self.q_norm, self.k_norm, self.eps = q_norm, k_norm, eps
+        self.scale = 1.0 / float(kv.head_dim) ** 0.5
+        self.q = torch.empty(rows, heads_q, kv.head_dim, dtype=torch.bfloat16, device=device)
+        ws = cure.cure_prompt_attn_workspace_size(rows, batch, heads_q, kv)
+        self.workspace = torch.empty(max(ws, 256), dtype=torch.uint8, device=device)
+
+    def layer(self, l: int, qkv: torch.Tensor, row_start: torch.Tensor, cache_len: torch.Tensor, k_cache: torch.Tensor,
+              v_cache: torch.Tensor, *, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Layer l: qkv bf16 [rows][(Hq + 2 Hkv) D] -> attention output [rows][Hq][D]; the cache gains the rows."""
+        n = qkv.shape[0]
+        if n > self.rows:
+            raise ValueError(f"PromptPass was made for {self.rows} rows, got {n}")
+        q, k, v = _parts(qkv, self.Hq, self.kv.heads_kv, self.kv.head_dim)
+        q = cure.cure_append_kv(k, v, k_cache, v_cache, self.kv, row_start, cache_len, self.rope, q=q,
+                                q_norm=_of_layer(self.q_norm, l), k_norm=_of_layer(self.k_norm, l), eps=self.eps,
+                                out=self.q[:n], stream=stream)
+        return cure.cure_prompt_attn(q, k_cache, v_cache, self.kv, row_start, cache_len, self.scale, out=out,
+                                     workspace=self.workspace, stream=stream)
+
+    @staticmethod
+    def advance(row_start: torch.Tensor, cache_len: torch.Tensor) -> torch.Tensor:
+        """The lengths behind the appended rows."""
+        return cache_len + (row_start[1:] - row_start[:-1])
 
 
 class RepairVerifyStep:
@@ -44,7 +101,8 @@ class RepairVerifyStep:
 
     def __init__(self, batch: int, block: int, vocab: int, topk: int, tau: float, budget: int,
                  branches: int, repair_depth: int, layers: int, heads_q: int, kv: cure.KVDesc,
-                 device: torch.device, max_ufp: int = 0, layer_map: Optional[List[int]] = None):
+                 device: torch.device, max_ufp: int = 0, layer_map: Optional[List[int]] = None,
+                 rope: Optional[cure.Rope] = None, q_norm=None, k_norm=None, eps: float = 1e-6):
         self.B, self.K, self.V, self.k = batch, block, vocab, topk
         self.tau, self.R, self.branches, self.depth = tau, budget, branches, repair_depth
         self.max_ufp = max_ufp
@@ -78,6 +136,9 @@ class RepairVerifyStep:
         self.rs = dict(draft_valid_len=torch.empty(B, **i32), replay_tokens=torch.empty(B, P, **i32),
                        n_replay=torch.empty(B, **i32))
         self.cache_len_out = torch.empty(B, **i32)
+        # for inputs that come as projections: the rotation, norm weights per layer, and the rows made of them
+        self.rope, self.q_norm, self.k_norm, self.eps = rope, q_norm, k_norm, eps
+        self._rows = None
         self._dev_inputs = None
         self._copy_stream = None
         self._n_host = None
@@ -92,6 +153,8 @@ class RepairVerifyStep:
                                     out=self.tree, stream=stream)
         kl = [k_caches[self.layer_map[l]] for l in range(self.layers)]
         vl = [v_caches[self.layer_map[l]] for l in range(self.layers)]
+        if x.qkv is not None:
+            x = self._rotate(x, tree["pos"], stream)
         if all(isinstance(t, torch.Tensor) and t.is_contiguous() and t.dim() == 5 and t.shape[0] == self.layers
                for t in (x.q, x.tree_k, x.tree_v)):
             cure.cure_tree_attn_layers(x.q, x.tree_k, x.tree_v, kl, vl, self.kv, x.cache_len, tree["n_nodes"],
@@ -107,6 +170,23 @@ class RepairVerifyStep:
                                  cache_len_out=self.cache_len_out, out=self.rs, stream=stream)
         return dict(score=self.score, tree=tree, attn=self.attn_out, acc=acc, resync=rs)
 
+    def _rotate(self, x: StepInputs, pos: torch.Tensor, stream) -> StepInputs:
+        """The step's Q/K/V from the layers' projections at the tree's positions (rows past a sequence's nodes
+        keep what they held)."""
+        if x.qkv.shape[:3] != (self.layers, self.B, self.n_max):
+            raise ValueError("qkv must be [layers][batch][n_max][..]")
+        if self._rows is None:
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+                self._rows = [torch.zeros(self.layers, self.B, self.n_max, h, self.D, dtype=torch.bfloat16,
+                                          device=self.attn_out.device)
+                              for h in (self.Hq, self.kv.heads_kv, self.kv.heads_kv)]
+        for l in range(self.layers):
+            cure.cure_rope_qkv(*_parts(x.qkv[l], self.Hq, self.kv.heads_kv, self.D), pos, self.rope,
+                               q_norm=_of_layer(self.q_norm, l), k_norm=_of_layer(self.k_norm, l), eps=self.eps,
+                               out=tuple(t[l] for t in self._rows), stream=stream)
+        q, tk, tv = self._rows
+        return dataclasses.replace(x, q=q, tree_k=tk, tree_v=tv, qkv=None)
+
     def run_from_host(self, xh: StepInputs, k_caches: List[torch.Tensor], v_caches: List[torch.Tensor],
                       stream=None) -> dict:
         """One step with its inputs in host memory (pinned, for copies that
@@ -118,6 +198,8 @@ class RepairVerifyStep:
         node counts back before it queues those copies, behind the layers'
         Q/K/V.  Smaller ones are copied whole, without that read-back.
         Results stay on the device, as in run()."""
+        if xh.qkv is not None:
+            raise ValueError("run_from_host takes q, tree_k and tree_v, not the layers' projections")
         fields = ("draft_logits", "root_tok", "cache_len", "q", "tree_k", "tree_v", "target_logits")
         dev = self.attn_out.device
         if self._dev_inputs is None or any(self._dev_inputs[f].shape != getattr(xh, f).shape for f in fields):
@@ -197,5 +279,6 @@ class RepairVerifyStep:
     def launches_per_step(self) -> int:
         """Library kernels one step launches: scan, tree, one attention kernel per
         layer, target argmax + walk, and the resync gather (its finalize runs in
-        the gather's grid, since the step's new lengths do not alias the old)."""
+        the gather's grid, since the step's new lengths do not alias the old).
+        Inputs that come as projections take one more per layer."""
         return 1 + 1 + self.layers + 2 + 1

@@ -277,6 +277,24 @@ def test_prompt_agrees_with_the_tree_attention(cure):
     _check(x, tree.view(B * n, Hq, D))
 
 
+def test_prompt_output_aligned_to_16_bytes_only(cure):
+    """32-byte stores need 32-byte alignment; an output that is aligned to 16 bytes gets the same bits."""
+    x = _case(cure, [0, 300], [150, 40], 8, 2, 16, 41)
+    want = _run(cure, x)
+    buf = torch.full((want.numel() + 8,), 3.5, dtype=torch.bfloat16, device=DEV)
+    got = _run(cure, x, out=buf[8:].view(want.shape))
+    assert got.data_ptr() % 32 == 16 and torch.equal(got, want) and torch.all(buf[:8] == 3.5)
+
+
+def test_prompt_whole_and_cut_units(cure):
+    """Shapes on both sides of the choice: many short units, few long ones, one CTA's worth, long and short together."""
+    for n, lens, Hq, Hkv in (([300] * 40, [0] * 40, 28, 4), ([900] * 3, [5000, 0, 20000], 7, 1), ([5], [0], 1, 1),
+                             ([1500, 1, 3, 700], [0, 40000, 9000, 10], 32, 8), ([33] * 200, [100] * 200, 4, 4)):
+        x = _case(cure, lens, n, Hq, Hkv, 16, sum(n))
+        _check(x, _run(cure, x), rows=[0, 1, 31, 200, 299, 650, 899, 1499, -1])
+    assert cure.cure_device_error() == 0
+
+
 def test_prompt_binding_refusals(cure):
     x = _case(cure, [0, 5], [4, 3], 8, 2, 16, 37)
     args = [x["q"], x["kc"], x["vc"], x["kv"], x["row_start"], x["cache_len"], SCALE]
