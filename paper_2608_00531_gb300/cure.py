@@ -15,6 +15,8 @@ import torch
 from . import _lib
 from ._lib import KVDesc, Rope, RopeScaling, TreeParams, check
 
+_BF16, _I32 = torch.bfloat16, torch.int32
+
 DEVERR_PAGE, DEVERR_SLOT, DEVERR_NODES = _lib.DEVERR_PAGE, _lib.DEVERR_SLOT, _lib.DEVERR_NODES
 
 
@@ -342,10 +344,8 @@ def rope_desc(rot_dim: int = 128, base: float = 10000.0, *, style: str = "half",
     return r
 
 
-def _here(t: Optional[torch.Tensor], name: str, dtype, dev: int) -> Optional[int]:
+def _here(t: torch.Tensor, name: str, dtype, dev: int) -> int:
     """_p() of a tensor that must also be on device `dev` and of a type."""
-    if t is None:
-        return None
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.get_device() != dev:
@@ -365,7 +365,7 @@ def _new(shape, dtype, stream) -> torch.Tensor:
 
 def _current(stream) -> tuple[int, int]:
     """The current device, and the handle of `stream` (None: the current one), which must be on it."""
-    dev = torch.cuda.current_device()
+    dev = torch._C._cuda_getDevice()
     if stream is None:
         return dev, torch._C._cuda_getCurrentRawStream(dev)
     if stream.device_index != dev:
@@ -374,35 +374,36 @@ def _current(stream) -> tuple[int, int]:
 
 
 def _head_rows(t: torch.Tensor, name: str, dev: int):
-    """(address, values from row to row, (rows, heads, head_dim)) of bf16 [...][heads][D]: heads end to end, the
-    leading dimensions one even step apart, as in a part of a fused projection's rows."""
-    if t.dtype is not torch.bfloat16:
+    """(address, values from row to row, rows, heads, head_dim) of bf16 [...][heads][D]: heads end to end, the
+    leading dimensions one even step apart, as in a part of a fused projection's rows.  (Written for few
+    attribute reads: a small call's host work outlasts its kernel.)"""
+    if t.dtype is not _BF16:
         raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
     if t.get_device() != dev:
         raise ValueError(f"{name} must be on the current CUDA device")
     sh = t.shape
     if len(sh) == 3:
         rows, H, D = sh
+        outer, inner = 1, rows
     elif len(sh) == 4:
         outer, inner, H, D = sh
         rows = outer * inner
     else:
         raise ValueError(f"{name} must be [rows][heads][head_dim] or [batch][rows][heads][head_dim]")
-    if rows <= 1 or t.is_contiguous():
-        ld = H * D
-        if rows == 0 or t.is_contiguous():
-            return t.data_ptr(), ld, (rows, H, D)
+    ld = H * D
+    if t.is_contiguous():
+        return t.data_ptr(), ld, rows, H, D
     st = t.stride()
     if rows > 1:
-        ld = st[-3] if len(sh) == 3 or inner > 1 else st[0]
-        if len(sh) == 4 and outer > 1 and inner > 1 and st[0] != inner * ld:
+        ld = st[-3] if inner > 1 else st[0]
+        if outer > 1 and inner > 1 and st[0] != inner * ld:
             raise ValueError(f"{name}: rows must lie one even step apart")
     if (D > 1 and st[-1] != 1) or (H > 1 and st[-2] != D):
         raise ValueError(f"{name}: a row's heads must lie end to end")
-    return t.data_ptr(), ld, (rows, H, D)
+    return t.data_ptr(), ld, rows, H, D
 
 
-_NO_ROWS = (None, 0, (0, 0, 0))
+_NO_ROWS = (None, 0, 0, 0, 0)
 
 
 def cure_rope_qkv(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor],
@@ -417,44 +418,40 @@ def cure_rope_qkv(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optio
     dev, s = _current(stream)
     if out is None:
         out = tuple(None if t is None else _new(t.shape, t.dtype, stream) for t in (q, k, v))
+    qo, ko, vo = out
     rows = pos.numel()
-    heads, args, D = [0, 0, 0], [], 128
-    for i, (t, o, nm) in enumerate(zip((q, k, v), out, "qkv")):
-        if t is None or o is None:
-            if t is not o:
-                raise ValueError(f"cure_rope_qkv: {nm} without its output, or an output without {nm}")
-            args.append((None, 0, None, 0))
-            continue
-        pi, li, shape = _head_rows(t, nm, dev)
-        po, lo, shape_o = _head_rows(o, "an output", dev)
-        if shape != shape_o or shape[0] != rows:
-            raise ValueError(f"cure_rope_qkv: {nm}, its output and pos must have the same rows and heads")
-        heads[i], D = shape[1], shape[2]
-        args.append((pi, li, po, lo))
-    (pq, lq, oq, loq), (pk, lk, ok, lok), (pv, lv, ov, lov) = args
-    if pk is not None and pv is not None and heads[1] != heads[2]:
-        raise ValueError("cure_rope_qkv: k and v must have the same heads")
-    if any(t is not None and t.shape[-1] != D for t in (q, k, v)):
-        raise ValueError("cure_rope_qkv: q, k and v must have one head_dim")
+    pq, lq, nq, hq, dq = _NO_ROWS if q is None else _head_rows(q, "q", dev)
+    pk, lk, nk, hk, dk = _NO_ROWS if k is None else _head_rows(k, "k", dev)
+    pv, lv, nv, hv, dv = _NO_ROWS if v is None else _head_rows(v, "v", dev)
+    oq, loq, noq, hoq, doq = _NO_ROWS if qo is None else _head_rows(qo, "q's output", dev)
+    ok, lok, nok, hok, dok = _NO_ROWS if ko is None else _head_rows(ko, "k's output", dev)
+    ov, lov, nov, hov, dov = _NO_ROWS if vo is None else _head_rows(vo, "v's output", dev)
+    if nq != noq or nk != nok or nv != nov or hq != hoq or hk != hok or hv != hov or dq != doq or dk != dok or dv != dov:
+        raise ValueError("cure_rope_qkv: an output must have its input's rows and heads")
+    D = dq or dk or dv or 128
+    if (q is not None and (nq != rows or dq != D)) or (k is not None and (nk != rows or dk != D)) or (
+            v is not None and (nv != rows or dv != D or (k is not None and hv != hk))):
+        raise ValueError("cure_rope_qkv: q, k, v and pos must have the same rows, k and v the same heads, and all one "
+                         "head_dim")
     check("cure_rope_qkv", _lib.load().cure_rope_qkv(
-        pq, pk, pv, lq, lk, lv, rows, heads[0], heads[1] or heads[2], D, _here(pos, "pos", torch.int32, dev),
-        None if rope is None else C.byref(rope), _norm(q_norm, "q_norm", dev), _norm(k_norm, "k_norm", dev), eps,
-        oq, ok, ov, loq, lok, lov, s))
+        pq, pk, pv, lq, lk, lv, rows, hq, hk or hv, D, _here(pos, "pos", _I32, dev),
+        None if rope is None else C.byref(rope), None if q_norm is None else _norm(q_norm, "q_norm", dev),
+        None if k_norm is None else _norm(k_norm, "k_norm", dev), eps, oq, ok, ov, loq, lok, lov, s))
     return out
 
 
-def _norm(w: Optional[torch.Tensor], name: str, dev: int) -> Optional[int]:
-    if w is not None and w.numel() != 128:
+def _norm(w: torch.Tensor, name: str, dev: int) -> int:
+    if w.numel() != 128:
         raise ValueError(f"{name} must hold one weight for each of a head's 128 values")
-    return _here(w, name, torch.bfloat16, dev)
+    return _here(w, name, _BF16, dev)
 
 
-def _cache_fits(t: torch.Tensor, kv: KVDesc, batch: int, name: str, dev: int) -> int:
-    """_here() of a cache that holds what its geometry says."""
-    rows = batch * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size
-    if t.numel() < rows * kv.heads_kv * kv.head_dim:
-        raise ValueError(f"{name} is smaller than its geometry")
-    return _here(t, name, torch.bfloat16, dev)
+def _caches(k: torch.Tensor, v: torch.Tensor, kv: KVDesc, batch: int, dev: int) -> tuple[int, int]:
+    """Addresses of a layer's caches, which must hold what their geometry says."""
+    size = (batch * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size) * kv.heads_kv * kv.head_dim
+    if k.numel() < size or v.numel() < size:
+        raise ValueError("a cache is smaller than its geometry")
+    return _here(k, "k_cache", _BF16, dev), _here(v, "v_cache", _BF16, dev)
 
 
 def _ragged(row_start: torch.Tensor, cache_len: torch.Tensor, kv: KVDesc) -> int:
@@ -480,28 +477,28 @@ def cure_append_kv(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
     advanced.  In-place tree rows: row_start = 0, n_max, 2 n_max, .., pos = the tree's ``pos``."""
     dev, s = _current(stream)
     B = _ragged(row_start, cache_len, kv)
-    pk, lk, shape = _head_rows(k, "k", dev)
-    pv, lv, shape_v = _head_rows(v, "v", dev)
-    rows = shape[0]
-    if shape != shape_v or shape[1] != kv.heads_kv or shape[2] != kv.head_dim:
+    Hkv, D = kv.heads_kv, kv.head_dim
+    pk, lk, rows, hk, dk = _head_rows(k, "k", dev)
+    pv, lv, nv, hv, dv = _head_rows(v, "v", dev)
+    if nv != rows or hk != Hkv or hv != Hkv or dk != D or dv != D:
         raise ValueError("cure_append_kv: k and v must have the same rows, the cache's heads and its head_dim")
     if q is None:
-        out, (pq, lq, shape_q), (po, lo, _) = None, _NO_ROWS, _NO_ROWS
+        out, (pq, lq, _, hq, _), (po, lo, _, _, _) = None, _NO_ROWS, _NO_ROWS
     else:
         if out is None:
             out = _new(q.shape, q.dtype, stream)
-        pq, lq, shape_q = _head_rows(q, "q", dev)
-        po, lo, shape_o = _head_rows(out, "out", dev)
-        if shape_q != shape_o or shape_q[0] != rows or shape_q[2] != kv.head_dim:
+        pq, lq, nq, hq, dq = _head_rows(q, "q", dev)
+        po, lo, no, ho, do = _head_rows(out, "out", dev)
+        if nq != rows or no != rows or ho != hq or dq != D or do != D:
             raise ValueError("cure_append_kv: q, its output and k must have the same rows and head_dim")
     if pos is not None and pos.numel() != rows:
         raise ValueError("cure_append_kv: pos must have an entry for every row")
+    kc, vc = _caches(k_cache, v_cache, kv, B, dev)
     check("cure_append_kv", _lib.load().cure_append_kv(
-        pq, pk, pv, lq, lk, lv, rows, shape_q[1], B, _here(row_start, "row_start", torch.int32, dev),
-        _here(cache_len, "cache_len", torch.int32, dev), _here(pos, "pos", torch.int32, dev), C.byref(kv),
-        _cache_fits(k_cache, kv, B, "k_cache", dev), _cache_fits(v_cache, kv, B, "v_cache", dev),
-        None if rope is None else C.byref(rope), _norm(q_norm, "q_norm", dev), _norm(k_norm, "k_norm", dev), eps, po,
-        lo, s))
+        pq, pk, pv, lq, lk, lv, rows, hq, B, _here(row_start, "row_start", _I32, dev),
+        _here(cache_len, "cache_len", _I32, dev), None if pos is None else _here(pos, "pos", _I32, dev), C.byref(kv),
+        kc, vc, None if rope is None else C.byref(rope), None if q_norm is None else _norm(q_norm, "q_norm", dev),
+        None if k_norm is None else _norm(k_norm, "k_norm", dev), eps, po, lo, s))
     return out
 
 
@@ -529,11 +526,11 @@ def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     if workspace is None:
         size = cure_prompt_attn_workspace_size(shape[0], B, shape[1], kv)
         workspace = _new((max(size, 256),), torch.uint8, stream)
+    kc, vc = _caches(k_cache, v_cache, kv, B, dev)
     check("cure_prompt_attn", _lib.load().cure_prompt_attn(
-        _here(q, "q", torch.bfloat16, dev), _cache_fits(k_cache, kv, B, "k_cache", dev),
-        _cache_fits(v_cache, kv, B, "v_cache", dev), C.byref(kv), _here(row_start, "row_start", torch.int32, dev),
-        _here(cache_len, "cache_len", torch.int32, dev), shape[0], B, shape[1], scale,
-        _here(out, "out", torch.bfloat16, dev), _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s))
+        _here(q, "q", _BF16, dev), kc, vc, C.byref(kv), _here(row_start, "row_start", _I32, dev),
+        _here(cache_len, "cache_len", _I32, dev), shape[0], B, shape[1], scale, _here(out, "out", _BF16, dev),
+        _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s))
     return out
 
 
