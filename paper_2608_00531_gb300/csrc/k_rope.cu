@@ -213,6 +213,7 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         const int hh = h0 + 2 * u + half;
+        if (h0 + 2 * u >= b) break;
         uint64_t va[2], vb[2], ya[2], yb[2];
         unpack<INTER>(x[u], va, vb);
 #pragma unroll
