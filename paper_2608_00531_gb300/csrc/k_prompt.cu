@@ -101,6 +101,9 @@ constexpr int kUnitCost = 2 * BN;
 // What joining the parts of units costs a call, and the fewest positions worth a CTA.
 constexpr int kJoinCost = 8 * BN;
 constexpr int kMinShare = 3 * BN;
+// Units of fewer positions on average, and those of a batch of more than 32, are
+// dealt out in turn: the reckoning that evens them out would take longer than they do.
+constexpr int kShortUnit = kUnitCost + 5 * BN;
 // A share's border that lies nearer to a unit's border than this moves there.
 constexpr int kSnap = 4 * BN;
 
@@ -141,47 +144,51 @@ __device__ __forceinline__ int small_quotient(int64_t a, int64_t b, int most) {
 
 // The units of a call, laid end to end, as the scheduler warp walks them.  Either
 // they are cut (positions as above, an even share of them for every CTA) or they
-// are dealt out whole in turn, one position each.
+// are dealt out whole, one position each; `falling`: the long ones first, the
+// sequences in the order of their lengths, their row groups from the last one down.
 //
 // A batch of up to 32 sequences stays in the warp's registers, a sequence a lane;
 // of a larger one the first positions lie in shared memory and the rest is read
 // again.  (A call's first piece was 5,000 cycles away, most of it dependent loads.)
 struct Walk {
-  const int64_t* start;  // first position of each sequence (large batches)
-  bool few;
-  Seq mine;              // few: the lane's sequence and its first position
+  const int64_t* start;   // large batches: first position of each sequence
+  bool few, falling;
+  Seq mine;               // few: the lane's sequence, its number and its first position
+  int number_of_mine;
   int64_t first_of_mine;
-  int B, Hkv, R;         // R: rows of a row group
+  int B, Hkv, R;          // R: rows of a row group
   bool split;
-  int P;                 // CTAs that take part
-  int64_t share;         // positions of one CTA (the last one takes the rest)
-  int64_t near;          // how far a share's border moves to a unit's border at most
-  // the unit at position ustart
+  int P;                  // CTAs that take part
+  int64_t share;          // positions of one CTA (the last one takes the rest)
+  int64_t near;           // how far a share's border moves to a unit's border at most
+  // the unit at position ustart: sequence i (number b), the k-th row group, head h
   Seq s;
-  int b, rg, h, groups;
+  int i, b, k, h, groups;
   int64_t ustart, cost;
 
-  __device__ __forceinline__ int64_t before(int k) const {  // positions of a head's row groups 0 .. k - 1
+  __device__ __forceinline__ int64_t before(int k) const {  // positions of a head's first k row groups
     return split ? k * (int64_t)(kUnitCost + s.L) + (int64_t)R * k * (k + 1) / 2 : k;
   }
   __device__ __forceinline__ int owner(int64_t p) const { return small_quotient(p, share, P - 1); }
   __device__ __forceinline__ void load(const PromptArgs& A) {
     if (few) {
-      s.r0 = __shfl_sync(0xffffffffu, mine.r0, b);
-      s.n = __shfl_sync(0xffffffffu, mine.n, b);
-      s.L = __shfl_sync(0xffffffffu, mine.L, b);
+      s.r0 = __shfl_sync(0xffffffffu, mine.r0, i);
+      s.n = __shfl_sync(0xffffffffu, mine.n, i);
+      s.L = __shfl_sync(0xffffffffu, mine.L, i);
+      b = __shfl_sync(0xffffffffu, number_of_mine, i);
     } else {
       int bad;
+      b = i;
       s = sequence(A, b, &bad);
     }
     groups = (s.n + R - 1) / R;
   }
-  __device__ __forceinline__ void price() { cost = split ? kUnitCost + s.L + (int64_t)(rg + 1) * R : 1; }
+  __device__ __forceinline__ void price() { cost = split ? kUnitCost + s.L + (int64_t)(k + 1) * R : 1; }
   __device__ __forceinline__ void seek(const PromptArgs& A, int64_t g) {  // the unit that holds position g
     int64_t first;  // of the last sequence that starts at or before it
     if (few) {
-      b = __popc(__ballot_sync(0xffffffffu, (int)(threadIdx.x & 31) < B && first_of_mine <= g)) - 1;
-      first = __shfl_sync(0xffffffffu, first_of_mine, b);
+      i = __popc(__ballot_sync(0xffffffffu, (int)(threadIdx.x & 31) < B && first_of_mine <= g)) - 1;
+      first = __shfl_sync(0xffffffffu, first_of_mine, i);
     } else {
       int lo = 0, hi = B;
       while (hi - lo > 1) {
@@ -189,38 +196,39 @@ struct Walk {
         if (start[mid] <= g) lo = mid;
         else hi = mid;
       }
-      b = lo;
-      first = start[b];
+      i = lo;
+      first = start[i];
     }
     load(A);
     const int64_t local = g - first;
-    // the last row group that starts at or before it: local = Hkv before(rg)
+    // the last row group that starts at or before it: local = Hkv before(k)
     if (split) {
       const float each = (float)(kUnitCost + s.L) + 0.5f * (float)R, l = (float)local / (float)Hkv;
-      rg = min(groups - 1, (int)(2.f * l / (each + sqrtf(each * each + 2.f * (float)R * l))));  // off by one at most
-      if (rg > 0 && Hkv * before(rg) > local) --rg;
-      if (rg < groups - 1 && Hkv * before(rg + 1) <= local) ++rg;
+      k = min(groups - 1, (int)(2.f * l / (each + sqrtf(each * each + 2.f * (float)R * l))));  // off by one at most
+      if (k > 0 && Hkv * before(k) > local) --k;
+      if (k < groups - 1 && Hkv * before(k + 1) <= local) ++k;
     } else {
-      rg = small_quotient(local, Hkv, groups - 1);
+      k = small_quotient(local, Hkv, groups - 1);
     }
     price();
-    h = small_quotient(local - Hkv * before(rg), cost, Hkv - 1);
-    ustart = first + Hkv * before(rg) + h * cost;
+    h = small_quotient(local - Hkv * before(k), cost, Hkv - 1);
+    ustart = first + Hkv * before(k) + h * cost;
   }
   __device__ __forceinline__ void advance(const PromptArgs& A) {  // to the next unit (there is one)
     ustart += cost;
     if (++h < Hkv) return;
     h = 0;
-    if (++rg == groups) {
-      rg = 0;
+    if (++k == groups) {
+      k = 0;
       do {
-        ++b;
+        ++i;
         load(A);
-      } while (groups == 0 && b + 1 < B);
+      } while (groups == 0 && i + 1 < B);
     }
     price();
   }
-  __device__ __forceinline__ int keys() const { return s.L + min((rg + 1) * R, s.n); }
+  __device__ __forceinline__ int row_group() const { return falling ? groups - 1 - k : k; }
+  __device__ __forceinline__ int keys() const { return s.L + min((row_group() + 1) * R, s.n); }
   __device__ __forceinline__ int tiles() const { return (keys() + BN - 1) / BN; }
   // Where the border p of a share, which lies in this unit, is drawn: at one of the
   // unit's borders if that is near (or if one side would be left without a tile).
@@ -235,7 +243,7 @@ struct Walk {
     Piece x;
     x.b = b;
     x.h = h;
-    x.rg = rg;
+    x.rg = row_group();
     x.r0 = s.r0;
     x.n = s.n;
     x.L = s.L;
@@ -720,54 +728,93 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         }
         return v;
       };
+      // A sequence a lane (of a large batch the last 32), and the totals.
       int64_t units = 0, cost = 0;
       int longest = 0;
+      Seq own{0, 0, 0};
       walk.few = A.batch <= 32;
       for (int base = 0; base < A.batch; base += 32) {
         const int b = base + lane;
-        Seq s{0, 0, 0};
+        own = Seq{0, 0, 0};
         if (b < A.batch) {
           int bad;
-          s = sequence(A, b, &bad);
+          own = sequence(A, b, &bad);
           if (bad && blockIdx.x == 0) flag(A.err, bad);
         }
-        walk.mine = s;
-        if (s.n > 0) longest = max(longest, s.L + s.n);
-        units += size_of(s).units;
-        cost += size_of(s).cost;
+        if (own.n > 0) longest = max(longest, own.L + own.n);
+        units += size_of(own).units;
+        cost += size_of(own).cost;
       }
-      const int64_t units_upto = scan(units), cost_upto = scan(cost);
-      walk.first_of_mine = units_upto - units;  // few: as whole units; else not used
-      const int64_t cost_first = cost_upto - cost;
-      units = __shfl_sync(0xffffffffu, units_upto, 31);
-      cost = __shfl_sync(0xffffffffu, cost_upto, 31);
+      units = __shfl_sync(0xffffffffu, scan(units), 31);
+      cost = __shfl_sync(0xffffffffu, scan(cost), 31);
       longest = __reduce_max_sync(0xffffffffu, longest);
-      // Whole units: the longest one if every CTA has one at most, else an even share and,
-      // on average over the CTAs that end last, half of the longest.  Cut units: an even
-      // share, which the pieces' fixed costs upset by some 8 %, and the joins.
-      const float share = (float)cost / (float)gridDim.x;
-      const float whole = units <= gridDim.x ? (float)(longest + kUnitCost) : share + 0.5f * (float)(longest + kUnitCost);
-      walk.split = whole > 1.08f * share + kJoinCost;
-      const int64_t run = walk.split ? cost : units;
-      if (walk.split) walk.first_of_mine = cost_first;
-      if (!walk.few) {
+      walk.P = (int)gridDim.x;
+      int64_t run = 0;  // positions
+      auto lay_out = [&](bool split, bool falling) {
+        walk.split = split;
+        walk.falling = falling;
+        run = split ? cost : units;
+        if (walk.few) {
+          int from = lane;
+          if (falling) {  // the lane whose sequence comes lane-th
+            const int length = own.n > 0 ? own.L + own.n : 0;
+            int rank = 0;
+#pragma unroll 1
+            for (int l = 0; l < 32; ++l) {
+              const int o = __shfl_sync(0xffffffffu, length, l);
+              rank += o > length || (o == length && l < lane);
+            }
+#pragma unroll 1
+            for (int l = 0; l < 32; ++l)
+              if (__shfl_sync(0xffffffffu, rank, l) == lane) from = l;
+          }
+          walk.mine.r0 = __shfl_sync(0xffffffffu, own.r0, from);
+          walk.mine.n = __shfl_sync(0xffffffffu, own.n, from);
+          walk.mine.L = __shfl_sync(0xffffffffu, own.L, from);
+          walk.number_of_mine = from;
+          const Size z = size_of(walk.mine);
+          walk.first_of_mine = scan(split ? z.cost : z.units) - (split ? z.cost : z.units);
+          return;
+        }
         int64_t upto = 0;
         for (int base = 0; base < A.batch; base += 32) {
           const int b = base + lane;
-          int64_t own = 0;
+          int64_t v = 0;
           if (b < A.batch) {
             int bad;
             const Size z = size_of(sequence(A, b, &bad));
-            own = walk.split ? z.cost : z.units;
+            v = split ? z.cost : z.units;
           }
-          const int64_t to = scan(own);
-          if (b < A.batch) start[b] = upto + to - own;
+          const int64_t to = scan(v);
+          if (b < A.batch) start[b] = upto + to - v;
           upto += __shfl_sync(0xffffffffu, to, 31);
         }
         __syncwarp();
+      };
+      // Which is faster, in positions.  Whole units end with the longest one if every CTA has
+      // one at most.  In turn they end with an even share and, in the CTAs that end last,
+      // half of the longest one.  Longest first they end with an even share, or with the
+      // (k + 1)-th round of units as long as those that it starts with; some 3 % more.  Cut
+      // units end with an even share, which the pieces' fixed costs upset by some 8 %, and
+      // the joins.
+      const float share = (float)cost / (float)walk.P;
+      const float cut = 1.08f * share + kJoinCost;
+      float whole = (float)(longest + kUnitCost);
+      const bool in_turn = units <= walk.P || !walk.few || cost < units * kShortUnit;
+      if (in_turn || whole > cut) {
+        if (units > walk.P) whole = share + 0.5f * whole;
+        lay_out(whole > cut, false);
+      } else {
+        lay_out(false, true);
+        whole = fmaxf(whole, share);
+#pragma unroll 1
+        for (int r = 1; r < 4 && (int64_t)r * walk.P < units; ++r) {
+          walk.seek(A, (int64_t)r * walk.P);
+          whole = fmaxf(whole, (float)(r + 1) * (float)(walk.keys() + kUnitCost));
+        }
+        if (1.03f * whole > cut) lay_out(true, false);
       }
       // every CTA that takes part in cut units has a tile of each unit that its range lies in
-      walk.P = (int)gridDim.x;
       if (walk.split) {
         if (share < (float)kMinShare) walk.P = max(1, (int)((float)run / (float)kMinShare));
         walk.share = (int64_t)((float)run / (float)walk.P * 0.999999f);
@@ -788,37 +835,85 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         __syncwarp();
         return true;
       };
-      // Whole units: every P-th.  Cut ones: the first and the last piece of the range, which
-      // may be parts of units, come first, so that parts are joined while the CTAs are in
-      // later pieces; then the units between.
       const int c = (int)blockIdx.x;
-      int64_t g = walk.split ? c * walk.share : c, g_end = run, last = run;
-      int64_t at = walk.split && c < walk.P - 1 ? g + walk.share : g;
-      Piece tail{};
-      for (int step = at > g ? 0 : 1;; ++step) {
-        bool end = c >= walk.P || at >= run;
-        if (!end && walk.split && step == 2) {
-          x = tail;
-          if (walk.ustart >= last) end = true;  // the range lies in one unit
-        } else if (!end) {
-          if (!walk.split || step < 2) walk.seek(A, at);
-          else if (walk.ustart + walk.cost >= last) end = true;
-          else walk.advance(A);
-          if (walk.split && step == 0) {  // the range's end: `last` is the unit that it lies in
-            g_end = walk.border(at);
-            last = walk.ustart;
-            tail = walk.within(last, g_end);
-            at = g;
-            continue;
+      bool ok = true;
+      if (!walk.split) {
+        // Whole units, every P-th; or longest first, the first ones by number and then in
+        // chunks of `team` units for a team of neighbouring CTAs, each chunk to the team that
+        // has the least to do by then: every CTA follows the same reckoning.  Neighbours take
+        // units side by side (the same rows' other heads, the same head's other rows): SMs
+        // close to each other get the same K and V tiles faster, 8 to 12 % of a tile's time.
+        // 32 ragged prompts of 64/8 heads: 334 us so, 355 every P-th (the busiest CTA 15 %
+        // above the mean); 64 prompts of 300: 105 so, 98 every P-th.
+        const int team = min(8, walk.P), teams = min(32, walk.P / team);
+        if (!walk.falling) {
+          for (int64_t u = c; ok && u < run; u += walk.P) {
+            walk.seek(A, u);
+            x = walk.within(0, run);
+            ok = put(x);
           }
-          if (walk.split && step == 1 && c > 0) g = walk.border(at);
-          x = walk.within(g, g_end);
+        } else if (c < teams * team) {
+          walk.seek(A, c);
+          x = walk.within(0, run);
+          ok = put(x);
+          uint32_t load = 0;  // of the lane's team, in tiles
+          // the chunk's first unit: head h of the k-th row group of a sequence
+          const int dk = team / walk.Hkv, dh = team % walk.Hkv;
+          int seq = 0, k = 0, h = 0;
+          walk.i = 0;
+          walk.load(A);
+          auto tiles_of = [&](int k) -> int {
+            return (walk.s.L + min((walk.groups - k) * walk.R, walk.s.n) + BN - 1) / BN;
+          };
+          int at = 0;
+          for (int q = 0; ok && at < (int)run; ++q, at += team) {
+            // tiles of the chunk's longest unit: its first, or the first of a sequence that
+            // begins in it
+            int T = tiles_of(k);
+            k += dk;
+            h += dh;
+            if (h >= walk.Hkv) {
+              h -= walk.Hkv;
+              ++k;
+            }
+            while (k >= walk.groups && seq + 1 < A.batch) {
+              k -= walk.groups;
+              walk.i = ++seq;
+              walk.load(A);
+              if (walk.groups > 0 && k + h > 0) T = max(T, tiles_of(0));
+            }
+            const uint32_t least = __reduce_min_sync(0xffffffffu, lane < teams ? load * 32 + lane : 0xffffffffu);
+            const int to = (int)(least & 31u);
+            if (lane == to) load += (uint32_t)T + 1;
+            if (to == c / team && q != to && at + c % team < (int)run) {
+              walk.seek(A, at + c % team);
+              x = walk.within(0, run);
+              ok = put(x);
+              walk.i = seq;
+              walk.load(A);
+            }
+          }
         }
-        if (end) x = Piece{};
-        else if (x.t0 >= x.t1) continue;
-        if (!put(x) || end) break;
-        if (!walk.split) at += walk.P;
+      } else if (c < walk.P) {
+        // Cut units: those inside the CTA's range, then the range's first and last piece,
+        // which may be parts of units.
+        int64_t g = c * walk.share, g_end = run, last = run;
+        if (c < walk.P - 1) {
+          walk.seek(A, g + walk.share);
+          g_end = walk.border(g + walk.share);
+          last = walk.ustart;  // of the unit that the range ends in
+        }
+        walk.seek(A, g);
+        if (c > 0) g = walk.border(g);
+        while (ok) {
+          x = walk.within(g, g_end);
+          if (x.t0 < x.t1) ok = put(x);
+          if (walk.ustart >= last || walk.ustart + walk.cost >= run) break;
+          walk.advance(A);
+        }
       }
+      x = Piece{};
+      if (ok) put(x);  // the end
     }
   }
 
