@@ -1061,6 +1061,15 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
   A.ws_o = reinterpret_cast<float*>(ws + counter_bytes(ctas));
   A.ws_lse = A.ws_o + (size_t)2 * ctas * 2 * BM * D;
   A.ws_inv = A.ws_lse + (size_t)2 * ctas * 2 * BM;
+  // Many units: after the whole of the call before.  CTAs that start under it take the SMs
+  // as they fall free, and then CTAs of neighbouring numbers, which take units side by
+  // side, are not close to each other.  us back to back, so and as a programmatic
+  // dependent: 17 units a CTA (32 ragged prompts) 332 and 359, 7 (8 of them) 96 and 102;
+  // 3.5 (chunks of 8 prompts) 276 and 275; one prompt of 200 13.1 and 12.1.
+  if ((int64_t)rows * heads_q > (int64_t)4 * 2 * BM * ctas) {
+    prompt_attn_kernel<<<ctas, kThreads, kSmemBytes, s>>>(mk, mv, mq, A);
+    return cudaGetLastError();
+  }
   return launch_pdl(prompt_attn_kernel, dim3(ctas), dim3(kThreads), kSmemBytes, s, mk, mv, mq, A);
 }
 
