@@ -177,6 +177,8 @@ class RepairVerifyStep:
             raise ValueError("qkv must be [layers][batch][n_max][..]")
         if self._rows is None:
             with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+                if torch.cuda.is_current_stream_capturing():  # the zeros would be part of the graph, not of the step
+                    raise RuntimeError("a step from projections must have run once before it is captured")
                 self._rows = [torch.zeros(self.layers, self.B, self.n_max, h, self.D, dtype=torch.bfloat16,
                                           device=self.attn_out.device)
                               for h in (self.Hq, self.kv.heads_kv, self.kv.heads_kv)]

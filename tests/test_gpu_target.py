@@ -185,6 +185,60 @@ def test_prompts_step_and_the_next_rows(mods):
     assert cure.cure_device_error() == 0
 
 
+def test_step_from_projections_captured(mods):
+    """Not before it has run once; then replays give what a run gives, also after other inputs."""
+    cure, step = mods
+    g = torch.Generator(device=DEV).manual_seed(9)
+    rnd = lambda *s: torch.empty(s, dtype=torch.bfloat16, device=DEV).normal_(generator=g)  # noqa: E731
+    B, K, R, V = 2, 4, 3, 500
+    c = _Caches(cure, [60, 40])
+    for t in c.k + c.v:
+        t.normal_(generator=g)
+    rope = cure.rope_desc(D, BASE)
+    x, y = (step.StepInputs(rnd(B, K, V), torch.randint(0, V, (B,), dtype=torch.int32, device=DEV, generator=g),
+                            _i32([20, 7]), None, None, None, None, rnd(B, 1 + K + R, V),
+                            qkv=rnd(LAYERS, B, 1 + K + R, (HQ + 2 * HKV) * D)) for _ in range(2))
+    make = lambda: step.RepairVerifyStep(B, K, V, 2, 1.0, R, 2, 1, LAYERS, HQ, c.kv, DEV, rope=rope)  # noqa: E731
+    st, graph = make(), torch.cuda.CUDAGraph()
+    stream = torch.cuda.Stream()
+    k0, v0 = ([t.clone() for t in ts] for ts in (c.k, c.v))
+
+    def fresh():
+        for a, b in zip(c.k + c.v, k0 + v0):
+            a.copy_(b)
+
+    def result(r):
+        return [t.clone() for t in (r["attn"], r["tree"]["n_nodes"], r["acc"]["accept_len"], *c.k, *c.v)]
+    inputs = [[t.clone() for t in (z.draft_logits, z.root_tok, z.target_logits, z.qkv)] for z in (x, y)]
+    want = []
+    for z in (x, y):
+        fresh()
+        want.append(result(make().run(z, c.k, c.v)))
+    fresh()
+    with pytest.raises(RuntimeError):
+        with torch.cuda.graph(graph):
+            st.run(x, c.k, c.v)
+    st, graph = make(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    st.run(y, c.k, c.v, stream=stream)
+    torch.cuda.synchronize()
+    fresh()
+    with torch.cuda.graph(graph):
+        r = st.run(x, c.k, c.v)
+    for i in (0, 1, 0):
+        for a, b in zip((x.draft_logits, x.root_tok, x.target_logits, x.qkv), inputs[i]):
+            a.copy_(b)
+        fresh()
+        graph.replay()
+        nodes = r["tree"]["n_nodes"].tolist()
+        for a, b in zip(result(r), want[i]):
+            if a.dim() == 5 and a.shape[:2] == (LAYERS, B):  # rows of nodes
+                assert all(torch.equal(a[:, j, :n], b[:, j, :n]) for j, n in enumerate(nodes))
+            else:
+                assert torch.equal(a, b)
+    assert cure.cure_device_error() == 0
+
+
 def test_refusals(mods):
     cure, step = mods
     c = _Caches(cure, [32])
