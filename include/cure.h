@@ -413,8 +413,8 @@ cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t l
  * cure_rope_qkv.  cache_len is not advanced: every layer of a model is appended
  * at the same lengths.  Rows outside row_start[0] .. row_start[batch] - 1 are
  * left out.  A slot past the capacity (CURE_DEVERR_SLOT), a missing or bad page
- * (CURE_DEVERR_PAGE) and a row_start that does not ascend (CURE_DEVERR_NODES)
- * leave the rows concerned out.  q, k, v, the norms, strides and alignment as in
+ * (CURE_DEVERR_PAGE) and a row_start that does not ascend from 0 or above
+ * (CURE_DEVERR_NODES) leave the rows concerned out.  q, k, v, the norms, strides and alignment as in
  * cure_rope_qkv; caches 16-byte aligned; the inputs may not overlap the caches.
  * No two rows of a call may have the same slot of the same page.
  */

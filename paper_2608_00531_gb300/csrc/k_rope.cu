@@ -144,9 +144,10 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
       }
     }
     if (seq >= A.batch) return;  // behind the last sequence
-    const int64_t i = row - A.row_start[seq];
-    if (i < 0) {  // before the first sequence, or row_start does not ascend
-      if (seq > 0 && lane == 0) flag(A.err, CURE_DEVERR_NODES);
+    const int start = A.row_start[seq];
+    const int64_t i = row - start;
+    if (i < 0 || start < 0 || row >= A.row_start[seq + 1]) {  // before the first sequence, or row_start does not ascend
+      if ((seq > 0 || i >= 0) && lane == 0) flag(A.err, CURE_DEVERR_NODES);
       return;
     }
     const int64_t slot = A.cache_len[seq] + i;

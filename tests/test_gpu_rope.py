@@ -328,6 +328,22 @@ def test_append_kv_bad_pages_and_slots(cure):
     assert bits & ~(cure.DEVERR_SLOT | cure.DEVERR_PAGE) == 0
 
 
+def test_append_kv_rows_of_no_sequence(cure):
+    """Where row_start does not ascend, a row goes to a sequence whose range holds it or nowhere."""
+    rng = np.random.default_rng(18)
+    kv = cure.kv_desc(2, D, 16)
+    k, v = (_randn(rng, 12, 2, D).to(DEV) for _ in range(2))
+
+    def run(start):
+        kc, vc = (torch.full((4, 16, 2, D), 2.25, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        cure.cure_append_kv(k, v, kc, vc, kv, _i32(start), _i32([0, 0, 0, 0]), cure.rope_desc(128, 10000.0))
+        bits = cure.cure_device_error()
+        return bits, (vc.view(-1, 2, D) != 2.25).any(-1).any(-1).cpu().numpy().nonzero()[0].tolist()
+    assert run([0, 10, 2, 3, 3]) == (cure.DEVERR_NODES, [0, 1])
+    assert run([-2, 3, 3, 3, 3]) == (cure.DEVERR_NODES, [])
+    assert run([2, 3, 3, 5, 6]) == (0, [0, 32, 33, 48])
+
+
 def test_empty_calls(cure):
     kv = cure.kv_desc(2, D, 8)
     kc, vc = (torch.full((1, 8, 2, D), 2.25, dtype=torch.bfloat16, device=DEV) for _ in range(2))
