@@ -843,7 +843,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         // has the least to do by then: every CTA follows the same reckoning.  Neighbours take
         // units side by side (the same rows' other heads, the same head's other rows): SMs
         // close to each other get the same K and V tiles faster, 8 to 12 % of a tile's time.
-        // 32 ragged prompts of 64/8 heads: 334 us so, 355 every P-th (the busiest CTA 15 %
+        // 32 ragged prompts of 28/4 heads: 334 us so, 355 every P-th (the busiest CTA 15 %
         // above the mean); 64 prompts of 300: 105 so, 98 every P-th.
         const int team = min(8, walk.P), teams = min(32, walk.P / team);
         if (!walk.falling) {
@@ -1066,11 +1066,17 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
   // side, are not close to each other.  us back to back, so and as a programmatic
   // dependent: 17 units a CTA (32 ragged prompts) 332 and 359, 7 (8 of them) 96 and 102;
   // 3.5 (chunks of 8 prompts) 276 and 275; one prompt of 200 13.1 and 12.1.
-  if ((int64_t)rows * heads_q > (int64_t)4 * 2 * BM * ctas) {
-    prompt_attn_kernel<<<ctas, kThreads, kSmemBytes, s>>>(mk, mv, mq, A);
-    return cudaGetLastError();
-  }
-  return launch_pdl(prompt_attn_kernel, dim3(ctas), dim3(kThreads), kSmemBytes, s, mk, mv, mq, A);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = (int64_t)rows * heads_q > (int64_t)4 * 2 * BM * ctas ? 0 : 1;
+  return cudaLaunchKernelEx(&cfg, prompt_attn_kernel, mk, mv, mq, A);
 }
 
 }  // namespace cure
