@@ -30,6 +30,17 @@
 // the PV product of its own M tile.  (With an S for each M tile and P over it, S
 // had to wait for PV to finish; both M tiles then ran in step, 1870 cycles of
 // softmax and 1940 of products a tile, one after the other.)
+//
+// Bound and measured (us back to back; part of the measured 1929 TFLOP/s or 6.78 TB/s).
+// Many keys: the products, M128 N128 at one S at a time, with the softmax of the other
+// M tile under them.  One prompt of 16384, 64/8 heads: 2800, 1571 TFLOP/s, 0.81 (3000 in
+// runs of a second, where the power cap leaves 1.9 GHz: 0.85 of what a library product
+// keeps up then).  Shorter units add what starting and ending one costs, some 2 tiles
+// of time, most of it the wait for Q: chunks of 8 prompts behind 1024 to 16000 tokens,
+// 28/4 heads, 273, 0.71; 32 prompts of 33 to 4096 332, 0.65.  Single tokens: the cache's
+// bytes, 64 sequences of 500 to 16000 tokens 190, 5.75 TB/s, 0.85.  One prompt of 200:
+// 12, latency.  (Q of each M tile requested by itself, as soon as that tile's last S is
+// done: 4 to 6 % slower on batches of prompts.)
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
