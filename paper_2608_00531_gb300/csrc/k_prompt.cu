@@ -145,11 +145,17 @@ struct alignas(16) Piece {
 };
 static_assert(sizeof(Piece) == 4 * kPieceInts, "as it lies in shared memory");
 
+__device__ __forceinline__ float sqrt_approx(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // a / b of nonnegative numbers for a quotient of at most `most` (below 2^22 or so).
 __device__ __forceinline__ int small_quotient(int64_t a, int64_t b, int most) {
-  int q = min(most, (int)((float)a / (float)b));  // off by one at most
-  if (q * b > a) --q;
-  if (q < most && (q + 1) * b <= a) ++q;
+  int q = min(most, (int)__fdividef((float)a, (float)b));  // off by one or two at most
+  while (q * b > a) --q;
+  while (q < most && (q + 1) * b <= a) ++q;
   return q;
 }
 
@@ -177,6 +183,13 @@ struct Walk {
   int i, b, k, h, groups;
   int64_t ustart, cost;
 
+  __device__ __forceinline__ int groups_of(int n) const {  // row groups of n rows
+    const int a = n + R - 1;  // below 2^24
+    int q = (int)__fdividef((float)a, (float)R);
+    while (q * R > a) --q;
+    while ((q + 1) * R <= a) ++q;
+    return q;
+  }
   __device__ __forceinline__ int64_t before(int k) const {  // positions of a head's first k row groups
     return split ? k * (int64_t)(kUnitCost + s.L) + (int64_t)R * k * (k + 1) / 2 : k;
   }
@@ -192,7 +205,7 @@ struct Walk {
       b = i;
       s = sequence(A, b, &bad);
     }
-    groups = (s.n + R - 1) / R;
+    groups = groups_of(s.n);
   }
   __device__ __forceinline__ void price() { cost = split ? kUnitCost + s.L + (int64_t)(k + 1) * R : 1; }
   __device__ __forceinline__ void seek(const PromptArgs& A, int64_t g) {  // the unit that holds position g
@@ -214,10 +227,11 @@ struct Walk {
     const int64_t local = g - first;
     // the last row group that starts at or before it: local = Hkv before(k)
     if (split) {
-      const float each = (float)(kUnitCost + s.L) + 0.5f * (float)R, l = (float)local / (float)Hkv;
-      k = min(groups - 1, (int)(2.f * l / (each + sqrtf(each * each + 2.f * (float)R * l))));  // off by one at most
-      if (k > 0 && Hkv * before(k) > local) --k;
-      if (k < groups - 1 && Hkv * before(k + 1) <= local) ++k;
+      const float each = (float)(kUnitCost + s.L) + 0.5f * (float)R, l = __fdividef((float)local, (float)Hkv);
+      // (off by one or two at most)
+      k = min(groups - 1, (int)__fdividef(2.f * l, each + sqrt_approx(each * each + 2.f * (float)R * l)));
+      while (k > 0 && Hkv * before(k) > local) --k;
+      while (k < groups - 1 && Hkv * before(k + 1) <= local) ++k;
     } else {
       k = small_quotient(local, Hkv, groups - 1);
     }
@@ -281,13 +295,42 @@ struct Walk {
   }
 };
 
+// A wait of all lanes of a warp: false where the CTA gives up, because this wait or
+// another has run out of tc::kWaitTimeoutCycles (which is reported at the CTA's end).
+// As tc::wait_warp, in half the code: what the roles run between them fits the
+// instruction cache or does not.  With the 64-bit clock, the report and two tries in
+// each of the 17 waits 8 prompts of 2048 took 213 us, so 206.
+__device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t abort_flag) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b32 t0, t;\n\t"
+      "mov.u32 t0, %%clock;\n"
+      "AGAIN:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra DONE;\n\t"
+      "ld.volatile.shared.u32 t, [%3];\n\t"
+      "setp.ne.u32 q, t, 0;\n\t"
+      "@q bra DONE;\n\t"
+      "mov.u32 t, %%clock;\n\t"
+      "sub.u32 t, t, t0;\n\t"
+      "setp.gt.u32 q, t, %4;\n\t"
+      "@q st.volatile.shared.u32 [%3], 1;\n\t"
+      "bra AGAIN;\n"
+      "DONE:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(abort_flag), "n"((uint32_t)kWaitTimeoutCycles)
+      : "memory");
+  return __all_sync(0xffffffffu, ok != 0);
+}
+
 // A role's place in the pieces that the scheduler has laid out.
 struct Pieces {
   uint32_t k;
   // The next one; false when there is none or the CTA has given up.  (All lanes of a warp.)
-  __device__ __forceinline__ bool next(const Bar& bar, const uint8_t* smem, volatile int* abort_flag, int* err, Piece& x) {
+  __device__ __forceinline__ bool next(const Bar& bar, const uint8_t* smem, uint32_t aborted, Piece& x) {
     const uint32_t slot = k % kPieces;
-    if (!wait_warp(bar(B_PIECE + slot), (k / kPieces) & 1u, abort_flag, err)) return false;
+    if (!await(bar(B_PIECE + slot), (k / kPieces) & 1u, aborted)) return false;
     const int4* p = reinterpret_cast<const int4*>(smem + kOffPieces + slot * (kPieceInts * 4));
     int4* d = reinterpret_cast<int4*>(&x);
 #pragma unroll
@@ -325,6 +368,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   const int G = A.G, npb = BM / G;
   const Bar bar{sb + kOffMisc};
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
+  const uint32_t aborted = sb + kOffAbort;
   volatile int* n_joins = reinterpret_cast<volatile int*>(smem + kOffJoins);
 
   // ---------------------------------------------------------------- set-up
@@ -389,7 +433,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     uint32_t sc = 0, r = 0;  // tiles of this M tile, ring tiles
     bool ok = true;
     uint32_t done = 0;  // pieces of this M tile
-    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
+    while (ok && pieces.next(bar, smem, aborted, x)) {
       const uint32_t r_piece = r;
       r += 2 * (uint32_t)(x.t1 - x.t0);
       if (m == 1 && !active1(x)) continue;
@@ -399,7 +443,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const int least = __shfl_sync(0xffffffffu, sees, 0), most = __shfl_sync(0xffffffffu, sees, 31);
       float m_run = -INFINITY, l_run = 0.f;
       for (int t = x.t0; t < x.t1; ++t) {
-        if (!wait_warp(bar(B_SFULL + m), sc & 1u, abort_flag, A.err)) { ok = false; break; }
+        if (!await(bar(B_SFULL + m), sc & 1u, aborted)) { ok = false; break; }
         ++sc;
         tc_fence_after();
         uint32_t v[4][32];
@@ -435,7 +479,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         if (need) m_run = m_new;
         // P's place and O are free once this M tile's PV product before is done
         if (sc > 1) {
-          if (!wait_warp(bar(B_PVDONE + m), (sc - 2) & 1u, abort_flag, A.err)) { ok = false; break; }
+          if (!await(bar(B_PVDONE + m), (sc - 2) & 1u, aborted)) { ok = false; break; }
           tc_fence_after();
         }
         const float nbase = m_run == -INFINITY ? 0.f : -m_run;
@@ -484,7 +528,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         const int valid = x.keys - t * BN;
         if (m == 0 && valid < BN) {
           const uint32_t rv = r_piece + 2 * (uint32_t)(t - x.t0) + 1;
-          if (!wait_warp(bar(B_FULL + rv % NS), (rv / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+          if (!await(bar(B_FULL + rv % NS), (rv / NS) & 1u, aborted)) { ok = false; break; }
           const uint32_t vb = sb + kOffRing + (rv % NS) * kTile;
           const bool paged = A.kv.layout == 1;
           const int unit = paged ? A.kv.page_size : 16;
@@ -503,7 +547,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       if (!ok) break;
       // What the epilogue needs to know of the row, once it is done with the piece before
       // (so that it also sees every phase of STAT).
-      if (done > 0 && !wait_warp(bar(B_OFREE + m), (done - 1) & 1u, abort_flag, A.err)) break;
+      if (done > 0 && !await(bar(B_OFREE + m), (done - 1) & 1u, aborted)) break;
       __stcg(A.ws_inv + ((int64_t)blockIdx.x * 2 + m) * BM + row, l_run > 0.f ? 1.f / l_run : 0.f);
       if (x.t1 - x.t0 < x.T)
         __stcg(A.ws_lse + (2 * (int64_t)blockIdx.x + (x.t0 == 0)) * (2 * BM) + m * BM + row, row_lse(m_run, l_run));
@@ -522,9 +566,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     // The epilogue's threads meet (an mbarrier, for a wait that ends when the CTA gives up).
     auto meet = [&]() -> bool {
       mbar_arrive(bar(B_JOIN));
-      return ok = wait_warp(bar(B_JOIN), joins++ & 1u, abort_flag, A.err);
+      return ok = await(bar(B_JOIN), joins++ & 1u, aborted);
     };
-    while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
+    while (ok && pieces.next(bar, smem, aborted, x)) {
       const bool whole = x.t1 - x.t0 == x.T;
       const int64_t slot = 2 * (int64_t)blockIdx.x + (x.t0 == 0);
 #pragma unroll 1
@@ -533,39 +577,35 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         // STAT first: the softmax has then seen all PV products but the last
         const uint32_t done = m ? done1++ : done0++;  // pieces before, and tiles with this one
         const uint32_t tiles = m ? tiles1 += (uint32_t)(x.t1 - x.t0) : tiles0 += (uint32_t)(x.t1 - x.t0);
-        if (!wait_warp(bar(B_STAT + m), done & 1u, abort_flag, A.err)) { ok = false; break; }
+        if (!await(bar(B_STAT + m), done & 1u, aborted)) { ok = false; break; }
         const float inv = __ldcg(A.ws_inv + ((int64_t)blockIdx.x * 2 + m) * BM + row);
-        if (!wait_warp(bar(B_PVDONE + m), (tiles - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
+        if (!await(bar(B_PVDONE + m), (tiles - 1) & 1u, aborted)) { ok = false; break; }
         tc_fence_after();
         const int i = (2 * x.rg + m) * npb + row / G;
         const bool vrow = row < npb * G && i < x.n;
         uint16_t* orow = A.out + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D;
         float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + m * BM + row;
 #pragma unroll 1
-        for (int q = 0; q < 2; ++q) {  // 64 columns
-          uint32_t o[2][32];
-          tmem_ld32(tO + m * D + q * 64, o[0]);
-          tmem_ld32(tO + m * D + q * 64 + 32, o[1]);
+        for (int q = 0; q < 4; ++q) {  // 32 columns
+          uint32_t o[32];
+          tmem_ld32(tO + m * D + q * 32, o);
           tmem_wait_ld();
+          if (whole) {
+            uint32_t v[16];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            if (whole) {
-              uint32_t v[16];
-#pragma unroll
-              for (int k = 0; k < 16; ++k)
-                v[k] = pack_bf16(__uint_as_float(o[e][2 * k]) * inv, __uint_as_float(o[e][2 * k + 1]) * inv);
-              if (vrow) {
-                st_global_32(orow + q * 64 + e * 32, v, wide);
-                st_global_32(orow + q * 64 + e * 32 + 16, v + 8, wide);
-              }
-            } else if (vrow) {
-              // a part of a unit: normalised O to the workspace, float4 columns [32][256 rows]
-#pragma unroll
-              for (int k = 0; k < 8; ++k)
-                po[(q * 16 + e * 8 + k) * (2 * BM)] =
-                    make_float4(__uint_as_float(o[e][4 * k]) * inv, __uint_as_float(o[e][4 * k + 1]) * inv,
-                                __uint_as_float(o[e][4 * k + 2]) * inv, __uint_as_float(o[e][4 * k + 3]) * inv);
+            for (int k = 0; k < 16; ++k)
+              v[k] = pack_bf16(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
+            if (vrow) {
+              st_global_32(orow + q * 32, v, wide);
+              st_global_32(orow + q * 32 + 16, v + 8, wide);
             }
+          } else if (vrow) {
+            // a part of a unit: normalised O to the workspace, float4 columns [32][256 rows]
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              po[(q * 8 + k) * (2 * BM)] =
+                  make_float4(__uint_as_float(o[4 * k]) * inv, __uint_as_float(o[4 * k + 1]) * inv,
+                              __uint_as_float(o[4 * k + 2]) * inv, __uint_as_float(o[4 * k + 3]) * inv);
           }
         }
         tc_fence_before();
@@ -590,7 +630,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const uint32_t qbytes = (uint32_t)(npb * G * 128);
       uint32_t qc = 0, issued = 0;  // pieces, ring tiles
       bool ok = true;
-      while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
+      while (ok && pieces.next(bar, smem, aborted, x)) {
         auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
           const int tok = t * BN + lane * ps;
           if (lane >= ppt || tok >= x.keys) return -1;
@@ -607,7 +647,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {  // the K tile, then the V tile
             const int st = (int)(issued % NS);
-            if (!wait_warp(bar(B_EMPTY + st), ((issued / NS) & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
+            if (!await(bar(B_EMPTY + st), ((issued / NS) & 1u) ^ 1u, aborted)) { ok = false; break; }
             const uint32_t full = bar(B_FULL + st), dst = sb + kOffRing + st * kTile;
             if (lane == 0) mbar_arrive_expect_tx(full, kTile);
             __syncwarp();
@@ -624,7 +664,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             __syncwarp();
             ++issued;
             if (t == x.t0 && kv == 0) {  // Q of both M tiles once the previous piece's S products are done
-              if (!wait_warp(bar(B_QEMPTY), (qc & 1u) ^ 1u, abort_flag, A.err)) { ok = false; break; }
+              if (!await(bar(B_QEMPTY), (qc & 1u) ^ 1u, aborted)) { ok = false; break; }
               ++qc;
               if (lane == 0) mbar_arrive_expect_tx(bar(B_QFULL), 4 * qbytes);
               __syncwarp();
@@ -648,8 +688,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const bool paged = A.kv.layout == 1;
       uint32_t qc = 0, r = 0, c = 0;  // pieces, ring tiles, products
       bool ok = true;
-      while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
-        if (!wait_warp(bar(B_QFULL), qc & 1u, abort_flag, A.err)) break;
+      while (ok && pieces.next(bar, smem, aborted, x)) {
+        if (!await(bar(B_QFULL), qc & 1u, aborted)) break;
         ++qc;
         const int mts = active1(x) ? 2 : 1;
         for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
@@ -658,13 +698,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           const uint32_t sbo = paged ? kPgGroup : 1024u, kh = paged ? kPgHalf : kKHalf;
 #pragma unroll 1
           for (int m = 0; m < mts; ++m) {
-            if (c > 0 && !wait_warp(bar(B_SFREE), (c - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
+            if (c > 0 && !await(bar(B_SFREE), (c - 1) & 1u, aborted)) { ok = false; break; }
             ++c;
             // The K tile, after SFREE: a parity wait is sound from the phase before on and
             // not later, and the stage's tile before this one, V of three tiles before, has
             // landed when the softmax of M tile 0 has loaded S of the tile before (it then
             // has seen the PV product of that V tile done).
-            if (m == 0 && !wait_warp(bar(B_FULL + sk), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+            if (m == 0 && !await(bar(B_FULL + sk), (r / NS) & 1u, aborted)) { ok = false; break; }
             tc_fence_after();
             mma_s_group(tmem + kColS, sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024), sdesc_sw128(ka, 16, sbo),
                         sdesc_sw128(ka + kh, 16, sbo), idS);
@@ -684,13 +724,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const bool paged = A.kv.layout == 1;
       uint32_t r = 1, c0 = 0, c1 = 0, done0 = 0, done1 = 0;  // ring tiles; products and pieces of each M tile
       bool ok = true;
-      while (ok && pieces.next(bar, smem, abort_flag, A.err, x)) {
+      while (ok && pieces.next(bar, smem, aborted, x)) {
         const int mts = active1(x) ? 2 : 1;
         for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
           const uint32_t sv = r % NS;
           // (the stage's K tile of two tiles before has landed: its S became the P that this
           // warp has waited for)
-          if (!wait_warp(bar(B_FULL + sv), (r / NS) & 1u, abort_flag, A.err)) { ok = false; break; }
+          if (!await(bar(B_FULL + sv), (r / NS) & 1u, aborted)) { ok = false; break; }
           // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
           const uint64_t vd =
               sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
@@ -700,9 +740,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             const uint32_t c = m ? c1++ : c0++;
             if (t == x.t0) {
               const uint32_t done = m ? done1++ : done0++;
-              if (done > 0 && !wait_warp(bar(B_OFREE + m), (done - 1) & 1u, abort_flag, A.err)) { ok = false; break; }
+              if (done > 0 && !await(bar(B_OFREE + m), (done - 1) & 1u, aborted)) { ok = false; break; }
             }
-            if (!wait_warp(bar(B_PFULL + m), c & 1u, abort_flag, A.err)) { ok = false; break; }
+            if (!await(bar(B_PFULL + m), c & 1u, aborted)) { ok = false; break; }
             tc_fence_after();
             mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0 ? 1u : 0u);
             mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64 + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
@@ -728,7 +768,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         int64_t units, cost;
       };
       auto size_of = [&](const Seq& s) -> Size {  // a sequence's positions of both kinds
-        const int64_t k = (s.n + walk.R - 1) / walk.R;
+        const int64_t k = walk.groups_of(s.n);
         return {walk.Hkv * k, walk.Hkv * (k * (kUnitCost + s.L) + walk.R * k * (k + 1) / 2)};
       };
       auto scan = [&](int64_t v) -> int64_t {  // sum over the lanes up to this one
@@ -760,33 +800,62 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       cost = __shfl_sync(0xffffffffu, scan(cost), 31);
       longest = __reduce_max_sync(0xffffffffu, longest);
       walk.P = (int)gridDim.x;
-      int64_t run = 0;  // positions
-      auto lay_out = [&](bool split, bool falling) {
-        walk.split = split;
-        walk.falling = falling;
-        run = split ? cost : units;
-        if (walk.few) {
-          int from = lane;
-          if (falling) {  // the lane whose sequence comes lane-th
-            const int length = own.n > 0 ? own.L + own.n : 0;
-            int rank = 0;
+      // Which is faster, in positions.  Whole units end with the longest one if every CTA has
+      // one at most.  In turn they end with an even share and, in the CTAs that end last,
+      // half of the longest one.  Longest first they end with an even share, or with the
+      // (k + 1)-th round of units as long as those that it starts with; some 3 % more.  Cut
+      // units end with an even share, which the pieces' fixed costs upset by some 8 %, and
+      // the joins.
+      const float share = __fdividef((float)cost, (float)walk.P);
+      const float cut = 1.08f * share + kJoinCost;
+      float whole = (float)(longest + kUnitCost);
+      walk.falling = walk.few && units > walk.P && cost >= units * kShortUnit && whole <= cut;
+      walk.mine = own;
+      walk.number_of_mine = lane;
+      if (walk.falling) {
+        // to each lane the sequence that comes lane-th
+        const int length = own.n > 0 ? own.L + own.n : 0;
+        int rank = 0, from = lane;
 #pragma unroll 1
-            for (int l = 0; l < 32; ++l) {
-              const int o = __shfl_sync(0xffffffffu, length, l);
-              rank += o > length || (o == length && l < lane);
-            }
-#pragma unroll 1
-            for (int l = 0; l < 32; ++l)
-              if (__shfl_sync(0xffffffffu, rank, l) == lane) from = l;
-          }
-          walk.mine.r0 = __shfl_sync(0xffffffffu, own.r0, from);
-          walk.mine.n = __shfl_sync(0xffffffffu, own.n, from);
-          walk.mine.L = __shfl_sync(0xffffffffu, own.L, from);
-          walk.number_of_mine = from;
-          const Size z = size_of(walk.mine);
-          walk.first_of_mine = scan(split ? z.cost : z.units) - (split ? z.cost : z.units);
-          return;
+        for (int l = 0; l < 32; ++l) {
+          const int o = __shfl_sync(0xffffffffu, length, l);
+          rank += o > length || (o == length && l < lane);
         }
+#pragma unroll 1
+        for (int l = 0; l < 32; ++l)
+          if (__shfl_sync(0xffffffffu, rank, l) == lane) from = l;
+        walk.mine.r0 = __shfl_sync(0xffffffffu, own.r0, from);
+        walk.mine.n = __shfl_sync(0xffffffffu, own.n, from);
+        walk.mine.L = __shfl_sync(0xffffffffu, own.L, from);
+        walk.number_of_mine = from;
+        // the keys of the units that the rounds begin with, where the lane's sequence has them
+        const int n = (int)size_of(walk.mine).units, first = (int)scan(n) - n;
+        float most = fmaxf(whole, share);
+#pragma unroll 1
+        for (int r = 1; r < 4; ++r) {
+          const int local = r * walk.P - first;
+          if (local >= 0 && local < n) {
+            const int rg = (n - 1 - local) / walk.Hkv;
+            const int keys = walk.mine.L + min((rg + 1) * walk.R, walk.mine.n);
+            most = fmaxf(most, (float)(r + 1) * (float)(keys + kUnitCost));
+          }
+        }
+        whole = 1.03f * __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+      } else if (units > walk.P) {
+        whole = share + 0.5f * whole;
+      }
+      walk.split = whole > cut;
+      if (walk.split) {
+        walk.falling = false;
+        walk.mine = own;
+        walk.number_of_mine = lane;
+      }
+      const int64_t run = walk.split ? cost : units;  // positions
+      if (walk.few) {
+        const Size z = size_of(walk.mine);
+        const int64_t v = walk.split ? z.cost : z.units;
+        walk.first_of_mine = scan(v) - v;
+      } else {
         int64_t upto = 0;
         for (int base = 0; base < A.batch; base += 32) {
           const int b = base + lane;
@@ -794,47 +863,18 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           if (b < A.batch) {
             int bad;
             const Size z = size_of(sequence(A, b, &bad));
-            v = split ? z.cost : z.units;
+            v = walk.split ? z.cost : z.units;
           }
           const int64_t to = scan(v);
           if (b < A.batch) start[b] = upto + to - v;
           upto += __shfl_sync(0xffffffffu, to, 31);
         }
         __syncwarp();
-      };
-      // Which is faster, in positions.  Whole units end with the longest one if every CTA has
-      // one at most.  In turn they end with an even share and, in the CTAs that end last,
-      // half of the longest one.  Longest first they end with an even share, or with the
-      // (k + 1)-th round of units as long as those that it starts with; some 3 % more.  Cut
-      // units end with an even share, which the pieces' fixed costs upset by some 8 %, and
-      // the joins.
-      const float share = (float)cost / (float)walk.P;
-      const float cut = 1.08f * share + kJoinCost;
-      float whole = (float)(longest + kUnitCost);
-      const bool in_turn = units <= walk.P || !walk.few || cost < units * kShortUnit;
-      if (in_turn || whole > cut) {
-        if (units > walk.P) whole = share + 0.5f * whole;
-        lay_out(whole > cut, false);
-      } else {
-        lay_out(false, true);
-        whole = fmaxf(whole, share);
-#pragma unroll 1
-        for (int r = 1; r < 4 && (int64_t)r * walk.P < units; ++r) {
-          walk.seek(A, (int64_t)r * walk.P);
-          whole = fmaxf(whole, (float)(r + 1) * (float)(walk.keys() + kUnitCost));
-        }
-        if (1.03f * whole > cut) lay_out(true, false);
-      }
-      // every CTA that takes part in cut units has a tile of each unit that its range lies in
-      if (walk.split) {
-        if (share < (float)kMinShare) walk.P = max(1, (int)((float)run / (float)kMinShare));
-        walk.share = (int64_t)((float)run / (float)walk.P * 0.999999f);
-        walk.near = min((int64_t)kSnap, max((int64_t)1, (walk.share - kUnitCost) / 2));
       }
       uint32_t k = 0;
       auto put = [&](const Piece& p) -> bool {
         const uint32_t slot = k % kPieces;
-        if (!wait_warp(bar(B_TAKEN + slot), ((k / kPieces) & 1u) ^ 1u, abort_flag, A.err)) return false;
+        if (!await(bar(B_TAKEN + slot), ((k / kPieces) & 1u) ^ 1u, aborted)) return false;
         ++k;
         if (lane == 0) {
           int4* d = reinterpret_cast<int4*>(smem + kOffPieces + slot * (kPieceInts * 4));
@@ -846,82 +886,76 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         __syncwarp();
         return true;
       };
-      const int c = (int)blockIdx.x;
-      bool ok = true;
-      if (!walk.split) {
-        // Whole units, every P-th; or longest first, the first ones by number and then in
-        // chunks of `team` units for a team of neighbouring CTAs, each chunk to the team that
-        // has the least to do by then: every CTA follows the same reckoning.  Neighbours take
-        // units side by side (the same rows' other heads, the same head's other rows): SMs
-        // close to each other get the same K and V tiles faster, 8 to 12 % of a tile's time.
-        // 32 ragged prompts of 28/4 heads: 334 us so, 355 every P-th (the busiest CTA 15 %
-        // above the mean); 64 prompts of 300: 105 so, 98 every P-th.
-        const int team = min(8, walk.P), teams = min(32, walk.P / team);
-        if (!walk.falling) {
-          for (int64_t u = c; ok && u < run; u += walk.P) {
-            walk.seek(A, u);
-            x = walk.within(0, run);
-            ok = put(x);
+      // Whole units, every P-th; or longest first, the first ones by number and then in
+      // chunks of `team` units for a team of neighbouring CTAs, each chunk to the team that
+      // has the least to do by then: every CTA follows the same reckoning.  Neighbours take
+      // units side by side (the same rows' other heads, the same head's other rows): SMs
+      // close to each other get the same K and V tiles faster, 8 to 12 % of a tile's time.
+      // 32 ragged prompts of 28/4 heads: 334 us so, 355 every P-th (the busiest CTA 15 %
+      // above the mean); 64 prompts of 300: 105 so, 98 every P-th.
+      const int c = (int)blockIdx.x, team = min(8, walk.P), teams = min(32, walk.P / team);
+      uint32_t load = 0;  // of the lane's team, in tiles
+      // the next chunk's first unit: head ch of the ck-th row group of the cs-th sequence
+      int at = 0, cs = 0, ck = 0, ch = 0;
+      int cL = __shfl_sync(0xffffffffu, walk.mine.L, 0), cn = __shfl_sync(0xffffffffu, walk.mine.n, 0);
+      auto next_of_team = [&]() -> int64_t {  // the CTA's next unit after its first; `run`: none
+        while (at < (int)run) {
+          // tiles of the chunk's longest unit: its first, or the first of a sequence that
+          // begins in it
+          int groups = walk.groups_of(cn);
+          int T = (cL + min((groups - ck) * walk.R, cn) + BN - 1) / BN;
+          ck += team / walk.Hkv;
+          ch += team % walk.Hkv;
+          if (ch >= walk.Hkv) {
+            ch -= walk.Hkv;
+            ++ck;
           }
-        } else if (c < teams * team) {
-          walk.seek(A, c);
-          x = walk.within(0, run);
-          ok = put(x);
-          uint32_t load = 0;  // of the lane's team, in tiles
-          // the chunk's first unit: head h of the k-th row group of a sequence
-          const int dk = team / walk.Hkv, dh = team % walk.Hkv;
-          int seq = 0, k = 0, h = 0;
-          walk.i = 0;
-          walk.load(A);
-          auto tiles_of = [&](int k) -> int {
-            return (walk.s.L + min((walk.groups - k) * walk.R, walk.s.n) + BN - 1) / BN;
-          };
-          int at = 0;
-          for (int q = 0; ok && at < (int)run; ++q, at += team) {
-            // tiles of the chunk's longest unit: its first, or the first of a sequence that
-            // begins in it
-            int T = tiles_of(k);
-            k += dk;
-            h += dh;
-            if (h >= walk.Hkv) {
-              h -= walk.Hkv;
-              ++k;
-            }
-            while (k >= walk.groups && seq + 1 < A.batch) {
-              k -= walk.groups;
-              walk.i = ++seq;
-              walk.load(A);
-              if (walk.groups > 0 && k + h > 0) T = max(T, tiles_of(0));
-            }
-            const uint32_t least = __reduce_min_sync(0xffffffffu, lane < teams ? load * 32 + lane : 0xffffffffu);
-            const int to = (int)(least & 31u);
-            if (lane == to) load += (uint32_t)T + 1;
-            if (to == c / team && q != to && at + c % team < (int)run) {
-              walk.seek(A, at + c % team);
-              x = walk.within(0, run);
-              ok = put(x);
-              walk.i = seq;
-              walk.load(A);
-            }
+          while (ck >= groups && cs + 1 < A.batch) {
+            ck -= groups;
+            ++cs;
+            cL = __shfl_sync(0xffffffffu, walk.mine.L, cs);
+            cn = __shfl_sync(0xffffffffu, walk.mine.n, cs);
+            groups = walk.groups_of(cn);
+            if (groups > 0 && ck + ch > 0) T = max(T, (cL + cn + BN - 1) / BN);
           }
+          const uint32_t least = __reduce_min_sync(0xffffffffu, lane < teams ? load * 32 + lane : 0xffffffffu);
+          const int to = (int)(least & 31u), u = at + c % team;
+          const bool first = at == to * team;
+          if (lane == to) load += (uint32_t)T + 1;
+          at += team;
+          if (to == c / team && !first && u < (int)run) return u;
         }
-      } else if (c < walk.P) {
-        // Cut units: those inside the CTA's range, then the range's first and last piece,
-        // which may be parts of units.
-        int64_t g = c * walk.share, g_end = run, last = run;
-        if (c < walk.P - 1) {
-          walk.seek(A, g + walk.share);
-          g_end = walk.border(g + walk.share);
-          last = walk.ustart;  // of the unit that the range ends in
-        }
+        return run;
+      };
+      // every CTA that takes part in cut units has a tile of each unit that its range lies in
+      if (walk.split) {
+        if (share < (float)kMinShare) walk.P = max(1, (int)((float)run * (1.f / kMinShare)));
+        walk.share = (int64_t)(__fdividef((float)run, (float)walk.P) * 0.999999f);
+        walk.near = min((int64_t)kSnap, max((int64_t)1, (walk.share - kUnitCost) / 2));
+      }
+      // A CTA of cut units finds its range's end first, then takes the units inside the range
+      // and the range's first and last piece, which may be parts of units.
+      bool ending = walk.split && c < walk.P - 1, ok = true;
+      int64_t g = walk.split ? (ending ? c + 1 : c) * walk.share : c;
+      int64_t g_end = run, last = run;  // the range's end, and the unit that it ends in
+      if (walk.split ? c >= walk.P : walk.falling && c >= teams * team) g = run;
+      while (ok && g < run) {
         walk.seek(A, g);
-        if (c > 0) g = walk.border(g);
-        while (ok) {
+        if (walk.split && g > 0) g = walk.border(g);
+        if (ending) {
+          g_end = g;
+          last = walk.ustart;
+          ending = false;
+          g = c * walk.share;
+          continue;
+        }
+        while (true) {
           x = walk.within(g, g_end);
           if (x.t0 < x.t1) ok = put(x);
-          if (walk.ustart >= last || walk.ustart + walk.cost >= run) break;
+          if (!walk.split || !ok || walk.ustart >= last || walk.ustart + walk.cost >= run) break;
           walk.advance(A);
         }
+        g = walk.split ? run : walk.falling ? next_of_team() : g + walk.P;
       }
       x = Piece{};
       if (ok) put(x);  // the end
@@ -934,7 +968,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
   tc_fence_before();
   __syncthreads();
-  if (!*abort_flag) {
+  if (*abort_flag) {
+    if (tid == 0) flag(A.err, CURE_DEVERR_TIMEOUT);
+  } else {
     for (int d = 0; d < *n_joins; ++d) {
       x = *reinterpret_cast<const Piece*>(smem + kOffPieces + (kPieces + d) * (kPieceInts * 4));
       __threadfence();
