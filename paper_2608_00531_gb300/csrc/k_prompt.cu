@@ -190,8 +190,11 @@ struct Walk {
     while ((q + 1) * R <= a) ++q;
     return q;
   }
-  __device__ __forceinline__ int64_t before(int k) const {  // positions of a head's first k row groups
-    return split ? k * (int64_t)(kUnitCost + s.L) + (int64_t)R * k * (k + 1) / 2 : k;
+  // the k-th row group's positions for a head: of the first, and what each adds
+  __device__ __forceinline__ int base() const { return split ? kUnitCost + s.L : 1; }
+  __device__ __forceinline__ int step() const { return split ? R : 0; }
+  __device__ __forceinline__ int64_t before(int k) const {  // a head's positions in front of the k-th row group
+    return k * (int64_t)base() + (int64_t)step() * k * (k + 1) / 2;
   }
   __device__ __forceinline__ int owner(int64_t p) const { return small_quotient(p, share, P - 1); }
   __device__ __forceinline__ void load(const PromptArgs& A) {
@@ -207,7 +210,7 @@ struct Walk {
     }
     groups = groups_of(s.n);
   }
-  __device__ __forceinline__ void price() { cost = split ? kUnitCost + s.L + (int64_t)(k + 1) * R : 1; }
+  __device__ __forceinline__ void price() { cost = base() + (int64_t)(k + 1) * step(); }
   __device__ __forceinline__ void seek(const PromptArgs& A, int64_t g) {  // the unit that holds position g
     int64_t first;  // of the last sequence that starts at or before it
     if (few) {
@@ -225,19 +228,20 @@ struct Walk {
     }
     load(A);
     const int64_t local = g - first;
-    // the last row group that starts at or before it: local = Hkv before(k)
-    if (split) {
-      const float each = (float)(kUnitCost + s.L) + 0.5f * (float)R, l = __fdividef((float)local, (float)Hkv);
-      // (off by one or two at most)
-      k = min(groups - 1, (int)__fdividef(2.f * l, each + sqrt_approx(each * each + 2.f * (float)R * l)));
-      while (k > 0 && Hkv * before(k) > local) --k;
-      while (k < groups - 1 && Hkv * before(k + 1) <= local) ++k;
-    } else {
-      k = small_quotient(local, Hkv, groups - 1);
+    // the last row group that starts at or before it: local = Hkv before(k), off by one or two at most
+    const float d = (float)step(), each = (float)base() + 0.5f * d, l = __fdividef((float)local, (float)Hkv);
+    k = min(groups - 1, (int)__fdividef(2.f * l, each + sqrt_approx(each * each + 2.f * d * l)));
+    int64_t at = Hkv * before(k);
+    while (k > 0 && at > local) at = Hkv * before(--k);
+    while (k < groups - 1) {
+      const int64_t next = Hkv * before(k + 1);
+      if (next > local) break;
+      at = next;
+      ++k;
     }
     price();
-    h = small_quotient(local - Hkv * before(k), cost, Hkv - 1);
-    ustart = first + Hkv * before(k) + h * cost;
+    h = small_quotient(local - at, cost, Hkv - 1);
+    ustart = first + at + h * cost;
   }
   __device__ __forceinline__ void advance(const PromptArgs& A) {  // to the next unit (there is one)
     ustart += cost;
@@ -628,9 +632,9 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const int ps = A.kv.page_size;
       const int ppt = A.kv.layout == 1 ? BN / ps : 0;  // pages (boxes) of a tile: 2 .. 16
       const uint32_t qbytes = (uint32_t)(npb * G * 128);
-      uint32_t qc = 0, issued = 0;  // pieces, ring tiles
-      bool ok = true;
-      while (ok && pieces.next(bar, smem, aborted, x)) {
+      uint32_t qc = 0, issued = 0;   // pieces, ring tiles
+      uint32_t st = 0, parity = 1u;  // the next ring tile's stage, and its wait's parity
+      while (pieces.next(bar, smem, aborted, x)) {
         auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
           const int tok = t * BN + lane * ps;
           if (lane >= ppt || tok >= x.keys) return -1;
@@ -641,42 +645,46 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           }
           return page;
         };
-        int page = page_of(x.t0);
-        for (int t = x.t0; ok && t < x.t1; ++t) {
-          const int next = t + 1 < x.t1 ? page_of(t + 1) : -1;
-#pragma unroll 1
-          for (int kv = 0; kv < 2; ++kv) {  // the K tile, then the V tile
-            const int st = (int)(issued % NS);
-            if (!await(bar(B_EMPTY + st), ((issued / NS) & 1u) ^ 1u, aborted)) { ok = false; break; }
-            const uint32_t full = bar(B_FULL + st), dst = sb + kOffRing + st * kTile;
-            if (lane == 0) mbar_arrive_expect_tx(full, kTile);
-            __syncwarp();
-            if (A.kv.layout == 1) {
-              if (lane < ppt) tma_load_5d(dst + lane * ps * 256, kv ? &tm_v : &tm_k, full, 0, 0, 2 * x.h, 0, page);
-            } else if (kv == 0) {
-              if (lane < 2) tma_load_3d(dst + lane * kKHalf, &tm_k, full, lane * 64, x.h, x.b * A.kv.max_len + t * BN);
-            } else if (lane < BN / 16) {
-              // 16 rows each; those past the unit's keys from behind the tensor, which reads zeros
-              const int row = t * BN + 16 * lane;
-              tma_load_4d(dst + lane * kVChunk, &tm_v, full, 0,
-                          row < x.keys ? x.b * A.kv.max_len + row : A.batch * A.kv.max_len, 0, x.h);
-            }
-            __syncwarp();
-            ++issued;
-            if (t == x.t0 && kv == 0) {  // Q of both M tiles once the previous piece's S products are done
-              if (!await(bar(B_QEMPTY), (qc & 1u) ^ 1u, aborted)) { ok = false; break; }
-              ++qc;
-              if (lane == 0) mbar_arrive_expect_tx(bar(B_QFULL), 4 * qbytes);
-              __syncwarp();
-              if (lane < 4)  // M tile lane / 2, d half lane % 2
-                tma_load_4d(sb + kOffQ + lane * kQHalf, &tm_q, bar(B_QFULL), (lane & 1) * 64, 0, x.h,
-                            x.r0 + (2 * x.rg + (lane >> 1)) * npb);
-              __syncwarp();
-            }
+        int page = -1, next = page_of(x.t0);
+        for (int i = 2 * x.t0; i < 2 * x.t1; ++i) {  // K and V tiles in turn
+          const int t = i >> 1, kv = i & 1;
+          if (!kv) {
+            page = next;
+            next = t + 1 < x.t1 ? page_of(t + 1) : -1;
           }
-          page = next;
+          if (!await(bar(B_EMPTY + st), parity, aborted)) goto produced;
+          const uint32_t full = bar(B_FULL + st), dst = sb + kOffRing + st * kTile;
+          if (lane == 0) mbar_arrive_expect_tx(full, kTile);
+          __syncwarp();
+          if (A.kv.layout == 1) {
+            if (lane < ppt) tma_load_5d(dst + lane * ps * 256, kv ? &tm_v : &tm_k, full, 0, 0, 2 * x.h, 0, page);
+          } else if (kv == 0) {
+            if (lane < 2) tma_load_3d(dst + lane * kKHalf, &tm_k, full, lane * 64, x.h, x.b * A.kv.max_len + t * BN);
+          } else if (lane < BN / 16) {
+            // 16 rows each; those past the unit's keys from behind the tensor, which reads zeros
+            const int row = t * BN + 16 * lane;
+            tma_load_4d(dst + lane * kVChunk, &tm_v, full, 0,
+                        row < x.keys ? x.b * A.kv.max_len + row : A.batch * A.kv.max_len, 0, x.h);
+          }
+          __syncwarp();
+          ++issued;
+          if (++st == NS) {
+            st = 0;
+            parity ^= 1u;
+          }
+          if (i == 2 * x.t0) {  // Q of both M tiles once the previous piece's S products are done
+            if (!await(bar(B_QEMPTY), (qc & 1u) ^ 1u, aborted)) goto produced;
+            ++qc;
+            if (lane == 0) mbar_arrive_expect_tx(bar(B_QFULL), 4 * qbytes);
+            __syncwarp();
+            if (lane < 4)  // M tile lane / 2, d half lane % 2
+              tma_load_4d(sb + kOffQ + lane * kQHalf, &tm_q, bar(B_QFULL), (lane & 1) * 64, 0, x.h,
+                          x.r0 + (2 * x.rg + (lane >> 1)) * npb);
+            __syncwarp();
+          }
         }
       }
+    produced:
       if (*abort_flag) {  // let copies in flight land before the CTA's smem goes away
         for (uint32_t i = (issued > NS ? issued - NS : 0); i < issued; ++i)
           wait_bounded(bar(B_FULL + i % NS), (i / NS) & 1u, abort_flag, A.err, false);
@@ -686,35 +694,38 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       // ================================================================ S products
       constexpr uint32_t idS = idesc_bf16_f32(BM, BN, false);
       const bool paged = A.kv.layout == 1;
-      uint32_t qc = 0, r = 0, c = 0;  // pieces, ring tiles, products
-      bool ok = true;
-      while (ok && pieces.next(bar, smem, aborted, x)) {
-        if (!await(bar(B_QFULL), qc & 1u, aborted)) break;
-        ++qc;
+      uint32_t qc = 0, c = 0;        // pieces, products
+      uint32_t st = 0, parity = 0u;  // the next K tile's stage, and its wait's parity
+      while (pieces.next(bar, smem, aborted, x)) {
+        if (!await(bar(B_QFULL), qc++ & 1u, aborted)) break;
         const int mts = active1(x) ? 2 : 1;
-        for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
-          const uint32_t sk = r % NS;
-          const uint32_t ka = sb + kOffRing + sk * kTile;
+        for (int t = x.t0; t < x.t1; ++t) {
+          const uint32_t ka = sb + kOffRing + st * kTile;
           const uint32_t sbo = paged ? kPgGroup : 1024u, kh = paged ? kPgHalf : kKHalf;
 #pragma unroll 1
           for (int m = 0; m < mts; ++m) {
-            if (c > 0 && !await(bar(B_SFREE), (c - 1) & 1u, aborted)) { ok = false; break; }
-            ++c;
+            // (the first product waits for the phase before the first, which counts as done)
+            if (!await(bar(B_SFREE), (c++ & 1u) ^ 1u, aborted)) goto scored;
             // The K tile, after SFREE: a parity wait is sound from the phase before on and
             // not later, and the stage's tile before this one, V of three tiles before, has
             // landed when the softmax of M tile 0 has loaded S of the tile before (it then
             // has seen the PV product of that V tile done).
-            if (m == 0 && !await(bar(B_FULL + sk), (r / NS) & 1u, aborted)) { ok = false; break; }
+            if (m == 0 && !await(bar(B_FULL + st), parity, aborted)) goto scored;
             tc_fence_after();
             mma_s_group(tmem + kColS, sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024), sdesc_sw128(ka, 16, sbo),
                         sdesc_sw128(ka + kh, 16, sbo), idS);
             commit_elect(bar(B_SFULL + m));
           }
-          if (!ok) break;
-          commit_elect(bar(B_EMPTY + sk));
+          commit_elect(bar(B_EMPTY + st));
           if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
+          st += 2;
+          if (st >= NS) {
+            st -= NS;
+            parity ^= 1u;
+          }
         }
       }
+    scored:
       __syncwarp();
       commit_elect(bar(B_DRAIN));
       wait_bounded(bar(B_DRAIN), 0, abort_flag, A.err, false);
@@ -722,36 +733,37 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       // ================================================================ PV products
       constexpr uint32_t idO = idesc_bf16_f32(BM, D, true);
       const bool paged = A.kv.layout == 1;
-      uint32_t r = 1, c0 = 0, c1 = 0, done0 = 0, done1 = 0;  // ring tiles; products and pieces of each M tile
-      bool ok = true;
-      while (ok && pieces.next(bar, smem, aborted, x)) {
+      uint32_t c0 = 0, c1 = 0, done0 = 0, done1 = 0;  // products and pieces of each M tile
+      uint32_t st = 1, parity = 0u;                   // the next V tile's stage, and its wait's parity
+      while (pieces.next(bar, smem, aborted, x)) {
         const int mts = active1(x) ? 2 : 1;
-        for (int t = x.t0; ok && t < x.t1; ++t, r += 2) {
-          const uint32_t sv = r % NS;
+        for (int t = x.t0; t < x.t1; ++t) {
           // (the stage's K tile of two tiles before has landed: its S became the P that this
           // warp has waited for)
-          if (!await(bar(B_FULL + sv), (r / NS) & 1u, aborted)) { ok = false; break; }
+          if (!await(bar(B_FULL + st), parity, aborted)) goto multiplied;
           // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
           const uint64_t vd =
-              sdesc_sw128(sb + kOffRing + sv * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
+              sdesc_sw128(sb + kOffRing + st * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
 #pragma unroll 1
           for (int m = 0; m < mts; ++m) {
             // the first product of a piece takes O over from the epilogue of the one before
-            const uint32_t c = m ? c1++ : c0++;
-            if (t == x.t0) {
-              const uint32_t done = m ? done1++ : done0++;
-              if (done > 0 && !await(bar(B_OFREE + m), (done - 1) & 1u, aborted)) { ok = false; break; }
-            }
-            if (!await(bar(B_PFULL + m), c & 1u, aborted)) { ok = false; break; }
+            // (from none at first: the phase before the first counts as done)
+            if (t == x.t0 && !await(bar(B_OFREE + m), ((m ? done1++ : done0++) & 1u) ^ 1u, aborted)) goto multiplied;
+            if (!await(bar(B_PFULL + m), (m ? c1++ : c0++) & 1u, aborted)) goto multiplied;
             tc_fence_after();
             mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0 ? 1u : 0u);
             mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64 + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
             commit_elect(bar(B_PVDONE + m));
           }
-          if (!ok) break;
-          commit_elect(bar(B_EMPTY + sv));
+          commit_elect(bar(B_EMPTY + st));
+          st += 2;
+          if (st >= NS) {
+            st -= NS;
+            parity ^= 1u;
+          }
         }
       }
+    multiplied:
       __syncwarp();
       commit_elect(bar(B_DRAIN + 1));
       wait_bounded(bar(B_DRAIN + 1), 0, abort_flag, A.err, false);
