@@ -295,6 +295,24 @@ def test_prompt_whole_and_cut_units(cure):
     assert cure.cure_device_error() == 0
 
 
+@pytest.mark.parametrize("B,lo,hi,past,Hq,Hkv,ps", [(12, 300, 2500, 0, 28, 4, 16), (32, 1, 1500, 900, 4, 4, 0),
+                                                    (33, 700, 1400, 500, 2, 2, 0), (64, 0, 1100, 2000, 28, 4, 32),
+                                                    (255, 130, 520, 700, 8, 1, 16), (256, 128, 128, 1000, 16, 2, 8)])
+def test_prompt_ragged_batches_of_whole_units(cure, B, lo, hi, past, Hq, Hkv, ps):
+    """Units that are dealt out by length, for batches that the scheduler keeps in registers and larger ones; with
+    sequences of no rows among them and equal lengths."""
+    rng = np.random.default_rng(B)
+    n = [int(v) for v in rng.integers(lo, hi + 1, B)]
+    n[B // 2] = n[B // 3] = 0
+    n[B // 4] = n[0]
+    lens = [int(v) for v in rng.integers(0, past + 1, B)]
+    x = _case(cure, lens, n, Hq, Hkv, ps, B)
+    got = _run(cure, x)
+    _check(x, got, rows=[0, 17, 35, 36, 255, 256, 511, 899, -1])
+    assert torch.equal(got, _run(cure, x))  # and every row is written, the same way
+    assert torch.all((got != 3.5).any(-1)) and cure.cure_device_error() == 0
+
+
 def test_prompt_binding_refusals(cure):
     x = _case(cure, [0, 5], [4, 3], 8, 2, 16, 37)
     args = [x["q"], x["kc"], x["vc"], x["kv"], x["row_start"], x["cache_len"], SCALE]
