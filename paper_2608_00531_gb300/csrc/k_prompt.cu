@@ -334,6 +334,73 @@ __device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t ab
   return __all_sync(0xffffffffu, ok != 0);
 }
 
+
+// The products of a tile and one M tile, issued by a lane that is elected once for them
+// and the commit behind them, on descriptors in halves, so that a step is one addition.
+// (Groups of steps on 64-bit descriptors and a commit with its own election: 2 % more
+// time, 6 % on a prompt of 16384.  The ring stage's and Q's commits in here as well,
+// under conditions: 2 % more.)
+//
+// S = Q_m K^T: 8 steps of 16 dims, the second 64 dims kQHalf and (K: k2) further on.
+__device__ __forceinline__ void issue_s(uint32_t d, uint64_t qd, uint64_t kd, uint32_t k2, uint32_t idesc,
+                                        uint32_t full) {
+  static_assert(kQHalf >> 4 == 1024, "as the steps are written");
+  asm volatile(
+      "{\n\t.reg .pred pf, pt, el;\n\t.reg .b64 a, b;\n\t.reg .b32 x, y;\n\t"
+      "elect.sync _|el, 0xffffffff;\n\t"
+      "setp.ne.b32 pf, 0, 0;\n\t"
+      "setp.eq.b32 pt, 0, 0;\n\t"
+      "mov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pf;\n\t"
+      "add.u32 x, %1, 2;\n\tadd.u32 y, %3, 2;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pt;\n\t"
+      "add.u32 x, %1, 4;\n\tadd.u32 y, %3, 4;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pt;\n\t"
+      "add.u32 x, %1, 6;\n\tadd.u32 y, %3, 6;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pt;\n\t"
+      "add.u32 x, %1, 1024;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {%5, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pt;\n\t"
+      "add.u32 x, %1, 1026;\n\tadd.u32 y, %5, 2;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pt;\n\t"
+      "add.u32 x, %1, 1028;\n\tadd.u32 y, %5, 4;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pt;\n\t"
+      "add.u32 x, %1, 1030;\n\tadd.u32 y, %5, 6;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pt;\n\t"
+      "@el tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n\t}\n" ::"r"(d),
+      "r"((uint32_t)qd), "r"((uint32_t)(qd >> 32)), "r"((uint32_t)kd), "r"((uint32_t)(kd >> 32)), "r"((uint32_t)kd + k2),
+      "r"(idesc), "r"(full)
+      : "memory");
+}
+// O_m (+)= P_m V: 8 steps of 16 keys, P 8 columns of bf16 pairs and V a chunk further on each.
+__device__ __forceinline__ void issue_pv(uint32_t d, uint32_t p, uint64_t vd, uint32_t idesc, uint32_t accumulate,
+                                         uint32_t done) {
+  static_assert(kVChunk >> 4 == 256, "as the steps are written");
+  asm volatile(
+      "{\n\t.reg .pred p0, pt, el;\n\t.reg .b64 b;\n\t.reg .b32 x, y;\n\t"
+      "elect.sync _|el, 0xffffffff;\n\t"
+      "setp.ne.b32 p0, %5, 0;\n\t"
+      "setp.eq.b32 pt, 0, 0;\n\t"
+      "mov.b64 b, {%2, %3};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p0;\n\t"
+      "add.u32 x, %1, 8;\n\tadd.u32 y, %2, 256;\n\tmov.b64 b, {y, %3};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, pt;\n\t"
+      "add.u32 x, %1, 16;\n\tadd.u32 y, %2, 512;\n\tmov.b64 b, {y, %3};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, pt;\n\t"
+      "add.u32 x, %1, 24;\n\tadd.u32 y, %2, 768;\n\tmov.b64 b, {y, %3};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, pt;\n\t"
+      "add.u32 x, %1, 32;\n\tadd.u32 y, %2, 1024;\n\tmov.b64 b, {y, %3};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, pt;\n\t"
+      "add.u32 x, %1, 40;\n\tadd.u32 y, %2, 1280;\n\tmov.b64 b, {y, %3};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, pt;\n\t"
+      "add.u32 x, %1, 48;\n\tadd.u32 y, %2, 1536;\n\tmov.b64 b, {y, %3};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, pt;\n\t"
+      "add.u32 x, %1, 56;\n\tadd.u32 y, %2, 1792;\n\tmov.b64 b, {y, %3};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, pt;\n\t"
+      "@el tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t}\n" ::"r"(d),
+      "r"(p), "r"((uint32_t)vd), "r"((uint32_t)(vd >> 32)), "r"(idesc), "r"(accumulate), "r"(done)
+      : "memory");
+}
+
 // A role's place in the pieces that the scheduler has laid out.
 struct Pieces {
   uint32_t k;
@@ -470,8 +537,10 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             if (t * BN + 32 * (q + 1) > least) {
+              const int left = min(max(lim - 32 * q, 0), 32);  // keys of the block that the row sees
+              const uint32_t seen = left == 32 ? 0xffffffffu : (1u << left) - 1u;
 #pragma unroll
-              for (int k = 32 * q; k < 32 * (q + 1); ++k) x_[k] = k < lim ? x_[k] : -INFINITY;
+              for (int k = 0; k < 32; ++k) x_[32 * q + k] = (seen >> k) & 1u ? x_[32 * q + k] : -INFINITY;
             }
           }
         }
@@ -718,9 +787,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             // has seen the PV product of that V tile done).
             if (m == 0 && !await(bar(B_FULL + st), parity, aborted)) goto scored;
             tc_fence_after();
-            mma_s_group(tmem + kColS, sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024), sdesc_sw128(ka, 16, sbo),
-                        sdesc_sw128(ka + kh, 16, sbo), idS);
-            commit_elect(bar(B_SFULL + m));
+            issue_s(tmem + kColS, sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024), sdesc_sw128(ka, 16, sbo), kh >> 4,
+                    idS, bar(B_SFULL + m));
           }
           commit_elect(bar(B_EMPTY + st));
           if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
@@ -757,9 +825,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             if (t == x.t0 && !await(bar(B_OFREE + m), ((m ? done1++ : done0++) & 1u) ^ 1u, aborted)) goto multiplied;
             if (!await(bar(B_PFULL + m), (m ? c1++ : c0++) & 1u, aborted)) goto multiplied;
             tc_fence_after();
-            mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0 ? 1u : 0u);
-            mma_pv_group(tmem + kColO + m * D, tmem + kColP + m * 64 + 32, vd + ((4 * kVChunk) >> 4), idO, 1u);
-            commit_elect(bar(B_PVDONE + m));
+            issue_pv(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0, bar(B_PVDONE + m));
           }
           commit_elect(bar(B_EMPTY + st));
           st += 2;
