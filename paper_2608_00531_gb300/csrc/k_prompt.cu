@@ -342,8 +342,8 @@ __device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t ab
 // under conditions: 2 % more.)
 //
 // S = Q_m K^T: 8 steps of 16 dims, the second 64 dims kQHalf and (K: k2) further on.
-__device__ __forceinline__ void issue_s(uint32_t d, uint64_t qd, uint64_t kd, uint32_t k2, uint32_t idesc,
-                                        uint32_t full) {
+__device__ __forceinline__ void issue_s(uint32_t d, uint32_t q, uint32_t q_hi, uint32_t k, uint32_t k_hi, uint32_t k2,
+                                        uint32_t idesc, uint32_t full) {
   static_assert(kQHalf >> 4 == 1024, "as the steps are written");
   asm volatile(
       "{\n\t.reg .pred pf, pt, el;\n\t.reg .b64 a, b;\n\t.reg .b32 x, y;\n\t"
@@ -367,13 +367,13 @@ __device__ __forceinline__ void issue_s(uint32_t d, uint64_t qd, uint64_t kd, ui
       "add.u32 x, %1, 1030;\n\tadd.u32 y, %5, 6;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
       "@el tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %6, pt;\n\t"
       "@el tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%7];\n\t}\n" ::"r"(d),
-      "r"((uint32_t)qd), "r"((uint32_t)(qd >> 32)), "r"((uint32_t)kd), "r"((uint32_t)(kd >> 32)), "r"((uint32_t)kd + k2),
+      "r"(q), "r"(q_hi), "r"(k), "r"(k_hi), "r"(k2),
       "r"(idesc), "r"(full)
       : "memory");
 }
 // O_m (+)= P_m V: 8 steps of 16 keys, P 8 columns of bf16 pairs and V a chunk further on each.
-__device__ __forceinline__ void issue_pv(uint32_t d, uint32_t p, uint64_t vd, uint32_t idesc, uint32_t accumulate,
-                                         uint32_t done) {
+__device__ __forceinline__ void issue_pv(uint32_t d, uint32_t p, uint32_t v, uint32_t v_hi, uint32_t idesc,
+                                         uint32_t accumulate, uint32_t done) {
   static_assert(kVChunk >> 4 == 256, "as the steps are written");
   asm volatile(
       "{\n\t.reg .pred p0, pt, el;\n\t.reg .b64 b;\n\t.reg .b32 x, y;\n\t"
@@ -397,7 +397,7 @@ __device__ __forceinline__ void issue_pv(uint32_t d, uint32_t p, uint64_t vd, ui
       "add.u32 x, %1, 56;\n\tadd.u32 y, %2, 1792;\n\tmov.b64 b, {y, %3};\n\t"
       "@el tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %4, pt;\n\t"
       "@el tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t}\n" ::"r"(d),
-      "r"(p), "r"((uint32_t)vd), "r"((uint32_t)(vd >> 32)), "r"(idesc), "r"(accumulate), "r"(done)
+      "r"(p), "r"(v), "r"(v_hi), "r"(idesc), "r"(accumulate), "r"(done)
       : "memory");
 }
 
@@ -771,12 +771,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const bool paged = A.kv.layout == 1;
       uint32_t qc = 0, c = 0;        // pieces, products
       uint32_t st = 0, parity = 0u;  // the next K tile's stage, and its wait's parity
+      const uint64_t qd = sdesc_sw128(sb + kOffQ, 16, 1024);
+      const uint64_t kd = sdesc_sw128(sb + kOffRing, 16, paged ? kPgGroup : 1024u);
+      const uint32_t k2 = (paged ? kPgHalf : kKHalf) >> 4;
       while (pieces.next(bar, smem, aborted, x)) {
         if (!await(bar(B_QFULL), qc++ & 1u, aborted)) break;
         const int mts = active1(x) ? 2 : 1;
         for (int t = x.t0; t < x.t1; ++t) {
-          const uint32_t ka = sb + kOffRing + st * kTile;
-          const uint32_t sbo = paged ? kPgGroup : 1024u, kh = paged ? kPgHalf : kKHalf;
+          const uint32_t k = (uint32_t)kd + st * (kTile >> 4);
 #pragma unroll 1
           for (int m = 0; m < mts; ++m) {
             // (the first product waits for the phase before the first, which counts as done)
@@ -787,8 +789,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             // has seen the PV product of that V tile done).
             if (m == 0 && !await(bar(B_FULL + st), parity, aborted)) goto scored;
             tc_fence_after();
-            issue_s(tmem + kColS, sdesc_sw128(sb + kOffQ + 2 * m * kQHalf, 16, 1024), sdesc_sw128(ka, 16, sbo), kh >> 4,
-                    idS, bar(B_SFULL + m));
+            issue_s(tmem + kColS, (uint32_t)qd + m * (2 * kQHalf >> 4), (uint32_t)(qd >> 32), k, (uint32_t)(kd >> 32),
+                    k + k2, idS, bar(B_SFULL + m));
           }
           commit_elect(bar(B_EMPTY + st));
           if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
@@ -809,15 +811,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const bool paged = A.kv.layout == 1;
       uint32_t c0 = 0, c1 = 0, done0 = 0, done1 = 0;  // products and pieces of each M tile
       uint32_t st = 1, parity = 0u;                   // the next V tile's stage, and its wait's parity
+      // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
+      const uint64_t vd = sdesc_sw128(sb + kOffRing, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
       while (pieces.next(bar, smem, aborted, x)) {
         const int mts = active1(x) ? 2 : 1;
         for (int t = x.t0; t < x.t1; ++t) {
           // (the stage's K tile of two tiles before has landed: its S became the P that this
           // warp has waited for)
           if (!await(bar(B_FULL + st), parity, aborted)) goto multiplied;
-          // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
-          const uint64_t vd =
-              sdesc_sw128(sb + kOffRing + st * kTile, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
 #pragma unroll 1
           for (int m = 0; m < mts; ++m) {
             // the first product of a piece takes O over from the epilogue of the one before
@@ -825,7 +826,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             if (t == x.t0 && !await(bar(B_OFREE + m), ((m ? done1++ : done0++) & 1u) ^ 1u, aborted)) goto multiplied;
             if (!await(bar(B_PFULL + m), (m ? c1++ : c0++) & 1u, aborted)) goto multiplied;
             tc_fence_after();
-            issue_pv(tmem + kColO + m * D, tmem + kColP + m * 64, vd, idO, t > x.t0, bar(B_PVDONE + m));
+            issue_pv(tmem + kColO + m * D, tmem + kColP + m * 64, (uint32_t)vd + st * (kTile >> 4), (uint32_t)(vd >> 32), idO,
+                     t > x.t0, bar(B_PVDONE + m));
           }
           commit_elect(bar(B_EMPTY + st));
           st += 2;
