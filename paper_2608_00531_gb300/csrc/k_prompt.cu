@@ -33,17 +33,16 @@
 //
 // Bound and measured (us back to back; part of the measured 1929 TFLOP/s or 6.78 TB/s).
 // Many keys: the products, M128 N128 at one S at a time, with the softmax of the other
-// M tile under them.  One prompt of 16384, 64/8 heads: 2750, 1600 TFLOP/s, 0.83 (2880 in
-// runs of a second, where the power cap leaves 1.9 GHz: 0.88 of what a library product
-// keeps up then).  Shorter units add what starting and ending one costs, 1 to 2 tiles
-// of time: chunks of 8 prompts behind 1024 to 16000 tokens, 28/4 heads, 265, 0.73; 32
-// prompts of 33 to 4096 312, 0.69.  Single tokens: the cache's bytes, 64 sequences of 500
-// to 16000 tokens 182, 6.0 TB/s, 0.88.  One prompt of 200: 11.4, latency.
+// M tile under them.  One prompt of 16384, 64/8 heads: 2530, 1738 TFLOP/s, 0.90 (2700 in
+// runs of a second under the power cap: 0.94 of what a library product keeps up then).  Shorter units add what starting and ending one costs, 1 to 2 tiles
+// of time: chunks of 8 prompts behind 1024 to 16000 tokens, 28/4 heads, 260, 0.74; 32
+// prompts of 33 to 4096 305, 0.71.  Single tokens: the cache's bytes, 64 sequences of 500
+// to 16000 tokens 183, 6.0 TB/s, 0.88.  One prompt of 200: 11.4, latency.
 //
 // Code.  All roles run at once, and what they run between them is about what the
 // instruction cache holds: 169 KB of code, most of it the scheduler's copies of its
 // parts and the waits, made short units a seventh slower (200 prompts of 20 to 150: 73,
-// and 64 with 100 KB).  Hence one copy of everything, waits of ten instructions, and
+// and 64 with 100 KB, 61 with 95).  Hence one copy of everything, waits of ten instructions, and
 // nothing unrolled that need not be.  (Q of each M tile on barriers of its own, and O
 // packed into registers before it is stored: no faster, and a third slower on short
 // units, for that reason.)
