@@ -239,6 +239,77 @@ def test_step_from_projections_captured(mods):
     assert cure.cure_device_error() == 0
 
 
+@pytest.mark.parametrize("ps", [0, 16])
+def test_cache_offsets_past_32_bits(mods, ps):
+    """Rows appended and read more than 2^31 values into a cache."""
+    cure, step = mods
+    g = torch.Generator(device=DEV).manual_seed(21)
+    n = [3, 0, 150]
+    if ps == 0:
+        cap = 2_100_000  # sequence 2 starts at value 2.15e9
+        kv = cure.kv_desc(HKV, D, cap)
+        shape = (3, cap, HKV, D)
+        at = [torch.arange(b * cap, b * cap + m, device=DEV) for b, m in enumerate(n)]
+    else:
+        pages = 270_000
+        table = torch.full((3, 10), -1, dtype=torch.int32)
+        table[0, 0], table[2] = 5, torch.arange(pages - 1, pages - 11, -1)
+        kv = cure.kv_desc(HKV, D, 10, block_table=table.to(DEV), page_size=ps, num_pages=pages)
+        shape = (pages, ps, HKV, D)
+        at = [(table[b, np.arange(m) // ps].long() * ps + torch.arange(m) % ps).to(DEV) for b, m in enumerate(n)]
+    kc, vc = (torch.empty(shape, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    assert kc.numel() > 2 ** 31 and int(at[2].max()) * HKV * D > 2 ** 31
+    x = torch.empty(sum(n), (HQ + 2 * HKV) * D, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    p = step.PromptPass(sum(n), 3, HQ, kv, cure.rope_desc(D, BASE), DEV)
+    out = p.layer(0, x, _i32([0, 3, 3, 153]), _i32([0, 0, 0]), kc, vc)
+    y = x.unflatten(-1, (-1, D))
+    for b, r in ((0, slice(0, 3)), (2, slice(3, 153))):
+        k, v = (t.view(-1, HKV, D)[at[b]] for t in (kc, vc))
+        assert torch.equal(v, y[r, HQ + HKV:])
+        plain = cure.cure_rope_qkv(None, y[r, HQ:HQ + HKV], None, torch.arange(n[b], dtype=torch.int32, device=DEV),
+                                        p.rope)[1]
+        assert torch.equal(k, plain)
+        o, size = _attention(p.q[r], k, v, 0)
+        assert torch.all((out[r].double() - o).abs() <= 2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -10) * size)
+    assert cure.cure_device_error() == 0
+
+
+def test_prompt_pass_captured_and_two_at_once(mods):
+    """Two layers over some thousand rows, captured and replayed on other inputs; two passes on two streams."""
+    cure, step = mods
+    g = torch.Generator(device=DEV).manual_seed(23)
+    n = [2500, 1, 1800, 0, 1700]
+    start = _i32([0] + [int(v) for v in np.cumsum(n)])
+    lens = _i32([0, 300, 40, 7, 0])
+    a, b = (_Caches(cure, [2500, 400, 2000, 100, 1800]) for _ in range(2))
+    for t in a.k + a.v:
+        t.normal_(generator=g)
+    for t, u in zip(b.k + b.v, a.k + a.v):
+        t.copy_(u)
+    make = lambda c: step.PromptPass(sum(n), 5, HQ, c.kv, cure.rope_desc(D, BASE), DEV)  # noqa: E731
+    x = torch.empty(2, LAYERS, sum(n), (HQ + 2 * HKV) * D, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+
+    def run(p, c, qkv, stream=None):
+        return [p.layer(l, qkv[l], start, lens, c.k[l], c.v[l], stream=stream) for l in range(LAYERS)]
+    p, q = make(a), make(b)
+    want = [[t.clone() for t in run(p, a, x[i])] for i in range(2)]
+    graph, qkv = torch.cuda.CUDAGraph(), x[0].clone()
+    with torch.cuda.graph(graph):
+        outs = run(p, a, qkv)
+    for i in (0, 1, 0):
+        qkv.copy_(x[i])
+        graph.replay()
+        assert all(torch.equal(s, t) for s, t in zip(outs, want[i]))
+    torch.cuda.synchronize()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        got = run(p, a, x[0], s), run(q, b, x[1], t)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(torch.equal(u, w) for u, w in zip(got[i], want[i]))
+    assert cure.cure_device_error() == 0
+
+
 def test_refusals(mods):
     cure, step = mods
     c = _Caches(cure, [32])
