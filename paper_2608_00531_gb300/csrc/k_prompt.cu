@@ -304,35 +304,11 @@ struct Walk {
   }
 };
 
-// A wait of all lanes of a warp: false where the CTA gives up, because this wait or
-// another has run out of tc::kWaitTimeoutCycles (which is reported at the CTA's end).
-// As tc::wait_warp, in half the code: what the roles run between them fits the
-// instruction cache or does not.  With the 64-bit clock, the report and two tries in
-// each of the 17 waits 8 prompts of 2048 took 213 us, so 206.
+// The roles' waits.  What the roles run between them fits the instruction cache or does
+// not: with tc::wait_warp in the 17 places 8 prompts of 2048 took 213 us, so 206.
 __device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t abort_flag) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .b32 t0, t;\n\t"
-      "mov.u32 t0, %%clock;\n"
-      "AGAIN:\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "@p bra DONE;\n\t"
-      "ld.volatile.shared.u32 t, [%3];\n\t"
-      "setp.ne.u32 q, t, 0;\n\t"
-      "@q bra DONE;\n\t"
-      "mov.u32 t, %%clock;\n\t"
-      "sub.u32 t, t, t0;\n\t"
-      "setp.gt.u32 q, t, %4;\n\t"
-      "@q st.volatile.shared.u32 [%3], 1;\n\t"
-      "bra AGAIN;\n"
-      "DONE:\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}\n"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(abort_flag), "n"((uint32_t)kWaitTimeoutCycles)
-      : "memory");
-  return __all_sync(0xffffffffu, ok != 0);
+  return wait_compact<(uint32_t)kWaitTimeoutCycles>(bar, parity, abort_flag);
 }
-
 
 // The products of a tile and one M tile, issued by a lane that is elected once for them
 // and the commit behind them, on descriptors in halves, so that a step is one addition.

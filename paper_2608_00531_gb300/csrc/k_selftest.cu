@@ -1,6 +1,7 @@
-// Failure-detection self-test: the library's bounded pipeline wait, run on a
-// barrier that nothing ever completes.  The wait must give up after its limit,
-// raise CURE_DEVERR_TIMEOUT in the device error word and return, leaving the
+// Failure-detection self-test: the library's bounded pipeline waits, run on a
+// barrier that nothing ever completes.  The compact one (with a limit of 2^20 cycles)
+// must set the abort flag and return false; then the other must give up after its
+// limit, raise CURE_DEVERR_TIMEOUT in the device error word and return, leaving the
 // context usable.  No fault, trap or hang is involved.
 #include "common.cuh"
 #include "tc_ptx.cuh"
@@ -17,6 +18,10 @@ __global__ void selftest_wait_kernel(int* err, long long limit) {
     tc::fence_mbar_init();
   }
   __syncthreads();
+  if (tc::wait_compact<1u << 20>(tc::smem_u32(&bar), 0, tc::smem_u32(&abort_flag))) return;
+  if (*const_cast<volatile int*>(&abort_flag) != 1) return;
+  __syncwarp();
+  if (threadIdx.x == 0) abort_flag = 0;
   if (threadIdx.x == 0) tc::wait_bounded(tc::smem_u32(&bar), 0, &abort_flag, err, true, limit);
 }
 

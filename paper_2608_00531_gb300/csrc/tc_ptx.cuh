@@ -43,7 +43,7 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
 }
 
 // Bounded wait on the phase of the given parity.  Every pipeline wait in the
-// library goes through it: after `limit` cycles (about half a second by
+// library goes through it or wait_compact: after `limit` cycles (about half a second by
 // default) it sets the CTA's abort flag, raises CURE_DEVERR_TIMEOUT in the
 // device error word and returns false, so that a logic error surfaces as an
 // error status instead of a hung GPU.  With `honour_abort` it also returns
@@ -62,6 +62,34 @@ __device__ __forceinline__ bool wait_bounded(uint32_t bar, uint32_t parity, vola
       return false;
     }
   }
+}
+
+// The same for all lanes of a warp in about half the code: false where the CTA gives up,
+// because this wait has run out (which sets the abort flag, a shared-memory address) or
+// another has set it.  Who calls it reports the flag at the CTA's end.
+template <uint32_t LIMIT>
+__device__ __forceinline__ bool wait_compact(uint32_t bar, uint32_t parity, uint32_t abort_flag) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b32 t0, t;\n\t"
+      "mov.u32 t0, %%clock;\n"
+      "AGAIN:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra DONE;\n\t"
+      "ld.volatile.shared.u32 t, [%3];\n\t"
+      "setp.ne.u32 q, t, 0;\n\t"
+      "@q bra DONE;\n\t"
+      "mov.u32 t, %%clock;\n\t"
+      "sub.u32 t, t, t0;\n\t"
+      "setp.gt.u32 q, t, %4;\n\t"
+      "@q st.volatile.shared.u32 [%3], 1;\n\t"
+      "bra AGAIN;\n"
+      "DONE:\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(abort_flag), "n"(LIMIT)
+      : "memory");
+  return __all_sync(0xffffffffu, ok != 0);
 }
 
 // ---------------------------------------------------------------- proxies
