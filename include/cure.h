@@ -469,8 +469,9 @@ cure_status cure_device_error(void* stream, int32_t* bits);
  * library's bounded pipeline waits, the two that every kernel's barrier waits go
  * through, on a barrier that nothing ever completes: the compact one for 2^20 SM
  * clock cycles, then the other with a limit of `limit_cycles` (1 .. 2^30, the
- * kernels' own limit).  Each gives up; the last raises CURE_DEVERR_TIMEOUT in the device error word and
- * returns; cure_device_error() then reports it, and the context stays usable.
+ * kernels' own limit).  Each gives up; the last raises CURE_DEVERR_TIMEOUT in the
+ * device error word and returns; cure_device_error() then reports it, and the
+ * context stays usable.
  */
 cure_status cure_selftest_wait_timeout(int64_t limit_cycles, void* stream);
 
