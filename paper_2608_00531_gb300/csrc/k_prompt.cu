@@ -34,10 +34,11 @@
 // Bound and measured (us back to back; part of the measured 1929 TFLOP/s or 6.78 TB/s).
 // Many keys: the products, M128 N128 at one S at a time, with the softmax of the other
 // M tile under them.  One prompt of 16384, 64/8 heads: 2530, 1738 TFLOP/s, 0.90 (2700 in
-// runs of a second under the power cap: 0.94 of what a library product keeps up then).  Shorter units add what starting and ending one costs, 1 to 2 tiles
-// of time: chunks of 8 prompts behind 1024 to 16000 tokens, 28/4 heads, 260, 0.74; 32
-// prompts of 33 to 4096 305, 0.71.  Single tokens: the cache's bytes, 64 sequences of 500
-// to 16000 tokens 183, 6.0 TB/s, 0.88.  One prompt of 200: 11.4, latency.
+// runs of a second under the power cap: 0.94 of what a library product keeps up then).
+// Shorter units add what starting and ending one costs, 1 to 2 tiles of time: chunks of
+// 8 prompts behind 1024 to 16000 tokens, 28/4 heads, 260, 0.74; 32 prompts of 33 to 4096
+// 305, 0.71.  Single tokens: the cache's bytes, 64 sequences of 500 to 16000 tokens 183,
+// 6.0 TB/s, 0.88.  One prompt of 200: 11.4, latency.
 //
 // Code.  All roles run at once, and what they run between them is about what the
 // instruction cache holds: 169 KB of code, most of it the scheduler's copies of its
@@ -801,8 +802,8 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
             if (t == x.t0 && !await(bar(B_OFREE + m), ((m ? done1++ : done0++) & 1u) ^ 1u, aborted)) goto multiplied;
             if (!await(bar(B_PFULL + m), (m ? c1++ : c0++) & 1u, aborted)) goto multiplied;
             tc_fence_after();
-            issue_pv(tmem + kColO + m * D, tmem + kColP + m * 64, (uint32_t)vd + st * (kTile >> 4), (uint32_t)(vd >> 32), idO,
-                     t > x.t0, bar(B_PVDONE + m));
+            issue_pv(tmem + kColO + m * D, tmem + kColP + m * 64, (uint32_t)vd + st * (kTile >> 4),
+                     (uint32_t)(vd >> 32), idO, t > x.t0, bar(B_PVDONE + m));
           }
           commit_elect(bar(B_EMPTY + st));
           st += 2;
