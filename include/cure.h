@@ -183,7 +183,8 @@ cure_status cure_build_tree(const cure_tree_params* p, const int32_t* top_ids, c
  * aligned.
  * workspace: device scratch of at least cure_tree_attn_workspace_size() bytes,
  * 256-byte aligned (split-KV partial results); its contents on entry do not
- * matter.  Calls that can overlap on the GPU must not share a workspace.
+ * matter.  Calls that can overlap on the GPU must not share a workspace; after
+ * CURE_DEVERR_TIMEOUT zero it before a captured call is replayed on it.
  * The kernel is launched as a programmatic dependent launch: it starts its
  * set-up while the previous kernel on the stream finishes and waits for that
  * kernel before reading any argument, so stream order is kept.

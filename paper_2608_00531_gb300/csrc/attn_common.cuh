@@ -21,8 +21,8 @@ struct AttnArgs {
   int units_max;   // piece counters in the workspace
   int unit_cost;   // fixed cost of a unit in the stream-K split, in 64-key tile times
   float scale_log2;
-  int* cnt;        // [units_max] (launch tag << 9) | pieces arrived, per unit
-  uint32_t tag;    // this launch's tag (set by the launcher)
+  PieceCount* cnt; // [units_max] (launch tag << 9) | pieces arrived, per unit
+  uint64_t tag;    // this launch's tag (set by the launcher)
   float* ws_o;     // [units_max + kAttnMaxCtas][32][256] float4 partial outputs
   float* ws_lse;   // [(units_max + kAttnMaxCtas) * 256] partial base-2 log-sum-exps
   uint16_t* out;

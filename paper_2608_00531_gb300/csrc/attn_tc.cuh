@@ -141,30 +141,32 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t
 }
 
 // A unit's piece counter holds (launch tag << 9) | pieces arrived.  A word
-// whose tag is not this launch's (left by an aborted launch, or never
-// written) counts as zero, so the workspace needs no reset; a completed unit
-// leaves zero behind, so an old word can only match a later tag if its launch
-// was aborted exactly 2^23 - 1 launches earlier.
+// whose tag is not this launch's (left by an aborted launch or by another user
+// of the memory, or never written) counts as zero, so the workspace needs no
+// reset.  Tags have 55 bits, far from each other and from small integers
+// (next_launch_tag): with 23 bits counted up from 1, words such as token ids
+// were taken for counts.  A completed unit leaves zero behind, which counts as
+// zero for the same call replayed from a graph, with the same tag.
 constexpr int kCountBits = 9;
 constexpr int kCountMask = (1 << kCountBits) - 1;
-__device__ __forceinline__ int count_of(int v, uint32_t tag) {
-  return ((uint32_t)v >> kCountBits) == tag ? (v & kCountMask) : 0;
+__device__ __forceinline__ int count_of(PieceCount v, uint64_t tag) {
+  return (v >> kCountBits) == tag ? (int)(v & kCountMask) : 0;
 }
 // This piece's arrival (after its release fence): the pieces arrived so far,
 // this one included.
-__device__ __forceinline__ int arrive(int* cnt, uint32_t tag) {
-  int old = *reinterpret_cast<volatile int*>(cnt);
+__device__ __forceinline__ int arrive(PieceCount* cnt, uint64_t tag) {
+  PieceCount old = *reinterpret_cast<volatile PieceCount*>(cnt);
   while (true) {
-    const int nw = (int)((tag << kCountBits) | (uint32_t)(count_of(old, tag) + 1));
-    const int prev = atomicCAS(cnt, old, nw);
-    if (prev == old) return nw & kCountMask;
+    const PieceCount nw = (PieceCount)(tag << kCountBits) | (PieceCount)(count_of(old, tag) + 1);
+    const PieceCount prev = atomicCAS(cnt, old, nw);
+    if (prev == old) return (int)(nw & kCountMask);
     old = prev;
   }
 }
 
-__device__ __forceinline__ int ld_acquire(const int* p) {
-  int v;
-  asm volatile("ld.acquire.gpu.global.b32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+__device__ __forceinline__ PieceCount ld_acquire(const PieceCount* p) {
+  PieceCount v;
+  asm volatile("ld.acquire.gpu.global.b64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
   return v;
 }
 

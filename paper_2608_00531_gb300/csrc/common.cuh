@@ -23,6 +23,12 @@ struct ApiRange {
 int* device_error_word();
 int num_sms();
 
+// A word of an attention workspace that counts a unit's pieces.
+using PieceCount = unsigned long long;
+// A number of 55 bits for a launch to mark its counters with: no two launches of
+// a process get the same one, and any other word has it by a chance of 2^-55.
+uint64_t next_launch_tag();
+
 // Device address of a __device__ variable of this library in the current
 // device's current context.  The address belongs to the context (a reset or
 // a re-created primary context gets a new one), so the cache is keyed by the

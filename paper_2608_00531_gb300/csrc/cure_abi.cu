@@ -5,6 +5,8 @@
 #include <math.h>
 #include <nvtx3/nvToolsExt.h>
 
+#include <atomic>
+#include <chrono>
 #include <mutex>
 
 #include "common.cuh"
@@ -135,6 +137,16 @@ int num_sms() {
     g_sms[d] = v;
   }
   return g_sms[d];
+}
+
+uint64_t next_launch_tag() {
+  // steps of an odd number, modulo 2^55: as many different tags, and neighbours lie
+  // far apart; from a start that differs from process to process
+  static std::atomic<uint64_t> launches{0};
+  static const uint64_t start =
+      (uint64_t)std::chrono::system_clock::now().time_since_epoch().count() ^ reinterpret_cast<uintptr_t>(&launches);
+  constexpr uint64_t kStep = 0x5851f42d4c957f;
+  return ((start + launches.fetch_add(1) + 1) * kStep) & ((1ull << 55) - 1);
 }
 
 }  // namespace cure

@@ -69,8 +69,8 @@ extern "C" cure_status cure_tree_attn_noalloc(const void* q, const void* tree_k,
   void* scratch = nullptr;
   if (device_symbol_address(cache, g_attn_scratch, &scratch) != cudaSuccess) return CURE_ERR_CUDA;
   // Nothing in the array is cleared.  Its front holds the split units' piece
-  // counters: every launch tags its counter words with a fresh launch number,
-  // a word carrying another launch's tag counts as zero, and a unit whose
+  // counters: every launch tags its counter words with a number of its own,
+  // a word without this launch's tag counts as zero, and a unit whose
   // pieces have all arrived writes zero back.  Every partial result that is
   // read back was written earlier in the same launch.
   const cudaError_t e = launch_tree_attn(

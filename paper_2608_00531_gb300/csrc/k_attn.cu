@@ -2,7 +2,7 @@
 // tcgen05 tree-attention kernel (k_attn_tc.cu).
 //
 // Workspace layout (caller-owned, 256-byte aligned):
-//   cnt     int32 [units_max], 256-byte rounded   (launch tag << 9) | pieces arrived,
+//   cnt     int64 [units_max], 256-byte rounded   (launch tag << 9) | pieces arrived,
 //                                                 per unit (any initial contents)
 //   ws_o    fp32  [units_max + kAttnMaxCtas][32][256] float4: per piece slot, column-major
 //                 partial outputs (float4 column c of row r at [slot][c][r])
@@ -24,7 +24,7 @@ bool plan_tree_attn(int batch, int n_max, int heads_q, const cure_kv_desc& kv, A
   const int rg_max = (n_max + 2 * npb - 1) / (2 * npb);
   AttnPlan p;
   p.units_max = batch * kv.heads_kv * rg_max;
-  p.ws_cnt = ((size_t)p.units_max * sizeof(int) + 255) / 256 * 256;
+  p.ws_cnt = ((size_t)p.units_max * sizeof(PieceCount) + 255) / 256 * 256;
   const size_t rows = (size_t)(p.units_max + kAttnMaxCtas) * 2 * kAttnRowsCta;
   p.ws_o = rows * kAttnD * sizeof(float);
   p.ws_lse = (rows * sizeof(float) + 255) / 256 * 256;
@@ -91,7 +91,7 @@ cudaError_t launch_tree_attn(const AttnPlan& plan, const uint16_t* q, const uint
   A.unit_cost = kAttnUnitCost;
   A.scale_log2 = scale * 1.4426950408889634f;
   char* ws = reinterpret_cast<char*>(workspace);
-  A.cnt = reinterpret_cast<int*>(ws);
+  A.cnt = reinterpret_cast<PieceCount*>(ws);
   A.ws_o = reinterpret_cast<float*>(ws + plan.ws_cnt);
   A.ws_lse = reinterpret_cast<float*>(ws + plan.ws_cnt + plan.ws_o);
   A.out = out;

@@ -1226,11 +1226,8 @@ cudaError_t launch_tree_attn_tc(const AttnArgs& A, const AttnRoute& route, cudaS
   ok = ok && make_kv_map(&mtk, tk, trows, Hkv, BN) && make_v_rows_map(&mtv, tv, trows, Hkv) &&
        make_q_map(&mq, A.q, trows, Hkv, A.G, BM / A.G);
   if (!ok) return cudaErrorInvalidValue;
-  // a fresh tag per launch makes the piece counters left in the workspace
-  // count as zero (1 .. 2^23 - 1; zero-filled memory is never current)
-  static std::atomic<uint32_t> launches{0};
   AttnArgs a = A;
-  a.tag = launches.fetch_add(1) % ((1u << (32 - kCountBits)) - 1) + 1;
+  a.tag = next_launch_tag();  // whatever the workspace's counters hold counts as zero
   cudaLaunchAttribute attr[2];
   cudaLaunchConfig_t cfg = cluster_config(attr, dim3(route.ctas), A.cluster > 0 ? A.cluster : 1);
   cfg.stream = s;

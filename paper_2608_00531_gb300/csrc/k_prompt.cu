@@ -102,8 +102,8 @@ struct PromptArgs {
   const int32_t* cache_len;
   int rows, batch, heads_q, G, cap;
   float scale_log2;
-  int* cnt;       // [CTAs] (launch tag << 9) | pieces arrived of the unit whose first piece the CTA has
-  uint32_t tag;   // this launch's tag
+  PieceCount* cnt;  // [CTAs] (launch tag << 9) | pieces arrived of the unit whose first piece the CTA has
+  uint64_t tag;     // this launch's tag
   float* ws_o;    // [2 * CTAs][32][256] float4 partial outputs
   float* ws_lse;  // [2 * CTAs][256] their base-2 log-sum-exps
   float* ws_inv;  // [CTAs][2 M tiles][128 rows] reciprocal row sums, softmax to epilogue
@@ -1115,7 +1115,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 // log-sum-exps [2 * CTAs]: of a CTA's pieces at most its first and its last are
 // parts of a unit; and the row sums that softmax warps leave for the epilogue.
 namespace {
-size_t counter_bytes(int ctas) { return ((size_t)ctas * sizeof(int) + 255) / 256 * 256; }
+size_t counter_bytes(int ctas) { return ((size_t)ctas * sizeof(PieceCount) + 255) / 256 * 256; }
 }  // namespace
 
 size_t prompt_attn_workspace() {
@@ -1161,12 +1161,10 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
   A.scale_log2 = scale * 1.4426950408889634f;
   A.out = out;
   A.err = err;
-  // a fresh tag per launch makes what the workspace's counters held count as zero
-  static std::atomic<uint32_t> launches{0};
-  A.tag = launches.fetch_add(1) % ((1u << (32 - kCountBits)) - 1) + 1;
+  A.tag = next_launch_tag();  // whatever the workspace's counters hold counts as zero
   const int ctas = num_sms();
   char* ws = static_cast<char*>(workspace);
-  A.cnt = reinterpret_cast<int*>(ws);
+  A.cnt = reinterpret_cast<PieceCount*>(ws);
   A.ws_o = reinterpret_cast<float*>(ws + counter_bytes(ctas));
   A.ws_lse = A.ws_o + (size_t)2 * ctas * 2 * BM * D;
   A.ws_inv = A.ws_lse + (size_t)2 * ctas * 2 * BM;
