@@ -506,14 +506,8 @@ def cure_prompt_attn_workspace_size(rows: int, batch: int, heads_q: int, kv: KVD
     return int(_lib.load().cure_prompt_attn_workspace_size(rows, batch, heads_q, C.byref(kv)))
 
 
-def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv: KVDesc,
-                     row_start: torch.Tensor, cache_len: torch.Tensor, scale: float, *,
-                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
-                     stream=None) -> torch.Tensor:
-    """Causal attention of packed rows over the cache for one layer: whole prompts, further chunks, single tokens.
-
-    q bf16 [rows][heads_q][D]; sequence b's rows row_start[b] .. row_start[b+1] - 1 stand at positions cache_len[b],
-    cache_len[b] + 1, .., and their K and V are in the cache already (cure_append_kv at the same lengths)."""
+def _prompt_attn_args(q, k_cache, v_cache, kv: KVDesc, row_start, cache_len, scale, out, workspace, stream):
+    """cure_prompt_attn's output and its C arguments, checked."""
     dev, s = _current(stream)
     B = _ragged(row_start, cache_len, kv)
     shape = q.shape
@@ -527,10 +521,22 @@ def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
         size = cure_prompt_attn_workspace_size(shape[0], B, shape[1], kv)
         workspace = _new((max(size, 256),), torch.uint8, stream)
     kc, vc = _caches(k_cache, v_cache, kv, B, dev)
-    check("cure_prompt_attn", _lib.load().cure_prompt_attn(
-        _here(q, "q", _BF16, dev), kc, vc, C.byref(kv), _here(row_start, "row_start", _I32, dev),
-        _here(cache_len, "cache_len", _I32, dev), shape[0], B, shape[1], scale, _here(out, "out", _BF16, dev),
-        _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s))
+    return out, (_here(q, "q", _BF16, dev), kc, vc, C.byref(kv), _here(row_start, "row_start", _I32, dev),
+                 _here(cache_len, "cache_len", _I32, dev), shape[0], B, shape[1], scale, _here(out, "out", _BF16, dev),
+                 _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s)
+
+
+def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv: KVDesc,
+                     row_start: torch.Tensor, cache_len: torch.Tensor, scale: float, *,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """Causal attention of packed rows over the cache for one layer: whole prompts, further chunks, single tokens.
+
+    q bf16 [rows][heads_q][D]; sequence b's rows row_start[b] .. row_start[b+1] - 1 stand at positions cache_len[b],
+    cache_len[b] + 1, .., and their K and V are in the cache already (cure_append_kv at the same lengths).  Up to 256
+    sequences and 2^22 rows."""
+    out, args = _prompt_attn_args(q, k_cache, v_cache, kv, row_start, cache_len, scale, out, workspace, stream)
+    check("cure_prompt_attn", _lib.load().cure_prompt_attn(*args))
     return out
 
 

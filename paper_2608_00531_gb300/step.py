@@ -65,16 +65,24 @@ class PromptPass:
 
     Sequence b's rows row_start[b] .. row_start[b+1] - 1 stand at positions cache_len[b], cache_len[b] + 1, ..; all
     layers run at the same lengths, and ``advance`` gives the lengths after the pass.  q_norm, k_norm: a weight
-    (bf16 [D]) per layer, or None."""
+    (bf16 [D]) per layer, or None.  Up to 256 sequences and 2^22 rows, as cure_prompt_attn takes.  A pass holds the
+    rotated rows and the attention's workspace: its layers run in one order, not on several streams at once."""
 
     def __init__(self, rows: int, batch: int, heads_q: int, kv: cure.KVDesc, rope: Optional[cure.Rope],
                  device: torch.device, q_norm=None, k_norm=None, eps: float = 1e-6):
         self.rows, self.B, self.Hq, self.kv, self.rope = rows, batch, heads_q, kv, rope
         self.q_norm, self.k_norm, self.eps = q_norm, k_norm, eps
         self.scale = 1.0 / float(kv.head_dim) ** 0.5
+        ws = self._workspace_size(rows, batch)
         self.q = torch.empty(rows, heads_q, kv.head_dim, dtype=torch.bfloat16, device=device)
-        ws = cure.cure_prompt_attn_workspace_size(rows, batch, heads_q, kv)
-        self.workspace = torch.empty(max(ws, 256), dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(ws, dtype=torch.uint8, device=device)
+
+    def _workspace_size(self, rows: int, batch: int) -> int:
+        ws = cure.cure_prompt_attn_workspace_size(rows, batch, self.Hq, self.kv)
+        if ws == 0:
+            raise ValueError(f"PromptPass: cure_prompt_attn does not take {rows} rows of {batch} sequences with "
+                             f"{self.Hq} / {self.kv.heads_kv} heads of {self.kv.head_dim}")
+        return ws
 
     def layer(self, l: int, qkv: torch.Tensor, row_start: torch.Tensor, cache_len: torch.Tensor, k_cache: torch.Tensor,
               v_cache: torch.Tensor, *, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -83,11 +91,19 @@ class PromptPass:
         if n > self.rows:
             raise ValueError(f"PromptPass was made for {self.rows} rows, got {n}")
         q, k, v = _parts(qkv, self.Hq, self.kv.heads_kv, self.kv.head_dim)
-        q = cure.cure_append_kv(k, v, k_cache, v_cache, self.kv, row_start, cache_len, self.rope, q=q,
-                                q_norm=_of_layer(self.q_norm, l), k_norm=_of_layer(self.k_norm, l), eps=self.eps,
-                                out=self.q[:n], stream=stream)
-        return cure.cure_prompt_attn(q, k_cache, v_cache, self.kv, row_start, cache_len, self.scale, out=out,
-                                     workspace=self.workspace, stream=stream)
+        # what the attention would refuse is refused before anything is appended
+        if cache_len.numel() > self.B:
+            self._workspace_size(n, cache_len.numel())
+        rows = self.q[:n]
+        out, args = cure._prompt_attn_args(rows, k_cache, v_cache, self.kv, row_start, cache_len, self.scale, out,
+                                           self.workspace, stream)
+        if out.data_ptr() % 16:
+            raise ValueError("out must be 16-byte aligned")
+        cure.cure_append_kv(k, v, k_cache, v_cache, self.kv, row_start, cache_len, self.rope, q=q,
+                            q_norm=_of_layer(self.q_norm, l), k_norm=_of_layer(self.k_norm, l), eps=self.eps,
+                            out=rows, stream=stream)
+        cure.check("cure_prompt_attn", cure._lib.load().cure_prompt_attn(*args))
+        return out
 
     @staticmethod
     def advance(row_start: torch.Tensor, cache_len: torch.Tensor) -> torch.Tensor:
