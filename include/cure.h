@@ -413,9 +413,12 @@ cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t l
  * q may be NULL (then q_out is not used); otherwise its rows go to q_out as in
  * cure_rope_qkv.  cache_len is not advanced: every layer of a model is appended
  * at the same lengths.  Rows outside row_start[0] .. row_start[batch] - 1 are
- * left out.  A slot past the capacity (CURE_DEVERR_SLOT), a missing or bad page
- * (CURE_DEVERR_PAGE) and a row_start that does not ascend from 0 or above
- * (CURE_DEVERR_NODES) leave the rows concerned out.  q, k, v, the norms, strides and alignment as in
+ * left out.  A slot past the capacity (CURE_DEVERR_SLOT) and a missing or bad page
+ * (CURE_DEVERR_PAGE) leave the rows concerned out.  Where row_start does not ascend
+ * from 0 or above, a row is written for a sequence whose range holds it or left out:
+ * with CURE_DEVERR_NODES if entries of row_start lie on both sides of it, without
+ * if it stands before row_start[0] or behind every other entry (cure_prompt_attn
+ * reports every such sequence).  q, k, v, the norms, strides and alignment as in
  * cure_rope_qkv; caches 16-byte aligned; the inputs may not overlap the caches.
  * No two rows of a call may have the same slot of the same page.
  */
