@@ -392,8 +392,11 @@ cure_status cure_rope_init_freqs(cure_rope* out, int32_t style, int32_t rot_dim,
  * may be parts of one projection's rows.  A tensor and its output may both be
  * NULL (left out).  An output may be its input (same address and stride); any
  * other overlap is not allowed.  head_dim = 128; all pointers 16-byte aligned,
- * strides multiples of 8 values that hold a row's heads.  The angles are exact
- * to 2^-32 of a turn at every position.  eps >= 0 and finite.
+ * strides multiples of 8 values that hold a row's heads.  An angle is off by less
+ * than 2^-25 of a turn (its fraction is rounded to a float at the end) and p times
+ * what turns[i] is off by: below 2^-53 for the plain frequencies, as they are made
+ * from 64-bit floats (p < 2^28: together below 2^-24; any p: below 2^-21).
+ * eps >= 0 and finite.
  */
 cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
                           int32_t rows, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const int32_t* pos,

@@ -9,9 +9,10 @@
 //
 // for the pair (a, b) of frequency i of a head at position p.  The angle is
 // kept in turns: f_i / 2 pi is a 64-bit binary fraction, so that p times it
-// modulo 2^64 is the exact fraction of a turn of that product at any position
-// (an error of p 2^-65 turns, below 2^-34 at every int32 position); its upper
-// 32 bits go to a float and through sincospif.
+// modulo 2^64 is the exact fraction of a turn of that product at any position;
+// what the table's entry is off by (it comes from 64-bit floats: below 2^-53 turns
+// for the plain frequencies) counts p times.  The fraction's upper 32 bits go to a
+// float, which rounds them by up to 2^-26 of a turn, and through sincospif.
 //
 // Layout.  Half a warp holds a head, 8 values a lane, and a warp takes a range of
 // one row's heads with the row's cosines and sines (times the norm weights) in
