@@ -455,8 +455,11 @@ cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t 
  * 256-byte aligned (what parts of a long row group hand to the part that joins
  * them); its contents on entry do not matter.  Calls that can overlap on the GPU
  * must not share a workspace, captured ones included; after CURE_DEVERR_TIMEOUT zero
- * it before a captured call is replayed on it.  The result does not depend on how a
- * call's work was shared out: the same bits call after call.
+ * it before a captured call is replayed on it.  The same call on the same device
+ * gives the same bits, call after call.  Where a long row group is cut into parts
+ * depends on the other sequences of the batch and on the number of SMs, and a
+ * row's last bits on where: it may differ within the rounding above between one
+ * batch and another.
  */
 cure_status cure_prompt_attn(const void* q, const void* k_cache, const void* v_cache, const cure_kv_desc* kv,
                              const int32_t* row_start, const int32_t* cache_len, int32_t rows, int32_t batch,
