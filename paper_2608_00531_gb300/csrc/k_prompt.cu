@@ -1025,11 +1025,13 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   }
 
   // ---- the units that this CTA joins, by all warps and with equal registers again
+  // (behind the barrier: a warp that had nothing to do must not take back the registers
+  // that a softmax warp still waits for, or with all of them gone that wait has no end)
   __syncwarp();
-  if (warp < 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 128;");
-  else asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
   tc_fence_before();
   __syncthreads();
+  if (warp < 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 128;");
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
   if (*abort_flag) {
     if (tid == 0) flag(A.err, CURE_DEVERR_TIMEOUT);
   } else {
