@@ -496,6 +496,19 @@ cure_status cure_selftest_lm_head_timeout(const void* hidden, const void* w_lm, 
                                           int32_t rank, int64_t limit_cycles, void* stream);
 
 /*
+ * Failure-detection self-test: cure_prompt_attn with a wait that runs out, after 2^20
+ * SM clock cycles, in one of the roles of its first CTA: the `wait`-th (from 1) of warp
+ * `warp` (0 .. 15), if it comes to that many.  CURE_DEVERR_TIMEOUT is then raised, and
+ * rows that the CTA had a part in may be left unwritten; the others are as ever, and so
+ * is the next call, on the same workspace too.
+ */
+cure_status cure_selftest_prompt_timeout(const void* q, const void* k_cache, const void* v_cache,
+                                         const cure_kv_desc* kv, const int32_t* row_start, const int32_t* cache_len,
+                                         int32_t rows, int32_t batch, int32_t heads_q, float scale, void* out,
+                                         void* workspace, size_t workspace_bytes, int32_t warp, int32_t wait,
+                                         void* stream);
+
+/*
  * Self-test: the form a cure_tree_attn call of this shape takes (`kv` and
  * `route` are HOST pointers; in_place != 0: the in-place layout).  route[0] is
  * the number of CTAs in each unit's cluster (0: the persistent form), route[1]

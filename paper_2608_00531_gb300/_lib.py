@@ -20,7 +20,7 @@ DEVERR_PAGE, DEVERR_SLOT, DEVERR_NODES, DEVERR_TOKEN, DEVERR_TIMEOUT = 0x1, 0x2,
 # every entry point the header declares
 EXPORTS = ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_tree_attn_workspace_size",
            "cure_accept", "cure_lm_head_argmax", "cure_lm_head_workspace_size", "cure_selftest_wait_timeout",
-           "cure_selftest_lm_head_timeout", "cure_selftest_attn_route",
+           "cure_selftest_lm_head_timeout", "cure_selftest_prompt_timeout", "cure_selftest_attn_route",
            "cure_sample_target", "cure_resync_kv", "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv",
            "cure_append_kv", "cure_prompt_attn", "cure_prompt_attn_workspace_size", "cure_device_error",
            "cure_status_string", "cure_abi_version")
@@ -99,6 +99,7 @@ def load() -> C.CDLL:
     lib.cure_append_kv.argtypes = [P, P, P, I64, I64, I64, I32, I32, I32, P, P, P, C.POINTER(KVDesc), P, P,
                                    C.POINTER(Rope), P, P, C.c_float, P, I64, P]
     lib.cure_prompt_attn.argtypes = [P, P, P, C.POINTER(KVDesc), P, P, I32, I32, I32, C.c_float, P, P, C.c_size_t, P]
+    lib.cure_selftest_prompt_timeout.argtypes = [*lib.cure_prompt_attn.argtypes[:-1], I32, I32, P]
     lib.cure_prompt_attn_workspace_size.argtypes = [I32, I32, I32, C.POINTER(KVDesc)]
     lib.cure_prompt_attn_workspace_size.restype = C.c_size_t
     lib.cure_device_error.argtypes = [P, C.POINTER(I32)]

@@ -133,12 +133,13 @@ struct RopeArgs {
 };
 cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s);
 
-// Causal attention of packed prompt rows over the cache.
+// Causal attention of packed prompt rows over the cache.  expire_warp >= 0 (self-test): that
+// warp's expire_wait-th wait in CTA 0 is on a barrier that nothing completes.
 size_t prompt_attn_workspace();
 cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
                                const cure_kv_desc& kv, const int32_t* row_start, const int32_t* cache_len, int rows,
                                int batch, int heads_q, float scale, uint16_t* out, void* workspace, int* err,
-                               cudaStream_t s);
+                               cudaStream_t s, int expire_warp = -1, int expire_wait = 0);
 
 // Fused LM head + argmax: launch plan for a shape (persistent pairs of CTAs, one
 // tile of nt hidden rows each, the vocabulary's 256-id tiles split into `groups`

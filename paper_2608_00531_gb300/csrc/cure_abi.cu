@@ -554,11 +554,10 @@ size_t cure_prompt_attn_workspace_size(int32_t rows, int32_t batch, int32_t head
   return prompt_shape_ok(rows, batch, heads_q, kv) == CURE_OK ? prompt_attn_workspace() : 0;
 }
 
-cure_status cure_prompt_attn(const void* q, const void* k_cache, const void* v_cache, const cure_kv_desc* kv,
-                             const int32_t* row_start, const int32_t* cache_len, int32_t rows, int32_t batch,
-                             int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
-                             void* stream) {
-  ApiRange range("cure_prompt_attn");
+static cure_status prompt_attn(const void* q, const void* k_cache, const void* v_cache, const cure_kv_desc* kv,
+                               const int32_t* row_start, const int32_t* cache_len, int32_t rows, int32_t batch,
+                               int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
+                               void* stream, int expire_warp, int expire_wait) {
   const cure_status st = prompt_shape_ok(rows, batch, heads_q, kv);
   if (st != CURE_OK) return st;
   if (!(scale > 0.f && scale <= FLT_MAX)) return CURE_ERR_INVALID_ARG;
@@ -571,7 +570,26 @@ cure_status cure_prompt_attn(const void* q, const void* k_cache, const void* v_c
   return from_cuda(launch_prompt_attn(static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_cache),
                                       static_cast<const uint16_t*>(v_cache), *kv, row_start, cache_len, rows, batch,
                                       heads_q, scale, static_cast<uint16_t*>(out), workspace, device_error_word(),
-                                      static_cast<cudaStream_t>(stream)));
+                                      static_cast<cudaStream_t>(stream), expire_warp, expire_wait));
+}
+
+cure_status cure_prompt_attn(const void* q, const void* k_cache, const void* v_cache, const cure_kv_desc* kv,
+                             const int32_t* row_start, const int32_t* cache_len, int32_t rows, int32_t batch,
+                             int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  ApiRange range("cure_prompt_attn");
+  return prompt_attn(q, k_cache, v_cache, kv, row_start, cache_len, rows, batch, heads_q, scale, out, workspace,
+                     workspace_bytes, stream, -1, 0);
+}
+
+cure_status cure_selftest_prompt_timeout(const void* q, const void* k_cache, const void* v_cache,
+                                         const cure_kv_desc* kv, const int32_t* row_start, const int32_t* cache_len,
+                                         int32_t rows, int32_t batch, int32_t heads_q, float scale, void* out,
+                                         void* workspace, size_t workspace_bytes, int32_t warp, int32_t wait,
+                                         void* stream) {
+  if (warp < 0 || warp > 15 || wait < 1) return CURE_ERR_INVALID_ARG;
+  return prompt_attn(q, k_cache, v_cache, kv, row_start, cache_len, rows, batch, heads_q, scale, out, workspace,
+                     workspace_bytes, stream, warp, wait);
 }
 
 cure_status cure_device_error(void* stream, int32_t* bits) {

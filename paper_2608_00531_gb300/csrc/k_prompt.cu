@@ -81,7 +81,8 @@ constexpr int kOffMisc = kOffRing + NS * kTile;
 enum {
   B_QFULL = 0, B_QEMPTY = 1, B_SFREE = 2, B_FULL = 3, B_EMPTY = B_FULL + NS, B_SFULL = B_EMPTY + NS,
   B_PFULL = B_SFULL + 2, B_PVDONE = B_PFULL + 2, B_STAT = B_PVDONE + 2, B_OFREE = B_STAT + 2, B_DRAIN = B_OFREE + 2,
-  B_JOIN = B_DRAIN + 2, B_PIECE = B_JOIN + 1, B_TAKEN = B_PIECE + kPieces, kNumBars = B_TAKEN + kPieces
+  B_JOIN = B_DRAIN + 2, B_PIECE = B_JOIN + 1, B_TAKEN = B_PIECE + kPieces, B_NEVER = B_TAKEN + kPieces,
+  kNumBars = B_NEVER + 1
 };
 constexpr int kOffTmemSlot = kOffMisc + 8 * kNumBars;
 constexpr int kOffAbort = kOffTmemSlot + 4;
@@ -109,6 +110,7 @@ struct PromptArgs {
   float* ws_inv;  // [CTAs][2 M tiles][128 rows] reciprocal row sums, softmax to epilogue
   uint16_t* out;
   int* err;
+  int expire_warp, expire_wait;  // self-test: the wait of CTA 0 that runs out, by its warp and number from 1
 };
 
 // Positions.  Every unit takes kUnitCost positions (what starting and ending a
@@ -307,9 +309,22 @@ struct Walk {
 
 // The roles' waits.  What the roles run between them fits the instruction cache or does
 // not: with tc::wait_warp in the 17 places 8 prompts of 2048 took 213 us, so 206.
-__device__ __forceinline__ bool await(uint32_t bar, uint32_t parity, uint32_t abort_flag) {
-  return wait_compact<(uint32_t)kWaitTimeoutCycles>(bar, parity, abort_flag);
-}
+template <bool EXPIRE>
+struct Await {
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, uint32_t abort_flag) {
+    return wait_compact<(uint32_t)kWaitTimeoutCycles>(bar, parity, abort_flag);
+  }
+};
+// In the self-test's kernel one wait of one warp is for what never comes.
+template <>
+struct Await<true> {
+  uint32_t never;  // a barrier that nothing completes
+  uint32_t left;   // waits up to and with that one (0: none)
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, uint32_t abort_flag) {
+    if (left > 0 && --left == 0) return wait_compact<1u << 20>(never, 0, abort_flag);
+    return wait_compact<(uint32_t)kWaitTimeoutCycles>(bar, parity, abort_flag);
+  }
+};
 
 // The products of a tile and one M tile, issued by a lane that is elected once for them
 // and the commit behind them, on descriptors in halves, so that a step is one addition.
@@ -381,7 +396,8 @@ __device__ __forceinline__ void issue_pv(uint32_t d, uint32_t p, uint32_t v, uin
 struct Pieces {
   uint32_t k;
   // The next one; false when there is none or the CTA has given up.  (All lanes of a warp.)
-  __device__ __forceinline__ bool next(const Bar& bar, const uint8_t* smem, uint32_t aborted, Piece& x) {
+  template <class Wait>
+  __device__ __forceinline__ bool next(Wait& await, const Bar& bar, const uint8_t* smem, uint32_t aborted, Piece& x) {
     const uint32_t slot = k % kPieces;
     if (!await(bar(B_PIECE + slot), (k / kPieces) & 1u, aborted)) return false;
     const int4* p = reinterpret_cast<const int4*>(smem + kOffPieces + slot * (kPieceInts * 4));
@@ -408,6 +424,7 @@ __device__ __forceinline__ void st_global_32(uint16_t* p, const uint32_t* v, boo
   }
 }
 
+template <bool EXPIRE>
 __global__ void __launch_bounds__(kThreads, 1)
 prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                    const __grid_constant__ CUtensorMap tm_q, const PromptArgs A) {
@@ -446,6 +463,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       mbar_init(bar(B_PIECE + i), 1);
       mbar_init(bar(B_TAKEN + i), kTakers);
     }
+    if constexpr (EXPIRE) mbar_init(bar(B_NEVER), 1);
     *abort_flag = 0;
     *n_joins = 0;
     fence_mbar_init();
@@ -468,6 +486,11 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmemSlot);
+  Await<EXPIRE> await;
+  if constexpr (EXPIRE) {
+    await.never = bar(B_NEVER);
+    await.left = blockIdx.x == 0 && warp == A.expire_warp ? (uint32_t)A.expire_wait : 0u;
+  }
   Pieces pieces{0};
   Piece x;
   // M tile 1 of a piece is active when its first row is one of the sequence's
@@ -486,7 +509,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     uint32_t sc = 0, r = 0;  // tiles of this M tile, ring tiles
     bool ok = true;
     uint32_t done = 0;  // pieces of this M tile
-    while (ok && pieces.next(bar, smem, aborted, x)) {
+    while (ok && pieces.next(await, bar, smem, aborted, x)) {
       const uint32_t r_piece = r;
       r += 2 * (uint32_t)(x.t1 - x.t0);
       if (m == 1 && !active1(x)) continue;
@@ -623,7 +646,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       mbar_arrive(bar(B_JOIN));
       return ok = await(bar(B_JOIN), joins++ & 1u, aborted);
     };
-    while (ok && pieces.next(bar, smem, aborted, x)) {
+    while (ok && pieces.next(await, bar, smem, aborted, x)) {
       const bool whole = x.t1 - x.t0 == x.T;
       const int64_t slot = 2 * (int64_t)blockIdx.x + (x.t0 == 0);
 #pragma unroll 1
@@ -685,7 +708,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const uint32_t qbytes = (uint32_t)(npb * G * 128);
       uint32_t qc = 0, issued = 0;   // pieces, ring tiles
       uint32_t st = 0, parity = 1u;  // the next ring tile's stage, and its wait's parity
-      while (pieces.next(bar, smem, aborted, x)) {
+      while (pieces.next(await, bar, smem, aborted, x)) {
         auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
           const int tok = t * BN + lane * ps;
           if (lane >= ppt || tok >= x.keys) return -1;
@@ -750,7 +773,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       const uint64_t qd = sdesc_sw128(sb + kOffQ, 16, 1024);
       const uint64_t kd = sdesc_sw128(sb + kOffRing, 16, paged ? kPgGroup : 1024u);
       const uint32_t k2 = (paged ? kPgHalf : kKHalf) >> 4;
-      while (pieces.next(bar, smem, aborted, x)) {
+      while (pieces.next(await, bar, smem, aborted, x)) {
         if (!await(bar(B_QFULL), qc++ & 1u, aborted)) break;
         const int mts = active1(x) ? 2 : 1;
         for (int t = x.t0; t < x.t1; ++t) {
@@ -789,7 +812,7 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       uint32_t st = 1, parity = 0u;                   // the next V tile's stage, and its wait's parity
       // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
       const uint64_t vd = sdesc_sw128(sb + kOffRing, paged ? kPgHalf : kVHalf, paged ? kPgGroup : 1024u);
-      while (pieces.next(bar, smem, aborted, x)) {
+      while (pieces.next(await, bar, smem, aborted, x)) {
         const int mts = active1(x) ? 2 : 1;
         for (int t = x.t0; t < x.t1; ++t) {
           // (the stage's K tile of two tiles before has landed: its S became the P that this
@@ -1128,15 +1151,17 @@ size_t prompt_attn_workspace() {
 cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const uint16_t* v_cache,
                                const cure_kv_desc& kv, const int32_t* row_start, const int32_t* cache_len, int rows,
                                int batch, int heads_q, float scale, uint16_t* out, void* workspace, int* err,
-                               cudaStream_t s) {
+                               cudaStream_t s, int expire_warp, int expire_wait) {
   static std::atomic<uint64_t> done{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(done.load() & bit)) {
-    e = cudaFuncSetAttribute(prompt_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-    if (e != cudaSuccess) return e;
+    for (auto kernel : {prompt_attn_kernel<false>, prompt_attn_kernel<true>}) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+      if (e != cudaSuccess) return e;
+    }
     done.fetch_or(bit);
   }
   const int Hkv = kv.heads_kv, G = heads_q / Hkv;
@@ -1163,6 +1188,8 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
   A.scale_log2 = scale * 1.4426950408889634f;
   A.out = out;
   A.err = err;
+  A.expire_warp = expire_warp;
+  A.expire_wait = expire_wait;
   A.tag = next_launch_tag();  // whatever the workspace's counters hold counts as zero
   const int ctas = num_sms();
   char* ws = static_cast<char*>(workspace);
@@ -1185,7 +1212,8 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = (int64_t)rows * heads_q > (int64_t)4 * 2 * BM * ctas ? 0 : 1;
-  return cudaLaunchKernelEx(&cfg, prompt_attn_kernel, mk, mv, mq, A);
+  return cudaLaunchKernelEx(&cfg, expire_warp < 0 ? prompt_attn_kernel<false> : prompt_attn_kernel<true>, mk, mv, mq,
+                            A);
 }
 
 }  // namespace cure

@@ -566,6 +566,18 @@ def cure_selftest_lm_head_timeout(hidden: torch.Tensor, w_lm: torch.Tensor, rank
     return out
 
 
+def cure_selftest_prompt_timeout(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv: KVDesc,
+                                 row_start: torch.Tensor, cache_len: torch.Tensor, scale: float, warp: int, wait: int, *,
+                                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                 stream=None) -> torch.Tensor:
+    """cure_prompt_attn with the `wait`-th wait of one warp of its first CTA running out (a failure-detection
+    self-test); read the outcome with cure_device_error()."""
+    out, args = _prompt_attn_args(q, k_cache, v_cache, kv, row_start, cache_len, scale, out, workspace, stream)
+    check("cure_selftest_prompt_timeout",
+          _lib.load().cure_selftest_prompt_timeout(*args[:-1], int(warp), int(wait), args[-1]))
+    return out
+
+
 def cure_selftest_attn_route(batch: int, n_max: int, heads_q: int, kv: KVDesc, in_place: bool) -> tuple[int, bool, int]:
     """The form a tree-attention call of this shape takes: CTAs per unit's cluster
     (0: persistent), pieces in two tile slots in turn, CTAs of the grid."""
