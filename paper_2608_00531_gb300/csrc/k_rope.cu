@@ -288,10 +288,16 @@ cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s) {
   RopeArgs a = args;
   const int heads = a.heads_q + 2 * a.heads_kv;
   // Few rows: a row's heads in parts, of one step's heads where all parts are resident
-  // at once, so that a row is over after one round of loads.  Many: a warp a row, so
-  // that its angles serve all heads (10940 rows of 36 heads: 44 us, in parts of 24 / 16 /
-  // 8 heads 49 / 60 / 70).  Between one and two waves of whole rows the second would be
-  // mostly idle: parts of two steps (4096 rows of 80 heads: 37 -> 32 us).
+  // at once, so that a row is over after one round of loads (us replayed, parts of 8 / 16
+  // / 32 heads / whole rows: 300 rows of 36 normed heads 3.8 / 4.5 / 6.5 / 6.8; 758 6.2 /
+  // 6.2 / 6.8 / 7.2; 1000 6.8 / 6.5 / 7.9 / 7.2; 758 rows of 80 heads 8.6 / 7.9 / 8.7 /
+  // 12.0).  Many: a warp a row, so that its angles serve all heads (2566 rows of 36 normed
+  // heads 16.1 / 16.7 / 17.7 / 13.6, 9000 of them 47.8 / 44.1 / 43.8 / 35.2).  In a second
+  // wave of whole rows that is mostly idle, parts of two steps are faster: up to some 11/8
+  // of a wave, and with 40 heads or more (with 36 the third part is a quarter full).  Parts
+  // of 16 / whole rows, normed: 80 heads, 4096 rows 34.9 / 39.2, 5000 41.6 / 42.0, 5472
+  // 45.2 / 43.6, 7200 58.0 / 50.2; 40 heads, 4096 21.7 / 23.1, 5000 25.8 / 24.6; 36 heads,
+  // 4096 22.9 / 21.6, 7200 35.8 / 27.2.
   const int64_t resident = (int64_t)num_sms() * 3 * kWarps;
   a.chunk_heads = heads;
   for (int n = 2 * kUnroll; n < heads; n *= 2)
@@ -299,7 +305,8 @@ cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s) {
       a.chunk_heads = n;
       break;
     }
-  if (a.chunk_heads == heads && a.rows > resident && a.rows < 2 * resident) a.chunk_heads = 4 * kUnroll;
+  if (a.chunk_heads == heads && heads >= 40 && a.rows > resident && 8 * (int64_t)a.rows < 11 * resident)
+    a.chunk_heads = 4 * kUnroll;
   a.chunks = (heads + a.chunk_heads - 1) / a.chunk_heads;
   const int64_t blocks = ((int64_t)a.rows * a.chunks + kWarps - 1) / kWarps;
   auto kernel = a.rope.style == 1 ? (append ? rope_kernel<true, true> : rope_kernel<false, true>)
