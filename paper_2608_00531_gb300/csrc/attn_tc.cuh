@@ -1,5 +1,7 @@
-// What the attention kernels on tcgen05 share: their MMA groups, TMA loads and
-// maps, waits by whole warps and packed arithmetic.
+// What the attention kernels on tcgen05 share: TMA loads and maps, commits, piece
+// counters and packed arithmetic; and the tree attention's MMA groups and waits by
+// whole warps (the prompt attention issues a tile of 128 keys at a time, with its
+// commit, and waits in less code: k_prompt.cu).
 #pragma once
 
 #include <cuda_bf16.h>

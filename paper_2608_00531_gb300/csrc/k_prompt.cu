@@ -36,8 +36,8 @@
 // M tile under them.  One prompt of 16384, 64/8 heads: 2530, 1738 TFLOP/s, 0.90 (2700 in
 // runs of a second under the power cap: 0.94 of what a library product keeps up then).
 // Shorter units add what starting and ending one costs, 1 to 2 tiles of time: chunks of
-// 8 prompts behind 1024 to 16000 tokens, 28/4 heads, 260, 0.74; 32 prompts of 33 to 4096
-// 305, 0.71.  Single tokens: the cache's bytes, 64 sequences of 500 to 16000 tokens 183,
+// 8 prompts behind 1024 to 16000 tokens, 28/4 heads, 260, 0.74 (279 in long runs); 32
+// prompts of 33 to 4096 305, 0.71 (329).  Single tokens: the cache's bytes, 64 sequences of 500 to 16000 tokens 183,
 // 6.0 TB/s, 0.88.  One prompt of 200: 11.4, latency.
 //
 // Code.  All roles run at once, and what they run between them is about what the
@@ -117,7 +117,8 @@ struct PromptArgs {
 // piece costs, in key times) and then one for each key of the last row that its
 // row group could have; tile t of it stands at the position of its first key.
 constexpr int kUnitCost = 2 * BN;
-// What joining the parts of units costs a call, and the fewest positions worth a CTA.
+// What joining the parts of units costs a call (7 to 8 us: a prompt of 200 or 1024 cut
+// needlessly), and the fewest positions worth a CTA.
 constexpr int kJoinCost = 8 * BN;
 constexpr int kMinShare = 3 * BN;
 // Units of fewer positions on average, and those of a batch of more than 32, are
@@ -890,7 +891,14 @@ prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
       // half of the longest one.  Longest first they end with an even share, or with the
       // (k + 1)-th round of units as long as those that it starts with; some 3 % more.  Cut
       // units end with an even share, which the pieces' fixed costs upset by some 8 %, and
-      // the joins.
+      // the joins.  Both ways, forced, us whole / cut, with whole : cut as estimated here:
+      //   one prompt of 200, 32/8 heads  10.9 / 18.5 (0.41)   8 chunks of up to 1024  477 / 551 (0.93)
+      //   one of 1024                    20.2 / 27.3 (0.73)   32 prompts up to 4096   801 / 884 (0.94)
+      //   8 of 700, 28/4 heads           43.9 / 41.8 (0.81)   64 chunks of up to 300  636 / 702 (0.99)
+      //   8 of 2048, 32/8 heads           208 / 223 (0.91)    single tokens of 256     202 / 189 (0.99)
+      //   100 of up to 1500, 28/4 heads   523 / 578 (0.92)    of 64, 4000 keys each   86.9 / 92.6 (1.06)
+      //   one of 16384, 64/8 heads       2687 / 2757 (0.95)   of 64, 500 to 16000      219 / 174 (1.34)
+      // The wrong side is taken by up to 7 %, within some 20 % of the border.
       const float share = __fdividef((float)cost, (float)walk.P);
       const float cut = 1.08f * share + kJoinCost;
       float whole = (float)(longest + kUnitCost);
