@@ -41,7 +41,7 @@ bool kv_ok(const cure_kv_desc* kv, cure_status* why) {
     return false;
   }
   if (kv->layout == 1) {
-    if (kv->page_size < 1 || kv->num_pages < 1 || !kv->block_table) return false;
+    if (kv->page_size < 1 || kv->num_pages < 1 || !kv->block_table || !aligned(kv->block_table, 4)) return false;
     if ((int64_t)kv->max_len * kv->page_size > INT32_MAX ||
         (int64_t)kv->num_pages * kv->page_size > INT32_MAX)
       return false;
@@ -488,7 +488,7 @@ cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t l
   if (st != CURE_OK) return st;
   if (head_dim != 128) return head_dim < 1 ? CURE_ERR_INVALID_ARG : CURE_ERR_UNSUPPORTED;
   if (rows == 0 || (heads_q == 0 && heads_kv == 0) || (!q && !k && !v)) return CURE_OK;
-  if (!pos) return CURE_ERR_INVALID_ARG;
+  if (!pos || !aligned(pos, 4)) return CURE_ERR_INVALID_ARG;
   if (rope) a.rope = *rope;
   a.err = device_error_word();
   return from_cuda(launch_rope(a, false, static_cast<cudaStream_t>(stream)));
@@ -533,7 +533,8 @@ cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t 
   const cure_status st = rope_args_ok(a, rope);
   if (st != CURE_OK) return st;
   if (rows == 0 || batch == 0) return CURE_OK;
-  if (!k || !v || !row_start || !cache_len) return CURE_ERR_INVALID_ARG;
+  if (!k || !v || !row_start || !cache_len || !aligned(row_start, 4) || !aligned(cache_len, 4) || !aligned(pos, 4))
+    return CURE_ERR_INVALID_ARG;
   if (rope) a.rope = *rope;
   a.err = device_error_word();
   return from_cuda(launch_rope(a, true, static_cast<cudaStream_t>(stream)));
@@ -564,7 +565,7 @@ static cure_status prompt_attn(const void* q, const void* k_cache, const void* v
   if (rows == 0 || batch == 0) return CURE_OK;
   if (!q || !k_cache || !v_cache || !row_start || !cache_len || !out || !workspace) return CURE_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) ||
-      !aligned(workspace, 256))
+      !aligned(workspace, 256) || !aligned(row_start, 4) || !aligned(cache_len, 4))
     return CURE_ERR_INVALID_ARG;
   if (workspace_bytes < prompt_attn_workspace()) return CURE_ERR_CAPACITY;
   return from_cuda(launch_prompt_attn(static_cast<const uint16_t*>(q), static_cast<const uint16_t*>(k_cache),
