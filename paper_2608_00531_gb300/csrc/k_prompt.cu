@@ -1160,17 +1160,17 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
                                const cure_kv_desc& kv, const int32_t* row_start, const int32_t* cache_len, int rows,
                                int batch, int heads_q, float scale, uint16_t* out, void* workspace, int* err,
                                cudaStream_t s, int expire_warp, int expire_wait) {
-  static std::atomic<uint64_t> done{0};
+  const bool expire = expire_warp >= 0;
+  const auto kernel = expire ? prompt_attn_kernel<true> : prompt_attn_kernel<false>;
+  static std::atomic<uint64_t> ready[2];  // devices on which each has its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
-  if (!(done.load() & bit)) {
-    for (auto kernel : {prompt_attn_kernel<false>, prompt_attn_kernel<true>}) {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-      if (e != cudaSuccess) return e;
-    }
-    done.fetch_or(bit);
+  if (!(ready[expire].load() & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e != cudaSuccess) return e;
+    ready[expire].fetch_or(bit);
   }
   const int Hkv = kv.heads_kv, G = heads_q / Hkv;
   CUtensorMap mk, mv, mq;
@@ -1220,8 +1220,7 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = (int64_t)rows * heads_q > (int64_t)4 * 2 * BM * ctas ? 0 : 1;
-  return cudaLaunchKernelEx(&cfg, expire_warp < 0 ? prompt_attn_kernel<false> : prompt_attn_kernel<true>, mk, mv, mq,
-                            A);
+  return cudaLaunchKernelEx(&cfg, kernel, mk, mv, mq, A);
 }
 
 }  // namespace cure
