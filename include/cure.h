@@ -443,16 +443,17 @@ cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t 
  * q, out: bf16 [rows][heads_q][D], out not overlapping any input; k_cache,
  * v_cache: one layer in the layout of `kv` (a HOST pointer).  Accumulation is
  * float32, with a rounding of up to 2^-24 of the sum for each 128 keys; the
- * probabilities are rounded to bf16 before the PV product.  A sequence of more
- * than 2^25 keys may be given up with CURE_DEVERR_TIMEOUT: what one CTA has to do
- * of it can outlast the limit of the kernel's waits.  What lies in the cache behind a sequence's last key does not matter; the V rows of
- * the sequence's own keys must be finite (a key that a row does not see weighs 0
- * in the product, not nothing).  Rows outside row_start[0] .. row_start[batch] - 1
- * are left unwritten, and so are the rows of a sequence that does not fit its
- * capacity (CURE_DEVERR_SLOT) or whose row_start does not ascend within
- * 0 .. rows (CURE_DEVERR_NODES).  A missing or bad page counts as zeros
- * (CURE_DEVERR_PAGE).  batch <= 256, rows <= 2^22, D = 128, heads_q / heads_kv <=
- * 128, scale > 0 and finite; all base pointers 16-byte aligned.
+ * probabilities are rounded to bf16 before the PV product.  A sequence of more than
+ * 2^25 keys may be given up with CURE_DEVERR_TIMEOUT: what one CTA has to do of it
+ * can outlast the limit of the kernel's waits.  What lies in the cache behind a
+ * sequence's last key does not matter; the V rows of the sequence's own keys must be
+ * finite (a key that a row does not see weighs 0 in the product, not nothing).  Rows
+ * outside row_start[0] .. row_start[batch] - 1 are left unwritten, and so are the
+ * rows of a sequence that does not fit its capacity (CURE_DEVERR_SLOT) or whose
+ * row_start does not ascend within 0 .. rows (CURE_DEVERR_NODES).  A missing or bad
+ * page counts as zeros (CURE_DEVERR_PAGE).  batch <= 256, rows <= 2^22, D = 128,
+ * heads_q / heads_kv <= 128, scale > 0 and finite; all base pointers 16-byte
+ * aligned.
  * workspace: device scratch of at least cure_prompt_attn_workspace_size() bytes,
  * 256-byte aligned (what parts of a long row group hand to the part that joins
  * them); its contents on entry do not matter.  Calls that can overlap on the GPU
