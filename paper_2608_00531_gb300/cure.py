@@ -507,7 +507,7 @@ def cure_prompt_attn_workspace_size(rows: int, batch: int, heads_q: int, kv: KVD
 
 
 def _prompt_attn_args(q, k_cache, v_cache, kv: KVDesc, row_start, cache_len, scale, out, workspace, stream):
-    """cure_prompt_attn's output and its C arguments, checked."""
+    """cure_prompt_attn's output, its workspace (to be held until the call is launched) and its C arguments, checked."""
     dev, s = _current(stream)
     B = _ragged(row_start, cache_len, kv)
     shape = q.shape
@@ -521,9 +521,10 @@ def _prompt_attn_args(q, k_cache, v_cache, kv: KVDesc, row_start, cache_len, sca
         size = cure_prompt_attn_workspace_size(shape[0], B, shape[1], kv)
         workspace = _new((max(size, 256),), torch.uint8, stream)
     kc, vc = _caches(k_cache, v_cache, kv, B, dev)
-    return out, (_here(q, "q", _BF16, dev), kc, vc, C.byref(kv), _here(row_start, "row_start", _I32, dev),
-                 _here(cache_len, "cache_len", _I32, dev), shape[0], B, shape[1], scale, _here(out, "out", _BF16, dev),
-                 _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s)
+    return out, workspace, (
+        _here(q, "q", _BF16, dev), kc, vc, C.byref(kv), _here(row_start, "row_start", _I32, dev),
+        _here(cache_len, "cache_len", _I32, dev), shape[0], B, shape[1], scale, _here(out, "out", _BF16, dev),
+        _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s)
 
 
 def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv: KVDesc,
@@ -535,7 +536,7 @@ def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     q bf16 [rows][heads_q][D]; sequence b's rows row_start[b] .. row_start[b+1] - 1 stand at positions cache_len[b],
     cache_len[b] + 1, .., and their K and V are in the cache already (cure_append_kv at the same lengths).  Up to 256
     sequences and 2^22 rows."""
-    out, args = _prompt_attn_args(q, k_cache, v_cache, kv, row_start, cache_len, scale, out, workspace, stream)
+    out, held, args = _prompt_attn_args(q, k_cache, v_cache, kv, row_start, cache_len, scale, out, workspace, stream)
     check("cure_prompt_attn", _lib.load().cure_prompt_attn(*args))
     return out
 
@@ -572,7 +573,7 @@ def cure_selftest_prompt_timeout(q: torch.Tensor, k_cache: torch.Tensor, v_cache
                                  stream=None) -> torch.Tensor:
     """cure_prompt_attn with the `wait`-th wait of one warp of its first CTA running out (a failure-detection
     self-test); read the outcome with cure_device_error()."""
-    out, args = _prompt_attn_args(q, k_cache, v_cache, kv, row_start, cache_len, scale, out, workspace, stream)
+    out, held, args = _prompt_attn_args(q, k_cache, v_cache, kv, row_start, cache_len, scale, out, workspace, stream)
     check("cure_selftest_prompt_timeout",
           _lib.load().cure_selftest_prompt_timeout(*args[:-1], int(warp), int(wait), args[-1]))
     return out

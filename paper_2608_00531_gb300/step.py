@@ -95,8 +95,8 @@ class PromptPass:
         if cache_len.numel() > self.B:
             self._workspace_size(n, cache_len.numel())
         rows = self.q[:n]
-        out, args = cure._prompt_attn_args(rows, k_cache, v_cache, self.kv, row_start, cache_len, self.scale, out,
-                                           self.workspace, stream)
+        out, _, args = cure._prompt_attn_args(rows, k_cache, v_cache, self.kv, row_start, cache_len, self.scale, out,
+                                              self.workspace, stream)
         if out.data_ptr() % 16:
             raise ValueError("out must be 16-byte aligned")
         cure.cure_append_kv(k, v, k_cache, v_cache, self.kv, row_start, cache_len, self.rope, q=q,

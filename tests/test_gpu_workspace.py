@@ -96,3 +96,29 @@ def test_tree_attention_counts_no_stale_words(cure):
     # which part of a unit comes last may move a value by a rounding to bf16 and float32's own
     _replay_on_all_fillings(call, ws, out, lambda o: ((o.float() - want).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -16).all())
     assert cure.cure_device_error() == 0
+
+
+def test_a_call_holds_its_own_workspace_until_it_is_launched(cure, monkeypatch):
+    """Without a workspace of the caller's, the call's own must not be free for another thread's tensors before the
+    kernel that uses it is queued."""
+    kv = cure.kv_desc(2, D, 64)
+    q = torch.zeros(4, 8, D, dtype=torch.bfloat16, device=DEV)
+    kc, vc = (torch.zeros(1, 64, 2, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    size = cure.cure_prompt_attn_workspace_size(4, 1, 8, kv)
+    lib, held = cure._lib.load(), []
+
+    class Library:
+        def __getattr__(self, name):
+            f = getattr(lib, name)
+            if name not in ("cure_prompt_attn", "cure_selftest_prompt_timeout"):
+                return f
+            return lambda *a: held.append(torch.cuda.memory_allocated()) or f(*a)
+    start, lens = _i32([0, 4]), _i32([0])
+    monkeypatch.setattr(cure._lib, "load", lambda: Library())
+    for call in (lambda: cure.cure_prompt_attn(q, kc, vc, kv, start, lens, SCALE),
+                 lambda: cure.cure_selftest_prompt_timeout(q, kc, vc, kv, start, lens, SCALE, 11, 1000)):
+        before = torch.cuda.memory_allocated()
+        call()
+        assert held.pop() >= before + size
+    torch.cuda.synchronize()
+    assert cure.cure_device_error() == 0
