@@ -24,6 +24,8 @@
  *                                           at their positions, as cure_tree_attn takes them
  *   cure_append_kv    Alg. 1 (input)        the same for prompt rows, K and V into the cache
  *   cure_prompt_attn  Alg. 1 (input)        causal attention of prompt rows over the cache
+ * Each with several positions a token (cure_rope_qkv_axes, cure_append_kv_axes), and over a cache
+ * held in 8 bits (cure_append_kv8, cure_prompt_attn8, cure_tree_attn8, cure_resync_kv8).
  *
  * Conventions shared by every call
  *  - Every pointer argument is a DEVICE pointer unless stated otherwise; the
@@ -471,6 +473,118 @@ cure_status cure_prompt_attn(const void* q, const void* k_cache, const void* v_c
 
 /* Bytes of workspace cure_prompt_attn needs for this shape on the current device (0 on a bad argument). */
 size_t cure_prompt_attn_workspace_size(int32_t rows, int32_t batch, int32_t heads_q, const cure_kv_desc* kv);
+
+/*
+ * Several positions a token (time, height and width of an image's or a video's
+ * patches): pair i of a head turns by the angle p[axis[i]] * f_i.  A HOST struct.
+ */
+typedef struct {
+  int32_t axes;         /* 1 .. 8 */
+  int32_t reserved;     /* 0 */
+  uint8_t axis[64];     /* 0 .. axes - 1: the axis whose position pair i turns by (read for i < rot_dim / 2) */
+} cure_rope_axes;
+
+/*
+ * cure_rope_qkv and cure_append_kv with a position on each of several axes: pos is
+ * device int32 [axes][rows], and a row is left out where any of its positions is
+ * negative.  axes (a HOST pointer) NULL: one axis, exactly as those calls; else pos must
+ * be given (cure_append_kv_axes: the slots are cache_len[b] + i as ever).
+ */
+cure_status cure_rope_qkv_axes(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                               int32_t rows, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const int32_t* pos,
+                               const cure_rope_axes* axes, const cure_rope* rope, const void* q_norm,
+                               const void* k_norm, float eps, void* q_out, void* k_out, void* v_out,
+                               int64_t ld_q_out, int64_t ld_k_out, int64_t ld_v_out, void* stream);
+cure_status cure_append_kv_axes(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                                int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
+                                const int32_t* cache_len, const int32_t* pos, const cure_rope_axes* axes,
+                                const cure_kv_desc* kv, void* k_cache, void* v_cache, const cure_rope* rope,
+                                const void* q_norm, const void* k_norm, float eps, void* q_out, int64_t ld_q_out,
+                                void* stream);
+
+/*
+ * A cache held in 8 bits.  K and V of a layer lie as `kv` says, with e4m3 codes (one
+ * byte: sign, 4 bits of exponent, 3 of mantissa; 448 at most, no infinity) in the place
+ * of bf16 values, and a float scale for each block of CURE_KV8_BLOCK slots and head:
+ *   k_scale, v_scale: [batch][ceil(max_len / 16)][heads_kv] (contiguous),
+ *                     [num_pages][page_size / 16][heads_kv] (paged)
+ *   value = code * scale
+ * Pages hold 16, 32 or 64 tokens (CURE_ERR_UNSUPPORTED otherwise).  The calls that write
+ * choose for a block s = 2^e, the least with |x| <= 448 s for every value x that it
+ * then holds (2^-40 <= s <= 2^40; s = 2^-40 for a block of zeros), and the code nearest
+ * to x / s (ties to even; values beyond 448 s saturate, a NaN stays one, and counts for
+ * nothing in s).  What a block held before, its slots below cache_len[b], is
+ * expressed anew where s changes: exactly, but for values below 2^-6 s, which are
+ * rounded to steps of 2^-9 s.  Slots of the block that hold nothing may change their
+ * meaning with its scale.
+ */
+#define CURE_KV8_BLOCK 16
+
+/*
+ * cure_append_kv (cure_append_kv_axes) into a cache in 8 bits.  Arguments, and which rows
+ * are left out with which error, are theirs; all values are computed in float32 and
+ * rounded once.  A sequence's rows up to the first that is left out for its slot or
+ * page count for its blocks; a row with pos < 0 between others leaves its slot without
+ * meaning.  Caches 16-byte aligned, scales 4-byte.  No two rows of a call may lie in the
+ * same block of the same page, unless they are of one sequence.  row_start must
+ * ascend: where it does not, rows are left out with CURE_DEVERR_NODES, or written
+ * for a sequence whose range holds them.
+ */
+cure_status cure_append_kv8(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                            int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
+                            const int32_t* cache_len, const int32_t* pos, const cure_rope_axes* axes,
+                            const cure_kv_desc* kv, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                            const cure_rope* rope, const void* q_norm, const void* k_norm, float eps, void* q_out,
+                            int64_t ld_q_out, void* stream);
+
+/*
+ * cure_prompt_attn over a cache in 8 bits: the same formula with k = code * scale, and
+ * the same rows, limits, errors and workspace rules.  Any scales from 2^-40 to 2^40
+ * will do, not only powers of two; others (NaN, too) count as the nearer of those two.
+ * Scores: q in two e4m3 parts, which hold it but for 2^-18 of its row's largest value;
+ * products of e4m3 in float32.  A probability times its block's scale is
+ * rounded to fp16, by up to 2^-11 of itself, or 2^-32 of the row's largest such term.
+ */
+cure_status cure_prompt_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                              const float* v_scale, const cure_kv_desc* kv, const int32_t* row_start,
+                              const int32_t* cache_len, int32_t rows, int32_t batch, int32_t heads_q, float scale,
+                              void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace cure_prompt_attn8 needs for this shape on the current device (0 on a bad argument). */
+size_t cure_prompt_attn8_workspace_size(int32_t rows, int32_t batch, int32_t heads_q, const cure_kv_desc* kv);
+
+/*
+ * cure_tree_attn over a cache in 8 bits, in the in-place layout: node j of sequence b
+ * lies in slot cache_len[b] + j (cure_append_kv8 with row_start = 0, n_max, 2 n_max, ..
+ * and the tree's positions).  out[b][j][h] = softmax(scale * q k^T) v over the cached
+ * keys 0 .. L_b - 1 and the nodes a with bit a of anc[b][j] set (0 where that leaves
+ * no key).  Rows j >= n_nodes[b] are left unwritten, and so are the rows of a sequence
+ * with n_nodes[b] outside 1 .. n_max (CURE_DEVERR_NODES) or that does not fit its capacity
+ * (CURE_DEVERR_SLOT); a missing or bad page counts as zeros (CURE_DEVERR_PAGE).  n_max <= 256,
+ * batch <= 256, heads_q / heads_kv <= 128.  Roundings and workspace rules as for cure_prompt_attn8.
+ */
+cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                            const float* v_scale, const cure_kv_desc* kv, const int32_t* cache_len,
+                            const int32_t* n_nodes, const uint64_t* anc, int32_t batch, int32_t n_max,
+                            int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/* Bytes of workspace cure_tree_attn8 needs for this shape on the current device (0 on a bad argument). */
+size_t cure_tree_attn8_workspace_size(int32_t batch, int32_t n_max, int32_t heads_q, const cure_kv_desc* kv);
+
+/*
+ * cure_resync_kv for caches in 8 bits: the path's rows are taken from tree_k/tree_v (bf16
+ * [layers][B][n_max][Hkv][D], not NULL: what the cache holds of the tree has been rounded
+ * with other rows' scales) and written as cure_append_kv8 writes rows behind the
+ * cache_len_in[b] tokens that a sequence holds.  k_scales, v_scales: HOST arrays of `layers`
+ * device pointers, as the caches.  Lengths and replay lists as in cure_resync_kv.
+ */
+cure_status cure_resync_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                            float* const* v_scales, const cure_kv_desc* kv, const void* tree_k, const void* tree_v,
+                            int32_t batch, int32_t n_max, int32_t block, const int32_t* path_nodes,
+                            const int32_t* accept_len, const int32_t* diverge_depth, const int32_t* out_tokens,
+                            const int32_t* cache_len_in, int32_t* cache_len_out, int32_t* draft_valid_len,
+                            int32_t* replay_tokens, int32_t* n_replay, void* stream);
 
 /* Reads and clears the device error word of the current device after
  * synchronising `stream`.  *bits receives the CURE_DEVERR_* bits (may be NULL).

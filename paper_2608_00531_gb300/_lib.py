@@ -23,6 +23,8 @@ EXPORTS = ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_tree_a
            "cure_selftest_lm_head_timeout", "cure_selftest_prompt_timeout", "cure_selftest_attn_route",
            "cure_sample_target", "cure_resync_kv", "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv",
            "cure_append_kv", "cure_prompt_attn", "cure_prompt_attn_workspace_size", "cure_device_error",
+           "cure_rope_qkv_axes", "cure_append_kv_axes", "cure_append_kv8", "cure_prompt_attn8",
+           "cure_prompt_attn8_workspace_size", "cure_tree_attn8", "cure_tree_attn8_workspace_size", "cure_resync_kv8",
            "cure_status_string", "cure_abi_version")
 
 
@@ -48,6 +50,10 @@ class Rope(C.Structure):
 class RopeScaling(C.Structure):
     _fields_ = [("kind", C.c_int32), ("reserved", C.c_int32), ("factor", C.c_double), ("low", C.c_double),
                 ("high", C.c_double), ("original", C.c_double)]
+
+
+class RopeAxes(C.Structure):
+    _fields_ = [("axes", C.c_int32), ("reserved", C.c_int32), ("axis", C.c_uint8 * 64)]
 
 
 class CureError(RuntimeError):
@@ -102,13 +108,32 @@ def load() -> C.CDLL:
     lib.cure_selftest_prompt_timeout.argtypes = [*lib.cure_prompt_attn.argtypes[:-1], I32, I32, P]
     lib.cure_prompt_attn_workspace_size.argtypes = [I32, I32, I32, C.POINTER(KVDesc)]
     lib.cure_prompt_attn_workspace_size.restype = C.c_size_t
+    lib.cure_rope_qkv_axes.argtypes = [P, P, P, I64, I64, I64, I32, I32, I32, I32, P, C.POINTER(RopeAxes),
+                                       C.POINTER(Rope), P, P, C.c_float, P, P, P, I64, I64, I64, P]
+    lib.cure_append_kv_axes.argtypes = [P, P, P, I64, I64, I64, I32, I32, I32, P, P, P, C.POINTER(RopeAxes),
+                                        C.POINTER(KVDesc), P, P, C.POINTER(Rope), P, P, C.c_float, P, I64, P]
+    lib.cure_append_kv8.argtypes = [P, P, P, I64, I64, I64, I32, I32, I32, P, P, P, C.POINTER(RopeAxes),
+                                    C.POINTER(KVDesc), P, P, P, P, C.POINTER(Rope), P, P, C.c_float, P, I64, P]
+    lib.cure_prompt_attn8.argtypes = [P, P, P, P, P, C.POINTER(KVDesc), P, P, I32, I32, I32, C.c_float, P, P, C.c_size_t,
+                                      P]
+    lib.cure_prompt_attn8_workspace_size.argtypes = [I32, I32, I32, C.POINTER(KVDesc)]
+    lib.cure_prompt_attn8_workspace_size.restype = C.c_size_t
+    lib.cure_tree_attn8.argtypes = [P, P, P, P, P, C.POINTER(KVDesc), P, P, P, I32, I32, I32, C.c_float, P, P, C.c_size_t,
+                                    P]
+    lib.cure_tree_attn8_workspace_size.argtypes = [I32, I32, I32, C.POINTER(KVDesc)]
+    lib.cure_tree_attn8_workspace_size.restype = C.c_size_t
+    lib.cure_resync_kv8.argtypes = [I32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
+                                    C.POINTER(C.c_void_p), C.POINTER(KVDesc), P, P, I32, I32, I32, P, P, P, P, P, P, P, P,
+                                    P, P]
     lib.cure_device_error.argtypes = [P, C.POINTER(I32)]
     lib.cure_status_string.argtypes = [C.c_int]
     lib.cure_status_string.restype = C.c_char_p
     lib.cure_abi_version.restype = I32
     for name in ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_accept",
                  "cure_resync_kv", "cure_device_error", "cure_sample_target", "cure_lm_head_argmax",
-                 "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv", "cure_append_kv", "cure_prompt_attn"):
+                 "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv", "cure_append_kv", "cure_prompt_attn",
+                 "cure_rope_qkv_axes", "cure_append_kv_axes", "cure_append_kv8", "cure_prompt_attn8", "cure_tree_attn8",
+                 "cure_resync_kv8"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib

@@ -126,12 +126,25 @@ struct RopeArgs {
   const int32_t *row_start, *cache_len;
   cure_kv_desc kv;
   cure_rope rope;
+  cure_rope_axes axes;  // axes.axes == 0: one position a row
   const uint16_t *q_norm, *k_norm;
   float eps;
   int chunks, chunk_heads;  // set by the launcher: a row's heads in `chunks` parts, a warp each
   int* err;
 };
 cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s);
+
+// The same into a cache in 8 bits (k_out, v_out: its codes).
+cudaError_t launch_append8(const RopeArgs& args, float* k_scale, float* v_scale, cudaStream_t s);
+// The accepted paths' rows of every layer into caches in 8 bits.
+struct LayerScales {
+  float* k[kMaxLayers];
+  float* v[kMaxLayers];
+};
+cudaError_t launch_paths8(int layers, const LayerPtrs& caches, const LayerScales& scales, const cure_kv_desc& kv,
+                          const uint16_t* tree_k, const uint16_t* tree_v, int batch, int n_max, int block,
+                          const int32_t* path_nodes, const int32_t* accept_len, const int32_t* cache_len, int* err,
+                          cudaStream_t s);
 
 // Causal attention of packed prompt rows over the cache.  expire_warp >= 0 (self-test): that
 // warp's expire_wait-th wait in CTA 0 is on a barrier that nothing completes.
@@ -140,6 +153,23 @@ cudaError_t launch_prompt_attn(const uint16_t* q, const uint16_t* k_cache, const
                                const cure_kv_desc& kv, const int32_t* row_start, const int32_t* cache_len, int rows,
                                int batch, int heads_q, float scale, uint16_t* out, void* workspace, int* err,
                                cudaStream_t s, int expire_warp = -1, int expire_wait = 0);
+
+// The same over a cache in 8 bits: causal, or (n_nodes not NULL) a tree's rows in place.
+struct Attn8Call {
+  const uint16_t* q;
+  const uint8_t *k_cache, *v_cache;
+  const float *k_scale, *v_scale;
+  cure_kv_desc kv;
+  const int32_t *row_start, *cache_len, *n_nodes;
+  const uint64_t* anc;
+  int rows, batch, n_max, heads_q;
+  float scale;
+  uint16_t* out;
+  void* workspace;
+  int* err;
+};
+size_t attn8_workspace();
+cudaError_t launch_attn8(const Attn8Call& c, cudaStream_t s);
 
 // Fused LM head + argmax: launch plan for a shape (persistent pairs of CTAs, one
 // tile of nt hidden rows each, the vocabulary's 256-id tiles split into `groups`

@@ -54,6 +54,9 @@ bool kv_ok(const cure_kv_desc* kv, cure_status* why) {
   return true;
 }
 
+// Whether a cache in 8 bits can have this geometry: whole scale blocks in a page.
+bool kv8_ok(const cure_kv_desc* kv) { return kv->layout == 0 || kv->page_size >= CURE_KV8_BLOCK; }
+
 }  // namespace
 
 // ---- context-keyed device addresses of the library's __device__ variables
@@ -436,7 +439,12 @@ cure_status cure_rope_init(cure_rope* out, int32_t style, int32_t rot_dim, doubl
 }
 
 // What cure_rope_qkv and cure_append_kv check alike.
-static cure_status rope_args_ok(const RopeArgs& a, const cure_rope* rope) {
+static cure_status rope_args_ok(const RopeArgs& a, const cure_rope* rope, const cure_rope_axes* axes) {
+  if (axes) {
+    if (axes->axes < 1 || axes->axes > 8) return CURE_ERR_INVALID_ARG;
+    for (int i = 0; rope && i < rope->rot_dim / 2 && i < 64; ++i)
+      if (axes->axis[i] >= axes->axes) return CURE_ERR_INVALID_ARG;
+  }
   if (a.rows < 0 || a.heads_q < 0 || a.heads_kv < 0 || !(a.eps >= 0.f && a.eps <= FLT_MAX)) return CURE_ERR_INVALID_ARG;
   if (a.heads_q > 4096 || a.heads_kv > 4096) return CURE_ERR_UNSUPPORTED;
   if (rope && (rope->style < 0 || rope->style > 1 || rope->rot_dim < 0 || rope->rot_dim > 128 ||
@@ -458,12 +466,11 @@ static cure_status rope_args_ok(const RopeArgs& a, const cure_rope* rope) {
   return CURE_OK;
 }
 
-cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
-                          int32_t rows, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const int32_t* pos,
-                          const cure_rope* rope, const void* q_norm, const void* k_norm, float eps, void* q_out,
-                          void* k_out, void* v_out, int64_t ld_q_out, int64_t ld_k_out, int64_t ld_v_out,
-                          void* stream) {
-  ApiRange range("cure_rope_qkv");
+static cure_status rope_qkv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                            int32_t rows, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const int32_t* pos,
+                            const cure_rope_axes* axes, const cure_rope* rope, const void* q_norm, const void* k_norm,
+                            float eps, void* q_out, void* k_out, void* v_out, int64_t ld_q_out, int64_t ld_k_out,
+                            int64_t ld_v_out, void* stream) {
   RopeArgs a = {};
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
@@ -484,24 +491,48 @@ cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t l
   a.q_norm = static_cast<const uint16_t*>(q_norm);
   a.k_norm = static_cast<const uint16_t*>(k_norm);
   a.eps = eps;
-  const cure_status st = rope_args_ok(a, rope);
+  const cure_status st = rope_args_ok(a, rope, axes);
   if (st != CURE_OK) return st;
   if (head_dim != 128) return head_dim < 1 ? CURE_ERR_INVALID_ARG : CURE_ERR_UNSUPPORTED;
   if (rows == 0 || (heads_q == 0 && heads_kv == 0) || (!q && !k && !v)) return CURE_OK;
   if (!pos || !aligned(pos, 4)) return CURE_ERR_INVALID_ARG;
   if (rope) a.rope = *rope;
+  if (axes) a.axes = *axes;
   a.err = device_error_word();
   return from_cuda(launch_rope(a, false, static_cast<cudaStream_t>(stream)));
 }
 
-cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
-                           int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
-                           const int32_t* cache_len, const int32_t* pos, const cure_kv_desc* kv, void* k_cache,
-                           void* v_cache, const cure_rope* rope, const void* q_norm, const void* k_norm, float eps,
-                           void* q_out, int64_t ld_q_out, void* stream) {
-  ApiRange range("cure_append_kv");
+cure_status cure_rope_qkv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                          int32_t rows, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const int32_t* pos,
+                          const cure_rope* rope, const void* q_norm, const void* k_norm, float eps, void* q_out,
+                          void* k_out, void* v_out, int64_t ld_q_out, int64_t ld_k_out, int64_t ld_v_out,
+                          void* stream) {
+  ApiRange range("cure_rope_qkv");
+  return rope_qkv(q, k, v, ld_q, ld_k, ld_v, rows, heads_q, heads_kv, head_dim, pos, nullptr, rope, q_norm, k_norm, eps, q_out,
+                  k_out, v_out, ld_q_out, ld_k_out, ld_v_out, stream);
+}
+
+cure_status cure_rope_qkv_axes(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                               int32_t rows, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const int32_t* pos,
+                               const cure_rope_axes* axes, const cure_rope* rope, const void* q_norm,
+                               const void* k_norm, float eps, void* q_out, void* k_out, void* v_out,
+                               int64_t ld_q_out, int64_t ld_k_out, int64_t ld_v_out, void* stream) {
+  ApiRange range("cure_rope_qkv_axes");
+  return rope_qkv(q, k, v, ld_q, ld_k, ld_v, rows, heads_q, heads_kv, head_dim, pos, axes, rope, q_norm, k_norm, eps, q_out,
+                  k_out, v_out, ld_q_out, ld_k_out, ld_v_out, stream);
+}
+
+static cure_status append_kv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                             int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
+                             const int32_t* cache_len, const int32_t* pos, const cure_rope_axes* axes,
+                             const cure_kv_desc* kv, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                             const cure_rope* rope, const void* q_norm, const void* k_norm, float eps, void* q_out,
+                             int64_t ld_q_out, void* stream) {
   cure_status why;
   if (!kv_ok(kv, &why)) return why;
+  const bool codes = k_scale || v_scale;  // a cache in 8 bits
+  if (codes && (!k_scale || !v_scale || !aligned(k_scale, 4) || !aligned(v_scale, 4))) return CURE_ERR_INVALID_ARG;
+  if (codes && !kv8_ok(kv)) return CURE_ERR_UNSUPPORTED;
   RopeArgs a = {};
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k);
@@ -530,14 +561,54 @@ cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t 
     a.q = a.k = a.v = nullptr;
     a.q_out = a.k_out = a.v_out = nullptr;
   }
-  const cure_status st = rope_args_ok(a, rope);
+  const cure_status st = rope_args_ok(a, rope, axes);
   if (st != CURE_OK) return st;
   if (rows == 0 || batch == 0) return CURE_OK;
-  if (!k || !v || !row_start || !cache_len || !aligned(row_start, 4) || !aligned(cache_len, 4) || !aligned(pos, 4))
+  if (!k || !v || !row_start || !cache_len || !aligned(row_start, 4) || !aligned(cache_len, 4) || !aligned(pos, 4) ||
+      (axes && !pos))
     return CURE_ERR_INVALID_ARG;
   if (rope) a.rope = *rope;
+  if (axes) a.axes = *axes;
   a.err = device_error_word();
-  return from_cuda(launch_rope(a, true, static_cast<cudaStream_t>(stream)));
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return from_cuda(codes ? launch_append8(a, k_scale, v_scale, s) : launch_rope(a, true, s));
+}
+
+cure_status cure_append_kv(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                           int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
+                           const int32_t* cache_len, const int32_t* pos, const cure_kv_desc* kv, void* k_cache,
+                           void* v_cache, const cure_rope* rope, const void* q_norm, const void* k_norm, float eps,
+                           void* q_out, int64_t ld_q_out, void* stream) {
+  ApiRange range("cure_append_kv");
+  return append_kv(q, k, v, ld_q, ld_k, ld_v, rows, heads_q, batch, row_start, cache_len, pos, nullptr, kv, k_cache, v_cache,
+                   nullptr, nullptr, rope, q_norm, k_norm, eps, q_out, ld_q_out, stream);
+}
+
+cure_status cure_append_kv_axes(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                                int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
+                                const int32_t* cache_len, const int32_t* pos, const cure_rope_axes* axes,
+                                const cure_kv_desc* kv, void* k_cache, void* v_cache, const cure_rope* rope,
+                                const void* q_norm, const void* k_norm, float eps, void* q_out, int64_t ld_q_out,
+                                void* stream) {
+  ApiRange range("cure_append_kv_axes");
+  return append_kv(q, k, v, ld_q, ld_k, ld_v, rows, heads_q, batch, row_start, cache_len, pos, axes, kv, k_cache, v_cache,
+                   nullptr, nullptr, rope, q_norm, k_norm, eps, q_out, ld_q_out, stream);
+}
+
+cure_status cure_append_kv8(const void* q, const void* k, const void* v, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                            int32_t rows, int32_t heads_q, int32_t batch, const int32_t* row_start,
+                            const int32_t* cache_len, const int32_t* pos, const cure_rope_axes* axes,
+                            const cure_kv_desc* kv, void* k_cache, void* v_cache, float* k_scale, float* v_scale,
+                            const cure_rope* rope, const void* q_norm, const void* k_norm, float eps, void* q_out,
+                            int64_t ld_q_out, void* stream) {
+  ApiRange range("cure_append_kv8");
+  cure_status why;
+  if (!kv_ok(kv, &why)) return why;
+  if (!kv8_ok(kv)) return CURE_ERR_UNSUPPORTED;
+  if (rows == 0 || batch == 0) k_scale = v_scale = nullptr;  // nothing to append, whatever the pointers
+  else if (!k_scale || !v_scale) return CURE_ERR_INVALID_ARG;
+  return append_kv(q, k, v, ld_q, ld_k, ld_v, rows, heads_q, batch, row_start, cache_len, pos, axes, kv, k_cache, v_cache,
+                   k_scale, v_scale, rope, q_norm, k_norm, eps, q_out, ld_q_out, stream);
 }
 
 // The units of a call: row groups of two M tiles' rows, for each kv head.
@@ -591,6 +662,134 @@ cure_status cure_selftest_prompt_timeout(const void* q, const void* k_cache, con
   if (warp < 0 || warp > 15 || wait < 1) return CURE_ERR_INVALID_ARG;
   return prompt_attn(q, k_cache, v_cache, kv, row_start, cache_len, rows, batch, heads_q, scale, out, workspace,
                      workspace_bytes, stream, warp, wait);
+}
+
+size_t cure_prompt_attn8_workspace_size(int32_t rows, int32_t batch, int32_t heads_q, const cure_kv_desc* kv) {
+  return prompt_shape_ok(rows, batch, heads_q, kv) == CURE_OK && kv8_ok(kv) ? attn8_workspace() : 0;
+}
+
+static cure_status tree8_shape_ok(int32_t batch, int32_t n_max, int32_t heads_q, const cure_kv_desc* kv) {
+  if (batch < 0 || n_max < 1) return CURE_ERR_INVALID_ARG;
+  if (n_max > kMaxNodes || batch > kAttnBatchLimit) return CURE_ERR_UNSUPPORTED;
+  return prompt_shape_ok(batch * n_max, batch, heads_q, kv);
+}
+
+size_t cure_tree_attn8_workspace_size(int32_t batch, int32_t n_max, int32_t heads_q, const cure_kv_desc* kv) {
+  return tree8_shape_ok(batch, n_max, heads_q, kv) == CURE_OK && kv8_ok(kv) ? attn8_workspace() : 0;
+}
+
+// What the two attention calls over a cache in 8 bits check alike.
+static cure_status attn8(Attn8Call& c, const cure_kv_desc* kv, size_t workspace_bytes, void* stream) {
+  if (!kv8_ok(kv)) return CURE_ERR_UNSUPPORTED;
+  if (!(c.scale > 0.f && c.scale <= FLT_MAX)) return CURE_ERR_INVALID_ARG;
+  if (c.rows == 0 || c.batch == 0) return CURE_OK;
+  if (!c.q || !c.k_cache || !c.v_cache || !c.k_scale || !c.v_scale || !c.cache_len || !c.out || !c.workspace ||
+      !aligned(c.q, 16) || !aligned(c.k_cache, 16) || !aligned(c.v_cache, 16) || !aligned(c.out, 16) ||
+      !aligned(c.workspace, 256) || !aligned(c.k_scale, 4) || !aligned(c.v_scale, 4) || !aligned(c.cache_len, 4))
+    return CURE_ERR_INVALID_ARG;
+  if (workspace_bytes < attn8_workspace()) return CURE_ERR_CAPACITY;
+  c.kv = *kv;
+  c.err = device_error_word();
+  return from_cuda(launch_attn8(c, static_cast<cudaStream_t>(stream)));
+}
+
+cure_status cure_prompt_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                              const float* v_scale, const cure_kv_desc* kv, const int32_t* row_start,
+                              const int32_t* cache_len, int32_t rows, int32_t batch, int32_t heads_q, float scale,
+                              void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  ApiRange range("cure_prompt_attn8");
+  const cure_status st = prompt_shape_ok(rows, batch, heads_q, kv);
+  if (st != CURE_OK) return st;
+  if (rows > 0 && batch > 0 && (!row_start || !aligned(row_start, 4))) return CURE_ERR_INVALID_ARG;
+  Attn8Call c = {};
+  c.q = static_cast<const uint16_t*>(q);
+  c.k_cache = static_cast<const uint8_t*>(k_cache);
+  c.v_cache = static_cast<const uint8_t*>(v_cache);
+  c.k_scale = k_scale;
+  c.v_scale = v_scale;
+  c.row_start = row_start;
+  c.cache_len = cache_len;
+  c.rows = rows;
+  c.batch = batch;
+  c.heads_q = heads_q;
+  c.scale = scale;
+  c.out = static_cast<uint16_t*>(out);
+  c.workspace = workspace;
+  return attn8(c, kv, workspace_bytes, stream);
+}
+
+cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                            const float* v_scale, const cure_kv_desc* kv, const int32_t* cache_len,
+                            const int32_t* n_nodes, const uint64_t* anc, int32_t batch, int32_t n_max,
+                            int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  ApiRange range("cure_tree_attn8");
+  const cure_status st = tree8_shape_ok(batch, n_max, heads_q, kv);
+  if (st != CURE_OK) return st;
+  if (batch > 0 && (!n_nodes || !anc || !aligned(n_nodes, 4) || !aligned(anc, 8))) return CURE_ERR_INVALID_ARG;
+  Attn8Call c = {};
+  c.q = static_cast<const uint16_t*>(q);
+  c.k_cache = static_cast<const uint8_t*>(k_cache);
+  c.v_cache = static_cast<const uint8_t*>(v_cache);
+  c.k_scale = k_scale;
+  c.v_scale = v_scale;
+  c.cache_len = cache_len;
+  c.n_nodes = n_nodes;
+  c.anc = anc;
+  c.rows = batch * n_max;
+  c.batch = batch;
+  c.n_max = n_max;
+  c.heads_q = heads_q;
+  c.scale = scale;
+  c.out = static_cast<uint16_t*>(out);
+  c.workspace = workspace;
+  return attn8(c, kv, workspace_bytes, stream);
+}
+
+cure_status cure_resync_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                            float* const* v_scales, const cure_kv_desc* kv, const void* tree_k, const void* tree_v,
+                            int32_t batch, int32_t n_max, int32_t block, const int32_t* path_nodes,
+                            const int32_t* accept_len, const int32_t* diverge_depth, const int32_t* out_tokens,
+                            const int32_t* cache_len_in, int32_t* cache_len_out, int32_t* draft_valid_len,
+                            int32_t* replay_tokens, int32_t* n_replay, void* stream) {
+  ApiRange range("cure_resync_kv8");
+  cure_status why;
+  if (!kv_ok(kv, &why)) return why;
+  if (!kv8_ok(kv)) return CURE_ERR_UNSUPPORTED;
+  if (layers < 0 || layers > kMaxLayers || batch < 0 || n_max < 1 || block < 1 || block > 32 || n_max < block + 1)
+    return CURE_ERR_INVALID_ARG;
+  if (batch == 0) return CURE_OK;
+  if (!path_nodes || !accept_len || !diverge_depth || !out_tokens || !cache_len_in || !cache_len_out ||
+      !draft_valid_len || !replay_tokens || !n_replay)
+    return CURE_ERR_INVALID_ARG;
+  LayerPtrs lp = {};
+  LayerScales ls = {};
+  if (layers > 0) {
+    if (!k_caches || !v_caches || !k_scales || !v_scales || !tree_k || !tree_v || !aligned(tree_k, 16) ||
+        !aligned(tree_v, 16))
+      return CURE_ERR_INVALID_ARG;
+    for (int l = 0; l < layers; ++l) {
+      if (!k_caches[l] || !v_caches[l] || !aligned(k_caches[l], 16) || !aligned(v_caches[l], 16) || !k_scales[l] ||
+          !v_scales[l] || !aligned(k_scales[l], 4) || !aligned(v_scales[l], 4))
+        return CURE_ERR_INVALID_ARG;
+      lp.k[l] = k_caches[l];
+      lp.v[l] = v_caches[l];
+      ls.k[l] = k_scales[l];
+      ls.v[l] = v_scales[l];
+    }
+  }
+  int* err = device_error_word();
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (layers > 0) {
+    const cudaError_t e = launch_paths8(layers, lp, ls, *kv, static_cast<const uint16_t*>(tree_k),
+                                        static_cast<const uint16_t*>(tree_v), batch, n_max, block, path_nodes,
+                                        accept_len, cache_len_in, err, s);
+    if (e != cudaSuccess) return CURE_ERR_CUDA;
+  }
+  // the lengths and the replay list, behind the rows
+  return from_cuda(launch_resync(0, lp, *kv, nullptr, nullptr, batch, n_max, block, path_nodes, accept_len,
+                                 diverge_depth, out_tokens, cache_len_in, cache_len_out, draft_valid_len,
+                                 replay_tokens, n_replay, err, s));
 }
 
 cure_status cure_device_error(void* stream, int32_t* bits) {

@@ -12,7 +12,9 @@
 // modulo 2^64 is the exact fraction of a turn of that product at any position;
 // what the table's entry is off by (it comes from 64-bit floats: below 2^-53 turns
 // for the plain frequencies) counts p times.  The fraction's upper 32 bits go to a
-// float, which rounds them by up to 2^-26 of a turn, and through sincospif.
+// float, which rounds them by up to 2^-26 of a turn, and through sincospif.  With
+// several axes each pair turns by its own axis's position: a warp's lanes read one
+// position each, and a lane's four pairs take theirs from them.
 //
 // Layout.  Half a warp holds a head, 8 values a lane, and a warp takes a range of
 // one row's heads with the row's cosines and sines (times the norm weights) in
@@ -85,7 +87,8 @@ __device__ __forceinline__ Raw pack(const uint64_t (&a)[2], const uint64_t (&b)[
   return y;
 }
 
-template <bool APPEND, bool INTER>
+// AXES: a position on each of several axes a row, the lane's pairs each by their own.
+template <bool APPEND, bool INTER, bool AXES>
 __global__ void __launch_bounds__(32 * kWarps, 3)
 rope_kernel(const __grid_constant__ RopeArgs A) {
   __shared__ uint64_t turns[64];
@@ -132,8 +135,14 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
     load(in_v, h - v0, h_end - v0, x);
   }
 
-  int p = A.pos ? A.pos[row] : 0;
-  if (p < 0) return;  // a row that holds no token
+  int p = 0;
+  if (AXES) {  // lane a: the position on axis a
+    if (lane < A.axes.axes) p = A.pos[(int64_t)lane * A.rows + row];
+    if (__any_sync(0xffffffffu, p < 0)) return;  // a row that holds no token
+  } else {
+    if (A.pos) p = A.pos[row];
+    if (p < 0) return;
+  }
   int64_t crow = row;  // the row of K's and V's outputs
   if (APPEND) {
     // the row's sequence: as many of the ends row_start[1..B] are at or before it
@@ -182,11 +191,17 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
 
   // cosines and sines of the lane's pairs: a' = a c + b ms, b' = b c + a s
   float c[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+  int at[4] = {p, p, p, p};  // the positions that the lane's pairs turn by
+  if (AXES) {
+    const uint32_t axis = reinterpret_cast<const uint32_t*>(A.axes.axis)[l16];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) at[e] = __shfl_sync(0xffffffffu, p, (axis >> (8 * e)) & 7u);
+  }
   if (rot && h < v0) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       // the fraction of a turn in 2^-32, as a signed number of half turns
-      const int32_t f = (int32_t)(uint32_t)(((uint64_t)(uint32_t)p * turns[4 * l16 + e]) >> 32);
+      const int32_t f = (int32_t)(uint32_t)(((uint64_t)(uint32_t)at[e] * turns[4 * l16 + e]) >> 32);
       sincospif((float)f * 0x1p-31f, &sn[e], &c[e]);
       c[e] *= A.rope.amplitude;
       sn[e] *= A.rope.amplitude;
@@ -309,8 +324,11 @@ cudaError_t launch_rope(const RopeArgs& args, bool append, cudaStream_t s) {
     a.chunk_heads = 4 * kUnroll;
   a.chunks = (heads + a.chunk_heads - 1) / a.chunk_heads;
   const int64_t blocks = ((int64_t)a.rows * a.chunks + kWarps - 1) / kWarps;
-  auto kernel = a.rope.style == 1 ? (append ? rope_kernel<true, true> : rope_kernel<false, true>)
-                                  : (append ? rope_kernel<true, false> : rope_kernel<false, false>);
+  auto kernel = a.rope.style == 1 ? (append ? rope_kernel<true, true, false> : rope_kernel<false, true, false>)
+                                  : (append ? rope_kernel<true, false, false> : rope_kernel<false, false, false>);
+  if (a.axes.axes > 0)
+    kernel = a.rope.style == 1 ? (append ? rope_kernel<true, true, true> : rope_kernel<false, true, true>)
+                               : (append ? rope_kernel<true, false, true> : rope_kernel<false, false, true>);
   return launch_pdl(kernel, dim3((unsigned)blocks), dim3(32 * kWarps), 0, s, a);
 }
 

@@ -13,9 +13,9 @@ from typing import Optional, Sequence
 import torch
 
 from . import _lib
-from ._lib import KVDesc, Rope, RopeScaling, TreeParams, check
+from ._lib import KVDesc, Rope, RopeAxes, RopeScaling, TreeParams, check
 
-_BF16, _I32 = torch.bfloat16, torch.int32
+_BF16, _I32, _F32, _E4M3 = torch.bfloat16, torch.int32, torch.float32, torch.float8_e4m3fn
 
 DEVERR_PAGE, DEVERR_SLOT, DEVERR_NODES = _lib.DEVERR_PAGE, _lib.DEVERR_SLOT, _lib.DEVERR_NODES
 
@@ -344,6 +344,19 @@ def rope_desc(rot_dim: int = 128, base: float = 10000.0, *, style: str = "half",
     return r
 
 
+def rope_axes(axis: Sequence[int]) -> RopeAxes:
+    """The axis whose position each pair of a head turns by, pair 0 first (e.g. [0] * 16 + [1] * 24 + [2] * 24 for
+    time, height and width in a run each): a host struct for the ``axes`` of cure_rope_qkv, cure_append_kv and
+    cure_append_kv8, whose ``pos`` then holds a position on each axis for every row, [axes][rows].  Up to 8 axes; pairs
+    that are not given (of a rotation of fewer dims) turn by axis 0."""
+    a = [int(x) for x in axis]
+    if not a or len(a) > 64:
+        raise ValueError(f"rope_axes: 1 to 64 pairs expected, got {len(a)}")
+    if min(a) < 0 or max(a) > 7:
+        raise ValueError("rope_axes: axes are numbered from 0 to 7")
+    return RopeAxes(axes=max(a) + 1, axis=(C.c_uint8 * 64)(*a))
+
+
 def _here(t: torch.Tensor, name: str, dtype, dev: int) -> int:
     """_p() of a tensor that must also be on device `dev` and of a type."""
     if t.dtype is not dtype:
@@ -408,18 +421,20 @@ _NO_ROWS = (None, 0, 0, 0, 0)
 
 def cure_rope_qkv(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optional[torch.Tensor],
                   pos: torch.Tensor, rope: Optional[Rope], *, q_norm: Optional[torch.Tensor] = None,
-                  k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, out=None, stream=None):
+                  k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, axes: Optional[RopeAxes] = None, out=None,
+                  stream=None):
     """Per-head norms and the rotation of q and k at the rows' positions, v copied: (q, k, v) as cure_tree_attn
     takes them, from (parts of) the rows of a fused projection.
 
     q bf16 [rows][heads_q][D] or [batch][rows][heads_q][D], k and v the same with heads_kv; pos int32, one per row
     (the tree's ``pos``): rows with pos < 0 are left out.  rope = None: no rotation.  Any of q, k, v may be None, and
-    its output with it."""
+    its output with it.  With ``axes`` (rope_axes) pos holds a position on each axis, [axes][rows], and a row is left
+    out where any of them is negative."""
     dev, s = _current(stream)
     if out is None:
         out = tuple(None if t is None else _new(t.shape, t.dtype, stream) for t in (q, k, v))
     qo, ko, vo = out
-    rows = pos.numel()
+    rows = pos.numel() if axes is None else _rows_of_axes(pos, axes)
     pq, lq, nq, hq, dq = _NO_ROWS if q is None else _head_rows(q, "q", dev)
     pk, lk, nk, hk, dk = _NO_ROWS if k is None else _head_rows(k, "k", dev)
     pv, lv, nv, hv, dv = _NO_ROWS if v is None else _head_rows(v, "v", dev)
@@ -433,11 +448,21 @@ def cure_rope_qkv(q: Optional[torch.Tensor], k: Optional[torch.Tensor], v: Optio
             v is not None and (nv != rows or dv != D or (k is not None and hv != hk))):
         raise ValueError("cure_rope_qkv: q, k, v and pos must have the same rows, k and v the same heads, and all one "
                          "head_dim")
-    check("cure_rope_qkv", _lib.load().cure_rope_qkv(
-        pq, pk, pv, lq, lk, lv, rows, hq, hk or hv, D, _here(pos, "pos", _I32, dev),
-        None if rope is None else C.byref(rope), None if q_norm is None else _norm(q_norm, "q_norm", dev),
-        None if k_norm is None else _norm(k_norm, "k_norm", dev), eps, oq, ok, ov, loq, lok, lov, s))
+    args = (None if rope is None else C.byref(rope), None if q_norm is None else _norm(q_norm, "q_norm", dev),
+            None if k_norm is None else _norm(k_norm, "k_norm", dev), eps, oq, ok, ov, loq, lok, lov, s)
+    p = _here(pos, "pos", _I32, dev)
+    if axes is None:
+        check("cure_rope_qkv", _lib.load().cure_rope_qkv(pq, pk, pv, lq, lk, lv, rows, hq, hk or hv, D, p, *args))
+    else:
+        check("cure_rope_qkv_axes", _lib.load().cure_rope_qkv_axes(pq, pk, pv, lq, lk, lv, rows, hq, hk or hv, D, p,
+                                                                   C.byref(axes), *args))
     return out
+
+
+def _rows_of_axes(pos: torch.Tensor, axes: RopeAxes) -> int:
+    if pos.dim() < 2 or pos.shape[0] != axes.axes:
+        raise ValueError(f"pos must hold a row of positions for each of {axes.axes} axes")
+    return pos.numel() // axes.axes
 
 
 def _norm(w: torch.Tensor, name: str, dev: int) -> int:
@@ -446,12 +471,12 @@ def _norm(w: torch.Tensor, name: str, dev: int) -> int:
     return _here(w, name, _BF16, dev)
 
 
-def _caches(k: torch.Tensor, v: torch.Tensor, kv: KVDesc, batch: int, dev: int) -> tuple[int, int]:
+def _caches(k: torch.Tensor, v: torch.Tensor, kv: KVDesc, batch: int, dev: int, dtype=_BF16) -> tuple[int, int]:
     """Addresses of a layer's caches, which must hold what their geometry says."""
     size = (batch * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size) * kv.heads_kv * kv.head_dim
     if k.numel() < size or v.numel() < size:
         raise ValueError("a cache is smaller than its geometry")
-    return _here(k, "k_cache", _BF16, dev), _here(v, "v_cache", _BF16, dev)
+    return _here(k, "k_cache", dtype, dev), _here(v, "v_cache", dtype, dev)
 
 
 def _ragged(row_start: torch.Tensor, cache_len: torch.Tensor, kv: KVDesc) -> int:
@@ -465,16 +490,9 @@ def _ragged(row_start: torch.Tensor, cache_len: torch.Tensor, kv: KVDesc) -> int
     return B
 
 
-def cure_append_kv(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv: KVDesc,
-                   row_start: torch.Tensor, cache_len: torch.Tensor, rope: Optional[Rope], *,
-                   q: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
-                   q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
-                   out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
-    """cure_rope_qkv of packed rows whose K and V go into the cache, sequence b's rows row_start[b] ..
-    row_start[b+1] - 1 to slots cache_len[b], cache_len[b] + 1, ..; returns q's rows (None without q).
-
-    A row's position is its slot, or its entry of ``pos`` (int32; < 0 leaves the row out).  cache_len is not
-    advanced.  In-place tree rows: row_start = 0, n_max, 2 n_max, .., pos = the tree's ``pos``."""
+def _append_args(k, v, k_cache, v_cache, kv: KVDesc, row_start, cache_len, rope, q, pos, axes, q_norm, k_norm, eps, out,
+                 stream, dtype):
+    """The arguments of an append, checked: q's output, those before the caches, the caches, those behind."""
     dev, s = _current(stream)
     B = _ragged(row_start, cache_len, kv)
     Hkv, D = kv.heads_kv, kv.head_dim
@@ -491,14 +509,75 @@ def cure_append_kv(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_ca
         po, lo, no, ho, do = _head_rows(out, "out", dev)
         if nq != rows or no != rows or ho != hq or dq != D or do != D:
             raise ValueError("cure_append_kv: q, its output and k must have the same rows and head_dim")
-    if pos is not None and pos.numel() != rows:
+    if axes is not None:
+        if pos is None:
+            raise ValueError("cure_append_kv: axes need positions")
+        if _rows_of_axes(pos, axes) != rows:
+            raise ValueError("cure_append_kv: pos must have an entry for every row")
+    elif pos is not None and pos.numel() != rows:
         raise ValueError("cure_append_kv: pos must have an entry for every row")
-    kc, vc = _caches(k_cache, v_cache, kv, B, dev)
-    check("cure_append_kv", _lib.load().cure_append_kv(
-        pq, pk, pv, lq, lk, lv, rows, hq, B, _here(row_start, "row_start", _I32, dev),
-        _here(cache_len, "cache_len", _I32, dev), None if pos is None else _here(pos, "pos", _I32, dev), C.byref(kv),
-        kc, vc, None if rope is None else C.byref(rope), None if q_norm is None else _norm(q_norm, "q_norm", dev),
-        None if k_norm is None else _norm(k_norm, "k_norm", dev), eps, po, lo, s))
+    kc, vc = _caches(k_cache, v_cache, kv, B, dev, dtype)
+    front = (pq, pk, pv, lq, lk, lv, rows, hq, B, _here(row_start, "row_start", _I32, dev),
+             _here(cache_len, "cache_len", _I32, dev), None if pos is None else _here(pos, "pos", _I32, dev))
+    back = (None if rope is None else C.byref(rope), None if q_norm is None else _norm(q_norm, "q_norm", dev),
+            None if k_norm is None else _norm(k_norm, "k_norm", dev), eps, po, lo, s)
+    return out, front, (kc, vc), back, B, dev
+
+
+def cure_append_kv(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, kv: KVDesc,
+                   row_start: torch.Tensor, cache_len: torch.Tensor, rope: Optional[Rope], *,
+                   q: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                   axes: Optional[RopeAxes] = None, q_norm: Optional[torch.Tensor] = None,
+                   k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6, out: Optional[torch.Tensor] = None,
+                   stream=None) -> Optional[torch.Tensor]:
+    """cure_rope_qkv of packed rows whose K and V go into the cache, sequence b's rows row_start[b] ..
+    row_start[b+1] - 1 to slots cache_len[b], cache_len[b] + 1, ..; returns q's rows (None without q).
+
+    A row's position is its slot, or its entry of ``pos`` (int32; < 0 leaves the row out), or with ``axes`` its
+    entries of pos [axes][rows].  cache_len is not advanced.  In-place tree rows: row_start = 0, n_max, 2 n_max, ..,
+    pos = the tree's ``pos``."""
+    out, front, caches, back, _, _ = _append_args(k, v, k_cache, v_cache, kv, row_start, cache_len, rope, q, pos, axes,
+                                                  q_norm, k_norm, eps, out, stream, _BF16)
+    if axes is None:
+        check("cure_append_kv", _lib.load().cure_append_kv(*front, C.byref(kv), *caches, *back))
+    else:
+        check("cure_append_kv_axes", _lib.load().cure_append_kv_axes(*front, C.byref(axes), C.byref(kv), *caches, *back))
+    return out
+
+
+KV8_BLOCK = 16  # slots of a scale of a cache in 8 bits
+
+
+def kv8_scale_shape(kv: KVDesc, batch: int) -> tuple[int, int, int]:
+    """The shape of the scales of a layer's K (or V) cache in 8 bits: a float32 for each block of 16 slots and head."""
+    if kv.layout == 0:
+        return batch, -(-kv.max_len // KV8_BLOCK), kv.heads_kv
+    return kv.num_pages, kv.page_size // KV8_BLOCK, kv.heads_kv
+
+
+def _scales(k: torch.Tensor, v: torch.Tensor, kv: KVDesc, batch: int, dev: int) -> tuple[int, int]:
+    a, b, c = kv8_scale_shape(kv, batch)
+    if k.numel() < a * b * c or v.numel() < a * b * c:
+        raise ValueError("scales are fewer than the cache's blocks and heads")
+    return _here(k, "k_scale", _F32, dev), _here(v, "v_scale", _F32, dev)
+
+
+def cure_append_kv8(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                    k_scale: torch.Tensor, v_scale: torch.Tensor, kv: KVDesc, row_start: torch.Tensor,
+                    cache_len: torch.Tensor, rope: Optional[Rope], *, q: Optional[torch.Tensor] = None,
+                    pos: Optional[torch.Tensor] = None, axes: Optional[RopeAxes] = None,
+                    q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """cure_append_kv into a cache held in 8 bits: k_cache, v_cache float8_e4m3fn codes in the geometry ``kv``,
+    k_scale, v_scale float32 (kv8_scale_shape), value = code * scale.
+
+    The scale of a block that gains rows becomes the least power of two for which all that the block then holds lies
+    within 448 of it.  Pages of 16, 32 or 64 tokens."""
+    out, front, caches, back, B, dev = _append_args(k, v, k_cache, v_cache, kv, row_start, cache_len, rope, q, pos, axes,
+                                                    q_norm, k_norm, eps, out, stream, _E4M3)
+    check("cure_append_kv8", _lib.load().cure_append_kv8(
+        *front, None if axes is None else C.byref(axes), C.byref(kv), *caches, *_scales(k_scale, v_scale, kv, B, dev),
+        *back))
     return out
 
 
@@ -539,6 +618,121 @@ def cure_prompt_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     out, held, args = _prompt_attn_args(q, k_cache, v_cache, kv, row_start, cache_len, scale, out, workspace, stream)
     check("cure_prompt_attn", _lib.load().cure_prompt_attn(*args))
     return out
+
+
+def cure_prompt_attn8_workspace_size(rows: int, batch: int, heads_q: int, kv: KVDesc) -> int:
+    return int(_lib.load().cure_prompt_attn8_workspace_size(rows, batch, heads_q, C.byref(kv)))
+
+
+def _prompt_attn8_args(q, k_cache, v_cache, k_scale, v_scale, kv: KVDesc, row_start, cache_len, scale, out, workspace,
+                       stream):
+    """As _prompt_attn_args, of cure_prompt_attn8."""
+    dev, s = _current(stream)
+    B = _ragged(row_start, cache_len, kv)
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != kv.head_dim:
+        raise ValueError("q must be [rows][heads_q][head_dim]")
+    if out is None:
+        out = _new(shape, torch.bfloat16, stream)
+    elif out.shape != shape:
+        raise ValueError("out must have q's shape")
+    if workspace is None:
+        size = cure_prompt_attn8_workspace_size(shape[0], B, shape[1], kv)
+        workspace = _new((max(size, 256),), torch.uint8, stream)
+    kc, vc = _caches(k_cache, v_cache, kv, B, dev, _E4M3)
+    ks, vs = _scales(k_scale, v_scale, kv, B, dev)
+    return out, workspace, (
+        _here(q, "q", _BF16, dev), kc, vc, ks, vs, C.byref(kv), _here(row_start, "row_start", _I32, dev),
+        _here(cache_len, "cache_len", _I32, dev), shape[0], B, shape[1], scale, _here(out, "out", _BF16, dev),
+        _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s)
+
+
+def cure_prompt_attn8(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor,
+                      v_scale: torch.Tensor, kv: KVDesc, row_start: torch.Tensor, cache_len: torch.Tensor, scale: float,
+                      *, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      stream=None) -> torch.Tensor:
+    """cure_prompt_attn over a cache held in 8 bits (cure_append_kv8): float8_e4m3fn codes and a float32 scale for
+    each block of 16 slots and head."""
+    out, held, args = _prompt_attn8_args(q, k_cache, v_cache, k_scale, v_scale, kv, row_start, cache_len, scale, out,
+                                         workspace, stream)
+    check("cure_prompt_attn8", _lib.load().cure_prompt_attn8(*args))
+    return out
+
+
+def cure_tree_attn8_workspace_size(batch: int, n_max: int, heads_q: int, kv: KVDesc) -> int:
+    return int(_lib.load().cure_tree_attn8_workspace_size(batch, n_max, heads_q, C.byref(kv)))
+
+
+def cure_tree_attn8(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor,
+                    v_scale: torch.Tensor, kv: KVDesc, cache_len: torch.Tensor, n_nodes: torch.Tensor,
+                    anc: torch.Tensor, scale: float, *, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """cure_tree_attn over a cache held in 8 bits, in the in-place layout: q bf16 [B][n_max][heads_q][D], node j's K/V
+    rows at slot cache_len[b] + j (cure_append_kv8 with row_start = 0, n_max, 2 n_max, .. and the tree's ``pos``)."""
+    dev, s = _current(stream)
+    shape = q.shape
+    if len(shape) != 4 or shape[3] != kv.head_dim:
+        raise ValueError("q must be [batch][n_max][heads_q][head_dim]")
+    B, n_max, Hq, _ = shape
+    if cache_len.numel() != B or n_nodes.numel() != B or anc.numel() != B * n_max * ((n_max + 63) // 64):
+        raise ValueError("cache_len and n_nodes must hold an entry for every sequence, anc the words of every node")
+    table = getattr(kv, "_keep", None)
+    if table is not None and table.numel() < B * kv.max_len:
+        raise ValueError("block_table has fewer rows than the batch has sequences")
+    if out is None:
+        out = _new(shape, torch.bfloat16, stream)
+    elif out.shape != shape:
+        raise ValueError("out must have q's shape")
+    if workspace is None:
+        workspace = _new((max(cure_tree_attn8_workspace_size(B, n_max, Hq, kv), 256),), torch.uint8, stream)
+    kc, vc = _caches(k_cache, v_cache, kv, B, dev, _E4M3)
+    ks, vs = _scales(k_scale, v_scale, kv, B, dev)
+    check("cure_tree_attn8", _lib.load().cure_tree_attn8(
+        _here(q, "q", _BF16, dev), kc, vc, ks, vs, C.byref(kv), _here(cache_len, "cache_len", _I32, dev),
+        _here(n_nodes, "n_nodes", _I32, dev), _here(anc, "anc", torch.int64, dev), B, n_max, Hq, scale,
+        _here(out, "out", _BF16, dev), _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s))
+    return out
+
+
+def cure_resync_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor],
+                    k_scales: Sequence[torch.Tensor], v_scales: Sequence[torch.Tensor], kv: KVDesc,
+                    tree_k: torch.Tensor, tree_v: torch.Tensor, acc: dict, cache_len_in: torch.Tensor, block: int, *,
+                    cache_len_out: Optional[torch.Tensor] = None, out=None, stream=None) -> dict:
+    """cure_resync_kv for caches held in 8 bits: the accepted path's rows of tree_k/tree_v (bf16
+    [layers][B][n_max][Hkv][D]) into every layer's cache, and the step's new lengths and replay lists."""
+    dev, s = _current(stream)
+    layers, B, n_max, Hkv, D = tree_k.shape
+    if tree_v.shape != tree_k.shape or Hkv != kv.heads_kv or D != kv.head_dim:
+        raise ValueError("cure_resync_kv8: tree_k and tree_v must have the same shape, the cache's heads and its head_dim")
+    if not len(k_caches) == len(v_caches) == len(k_scales) == len(v_scales) == layers:
+        raise ValueError("cure_resync_kv8: one cache, its scales and one slice of the tree per layer")
+    P = block + 2
+    i32 = lambda t, name, n: _sized(t, name, n, dev)  # noqa: E731
+    if cache_len_out is None:
+        cache_len_out = _new((B,), _I32, stream)
+    if out is None:
+        out = dict(draft_valid_len=_new((B,), _I32, stream), replay_tokens=_new((B, P), _I32, stream),
+                   n_replay=_new((B,), _I32, stream))
+    caches = [_caches(k, v, kv, B, dev, _E4M3) for k, v in zip(k_caches, v_caches)]
+    scales = [_scales(k, v, kv, B, dev) for k, v in zip(k_scales, v_scales)]
+    array = C.c_void_p * max(1, layers)
+    kp, vp, ksp, vsp = (array(*[x[i] for x in t]) for t in (caches, scales) for i in (0, 1))
+    check("cure_resync_kv8", _lib.load().cure_resync_kv8(
+        layers, kp, vp, ksp, vsp, C.byref(kv), _here(tree_k, "tree_k", _BF16, dev), _here(tree_v, "tree_v", _BF16, dev), B,
+        n_max, block, i32(acc["path_nodes"], "path_nodes", B * P), i32(acc["accept_len"], "accept_len", B),
+        i32(acc["diverge_depth"], "diverge_depth", B), i32(acc["out_tokens"], "out_tokens", B * P),
+        i32(cache_len_in, "cache_len_in", B), i32(cache_len_out, "cache_len_out", B),
+        i32(out["draft_valid_len"], "draft_valid_len", B), i32(out["replay_tokens"], "replay_tokens", B * P),
+        i32(out["n_replay"], "n_replay", B), s))
+    out["cache_len"] = cache_len_out
+    return out
+
+
+def _sized(t: torch.Tensor, name: str, n: int, dev: int) -> int:
+    """_here() of an int32 tensor that must hold n entries."""
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold {n} entries")
+    return _here(t, name, _I32, dev)
 
 
 def cure_device_error(stream=None) -> int:

@@ -15,6 +15,9 @@ step then norms and rotates them itself (``rope``).
 ``PromptPass`` fills the caches that a step starts from: the attention layers
 of the target over packed prompts, chunks of prompts or single tokens.
 
+Both also take caches held in 8 bits: float8_e4m3fn codes, and their scales
+(``cure.kv8_scale_shape``) beside them.
+
 ``run_from_host`` takes the same inputs in (pinned) host memory and streams
 them in on a copy stream in the order the stages consume them (draft logits,
 then each layer's Q/K/V, then the target logits of the tree's nodes); each
@@ -85,8 +88,13 @@ class PromptPass:
         return ws
 
     def layer(self, l: int, qkv: torch.Tensor, row_start: torch.Tensor, cache_len: torch.Tensor, k_cache: torch.Tensor,
-              v_cache: torch.Tensor, *, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        """Layer l: qkv bf16 [rows][(Hq + 2 Hkv) D] -> attention output [rows][Hq][D]; the cache gains the rows."""
+              v_cache: torch.Tensor, *, scales=None, pos: Optional[torch.Tensor] = None,
+              axes: Optional[cure.RopeAxes] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Layer l: qkv bf16 [rows][(Hq + 2 Hkv) D] -> attention output [rows][Hq][D]; the cache gains the rows.
+
+        scales: (k_scale, v_scale) of a cache held in 8 bits.  pos, axes: the rows' positions, where they are not their
+        places in their sequences (cure_append_kv); rows see the keys up to their own place whatever their positions,
+        so none may be negative."""
         n = qkv.shape[0]
         if n > self.rows:
             raise ValueError(f"PromptPass was made for {self.rows} rows, got {n}")
@@ -95,14 +103,19 @@ class PromptPass:
         if cache_len.numel() > self.B:
             self._workspace_size(n, cache_len.numel())
         rows = self.q[:n]
-        out, _, args = cure._prompt_attn_args(rows, k_cache, v_cache, self.kv, row_start, cache_len, self.scale, out,
-                                              self.workspace, stream)
+        caches = (k_cache, v_cache) if scales is None else (k_cache, v_cache, *scales)
+        of = cure._prompt_attn_args if scales is None else cure._prompt_attn8_args
+        out, _, args = of(rows, *caches, self.kv, row_start, cache_len, self.scale, out, self.workspace, stream)
         if out.data_ptr() % 16:
             raise ValueError("out must be 16-byte aligned")
-        cure.cure_append_kv(k, v, k_cache, v_cache, self.kv, row_start, cache_len, self.rope, q=q,
-                            q_norm=_of_layer(self.q_norm, l), k_norm=_of_layer(self.k_norm, l), eps=self.eps,
-                            out=rows, stream=stream)
-        cure.check("cure_prompt_attn", cure._lib.load().cure_prompt_attn(*args))
+        append = cure.cure_append_kv if scales is None else cure.cure_append_kv8
+        append(k, v, *caches, self.kv, row_start, cache_len, self.rope, q=q, pos=pos, axes=axes,
+               q_norm=_of_layer(self.q_norm, l), k_norm=_of_layer(self.k_norm, l), eps=self.eps, out=rows,
+               stream=stream)
+        if scales is None:
+            cure.check("cure_prompt_attn", cure._lib.load().cure_prompt_attn(*args))
+        else:
+            cure.check("cure_prompt_attn8", cure._lib.load().cure_prompt_attn8(*args))
         return out
 
     @staticmethod
@@ -155,13 +168,16 @@ class RepairVerifyStep:
         # for inputs that come as projections: the rotation, norm weights per layer, and the rows made of them
         self.rope, self.q_norm, self.k_norm, self.eps = rope, q_norm, k_norm, eps
         self._rows = None
+        self._starts = self._workspace8 = None  # for caches in 8 bits: the trees' rows in a packed batch, the workspace
         self._dev_inputs = None
         self._copy_stream = None
         self._n_host = None
         self.last_h2d_bytes = 0  # host-to-device bytes of the last run_from_host
 
     def run(self, x: StepInputs, k_caches: List[torch.Tensor], v_caches: List[torch.Tensor],
-            stream=None) -> dict:
+            stream=None, scales=None) -> dict:
+        """One step.  scales: (k_scales, v_scales), a tensor for each cache, where the caches are held in 8 bits; the
+        tree's rows then go into the caches, behind the sequences' tokens, and are attended to there."""
         ids, vals, margin, logp1 = cure.cure_score_draft(x.draft_logits, self.k, out=self.score,
                                                          stream=stream)
         tree = cure.cure_build_tree(ids, margin, x.root_tok, x.cache_len, self.tau, self.R,
@@ -171,7 +187,10 @@ class RepairVerifyStep:
         vl = [v_caches[self.layer_map[l]] for l in range(self.layers)]
         if x.qkv is not None:
             x = self._rotate(x, tree["pos"], stream)
-        if all(isinstance(t, torch.Tensor) and t.is_contiguous() and t.dim() == 5 and t.shape[0] == self.layers
+        if scales is not None:
+            sl = [[t[self.layer_map[l]] for l in range(self.layers)] for t in scales]
+            self._attend8(x, kl, vl, *sl, tree, stream)
+        elif all(isinstance(t, torch.Tensor) and t.is_contiguous() and t.dim() == 5 and t.shape[0] == self.layers
                for t in (x.q, x.tree_k, x.tree_v)):
             cure.cure_tree_attn_layers(x.q, x.tree_k, x.tree_v, kl, vl, self.kv, x.cache_len, tree["n_nodes"],
                                        tree["anc"], self.scale, self.attn_out, self.workspace, stream=stream)
@@ -182,9 +201,30 @@ class RepairVerifyStep:
                                     workspace=self.workspace, stream=stream)
         acc = cure.cure_accept(tree, self.K, target_logits=x.target_logits, targ=self.targ,
                                out=self.acc, stream=stream)
-        rs = cure.cure_resync_kv(kl, vl, self.kv, x.tree_k, x.tree_v, acc, x.cache_len, self.K,
-                                 cache_len_out=self.cache_len_out, out=self.rs, stream=stream)
+        if scales is not None:
+            rs = cure.cure_resync_kv8(kl, vl, *sl, self.kv, x.tree_k, x.tree_v, acc, x.cache_len, self.K,
+                                      cache_len_out=self.cache_len_out, out=self.rs, stream=stream)
+        else:
+            rs = cure.cure_resync_kv(kl, vl, self.kv, x.tree_k, x.tree_v, acc, x.cache_len, self.K,
+                                     cache_len_out=self.cache_len_out, out=self.rs, stream=stream)
         return dict(score=self.score, tree=tree, attn=self.attn_out, acc=acc, resync=rs)
+
+    def _attend8(self, x: StepInputs, kl, vl, ksl, vsl, tree: dict, stream) -> None:
+        """The layers' tree attention over caches in 8 bits, each layer's tree rows appended in place before it."""
+        if self._starts is None:
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("a step over caches in 8 bits must have run once before it is captured")
+                dev = self.attn_out.device
+                self._starts = torch.arange(0, (self.B + 1) * self.n_max, self.n_max, dtype=torch.int32, device=dev)
+                size = cure.cure_tree_attn8_workspace_size(self.B, self.n_max, self.Hq, self.kv)
+                self._workspace8 = torch.empty(max(size, 256), dtype=torch.uint8, device=dev)
+        for l in range(self.layers):
+            caches = (kl[l], vl[l], ksl[l], vsl[l])
+            cure.cure_append_kv8(x.tree_k[l], x.tree_v[l], *caches, self.kv, self._starts, x.cache_len, None,
+                                 pos=tree["pos"], stream=stream)
+            cure.cure_tree_attn8(x.q[l], *caches, self.kv, x.cache_len, tree["n_nodes"], tree["anc"], self.scale,
+                                 out=self.attn_out[l], workspace=self._workspace8, stream=stream)
 
     def _rotate(self, x: StepInputs, pos: torch.Tensor, stream) -> StepInputs:
         """The step's Q/K/V from the layers' projections at the tree's positions (rows past a sequence's nodes
@@ -298,5 +338,6 @@ class RepairVerifyStep:
         """Library kernels one step launches: scan, tree, one attention kernel per
         layer, target argmax + walk, and the resync gather (its finalize runs in
         the gather's grid, since the step's new lengths do not alias the old).
-        Inputs that come as projections take one more per layer."""
+        Inputs that come as projections take one more per layer; caches in 8 bits one more per
+        layer, and one more in all."""
         return 1 + 1 + self.layers + 2 + 1
