@@ -1,131 +1,844 @@
 // Attention of packed rows over a cache held in 8 bits (e4m3 codes, a scale for each block
-// of 16 slots and head): causal (cure_prompt_attn8), or a repair tree's rows in place
-// (cure_tree_attn8).
+// of 16 slots and head), on tcgen05 tensor cores: causal (cure_prompt_attn8), or a repair
+// tree's rows in place (cure_tree_attn8).
 //
-//   out_i = sum_j softmax_j(scale q_i k_j) v_j,   k_j = ks_j K_j,  v_j = vs_j V_j
+//   out_i = sum_j softmax_j(c q_i k_j) v_j,   k_j = ks_j K_j,  v_j = vs_j V_j
 //
-// A CTA takes a row's query head, its four warps every fourth key, a lane four dims;
-// one pass with the running maximum and sum.
-#include "attn_tc.cuh"
-#include "common.cuh"
+// with codes K, V and their blocks' scales ks, vs.
+//
+// Scores.  K goes from memory to the tensor cores as it is.  q (8 significant bits) is two
+// e4m3 values (4 bits each): with its row scaled by a power of two to at most 448,
+//   q = q1 + q2,  q1 = e4m3(q),  q2 = e4m3(q - q1)
+// is exact down to 2^-9 of steps, 2^-18 of the row's largest value.  S = q1 K + q2 K are 8
+// products of 32 dims where bf16 has 8 of 16, at twice the rate.
+//
+// Weights.  V's codes are widened to fp16 (exact), and P is fp16 with the block's scale in it:
+//   P'_j = 2^(s_j + log2 vs_j - M + 7),  M the running maximum of s_j + log2 vs_j
+// so that a rounding is relative to what a term adds to the output, whatever the scales, and
+// the smallest steps (2^-24 of fp16) are 2^-31 of the largest term.  The sum of weights is
+// kept in float32 as sum_blocks (sum P') / vs.
+//
+// Units, pieces and the scheduler are those of the bf16 kernel (prompt_units.cuh).  Roles (16
+// warps):
+//   warps 0-3 / 4-7   softmax of M tile 0 / 1, a thread a row
+//   warp 8            TMA producer: K and V tiles (16 KiB each), and their blocks' scales
+//   warp 9            issues S = Q K^T (M128 N128, K 2 x 128) of M tiles 0 and 1 in turn
+//   warp 10           issues O += P' V (A = P' from TMEM)
+//   warp 11           lays out the CTA's pieces of work
+//   warps 12-15       Q into its parts, V tiles to fp16, and the epilogue: a piece's rows go
+//                     out once the next one's Q and first V tile are on their way
+// TMEM as there: S (128) | P[2] (64 each) | O[2] (128 each).  A piece whose rows fit one M
+// tile (single tokens, small trees) takes its tiles in turn with both softmax groups, each
+// with an O and sums of its own, which the epilogue adds up: a group's exponentials would
+// otherwise take longer than a tile's bytes.
+#include "prompt_units.cuh"
 
 namespace cure {
 namespace {
 
-using namespace tc;
+using namespace prompt;
 
-constexpr int kD = 128;
+constexpr int NK = 3, NV = 2, NW = 2;   // stages: K tiles, V tiles, V tiles in fp16
 constexpr int kBlk = CURE_KV8_BLOCK;
+constexpr int kBlocks = BN / kBlk;      // of a tile
+constexpr int kTile = BN * D;           // 16 KiB of codes
+constexpr int kTileW = kTile * 2;
+constexpr int kScaleSlots = 8;          // tiles whose scales lie in shared memory
+constexpr int kOffQ = 0;                       // Q[m][part]
+constexpr int kOffK = kOffQ + 4 * kQHalf;      // K[stage]
+constexpr int kOffV = kOffK + NK * kTile;      // V[stage]
+constexpr int kOffW = kOffV + NV * kTile;      // V in fp16[stage]: chunks of 16 keys, [d half][16 keys][64 d]
+constexpr int kOffMisc = kOffW + NW * kTileW;
+enum {
+  B_QFULL = 0, B_QEMPTY, B_SFREE, B_KFULL, B_KEMPTY = B_KFULL + NK, B_VFULL = B_KEMPTY + NK, B_VEMPTY = B_VFULL + NV,
+  B_WFULL = B_VEMPTY + NV, B_WEMPTY = B_WFULL + NW, B_SFULL = B_WEMPTY + NW, B_PFULL = B_SFULL + 2,
+  B_PVDONE = B_PFULL + 2, B_STAT = B_PVDONE + 2, B_OFREE = B_STAT + 2, B_DRAIN = B_OFREE + 2, B_JOIN = B_DRAIN + 2,
+  B_PIECE = B_JOIN + 1, B_TAKEN = B_PIECE + kPieces, kNumBars = B_TAKEN + kPieces
+};
+constexpr int kOffTmemSlot = kOffMisc + 8 * kNumBars;
+constexpr int kOffAbort = kOffTmemSlot + 4;
+constexpr int kOffJoins = kOffAbort + 4;                        // units that this CTA joins at its end
+constexpr int kOffPieces = (kOffJoins + 4 + 15) / 16 * 16;      // int [kPieces][kPieceInts], then [2] to join
+constexpr int kOffPrefix = kOffPieces + (kPieces + 2) * kPieceInts * 4;  // int64 first position of each sequence [B+1]
+constexpr int kOffScales = (kOffPrefix + 8 * (kAttnMaxBatch + 1) + 15) / 16 * 16;  // float [slot][ks, log2 vs, 1 / vs][8]
+constexpr int kOffQScale = kOffScales + kScaleSlots * 3 * kBlocks * 4;  // float [piece % 2][m][row]
+constexpr int kOffInv = kOffQScale + 4 * BM * 4;                // float [group][row]: reciprocal row sums
+constexpr int kOffLse = kOffInv + 2 * BM * 4;                   // float [group][row]: base-2 log-sum-exps
+constexpr int kOffKept = kOffLse + 2 * BM * 4;                  // the epilogue's piece, a copy for each of its warps
+constexpr int kSmemBytes = kOffKept + 4 * kPieceInts * 4;
+static_assert(kSmemBytes <= 232448, "fits the 227 KiB opt-in");
+struct Lay {  // where the pieces lie, for what prompt_units.cuh shares
+  static constexpr int pieces = kOffPieces, prefix = kOffPrefix, piece_bar = B_PIECE, taken_bar = B_TAKEN;
+};
 
-__device__ __forceinline__ float4 widen(uint32_t w) {
-  uint32_t a, b;
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\t"
-      "cvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}\n"
-      : "=r"(a), "=r"(b)
+struct Args8 : PromptArgs {
+  const uint16_t* q;
+  const float *k_scale, *v_scale;
+  // a tree's rows (Tree8)
+  const int32_t* n_nodes;
+  const uint64_t* anc;
+  int n_max;
+};
+struct Tree8 : Args8 {
+  static constexpr bool kTree = true;
+};
+
+// Two float as fp16 (lo in the low half), and e4m3 pairs to and from fp16 pairs.
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ void widen(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}\n"
+      : "=r"(lo), "=r"(hi)
       : "r"(w));
-  const float2 p = __half22float2(*reinterpret_cast<__half2*>(&a)), q = __half22float2(*reinterpret_cast<__half2*>(&b));
-  return make_float4(p.x, p.y, q.x, q.y);
+}
+__device__ __forceinline__ uint32_t narrow(uint32_t lo, uint32_t hi) {
+  uint32_t w;
+  asm("{\n\t.reg .b16 a, b;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\t"
+      "mov.b32 %0, {a, b};\n\t}\n"
+      : "=r"(w)
+      : "r"(lo), "r"(hi));
+  return w;
+}
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
 }
 
-__global__ void __launch_bounds__(128) attn8_kernel(const Attn8Call A) {
-  pdl_begin();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int row = blockIdx.x, h = blockIdx.y, Hkv = A.kv.heads_kv, hk = h / (A.heads_q / Hkv);
-  int b, i, n;
-  if (A.n_nodes) {
-    b = row / A.n_max;
-    i = row % A.n_max;
-    n = A.n_nodes[b];
-    if (n < 1 || n > A.n_max) {
-      if (threadIdx.x == 0) flag(A.err, CURE_DEVERR_NODES);
-      return;
-    }
-    if (i >= n) return;
-  } else {
-    for (b = 0; b < A.batch && A.row_start[b + 1] <= row; ++b) {}
-    if (b == A.batch || row < A.row_start[b]) return;
-    i = row - A.row_start[b];
-    n = A.row_start[b + 1] - A.row_start[b];
-    if (A.row_start[b] < 0 || A.row_start[b + 1] > A.rows) {
-      if (threadIdx.x == 0) flag(A.err, CURE_DEVERR_NODES);
-      return;
-    }
-  }
-  const int L = A.cache_len[b];
-  const int64_t cap = A.kv.layout == 0 ? A.kv.max_len : (int64_t)A.kv.max_len * A.kv.page_size;
-  if (L < 0 || (int64_t)L + n > cap) {
-    if (threadIdx.x == 0) flag(A.err, CURE_DEVERR_SLOT);
+// Lane i of the warp reads TMEM lane (taddr.lane + i), 16 columns.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+
+// S = Q_m K^T: 4 steps of 32 dims with q1, then with q2 (kQHalf further on).
+__device__ __forceinline__ void issue_s(uint32_t d, uint32_t q, uint32_t q_hi, uint32_t k, uint32_t k_hi, uint32_t idesc,
+                                        uint32_t full) {
+  static_assert(kQHalf >> 4 == 1024, "as the steps are written");
+  asm volatile(
+      "{\n\t.reg .pred pf, pt, el;\n\t.reg .b64 a, b0, b1, b2, b3;\n\t.reg .b32 x;\n\t"
+      "elect.sync _|el, 0xffffffff;\n\t"
+      "setp.ne.b32 pf, 0, 0;\n\t"
+      "setp.eq.b32 pt, 0, 0;\n\t"
+      "mov.b64 a, {%1, %2};\n\tmov.b64 b0, {%3, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b0, %5, pf;\n\t"
+      "add.u32 x, %1, 2;\n\tmov.b64 a, {x, %2};\n\tadd.u32 x, %3, 2;\n\tmov.b64 b1, {x, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b1, %5, pt;\n\t"
+      "add.u32 x, %1, 4;\n\tmov.b64 a, {x, %2};\n\tadd.u32 x, %3, 4;\n\tmov.b64 b2, {x, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b2, %5, pt;\n\t"
+      "add.u32 x, %1, 6;\n\tmov.b64 a, {x, %2};\n\tadd.u32 x, %3, 6;\n\tmov.b64 b3, {x, %4};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b3, %5, pt;\n\t"
+      "add.u32 x, %1, 1024;\n\tmov.b64 a, {x, %2};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b0, %5, pt;\n\t"
+      "add.u32 x, %1, 1026;\n\tmov.b64 a, {x, %2};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b1, %5, pt;\n\t"
+      "add.u32 x, %1, 1028;\n\tmov.b64 a, {x, %2};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b2, %5, pt;\n\t"
+      "add.u32 x, %1, 1030;\n\tmov.b64 a, {x, %2};\n\t"
+      "@el tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b3, %5, pt;\n\t"
+      "@el tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t}\n" ::"r"(d),
+      "r"(q), "r"(q_hi), "r"(k), "r"(k_hi), "r"(idesc), "r"(full)
+      : "memory");
+}
+
+// Instruction descriptor with float32 D and A, B of format 0: fp16 in kind::f16, e4m3 in kind::f8f6f4.
+__host__ __device__ constexpr uint32_t idesc_0(int M, int N, bool b_mn_major) {
+  return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+constexpr float kLift = 7.f;  // P' is 2^kLift times what it stands for: at most 2^15 with the lag of 2^8
+
+template <class Args>
+__global__ void __launch_bounds__(kThreads, 1)
+attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Args A) {
+  constexpr bool kTree = Args::kTree;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t sb = smem_u32(smem);
+  if (sb & 1023u) {  // the swizzled tiles need a 1 KiB-aligned base
+    if (tid == 0) flag(A.err, CURE_DEVERR_ALIGN);
     return;
   }
-  const uint64_t* anc = A.n_nodes ? A.anc + (int64_t)row * ((A.n_max + 63) / 64) : nullptr;
-  const int keys = A.n_nodes ? L + n : L + i + 1;
-  const uint2 qw = *reinterpret_cast<const uint2*>(A.q + ((int64_t)row * A.heads_q + h) * kD + 4 * lane);
-  const float c = A.scale * 1.4426950408889634f;
-  const float q0 = __uint_as_float(qw.x << 16) * c, q1 = __uint_as_float(qw.x & 0xffff0000u) * c,
-              q2 = __uint_as_float(qw.y << 16) * c, q3 = __uint_as_float(qw.y & 0xffff0000u) * c;
-  float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int j = warp; j < keys; j += 4) {
-    if (anc && j >= L && !(anc[(j - L) >> 6] >> ((j - L) & 63) & 1u)) continue;
-    int64_t crow, place;
-    float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-    bool there = true;
-    if (A.kv.layout == 0) {
-      crow = (int64_t)b * A.kv.max_len + j;
-      place = (int64_t)b * ((A.kv.max_len + kBlk - 1) / kBlk) + j / kBlk;
-    } else {
-      const int ps = A.kv.page_size, page = A.kv.block_table[(int64_t)b * A.kv.max_len + j / ps];
-      there = page >= 0 && page < A.kv.num_pages;
-      crow = (int64_t)page * ps + j % ps;
-      place = crow / kBlk;
-      if (!there && threadIdx.x == 0) flag(A.err, CURE_DEVERR_PAGE);
+  const int G = A.G, npb = BM / G;
+  const Bar bar{sb + kOffMisc};
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
+  const uint32_t aborted = sb + kOffAbort;
+  volatile int* n_joins = reinterpret_cast<volatile int*>(smem + kOffJoins);
+  float* q_scale = reinterpret_cast<float*>(smem + kOffQScale);
+  float* row_inv = reinterpret_cast<float*>(smem + kOffInv);
+  float* lse_of = reinterpret_cast<float*>(smem + kOffLse);
+
+  // ---------------------------------------------------------------- set-up
+  if (tid == 0) {
+    mbar_init(bar(B_QFULL), BM);
+    mbar_init(bar(B_QEMPTY), 1);
+    mbar_init(bar(B_SFREE), BM);
+    for (int i = 0; i < NK; ++i) {
+      mbar_init(bar(B_KFULL + i), 1);
+      mbar_init(bar(B_KEMPTY + i), 1);
     }
-    float ks = 0.f, vs = 0.f;
-    if (there) {
-      k = widen(*reinterpret_cast<const uint32_t*>(A.k_cache + (crow * Hkv + hk) * kD + 4 * lane));
-      v = widen(*reinterpret_cast<const uint32_t*>(A.v_cache + (crow * Hkv + hk) * kD + 4 * lane));
-      ks = fminf(fmaxf(A.k_scale[place * Hkv + hk], 0x1p-40f), 0x1p40f);
-      vs = fminf(fmaxf(A.v_scale[place * Hkv + hk], 0x1p-40f), 0x1p40f);
+    for (int i = 0; i < NV; ++i) {
+      mbar_init(bar(B_VFULL + i), 1);
+      mbar_init(bar(B_VEMPTY + i), 4);
     }
-    float x = (q0 * k.x + q1 * k.y) + (q2 * k.z + q3 * k.w);
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
-    x *= ks;
-    const float mn = fmaxf(m, x), a = ex2(m - mn), p = ex2(x - mn);
-    m = mn;
-    l = l * a + p;
-    o = make_float4(o.x * a + p * vs * v.x, o.y * a + p * vs * v.y, o.z * a + p * vs * v.z, o.w * a + p * vs * v.w);
+    for (int i = 0; i < NW; ++i) {
+      mbar_init(bar(B_WFULL + i), 4);
+      mbar_init(bar(B_WEMPTY + i), 1);
+    }
+    for (int m = 0; m < 2; ++m) {
+      mbar_init(bar(B_SFULL + m), 1);
+      mbar_init(bar(B_PFULL + m), BM);
+      mbar_init(bar(B_PVDONE + m), 1);
+      mbar_init(bar(B_STAT + m), BM);
+      mbar_init(bar(B_OFREE + m), BM);
+      mbar_init(bar(B_DRAIN + m), 1);
+    }
+    mbar_init(bar(B_JOIN), BM);
+    for (int i = 0; i < kPieces; ++i) {
+      mbar_init(bar(B_PIECE + i), 1);
+      mbar_init(bar(B_TAKEN + i), kTakers);
+    }
+    *abort_flag = 0;
+    *n_joins = 0;
+    fence_mbar_init();
   }
-  __shared__ float sm[4], sl[4];
-  __shared__ float4 so[4][32];
-  if (lane == 0) {
-    sm[warp] = m;
-    sl[warp] = l;
+  if (warp == 0) tmem_alloc(sb + kOffTmemSlot, kTmemCols);
+  if (warp == 8 && lane == 0) {
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
   }
-  so[warp][lane] = o;
+  pdl_begin();
+  tc_fence_before();
   __syncthreads();
-  if (warp > 0) return;
-  const float M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  float L4 = 0.f;
-  o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int w = 0; w < 4; ++w) {
-    if (sm[w] == -INFINITY) continue;
-    const float a = ex2(sm[w] - M);
-    L4 += a * sl[w];
-    const float4 t = so[w][lane];
-    o = make_float4(o.x + a * t.x, o.y + a * t.y, o.z + a * t.z, o.w + a * t.w);
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmemSlot);
+  Await<false> await;
+  Pieces pieces{0};
+  Piece x;
+  // Whether a piece has rows in both M tiles; else both softmax groups take M tile 0's, a tile each in turn.
+  auto two_tiles = [&](const Piece& x) { return (2 * x.rg + 1) * npb < x.n; };
+
+  // (128 * (2 * 160 + 96 + 96) = 512 * 128 registers, what the block was launched with)
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+    // ================================================================ softmax
+    const int m = warp >> 2;
+    const int row = tid & 127;  // row within the M tile = TMEM lane
+    const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t tS = tl + kColS, tP = tl + kColP + m * 64, tO = tl + kColO + m * D;
+    uint32_t sc = 0, tiles = 0, pc = 0;  // tiles of this group, tiles and pieces of the CTA
+    bool ok = true;
+    uint32_t done = 0;  // pieces of this group
+    while (ok && pieces.next<Lay>(await, bar, smem, aborted, x)) {
+      const uint32_t tile0 = tiles;
+      tiles += (uint32_t)(x.t1 - x.t0);
+      const bool two = two_tiles(x);
+      const int mq = two ? m : 0, step = two ? 1 : 2;  // the M tile whose rows these are
+      const int first = x.t0 + m - mq;
+      const float* qs = q_scale + ((pc++ & 1u) * 2 + mq) * BM + row;
+      if (first >= x.t1) continue;
+      const int i0 = (2 * x.rg + mq) * npb;
+      const int i = i0 + row / G;  // the row's place in its sequence
+      const bool idle = (warp & 3) * 32 >= min(npb, x.n - i0) * G;  // no row of the warp is one of the sequence's
+      // keys that the row sees (a tree's: at most), the fewest and the most that a row of this warp sees
+      const int sees = kTree ? x.L + x.n : x.L + i + 1;
+      const int least = kTree ? x.L : __shfl_sync(0xffffffffu, sees, 0), most = __shfl_sync(0xffffffffu, sees, 31);
+      float m_run = -INFINITY, l_run = 0.f, c = 0.f;
+      for (int t = first; t < x.t1; t += step) {
+        if (!await(bar(B_SFULL + m), sc & 1u, aborted)) { ok = false; break; }
+        ++sc;
+        tc_fence_after();
+        if (idle) {  // its rows of P' and O may hold anything
+          mbar_arrive(bar(B_SFREE));
+          if (sc > 1 && !await(bar(B_PVDONE + m), (sc - 2) & 1u, aborted)) { ok = false; break; }
+          mbar_arrive(bar(B_PFULL + m));
+          continue;
+        }
+        uint32_t v[4][32];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(tS + 32 * q, v[q]);
+        tmem_wait_ld();
+        tc_fence_before();
+        mbar_arrive(bar(B_SFREE));  // the next product may take S
+        if (t == first) c = A.scale_log2 * *qs;
+        // (a tile's scales stay until the eighth tile behind it, which is loaded after this one's softmax)
+        const float4* scales =
+            reinterpret_cast<const float4*>(smem + kOffScales + ((tile0 + (uint32_t)(t - x.t0)) % kScaleSlots) * (3 * kBlocks * 4));
+        float x_[BN];
+#pragma unroll
+        for (int k = 0; k < BN; ++k) x_[k] = __uint_as_float(v[k >> 5][k & 31]);
+        if ((t + 1) * BN > least) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int at = t * BN + 32 * q;  // the block's first key
+            if (at + 32 > least) {
+              const int left = min(max(sees - at, 0), 32);  // keys of the block that the row sees
+              uint32_t seen = left == 32 ? 0xffffffffu : (1u << left) - 1u;
+              if constexpr (kTree) {
+                const int words = 2 * ((A.n_max + 63) / 64), base = at - x.L;  // the node of the block's first key
+                const uint32_t* anc = reinterpret_cast<const uint32_t*>(A.anc) + (int64_t)(x.r0 + i) * words;
+                auto word = [&](int k) -> uint32_t { return i < x.n && k < words ? __ldg(anc + k) : 0u; };
+                seen &= base >= 0 ? __funnelshift_r(word(base >> 5), word((base >> 5) + 1), base & 31)
+                                  : (word(0) << -base) | ((1u << -base) - 1u);
+              }
+#pragma unroll
+              for (int k = 0; k < 32; ++k) x_[32 * q + k] = (seen >> k) & 1u ? x_[32 * q + k] : -INFINITY;
+            }
+          }
+        }
+        // the maximum of s + log2 vs: of each block's scores first (a factor never 0: it meets -infinity)
+        float mt = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < kBlocks; b += 4) {
+          const float4 ks = scales[b / 4], lv = scales[kBlocks / 4 + b / 4];
+          const float k4[4] = {ks.x, ks.y, ks.z, ks.w}, l4[4] = {lv.x, lv.y, lv.z, lv.w};
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const float* y = x_ + (b + u) * kBlk;
+            float a0 = fmax3(y[0], y[1], y[2]), a1 = fmax3(y[3], y[4], y[5]);
+            a0 = fmax3(a0, y[6], y[7]);
+            a1 = fmax3(a1, y[8], y[9]);
+            a0 = fmax3(a0, y[10], y[11]);
+            a1 = fmax3(a1, y[12], y[13]);
+            a0 = fmax3(a0, y[14], y[15]);
+            mt = fmaxf(mt, fmaf(fmaxf(a0, a1), fmaxf(c * k4[u], FLT_MIN), l4[u]));
+          }
+        }
+        const float m_new = fmaxf(m_run, mt);
+        const bool need = m_new > m_run + 8.0f;
+        const float alpha = need ? ex2(m_run - m_new) : 1.f;
+        if (need) m_run = m_new;
+        // P's place and O are free once this group's PV product before is done
+        if (sc > 1) {
+          if (!await(bar(B_PVDONE + m), (sc - 2) & 1u, aborted)) { ok = false; break; }
+          tc_fence_after();
+        }
+        const float nbase = m_run == -INFINITY ? 0.f : kLift - m_run;
+        uint64_t sum = f2_pack(0.f, 0.f);
+        auto exponentials = [&](int q) {  // of 32 keys
+          uint32_t pk[16];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const int b = 2 * q + u;
+            const float cb = fmaxf(c * reinterpret_cast<const float*>(scales)[b], FLT_MIN);
+            const float lv = reinterpret_cast<const float*>(scales)[kBlocks + b];
+            const float iv = reinterpret_cast<const float*>(scales)[2 * kBlocks + b];
+            const uint64_t c2 = f2_pack(cb, cb), nb2 = f2_pack(nbase + lv, nbase + lv);
+            uint64_t part = f2_pack(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              float a0, a1;
+              f2_unpack(f2_fma(f2_pack(x_[16 * b + 2 * k], x_[16 * b + 2 * k + 1]), c2, nb2), a0, a1);
+              const float p0 = ex2(a0), p1 = ex2(a1);
+              part = f2_add(part, f2_pack(p0, p1));
+              pk[8 * u + k] = pack_f16(p0, p1);
+            }
+            sum = f2_fma(part, f2_pack(iv, iv), sum);
+          }
+          tmem_st16(tP + 16 * q, pk);
+        };
+        exponentials(0);
+        exponentials(1);
+        if (t * BN + BN / 2 < most) {
+          exponentials(2);
+          exponentials(3);
+        } else {  // keys that no row of the warp sees
+          const uint32_t zero[16] = {};
+          tmem_st16(tP + 32, zero);
+          tmem_st16(tP + 48, zero);
+        }
+        float s0, s1;
+        f2_unpack(sum, s0, s1);
+        l_run = l_run * alpha + (s0 + s1);
+        if (t > first && __any_sync(0xffffffffu, need)) {
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            uint32_t o[32];
+            tmem_ld32(tO + q * 32, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+            tmem_st32(tO + q * 32, o);
+          }
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar(B_PFULL + m));
+      }
+      if (!ok) break;
+      // What the epilogue needs to know of the row, once it is done with the piece before.
+      if (done > 0 && !await(bar(B_OFREE + m), (done - 1) & 1u, aborted)) break;
+      row_inv[m * BM + row] = l_run > 0.f ? 1.f / l_run : 0.f;
+      lse_of[m * BM + row] = row_lse(m_run - kLift, l_run);
+      mbar_arrive(bar(B_STAT + m));
+      ++done;
+    }
+  } else if (warp >= 12) {
+    // ================================================================ Q, V tiles, epilogue
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    const int row = tid & 127;  // row within an M tile = TMEM lane
+    const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColO;
+    const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
+    uint32_t done0 = 0, done1 = 0, tiles0 = 0, tiles1 = 0, joins = 0, pc = 0, vt = 0;
+    bool ok = true, have = false;
+    Piece* kept = reinterpret_cast<Piece*>(smem + kOffKept) + (warp & 3);  // (registers are short)
+    // The epilogue's threads meet (an mbarrier, for a wait that ends when the CTA gives up).
+    auto meet = [&]() -> bool {
+      mbar_arrive(bar(B_JOIN));
+      return ok = await(bar(B_JOIN), joins++ & 1u, aborted);
+    };
+    while (ok) {
+      const bool more = pieces.next<Lay>(await, bar, smem, aborted, x);
+      if (!more && !have) break;
+      if (more) {
+        // ---- Q of the piece, once the S products of the one before are done
+        if (!await(bar(B_QEMPTY), (pc & 1u) ^ 1u, aborted)) break;
+        const int mts = two_tiles(x) ? 2 : 1;
+#pragma unroll 1
+        for (int m = 0; m < mts; ++m) {
+          const int i = (2 * x.rg + m) * npb + row / G;
+          uint4 w[16];
+          if (row < npb * G && i < x.n) {
+            const uint4* src =
+                reinterpret_cast<const uint4*>(A.q + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = __ldg(src + k);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          // the row's largest value: bf16 magnitudes in order as integers, two at a time
+          __nv_bfloat162 big = __float2bfloat162_rn(0.f);
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) big = __hmax2(big, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&u[e])));
+          }
+          const float amax = fmaxf(__low2float(big), __high2float(big));
+          // 2^e, the least with amax <= 448 * 2^e (448 = 1.75 * 2^8), not below 2^-60
+          const uint32_t bits = __float_as_uint(amax);
+          const int e = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -60), 120);
+          q_scale[((pc & 1u) * 2 + m) * BM + row] = __uint_as_float((uint32_t)(127 + e) << 23);
+          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+          const uint32_t dst = sb + kOffQ + m * 2 * kQHalf + row * 128;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) {  // 16 dims
+            const uint32_t in[8] = {w[2 * u].x,     w[2 * u].y,     w[2 * u].z,     w[2 * u].w,
+                                    w[2 * u + 1].x, w[2 * u + 1].y, w[2 * u + 1].z, w[2 * u + 1].w};
+            uint32_t q1[4], q2[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t f[2], r[2];
+#pragma unroll
+              for (int z = 0; z < 2; ++z)
+                f[z] = pack_f16(__uint_as_float(in[2 * k + z] << 16) * inv,
+                                __uint_as_float(in[2 * k + z] & 0xffff0000u) * inv);
+              q1[k] = narrow(f[0], f[1]);
+              widen(q1[k], r[0], r[1]);
+              q2[k] = narrow(sub_f16x2(f[0], r[0]), sub_f16x2(f[1], r[1]));
+            }
+            const uint32_t to = dst + ((u ^ (row & 7)) << 4);
+            st_shared_v4(to, q1[0], q1[1], q1[2], q1[3]);
+            st_shared_v4(to + kQHalf, q2[0], q2[1], q2[2], q2[3]);
+          }
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(bar(B_QFULL));
+        ++pc;
+      }
+      for (int t = more ? x.t0 : 0, t_end = more ? x.t1 : 1; ok && t < t_end; ++t) {
+        if (more) {
+          // ---- a V tile to fp16: 16 codes a load; keys behind the unit's last one count as zeros,
+          // so that what lies there cannot reach O through 0 * NaN
+          const uint32_t vs = vt % NV, ws = vt % NW;
+          if (!await(bar(B_VFULL + vs), (vt / NV) & 1u, aborted) ||
+              !await(bar(B_WEMPTY + ws), ((vt / NW) & 1u) ^ 1u, aborted)) {
+            ok = false;
+            break;
+          }
+          ++vt;
+          const uint32_t src = sb + kOffV + vs * kTile + row * 16;
+          uint4 w[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = ld_shared_v4(src + j * 2048);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_VEMPTY + vs));
+          const int valid = x.keys - t * BN, key = row >> 3, seg = row & 7;  // keys 16 j + key, dims 16 seg ..
+          if (valid < BN) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (16 * j + key >= valid) w[j] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          // The two 16-byte units of a lane, the second first in the second half of the dims
+          // (the halves lie 2 KiB apart, on the same banks).
+          const int hf = seg >> 2, u0 = ((seg & 3) * 2 + hf) ^ (key & 7), u1 = ((seg & 3) * 2 + 1 - hf) ^ (key & 7);
+          const uint32_t dst = sb + kOffW + ws * kTileW + hf * kVHalf + key * 128;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            uint32_t a[8];
+            widen(w[j].x, a[0], a[1]);
+            widen(w[j].y, a[2], a[3]);
+            widen(w[j].z, a[4], a[5]);
+            widen(w[j].w, a[6], a[7]);
+            const uint32_t to = dst + j * kVChunk;
+            st_shared_v4(to + (u0 << 4), hf ? a[4] : a[0], hf ? a[5] : a[1], hf ? a[6] : a[2], hf ? a[7] : a[3]);
+            st_shared_v4(to + (u1 << 4), hf ? a[0] : a[4], hf ? a[1] : a[5], hf ? a[2] : a[6], hf ? a[3] : a[7]);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(B_WFULL + ws));
+        }
+        if (!have) continue;
+        // ---- the piece before: its rows
+        have = false;
+        const Piece prev = *kept;
+        const int nt = prev.t1 - prev.t0;
+        const bool whole = nt == prev.T, two = two_tiles(prev), both = !two && nt > 1;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (prev.t0 == 0);
+        tiles0 += (uint32_t)(two ? nt : (nt + 1) / 2);
+        tiles1 += (uint32_t)(two ? nt : nt / 2);
+#pragma unroll 1
+        for (int m = 0; m < (two ? 2 : 1); ++m) {
+          // STAT first: the softmax has then seen all PV products but the last
+          if (!await(bar(B_STAT + m), (m ? done1++ : done0++) & 1u, aborted) ||
+              !await(bar(B_PVDONE + m), ((m ? tiles1 : tiles0) - 1) & 1u, aborted)) {
+            ok = false;
+            break;
+          }
+          float f0 = row_inv[m * BM + row], f1 = 0.f, lse = lse_of[m * BM + row];
+          if (both) {
+            if (!await(bar(B_STAT + 1), done1++ & 1u, aborted) ||
+                !await(bar(B_PVDONE + 1), (tiles1 - 1) & 1u, aborted)) {
+              ok = false;
+              break;
+            }
+            const float l1 = lse_of[BM + row], top = fmaxf(lse, l1), w0 = ex2(lse - top), w1 = ex2(l1 - top);
+            const float r = 1.f / (w0 + w1);
+            f0 *= w0 * r;
+            f1 = row_inv[BM + row] * w1 * r;
+            lse = top + log2f(w0 + w1);
+          }
+          tc_fence_after();
+          const int i = (2 * prev.rg + m) * npb + row / G;
+          const bool vrow = row < npb * G && i < prev.n;
+          uint16_t* orow = A.out + ((int64_t)(prev.r0 + i) * A.heads_q + prev.h * G + row % G) * D;
+          float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + m * BM + row;
+          if (!whole) __stcg(A.ws_lse + slot * (2 * BM) + m * BM + row, lse);
+#pragma unroll 1
+          for (int q = 0; q < 8; ++q) {  // 16 columns
+            uint32_t o[16];
+            tmem_ld16(tO + m * D + q * 16, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f0);
+            if (both) {
+              uint32_t o1[16];
+              tmem_ld16(tO + D + q * 16, o1);
+              tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 16; ++k)
+                o[k] = __float_as_uint(fmaf(__uint_as_float(o1[k]), f1, __uint_as_float(o[k])));
+            }
+            if (!vrow) {
+            } else if (whole) {
+              uint32_t v[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
+              st_global_32(orow + q * 16, v, wide);
+            } else {
+              // a part of a unit: normalised O to the workspace, float4 columns [32][256 rows]
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                po[(q * 4 + k) * (2 * BM)] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
+                                                         __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+            }
+          }
+          tc_fence_before();
+          mbar_arrive(bar(B_OFREE + m));
+          if (both) mbar_arrive(bar(B_OFREE + 1));
+        }
+        if (!ok || whole) continue;
+        // The CTA whose part arrives last joins the unit when its own pieces are done.
+        __threadfence();
+        if (!meet()) break;
+        if (tid == 12 * 32 && !*abort_flag && arrive(A.cnt + prev.o0, A.tag) == prev.parts) {
+          A.cnt[prev.o0] = 0;  // a completed unit leaves a zero word behind
+          *reinterpret_cast<Piece*>(smem + kOffPieces + (kPieces + *n_joins) * (kPieceInts * 4)) = prev;
+          *n_joins = *n_joins + 1;
+        }
+      }
+      if (!more) break;
+      __syncwarp();
+      if (lane == 0) *kept = x;
+      __syncwarp();
+      have = true;
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    if (warp == 8) {
+      // ================================================================ producer
+      const int ps = A.kv.page_size;
+      const bool paged = A.kv.layout == 1;
+      const int ppt = paged ? BN / ps : 0;  // pages (boxes) of a tile: 2 .. 8
+      uint32_t kt = 0, vt = 0;              // tiles issued
+      while (pieces.next<Lay>(await, bar, smem, aborted, x)) {
+        auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
+          const int tok = t * BN + lane * ps;
+          if (lane >= ppt || t >= x.t1 || tok >= x.keys) return -1;
+          const int page = A.kv.block_table[(int64_t)x.b * A.kv.max_len + tok / ps];
+          if (page < 0 || page >= A.kv.num_pages) {
+            flag(A.err, CURE_DEVERR_PAGE);
+            return -1;
+          }
+          return page;
+        };
+        // lanes 0-7, 8-15: the scales of K's and V's blocks in tile t, whose pages the lanes hold
+        auto scale_of = [&](int t, int page) -> float {
+          const int blk = lane & 7, tok = t * BN + blk * kBlk;
+          int64_t place;
+          if (paged) {
+            const int p = __shfl_sync(0xffffffffu, page, blk * kBlk / ps);
+            place = p < 0 ? -1 : (int64_t)p * (ps / kBlk) + blk * kBlk % ps / kBlk;
+          } else {
+            place = (int64_t)x.b * ((A.kv.max_len + kBlk - 1) / kBlk) + t * kBlocks + blk;
+          }
+          if (lane >= 16 || t >= x.t1 || tok >= x.keys || place < 0) return 1.f;
+          return __ldg((lane < 8 ? A.k_scale : A.v_scale) + place * A.kv.heads_kv + x.h);
+        };
+        int page_v = -1, page = page_of(x.t0), page1 = page_of(x.t0 + 1);
+        float scale = scale_of(x.t0, page);
+        for (int u = x.t0; u <= x.t1; ++u) {  // K of tile u, then V of the tile before
+          const int page2 = page_of(u + 2);
+          const float scale1 = scale_of(u + 1, page1);
+#pragma unroll 1
+          for (int kv = 0; kv < 2; ++kv) {
+            if (kv ? u == x.t0 : u == x.t1) continue;
+            const uint32_t n = kv ? vt : kt, st = kv ? n % NV : n % NK, round = kv ? n / NV : n / NK;
+            const uint32_t full = bar((kv ? B_VFULL : B_KFULL) + st), empty = bar((kv ? B_VEMPTY : B_KEMPTY) + st);
+            const uint32_t dst = sb + (kv ? kOffV : kOffK) + st * kTile;
+            if (!await(empty, (round & 1u) ^ 1u, aborted)) goto produced;
+            if (!kv && lane < 16) {
+              float* to = reinterpret_cast<float*>(smem + kOffScales) + (n % kScaleSlots) * (3 * kBlocks) + (lane & 7);
+              const float s = fminf(fmaxf(scale, 0x1p-40f), 0x1p40f);
+              if (lane < 8) {
+                to[0] = s;
+              } else {
+                to[kBlocks] = log2f(s);
+                to[2 * kBlocks] = 1.f / s;
+              }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive_expect_tx(full, kTile);
+            __syncwarp();
+            const CUtensorMap* map = kv ? &tm_v : &tm_k;
+            if (paged) {
+              if (lane < ppt) tma_load_4d(dst + lane * ps * D, map, full, 0, x.h, 0, kv ? page_v : page);
+            } else if (lane == 0) {
+              tma_load_4d(dst, map, full, 0, x.h, (kv ? u - 1 : u) * BN, x.b);
+            }
+            __syncwarp();
+            if (kv) ++vt;
+            else ++kt;
+          }
+          page_v = page;
+          page = page1;
+          page1 = page2;
+          scale = scale1;
+        }
+      }
+    produced:
+      if (*abort_flag) {  // let copies in flight land before the CTA's smem goes away
+        for (uint32_t i = (kt > NK ? kt - NK : 0); i < kt; ++i)
+          wait_bounded(bar(B_KFULL + i % NK), (i / NK) & 1u, abort_flag, A.err, false);
+        for (uint32_t i = (vt > NV ? vt - NV : 0); i < vt; ++i)
+          wait_bounded(bar(B_VFULL + i % NV), (i / NV) & 1u, abort_flag, A.err, false);
+      }
+    } else if (warp == 9) {
+      // ================================================================ S products
+      constexpr uint32_t idS = idesc_0(BM, BN, false);
+      uint32_t qc = 0, c = 0, kt = 0;  // pieces, products, K tiles
+      const uint64_t qd = sdesc_sw128(sb + kOffQ, 16, 1024), kd = sdesc_sw128(sb + kOffK, 16, 1024);
+      while (pieces.next<Lay>(await, bar, smem, aborted, x)) {
+        if (!await(bar(B_QFULL), qc++ & 1u, aborted)) break;
+        const bool two = two_tiles(x);
+        for (int t = x.t0; t < x.t1; ++t, ++kt) {
+          const uint32_t st = kt % NK;
+          if (!await(bar(B_KFULL + st), (kt / NK) & 1u, aborted)) goto scored;
+#pragma unroll 1
+          for (int m = 0; m < (two ? 2 : 1); ++m) {
+            // (the first product waits for the phase before the first, which counts as done)
+            if (!await(bar(B_SFREE), (c++ & 1u) ^ 1u, aborted)) goto scored;
+            tc_fence_after();
+            issue_s(tmem + kColS, (uint32_t)qd + m * (2 * kQHalf >> 4), (uint32_t)(qd >> 32),
+                    (uint32_t)kd + st * (kTile >> 4), (uint32_t)(kd >> 32), idS,
+                    bar(B_SFULL + (two ? m : (t - x.t0) & 1)));
+          }
+          commit_elect(bar(B_KEMPTY + st));
+          if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
+        }
+      }
+    scored:
+      __syncwarp();
+      commit_elect(bar(B_DRAIN));
+      wait_bounded(bar(B_DRAIN), 0, abort_flag, A.err, false);
+    } else if (warp == 10) {
+      // ================================================================ PV products
+      constexpr uint32_t idO = idesc_0(BM, D, true);
+      uint32_t c0 = 0, c1 = 0, done0 = 0, done1 = 0, vt = 0;  // products and pieces of each group, V tiles
+      // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
+      const uint64_t vd = sdesc_sw128(sb + kOffW, kVHalf, 1024);
+      while (pieces.next<Lay>(await, bar, smem, aborted, x)) {
+        const bool two = two_tiles(x);
+        for (int t = x.t0; t < x.t1; ++t, ++vt) {
+          const uint32_t st = vt % NW;
+          if (!await(bar(B_WFULL + st), (vt / NW) & 1u, aborted)) goto multiplied;
+          const int turn = two ? 0 : (t - x.t0) & 1;
+#pragma unroll 1
+          for (int m = turn; m < (two ? 2 : turn + 1); ++m) {
+            // a group's first product of a piece takes O over from the epilogue of the one before
+            // (from none at first: the phase before the first counts as done)
+            const bool fresh = t - x.t0 == turn;
+            if (fresh && !await(bar(B_OFREE + m), ((m ? done1++ : done0++) & 1u) ^ 1u, aborted)) goto multiplied;
+            if (!await(bar(B_PFULL + m), (m ? c1++ : c0++) & 1u, aborted)) goto multiplied;
+            tc_fence_after();
+            issue_pv(tmem + kColO + m * D, tmem + kColP + m * 64, (uint32_t)vd + st * (kTileW >> 4),
+                     (uint32_t)(vd >> 32), idO, !fresh, bar(B_PVDONE + m));
+          }
+          commit_elect(bar(B_WEMPTY + st));
+        }
+      }
+    multiplied:
+      __syncwarp();
+      commit_elect(bar(B_DRAIN + 1));
+      wait_bounded(bar(B_DRAIN + 1), 0, abort_flag, A.err, false);
+    } else {
+      // ================================================================ scheduler
+      schedule<Lay>(A, npb, await, bar, smem, aborted, lane);
+    }
   }
-  const float inv = L4 > 0.f ? 1.f / L4 : 0.f;
-  *reinterpret_cast<uint2*>(A.out + ((int64_t)row * A.heads_q + h) * kD + 4 * lane) =
-      make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+
+  // ---- the units that this CTA joins, by all warps and with equal registers again
+  // (behind the barrier: a warp that had nothing to do must not take back the registers
+  // that a softmax warp still waits for)
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp < 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 128;");
+  else asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+  if (*abort_flag) {
+    if (tid == 0) flag(A.err, CURE_DEVERR_TIMEOUT);
+  } else {
+    join_units<Lay>(A, npb, smem, *n_joins, warp, lane);
+  }
+  if (warp == 0) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+// One layer's codes as (d, head, token in its page or sequence, page or sequence); boxes of 128 d x
+// 1 head x `box` tokens, what lies outside reads as zeros.
+bool make_codes_map(CUtensorMap* m, const uint8_t* base, const cure_kv_desc& kv, int batch, bool swizzled) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  const bool paged = kv.layout == 1;
+  const cuuint64_t tokens = paged ? kv.page_size : kv.max_len > 0 ? kv.max_len : 1;
+  const cuuint64_t row = (cuuint64_t)kv.heads_kv * D;
+  cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)kv.heads_kv, tokens, (cuuint64_t)(paged ? kv.num_pages : batch)};
+  cuuint64_t strides[3] = {(cuuint64_t)D, row, row * tokens};
+  cuuint32_t box[4] = {(cuuint32_t)D, 1, (cuuint32_t)(paged ? kv.page_size : BN), 1};
+  cuuint32_t es[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(base), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+size_t counter_bytes(int ctas) { return ((size_t)ctas * sizeof(PieceCount) + 255) / 256 * 256; }
+
+template <class Args>
+cudaError_t launch(const Attn8Call& c, Args& A, cudaStream_t s) {
+  const auto kernel = attn8_kernel<Args>;
+  static std::atomic<uint64_t> ready;  // devices on which it has its shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(ready.load() & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit);
+  }
+  CUtensorMap mk, mv;
+  if (!make_codes_map(&mk, c.k_cache, c.kv, c.batch, true) || !make_codes_map(&mv, c.v_cache, c.kv, c.batch, false))
+    return cudaErrorInvalidValue;
+  A.kv = c.kv;
+  A.row_start = c.row_start;
+  A.cache_len = c.cache_len;
+  A.rows = c.rows;
+  A.batch = c.batch;
+  A.heads_q = c.heads_q;
+  A.G = c.heads_q / c.kv.heads_kv;
+  A.cap = std::min(c.kv.layout == 0 ? c.kv.max_len : c.kv.max_len * c.kv.page_size, INT32_MAX - 2 * BN);
+  A.scale_log2 = c.scale * 1.4426950408889634f;
+  A.out = c.out;
+  A.err = c.err;
+  A.q = c.q;
+  A.k_scale = c.k_scale;
+  A.v_scale = c.v_scale;
+  A.n_nodes = c.n_nodes;
+  A.anc = c.anc;
+  A.n_max = c.n_max;
+  A.tag = next_launch_tag();  // whatever the workspace's counters hold counts as zero
+  const int ctas = num_sms();
+  char* ws = static_cast<char*>(c.workspace);
+  A.cnt = reinterpret_cast<PieceCount*>(ws);
+  A.ws_o = reinterpret_cast<float*>(ws + counter_bytes(ctas));
+  A.ws_lse = A.ws_o + (size_t)2 * ctas * 2 * BM * D;
+  // many units: after the whole of the call before (as in k_prompt.cu)
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = (int64_t)c.rows * c.heads_q > (int64_t)4 * 2 * BM * ctas ? 0 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, mk, mv, A);
 }
 
 }  // namespace
 
-size_t attn8_workspace() { return prompt_attn_workspace(); }
+// Workspace: piece counters [CTAs] (256-byte rounded), partial outputs and their log-sum-exps
+// [2 * CTAs]: of a CTA's pieces at most its first and its last are parts of a unit.
+size_t attn8_workspace() {
+  const int ctas = num_sms();
+  return counter_bytes(ctas) + (size_t)ctas * 2 * 2 * BM * (D + 1) * sizeof(float);
+}
 
 cudaError_t launch_attn8(const Attn8Call& c, cudaStream_t s) {
-  return launch_pdl(attn8_kernel, dim3((unsigned)c.rows, (unsigned)c.heads_q), dim3(128), 0, s, c);
+  if (c.n_nodes) {
+    Tree8 A = {};
+    return launch(c, A, s);
+  }
+  Args8 A = {};
+  return launch(c, A, s);
 }
 
 }  // namespace cure

@@ -148,8 +148,9 @@ struct Walk {
     return q;
   }
   // the k-th row group's positions for a head: of the first, and what each adds
-  __device__ __forceinline__ int base() const { return split ? kUnitCost + s.L : 1; }
-  __device__ __forceinline__ int step() const { return split ? R : 0; }
+  // (a tree's row groups all see its last node)
+  __device__ __forceinline__ int base() const { return split ? kUnitCost + s.L + (Args::kTree ? groups * R : 0) : 1; }
+  __device__ __forceinline__ int step() const { return split && !Args::kTree ? R : 0; }
   __device__ __forceinline__ int64_t before(int k) const {  // a head's positions in front of the k-th row group
     return k * (int64_t)base() + (int64_t)step() * k * (k + 1) / 2;
   }
@@ -355,7 +356,7 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
   };
   auto size_of = [&](const Seq& s) -> Size {  // a sequence's positions of both kinds
     const int64_t k = walk.groups_of(s.n);
-    return {walk.Hkv * k, walk.Hkv * (k * (kUnitCost + s.L) + walk.R * k * (k + 1) / 2)};
+    return {walk.Hkv * k, walk.Hkv * (k * (kUnitCost + s.L) + walk.R * (Args::kTree ? k * k : k * (k + 1) / 2))};
   };
   auto scan = [&](int64_t v) -> int64_t {  // sum over the lanes up to this one
 #pragma unroll
