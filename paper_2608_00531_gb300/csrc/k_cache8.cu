@@ -9,13 +9,15 @@
 // scale keeps its digits, as e4m3 is a floating type: only what falls below its normal
 // range (2^-6 s) is rounded again.
 //
-// Layout.  A CTA takes the blocks that begin in its range of packed rows (a block's
-// rows in one call are neighbours), a warp one head of K or V of a block at a time: half a
-// warp a row, 8 values a lane, all 16 rows in registers (rows that the block holds already
-// are decoded into the same places), so that every value is read once, the largest is
-// found by one reduction, and the codes go out behind it.  The rows' cosines and sines
-// are made once a block in shared memory, for all heads of K and Q.
+// Layout.  A CTA takes the blocks that begin in its range of packed rows (a block's rows in
+// one call are neighbours).  Each of its 16 half warps has one slot of a block for all heads, 8 values a
+// lane: a row of the call, with the row's cosines and sines in registers, or one that the block
+// holds already.  kHeads heads of K and V at a time are loaded, normed and turned, and their rows' largest
+// values meet in shared memory; behind the barrier each half warp writes its codes.  Heads of Q go the
+// same way without meeting; where a block gains few rows, all half warps share those rows' heads.
 #include <cuda_bf16.h>
+
+#include <algorithm>
 
 #include "attn_tc.cuh"
 #include "common.cuh"
@@ -104,99 +106,93 @@ __device__ __forceinline__ void widen(const Raw& x, float* y) {
   y[7] = hi_f(x.b.y);
 }
 
-// Head norm and rotation of a lane's values (all 16 lanes of the half warp).  cs: the row's
-// cosines and sines.
+// The rotation (and, before it, the head norm: weights w times the row's factor rs) of a lane's
+// values by its four pairs' cosines and sines.
 template <bool INTER>
-__device__ __forceinline__ void norm_rotate(float* y, const float* w, bool norm, float eps, const float2* cs, bool rot,
-                                            int l16) {
+__device__ __forceinline__ void norm_rotate(float* y, const float* w, bool norm, float rs, const float* c, const float* sn,
+                                            bool rot) {
   if (norm) {
-    float ss = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    const float rs = rsqrtf(ss * (1.f / kD) + eps);
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = y[e] * rs * w[e];
   }
   if (rot) {
-    const float4* t = reinterpret_cast<const float4*>(cs + 4 * l16);
-    const float4 t0 = t[0], t1 = t[1];
-    const float c[4] = {t0.x, t0.z, t1.x, t1.z}, s[4] = {t0.y, t0.w, t1.y, t1.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int i = INTER ? 2 * e : e, j = INTER ? 2 * e + 1 : e + 4;
       const float a = y[i], b = y[j];
-      y[i] = fmaf(-b, s[e], a * c[e]);
-      y[j] = fmaf(a, s[e], b * c[e]);
+      y[i] = fmaf(-b, sn[e], a * c[e]);
+      y[j] = fmaf(a, sn[e], b * c[e]);
     }
   }
 }
+// The norm's factor of a row that half a warp holds.
+__device__ __forceinline__ float norm_factor(const float* y, float eps) {
+  float ss = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  return rsqrtf(ss * (1.f / kD) + eps);
+}
 
-// One head of a block (a warp): rows `fresh` (bits of the block's slots) from row(t), those of
-// `held` as they stand; the new codes and scale.  `codes`: the head's codes of the block's
-// slot 0, `ld` bytes from slot to slot.
-template <bool INTER, bool TURN, class Row>
-__device__ __forceinline__ void quantise_head(const Row& row, uint32_t fresh, uint32_t held, uint8_t* codes, int64_t ld,
-                                              float* scale, const Lane& p, const float* w, bool norm, float eps,
-                                              const float2 (*cs)[64], int lane) {
-  const int l16 = lane & 15, half = lane >> 4;
-  float y[8][8];
-  Raw x[8];
+constexpr int kHeads = 2;  // of K and V between two barriers
+
+// What a half warp has in the slot of its block.
+enum Slot { kNone, kHeld, kFresh };
+
+// kHeads heads of a block's K or V, all threads of the CTA: y the rows' values (kNone: any), `codes` each
+// head's codes of the half warp's slot (NULL: no head), `scale` its place.
+__device__ __forceinline__ void quantise(float (&y)[kHeads][8], Slot what, uint8_t* const (&codes)[kHeads],
+                                         float* const (&scale)[kHeads], const float (&old)[kHeads], const Lane& p,
+                                         float (*part)[16], int hw, int l16) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int t = 2 * j + half;
-    x[j].a = x[j].b = make_uint2(0u, 0u);
-    if (fresh >> t & 1u) {
-      x[j] = load_raw(row(t), p);
-    } else if (held >> t & 1u) {
-      x[j].a.x = *reinterpret_cast<const uint32_t*>(codes + t * ld + p.off_a);
-      x[j].a.y = *reinterpret_cast<const uint32_t*>(codes + t * ld + p.off_b);
-    }
+  for (int u = 0; u < kHeads; ++u) {
+    float amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[u][e]));  // (a NaN counts for nothing)
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if (l16 == 0) part[u][hw] = what == kNone ? 0.f : amax;
   }
-  const float old = held ? *scale : 1.f;
-  float amax = 0.f;
+  __syncthreads();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int t = 2 * j + half;
-    if ((fresh | held) >> (2 * j) & 3u) {  // (both halves of the warp: the norm's sums take all lanes)
-      if (held >> t & 1u) {
-        from_codes(x[j].a.x, y[j]);
-        from_codes(x[j].a.y, y[j] + 4);
+  for (int u = 0; u < kHeads; ++u) {
+    if (!codes[u]) break;
+    float amax = part[u][l16];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[j][e] *= old;
-      } else {
-        widen(x[j], y[j]);
-      }
-      if (TURN) {
-        float z[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = y[j][e];
-        norm_rotate<INTER>(z, w, norm, eps, cs[t], p.rot, l16);
-        if (fresh >> t & 1u) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[j][e] = z[e];
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[j][e]));  // (a NaN counts for nothing)
+    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    const int e = scale_exponent(amax);
+    const float s = power(e), inv = power(-e);
+    if (what == kFresh || (what == kHeld && s != old[u])) {  // (what is held stays as it is under the same scale)
+      *reinterpret_cast<uint32_t*>(codes[u] + p.off_a) =
+          to_codes(y[u][0] * inv, y[u][1] * inv, y[u][2] * inv, y[u][3] * inv);
+      *reinterpret_cast<uint32_t*>(codes[u] + p.off_b) =
+          to_codes(y[u][4] * inv, y[u][5] * inv, y[u][6] * inv, y[u][7] * inv);
     }
+    if (hw == 0 && l16 == 0) *scale[u] = s;
   }
-  // as integers, which are ordered as the values are
-  const int e = scale_exponent(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(amax))));
-  const float s = power(e), inv = power(-e);
-  const uint32_t out = s == old ? fresh : fresh | held;
+}
+
+// A half warp's values of a head as they lie: a row's, or the block's codes.
+__device__ __forceinline__ Raw load_slot(Slot what, const uint16_t* row, const uint8_t* codes, const Lane& p) {
+  Raw x;
+  x.a = x.b = make_uint2(0u, 0u);
+  if (what == kFresh) x = load_raw(row, p);
+  if (what == kHeld) {
+    x.a.x = *reinterpret_cast<const uint32_t*>(codes + p.off_a);
+    x.a.y = *reinterpret_cast<const uint32_t*>(codes + p.off_b);
+  }
+  return x;
+}
+__device__ __forceinline__ void value_of(const Raw& x, Slot what, float old, float* y) {
+  if (what == kHeld) {
+    from_codes(x.a.x, y);
+    from_codes(x.a.y, y + 4);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int t = 2 * j + half;
-    if (out >> t & 1u) {
-      *reinterpret_cast<uint32_t*>(codes + t * ld + p.off_a) =
-          to_codes(y[j][0] * inv, y[j][1] * inv, y[j][2] * inv, y[j][3] * inv);
-      *reinterpret_cast<uint32_t*>(codes + t * ld + p.off_b) =
-          to_codes(y[j][4] * inv, y[j][5] * inv, y[j][6] * inv, y[j][7] * inv);
-    }
+    for (int e = 0; e < 8; ++e) y[e] *= old;
+  } else {
+    widen(x, y);
   }
-  if (lane == 0) *scale = s;
 }
 
 // The page of a block of 16 slots, or the sequence's own range: the row of its slot 0 in the
@@ -226,47 +222,65 @@ struct Append8Args {
 };
 
 template <bool INTER>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, 3)
 append8_kernel(const __grid_constant__ Append8Args G) {
   const RopeArgs& A = G.r;
   __shared__ uint64_t turns[64];
-  __shared__ float2 cs[kBlk][64];
-  __shared__ uint32_t skip;  // rows of the block with a negative position
+  __shared__ float part[2][kHeads][16];
   if (threadIdx.x < 64) turns[threadIdx.x] = A.rope.turns[threadIdx.x];
+  __syncthreads();
   pdl_begin();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, l16 = lane & 15, half = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 31, l16 = lane & 15, hw = tid >> 4;
   const int Hq = A.heads_q, Hkv = A.heads_kv;
   const int first = blockIdx.x * G.range;
   const int end = min(first + G.range, A.rows);
   const Lane turned = lane_of<INTER>(l16, A.rope.rot_dim), plain = lane_of<true>(l16, 0);
   const int n_axes = A.axes.axes;
   const int64_t cap = A.kv.layout == 0 ? A.kv.max_len : (int64_t)A.kv.max_len * A.kv.page_size;
+  const bool tell = tid == 0 && blockIdx.y == 0;
+  int buf = 0;
 
   for (int row = first; row < end;) {
-    // the row's sequence: as many of the ends row_start[1..B] are at or before it
-    int seq = 0;
+    // The row's sequence: as many of the ends row_start[1..B] are at or before it.  Its first row, the
+    // row behind its last and its length come along with the search.
+    int seq = 0, start = A.row_start[0], stop = A.rows, L = 0;
     for (int base = 0; base < A.batch; base += 256) {
-      int e[8];
+      int e[8], len[8], n = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int b = base + 32 * i + lane;
         e[i] = b < A.batch ? A.row_start[b + 1] : INT32_MAX;
+        len[i] = b < A.batch ? A.cache_len[b] : 0;
+      }
+      const int last = base + 256 < A.batch ? __shfl_sync(0xffffffffu, e[7], 31) : INT32_MAX;
+      if (last <= row) {  // (ascending: all of these are)
+        seq += 256;
+        start = last;
+        continue;
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) seq += __popc(__ballot_sync(0xffffffffu, e[i] <= row));
+      for (int i = 0; i < 8; ++i) n += __popc(__ballot_sync(0xffffffffu, e[i] <= row));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (n > 0 && (n - 1) / 32 == i) start = __shfl_sync(0xffffffffu, e[i], (n - 1) & 31);
+        if (n / 32 == i) {
+          stop = min(stop, __shfl_sync(0xffffffffu, e[i], n & 31));
+          L = __shfl_sync(0xffffffffu, len[i], n & 31);
+        }
+      }
+      seq += n;
+      break;
     }
     if (seq >= A.batch) return;  // behind the last sequence
-    const int start = A.row_start[seq], stop = min(A.row_start[seq + 1], A.rows);
     const int i = row - start;
     if (i < 0 || start < 0 || row >= stop) {  // before the first sequence, or row_start does not ascend
-      if ((seq > 0 || i >= 0) && tid == 0 && blockIdx.y == 0) flag(A.err, CURE_DEVERR_NODES);
+      if ((seq > 0 || i >= 0) && tell) flag(A.err, CURE_DEVERR_NODES);
       ++row;
       continue;
     }
-    const int L = A.cache_len[seq];
     const int64_t slot = (int64_t)L + i;
     if (slot < 0 || slot >= cap) {
-      if (tid == 0 && blockIdx.y == 0) flag(A.err, CURE_DEVERR_SLOT);
+      if (tell) flag(A.err, CURE_DEVERR_SLOT);
       ++row;
       continue;
     }
@@ -278,83 +292,113 @@ append8_kernel(const __grid_constant__ Append8Args G) {
     const int m = (int)min((int64_t)min(kBlk - t0, stop - row), cap - slot);  // the block's rows
     const int row0 = row;
     row += m;
-    int64_t crow, place;
-    if (!place_of(A.kv, seq, blk, &crow, &place, A.err, tid == 0 && blockIdx.y == 0)) continue;
+    int64_t crow = 0, place = 0;
+    const bool there = place_of(A.kv, seq, blk, &crow, &place, A.err, tell);
 
-    // ---- the rows' angles, and which of them hold no token
-    __syncthreads();  // (the block before is done with them)
-    if (tid == 0) skip = 0;
-    __syncthreads();
-    if (A.pos && tid < m) {
-      bool none = false;
-      for (int a = 0; a < max(1, n_axes); ++a) none |= A.pos[(int64_t)a * A.rows + row0 + tid] < 0;
-      if (none) atomicOr(&skip, 1u << (t0 + tid));
+    // Half warps 0 .. m - 1 have the rows, the last t0 what the block holds; for Q row r = hw % m.
+    const int r = hw % m, t = (t0 + hw) & (kBlk - 1);
+    int p = (int)(slot + r);
+    bool none = false;  // row r holds no token
+    if (n_axes > 0) {
+      // lane a: the position on axis a
+      p = l16 < n_axes ? A.pos[(int64_t)l16 * A.rows + row0 + r] : 0;
+      none = __ballot_sync(0xffffffffu, p < 0) >> (lane & 16) & 0xffffu;
+    } else if (A.pos) {
+      p = A.pos[row0 + r];
+      none = p < 0;
     }
-    const int pairs = A.rope.rot_dim / 2;
-    for (int k = tid; k < m * 64; k += kThreads) {
-      const int r = k >> 6, pair = k & 63;
-      if (pair < pairs) {
-        const int axis = n_axes > 0 ? A.axes.axis[pair] : 0;
-        const int p = A.pos ? A.pos[(int64_t)axis * A.rows + row0 + r] : (int)(slot + r);
-        // the fraction of a turn in 2^-32, as a signed number of half turns
-        const int32_t f = (int32_t)(uint32_t)(((uint64_t)(uint32_t)p * turns[pair]) >> 32);
-        float2 c;
-        sincospif((float)f * 0x1p-31f, &c.y, &c.x);
-        cs[t0 + r][pair] = make_float2(c.x * A.rope.amplitude, c.y * A.rope.amplitude);
-      }
-    }
-    __syncthreads();
-    const uint32_t rows_in = ((1u << m) - 1u) << t0;
-    const uint32_t fresh = rows_in & ~skip;
-    const uint32_t held = i == 0 ? (1u << t0) - 1u : 0u;
-    if (fresh == 0) continue;
+    const Slot what = hw < m ? (none ? kNone : kFresh) : t < t0 && i == 0 ? kHeld : kNone;
+    if (!__syncthreads_or(what == kFresh) || !there) continue;  // (also: the block before is done with `part`)
 
-    // ---- heads of K and V, then those of Q
-    const int64_t ld = (int64_t)Hkv * kD;
-    for (int h = blockIdx.y * kWarps + warp; h < 2 * Hkv; h += gridDim.y * kWarps) {
-      const bool is_v = h >= Hkv;
-      const int hh = is_v ? h - Hkv : h;
-      if (is_v) {
-        auto src = [&](int t) { return A.v + (int64_t)(row0 + t - t0) * A.ld_v + hh * kD; };
-        quantise_head<true, false>(src, fresh, held, reinterpret_cast<uint8_t*>(A.v_out) + crow * ld + hh * kD, ld,
-                                   G.v_scale + place * Hkv + hh, plain, nullptr, false, 0.f, nullptr, lane);
-      } else {
-        float w[8];
-        if (A.k_norm) widen(load_raw(A.k_norm, turned), w);
-        auto src = [&](int t) { return A.k + (int64_t)(row0 + t - t0) * A.ld_k + hh * kD; };
-        quantise_head<INTER, true>(src, fresh, held, reinterpret_cast<uint8_t*>(A.k_out) + crow * ld + hh * kD, ld,
-                                   G.k_scale + place * Hkv + hh, turned, w, A.k_norm != nullptr, A.eps, cs, lane);
-      }
-    }
-    if (A.q) {
-      // (row, head) pairs, half a warp each, four at a time
-      float w[8];
-      if (A.q_norm) widen(load_raw(A.q_norm, turned), w);
-      const int todo = m * Hq;
-      constexpr int U = 4;
-      for (int k0 = (blockIdx.y * kWarps + warp) * 2 * U; k0 < todo; k0 += gridDim.y * kWarps * 2 * U) {
-        Raw x[U];
-        int r[U], hh[U];
-        bool there[U];
+    // cosines and sines of the lane's pairs
+    float c[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+    int at[4] = {p, p, p, p};
+    if (n_axes > 0) {
+      const uint32_t axis = reinterpret_cast<const uint32_t*>(A.axes.axis)[l16];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int k = k0 + 2 * u + half;
-          r[u] = k / Hq;
-          hh[u] = k - r[u] * Hq;
-          there[u] = k < todo && (fresh >> (t0 + r[u]) & 1u);
-          x[u].a = x[u].b = make_uint2(0u, 0u);
-          if (there[u]) x[u] = load_raw(A.q + (int64_t)(row0 + r[u]) * A.ld_q + hh[u] * kD, turned);
+      for (int e = 0; e < 4; ++e) at[e] = __shfl_sync(0xffffffffu, p, (lane & 16) | ((axis >> (8 * e)) & 7u));
+    }
+    if (turned.rot) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        // the fraction of a turn in 2^-32, as a signed number of half turns
+        const int32_t f = (int32_t)(uint32_t)(((uint64_t)(uint32_t)at[e] * turns[4 * l16 + e]) >> 32);
+        sincospif((float)f * 0x1p-31f, &sn[e], &c[e]);
+        c[e] *= A.rope.amplitude;
+        sn[e] *= A.rope.amplitude;
+      }
+    }
+
+    // ---- heads of K, then of V
+    const int64_t ld = (int64_t)Hkv * kD, at_slot = (crow + t) * ld;
+    float w[8];
+#pragma unroll 1
+    for (int kv = 0; kv < 2; ++kv) {
+      const Lane lp = kv ? plain : turned;
+      const uint16_t* in = (kv ? A.v + (row0 + hw) * A.ld_v : A.k + (row0 + hw) * A.ld_k);
+      uint8_t* base = reinterpret_cast<uint8_t*>(kv ? A.v_out : A.k_out) + at_slot;
+      float* scales = (kv ? G.v_scale : G.k_scale) + place * Hkv;
+      const bool norm = !kv && A.k_norm;
+      if (norm) widen(load_raw(A.k_norm, lp), w);
+      for (int h = blockIdx.y * kHeads; h < Hkv; h += gridDim.y * kHeads) {
+        Raw x[kHeads];
+        float old[kHeads], y[kHeads][8];
+        uint8_t* codes[kHeads];
+        float* scale[kHeads];
+#pragma unroll
+        for (int u = 0; u < kHeads; ++u) {
+          const bool is = h + u < Hkv;
+          codes[u] = is ? base + (h + u) * kD : nullptr;
+          scale[u] = scales + h + u;
+          x[u] = load_slot(is ? what : kNone, in + (h + u) * kD, codes[u], lp);
+          old[u] = is && t0 > 0 ? *scale[u] : 1.f;
         }
 #pragma unroll
+        for (int u = 0; u < kHeads; ++u) {
+          value_of(x[u], what, old[u], y[u]);
+          if (!kv) {
+            const float rs = norm ? norm_factor(y[u], A.eps) : 1.f;  // (all lanes, whatever they have)
+            if (what == kFresh) norm_rotate<INTER>(y[u], w, norm, rs, c, sn, lp.rot);
+          }
+        }
+        quantise(y, what, codes, scale, old, lp, part[buf], hw, l16);
+        buf ^= 1;
+      }
+    }
+
+    // ---- heads of Q: half warp hw those of row hw % m from the (hw / m)-th on
+    if (A.q) {
+      const int shares = kBlk / m, parts = gridDim.y * shares;
+      if (A.q_norm) widen(load_raw(A.q_norm, turned), w);
+      const uint16_t* in = A.q + (int64_t)(row0 + r) * A.ld_q;
+      uint16_t* out = A.q_out + (int64_t)(row0 + r) * A.ld_q_out;
+      const bool mine = hw < m * shares && !none;
+      constexpr int U = 4;
+      Raw x[U];
+      auto load = [&](int h0) {
+#pragma unroll
         for (int u = 0; u < U; ++u) {
+          const int h = h0 + u * parts + blockIdx.y * shares + hw / m;
+          x[u] = load_slot(mine && h < Hq ? kFresh : kNone, in + h * kD, nullptr, turned);
+        }
+      };
+      load(0);
+      for (int h0 = 0; h0 < Hq; h0 += U * parts) {
+        Raw now[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) now[u] = x[u];
+        load(h0 + U * parts);  // (none behind the last)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int h = h0 + u * parts + blockIdx.y * shares + hw / m;
           float y[8];
-          widen(x[u], y);
-          norm_rotate<INTER>(y, w, A.q_norm != nullptr, A.eps, cs[(t0 + r[u]) & 15], turned.rot, l16);
-          if (there[u]) {
-            uint16_t* out = A.q_out + (int64_t)(row0 + r[u]) * A.ld_q_out + hh[u] * kD;
-            *reinterpret_cast<uint2*>(out + turned.off_a) =
+          widen(now[u], y);
+          const float rs = A.q_norm ? norm_factor(y, A.eps) : 1.f;
+          norm_rotate<INTER>(y, w, A.q_norm != nullptr, rs, c, sn, turned.rot);
+          if (mine && h < Hq) {
+            *reinterpret_cast<uint2*>(out + h * kD + turned.off_a) =
                 make_uint2(tc::pack_bf16(y[0], y[1]), tc::pack_bf16(y[2], y[3]));
-            *reinterpret_cast<uint2*>(out + turned.off_b) =
+            *reinterpret_cast<uint2*>(out + h * kD + turned.off_b) =
                 make_uint2(tc::pack_bf16(y[4], y[5]), tc::pack_bf16(y[6], y[7]));
           }
         }
@@ -373,18 +417,18 @@ struct Paths8Args {
   int* err;
 };
 
-// The k-th block that sequence b's accepted path reaches (blockIdx.x = b * blocks + k), a
-// head of K or V of a layer a warp.
-__global__ void __launch_bounds__(kThreads, 2)
+// The k-th block that sequence b's accepted path reaches (blockIdx.x = b * blocks + k).
+__global__ void __launch_bounds__(kThreads, 3)
 paths8_kernel(const __grid_constant__ Paths8Args A) {
+  __shared__ float part[2][kHeads][16];
   pdl_begin();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int tid = threadIdx.x, l16 = tid & 15, hw = tid >> 4;
   const int blocks = (A.block + 1 + kBlk - 2) / kBlk + 1;
   const int b = blockIdx.x / blocks, k = blockIdx.x % blocks;
   const int Hkv = A.kv.heads_kv, P = A.block + 2;
   const int n = min(A.accept_len[b], A.block) + 1;  // rows of the path
   const int L = A.cache_len[b];
-  const bool tell = threadIdx.x == 0 && blockIdx.y == 0;
+  const bool tell = tid == 0 && blockIdx.y == 0;
   const int64_t cap = A.kv.layout == 0 ? A.kv.max_len : (int64_t)A.kv.max_len * A.kv.page_size;
   if (n < 1) return;
   if (L < 0 || (int64_t)L + n > cap) {
@@ -398,32 +442,39 @@ paths8_kernel(const __grid_constant__ Paths8Args A) {
   if (from >= to) return;
   int64_t crow, place;
   if (!place_of(A.kv, b, blk, &crow, &place, A.err, tell)) return;
-  // lane t: the node of slot t
-  int node = -1;
-  if (lane >= from && lane < to) {
-    node = A.path_nodes[(int64_t)b * P + (int)(slot0 + lane - L)];
-    if (node < 0 || node >= A.n_max) {
-      if (warp == 0 && blockIdx.y == 0) flag(A.err, CURE_DEVERR_NODES);
-      node = -1;
-    }
+  Slot what = hw < from ? kHeld : kNone;
+  int node = 0;
+  if (hw >= from && hw < to) {
+    node = A.path_nodes[(int64_t)b * P + (int)(slot0 + hw - L)];
+    if (node >= 0 && node < A.n_max) what = kFresh;
+    else if (l16 == 0 && blockIdx.y == 0) flag(A.err, CURE_DEVERR_NODES);
   }
-  const uint32_t fresh = __ballot_sync(0xffffffffu, node >= 0), held = (1u << from) - 1u;
-  if (fresh == 0) return;
-  int nodes[8];  // of the half warp's rows
+  if (!__syncthreads_or(what == kFresh)) return;
+  const Lane plain = lane_of<true>(l16, 0);
+  const int64_t ld = (int64_t)Hkv * kD, at_slot = (crow + hw) * ld;
+  const int groups = (Hkv + kHeads - 1) / kHeads;
+  int buf = 0;
+  for (int item = blockIdx.y; item < A.layers * 2 * groups; item += gridDim.y) {
+    const int l = item / (2 * groups), kv = item / groups & 1, h = item % groups * kHeads;
+    const uint16_t* in = (kv ? A.tree_v : A.tree_k) + (((int64_t)l * A.batch + b) * A.n_max + node) * ld;
+    uint8_t* base = static_cast<uint8_t*>(kv ? A.caches.v[l] : A.caches.k[l]) + at_slot;
+    float* scales = (kv ? A.scales.v[l] : A.scales.k[l]) + place * Hkv;
+    Raw x[kHeads];
+    float old[kHeads], y[kHeads][8];
+    uint8_t* codes[kHeads];
+    float* scale[kHeads];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) nodes[j] = __shfl_sync(0xffffffffu, node, 2 * j + (lane >> 4));
-  const Lane plain = lane_of<true>(lane & 15, 0);
-  const int64_t ld = (int64_t)Hkv * kD;
-  const int total = A.layers * 2 * Hkv;
-  for (int item = blockIdx.y * kWarps + warp; item < total; item += gridDim.y * kWarps) {
-    const int l = item / (2 * Hkv), h = item % (2 * Hkv);
-    const bool is_v = h >= Hkv;
-    const int hh = is_v ? h - Hkv : h;
-    const uint16_t* tree = (is_v ? A.tree_v : A.tree_k) + ((int64_t)l * A.batch + b) * A.n_max * ld + hh * kD;
-    uint8_t* codes = static_cast<uint8_t*>(is_v ? A.caches.v[l] : A.caches.k[l]) + crow * ld + hh * kD;
-    float* scale = (is_v ? A.scales.v[l] : A.scales.k[l]) + place * Hkv + hh;
-    auto src = [&](int t) { return tree + nodes[t >> 1] * ld; };
-    quantise_head<true, false>(src, fresh, held, codes, ld, scale, plain, nullptr, false, 0.f, nullptr, lane);
+    for (int u = 0; u < kHeads; ++u) {
+      const bool is = h + u < Hkv;
+      codes[u] = is ? base + (h + u) * kD : nullptr;
+      scale[u] = scales + h + u;
+      x[u] = load_slot(is ? what : kNone, in + (h + u) * kD, codes[u], plain);
+      old[u] = is && from > 0 ? *scale[u] : 1.f;
+    }
+#pragma unroll
+    for (int u = 0; u < kHeads; ++u) value_of(x[u], what, old[u], y[u]);
+    quantise(y, what, codes, scale, old, plain, part[buf], hw, l16);
+    buf ^= 1;
   }
 }
 
@@ -439,10 +490,9 @@ cudaError_t launch_append8(const RopeArgs& args, float* k_scale, float* v_scale,
   while (a.range < kBlk && (int64_t)2 * a.range * args.batch <= args.rows) a.range *= 2;
   const int64_t ctas = ((int64_t)args.rows + a.range - 1) / a.range;
   // few blocks: their heads in parts
-  const int64_t want = (int64_t)num_sms() * 2;
-  const int most = (2 * args.heads_kv + kWarps - 1) / kWarps;
-  int parts = (int)((want + ctas - 1) / ctas);
-  if (parts > most) parts = most;
+  const int64_t want = (int64_t)num_sms() * 3;
+  const int most = std::max((args.heads_kv + kHeads - 1) / kHeads, (args.heads_q + 7) / 8);
+  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(want / ctas, most));
   auto kernel = args.rope.style == 1 ? append8_kernel<true> : append8_kernel<false>;
   return launch_pdl(kernel, dim3((unsigned)ctas, (unsigned)parts), dim3(kThreads), 0, s, a);
 }
@@ -466,8 +516,7 @@ cudaError_t launch_paths8(int layers, const LayerPtrs& caches, const LayerScales
   a.cache_len = cache_len;
   a.err = err;
   const int blocks = (block + 1 + kBlk - 2) / kBlk + 1;
-  const int items = layers * 2 * kv.heads_kv;
-  const int parts = (items + kWarps - 1) / kWarps;
+  const int parts = layers * 2 * ((kv.heads_kv + kHeads - 1) / kHeads);
   return launch_pdl(paths8_kernel, dim3((unsigned)(batch * blocks), (unsigned)(parts < 65535 ? parts : 65535)),
                     dim3(kThreads), 0, s, a);
 }

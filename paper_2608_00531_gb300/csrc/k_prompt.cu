@@ -77,7 +77,7 @@ constexpr int kOffPrefix = kOffPieces + (kPieces + 2) * kPieceInts * 4;  // int6
 constexpr int kSmemBytes = kOffPrefix + 8 * (kAttnMaxBatch + 1);
 static_assert(kSmemBytes <= 232448, "fits the 227 KiB opt-in");
 struct Lay {  // where the pieces lie, for what prompt_units.cuh shares
-  static constexpr int pieces = kOffPieces, prefix = kOffPrefix, piece_bar = B_PIECE, taken_bar = B_TAKEN;
+  static constexpr int m_tiles = 2, threads = kThreads, pieces = kOffPieces, prefix = kOffPrefix, piece_bar = B_PIECE, taken_bar = B_TAKEN;
 };
 
 // The products of a tile and one M tile, issued by a lane that is elected once for them

@@ -31,44 +31,51 @@
 // tile (single tokens, small trees) takes its tiles in turn with both softmax groups, each
 // with an O and sums of its own, which the epilogue adds up: a group's exponentials would
 // otherwise take longer than a tile's bytes.
-#include "prompt_units.cuh"
+#include "prompt8.cuh"
 
 namespace cure {
 namespace {
 
 using namespace prompt;
 
-constexpr int NK = 3, NV = 2, NW = 2;   // stages: K tiles, V tiles, V tiles in fp16
 constexpr int kBlk = CURE_KV8_BLOCK;
 constexpr int kBlocks = BN / kBlk;      // of a tile
 constexpr int kTile = BN * D;           // 16 KiB of codes
 constexpr int kTileW = kTile * 2;
-constexpr int kScaleSlots = 8;          // tiles whose scales lie in shared memory
-constexpr int kOffQ = 0;                       // Q[m][part]
-constexpr int kOffK = kOffQ + 4 * kQHalf;      // K[stage]
-constexpr int kOffV = kOffK + NK * kTile;      // V[stage]
-constexpr int kOffW = kOffV + NV * kTile;      // V in fp16[stage]: chunks of 16 keys, [d half][16 keys][64 d]
-constexpr int kOffMisc = kOffW + NW * kTileW;
-enum {
-  B_QFULL = 0, B_QEMPTY, B_SFREE, B_KFULL, B_KEMPTY = B_KFULL + NK, B_VFULL = B_KEMPTY + NK, B_VEMPTY = B_VFULL + NV,
-  B_WFULL = B_VEMPTY + NV, B_WEMPTY = B_WFULL + NW, B_SFULL = B_WEMPTY + NW, B_PFULL = B_SFULL + 2,
-  B_PVDONE = B_PFULL + 2, B_STAT = B_PVDONE + 2, B_OFREE = B_STAT + 2, B_DRAIN = B_OFREE + 2, B_JOIN = B_DRAIN + 2,
-  B_PIECE = B_JOIN + 1, B_TAKEN = B_PIECE + kPieces, kNumBars = B_TAKEN + kPieces
-};
-constexpr int kOffTmemSlot = kOffMisc + 8 * kNumBars;
-constexpr int kOffAbort = kOffTmemSlot + 4;
-constexpr int kOffJoins = kOffAbort + 4;                        // units that this CTA joins at its end
-constexpr int kOffPieces = (kOffJoins + 4 + 15) / 16 * 16;      // int [kPieces][kPieceInts], then [2] to join
-constexpr int kOffPrefix = kOffPieces + (kPieces + 2) * kPieceInts * 4;  // int64 first position of each sequence [B+1]
-constexpr int kOffScales = (kOffPrefix + 8 * (kAttnMaxBatch + 1) + 15) / 16 * 16;  // float [slot][ks, log2 vs, 1 / vs][8]
-constexpr int kOffQScale = kOffScales + kScaleSlots * 3 * kBlocks * 4;  // float [piece % 2][m][row]
-constexpr int kOffInv = kOffQScale + 4 * BM * 4;                // float [group][row]: reciprocal row sums
-constexpr int kOffLse = kOffInv + 2 * BM * 4;                   // float [group][row]: base-2 log-sum-exps
-constexpr int kOffKept = kOffLse + 2 * BM * 4;                  // the epilogue's piece, a copy for each of its warps
-constexpr int kSmemBytes = kOffKept + 4 * kPieceInts * 4;
-static_assert(kSmemBytes <= 232448, "fits the 227 KiB opt-in");
-struct Lay {  // where the pieces lie, for what prompt_units.cuh shares
-  static constexpr int pieces = kOffPieces, prefix = kOffPrefix, piece_bar = B_PIECE, taken_bar = B_TAKEN;
+constexpr int kQuad = 4;                // tiles whose pages and scales are looked up together
+constexpr int kScaleSlots = 8;          // quads whose scales lie in shared memory
+constexpr int kScaleFloats = 3 * kBlocks * 2;  // of a tile, each twice (pairs for packed arithmetic)
+
+// Shared memory and barriers of the kernel for units of MT M tiles.  With one, Q takes half
+// the place, and two more tiles are on their way.
+template <int MT>
+struct Layout {
+  static constexpr int m_tiles = MT, threads = kThreads;
+  static constexpr int NK = MT == 1 ? 4 : 3, NV = MT == 1 ? 3 : 2, NW = 2;  // stages: K tiles, V tiles, V tiles in fp16
+  enum : int {
+    B_QFULL = 0, B_QEMPTY, B_SFREE, B_KFULL, B_KEMPTY = B_KFULL + NK, B_VFULL = B_KEMPTY + NK, B_VEMPTY = B_VFULL + NV,
+    B_WFULL = B_VEMPTY + NV, B_WEMPTY = B_WFULL + NW, B_SFULL = B_WEMPTY + NW, B_PFULL = B_SFULL + 2,
+    B_PVDONE = B_PFULL + 2, B_STAT = B_PVDONE + 2, B_OFREE = B_STAT + 2, B_DRAIN = B_OFREE + 2, B_JOIN = B_DRAIN + 2,
+    B_SCALES = B_JOIN + 1, piece_bar = B_SCALES + kScaleSlots, taken_bar = piece_bar + kPieces,
+    num_bars = taken_bar + kPieces
+  };
+  static constexpr int q = 0;                        // Q[m][part]
+  static constexpr int k = q + MT * 2 * kQHalf;      // K[stage]
+  static constexpr int v = k + NK * kTile;           // V[stage]
+  static constexpr int w = v + NV * kTile;           // V in fp16[stage]: chunks of 16 keys, [d half][16 keys][64 d]
+  static constexpr int bars = w + NW * kTileW;
+  static constexpr int tmem_slot = bars + 8 * num_bars;
+  static constexpr int abort = tmem_slot + 4;
+  static constexpr int joins = abort + 4;                      // units that this CTA joins at its end
+  static constexpr int pieces = (joins + 4 + 15) / 16 * 16;    // int [kPieces][kPieceInts], then [2] to join
+  static constexpr int prefix = pieces + (kPieces + 2) * kPieceInts * 4;  // int64 first position of each sequence [B+1]
+  static constexpr int scales = (prefix + 8 * (kAttnMaxBatch + 1) + 15) / 16 * 16;  // float [slot][tile][ks, log2 vs, 1 / vs][8][2]
+  static constexpr int q_scale = scales + kScaleSlots * kQuad * kScaleFloats * 4;   // float [piece % 2][m][row]
+  static constexpr int inv = q_scale + 4 * BM * 4;             // float [group][row]: reciprocal row sums
+  static constexpr int lse = inv + 2 * BM * 4;                 // float [group][row]: base-2 log-sum-exps
+  static constexpr int kept = lse + 2 * BM * 4;                // the epilogue's piece, a copy for each of its warps
+  static constexpr int bytes = kept + 4 * kPieceInts * 4;
+  static_assert(bytes <= 232448, "fits the 227 KiB opt-in");
 };
 
 struct Args8 : PromptArgs {
@@ -107,6 +114,11 @@ __device__ __forceinline__ uint32_t narrow(uint32_t lo, uint32_t hi) {
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
 __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
@@ -160,12 +172,27 @@ __host__ __device__ constexpr uint32_t idesc_0(int M, int N, bool b_mn_major) {
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+// Whether the phase of the given parity is over, for all lanes of a warp (no waiting).
+__device__ __forceinline__ bool test_warp(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return __all_sync(0xffffffffu, ok != 0);
+}
+
 constexpr float kLift = 7.f;  // P' is 2^kLift times what it stands for: at most 2^15 with the lag of 2^8
 
-template <class Args>
+template <class Args, int MT>
 __global__ void __launch_bounds__(kThreads, 1)
 attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Args A) {
   constexpr bool kTree = Args::kTree;
+  using Lay = Layout<MT>;
+  constexpr int NK = Lay::NK, NV = Lay::NV, NW = Lay::NW;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sb = smem_u32(smem);
@@ -174,49 +201,50 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     return;
   }
   const int G = A.G, npb = BM / G;
-  const Bar bar{sb + kOffMisc};
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + kOffAbort);
-  const uint32_t aborted = sb + kOffAbort;
-  volatile int* n_joins = reinterpret_cast<volatile int*>(smem + kOffJoins);
-  float* q_scale = reinterpret_cast<float*>(smem + kOffQScale);
-  float* row_inv = reinterpret_cast<float*>(smem + kOffInv);
-  float* lse_of = reinterpret_cast<float*>(smem + kOffLse);
+  const Bar bar{sb + Lay::bars};
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + Lay::abort);
+  const uint32_t aborted = sb + Lay::abort;
+  volatile int* n_joins = reinterpret_cast<volatile int*>(smem + Lay::joins);
+  float* q_scale = reinterpret_cast<float*>(smem + Lay::q_scale);
+  float* row_inv = reinterpret_cast<float*>(smem + Lay::inv);
+  float* lse_of = reinterpret_cast<float*>(smem + Lay::lse);
 
   // ---------------------------------------------------------------- set-up
   if (tid == 0) {
-    mbar_init(bar(B_QFULL), BM);
-    mbar_init(bar(B_QEMPTY), 1);
-    mbar_init(bar(B_SFREE), BM);
+    mbar_init(bar(Lay::B_QFULL), BM);
+    mbar_init(bar(Lay::B_QEMPTY), 1);
+    mbar_init(bar(Lay::B_SFREE), BM);
     for (int i = 0; i < NK; ++i) {
-      mbar_init(bar(B_KFULL + i), 1);
-      mbar_init(bar(B_KEMPTY + i), 1);
+      mbar_init(bar(Lay::B_KFULL + i), 1);
+      mbar_init(bar(Lay::B_KEMPTY + i), 1);
     }
     for (int i = 0; i < NV; ++i) {
-      mbar_init(bar(B_VFULL + i), 1);
-      mbar_init(bar(B_VEMPTY + i), 4);
+      mbar_init(bar(Lay::B_VFULL + i), 1);
+      mbar_init(bar(Lay::B_VEMPTY + i), 4);
     }
     for (int i = 0; i < NW; ++i) {
-      mbar_init(bar(B_WFULL + i), 4);
-      mbar_init(bar(B_WEMPTY + i), 1);
+      mbar_init(bar(Lay::B_WFULL + i), 4);
+      mbar_init(bar(Lay::B_WEMPTY + i), 1);
     }
     for (int m = 0; m < 2; ++m) {
-      mbar_init(bar(B_SFULL + m), 1);
-      mbar_init(bar(B_PFULL + m), BM);
-      mbar_init(bar(B_PVDONE + m), 1);
-      mbar_init(bar(B_STAT + m), BM);
-      mbar_init(bar(B_OFREE + m), BM);
-      mbar_init(bar(B_DRAIN + m), 1);
+      mbar_init(bar(Lay::B_SFULL + m), 1);
+      mbar_init(bar(Lay::B_PFULL + m), BM);
+      mbar_init(bar(Lay::B_PVDONE + m), 1);
+      mbar_init(bar(Lay::B_STAT + m), BM);
+      mbar_init(bar(Lay::B_OFREE + m), BM);
+      mbar_init(bar(Lay::B_DRAIN + m), 1);
     }
-    mbar_init(bar(B_JOIN), BM);
+    mbar_init(bar(Lay::B_JOIN), BM);
+    for (int i = 0; i < kScaleSlots; ++i) mbar_init(bar(Lay::B_SCALES + i), 1);
     for (int i = 0; i < kPieces; ++i) {
-      mbar_init(bar(B_PIECE + i), 1);
-      mbar_init(bar(B_TAKEN + i), kTakers);
+      mbar_init(bar(Lay::piece_bar + i), 1);
+      mbar_init(bar(Lay::taken_bar + i), kTakers);
     }
     *abort_flag = 0;
     *n_joins = 0;
     fence_mbar_init();
   }
-  if (warp == 0) tmem_alloc(sb + kOffTmemSlot, kTmemCols);
+  if (warp == 0) tmem_alloc(sb + Lay::tmem_slot, kTmemCols);
   if (warp == 8 && lane == 0) {
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
@@ -225,33 +253,33 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmemSlot);
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + Lay::tmem_slot);
   Await<false> await;
   Pieces pieces{0};
   Piece x;
   // Whether a piece has rows in both M tiles; else both softmax groups take M tile 0's, a tile each in turn.
-  auto two_tiles = [&](const Piece& x) { return (2 * x.rg + 1) * npb < x.n; };
+  auto two_tiles = [&](const Piece& x) { return MT == 2 && (2 * x.rg + 1) * npb < x.n; };
 
   // (128 * (2 * 160 + 96 + 96) = 512 * 128 registers, what the block was launched with)
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     // ================================================================ softmax
     const int m = warp >> 2;
     const int row = tid & 127;  // row within the M tile = TMEM lane
     const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t tS = tl + kColS, tP = tl + kColP + m * 64, tO = tl + kColO + m * D;
-    uint32_t sc = 0, tiles = 0, pc = 0;  // tiles of this group, tiles and pieces of the CTA
+    uint32_t sc = 0, quads = 0, pc = 0;  // tiles of this group, quads and pieces of the CTA
     bool ok = true;
     uint32_t done = 0;  // pieces of this group
     while (ok && pieces.next<Lay>(await, bar, smem, aborted, x)) {
-      const uint32_t tile0 = tiles;
-      tiles += (uint32_t)(x.t1 - x.t0);
+      const uint32_t at = quads * kQuad;  // the piece's first place among the scales
+      quads += (uint32_t)(x.t1 - x.t0 + kQuad - 1) / kQuad;
       const bool two = two_tiles(x);
       const int mq = two ? m : 0, step = two ? 1 : 2;  // the M tile whose rows these are
       const int first = x.t0 + m - mq;
       const float* qs = q_scale + ((pc++ & 1u) * 2 + mq) * BM + row;
       if (first >= x.t1) continue;
-      const int i0 = (2 * x.rg + mq) * npb;
+      const int i0 = (MT * x.rg + mq) * npb;
       const int i = i0 + row / G;  // the row's place in its sequence
       const bool idle = (warp & 3) * 32 >= min(npb, x.n - i0) * G;  // no row of the warp is one of the sequence's
       // keys that the row sees (a tree's: at most), the fewest and the most that a row of this warp sees
@@ -259,13 +287,13 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       const int least = kTree ? x.L : __shfl_sync(0xffffffffu, sees, 0), most = __shfl_sync(0xffffffffu, sees, 31);
       float m_run = -INFINITY, l_run = 0.f, c = 0.f;
       for (int t = first; t < x.t1; t += step) {
-        if (!await(bar(B_SFULL + m), sc & 1u, aborted)) { ok = false; break; }
+        if (!await(bar(Lay::B_SFULL + m), sc & 1u, aborted)) { ok = false; break; }
         ++sc;
         tc_fence_after();
         if (idle) {  // its rows of P' and O may hold anything
-          mbar_arrive(bar(B_SFREE));
-          if (sc > 1 && !await(bar(B_PVDONE + m), (sc - 2) & 1u, aborted)) { ok = false; break; }
-          mbar_arrive(bar(B_PFULL + m));
+          mbar_arrive(bar(Lay::B_SFREE));
+          if (sc > 1 && !await(bar(Lay::B_PVDONE + m), (sc - 2) & 1u, aborted)) { ok = false; break; }
+          mbar_arrive(bar(Lay::B_PFULL + m));
           continue;
         }
         uint32_t v[4][32];
@@ -273,23 +301,25 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         for (int q = 0; q < 4; ++q) tmem_ld32(tS + 32 * q, v[q]);
         tmem_wait_ld();
         tc_fence_before();
-        mbar_arrive(bar(B_SFREE));  // the next product may take S
-        if (t == first) c = A.scale_log2 * *qs;
-        // (a tile's scales stay until the eighth tile behind it, which is loaded after this one's softmax)
+        mbar_arrive(bar(Lay::B_SFREE));  // the next product may take S
+        // (within bounds where a block's factor is never 0, which would meet -infinity)
+        if (t == first) c = fminf(fmaxf(A.scale_log2 * *qs, 0x1p-80f), 0x1p80f);
+        // The tile's scales (the S product has waited for them).  They stay for as long as it takes: their
+        // slot is written again for the eighth quad from here, once S of all but its last three tiles is done.
         const float4* scales =
-            reinterpret_cast<const float4*>(smem + kOffScales + ((tile0 + (uint32_t)(t - x.t0)) % kScaleSlots) * (3 * kBlocks * 4));
+            reinterpret_cast<const float4*>(smem + Lay::scales + (at + (uint32_t)(t - x.t0)) % (kScaleSlots * kQuad) * (kScaleFloats * 4));
         float x_[BN];
 #pragma unroll
         for (int k = 0; k < BN; ++k) x_[k] = __uint_as_float(v[k >> 5][k & 31]);
         if ((t + 1) * BN > least) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const int at = t * BN + 32 * q;  // the block's first key
-            if (at + 32 > least) {
-              const int left = min(max(sees - at, 0), 32);  // keys of the block that the row sees
+            const int key = t * BN + 32 * q;  // the block's first
+            if (key + 32 > least) {
+              const int left = min(max(sees - key, 0), 32);  // keys of the block that the row sees
               uint32_t seen = left == 32 ? 0xffffffffu : (1u << left) - 1u;
               if constexpr (kTree) {
-                const int words = 2 * ((A.n_max + 63) / 64), base = at - x.L;  // the node of the block's first key
+                const int words = 2 * ((A.n_max + 63) / 64), base = key - x.L;  // the node of the block's first key
                 const uint32_t* anc = reinterpret_cast<const uint32_t*>(A.anc) + (int64_t)(x.r0 + i) * words;
                 auto word = [&](int k) -> uint32_t { return i < x.n && k < words ? __ldg(anc + k) : 0u; };
                 seen &= base >= 0 ? __funnelshift_r(word(base >> 5), word((base >> 5) + 1), base & 31)
@@ -300,23 +330,21 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             }
           }
         }
-        // the maximum of s + log2 vs: of each block's scores first (a factor never 0: it meets -infinity)
+        // the maximum of s + log2 vs, from each block's largest score
         float mt = -INFINITY;
+        auto largest = [&](int b) -> float {
+          const float* y = x_ + b * kBlk;
+          float a0 = fmax3(y[0], y[1], y[2]), a1 = fmax3(y[3], y[4], y[5]);
+          a0 = fmax3(a0, y[6], y[7]);
+          a1 = fmax3(a1, y[8], y[9]);
+          a0 = fmax3(a0, y[10], y[11]);
+          a1 = fmax3(a1, y[12], y[13]);
+          return fmax3(fmaxf(a0, a1), y[14], y[15]);
+        };
 #pragma unroll
-        for (int b = 0; b < kBlocks; b += 4) {
-          const float4 ks = scales[b / 4], lv = scales[kBlocks / 4 + b / 4];
-          const float k4[4] = {ks.x, ks.y, ks.z, ks.w}, l4[4] = {lv.x, lv.y, lv.z, lv.w};
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const float* y = x_ + (b + u) * kBlk;
-            float a0 = fmax3(y[0], y[1], y[2]), a1 = fmax3(y[3], y[4], y[5]);
-            a0 = fmax3(a0, y[6], y[7]);
-            a1 = fmax3(a1, y[8], y[9]);
-            a0 = fmax3(a0, y[10], y[11]);
-            a1 = fmax3(a1, y[12], y[13]);
-            a0 = fmax3(a0, y[14], y[15]);
-            mt = fmaxf(mt, fmaf(fmaxf(a0, a1), fmaxf(c * k4[u], FLT_MIN), l4[u]));
-          }
+        for (int b = 0; b < kBlocks; b += 2) {
+          const float4 ks = scales[b / 2], lv = scales[kBlocks / 2 + b / 2];
+          mt = fmax3(mt, fmaf(largest(b), c * ks.x, lv.x), fmaf(largest(b + 1), c * ks.z, lv.z));
         }
         const float m_new = fmaxf(m_run, mt);
         const bool need = m_new > m_run + 8.0f;
@@ -324,31 +352,28 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         if (need) m_run = m_new;
         // P's place and O are free once this group's PV product before is done
         if (sc > 1) {
-          if (!await(bar(B_PVDONE + m), (sc - 2) & 1u, aborted)) { ok = false; break; }
+          if (!await(bar(Lay::B_PVDONE + m), (sc - 2) & 1u, aborted)) { ok = false; break; }
           tc_fence_after();
         }
         const float nbase = m_run == -INFINITY ? 0.f : kLift - m_run;
         uint64_t sum = f2_pack(0.f, 0.f);
+        const uint64_t cc = f2_pack(c, c), nn = f2_pack(nbase, nbase);
         auto exponentials = [&](int q) {  // of 32 keys
+          const float4 ks = scales[q], lv = scales[kBlocks / 2 + q], iv = scales[kBlocks + q];
+          const uint64_t c2[2] = {f2_mul(cc, f2_pack(ks.x, ks.y)), f2_mul(cc, f2_pack(ks.z, ks.w))};
+          const uint64_t nb2[2] = {f2_add(nn, f2_pack(lv.x, lv.y)), f2_add(nn, f2_pack(lv.z, lv.w))};
           uint32_t pk[16];
+          uint64_t part[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int b = 2 * q + u;
-            const float cb = fmaxf(c * reinterpret_cast<const float*>(scales)[b], FLT_MIN);
-            const float lv = reinterpret_cast<const float*>(scales)[kBlocks + b];
-            const float iv = reinterpret_cast<const float*>(scales)[2 * kBlocks + b];
-            const uint64_t c2 = f2_pack(cb, cb), nb2 = f2_pack(nbase + lv, nbase + lv);
-            uint64_t part = f2_pack(0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              float a0, a1;
-              f2_unpack(f2_fma(f2_pack(x_[16 * b + 2 * k], x_[16 * b + 2 * k + 1]), c2, nb2), a0, a1);
-              const float p0 = ex2(a0), p1 = ex2(a1);
-              part = f2_add(part, f2_pack(p0, p1));
-              pk[8 * u + k] = pack_f16(p0, p1);
-            }
-            sum = f2_fma(part, f2_pack(iv, iv), sum);
+          for (int k = 0; k < 16; ++k) {
+            const int u = k >> 3;
+            float a0, a1;
+            f2_unpack(f2_fma(f2_pack(x_[32 * q + 2 * k], x_[32 * q + 2 * k + 1]), c2[u], nb2[u]), a0, a1);
+            const float p0 = ex2(a0), p1 = ex2(a1);
+            part[u] = f2_add(part[u], f2_pack(p0, p1));
+            pk[k] = pack_f16(p0, p1);
           }
+          sum = f2_fma(part[0], f2_pack(iv.x, iv.y), f2_fma(part[1], f2_pack(iv.z, iv.w), sum));
           tmem_st16(tP + 16 * q, pk);
         };
         exponentials(0);
@@ -377,14 +402,14 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         }
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(bar(B_PFULL + m));
+        mbar_arrive(bar(Lay::B_PFULL + m));
       }
       if (!ok) break;
       // What the epilogue needs to know of the row, once it is done with the piece before.
-      if (done > 0 && !await(bar(B_OFREE + m), (done - 1) & 1u, aborted)) break;
+      if (done > 0 && !await(bar(Lay::B_OFREE + m), (done - 1) & 1u, aborted)) break;
       row_inv[m * BM + row] = l_run > 0.f ? 1.f / l_run : 0.f;
       lse_of[m * BM + row] = row_lse(m_run - kLift, l_run);
-      mbar_arrive(bar(B_STAT + m));
+      mbar_arrive(bar(Lay::B_STAT + m));
       ++done;
     }
   } else if (warp >= 12) {
@@ -395,22 +420,22 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
     uint32_t done0 = 0, done1 = 0, tiles0 = 0, tiles1 = 0, joins = 0, pc = 0, vt = 0;
     bool ok = true, have = false;
-    Piece* kept = reinterpret_cast<Piece*>(smem + kOffKept) + (warp & 3);  // (registers are short)
+    Piece* kept = reinterpret_cast<Piece*>(smem + Lay::kept) + (warp & 3);  // (registers are short)
     // The epilogue's threads meet (an mbarrier, for a wait that ends when the CTA gives up).
     auto meet = [&]() -> bool {
-      mbar_arrive(bar(B_JOIN));
-      return ok = await(bar(B_JOIN), joins++ & 1u, aborted);
+      mbar_arrive(bar(Lay::B_JOIN));
+      return ok = await(bar(Lay::B_JOIN), joins++ & 1u, aborted);
     };
     while (ok) {
       const bool more = pieces.next<Lay>(await, bar, smem, aborted, x);
       if (!more && !have) break;
       if (more) {
         // ---- Q of the piece, once the S products of the one before are done
-        if (!await(bar(B_QEMPTY), (pc & 1u) ^ 1u, aborted)) break;
+        if (!await(bar(Lay::B_QEMPTY), (pc & 1u) ^ 1u, aborted)) break;
         const int mts = two_tiles(x) ? 2 : 1;
 #pragma unroll 1
         for (int m = 0; m < mts; ++m) {
-          const int i = (2 * x.rg + m) * npb + row / G;
+          const int i = (MT * x.rg + m) * npb + row / G;
           uint4 w[16];
           if (row < npb * G && i < x.n) {
             const uint4* src =
@@ -435,7 +460,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           const int e = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -60), 120);
           q_scale[((pc & 1u) * 2 + m) * BM + row] = __uint_as_float((uint32_t)(127 + e) << 23);
           const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-          const uint32_t dst = sb + kOffQ + m * 2 * kQHalf + row * 128;
+          const uint32_t dst = sb + Lay::q + m * 2 * kQHalf + row * 128;
 #pragma unroll
           for (int u = 0; u < 8; ++u) {  // 16 dims
             const uint32_t in[8] = {w[2 * u].x,     w[2 * u].y,     w[2 * u].z,     w[2 * u].w,
@@ -458,7 +483,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           }
         }
         fence_proxy_async_smem();
-        mbar_arrive(bar(B_QFULL));
+        mbar_arrive(bar(Lay::B_QFULL));
         ++pc;
       }
       for (int t = more ? x.t0 : 0, t_end = more ? x.t1 : 1; ok && t < t_end; ++t) {
@@ -466,28 +491,29 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           // ---- a V tile to fp16: 16 codes a load; keys behind the unit's last one count as zeros,
           // so that what lies there cannot reach O through 0 * NaN
           const uint32_t vs = vt % NV, ws = vt % NW;
-          if (!await(bar(B_VFULL + vs), (vt / NV) & 1u, aborted) ||
-              !await(bar(B_WEMPTY + ws), ((vt / NW) & 1u) ^ 1u, aborted)) {
+          if (!await(bar(Lay::B_VFULL + vs), (vt / NV) & 1u, aborted) ||
+              !await(bar(Lay::B_WEMPTY + ws), ((vt / NW) & 1u) ^ 1u, aborted)) {
             ok = false;
             break;
           }
           ++vt;
-          const uint32_t src = sb + kOffV + vs * kTile + row * 16;
+          // A lane's 16 dims of keys 16 j + key.  Eight lanes take 64 dims of each of two keys whose
+          // numbers differ by 5: in the swizzled tiles their loads then lie on all banks (bit 2), and
+          // so do their stores, every second unit of a key (bit 0).
+          const int hf = (row >> 3) & 1, s4 = row & 3, key = ((row >> 4) * 2) ^ ((row >> 2) & 1 ? 5 : 0);
+          const uint32_t src = sb + Lay::v + vs * kTile + key * D + (((hf * 4 + s4) ^ (key & 7)) << 4);
           uint4 w[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) w[j] = ld_shared_v4(src + j * 2048);
+          for (int j = 0; j < 8; ++j) w[j] = ld_shared_v4(src + j * (16 * D));
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(B_VEMPTY + vs));
-          const int valid = x.keys - t * BN, key = row >> 3, seg = row & 7;  // keys 16 j + key, dims 16 seg ..
+          if (lane == 0) mbar_arrive(bar(Lay::B_VEMPTY + vs));
+          const int valid = x.keys - t * BN;
           if (valid < BN) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
               if (16 * j + key >= valid) w[j] = make_uint4(0u, 0u, 0u, 0u);
           }
-          // The two 16-byte units of a lane, the second first in the second half of the dims
-          // (the halves lie 2 KiB apart, on the same banks).
-          const int hf = seg >> 2, u0 = ((seg & 3) * 2 + hf) ^ (key & 7), u1 = ((seg & 3) * 2 + 1 - hf) ^ (key & 7);
-          const uint32_t dst = sb + kOffW + ws * kTileW + hf * kVHalf + key * 128;
+          const uint32_t dst = sb + Lay::w + ws * kTileW + hf * kVHalf + key * 128, u0 = (uint32_t)((2 * s4) ^ (key & 7)) << 4;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             uint32_t a[8];
@@ -496,12 +522,12 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             widen(w[j].z, a[4], a[5]);
             widen(w[j].w, a[6], a[7]);
             const uint32_t to = dst + j * kVChunk;
-            st_shared_v4(to + (u0 << 4), hf ? a[4] : a[0], hf ? a[5] : a[1], hf ? a[6] : a[2], hf ? a[7] : a[3]);
-            st_shared_v4(to + (u1 << 4), hf ? a[0] : a[4], hf ? a[1] : a[5], hf ? a[2] : a[6], hf ? a[3] : a[7]);
+            st_shared_v4(to + u0, a[0], a[1], a[2], a[3]);
+            st_shared_v4(to + (u0 ^ 16), a[4], a[5], a[6], a[7]);
           }
           fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(B_WFULL + ws));
+          if (lane == 0) mbar_arrive(bar(Lay::B_WFULL + ws));
         }
         if (!have) continue;
         // ---- the piece before: its rows
@@ -515,15 +541,15 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
 #pragma unroll 1
         for (int m = 0; m < (two ? 2 : 1); ++m) {
           // STAT first: the softmax has then seen all PV products but the last
-          if (!await(bar(B_STAT + m), (m ? done1++ : done0++) & 1u, aborted) ||
-              !await(bar(B_PVDONE + m), ((m ? tiles1 : tiles0) - 1) & 1u, aborted)) {
+          if (!await(bar(Lay::B_STAT + m), (m ? done1++ : done0++) & 1u, aborted) ||
+              !await(bar(Lay::B_PVDONE + m), ((m ? tiles1 : tiles0) - 1) & 1u, aborted)) {
             ok = false;
             break;
           }
           float f0 = row_inv[m * BM + row], f1 = 0.f, lse = lse_of[m * BM + row];
           if (both) {
-            if (!await(bar(B_STAT + 1), done1++ & 1u, aborted) ||
-                !await(bar(B_PVDONE + 1), (tiles1 - 1) & 1u, aborted)) {
+            if (!await(bar(Lay::B_STAT + 1), done1++ & 1u, aborted) ||
+                !await(bar(Lay::B_PVDONE + 1), (tiles1 - 1) & 1u, aborted)) {
               ok = false;
               break;
             }
@@ -534,7 +560,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             lse = top + log2f(w0 + w1);
           }
           tc_fence_after();
-          const int i = (2 * prev.rg + m) * npb + row / G;
+          const int i = (MT * prev.rg + m) * npb + row / G;
           const bool vrow = row < npb * G && i < prev.n;
           uint16_t* orow = A.out + ((int64_t)(prev.r0 + i) * A.heads_q + prev.h * G + row % G) * D;
           float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + m * BM + row;
@@ -569,16 +595,16 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             }
           }
           tc_fence_before();
-          mbar_arrive(bar(B_OFREE + m));
-          if (both) mbar_arrive(bar(B_OFREE + 1));
+          mbar_arrive(bar(Lay::B_OFREE + m));
+          if (both) mbar_arrive(bar(Lay::B_OFREE + 1));
         }
         if (!ok || whole) continue;
         // The CTA whose part arrives last joins the unit when its own pieces are done.
         __threadfence();
         if (!meet()) break;
-        if (tid == 12 * 32 && !*abort_flag && arrive(A.cnt + prev.o0, A.tag) == prev.parts) {
+        if (tid == 12 * 32 && !*abort_flag && arrive_at(A.cnt + prev.o0, A.tag) == prev.parts) {
           A.cnt[prev.o0] = 0;  // a completed unit leaves a zero word behind
-          *reinterpret_cast<Piece*>(smem + kOffPieces + (kPieces + *n_joins) * (kPieceInts * 4)) = prev;
+          *reinterpret_cast<Piece*>(smem + Lay::pieces + (kPieces + *n_joins) * (kPieceInts * 4)) = prev;
           *n_joins = *n_joins + 1;
         }
       }
@@ -589,17 +615,20 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       have = true;
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 8) {
       // ================================================================ producer
       const int ps = A.kv.page_size;
       const bool paged = A.kv.layout == 1;
       const int ppt = paged ? BN / ps : 0;  // pages (boxes) of a tile: 2 .. 8
-      uint32_t kt = 0, vt = 0;              // tiles issued
+      uint32_t kt = 0, vt = 0, quads = 0;   // tiles issued, quads whose scales are out
       while (pieces.next<Lay>(await, bar, smem, aborted, x)) {
-        auto page_of = [&](int t) -> int {  // lane p: page p of tile t; a missing one reads zeros
-          const int tok = t * BN + lane * ps;
-          if (lane >= ppt || t >= x.t1 || tok >= x.keys) return -1;
+        // Pages and scales are looked up a quad of tiles at a time, two quads and one ahead of their
+        // use (one tile ahead, a tile took as long as a load).  Lane 8 i + p: page p of the quad's tile
+        // i (a missing one reads zeros), and the scales of its block p.
+        auto pages_of = [&](int q) -> int {
+          const int t = x.t0 + q * kQuad + (lane >> 3), p = lane & 7, tok = t * BN + p * ps;
+          if (p >= ppt || t >= x.t1 || tok >= x.keys) return -1;
           const int page = A.kv.block_table[(int64_t)x.b * A.kv.max_len + tok / ps];
           if (page < 0 || page >= A.kv.num_pages) {
             flag(A.err, CURE_DEVERR_PAGE);
@@ -607,125 +636,149 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           }
           return page;
         };
-        // lanes 0-7, 8-15: the scales of K's and V's blocks in tile t, whose pages the lanes hold
-        auto scale_of = [&](int t, int page) -> float {
-          const int blk = lane & 7, tok = t * BN + blk * kBlk;
+        auto scales_of = [&](int q, int pages) -> float2 {
+          const int t = x.t0 + q * kQuad + (lane >> 3), blk = lane & 7;
           int64_t place;
           if (paged) {
-            const int p = __shfl_sync(0xffffffffu, page, blk * kBlk / ps);
-            place = p < 0 ? -1 : (int64_t)p * (ps / kBlk) + blk * kBlk % ps / kBlk;
+            const int page = __shfl_sync(0xffffffffu, pages, (lane & 24) | (blk * kBlk / ps));
+            place = page < 0 ? -1 : (int64_t)page * (ps / kBlk) + blk * kBlk % ps / kBlk;
           } else {
             place = (int64_t)x.b * ((A.kv.max_len + kBlk - 1) / kBlk) + t * kBlocks + blk;
           }
-          if (lane >= 16 || t >= x.t1 || tok >= x.keys || place < 0) return 1.f;
-          return __ldg((lane < 8 ? A.k_scale : A.v_scale) + place * A.kv.heads_kv + x.h);
+          if (t >= x.t1 || t * BN + blk * kBlk >= x.keys || place < 0) return make_float2(1.f, 1.f);
+          return make_float2(__ldg(A.k_scale + place * A.kv.heads_kv + x.h), __ldg(A.v_scale + place * A.kv.heads_kv + x.h));
         };
-        int page_v = -1, page = page_of(x.t0), page1 = page_of(x.t0 + 1);
-        float scale = scale_of(x.t0, page);
-        for (int u = x.t0; u <= x.t1; ++u) {  // K of tile u, then V of the tile before
-          const int page2 = page_of(u + 2);
-          const float scale1 = scale_of(u + 1, page1);
-#pragma unroll 1
-          for (int kv = 0; kv < 2; ++kv) {
-            if (kv ? u == x.t0 : u == x.t1) continue;
-            const uint32_t n = kv ? vt : kt, st = kv ? n % NV : n % NK, round = kv ? n / NV : n / NK;
-            const uint32_t full = bar((kv ? B_VFULL : B_KFULL) + st), empty = bar((kv ? B_VEMPTY : B_KEMPTY) + st);
-            const uint32_t dst = sb + (kv ? kOffV : kOffK) + st * kTile;
-            if (!await(empty, (round & 1u) ^ 1u, aborted)) goto produced;
-            if (!kv && lane < 16) {
-              float* to = reinterpret_cast<float*>(smem + kOffScales) + (n % kScaleSlots) * (3 * kBlocks) + (lane & 7);
-              const float s = fminf(fmaxf(scale, 0x1p-40f), 0x1p40f);
-              if (lane < 8) {
-                to[0] = s;
-              } else {
-                to[kBlocks] = log2f(s);
-                to[2 * kBlocks] = 1.f / s;
-              }
+        const int nt = x.t1 - x.t0;
+        // of the quad before, this one (the last K tile's) and the next one
+        int pages_1 = -1, pages0 = pages_of(0), pages1 = pages_of(1);
+        float2 scales0 = scales_of(0, pages0), scales1;
+        // K and V tiles, each as soon as it has a free stage
+        for (int ik = 0, iv = 0; iv < nt;) {
+          bool is_v;
+          for (const uint32_t began = clock();;) {
+            if (ik < nt && ik < iv + NK && test_warp(bar(Lay::B_KEMPTY + kt % NK), ((kt / NK) & 1u) ^ 1u)) {
+              is_v = false;
+              break;
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive_expect_tx(full, kTile);
-            __syncwarp();
-            const CUtensorMap* map = kv ? &tm_v : &tm_k;
-            if (paged) {
-              if (lane < ppt) tma_load_4d(dst + lane * ps * D, map, full, 0, x.h, 0, kv ? page_v : page);
-            } else if (lane == 0) {
-              tma_load_4d(dst, map, full, 0, x.h, (kv ? u - 1 : u) * BN, x.b);
+            if (iv < ik && test_warp(bar(Lay::B_VEMPTY + vt % NV), ((vt / NV) & 1u) ^ 1u)) {
+              is_v = true;
+              break;
             }
-            __syncwarp();
-            if (kv) ++vt;
-            else ++kt;
+            if (__any_sync(0xffffffffu, *abort_flag != 0)) goto produced;
+            if ((uint32_t)clock() - began > (uint32_t)kWaitTimeoutCycles) *abort_flag = 1;
           }
-          page_v = page;
-          page = page1;
-          page1 = page2;
-          scale = scale1;
+          int page;
+          if (is_v) {  // (at most NK - 1 tiles behind K: in its quad or the one before)
+            page = __shfl_sync(0xffffffffu, iv / kQuad == (ik - 1) / kQuad ? pages0 : pages_1, iv % kQuad * 8 | (lane & 7));
+          } else {
+            if (ik % kQuad == 0) {
+              if (ik > 0) {
+                pages_1 = pages0;
+                pages0 = pages1;
+                scales0 = scales1;
+                pages1 = pages_of(ik / kQuad + 1);
+              }
+              scales1 = scales_of(ik / kQuad + 1, pages1);
+            }
+            page = __shfl_sync(0xffffffffu, pages0, ik % kQuad * 8 | (lane & 7));
+          }
+          const uint32_t st = is_v ? vt++ % NV : kt++ % NK;
+          const uint32_t full = bar((is_v ? Lay::B_VFULL : Lay::B_KFULL) + st);
+          const uint32_t dst = sb + (is_v ? Lay::v : Lay::k) + st * kTile;
+          if (lane == 0) mbar_arrive_expect_tx(full, kTile);
+          __syncwarp();
+          const CUtensorMap* map = is_v ? &tm_v : &tm_k;
+          if (paged) {
+            if (lane < ppt) tma_load_4d(dst + lane * ps * D, map, full, 0, x.h, 0, page);
+          } else if (lane == 0) {
+            tma_load_4d(dst, map, full, 0, x.h, (x.t0 + (is_v ? iv : ik)) * BN, x.b);
+          }
+          __syncwarp();
+          if (is_v) {
+            ++iv;
+          } else if (ik++ % kQuad == 0) {  // the quad's scales
+            float2* to = reinterpret_cast<float2*>(smem + Lay::scales) +
+                         (quads % kScaleSlots * kQuad + (lane >> 3)) * (kScaleFloats / 2) + (lane & 7);
+            const float ks = fminf(fmaxf(scales0.x, 0x1p-40f), 0x1p40f), vs = fminf(fmaxf(scales0.y, 0x1p-40f), 0x1p40f);
+            const float lv = log2f(vs), rv = 1.f / vs;
+            to[0] = make_float2(ks, ks);
+            to[kBlocks] = make_float2(lv, lv);
+            to[2 * kBlocks] = make_float2(rv, rv);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(Lay::B_SCALES + quads % kScaleSlots));
+            ++quads;
+          }
         }
       }
     produced:
       if (*abort_flag) {  // let copies in flight land before the CTA's smem goes away
         for (uint32_t i = (kt > NK ? kt - NK : 0); i < kt; ++i)
-          wait_bounded(bar(B_KFULL + i % NK), (i / NK) & 1u, abort_flag, A.err, false);
+          wait_bounded(bar(Lay::B_KFULL + i % NK), (i / NK) & 1u, abort_flag, A.err, false);
         for (uint32_t i = (vt > NV ? vt - NV : 0); i < vt; ++i)
-          wait_bounded(bar(B_VFULL + i % NV), (i / NV) & 1u, abort_flag, A.err, false);
+          wait_bounded(bar(Lay::B_VFULL + i % NV), (i / NV) & 1u, abort_flag, A.err, false);
       }
     } else if (warp == 9) {
       // ================================================================ S products
       constexpr uint32_t idS = idesc_0(BM, BN, false);
-      uint32_t qc = 0, c = 0, kt = 0;  // pieces, products, K tiles
-      const uint64_t qd = sdesc_sw128(sb + kOffQ, 16, 1024), kd = sdesc_sw128(sb + kOffK, 16, 1024);
+      uint32_t qc = 0, c = 0, kt = 0, quads = 0;  // pieces, products, K tiles, quads of scales
+      const uint64_t qd = sdesc_sw128(sb + Lay::q, 16, 1024), kd = sdesc_sw128(sb + Lay::k, 16, 1024);
       while (pieces.next<Lay>(await, bar, smem, aborted, x)) {
-        if (!await(bar(B_QFULL), qc++ & 1u, aborted)) break;
+        if (!await(bar(Lay::B_QFULL), qc++ & 1u, aborted)) break;
         const bool two = two_tiles(x);
         for (int t = x.t0; t < x.t1; ++t, ++kt) {
           const uint32_t st = kt % NK;
-          if (!await(bar(B_KFULL + st), (kt / NK) & 1u, aborted)) goto scored;
+          if (!await(bar(Lay::B_KFULL + st), (kt / NK) & 1u, aborted)) goto scored;
+          if ((t - x.t0) % kQuad == 0) {  // the softmax reads them once it has S
+            if (!await(bar(Lay::B_SCALES + quads % kScaleSlots), (quads / kScaleSlots) & 1u, aborted)) goto scored;
+            ++quads;
+          }
 #pragma unroll 1
           for (int m = 0; m < (two ? 2 : 1); ++m) {
             // (the first product waits for the phase before the first, which counts as done)
-            if (!await(bar(B_SFREE), (c++ & 1u) ^ 1u, aborted)) goto scored;
+            if (!await(bar(Lay::B_SFREE), (c++ & 1u) ^ 1u, aborted)) goto scored;
             tc_fence_after();
             issue_s(tmem + kColS, (uint32_t)qd + m * (2 * kQHalf >> 4), (uint32_t)(qd >> 32),
                     (uint32_t)kd + st * (kTile >> 4), (uint32_t)(kd >> 32), idS,
-                    bar(B_SFULL + (two ? m : (t - x.t0) & 1)));
+                    bar(Lay::B_SFULL + (two ? m : (t - x.t0) & 1)));
           }
-          commit_elect(bar(B_KEMPTY + st));
-          if (t == x.t1 - 1) commit_elect(bar(B_QEMPTY));  // the piece's last use of Q
+          commit_elect(bar(Lay::B_KEMPTY + st));
+          if (t == x.t1 - 1) commit_elect(bar(Lay::B_QEMPTY));  // the piece's last use of Q
         }
       }
     scored:
       __syncwarp();
-      commit_elect(bar(B_DRAIN));
-      wait_bounded(bar(B_DRAIN), 0, abort_flag, A.err, false);
+      commit_elect(bar(Lay::B_DRAIN));
+      wait_bounded(bar(Lay::B_DRAIN), 0, abort_flag, A.err, false);
     } else if (warp == 10) {
       // ================================================================ PV products
       constexpr uint32_t idO = idesc_0(BM, D, true);
       uint32_t c0 = 0, c1 = 0, done0 = 0, done1 = 0, vt = 0;  // products and pieces of each group, V tiles
       // V as an MN-major operand: the d halves LBO apart, 8-key groups SBO apart
-      const uint64_t vd = sdesc_sw128(sb + kOffW, kVHalf, 1024);
+      const uint64_t vd = sdesc_sw128(sb + Lay::w, kVHalf, 1024);
       while (pieces.next<Lay>(await, bar, smem, aborted, x)) {
         const bool two = two_tiles(x);
         for (int t = x.t0; t < x.t1; ++t, ++vt) {
           const uint32_t st = vt % NW;
-          if (!await(bar(B_WFULL + st), (vt / NW) & 1u, aborted)) goto multiplied;
+          if (!await(bar(Lay::B_WFULL + st), (vt / NW) & 1u, aborted)) goto multiplied;
           const int turn = two ? 0 : (t - x.t0) & 1;
 #pragma unroll 1
           for (int m = turn; m < (two ? 2 : turn + 1); ++m) {
             // a group's first product of a piece takes O over from the epilogue of the one before
             // (from none at first: the phase before the first counts as done)
             const bool fresh = t - x.t0 == turn;
-            if (fresh && !await(bar(B_OFREE + m), ((m ? done1++ : done0++) & 1u) ^ 1u, aborted)) goto multiplied;
-            if (!await(bar(B_PFULL + m), (m ? c1++ : c0++) & 1u, aborted)) goto multiplied;
+            if (fresh && !await(bar(Lay::B_OFREE + m), ((m ? done1++ : done0++) & 1u) ^ 1u, aborted)) goto multiplied;
+            if (!await(bar(Lay::B_PFULL + m), (m ? c1++ : c0++) & 1u, aborted)) goto multiplied;
             tc_fence_after();
             issue_pv(tmem + kColO + m * D, tmem + kColP + m * 64, (uint32_t)vd + st * (kTileW >> 4),
-                     (uint32_t)(vd >> 32), idO, !fresh, bar(B_PVDONE + m));
+                     (uint32_t)(vd >> 32), idO, !fresh, bar(Lay::B_PVDONE + m));
           }
-          commit_elect(bar(B_WEMPTY + st));
+          commit_elect(bar(Lay::B_WEMPTY + st));
         }
       }
     multiplied:
       __syncwarp();
-      commit_elect(bar(B_DRAIN + 1));
-      wait_bounded(bar(B_DRAIN + 1), 0, abort_flag, A.err, false);
+      commit_elect(bar(Lay::B_DRAIN + 1));
+      wait_bounded(bar(Lay::B_DRAIN + 1), 0, abort_flag, A.err, false);
     } else {
       // ================================================================ scheduler
       schedule<Lay>(A, npb, await, bar, smem, aborted, lane);
@@ -751,28 +804,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   }
 }
 
-// One layer's codes as (d, head, token in its page or sequence, page or sequence); boxes of 128 d x
-// 1 head x `box` tokens, what lies outside reads as zeros.
-bool make_codes_map(CUtensorMap* m, const uint8_t* base, const cure_kv_desc& kv, int batch, bool swizzled) {
-  auto fn = encode_fn();
-  if (!fn) return false;
-  const bool paged = kv.layout == 1;
-  const cuuint64_t tokens = paged ? kv.page_size : kv.max_len > 0 ? kv.max_len : 1;
-  const cuuint64_t row = (cuuint64_t)kv.heads_kv * D;
-  cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)kv.heads_kv, tokens, (cuuint64_t)(paged ? kv.num_pages : batch)};
-  cuuint64_t strides[3] = {(cuuint64_t)D, row, row * tokens};
-  cuuint32_t box[4] = {(cuuint32_t)D, 1, (cuuint32_t)(paged ? kv.page_size : BN), 1};
-  cuuint32_t es[4] = {1, 1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(base), dims, strides, box, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-size_t counter_bytes(int ctas) { return ((size_t)ctas * sizeof(PieceCount) + 255) / 256 * 256; }
-
-template <class Args>
+template <int MT, class Args>
 cudaError_t launch(const Attn8Call& c, Args& A, cudaStream_t s) {
-  const auto kernel = attn8_kernel<Args>;
+  const auto kernel = attn8_kernel<Args, MT>;
+  constexpr int kSmemBytes = Layout<MT>::bytes;
   static std::atomic<uint64_t> ready;  // devices on which it has its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -784,31 +819,17 @@ cudaError_t launch(const Attn8Call& c, Args& A, cudaStream_t s) {
     ready.fetch_or(bit);
   }
   CUtensorMap mk, mv;
-  if (!make_codes_map(&mk, c.k_cache, c.kv, c.batch, true) || !make_codes_map(&mv, c.v_cache, c.kv, c.batch, false))
+  const int box = c.kv.layout == 1 ? c.kv.page_size : BN;
+  if (!make_codes_map(&mk, c.k_cache, c.kv, c.batch, box) || !make_codes_map(&mv, c.v_cache, c.kv, c.batch, box))
     return cudaErrorInvalidValue;
-  A.kv = c.kv;
-  A.row_start = c.row_start;
-  A.cache_len = c.cache_len;
-  A.rows = c.rows;
-  A.batch = c.batch;
-  A.heads_q = c.heads_q;
-  A.G = c.heads_q / c.kv.heads_kv;
-  A.cap = std::min(c.kv.layout == 0 ? c.kv.max_len : c.kv.max_len * c.kv.page_size, INT32_MAX - 2 * BN);
-  A.scale_log2 = c.scale * 1.4426950408889634f;
-  A.out = c.out;
-  A.err = c.err;
+  fill_args8(c, &A);
   A.q = c.q;
   A.k_scale = c.k_scale;
   A.v_scale = c.v_scale;
   A.n_nodes = c.n_nodes;
   A.anc = c.anc;
   A.n_max = c.n_max;
-  A.tag = next_launch_tag();  // whatever the workspace's counters hold counts as zero
   const int ctas = num_sms();
-  char* ws = static_cast<char*>(c.workspace);
-  A.cnt = reinterpret_cast<PieceCount*>(ws);
-  A.ws_o = reinterpret_cast<float*>(ws + counter_bytes(ctas));
-  A.ws_lse = A.ws_o + (size_t)2 * ctas * 2 * BM * D;
   // many units: after the whole of the call before (as in k_prompt.cu)
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(ctas);
@@ -825,20 +846,21 @@ cudaError_t launch(const Attn8Call& c, Args& A, cudaStream_t s) {
 
 }  // namespace
 
-// Workspace: piece counters [CTAs] (256-byte rounded), partial outputs and their log-sum-exps
-// [2 * CTAs]: of a CTA's pieces at most its first and its last are parts of a unit.
 size_t attn8_workspace() {
   const int ctas = num_sms();
-  return counter_bytes(ctas) + (size_t)ctas * 2 * 2 * BM * (D + 1) * sizeof(float);
+  return counter_bytes8(ctas) + (size_t)ctas * 2 * 2 * BM * (D + 1) * sizeof(float);
 }
 
 cudaError_t launch_attn8(const Attn8Call& c, cudaStream_t s) {
+  if (tokens8_fits(c)) return launch_tokens8(c, s);
+  // Sequences whose rows' heads fit one M tile on average: units of one M tile.
+  const bool one = c.rows <= (int64_t)c.batch * (BM / (c.heads_q / c.kv.heads_kv));
   if (c.n_nodes) {
     Tree8 A = {};
-    return launch(c, A, s);
+    return one ? launch<1>(c, A, s) : launch<2>(c, A, s);
   }
   Args8 A = {};
-  return launch(c, A, s);
+  return one ? launch<1>(c, A, s) : launch<2>(c, A, s);
 }
 
 }  // namespace cure

@@ -349,7 +349,7 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
   walk.start = start;
   walk.B = A.batch;
   walk.Hkv = A.kv.heads_kv;
-  walk.R = 2 * npb;
+  walk.R = LAY::m_tiles * npb;
   // Totals first: whether to cut units is chosen by them.
   struct Size {
     int64_t units, cost;
@@ -564,13 +564,14 @@ __device__ __forceinline__ void join_units(const Args& A, int npb, const uint8_t
     x = *reinterpret_cast<const Piece*>(smem + LAY::pieces + (kPieces + d) * (kPieceInts * 4));
     __threadfence();
     // rows 0 .. v0 - 1 of M tile 0 and 0 .. v1 - 1 of M tile 1
-    const int v0 = min(npb, x.n - 2 * x.rg * npb) * G, v1 = max(0, min(npb, x.n - (2 * x.rg + 1) * npb)) * G;
+    const int v0 = min(npb, x.n - LAY::m_tiles * x.rg * npb) * G,
+              v1 = LAY::m_tiles == 1 ? 0 : max(0, min(npb, x.n - (2 * x.rg + 1) * npb)) * G;
     const int rows8 = (v0 + v1 + 7) / 8;
     // A warp takes 8 rows and 4 * C of the 32 float4 columns, N parts' loads in flight:
     //   O = sum_p 2^(lse_p) O_p / sum_p 2^(lse_p), relative to the maximum so far
     auto join = [&](auto ctag, auto ntag) {
       constexpr int C = decltype(ctag)::value, N = decltype(ntag)::value;
-      for (int task = warp; task < rows8 * (8 / C); task += kThreads / 32) {
+      for (int task = warp; task < rows8 * (8 / C); task += LAY::threads / 32) {
         const int k = task / (8 / C) * 8 + (lane >> 2), c0 = task % (8 / C) * 4 * C + (lane & 3);
         if (k >= v0 + v1) continue;
         const int mt = k >= v0, rr = mt ? k - v0 : k;
@@ -619,7 +620,7 @@ __device__ __forceinline__ void join_units(const Args& A, int npb, const uint8_t
         }
         const float winv = 1.f / wsum;
         uint16_t* orow =
-            A.out + ((int64_t)(x.r0 + (2 * x.rg + mt) * npb + rr / G) * A.heads_q + x.h * G + rr % G) * D;
+            A.out + ((int64_t)(x.r0 + (LAY::m_tiles * x.rg + mt) * npb + rr / G) * A.heads_q + x.h * G + rr % G) * D;
 #pragma unroll
         for (int j = 0; j < C; ++j)
           *reinterpret_cast<uint2*>(orow + (c0 + 4 * j) * 4) =

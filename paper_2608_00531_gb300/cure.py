@@ -713,10 +713,12 @@ def cure_resync_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.T
     if out is None:
         out = dict(draft_valid_len=_new((B,), _I32, stream), replay_tokens=_new((B, P), _I32, stream),
                    n_replay=_new((B,), _I32, stream))
-    caches = [_caches(k, v, kv, B, dev, _E4M3) for k, v in zip(k_caches, v_caches)]
-    scales = [_scales(k, v, kv, B, dev) for k, v in zip(k_scales, v_scales)]
+    size = (B * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size) * kv.heads_kv * kv.head_dim
+    a, b, c = kv8_scale_shape(kv, B)
     array = C.c_void_p * max(1, layers)
-    kp, vp, ksp, vsp = (array(*[x[i] for x in t]) for t in (caches, scales) for i in (0, 1))
+    kp, vp, ksp, vsp = (array(*_pointers(t, nm, dtype, n, dev)) for t, nm, dtype, n in (
+        (k_caches, "a k_cache", _E4M3, size), (v_caches, "a v_cache", _E4M3, size),
+        (k_scales, "a k_scale", _F32, a * b * c), (v_scales, "a v_scale", _F32, a * b * c)))
     check("cure_resync_kv8", _lib.load().cure_resync_kv8(
         layers, kp, vp, ksp, vsp, C.byref(kv), _here(tree_k, "tree_k", _BF16, dev), _here(tree_v, "tree_v", _BF16, dev), B,
         n_max, block, i32(acc["path_nodes"], "path_nodes", B * P), i32(acc["accept_len"], "accept_len", B),
@@ -725,6 +727,18 @@ def cure_resync_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.T
         i32(out["draft_valid_len"], "draft_valid_len", B), i32(out["replay_tokens"], "replay_tokens", B * P),
         i32(out["n_replay"], "n_replay", B), s))
     out["cache_len"] = cache_len_out
+    return out
+
+
+def _pointers(tensors, name: str, dtype, n: int, dev: int) -> list:
+    """Addresses of the layers' tensors, each of a type, on device `dev`, contiguous and of at least n entries.  (In one
+    loop: hundreds of calls' checks would outlast their kernel.)"""
+    out = []
+    for t in tensors:
+        if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous() or t.numel() < n:
+            _here(t, name, dtype, dev)
+            raise ValueError(f"{name} is smaller than its geometry")
+        out.append(t.data_ptr())
     return out
 
 
