@@ -25,7 +25,7 @@
 //   warp 9            issues S = Q K^T (M128 N128, K 2 x 128) of M tiles 0 and 1 in turn
 //   warp 10           issues O += P' V (A = P' from TMEM)
 //   warp 11           lays out the CTA's pieces of work
-//   warps 12-15       Q into its parts, V tiles to fp16, and the epilogue: a piece's rows go
+//   warps 12-15       Q (by TMA) into its parts, V tiles to fp16, and the epilogue: a piece's rows go
 //                     out once the next one's Q and first V tile are on their way
 // TMEM as there: S (128) | P[2] (64 each) | O[2] (128 each).  A piece whose rows fit one M
 // tile (single tokens, small trees) takes its tiles in turn with both softmax groups, each
@@ -53,7 +53,7 @@ struct Layout {
   static constexpr int m_tiles = MT, threads = kThreads;
   static constexpr int NK = MT == 1 ? 4 : 3, NV = MT == 1 ? 3 : 2, NW = 2;  // stages: K tiles, V tiles, V tiles in fp16
   enum : int {
-    B_QFULL = 0, B_QEMPTY, B_SFREE, B_KFULL, B_KEMPTY = B_KFULL + NK, B_VFULL = B_KEMPTY + NK, B_VEMPTY = B_VFULL + NV,
+    B_QFULL = 0, B_QEMPTY = 2, B_QRAW, B_SFREE, B_KFULL, B_KEMPTY = B_KFULL + NK, B_VFULL = B_KEMPTY + NK, B_VEMPTY = B_VFULL + NV,
     B_WFULL = B_VEMPTY + NV, B_WEMPTY = B_WFULL + NW, B_SFULL = B_WEMPTY + NW, B_PFULL = B_SFULL + 2,
     B_PVDONE = B_PFULL + 2, B_STAT = B_PVDONE + 2, B_OFREE = B_STAT + 2, B_DRAIN = B_OFREE + 2, B_JOIN = B_DRAIN + 2,
     B_SCALES = B_JOIN + 1, piece_bar = B_SCALES + kScaleSlots, taken_bar = piece_bar + kPieces,
@@ -79,12 +79,12 @@ struct Layout {
 };
 
 struct Args8 : PromptArgs {
-  const uint16_t* q;
   const float *k_scale, *v_scale;
   // a tree's rows (Tree8)
   const int32_t* n_nodes;
   const uint64_t* anc;
   int n_max;
+  int cluster;  // CTAs of a unit's cluster (CLUSTER)
 };
 struct Tree8 : Args8 {
   static constexpr bool kTree = true;
@@ -172,24 +172,35 @@ __host__ __device__ constexpr uint32_t idesc_0(int M, int N, bool b_mn_major) {
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
-// Whether the phase of the given parity is over, for all lanes of a warp (no waiting).
-__device__ __forceinline__ bool test_warp(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}\n"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return __all_sync(0xffffffffu, ok != 0);
-}
-
 constexpr float kLift = 7.f;  // P' is 2^kLift times what it stands for: at most 2^15 with the lag of 2^8
 
-template <class Args, int MT>
+// ---- clusters: barrier, a peer's address of a shared-memory variable, loads from it
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float ld_cluster(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 ld_cluster_v4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+  return v;
+}
+
+// CLUSTER (a tree's rows, MT = 1): each unit has a cluster of A.cluster CTAs to itself, which take an equal
+// part of its tiles each and join them through distributed shared memory.
+template <class Args, int MT, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 1)
-attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const Args A) {
+attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+             const __grid_constant__ CUtensorMap tm_q, const Args A) {
   constexpr bool kTree = Args::kTree;
   using Lay = Layout<MT>;
   constexpr int NK = Lay::NK, NV = Lay::NV, NW = Lay::NW;
@@ -212,7 +223,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   // ---------------------------------------------------------------- set-up
   if (tid == 0) {
     mbar_init(bar(Lay::B_QFULL), BM);
+    mbar_init(bar(Lay::B_QFULL + 1), BM);
     mbar_init(bar(Lay::B_QEMPTY), 1);
+    mbar_init(bar(Lay::B_QRAW), 1);
     mbar_init(bar(Lay::B_SFREE), BM);
     for (int i = 0; i < NK; ++i) {
       mbar_init(bar(Lay::B_KFULL + i), 1);
@@ -248,6 +261,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   if (warp == 8 && lane == 0) {
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
+    tma_prefetch_desc(&tm_q);
   }
   pdl_begin();
   tc_fence_before();
@@ -418,7 +432,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     const int row = tid & 127;  // row within an M tile = TMEM lane
     const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColO;
     const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
-    uint32_t done0 = 0, done1 = 0, tiles0 = 0, tiles1 = 0, joins = 0, pc = 0, vt = 0;
+    uint32_t done0 = 0, done1 = 0, tiles0 = 0, tiles1 = 0, joins = 0, pc = 0, vt = 0, q_raw = 0;
     bool ok = true, have = false;
     Piece* kept = reinterpret_cast<Piece*>(smem + Lay::kept) + (warp & 3);  // (registers are short)
     // The epilogue's threads meet (an mbarrier, for a wait that ends when the CTA gives up).
@@ -430,19 +444,28 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       const bool more = pieces.next<Lay>(await, bar, smem, aborted, x);
       if (!more && !have) break;
       if (more) {
-        // ---- Q of the piece, once the S products of the one before are done
+        // ---- Q of the piece, once the S products of the one before are done: bf16 rows by TMA (dims 0-63
+        // where q1 goes, the others in q2's place), which each thread takes out and puts back as its row's parts
         if (!await(bar(Lay::B_QEMPTY), (pc & 1u) ^ 1u, aborted)) break;
         const int mts = two_tiles(x) ? 2 : 1;
+        if (warp == 12) {
+          if (lane == 0) mbar_arrive_expect_tx(bar(Lay::B_QRAW), (uint32_t)(2 * mts * npb * G * 128));
+          __syncwarp();
+          if (lane < 2 * mts)  // M tile lane / 2, d half lane % 2
+            tma_load_4d(sb + Lay::q + lane * kQHalf, &tm_q, bar(Lay::B_QRAW), (lane & 1) * 64, 0, x.h,
+                        x.r0 + (MT * x.rg + (lane >> 1)) * npb);
+          __syncwarp();
+        }
+        q_raw = pc + 1;
+        if (!await(bar(Lay::B_QRAW), pc & 1u, aborted)) break;
 #pragma unroll 1
         for (int m = 0; m < mts; ++m) {
           const int i = (MT * x.rg + m) * npb + row / G;
+          const uint32_t dst = sb + Lay::q + m * 2 * kQHalf + row * 128;
           uint4 w[16];
-          if (row < npb * G && i < x.n) {
-            const uint4* src =
-                reinterpret_cast<const uint4*>(A.q + ((int64_t)(x.r0 + i) * A.heads_q + x.h * G + row % G) * D);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) w[k] = __ldg(src + k);
-          } else {
+          for (int k = 0; k < 16; ++k) w[k] = ld_shared_v4(dst + (k >> 3) * kQHalf + (((k & 7) ^ (row & 7)) << 4));
+          if (row >= npb * G || i >= x.n) {
 #pragma unroll
             for (int k = 0; k < 16; ++k) w[k] = make_uint4(0u, 0u, 0u, 0u);
           }
@@ -460,7 +483,6 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           const int e = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -60), 120);
           q_scale[((pc & 1u) * 2 + m) * BM + row] = __uint_as_float((uint32_t)(127 + e) << 23);
           const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-          const uint32_t dst = sb + Lay::q + m * 2 * kQHalf + row * 128;
 #pragma unroll
           for (int u = 0; u < 8; ++u) {  // 16 dims
             const uint32_t in[8] = {w[2 * u].x,     w[2 * u].y,     w[2 * u].z,     w[2 * u].w,
@@ -481,9 +503,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             st_shared_v4(to, q1[0], q1[1], q1[2], q1[3]);
             st_shared_v4(to + kQHalf, q2[0], q2[1], q2[2], q2[3]);
           }
+          fence_proxy_async_smem();
+          mbar_arrive(bar(Lay::B_QFULL + m));
         }
-        fence_proxy_async_smem();
-        mbar_arrive(bar(Lay::B_QFULL));
         ++pc;
       }
       for (int t = more ? x.t0 : 0, t_end = more ? x.t1 : 1; ok && t < t_end; ++t) {
@@ -564,7 +586,13 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           const bool vrow = row < npb * G && i < prev.n;
           uint16_t* orow = A.out + ((int64_t)(prev.r0 + i) * A.heads_q + prev.h * G + row % G) * D;
           float4* po = reinterpret_cast<float4*>(A.ws_o) + slot * (32 * 2 * BM) + m * BM + row;
-          if (!whole) __stcg(A.ws_lse + slot * (2 * BM) + m * BM + row, lse);
+          constexpr int kPlaces = CLUSTER ? BM : 2 * BM;  // rows of a float4 column
+          if (CLUSTER) {  // (no product reads V any more)
+            po = reinterpret_cast<float4*>(smem + Lay::w) + row;
+            lse_of[row] = lse;
+          } else if (!whole) {
+            __stcg(A.ws_lse + slot * (2 * BM) + m * BM + row, lse);
+          }
 #pragma unroll 1
           for (int q = 0; q < 8; ++q) {  // 16 columns
             uint32_t o[16];
@@ -581,7 +609,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                 o[k] = __float_as_uint(fmaf(__uint_as_float(o1[k]), f1, __uint_as_float(o[k])));
             }
             if (!vrow) {
-            } else if (whole) {
+            } else if (whole && !CLUSTER) {
               uint32_t v[8];
 #pragma unroll
               for (int k = 0; k < 8; ++k) v[k] = pack_bf16(__uint_as_float(o[2 * k]), __uint_as_float(o[2 * k + 1]));
@@ -590,7 +618,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
               // a part of a unit: normalised O to the workspace, float4 columns [32][256 rows]
 #pragma unroll
               for (int k = 0; k < 4; ++k)
-                po[(q * 4 + k) * (2 * BM)] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
+                po[(q * 4 + k) * kPlaces] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]),
                                                          __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
             }
           }
@@ -598,7 +626,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           mbar_arrive(bar(Lay::B_OFREE + m));
           if (both) mbar_arrive(bar(Lay::B_OFREE + 1));
         }
-        if (!ok || whole) continue;
+        if (!ok || whole || CLUSTER) continue;
         // The CTA whose part arrives last joins the unit when its own pieces are done.
         __threadfence();
         if (!meet()) break;
@@ -614,6 +642,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       __syncwarp();
       have = true;
     }
+    if (*abort_flag && q_raw > 0)  // let the copies in flight land before the CTA's smem goes away
+      wait_bounded(bar(Lay::B_QRAW), (q_raw - 1) & 1u, abort_flag, A.err, false);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == 8) {
@@ -652,21 +682,27 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         // of the quad before, this one (the last K tile's) and the next one
         int pages_1 = -1, pages0 = pages_of(0), pages1 = pages_of(1);
         float2 scales0 = scales_of(0, pages0), scales1;
+        bool unsaid = false;  // whether the quad's scales are still to be put into shared memory
+        auto say = [&]() {
+          float2* to = reinterpret_cast<float2*>(smem + Lay::scales) +
+                       (quads % kScaleSlots * kQuad + (lane >> 3)) * (kScaleFloats / 2) + (lane & 7);
+          const float ks = fminf(fmaxf(scales0.x, 0x1p-40f), 0x1p40f), vs = fminf(fmaxf(scales0.y, 0x1p-40f), 0x1p40f);
+          const float lv = log2f(vs), rv = 1.f / vs;
+          to[0] = make_float2(ks, ks);
+          to[kBlocks] = make_float2(lv, lv);
+          to[2 * kBlocks] = make_float2(rv, rv);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(Lay::B_SCALES + quads % kScaleSlots));
+          ++quads;
+          unsaid = false;
+        };
         // K and V tiles, each as soon as it has a free stage
         for (int ik = 0, iv = 0; iv < nt;) {
-          bool is_v;
-          for (const uint32_t began = clock();;) {
-            if (ik < nt && ik < iv + NK && test_warp(bar(Lay::B_KEMPTY + kt % NK), ((kt / NK) & 1u) ^ 1u)) {
-              is_v = false;
-              break;
-            }
-            if (iv < ik && test_warp(bar(Lay::B_VEMPTY + vt % NV), ((vt / NV) & 1u) ^ 1u)) {
-              is_v = true;
-              break;
-            }
-            if (__any_sync(0xffffffffu, *abort_flag != 0)) goto produced;
-            if ((uint32_t)clock() - began > (uint32_t)kWaitTimeoutCycles) *abort_flag = 1;
-          }
+          const bool is_v = ik == nt || ik > iv + 1;
+          if (unsaid && (is_v ? iv > 0 : ik % kQuad == 0)) say();
+          if (!await(is_v ? bar(Lay::B_VEMPTY + vt % NV) : bar(Lay::B_KEMPTY + kt % NK),
+                     ((is_v ? vt / NV : kt / NK) & 1u) ^ 1u, aborted))
+            goto produced;
           int page;
           if (is_v) {  // (at most NK - 1 tiles behind K: in its quad or the one before)
             page = __shfl_sync(0xffffffffu, iv / kQuad == (ik - 1) / kQuad ? pages0 : pages_1, iv % kQuad * 8 | (lane & 7));
@@ -696,19 +732,11 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           __syncwarp();
           if (is_v) {
             ++iv;
-          } else if (ik++ % kQuad == 0) {  // the quad's scales
-            float2* to = reinterpret_cast<float2*>(smem + Lay::scales) +
-                         (quads % kScaleSlots * kQuad + (lane >> 3)) * (kScaleFloats / 2) + (lane & 7);
-            const float ks = fminf(fmaxf(scales0.x, 0x1p-40f), 0x1p40f), vs = fminf(fmaxf(scales0.y, 0x1p-40f), 0x1p40f);
-            const float lv = log2f(vs), rv = 1.f / vs;
-            to[0] = make_float2(ks, ks);
-            to[kBlocks] = make_float2(lv, lv);
-            to[2 * kBlocks] = make_float2(rv, rv);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(Lay::B_SCALES + quads % kScaleSlots));
-            ++quads;
+          } else if (ik++ % kQuad == 0) {
+            unsaid = true;
           }
         }
+        if (unsaid) say();
       }
     produced:
       if (*abort_flag) {  // let copies in flight land before the CTA's smem goes away
@@ -720,10 +748,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     } else if (warp == 9) {
       // ================================================================ S products
       constexpr uint32_t idS = idesc_0(BM, BN, false);
-      uint32_t qc = 0, c = 0, kt = 0, quads = 0;  // pieces, products, K tiles, quads of scales
+      uint32_t q0 = 0, q1 = 0, c = 0, kt = 0, quads = 0;  // pieces of each M tile, products, K tiles, quads of scales
       const uint64_t qd = sdesc_sw128(sb + Lay::q, 16, 1024), kd = sdesc_sw128(sb + Lay::k, 16, 1024);
       while (pieces.next<Lay>(await, bar, smem, aborted, x)) {
-        if (!await(bar(Lay::B_QFULL), qc++ & 1u, aborted)) break;
         const bool two = two_tiles(x);
         for (int t = x.t0; t < x.t1; ++t, ++kt) {
           const uint32_t st = kt % NK;
@@ -736,6 +763,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           for (int m = 0; m < (two ? 2 : 1); ++m) {
             // (the first product waits for the phase before the first, which counts as done)
             if (!await(bar(Lay::B_SFREE), (c++ & 1u) ^ 1u, aborted)) goto scored;
+            if (t == x.t0 && !await(bar(Lay::B_QFULL + m), (m ? q1++ : q0++) & 1u, aborted)) goto scored;
             tc_fence_after();
             issue_s(tmem + kColS, (uint32_t)qd + m * (2 * kQHalf >> 4), (uint32_t)(qd >> 32),
                     (uint32_t)kd + st * (kTile >> 4), (uint32_t)(kd >> 32), idS,
@@ -781,7 +809,38 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       wait_bounded(bar(Lay::B_DRAIN + 1), 0, abort_flag, A.err, false);
     } else {
       // ================================================================ scheduler
-      schedule<Lay>(A, npb, await, bar, smem, aborted, lane);
+      if constexpr (CLUSTER) {
+        // the one piece of this CTA, if the unit has so many tiles
+        const int rank = (int)blockIdx.x % A.cluster, u = (int)blockIdx.x / A.cluster, Hkv = A.kv.heads_kv;
+        const int groups = (A.n_max + npb - 1) / npb;
+        int bad;
+        x = Piece{};
+        x.b = u / (Hkv * groups);
+        x.h = u % Hkv;
+        x.rg = u / Hkv % groups;
+        const Seq q = sequence(A, x.b, &bad);
+        if (bad && rank == 0 && x.h == 0 && x.rg == 0) flag(A.err, bad);
+        x.r0 = q.r0;
+        x.n = q.n;
+        x.L = q.L;
+        x.keys = q.L + q.n;
+        x.T = (x.keys + BN - 1) / BN;
+        x.t0 = x.T * rank / A.cluster;
+        x.t1 = x.T * (rank + 1) / A.cluster;
+        if (x.rg * npb >= q.n) x.t1 = x.t0 = 0;  // no rows
+        if (lane == 0) {
+          Piece* to = reinterpret_cast<Piece*>(smem + Lay::pieces);
+          to[0] = x;
+          mbar_arrive(bar(Lay::piece_bar));
+          if (x.t0 < x.t1) {
+            to[1] = Piece{};
+            mbar_arrive(bar(Lay::piece_bar + 1));
+          }
+        }
+        __syncwarp();
+      } else {
+        schedule<Lay>(A, npb, await, bar, smem, aborted, lane);
+      }
     }
   }
 
@@ -793,9 +852,53 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   __syncthreads();
   if (warp < 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 128;");
   else asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
-  if (*abort_flag) {
-    if (tid == 0) flag(A.err, CURE_DEVERR_TIMEOUT);
-  } else {
+  if (*abort_flag && tid == 0) flag(A.err, CURE_DEVERR_TIMEOUT);
+  if constexpr (CLUSTER) {
+    // Each CTA of the cluster joins some of the unit's rows, a float4 a thread:
+    //   O = sum_p 2^(lse_p) O_p / sum_p 2^(lse_p) over the parts that saw a key
+    const Piece& p = *reinterpret_cast<const Piece*>(smem + Lay::pieces);
+    if (p.t0 >= p.t1 || *abort_flag)  // this CTA's part has none
+      for (int i = tid; i < BM; i += kThreads) lse_of[i] = -FLT_MAX;
+    cluster_sync();
+    const int rank = (int)blockIdx.x % A.cluster;
+    const int rows = min(npb, p.n - p.rg * npb) * G, each = (max(rows, 0) + A.cluster - 1) / A.cluster;
+    const int first = rank * each, mine = min(each, rows - first);
+    for (int i = tid; i < mine * 32; i += kThreads) {
+      const int r = first + i % mine, c = i / mine;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float top = -FLT_MAX, total = 0.f;
+      const uint32_t l_at = sb + Lay::lse + r * 4, o_at = sb + Lay::w + (c * BM + r) * 16;
+      for (int q0 = 0; q0 < A.cluster; q0 += 4) {
+        float w[4], best = top;
+        float4 o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int from = min(q0 + q, A.cluster - 1);
+          w[q] = ld_cluster(map_rank(l_at, from));
+          o[q] = ld_cluster_v4(map_rank(o_at, from));
+          if (q0 + q >= A.cluster) w[q] = -FLT_MAX;
+          best = fmaxf(best, w[q]);
+        }
+        const float a = ex2(top - best);
+        top = best;
+        total *= a;
+        acc = make_float4(acc.x * a, acc.y * a, acc.z * a, acc.w * a);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (w[q] == -FLT_MAX) continue;  // (what stands there may be anything)
+          const float wq = ex2(w[q] - top);
+          total += wq;
+          acc = make_float4(fmaf(wq, o[q].x, acc.x), fmaf(wq, o[q].y, acc.y), fmaf(wq, o[q].z, acc.z),
+                            fmaf(wq, o[q].w, acc.w));
+        }
+      }
+      const float inv = total > 0.f ? 1.f / total : 0.f;
+      uint16_t* orow = A.out + ((int64_t)(p.r0 + p.rg * npb + r / G) * A.heads_q + p.h * G + r % G) * D;
+      *reinterpret_cast<uint2*>(orow + 4 * c) =
+          make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    }
+    cluster_sync();  // the peers have read this CTA's shared memory
+  } else if (!*abort_flag) {
     join_units<Lay>(A, npb, smem, *n_joins, warp, lane);
   }
   if (warp == 0) {
@@ -804,44 +907,92 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   }
 }
 
-template <int MT, class Args>
-cudaError_t launch(const Attn8Call& c, Args& A, cudaStream_t s) {
-  const auto kernel = attn8_kernel<Args, MT>;
-  constexpr int kSmemBytes = Layout<MT>::bytes;
-  static std::atomic<uint64_t> ready;  // devices on which it has its shared memory
+// Dynamic shared memory (and clusters above the portable size), once per device.
+template <class Args, int MT, bool CLUSTER>
+cudaError_t set_up() {
+  static std::atomic<uint64_t> ready;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
-  if (!(ready.load() & bit)) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-    if (e != cudaSuccess) return e;
-    ready.fetch_or(bit);
+  if (ready.load() & bit) return cudaSuccess;
+  const auto kernel = attn8_kernel<Args, MT, CLUSTER>;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<MT>::bytes);
+  if (e == cudaSuccess && CLUSTER) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) ready.fetch_or(bit);
+  return e;
+}
+
+// Clusters of `size` CTAs that the device holds at once (a cluster lies within one GPC, so fewer than
+// SMs / size).
+int max_clusters(int size) {
+  static std::atomic<int> known[64][kAttnMaxCluster + 1];  // 1 + the count; 0: not asked yet
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || set_up<Tree8, 1, true>() != cudaSuccess) return 0;
+  int n = known[dev][size].load();
+  if (n == 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(size);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Layout<1>::bytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = size;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, attn8_kernel<Tree8, 1, true>, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    known[dev][size].store(++n);
   }
-  CUtensorMap mk, mv;
+  return n - 1;
+}
+
+// CTAs of each unit's cluster for `units` units of one M tile; 0: units cut among all CTAs instead (the
+// faster form where a cluster would have two: 8 trees of up to 33 nodes, 28/4 heads, 50.5 us so, 53.7 in
+// clusters of 2; 4 of them 51.1 and, in clusters of 4, 36.9; one of 25 nodes, 32/8 heads, 30.7 and 18.5).
+int cluster_size(int64_t units) {
+  for (int c = kAttnMaxCluster; c >= 3; --c)
+    if (units <= max_clusters(c)) return c;
+  return 0;
+}
+
+template <int MT, bool CLUSTER, class Args>
+cudaError_t launch(const Attn8Call& c, Args& A, int grid, cudaStream_t s) {
+  const cudaError_t e = set_up<Args, MT, CLUSTER>();
+  if (e != cudaSuccess) return e;
+  CUtensorMap mk, mv, mq;
   const int box = c.kv.layout == 1 ? c.kv.page_size : BN;
-  if (!make_codes_map(&mk, c.k_cache, c.kv, c.batch, box) || !make_codes_map(&mv, c.v_cache, c.kv, c.batch, box))
+  if (!make_codes_map(&mk, c.k_cache, c.kv, c.batch, box) || !make_codes_map(&mv, c.v_cache, c.kv, c.batch, box) ||
+      !make_q_map(&mq, c.q, (uint64_t)c.rows, c.kv.heads_kv, c.heads_q / c.kv.heads_kv, BM * c.kv.heads_kv / c.heads_q))
     return cudaErrorInvalidValue;
   fill_args8(c, &A);
-  A.q = c.q;
   A.k_scale = c.k_scale;
   A.v_scale = c.v_scale;
   A.n_nodes = c.n_nodes;
   A.anc = c.anc;
   A.n_max = c.n_max;
-  const int ctas = num_sms();
-  // many units: after the whole of the call before (as in k_prompt.cu)
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas);
+  cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.dynamicSmemBytes = Layout<MT>::bytes;
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchAttribute attr[2];
   cfg.attrs = attr;
-  cfg.numAttrs = (int64_t)c.rows * c.heads_q > (int64_t)4 * 2 * BM * ctas ? 0 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, mk, mv, A);
+  if (CLUSTER) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = A.cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+  }
+  // many units: after the whole of the call before (as in k_prompt.cu)
+  if ((int64_t)c.rows * c.heads_q <= (int64_t)4 * 2 * BM * num_sms()) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  return cudaLaunchKernelEx(&cfg, attn8_kernel<Args, MT, CLUSTER>, mk, mv, mq, A);
 }
 
 }  // namespace
@@ -854,13 +1005,19 @@ size_t attn8_workspace() {
 cudaError_t launch_attn8(const Attn8Call& c, cudaStream_t s) {
   if (tokens8_fits(c)) return launch_tokens8(c, s);
   // Sequences whose rows' heads fit one M tile on average: units of one M tile.
-  const bool one = c.rows <= (int64_t)c.batch * (BM / (c.heads_q / c.kv.heads_kv));
+  const int npb = BM / (c.heads_q / c.kv.heads_kv);
+  const bool one = c.rows <= (int64_t)c.batch * npb;
+  const int sms = num_sms();
   if (c.n_nodes) {
     Tree8 A = {};
-    return one ? launch<1>(c, A, s) : launch<2>(c, A, s);
+    // few units: a cluster of CTAs each
+    const int64_t units = (int64_t)c.batch * c.kv.heads_kv * ((c.n_max + npb - 1) / npb);
+    A.cluster = units * 2 <= sms ? cluster_size(units) : 0;
+    if (A.cluster > 0) return launch<1, true>(c, A, (int)units * A.cluster, s);
+    return one ? launch<1, false>(c, A, sms, s) : launch<2, false>(c, A, sms, s);
   }
   Args8 A = {};
-  return one ? launch<1>(c, A, s) : launch<2>(c, A, s);
+  return one ? launch<1, false>(c, A, sms, s) : launch<2, false>(c, A, sms, s);
 }
 
 }  // namespace cure
