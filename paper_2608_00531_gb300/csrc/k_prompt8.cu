@@ -428,7 +428,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     }
   } else if (warp >= 12) {
     // ================================================================ Q, V tiles, epilogue
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     const int row = tid & 127;  // row within an M tile = TMEM lane
     const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColO;
     const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
@@ -645,7 +645,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     if (*abort_flag && q_raw > 0)  // let the copies in flight land before the CTA's smem goes away
       wait_bounded(bar(Lay::B_QRAW), (q_raw - 1) & 1u, abort_flag, A.err, false);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == 8) {
       // ================================================================ producer
       const int ps = A.kv.page_size;
