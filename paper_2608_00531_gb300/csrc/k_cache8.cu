@@ -15,24 +15,21 @@
 // holds already.  kHeads heads of K and V at a time are loaded, normed and turned, and their rows' largest
 // values meet in shared memory; behind the barrier each half warp writes its codes.  Heads of Q go the
 // same way without meeting; where a block gains few rows, all half warps share those rows' heads.
-#include <cuda_bf16.h>
-
 #include <algorithm>
 
-#include "attn_tc.cuh"
-#include "common.cuh"
+#include "rope_math.cuh"
 
 namespace cure {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
+using rope::hi_f;
+using rope::lo_f;
+using rope::Raw;
+
+constexpr int kThreads = 256;
 constexpr int kD = 128;
 constexpr int kBlk = CURE_KV8_BLOCK;
 static_assert(kBlk == 16, "16 rows in 8 steps of two");
-
-__device__ __forceinline__ float lo_f(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float hi_f(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
 // Four values as codes (ties to even; beyond 448: 448; NaN stays one), and back.
 __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
@@ -85,9 +82,6 @@ __device__ __forceinline__ Lane lane_of(int l16, int rot_dim) {
   return p;
 }
 
-struct Raw {  // a lane's values of one row as they lie in memory
-  uint2 a, b;
-};
 __device__ __forceinline__ Raw load_raw(const uint16_t* row, const Lane& p) {
   Raw x;
   x.a = *reinterpret_cast<const uint2*>(row + p.off_a);
@@ -135,18 +129,20 @@ __device__ __forceinline__ float norm_factor(const float* y, float eps) {
   return rsqrtf(ss * (1.f / kD) + eps);
 }
 
-constexpr int kHeads = 2;  // of K and V between two barriers
+constexpr int kHeads = 2;   // of K and V between two barriers: in the append
+constexpr int kHeadsP = 4;  // .. in the commit
 
 // What a half warp has in the slot of its block.
 enum Slot { kNone, kHeld, kFresh };
 
-// kHeads heads of a block's K or V, all threads of the CTA: y the rows' values (kNone: any), `codes` each
+// N heads of a block's K or V, all threads of the CTA: y the rows' values (kNone: any), `codes` each
 // head's codes of the half warp's slot (NULL: no head), `scale` its place.
-__device__ __forceinline__ void quantise(float (&y)[kHeads][8], Slot what, uint8_t* const (&codes)[kHeads],
-                                         float* const (&scale)[kHeads], const float (&old)[kHeads], const Lane& p,
+template <int N>
+__device__ __forceinline__ void quantise(float (&y)[N][8], Slot what, uint8_t* const (&codes)[N],
+                                         float* const (&scale)[N], const float (&old)[N], const Lane& p,
                                          float (*part)[16], int hw, int l16) {
 #pragma unroll
-  for (int u = 0; u < kHeads; ++u) {
+  for (int u = 0; u < N; ++u) {
     float amax = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[u][e]));  // (a NaN counts for nothing)
@@ -156,7 +152,7 @@ __device__ __forceinline__ void quantise(float (&y)[kHeads][8], Slot what, uint8
   }
   __syncthreads();
 #pragma unroll
-  for (int u = 0; u < kHeads; ++u) {
+  for (int u = 0; u < N; ++u) {
     if (!codes[u]) break;
     float amax = part[u][l16];
 #pragma unroll
@@ -420,7 +416,7 @@ struct Paths8Args {
 // The k-th block that sequence b's accepted path reaches (blockIdx.x = b * blocks + k).
 __global__ void __launch_bounds__(kThreads, 3)
 paths8_kernel(const __grid_constant__ Paths8Args A) {
-  __shared__ float part[2][kHeads][16];
+  __shared__ float part[2][kHeadsP][16];
   pdl_begin();
   const int tid = threadIdx.x, l16 = tid & 15, hw = tid >> 4;
   const int blocks = (A.block + 1 + kBlk - 2) / kBlk + 1;
@@ -452,19 +448,19 @@ paths8_kernel(const __grid_constant__ Paths8Args A) {
   if (!__syncthreads_or(what == kFresh)) return;
   const Lane plain = lane_of<true>(l16, 0);
   const int64_t ld = (int64_t)Hkv * kD, at_slot = (crow + hw) * ld;
-  const int groups = (Hkv + kHeads - 1) / kHeads;
+  const int groups = (Hkv + kHeadsP - 1) / kHeadsP;
   int buf = 0;
   for (int item = blockIdx.y; item < A.layers * 2 * groups; item += gridDim.y) {
-    const int l = item / (2 * groups), kv = item / groups & 1, h = item % groups * kHeads;
+    const int l = item / (2 * groups), kv = item / groups & 1, h = item % groups * kHeadsP;
     const uint16_t* in = (kv ? A.tree_v : A.tree_k) + (((int64_t)l * A.batch + b) * A.n_max + node) * ld;
     uint8_t* base = static_cast<uint8_t*>(kv ? A.caches.v[l] : A.caches.k[l]) + at_slot;
     float* scales = (kv ? A.scales.v[l] : A.scales.k[l]) + place * Hkv;
-    Raw x[kHeads];
-    float old[kHeads], y[kHeads][8];
-    uint8_t* codes[kHeads];
-    float* scale[kHeads];
+    Raw x[kHeadsP];
+    float old[kHeadsP], y[kHeadsP][8];
+    uint8_t* codes[kHeadsP];
+    float* scale[kHeadsP];
 #pragma unroll
-    for (int u = 0; u < kHeads; ++u) {
+    for (int u = 0; u < kHeadsP; ++u) {
       const bool is = h + u < Hkv;
       codes[u] = is ? base + (h + u) * kD : nullptr;
       scale[u] = scales + h + u;
@@ -472,7 +468,7 @@ paths8_kernel(const __grid_constant__ Paths8Args A) {
       old[u] = is && from > 0 ? *scale[u] : 1.f;
     }
 #pragma unroll
-    for (int u = 0; u < kHeads; ++u) value_of(x[u], what, old[u], y[u]);
+    for (int u = 0; u < kHeadsP; ++u) value_of(x[u], what, old[u], y[u]);
     quantise(y, what, codes, scale, old, plain, part[buf], hw, l16);
     buf ^= 1;
   }
@@ -516,7 +512,7 @@ cudaError_t launch_paths8(int layers, const LayerPtrs& caches, const LayerScales
   a.cache_len = cache_len;
   a.err = err;
   const int blocks = (block + 1 + kBlk - 2) / kBlk + 1;
-  const int parts = layers * 2 * ((kv.heads_kv + kHeads - 1) / kHeads);
+  const int parts = layers * 2 * ((kv.heads_kv + kHeadsP - 1) / kHeadsP);
   return launch_pdl(paths8_kernel, dim3((unsigned)(batch * blocks), (unsigned)(parts < 65535 ? parts : 65535)),
                     dim3(kThreads), 0, s, a);
 }

@@ -31,61 +31,16 @@
 // 8 heads 2.6 us, 758 rows of 28 + 2 x 4 heads with norms 7.4 us (1.9 TB/s).  (Loads of
 // the next step into each place as it falls free: 63 us for the 10940 rows, as the
 // four places' sums then run one after the other.)
-#include <cuda_bf16.h>
-
-#include "attn_tc.cuh"
-#include "common.cuh"
+#include "rope_math.cuh"
 
 namespace cure {
 namespace {
 
+using namespace rope;
+
 constexpr int kWarps = 8;
 constexpr int kD = 128;
 constexpr int kUnroll = 4;  // heads of one step of a warp: 2 * kUnroll, their loads in flight together
-
-__device__ __forceinline__ float lo_f(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float hi_f(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
-struct Raw {  // a lane's values of one head as they lie in memory
-  uint2 a, b;
-};
-// Its four pairs: first and second values, two pairs to a register pair.
-template <bool INTER>
-__device__ __forceinline__ void unpack(const Raw& x, uint64_t (&a)[2], uint64_t (&b)[2]) {
-  if (INTER) {
-    a[0] = tc::f2_pack(lo_f(x.a.x), lo_f(x.a.y));
-    b[0] = tc::f2_pack(hi_f(x.a.x), hi_f(x.a.y));
-    a[1] = tc::f2_pack(lo_f(x.b.x), lo_f(x.b.y));
-    b[1] = tc::f2_pack(hi_f(x.b.x), hi_f(x.b.y));
-  } else {
-    a[0] = tc::f2_pack(lo_f(x.a.x), hi_f(x.a.x));
-    a[1] = tc::f2_pack(lo_f(x.a.y), hi_f(x.a.y));
-    b[0] = tc::f2_pack(lo_f(x.b.x), hi_f(x.b.x));
-    b[1] = tc::f2_pack(lo_f(x.b.y), hi_f(x.b.y));
-  }
-}
-template <bool INTER>
-__device__ __forceinline__ Raw pack(const uint64_t (&a)[2], const uint64_t (&b)[2]) {
-  float a0, a1, a2, a3, b0, b1, b2, b3;
-  tc::f2_unpack(a[0], a0, a1);
-  tc::f2_unpack(a[1], a2, a3);
-  tc::f2_unpack(b[0], b0, b1);
-  tc::f2_unpack(b[1], b2, b3);
-  Raw y;
-  if (INTER) {
-    y.a = make_uint2(tc::pack_bf16(a0, b0), tc::pack_bf16(a1, b1));
-    y.b = make_uint2(tc::pack_bf16(a2, b2), tc::pack_bf16(a3, b3));
-  } else {
-    y.a = make_uint2(tc::pack_bf16(a0, a1), tc::pack_bf16(a2, a3));
-    y.b = make_uint2(tc::pack_bf16(b0, b1), tc::pack_bf16(b2, b3));
-  }
-  return y;
-}
 
 // AXES: a position on each of several axes a row, the lane's pairs each by their own.
 template <bool APPEND, bool INTER, bool AXES>
@@ -210,29 +165,7 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
 
   // heads [a, b) of one tensor; `have`: x holds the first step's values
   auto pass = [&](const uint16_t* in, uint16_t* out, int a, int b, const uint16_t* norm, bool have) {
-    uint64_t ca[2], cb[2], sa[2], sb[2];  // factors of a and b: a' = ca a + sb b, b' = cb b + sa a
-    {
-      float wa[4] = {1.f, 1.f, 1.f, 1.f}, wb[4] = {1.f, 1.f, 1.f, 1.f};
-      if (norm) {
-        Raw w;
-        w.a = *reinterpret_cast<const uint2*>(norm + off_a);
-        w.b = *reinterpret_cast<const uint2*>(norm + off_b);
-        uint64_t pa[2], pb[2];
-        unpack<INTER>(w, pa, pb);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          tc::f2_unpack(pa[e], wa[2 * e], wa[2 * e + 1]);
-          tc::f2_unpack(pb[e], wb[2 * e], wb[2 * e + 1]);
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        ca[e] = tc::f2_pack(c[2 * e] * wa[2 * e], c[2 * e + 1] * wa[2 * e + 1]);
-        cb[e] = tc::f2_pack(c[2 * e] * wb[2 * e], c[2 * e + 1] * wb[2 * e + 1]);
-        sa[e] = tc::f2_pack(sn[2 * e] * wa[2 * e], sn[2 * e + 1] * wa[2 * e + 1]);
-        sb[e] = tc::f2_pack(-sn[2 * e] * wb[2 * e], -sn[2 * e + 1] * wb[2 * e + 1]);
-      }
-    }
+    const Factors f = factors<INTER>(c, sn, norm, off_a, off_b);
     for (int h0 = a; h0 < b; h0 += 2 * kUnroll) {
       if (!have) load(in, h0, b, x);
       have = false;
@@ -240,37 +173,11 @@ rope_kernel(const __grid_constant__ RopeArgs A) {
       for (int u = 0; u < kUnroll; ++u) {
         const int hh = h0 + 2 * u + half;
         if (h0 + 2 * u >= b) break;
-        uint64_t va[2], vb[2], ya[2], yb[2];
+        uint64_t va[2], vb[2];
         unpack<INTER>(x[u], va, vb);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          ya[e] = f2_mul(va[e], ca[e]);
-          yb[e] = f2_mul(vb[e], cb[e]);
-          if (rot) {  // a value that is not rotated must not meet 0 * infinity
-            ya[e] = tc::f2_fma(vb[e], sb[e], ya[e]);
-            yb[e] = tc::f2_fma(va[e], sa[e], yb[e]);
-          }
-        }
-        if (norm) {
-          uint64_t ss = f2_mul(va[0], va[0]);
-          ss = tc::f2_fma(va[1], va[1], ss);
-          ss = tc::f2_fma(vb[0], vb[0], ss);
-          ss = tc::f2_fma(vb[1], vb[1], ss);
-          float s0, s1;
-          tc::f2_unpack(ss, s0, s1);
-          s0 += s1;
-#pragma unroll
-          for (int o = 8; o > 0; o >>= 1) s0 += __shfl_xor_sync(0xffffffffu, s0, o);
-          const float rs = rsqrtf(s0 * (1.f / kD) + A.eps);
-          const uint64_t rs2 = tc::f2_pack(rs, rs);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            ya[e] = f2_mul(ya[e], rs2);
-            yb[e] = f2_mul(yb[e], rs2);
-          }
-        }
+        norm_rotate(va, vb, f, norm != nullptr, A.eps, rot);
         if (hh < b) {
-          const Raw y = pack<INTER>(ya, yb);
+          const Raw y = pack<INTER>(va, vb);
           *reinterpret_cast<uint2*>(out + hh * kD + off_a) = y.a;
           *reinterpret_cast<uint2*>(out + hh * kD + off_b) = y.b;
         }
