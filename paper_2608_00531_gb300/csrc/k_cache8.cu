@@ -29,7 +29,7 @@ using rope::Raw;
 constexpr int kThreads = 256;
 constexpr int kD = 128;
 constexpr int kBlk = CURE_KV8_BLOCK;
-static_assert(kBlk == 16, "16 rows in 8 steps of two");
+static_assert(kBlk == 16, "a half warp a slot, 16 lanes a row");
 
 // Four values as codes (ties to even; beyond 448: 448; NaN stays one), and back.
 __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d) {
@@ -192,9 +192,8 @@ __device__ __forceinline__ void value_of(const Raw& x, Slot what, float old, flo
 }
 
 // The page of a block of 16 slots, or the sequence's own range: the row of its slot 0 in the
-// cache and its place among the scales; false (error word set) where there is none.
-__device__ __forceinline__ bool place_of(const cure_kv_desc& kv, int seq, int blk, int64_t* row, int64_t* place, int* err,
-                                         bool tell) {
+// cache and its place among the scales; false where there is none.
+__device__ __forceinline__ bool place_of(const cure_kv_desc& kv, int seq, int blk, int64_t* row, int64_t* place) {
   if (kv.layout == 0) {
     *row = (int64_t)seq * kv.max_len + (int64_t)blk * kBlk;
     *place = (int64_t)seq * ((kv.max_len + kBlk - 1) / kBlk) + blk;
@@ -202,10 +201,7 @@ __device__ __forceinline__ bool place_of(const cure_kv_desc& kv, int seq, int bl
   }
   const int per = kv.page_size / kBlk;
   const int page = kv.block_table[(int64_t)seq * kv.max_len + blk / per];
-  if (page < 0 || page >= kv.num_pages) {
-    if (tell) flag(err, CURE_DEVERR_PAGE);
-    return false;
-  }
+  if (page < 0 || page >= kv.num_pages) return false;
   *place = (int64_t)page * per + blk % per;
   *row = *place * kBlk;
   return true;
@@ -276,7 +272,9 @@ append8_kernel(const __grid_constant__ Append8Args G) {
     }
     const int64_t slot = (int64_t)L + i;
     if (slot < 0 || slot >= cap) {
-      if (tell) flag(A.err, CURE_DEVERR_SLOT);
+      bool none = false;  // a row that holds no token needs no slot
+      for (int a = 0; A.pos && a < max(1, n_axes); ++a) none |= A.pos[(int64_t)a * A.rows + row] < 0;
+      if (tell && !none) flag(A.err, CURE_DEVERR_SLOT);
       ++row;
       continue;
     }
@@ -289,7 +287,7 @@ append8_kernel(const __grid_constant__ Append8Args G) {
     const int row0 = row;
     row += m;
     int64_t crow = 0, place = 0;
-    const bool there = place_of(A.kv, seq, blk, &crow, &place, A.err, tell);
+    const bool there = place_of(A.kv, seq, blk, &crow, &place);
 
     // Half warps 0 .. m - 1 have the rows, the last t0 what the block holds; for Q row r = hw % m.
     const int r = hw % m, t = (t0 + hw) & (kBlk - 1);
@@ -304,7 +302,11 @@ append8_kernel(const __grid_constant__ Append8Args G) {
       none = p < 0;
     }
     const Slot what = hw < m ? (none ? kNone : kFresh) : t < t0 && i == 0 ? kHeld : kNone;
-    if (!__syncthreads_or(what == kFresh) || !there) continue;  // (also: the block before is done with `part`)
+    if (!__syncthreads_or(what == kFresh)) continue;  // (also: the block before is done with `part`)
+    if (!there) {
+      if (tell) flag(A.err, CURE_DEVERR_PAGE);
+      continue;
+    }
 
     // cosines and sines of the lane's pairs
     float c[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
@@ -437,7 +439,10 @@ paths8_kernel(const __grid_constant__ Paths8Args A) {
   const int to = (int)min((int64_t)kBlk, min((int64_t)L + n, cap) - slot0);
   if (from >= to) return;
   int64_t crow, place;
-  if (!place_of(A.kv, b, blk, &crow, &place, A.err, tell)) return;
+  if (!place_of(A.kv, b, blk, &crow, &place)) {
+    if (tell) flag(A.err, CURE_DEVERR_PAGE);
+    return;
+  }
   Slot what = hw < from ? kHeld : kNone;
   int node = 0;
   if (hw >= from && hw < to) {

@@ -302,6 +302,27 @@ def test_append_errors(cure):
     assert cure.cure_device_error() & cure.DEVERR_NODES
 
 
+def test_append_rows_without_tokens_need_no_place(cure):
+    """Trees near the capacity, in place: rows behind a sequence's nodes may lie behind the cache and its pages."""
+    Hkv, n_max = 2, 20
+    for ps in (0, 16):
+        c = Cache(cure, [40, 33], Hkv, ps, 17 + ps)
+        lens, nodes = [c.kv.max_len * max(ps, 1) - 5, 28], [5, 5]
+        if ps:
+            c.table[1, 2:] = -1  # (sequence 1: 33 tokens in 3 pages, of which 2 hold what is written)
+            c.kv._keep.copy_(torch.from_numpy(c.table))
+            nodes[1] = 4
+        x = torch.randn(2 * n_max, Hkv, D, device=DEV).bfloat16()
+        pos = torch.full((2, n_max), -1, dtype=torch.int32, device=DEV)
+        for b in range(2):
+            pos[b, :nodes[b]] = lens[b]
+        before = c.copy()
+        cure.cure_append_kv8(x, x, *c.args(), _i32([0, n_max, 2 * n_max]), _i32(lens), None, pos=pos)
+        assert cure.cure_device_error() == 0
+        taken = [r % n_max < nodes[r // n_max] for r in range(2 * n_max)]
+        _check_append(c, before, lens, nodes, [0, n_max, 2 * n_max], (x, x), taken)
+
+
 # ---------------------------------------------------------------- attention
 def _attention_ref(x, q, b, end, mask):
     """Rows q [n][Hq][D] over the first `end` keys of sequence b (mask [n][end]: not seen): output and tolerance."""
@@ -400,6 +421,88 @@ def test_few_tokens(cure):
     for n in (2, 5, 8, 18, 19):
         x = _prompt(cure, [700, 5000, 0, 129], [n, 1, n, n], 28, 4, 32, n)
         _check(x, _run(cure, x))
+    assert cure.cure_device_error() == 0
+
+
+def test_few_rows_on_average(cure):
+    """Batches whose rows are few on average, all of them in one sequence: more units than one of it."""
+    for n in ([16, 0, 0, 0, 0, 0, 0, 0], [0, 9, 0, 1, 0, 2, 0, 0], [100] + [0] * 7, [0, 37, 0, 0, 0, 1, 0, 100]):
+        for Hq, Hkv in ((14, 2), (3, 3)):
+            x = _prompt(cure, [700, 5, 0, 129, 0, 16, 0, 40], n, Hq, Hkv, 16, sum(n) + Hq)
+            _check(x, _run(cure, x))
+    assert cure.cure_device_error() == 0
+
+
+def test_outputs_aligned_to_16_bytes(cure):
+    """Outputs that begin 16 bytes behind a 32-byte boundary, in each form of the attention."""
+    for lens, n, Hq in (([300, 0], [200, 70], 8), ([300, 1000, 50], [1, 1, 1], 8), ([1000, 30], [9, 12], 8)):
+        x = _prompt(cure, lens, n, Hq, 2, 16, 5)
+        buf = torch.full((x["q"].numel() + 8,), 3.5, dtype=torch.bfloat16, device=DEV)
+        out = buf[8:].view(x["q"].shape)
+        assert out.data_ptr() % 32 == 16
+        _check(x, _run(cure, x, out=out))
+        assert torch.all(buf[:8] == 3.5)
+    x = _tree(cure, [100, 500], [20, 9], 20, 8, 2, 16, 3)
+    want = _run_tree(cure, x)
+    buf = torch.full((x["q"].numel() + 8,), 3.5, dtype=torch.bfloat16, device=DEV)
+    got = cure.cure_tree_attn8(x["q"], *x["cache"].args(), x["cache_len"], x["n_nodes"], x["anc"], SCALE,
+                               out=buf[8:].view(x["q"].shape))
+    assert torch.equal(got, want) and torch.all(buf[:8] == 3.5) and cure.cure_device_error() == 0
+
+
+def test_caches_past_32_bits(cure):
+    """Pages whose codes lie 2^32 bytes and more behind the cache's beginning: append, attention of each form, commit."""
+    Hkv, ps, pages = 8, 64, 70000  # 4.6 GB of codes each
+    lens, n = [100, 200, 0], [30, 1, 300]
+    small = Cache(cure, [160, 260, 400], Hkv, ps, 4)
+    c = Cache.__new__(Cache)
+    c.Hkv, c.ps, c.table = Hkv, ps, small.table.copy()
+    c.table[c.table >= 0] += pages - small.codes[0].shape[0]
+    c.codes = [torch.empty(pages, ps, Hkv, D, dtype=torch.uint8, device=DEV).view(E4M3) for _ in range(2)]
+    c.scales = [torch.empty(pages, ps // BLK, Hkv, device=DEV) for _ in range(2)]
+    assert int(c.table[0, 0]) * ps * Hkv * D > 2 ** 32
+    k = small.codes[0].shape[0]
+    for w in (0, 1):
+        c.codes[w].view(torch.uint8)[-k:] = small.codes[w].view(torch.uint8)
+        c.scales[w][-k:] = small.scales[w]
+    c.kv = cure.kv_desc(Hkv, D, c.table.shape[1], block_table=torch.from_numpy(c.table).to(DEV), page_size=ps, num_pages=pages)
+    start = _packed(n, 0)
+    x = torch.randn(start[-1], Hkv, D, device=DEV).bfloat16()
+    tree = torch.randn(1, 3, 9, Hkv, D, device=DEV).bfloat16()
+    acc = dict(path_nodes=_i32([[0, 1, 2, -1, -1, -1]] * 3), accept_len=_i32([2] * 3), diverge_depth=_i32([-1] * 3),
+               out_tokens=_i32([[1] * 6] * 3))
+    q = torch.randn(start[-1], 16, D, device=DEV).bfloat16()
+    t = _tree(cure, [10, 20, 30], [9, 9, 9], 9, 16, Hkv, ps, 9)
+    outs = []
+    for at in (small, c):
+        cure.cure_append_kv8(x, -x, *at.args(), _i32(start), _i32(lens), None)
+        outs.append([cure.cure_prompt_attn8(q, *at.args(), _i32(start), _i32(lens), SCALE),
+                     cure.cure_prompt_attn8(q[:3].contiguous(), *at.args(), _i32([0, 1, 2, 3]), _i32(lens), SCALE),
+                     cure.cure_tree_attn8(t["q"], *at.args(), _i32(lens), t["n_nodes"], t["anc"], SCALE)])
+        cure.cure_resync_kv8([at.codes[0]], [at.codes[1]], [at.scales[0]], [at.scales[1]], at.kv, tree, tree, acc,
+                             _i32(lens), 4)
+    assert cure.cure_device_error() == 0
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+    for w in (0, 1):
+        assert torch.equal(c.codes[w].view(torch.uint8)[-k:], small.codes[w].view(torch.uint8))
+        assert torch.equal(c.scales[w][-k:].nan_to_num(nan=-1.0), small.scales[w].nan_to_num(nan=-1.0))
+
+
+def test_two_calls_at_once(cure):
+    """Calls of each form on two streams, with workspaces of their own."""
+    forms = [_prompt(cure, [0, 3000], [700, 5], 28, 4, 16, 1), _prompt(cure, [4000, 9000, 20], [1, 1, 1], 28, 4, 16, 2)]
+    want = [_run(cure, x).clone() for x in forms]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.full_like(x["q"], 3.5) for x in forms] for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s, o in zip(streams, outs):
+            for x, out in zip(forms, o):
+                cure.cure_prompt_attn8(x["q"], *x["cache"].args(), x["row_start"], x["cache_len"], SCALE, out=out, stream=s)
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(a, b) for a, b in zip(o, want))
     assert cure.cure_device_error() == 0
 
 
