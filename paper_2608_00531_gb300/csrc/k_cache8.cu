@@ -140,24 +140,24 @@ enum Slot { kNone, kHeld, kFresh };
 template <int N>
 __device__ __forceinline__ void quantise(float (&y)[N][8], Slot what, uint8_t* const (&codes)[N],
                                          float* const (&scale)[N], const float (&old)[N], const Lane& p,
-                                         float (*part)[16], int hw, int l16) {
+                                         uint32_t (*part)[kThreads / 32]) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     float amax = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(y[u][e]));  // (a NaN counts for nothing)
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    if (l16 == 0) part[u][hw] = what == kNone ? 0.f : amax;
+    // of both half warps' slots; as integers, which are ordered as the values are
+    const uint32_t top = __reduce_max_sync(0xffffffffu, what == kNone ? 0u : __float_as_uint(amax));
+    if (lane == 0) part[u][warp] = top;
   }
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     if (!codes[u]) break;
-    float amax = part[u][l16];
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    const int e = scale_exponent(amax);
+    const uint4 p0 = reinterpret_cast<const uint4*>(part[u])[0], p1 = reinterpret_cast<const uint4*>(part[u])[1];
+    const uint32_t top = max(max(max(p0.x, p0.y), max(p0.z, p0.w)), max(max(p1.x, p1.y), max(p1.z, p1.w)));
+    const int e = scale_exponent(__uint_as_float(top));
     const float s = power(e), inv = power(-e);
     if (what == kFresh || (what == kHeld && s != old[u])) {  // (what is held stays as it is under the same scale)
       *reinterpret_cast<uint32_t*>(codes[u] + p.off_a) =
@@ -165,7 +165,7 @@ __device__ __forceinline__ void quantise(float (&y)[N][8], Slot what, uint8_t* c
       *reinterpret_cast<uint32_t*>(codes[u] + p.off_b) =
           to_codes(y[u][4] * inv, y[u][5] * inv, y[u][6] * inv, y[u][7] * inv);
     }
-    if (hw == 0 && l16 == 0) *scale[u] = s;
+    if (threadIdx.x == 0) *scale[u] = s;
   }
 }
 
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 3)
 append8_kernel(const __grid_constant__ Append8Args G) {
   const RopeArgs& A = G.r;
   __shared__ uint64_t turns[64];
-  __shared__ float part[2][kHeads][16];
+  __shared__ __align__(16) uint32_t part[2][kHeads][kThreads / 32];
   if (threadIdx.x < 64) turns[threadIdx.x] = A.rope.turns[threadIdx.x];
   __syncthreads();
   pdl_begin();
@@ -330,38 +330,52 @@ append8_kernel(const __grid_constant__ Append8Args G) {
     // ---- heads of K, then of V
     const int64_t ld = (int64_t)Hkv * kD, at_slot = (crow + t) * ld;
     float w[8];
-#pragma unroll 1
-    for (int kv = 0; kv < 2; ++kv) {
+    if (A.k_norm) widen(load_raw(A.k_norm, turned), w);
+    const int groups = (Hkv + kHeads - 1) / kHeads;  // of K, and of V; the next one's values are on their way
+    Raw x[kHeads];
+    float old[kHeads];
+    auto load = [&](int g) {
+      const bool kv = g >= groups;
+      const int h = (kv ? g - groups : g) * kHeads;
+      const uint16_t* in = kv ? A.v + (row0 + hw) * A.ld_v : A.k + (row0 + hw) * A.ld_k;
+      const uint8_t* codes = reinterpret_cast<const uint8_t*>(kv ? A.v_out : A.k_out) + at_slot;
+      const float* scales = (kv ? G.v_scale : G.k_scale) + place * Hkv;
       const Lane lp = kv ? plain : turned;
-      const uint16_t* in = (kv ? A.v + (row0 + hw) * A.ld_v : A.k + (row0 + hw) * A.ld_k);
+#pragma unroll
+      for (int u = 0; u < kHeads; ++u) {
+        const bool is = g < 2 * groups && h + u < Hkv;
+        x[u] = load_slot(is ? what : kNone, in + (h + u) * kD, codes + (h + u) * kD, lp);
+        old[u] = is && t0 > 0 ? scales[h + u] : 1.f;
+      }
+    };
+    load(blockIdx.y);
+#pragma unroll 1
+    for (int g = blockIdx.y; g < 2 * groups; g += gridDim.y) {
+      const bool kv = g >= groups;
+      const int h = (kv ? g - groups : g) * kHeads;
+      const Lane lp = kv ? plain : turned;
       uint8_t* base = reinterpret_cast<uint8_t*>(kv ? A.v_out : A.k_out) + at_slot;
       float* scales = (kv ? G.v_scale : G.k_scale) + place * Hkv;
-      const bool norm = !kv && A.k_norm;
-      if (norm) widen(load_raw(A.k_norm, lp), w);
-      for (int h = blockIdx.y * kHeads; h < Hkv; h += gridDim.y * kHeads) {
-        Raw x[kHeads];
-        float old[kHeads], y[kHeads][8];
-        uint8_t* codes[kHeads];
-        float* scale[kHeads];
+      float y[kHeads][8], was[kHeads];
+      uint8_t* codes[kHeads];
+      float* scale[kHeads];
 #pragma unroll
-        for (int u = 0; u < kHeads; ++u) {
-          const bool is = h + u < Hkv;
-          codes[u] = is ? base + (h + u) * kD : nullptr;
-          scale[u] = scales + h + u;
-          x[u] = load_slot(is ? what : kNone, in + (h + u) * kD, codes[u], lp);
-          old[u] = is && t0 > 0 ? *scale[u] : 1.f;
-        }
-#pragma unroll
-        for (int u = 0; u < kHeads; ++u) {
-          value_of(x[u], what, old[u], y[u]);
-          if (!kv) {
-            const float rs = norm ? norm_factor(y[u], A.eps) : 1.f;  // (all lanes, whatever they have)
-            if (what == kFresh) norm_rotate<INTER>(y[u], w, norm, rs, c, sn, lp.rot);
-          }
-        }
-        quantise(y, what, codes, scale, old, lp, part[buf], hw, l16);
-        buf ^= 1;
+      for (int u = 0; u < kHeads; ++u) {
+        codes[u] = h + u < Hkv ? base + (h + u) * kD : nullptr;
+        scale[u] = scales + h + u;
+        was[u] = old[u];
+        value_of(x[u], what, was[u], y[u]);
       }
+      load(g + gridDim.y);
+      if (!kv) {
+#pragma unroll
+        for (int u = 0; u < kHeads; ++u) {
+          const float rs = A.k_norm ? norm_factor(y[u], A.eps) : 1.f;  // (all lanes, whatever they have)
+          if (what == kFresh) norm_rotate<INTER>(y[u], w, A.k_norm != nullptr, rs, c, sn, lp.rot);
+        }
+      }
+      quantise(y, what, codes, scale, was, lp, part[buf]);
+      buf ^= 1;
     }
 
     // ---- heads of Q: half warp hw those of row hw % m from the (hw / m)-th on
@@ -418,7 +432,7 @@ struct Paths8Args {
 // The k-th block that sequence b's accepted path reaches (blockIdx.x = b * blocks + k).
 __global__ void __launch_bounds__(kThreads, 3)
 paths8_kernel(const __grid_constant__ Paths8Args A) {
-  __shared__ float part[2][kHeadsP][16];
+  __shared__ __align__(16) uint32_t part[2][kHeadsP][kThreads / 32];
   pdl_begin();
   const int tid = threadIdx.x, l16 = tid & 15, hw = tid >> 4;
   const int blocks = (A.block + 1 + kBlk - 2) / kBlk + 1;
@@ -474,7 +488,7 @@ paths8_kernel(const __grid_constant__ Paths8Args A) {
     }
 #pragma unroll
     for (int u = 0; u < kHeadsP; ++u) value_of(x[u], what, old[u], y[u]);
-    quantise(y, what, codes, scale, old, plain, part[buf], hw, l16);
+    quantise(y, what, codes, scale, old, plain, part[buf]);
     buf ^= 1;
   }
 }
