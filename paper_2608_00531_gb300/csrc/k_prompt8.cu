@@ -20,17 +20,26 @@
 //
 // Units, pieces and the scheduler are those of the bf16 kernel (prompt_units.cuh).  Roles (16
 // warps):
-//   warps 0-3 / 4-7   softmax of M tile 0 / 1, a thread a row
-//   warp 8            TMA producer: K and V tiles (16 KiB each), and their blocks' scales
+//   warps 0-3 / 4-7   Q of M tile 0 / 1 into its parts, and its softmax, a thread a row
+//   warp 8            TMA producer: Q, K and V tiles (16 KiB each), and the blocks' scales
 //   warp 9            issues S = Q K^T (M128 N128, K 2 x 128) of M tiles 0 and 1 in turn
 //   warp 10           issues O += P' V (A = P' from TMEM)
 //   warp 11           lays out the CTA's pieces of work
-//   warps 12-15       Q (by TMA) into its parts, V tiles to fp16, and the epilogue: a piece's rows go
-//                     out once the next one's Q and first V tile are on their way
+//   warps 12-15       V tiles to fp16, and the epilogue: a piece's rows go out behind the next one's
+//                     first V tile
 // TMEM as there: S (128) | P[2] (64 each) | O[2] (128 each).  A piece whose rows fit one M
 // tile (single tokens, small trees) takes its tiles in turn with both softmax groups, each
 // with an O and sums of its own, which the epilogue adds up: a group's exponentials would
 // otherwise take longer than a tile's bytes.
+//
+// Bound: a tile of 128 keys and two M tiles takes 1.43 us, most of it the softmax warps' 256 x 128
+// exponentials, sums and conversions (with the exponentials left out a document takes a quarter
+// less; the products' own time is 1.1), and a unit about 5 us on top until its first scores are there
+// and its last rows out.  One document of 16384 tokens, 64 heads and 8 of K and V: 3.0 ms, 1.46 PFLOP/s
+// of the attention's operations; 32 prompts of 33 to 4096 tokens, 28 heads and 4: 263 us.  There, Q
+// taken apart by warps 12-15 in front of the piece's V tiles took 288, Q asked for behind the first V
+// tile instead of in front of the first K tile 269.  Registers of a thread for softmax, warps 12-15 and
+// the rest: 168 / 88 / 88 (184 / 80 / 64 takes 274, 160 / 104 / 88 282; a few words spill in each).
 #include "prompt8.cuh"
 
 namespace cure {
@@ -53,7 +62,8 @@ struct Layout {
   static constexpr int m_tiles = MT, threads = kThreads;
   static constexpr int NK = MT == 1 ? 4 : 3, NV = MT == 1 ? 3 : 2, NW = 2;  // stages: K tiles, V tiles, V tiles in fp16
   enum : int {
-    B_QFULL = 0, B_QEMPTY = 2, B_QRAW, B_SFREE, B_KFULL, B_KEMPTY = B_KFULL + NK, B_VFULL = B_KEMPTY + NK, B_VEMPTY = B_VFULL + NV,
+    B_QFULL = 0, B_QRAW = 2, B_QEMPTY = 4, B_SFREE = 6,
+    B_KFULL, B_KEMPTY = B_KFULL + NK, B_VFULL = B_KEMPTY + NK, B_VEMPTY = B_VFULL + NV,
     B_WFULL = B_VEMPTY + NV, B_WEMPTY = B_WFULL + NW, B_SFULL = B_WEMPTY + NW, B_PFULL = B_SFULL + 2,
     B_PVDONE = B_PFULL + 2, B_STAT = B_PVDONE + 2, B_OFREE = B_STAT + 2, B_DRAIN = B_OFREE + 2, B_JOIN = B_DRAIN + 2,
     B_SCALES = B_JOIN + 1, piece_bar = B_SCALES + kScaleSlots, taken_bar = piece_bar + kPieces,
@@ -225,7 +235,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     mbar_init(bar(Lay::B_QFULL), BM);
     mbar_init(bar(Lay::B_QFULL + 1), BM);
     mbar_init(bar(Lay::B_QEMPTY), 1);
+    mbar_init(bar(Lay::B_QEMPTY + 1), 1);
     mbar_init(bar(Lay::B_QRAW), 1);
+    mbar_init(bar(Lay::B_QRAW + 1), 1);
     mbar_init(bar(Lay::B_SFREE), BM);
     for (int i = 0; i < NK; ++i) {
       mbar_init(bar(Lay::B_KFULL + i), 1);
@@ -285,12 +297,62 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     uint32_t sc = 0, quads = 0, pc = 0;  // tiles of this group, quads and pieces of the CTA
     bool ok = true;
     uint32_t done = 0;  // pieces of this group
+    // Q of the group's M tile: bf16 rows (dims 0-63 where q1 goes, the others in q2's place), which each thread
+    // takes out and puts back as its row's parts
+    uint32_t got = 0;
+    const uint32_t q_row = sb + Lay::q + m * 2 * kQHalf + row * 128;
     while (ok && pieces.next<Lay>(await, bar, smem, aborted, x)) {
       const uint32_t at = quads * kQuad;  // the piece's first place among the scales
       quads += (uint32_t)(x.t1 - x.t0 + kQuad - 1) / kQuad;
       const bool two = two_tiles(x);
       const int mq = two ? m : 0, step = two ? 1 : 2;  // the M tile whose rows these are
       const int first = x.t0 + m - mq;
+      if (two || m == 0) {
+        if (!await(bar(Lay::B_QRAW + m), got++ & 1u, aborted)) break;
+        uint4 w[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) w[k] = ld_shared_v4(q_row + (k >> 3) * kQHalf + (((k & 7) ^ (row & 7)) << 4));
+        if (row >= npb * G || (MT * x.rg + m) * npb + row / G >= x.n) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) w[k] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        // the row's largest value: bf16 magnitudes in order as integers, two at a time
+        __nv_bfloat162 big = __float2bfloat162_rn(0.f);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) big = __hmax2(big, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&u[e])));
+        }
+        const float amax = fmaxf(__low2float(big), __high2float(big));
+        // 2^e, the least with amax <= 448 * 2^e (448 = 1.75 * 2^8), not below 2^-60
+        const uint32_t bits = __float_as_uint(amax);
+        const int e = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -60), 120);
+        q_scale[((pc & 1u) * 2 + m) * BM + row] = __uint_as_float((uint32_t)(127 + e) << 23);
+        const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {  // 16 dims
+          const uint32_t in[8] = {w[2 * u].x,     w[2 * u].y,     w[2 * u].z,     w[2 * u].w,
+                                  w[2 * u + 1].x, w[2 * u + 1].y, w[2 * u + 1].z, w[2 * u + 1].w};
+          uint32_t q1[4], q2[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t f[2], r[2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z)
+              f[z] = pack_f16(__uint_as_float(in[2 * k + z] << 16) * inv,
+                              __uint_as_float(in[2 * k + z] & 0xffff0000u) * inv);
+            q1[k] = narrow(f[0], f[1]);
+            widen(q1[k], r[0], r[1]);
+            q2[k] = narrow(sub_f16x2(f[0], r[0]), sub_f16x2(f[1], r[1]));
+          }
+          const uint32_t to = q_row + ((u ^ (row & 7)) << 4);
+          st_shared_v4(to, q1[0], q1[1], q1[2], q1[3]);
+          st_shared_v4(to + kQHalf, q2[0], q2[1], q2[2], q2[3]);
+        }
+        fence_proxy_async_smem();
+        mbar_arrive(bar(Lay::B_QFULL + m));
+      }
       const float* qs = q_scale + ((pc++ & 1u) * 2 + mq) * BM + row;
       if (first >= x.t1) continue;
       const int i0 = (MT * x.rg + mq) * npb;
@@ -315,9 +377,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         for (int q = 0; q < 4; ++q) tmem_ld32(tS + 32 * q, v[q]);
         tmem_wait_ld();
         tc_fence_before();
-        mbar_arrive(bar(Lay::B_SFREE));  // the next product may take S
-        // (within bounds where a block's factor is never 0, which would meet -infinity)
+        // The row's factor, read before S is given back: that of the piece after the next takes its place.
+        // (Within bounds where a block's factor is never 0, which would meet -infinity.)
         if (t == first) c = fminf(fmaxf(A.scale_log2 * *qs, 0x1p-80f), 0x1p80f);
+        mbar_arrive(bar(Lay::B_SFREE));  // the next product may take S
         // The tile's scales (the S product has waited for them).  They stay for as long as it takes: their
         // slot is written again for the eighth quad from here, once S of all but its last three tiles is done.
         const float4* scales =
@@ -427,12 +490,12 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       ++done;
     }
   } else if (warp >= 12) {
-    // ================================================================ Q, V tiles, epilogue
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    // ================================================================ V tiles, epilogue
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     const int row = tid & 127;  // row within an M tile = TMEM lane
     const uint32_t tO = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColO;
     const bool wide = (reinterpret_cast<uintptr_t>(A.out) & 31) == 0;
-    uint32_t done0 = 0, done1 = 0, tiles0 = 0, tiles1 = 0, joins = 0, pc = 0, vt = 0, q_raw = 0;
+    uint32_t done0 = 0, done1 = 0, tiles0 = 0, tiles1 = 0, joins = 0, vt = 0;
     bool ok = true, have = false;
     Piece* kept = reinterpret_cast<Piece*>(smem + Lay::kept) + (warp & 3);  // (registers are short)
     // The epilogue's threads meet (an mbarrier, for a wait that ends when the CTA gives up).
@@ -443,71 +506,6 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     while (ok) {
       const bool more = pieces.next<Lay>(await, bar, smem, aborted, x);
       if (!more && !have) break;
-      if (more) {
-        // ---- Q of the piece, once the S products of the one before are done: bf16 rows by TMA (dims 0-63
-        // where q1 goes, the others in q2's place), which each thread takes out and puts back as its row's parts
-        if (!await(bar(Lay::B_QEMPTY), (pc & 1u) ^ 1u, aborted)) break;
-        const int mts = two_tiles(x) ? 2 : 1;
-        if (warp == 12) {
-          if (lane == 0) mbar_arrive_expect_tx(bar(Lay::B_QRAW), (uint32_t)(2 * mts * npb * G * 128));
-          __syncwarp();
-          if (lane < 2 * mts)  // M tile lane / 2, d half lane % 2
-            tma_load_4d(sb + Lay::q + lane * kQHalf, &tm_q, bar(Lay::B_QRAW), (lane & 1) * 64, 0, x.h,
-                        x.r0 + (MT * x.rg + (lane >> 1)) * npb);
-          __syncwarp();
-        }
-        q_raw = pc + 1;
-        if (!await(bar(Lay::B_QRAW), pc & 1u, aborted)) break;
-#pragma unroll 1
-        for (int m = 0; m < mts; ++m) {
-          const int i = (MT * x.rg + m) * npb + row / G;
-          const uint32_t dst = sb + Lay::q + m * 2 * kQHalf + row * 128;
-          uint4 w[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) w[k] = ld_shared_v4(dst + (k >> 3) * kQHalf + (((k & 7) ^ (row & 7)) << 4));
-          if (row >= npb * G || i >= x.n) {
-#pragma unroll
-            for (int k = 0; k < 16; ++k) w[k] = make_uint4(0u, 0u, 0u, 0u);
-          }
-          // the row's largest value: bf16 magnitudes in order as integers, two at a time
-          __nv_bfloat162 big = __float2bfloat162_rn(0.f);
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) big = __hmax2(big, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&u[e])));
-          }
-          const float amax = fmaxf(__low2float(big), __high2float(big));
-          // 2^e, the least with amax <= 448 * 2^e (448 = 1.75 * 2^8), not below 2^-60
-          const uint32_t bits = __float_as_uint(amax);
-          const int e = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -60), 120);
-          q_scale[((pc & 1u) * 2 + m) * BM + row] = __uint_as_float((uint32_t)(127 + e) << 23);
-          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {  // 16 dims
-            const uint32_t in[8] = {w[2 * u].x,     w[2 * u].y,     w[2 * u].z,     w[2 * u].w,
-                                    w[2 * u + 1].x, w[2 * u + 1].y, w[2 * u + 1].z, w[2 * u + 1].w};
-            uint32_t q1[4], q2[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              uint32_t f[2], r[2];
-#pragma unroll
-              for (int z = 0; z < 2; ++z)
-                f[z] = pack_f16(__uint_as_float(in[2 * k + z] << 16) * inv,
-                                __uint_as_float(in[2 * k + z] & 0xffff0000u) * inv);
-              q1[k] = narrow(f[0], f[1]);
-              widen(q1[k], r[0], r[1]);
-              q2[k] = narrow(sub_f16x2(f[0], r[0]), sub_f16x2(f[1], r[1]));
-            }
-            const uint32_t to = dst + ((u ^ (row & 7)) << 4);
-            st_shared_v4(to, q1[0], q1[1], q1[2], q1[3]);
-            st_shared_v4(to + kQHalf, q2[0], q2[1], q2[2], q2[3]);
-          }
-          fence_proxy_async_smem();
-          mbar_arrive(bar(Lay::B_QFULL + m));
-        }
-        ++pc;
-      }
       for (int t = more ? x.t0 : 0, t_end = more ? x.t1 : 1; ok && t < t_end; ++t) {
         if (more) {
           // ---- a V tile to fp16: 16 codes a load; keys behind the unit's last one count as zeros,
@@ -642,16 +640,15 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       __syncwarp();
       have = true;
     }
-    if (*abort_flag && q_raw > 0)  // let the copies in flight land before the CTA's smem goes away
-      wait_bounded(bar(Lay::B_QRAW), (q_raw - 1) & 1u, abort_flag, A.err, false);
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 8) {
       // ================================================================ producer
       const int ps = A.kv.page_size;
       const bool paged = A.kv.layout == 1;
       const int ppt = paged ? BN / ps : 0;  // pages (boxes) of a tile: 2 .. 8
       uint32_t kt = 0, vt = 0, quads = 0;   // tiles issued, quads whose scales are out
+      uint32_t q0 = 0, q1 = 0;              // pieces whose M tile of Q is issued
       while (pieces.next<Lay>(await, bar, smem, aborted, x)) {
         // Pages and scales are looked up a quad of tiles at a time, two quads and one ahead of their
         // use (one tile ahead, a tile took as long as a load).  Lane 8 i + p: page p of the quad's tile
@@ -696,7 +693,22 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           ++quads;
           unsaid = false;
         };
-        // K and V tiles, each as soon as it has a free stage
+        // Q of the piece, an M tile once the S products of the one before in its place are done
+        auto ask = [&]() -> bool {
+          for (int m = 0; m < (two_tiles(x) ? 2 : 1); ++m) {
+            if (!await(bar(Lay::B_QEMPTY + m), ((m ? q1 : q0) & 1u) ^ 1u, aborted)) return false;
+            if (m) ++q1;
+            else ++q0;
+            if (lane == 0) mbar_arrive_expect_tx(bar(Lay::B_QRAW + m), (uint32_t)(2 * npb * G * 128));
+            __syncwarp();
+            if (lane < 2)
+              tma_load_4d(sb + Lay::q + (2 * m + lane) * kQHalf, &tm_q, bar(Lay::B_QRAW + m), lane * 64, 0, x.h,
+                          x.r0 + (MT * x.rg + m) * npb);
+            __syncwarp();
+          }
+          return true;
+        };
+        if (!ask()) goto produced;
         for (int ik = 0, iv = 0; iv < nt;) {
           const bool is_v = ik == nt || ik > iv + 1;
           if (unsaid && (is_v ? iv > 0 : ik % kQuad == 0)) say();
@@ -744,6 +756,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           wait_bounded(bar(Lay::B_KFULL + i % NK), (i / NK) & 1u, abort_flag, A.err, false);
         for (uint32_t i = (vt > NV ? vt - NV : 0); i < vt; ++i)
           wait_bounded(bar(Lay::B_VFULL + i % NV), (i / NV) & 1u, abort_flag, A.err, false);
+        if (q0 > 0) wait_bounded(bar(Lay::B_QRAW), (q0 - 1) & 1u, abort_flag, A.err, false);
+        if (q1 > 0) wait_bounded(bar(Lay::B_QRAW + 1), (q1 - 1) & 1u, abort_flag, A.err, false);
       }
     } else if (warp == 9) {
       // ================================================================ S products
@@ -768,9 +782,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             issue_s(tmem + kColS, (uint32_t)qd + m * (2 * kQHalf >> 4), (uint32_t)(qd >> 32),
                     (uint32_t)kd + st * (kTile >> 4), (uint32_t)(kd >> 32), idS,
                     bar(Lay::B_SFULL + (two ? m : (t - x.t0) & 1)));
+            if (t == x.t1 - 1) commit_elect(bar(Lay::B_QEMPTY + m));  // the piece's last use of the M tile of Q
           }
           commit_elect(bar(Lay::B_KEMPTY + st));
-          if (t == x.t1 - 1) commit_elect(bar(Lay::B_QEMPTY));  // the piece's last use of Q
         }
       }
     scored:
