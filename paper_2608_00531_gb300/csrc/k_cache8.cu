@@ -12,9 +12,18 @@
 // Layout.  A CTA takes the blocks that begin in its range of packed rows (a block's rows in
 // one call are neighbours).  Each of its 16 half warps has one slot of a block for all heads, 8 values a
 // lane: a row of the call, with the row's cosines and sines in registers, or one that the block
-// holds already.  kHeads heads of K and V at a time are loaded, normed and turned, and their rows' largest
-// values meet in shared memory; behind the barrier each half warp writes its codes.  Heads of Q go the
-// same way without meeting; where a block gains few rows, all half warps share those rows' heads.
+// holds already.  Two or four heads of K and V at a time are loaded, normed and turned, and their rows'
+// largest values meet in shared memory; behind the barrier each half warp writes its codes, while the next
+// heads' values are on their way.  Heads of Q go the same way without meeting; where a block gains few
+// rows, all half warps share those rows' heads.
+//
+// Bound: latency.  A block is a chain of look-ups (sequence, length, page: 2.5 us), its rows' angles, and
+// a meeting of 1 to 1.5 us for each group of heads.  Single tokens of 200 sequences (32 and 8 heads): 12.5 us;
+// 19241 rows in 32 chunks behind cached ones (28 and 4 heads, norms, three axes): 91 us, 3.7 TB/s, of which
+// finding the places takes 20 us, K and V 40 and Q 45 when left out in turn.  A head a warp with its 16 rows
+// in registers took 143 us there (100 KB of code), rows staged in shared memory 117, Q in a launch of its own
+// 116.  The accepted paths' rows (a block's four heads of one layer at a time, no rotation): 32 paths in 28
+// layers 19 us with the lengths' launch.
 #include <algorithm>
 
 #include "rope_math.cuh"
@@ -129,8 +138,7 @@ __device__ __forceinline__ float norm_factor(const float* y, float eps) {
   return rsqrtf(ss * (1.f / kD) + eps);
 }
 
-constexpr int kHeads = 2;   // of K and V between two barriers: in the append
-constexpr int kHeadsP = 4;  // .. in the commit
+constexpr int kHeadsP = 4;  // of K and V between two barriers: in the commit
 
 // What a half warp has in the slot of its block.
 enum Slot { kNone, kHeld, kFresh };
@@ -213,8 +221,11 @@ struct Append8Args {
   int range;  // packed rows whose blocks a CTA takes
 };
 
-template <bool INTER>
-__global__ void __launch_bounds__(kThreads, 3)
+// CTAs to an SM, with kHeads heads of K or V between two barriers.
+constexpr int resident(int kHeads) { return kHeads == 2 ? 3 : 2; }
+
+template <bool INTER, int kHeads>
+__global__ void __launch_bounds__(kThreads, resident(kHeads))
 append8_kernel(const __grid_constant__ Append8Args G) {
   const RopeArgs& A = G.r;
   __shared__ uint64_t turns[64];
@@ -504,11 +515,21 @@ cudaError_t launch_append8(const RopeArgs& args, float* k_scale, float* v_scale,
   a.range = 1;
   while (a.range < kBlk && (int64_t)2 * a.range * args.batch <= args.rows) a.range *= 2;
   const int64_t ctas = ((int64_t)args.rows + a.range - 1) / a.range;
-  // few blocks: their heads in parts
-  const int64_t want = (int64_t)num_sms() * 3;
-  const int most = std::max((args.heads_kv + kHeads - 1) / kHeads, (args.heads_q + 7) / 8);
-  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(want / ctas, most));
-  auto kernel = args.rope.style == 1 ? append8_kernel<true> : append8_kernel<false>;
+  // Few blocks: their heads in parts, a pair of heads each where that leaves every SM at most one CTA.
+  const int64_t sms = num_sms();
+  const int groups = (args.heads_kv + 1) / 2;  // pairs of heads of K, and of V
+  const int most = ctas * 2 * groups <= sms ? 2 * groups : std::max(groups, (args.heads_q + 7) / 8);
+  auto parts_of = [&](int heads) -> int {
+    return (int)std::max<int64_t>(1, std::min<int64_t>(sms * resident(heads) / ctas, most));
+  };
+  // Calls of few rows wait for meetings: four heads meet at a time, in fewer CTAs to an SM.  Single tokens of
+  // 64 / 300 / 500 sequences 8.8 -> 7.0, 18.0 -> 12.8, 26.7 -> 22.9 us (8 heads of K and V), 32 trees of 33
+  // rows 22.2 -> 18.0, 100 of 9 rows 19.9 -> 20.3.  Longer calls want the CTAs: 32 chunks of 100 rows 33.8 with
+  // two heads, 39.3 with four; 19241 rows 91 and 94.
+  const bool four = args.rows < 8 * sms && parts_of(2) < 2 * groups;
+  const int parts = parts_of(four ? 4 : 2);
+  auto kernel = args.rope.style == 1 ? four ? append8_kernel<true, 4> : append8_kernel<true, 2>
+                                     : four ? append8_kernel<false, 4> : append8_kernel<false, 2>;
   return launch_pdl(kernel, dim3((unsigned)ctas, (unsigned)parts), dim3(kThreads), 0, s, a);
 }
 
