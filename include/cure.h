@@ -523,9 +523,8 @@ cure_status cure_append_kv_axes(const void* q, const void* k, const void* v, int
 /*
  * cure_append_kv (cure_append_kv_axes) into a cache in 8 bits.  Arguments, and which rows
  * are left out with which error, are theirs; all values are computed in float32 and
- * rounded once.  A sequence's rows up to the first that is left out for its slot or
- * page count for its blocks; a row with pos < 0 between others leaves its slot without
- * meaning.  Caches 16-byte aligned, scales 4-byte.  No two rows of a call may lie in the
+ * rounded once.  A row that is left out does not count for its block's scale; one with
+ * pos < 0 among others leaves its slot without meaning.  Caches 16-byte aligned, scales 4-byte.  No two rows of a call may lie in the
  * same block of the same page, unless they are of one sequence.  row_start must
  * ascend: where it does not, rows are left out with CURE_DEVERR_NODES, or written
  * for a sequence whose range holds them.
@@ -544,6 +543,8 @@ cure_status cure_append_kv8(const void* q, const void* k, const void* v, int64_t
  * Scores: q in two e4m3 parts, which hold it but for 2^-18 of its row's largest value;
  * products of e4m3 in float32.  A probability times its block's scale is
  * rounded to fp16, by up to 2^-11 of itself, or 2^-32 of the row's largest such term.
+ * q must be finite, and V's codes in a sequence's own slots must not be NaN (K's may be
+ * where a row does not see them).
  */
 cure_status cure_prompt_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
                               const float* v_scale, const cure_kv_desc* kv, const int32_t* row_start,
@@ -561,7 +562,8 @@ size_t cure_prompt_attn8_workspace_size(int32_t rows, int32_t batch, int32_t hea
  * no key).  Rows j >= n_nodes[b] are left unwritten, and so are the rows of a sequence
  * with n_nodes[b] outside 1 .. n_max (CURE_DEVERR_NODES) or that does not fit its capacity
  * (CURE_DEVERR_SLOT); a missing or bad page counts as zeros (CURE_DEVERR_PAGE).  n_max <= 256,
- * batch <= 256, heads_q / heads_kv <= 128.  Roundings and workspace rules as for cure_prompt_attn8.
+ * batch <= 256, heads_q / heads_kv <= 128.  Roundings, workspace rules, and what q and V must
+ * not hold (the tree's own slots included) as for cure_prompt_attn8.
  */
 cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
                             const float* v_scale, const cure_kv_desc* kv, const int32_t* cache_len,

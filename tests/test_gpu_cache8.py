@@ -198,6 +198,22 @@ def test_append_exact(cure, ps, Hq, Hkv):
     assert cure.cure_device_error() == 0
 
 
+@pytest.mark.parametrize("n", [[700, 9, 0, 801], [3] * 500, [1] * 300, [1], [17, 1, 16]])
+@pytest.mark.parametrize("Hq,Hkv", [(28, 4), (5, 5), (2, 2)])
+def test_append_many_and_few_rows(cure, n, Hq, Hkv):
+    """Rows without a rotation: the values themselves, whatever heads meet at a time."""
+    lens = [(7 * b) % 37 for b in range(len(n))]
+    c = Cache(cure, [a + b for a, b in zip(lens, n)], Hkv, 16, len(n) + Hkv)
+    start = _packed(n, 0)
+    g = torch.Generator(device=DEV).manual_seed(6)
+    k, v, q = (torch.empty(start[-1], h, D, dtype=torch.bfloat16, device=DEV).normal_(0.0, 2.0, generator=g)
+               for h in (Hkv, Hkv, Hq))
+    before = c.copy()
+    got = cure.cure_append_kv8(k, v, *c.args(), _i32(start), _i32(lens), None, q=q)
+    _check_append(c, before, lens, n, start, (k.double(), v.double()))
+    assert torch.equal(got, q) and cure.cure_device_error() == 0
+
+
 @pytest.mark.parametrize("style,rot,norm,axes", [("half", 128, False, None), ("interleaved", 128, True, None),
                                                  ("half", 64, True, "runs"), ("interleaved", 96, False, "turns"),
                                                  ("half", 128, True, "turns")])
@@ -662,6 +678,35 @@ def test_tree_long_batch_and_errors(cure):
     assert cure.cure_device_error() == cure.DEVERR_SLOT and torch.all(got[0] == 3.5)
 
 
+@pytest.mark.parametrize("lens,n_max", [([4096], 25), ([3000, 100, 900, 0] * 4, 33), ([700], 200)])
+def test_tree_same_bits_streams_and_graphs(cure, lens, n_max):
+    """Call after call, on another stream, in two graphs with workspaces of their own."""
+    x = _tree(cure, lens, [n_max] * len(lens), n_max, 28, 4, 16, n_max)
+    first = _run_tree(cure, x).clone()
+    _check_tree(x, first)
+    assert torch.equal(_run_tree(cure, x), first)
+    s, out = torch.cuda.Stream(), torch.full_like(x["q"], 3.5)
+    torch.cuda.synchronize()
+    args = (x["q"], *x["cache"].args(), x["cache_len"], x["n_nodes"], x["anc"], SCALE)
+    cure.cure_tree_attn8(*args, out=out, stream=s)
+    s.synchronize()
+    assert torch.equal(out, first)
+    size = cure.cure_tree_attn8_workspace_size(len(lens), n_max, 28, x["cache"].kv)
+    graphs, outs = [], []
+    for _ in range(2):
+        ws, o = torch.empty(size, dtype=torch.uint8, device=DEV), torch.full_like(x["q"], 3.5)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cure.cure_tree_attn8(*args, out=o, workspace=ws)
+        graphs.append((g, ws))
+        outs.append(o)
+    for _ in range(3):
+        graphs[0][0].replay()
+        graphs[1][0].replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], first) and torch.equal(outs[1], first) and cure.cure_device_error() == 0
+
+
 # ---------------------------------------------------------------- commit
 @pytest.mark.parametrize("ps", [0, 16, 64])
 @pytest.mark.parametrize("K,layers", [(16, 3), (32, 1), (1, 2)])
@@ -840,4 +885,53 @@ def test_prompt_then_steps(cure):
                     assert torch.all((v - want).abs() <= tol)
         cache_len = r["resync"]["cache_len"].clone()
         assert cache_len.tolist() == [x + y + 1 for x, y in zip(L, a)]
+    assert cure.cure_device_error() == 0
+
+
+def test_captured_passes_and_steps(cure):
+    """A prompt's pass and the step behind it, captured and replayed, write and give what they do when called."""
+    from paper_2608_00531_gb300.step import PromptPass, RepairVerifyStep, StepInputs
+    B, K, V, R, layers, Hq, Hkv, n = 3, 8, 512, 6, 2, 8, 2, [40, 7, 129]
+    n_max, start = 1 + K + R, _packed(n, 0)
+    g = torch.Generator(device=DEV).manual_seed(78)
+    rnd = lambda *s: torch.empty(s, dtype=torch.bfloat16, device=DEV).normal_(0.0, 1.0, generator=g)  # noqa: E731
+    caches = [Cache(cure, [x + 60 for x in n], Hkv, 0, 8 + l) for l in range(layers)]
+    kv = caches[0].kv
+    p = PromptPass(start[-1], B, Hq, kv, cure.rope_desc(128, 1e6), DEV)
+    step = RepairVerifyStep(B, K, V, 3, 1.0, R, 2, 1, layers, Hq, kv, DEV)
+    ks, vs = [c.codes[0] for c in caches], [c.codes[1] for c in caches]
+    scales = ([c.scales[0] for c in caches], [c.scales[1] for c in caches])
+    row_start, none, held = _i32(start), _i32([0] * B), _i32(n)
+    qkv = [rnd(start[-1], (Hq + 2 * Hkv) * D) for _ in range(layers)]
+    x = StepInputs(rnd(B, K, V), _i32([0] * B), held, None, rnd(layers, B, n_max, Hq, D), rnd(layers, B, n_max, Hkv, D),
+                   rnd(layers, B, n_max, Hkv, D), rnd(B, n_max, V))
+    outs = [torch.empty(start[-1], Hq, D, dtype=torch.bfloat16, device=DEV) for _ in range(layers)]
+
+    def run():
+        for l, c in enumerate(caches):
+            p.layer(l, qkv[l], row_start, none, *c.codes, scales=c.scales, out=outs[l])
+        return step.run(x, ks, vs, scales=scales)
+
+    state = [t for c in caches for t in (*(k.view(torch.uint8) for k in c.codes), *c.scales)]
+    fresh = [t.clone() for t in state]
+    with pytest.raises(RuntimeError, match="before it is captured"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            run()
+    r = run()
+    nn = r["tree"]["n_nodes"].tolist()
+    rows = [(l, b, slice(0, nn[b])) for l in range(layers) for b in range(B)]
+    want = [t.clone() for t in (*outs, *(r["attn"][i] for i in rows), *state, *r["resync"].values())]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = run()
+    for _ in range(2):
+        for t, f in zip(state, fresh):
+            t.copy_(f)
+        for t in (*outs, r["attn"], *r["resync"].values()):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = (*outs, *(r["attn"][i] for i in rows), *state, *r["resync"].values())
+        assert len(got) == len(want)
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(got, want))
     assert cure.cure_device_error() == 0
