@@ -676,10 +676,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           return make_float2(__ldg(A.k_scale + place * A.kv.heads_kv + x.h), __ldg(A.v_scale + place * A.kv.heads_kv + x.h));
         };
         const int nt = x.t1 - x.t0;
-        // of the quad before, this one (the last K tile's) and the next one
-        int pages_1 = -1, pages0 = pages_of(0), pages1 = pages_of(1);
+        // of this quad and the next one
+        int pages0 = pages_of(0), pages1 = pages_of(1);
         float2 scales0 = scales_of(0, pages0), scales1;
-        bool unsaid = false;  // whether the quad's scales are still to be put into shared memory
+        bool is_v = false, unsaid = false;  // what comes next; whether the quad's scales are still to be put into shared memory
         auto say = [&]() {
           float2* to = reinterpret_cast<float2*>(smem + Lay::scales) +
                        (quads % kScaleSlots * kQuad + (lane >> 3)) * (kScaleFloats / 2) + (lane & 7);
@@ -709,27 +709,23 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           return true;
         };
         if (!ask()) goto produced;
-        for (int ik = 0, iv = 0; iv < nt;) {
-          const bool is_v = ik == nt || ik > iv + 1;
-          if (unsaid && (is_v ? iv > 0 : ik % kQuad == 0)) say();
+        // K and V tiles in turn (with a second K tile in front of the first V tile 25 nodes behind 4096 tokens
+        // take 15.7, not 15.1 us)
+        for (int t = 0; t < nt;) {
+          if (is_v && unsaid && t > 0) say();
           if (!await(is_v ? bar(Lay::B_VEMPTY + vt % NV) : bar(Lay::B_KEMPTY + kt % NK),
                      ((is_v ? vt / NV : kt / NK) & 1u) ^ 1u, aborted))
             goto produced;
-          int page;
-          if (is_v) {  // (at most NK - 1 tiles behind K: in its quad or the one before)
-            page = __shfl_sync(0xffffffffu, iv / kQuad == (ik - 1) / kQuad ? pages0 : pages_1, iv % kQuad * 8 | (lane & 7));
-          } else {
-            if (ik % kQuad == 0) {
-              if (ik > 0) {
-                pages_1 = pages0;
-                pages0 = pages1;
-                scales0 = scales1;
-                pages1 = pages_of(ik / kQuad + 1);
-              }
-              scales1 = scales_of(ik / kQuad + 1, pages1);
+          if (!is_v && t % kQuad == 0) {
+            if (t > 0) {
+              pages0 = pages1;
+              scales0 = scales1;
+              pages1 = pages_of(t / kQuad + 1);
             }
-            page = __shfl_sync(0xffffffffu, pages0, ik % kQuad * 8 | (lane & 7));
+            scales1 = scales_of(t / kQuad + 1, pages1);
+            unsaid = true;
           }
+          const int page = __shfl_sync(0xffffffffu, pages0, t % kQuad * 8 | (lane & 7));
           const uint32_t st = is_v ? vt++ % NV : kt++ % NK;
           const uint32_t full = bar((is_v ? Lay::B_VFULL : Lay::B_KFULL) + st);
           const uint32_t dst = sb + (is_v ? Lay::v : Lay::k) + st * kTile;
@@ -739,14 +735,11 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           if (paged) {
             if (lane < ppt) tma_load_4d(dst + lane * ps * D, map, full, 0, x.h, 0, page);
           } else if (lane == 0) {
-            tma_load_4d(dst, map, full, 0, x.h, (x.t0 + (is_v ? iv : ik)) * BN, x.b);
+            tma_load_4d(dst, map, full, 0, x.h, (x.t0 + t) * BN, x.b);
           }
           __syncwarp();
-          if (is_v) {
-            ++iv;
-          } else if (ik++ % kQuad == 0) {
-            unsaid = true;
-          }
+          t += is_v;
+          is_v = !is_v;
         }
         if (unsaid) say();
       }
