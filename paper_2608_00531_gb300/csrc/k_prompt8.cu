@@ -56,10 +56,10 @@ constexpr int kScaleSlots = 8;          // quads whose scales lie in shared memo
 constexpr int kScaleFloats = 3 * kBlocks * 2;  // of a tile, each twice (pairs for packed arithmetic)
 
 // Shared memory and barriers of the kernel for units of MT M tiles.  With one, Q takes half
-// the place, and two more tiles are on their way.
+// the place, and two more tiles are on their way (which gains nothing where units are cut).
 template <int MT>
 struct Layout {
-  static constexpr int m_tiles = MT, threads = kThreads;
+  [[maybe_unused]] static constexpr int m_tiles = MT, threads = kThreads;
   static constexpr int NK = MT == 1 ? 4 : 3, NV = MT == 1 ? 3 : 2, NW = 2;  // stages: K tiles, V tiles, V tiles in fp16
   enum : int {
     B_QFULL = 0, B_QRAW = 2, B_QEMPTY = 4, B_SFREE = 6,
@@ -205,13 +205,14 @@ __device__ __forceinline__ float4 ld_cluster_v4(uint32_t a) {
   return v;
 }
 
-// CLUSTER (a tree's rows, MT = 1): each unit has a cluster of A.cluster CTAs to itself, which take an equal
-// part of its tiles each and join them through distributed shared memory.
-template <class Args, int MT, bool CLUSTER>
+// Units of two M tiles; or with CLUSTER (a tree's rows) of one, each with a cluster of A.cluster CTAs to
+// itself, which take an equal part of its tiles each and join them through distributed shared memory.
+template <class Args, bool CLUSTER>
 __global__ void __launch_bounds__(kThreads, 1)
 attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
              const __grid_constant__ CUtensorMap tm_q, const Args A) {
   constexpr bool kTree = Args::kTree;
+  constexpr int MT = CLUSTER ? 1 : 2;
   using Lay = Layout<MT>;
   constexpr int NK = Lay::NK, NV = Lay::NV, NW = Lay::NW;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -286,7 +287,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   // Whether a piece has rows in both M tiles; else both softmax groups take M tile 0's, a tile each in turn.
   auto two_tiles = [&](const Piece& x) { return MT == 2 && (2 * x.rg + 1) * npb < x.n; };
 
-  // (128 * (2 * 160 + 96 + 96) = 512 * 128 registers, what the block was launched with)
+  // (128 * (2 * 168 + 88 + 88) = 512 * 128 registers, what the block was launched with)
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     // ================================================================ softmax
@@ -915,7 +916,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
 }
 
 // Dynamic shared memory (and clusters above the portable size), once per device.
-template <class Args, int MT, bool CLUSTER>
+template <class Args, bool CLUSTER>
 cudaError_t set_up() {
   static std::atomic<uint64_t> ready;
   int dev = 0;
@@ -923,8 +924,8 @@ cudaError_t set_up() {
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (ready.load() & bit) return cudaSuccess;
-  const auto kernel = attn8_kernel<Args, MT, CLUSTER>;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<MT>::bytes);
+  const auto kernel = attn8_kernel<Args, CLUSTER>;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<CLUSTER ? 1 : 2>::bytes);
   if (e == cudaSuccess && CLUSTER) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) ready.fetch_or(bit);
   return e;
@@ -935,7 +936,7 @@ cudaError_t set_up() {
 int max_clusters(int size) {
   static std::atomic<int> known[64][kAttnMaxCluster + 1];  // 1 + the count; 0: not asked yet
   int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || set_up<Tree8, 1, true>() != cudaSuccess) return 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64 || set_up<Tree8, true>() != cudaSuccess) return 0;
   int n = known[dev][size].load();
   if (n == 0) {
     cudaLaunchConfig_t cfg = {};
@@ -948,7 +949,7 @@ int max_clusters(int size) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, attn8_kernel<Tree8, 1, true>, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&n, attn8_kernel<Tree8, true>, &cfg) != cudaSuccess) {
       cudaGetLastError();
       n = 0;
     }
@@ -966,9 +967,9 @@ int cluster_size(int64_t units) {
   return 0;
 }
 
-template <int MT, bool CLUSTER, class Args>
+template <bool CLUSTER, class Args>
 cudaError_t launch(const Attn8Call& c, Args& A, int grid, cudaStream_t s) {
-  const cudaError_t e = set_up<Args, MT, CLUSTER>();
+  const cudaError_t e = set_up<Args, CLUSTER>();
   if (e != cudaSuccess) return e;
   CUtensorMap mk, mv, mq;
   const int box = c.kv.layout == 1 ? c.kv.page_size : BN;
@@ -984,7 +985,7 @@ cudaError_t launch(const Attn8Call& c, Args& A, int grid, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Layout<MT>::bytes;
+  cfg.dynamicSmemBytes = Layout<CLUSTER ? 1 : 2>::bytes;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   cfg.attrs = attr;
@@ -999,7 +1000,7 @@ cudaError_t launch(const Attn8Call& c, Args& A, int grid, cudaStream_t s) {
     attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
   }
-  return cudaLaunchKernelEx(&cfg, attn8_kernel<Args, MT, CLUSTER>, mk, mv, mq, A);
+  return cudaLaunchKernelEx(&cfg, attn8_kernel<Args, CLUSTER>, mk, mv, mq, A);
 }
 
 }  // namespace
@@ -1011,20 +1012,17 @@ size_t attn8_workspace() {
 
 cudaError_t launch_attn8(const Attn8Call& c, cudaStream_t s) {
   if (tokens8_fits(c)) return launch_tokens8(c, s);
-  // Sequences whose rows' heads fit one M tile on average: units of one M tile.
-  const int npb = BM / (c.heads_q / c.kv.heads_kv);
-  const bool one = c.rows <= (int64_t)c.batch * npb;
   const int sms = num_sms();
   if (c.n_nodes) {
     Tree8 A = {};
     // few units: a cluster of CTAs each
+    const int npb = BM / (c.heads_q / c.kv.heads_kv);
     const int64_t units = (int64_t)c.batch * c.kv.heads_kv * ((c.n_max + npb - 1) / npb);
     A.cluster = units * 2 <= sms ? cluster_size(units) : 0;
-    if (A.cluster > 0) return launch<1, true>(c, A, (int)units * A.cluster, s);
-    return one ? launch<1, false>(c, A, sms, s) : launch<2, false>(c, A, sms, s);
+    return A.cluster > 0 ? launch<true>(c, A, (int)units * A.cluster, s) : launch<false>(c, A, sms, s);
   }
   Args8 A = {};
-  return one ? launch<1, false>(c, A, sms, s) : launch<2, false>(c, A, sms, s);
+  return launch<false>(c, A, sms, s);
 }
 
 }  // namespace cure
