@@ -59,7 +59,7 @@ constexpr int kScaleFloats = 3 * kBlocks * 2;  // of a tile, each twice (pairs f
 // the place, and two more tiles are on their way (which gains nothing where units are cut).
 template <int MT>
 struct Layout {
-  [[maybe_unused]] static constexpr int m_tiles = MT, threads = kThreads;
+  static constexpr int m_tiles = MT, threads = kThreads;
   static constexpr int NK = MT == 1 ? 4 : 3, NV = MT == 1 ? 3 : 2, NW = 2;  // stages: K tiles, V tiles, V tiles in fp16
   enum : int {
     B_QFULL = 0, B_QRAW = 2, B_QEMPTY = 4, B_SFREE = 6,
@@ -212,8 +212,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
              const __grid_constant__ CUtensorMap tm_q, const Args A) {
   constexpr bool kTree = Args::kTree;
-  constexpr int MT = CLUSTER ? 1 : 2;
-  using Lay = Layout<MT>;
+  using Lay = Layout<CLUSTER ? 1 : 2>;
+  constexpr int MT = Lay::m_tiles;
   constexpr int NK = Lay::NK, NV = Lay::NV, NW = Lay::NW;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -984,7 +984,7 @@ cudaError_t launch(const Attn8Call& c, Args& A, int grid, cudaStream_t s) {
   A.n_max = c.n_max;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(Layout<CLUSTER ? 1 : 2>::threads);
   cfg.dynamicSmemBytes = Layout<CLUSTER ? 1 : 2>::bytes;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];

@@ -28,7 +28,8 @@
 // 6.78); 10940 rows of 28 + 2 x 4 heads with norms into 16-token pages 42 us, 4.76
 // TB/s: three waves of warps, each with its look-ups and six rounds of loads, and the
 // norm's sums (39 us without them).  Few rows are bound by latency: 17 rows of 32 + 2 x
-// 8 heads 2.6 us, 758 rows of 28 + 2 x 4 heads with norms 7.4 us (1.9 TB/s).  (Loads of
+// 8 heads 2.6 us, 758 rows of 28 + 2 x 4 heads with norms 7.4 us (1.9 TB/s).  With three axes
+// 23567 rows of 32 + 2 x 8 heads and norms 95.7 us, 6.05 TB/s; 1056 of 28 + 2 x 4 6.0 us.  (Loads of
 // the next step into each place as it falls free: 63 us for the 10940 rows, as the
 // four places' sums then run one after the other.)
 #include "rope_math.cuh"
