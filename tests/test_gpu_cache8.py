@@ -709,7 +709,7 @@ def test_tree_same_bits_streams_and_graphs(cure, lens, n_max):
 
 # ---------------------------------------------------------------- commit
 @pytest.mark.parametrize("ps", [0, 16, 64])
-@pytest.mark.parametrize("K,layers", [(16, 3), (32, 1), (1, 2)])
+@pytest.mark.parametrize("K,layers", [(16, 3), (32, 1), (1, 2), (1, 128)])
 def test_commit(cure, ps, K, layers):
     """The path's rows as an append of them would write, lengths and replay lists as cure_resync_kv gives them."""
     B, Hkv, n_max = 5, 2, 2 * K + 1
