@@ -32,14 +32,14 @@
 // with an O and sums of its own, which the epilogue adds up: a group's exponentials would
 // otherwise take longer than a tile's bytes.
 //
-// Bound: a tile of 128 keys and two M tiles takes 1.43 us, most of it the softmax warps' 256 x 128
-// exponentials, sums and conversions (with the exponentials left out a document takes a quarter
-// less; the products' own time is 1.1), and a unit about 5 us on top until its first scores are there
-// and its last rows out.  One document of 16384 tokens, 64 heads and 8 of K and V: 3.0 ms, 1.46 PFLOP/s
-// of the attention's operations; 32 prompts of 33 to 4096 tokens, 28 heads and 4: 263 us.  There, Q
-// taken apart by warps 12-15 in front of the piece's V tiles took 288, Q asked for behind the first V
-// tile instead of in front of the first K tile 269.  Registers of a thread for softmax, warps 12-15 and
-// the rest: 168 / 88 / 88 (184 / 80 / 64 takes 274, 160 / 104 / 88 282; a few words spill in each).
+// Bound: the softmax warps' chain.  A tile of 128 keys and two M tiles takes 1.5 us of their exponentials,
+// sums and conversions (the products' own time is 1.1), and a unit about 5 us on top until its first scores
+// are there and its last rows out.  One document of 16384 tokens, 64 heads and 8 of K and V: 2.9 ms, 1.52
+// PFLOP/s of the attention's operations; 32 prompts of 33 to 4096 tokens, 28 heads and 4: 247 us.  The blocks'
+// largest scores come with the scores from TMEM (tcgen05.ld.red): found in registers, 260 us and 3.06 ms.  Q taken
+// apart by warps 12-15 in front of the piece's V tiles cost 25 us of the prompts, Q asked for behind the first
+// V tile instead of in front of the first K tile 6.  Registers of a thread for softmax, warps 12-15 and the
+// rest: 168 / 88 / 88 (184 / 80 / 64 took 274 us where they took 263, 160 / 104 / 88 282; a few words spill in each).
 #include "prompt8.cuh"
 
 namespace cure {
@@ -203,6 +203,16 @@ __device__ __forceinline__ float4 ld_cluster_v4(uint32_t a) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
                : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
   return v;
+}
+
+// 16 columns of TMEM of the lane's row, and the largest of them.
+__device__ __forceinline__ void tmem_ld16_max(uint32_t taddr, uint32_t* r, float& top) {
+  asm volatile(
+      "tcgen05.ld.red.sync.aligned.32x32b.x16.max.f32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, %16, [%17];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=f"(top)
+      : "r"(taddr));
 }
 
 // Units of two M tiles; or with CLUSTER (a tree's rows) of one, each with a cluster of A.cluster CTAs to
@@ -373,9 +383,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           mbar_arrive(bar(Lay::B_PFULL + m));
           continue;
         }
-        uint32_t v[4][32];
+        uint32_t v[BN];
+        float top[kBlocks];  // each block's largest score
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_ld32(tS + 32 * q, v[q]);
+        for (int b = 0; b < kBlocks; ++b) tmem_ld16_max(tS + kBlk * b, v + kBlk * b, top[b]);
         tmem_wait_ld();
         tc_fence_before();
         // The row's factor, read before S is given back: that of the piece after the next takes its place.
@@ -388,8 +399,17 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             reinterpret_cast<const float4*>(smem + Lay::scales + (at + (uint32_t)(t - x.t0)) % (kScaleSlots * kQuad) * (kScaleFloats * 4));
         float x_[BN];
 #pragma unroll
-        for (int k = 0; k < BN; ++k) x_[k] = __uint_as_float(v[k >> 5][k & 31]);
+        for (int k = 0; k < BN; ++k) x_[k] = __uint_as_float(v[k]);
         if ((t + 1) * BN > least) {
+          auto largest = [&](int b) -> float {
+            const float* y = x_ + b * kBlk;
+            float a0 = fmax3(y[0], y[1], y[2]), a1 = fmax3(y[3], y[4], y[5]);
+            a0 = fmax3(a0, y[6], y[7]);
+            a1 = fmax3(a1, y[8], y[9]);
+            a0 = fmax3(a0, y[10], y[11]);
+            a1 = fmax3(a1, y[12], y[13]);
+            return fmax3(fmaxf(a0, a1), y[14], y[15]);
+          };
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const int key = t * BN + 32 * q;  // the block's first
@@ -405,24 +425,17 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
               }
 #pragma unroll
               for (int k = 0; k < 32; ++k) x_[32 * q + k] = (seen >> k) & 1u ? x_[32 * q + k] : -INFINITY;
+              top[2 * q] = largest(2 * q);
+              top[2 * q + 1] = largest(2 * q + 1);
             }
           }
         }
-        // the maximum of s + log2 vs, from each block's largest score
+        // the maximum of s + log2 vs
         float mt = -INFINITY;
-        auto largest = [&](int b) -> float {
-          const float* y = x_ + b * kBlk;
-          float a0 = fmax3(y[0], y[1], y[2]), a1 = fmax3(y[3], y[4], y[5]);
-          a0 = fmax3(a0, y[6], y[7]);
-          a1 = fmax3(a1, y[8], y[9]);
-          a0 = fmax3(a0, y[10], y[11]);
-          a1 = fmax3(a1, y[12], y[13]);
-          return fmax3(fmaxf(a0, a1), y[14], y[15]);
-        };
 #pragma unroll
         for (int b = 0; b < kBlocks; b += 2) {
           const float4 ks = scales[b / 2], lv = scales[kBlocks / 2 + b / 2];
-          mt = fmax3(mt, fmaf(largest(b), c * ks.x, lv.x), fmaf(largest(b + 1), c * ks.z, lv.z));
+          mt = fmax3(mt, fmaf(top[b], c * ks.x, lv.x), fmaf(top[b + 1], c * ks.z, lv.z));
         }
         const float m_new = fmaxf(m_run, mt);
         const bool need = m_new > m_run + 8.0f;
