@@ -50,6 +50,9 @@ struct Lay {
 };
 
 struct TokenArgs : PromptArgs {
+  // Its start and end cost a unit 5 us; a tile, 0.55 (64 sequences of 500 to 16000 keys: 111 us with 2, 106 with 4,
+  // 99 with 6, 96 with 8 to 10, 99 with 16).
+  static constexpr int kUnitCost = 9 * BN;
   const uint16_t* q;
   const float *k_scale, *v_scale;
 };
@@ -452,10 +455,10 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 }  // namespace
 
 // Sequences whose rows fit one unit on average.  Against k_prompt8.cu: 64 sequences of 1 / 2 rows behind
-// 500 to 8000 keys (28 and 4 heads) 83 / 85 and 101 / 107 us, of 4 rows (32 and 8 heads) 153 and 197.
-// A long chunk among them is read again for each of its units: one of 300 rows beside 128 single tokens 188 and
-// 267, one of 64 beside 63 82 and 72, one of 100 rows behind 8000 keys beside 40 158 and 88.  (A launch of each
-// for the sequences that it suits: 92, 162, 199, 109, 122 where these are 85, 153, 188, 82, 158.)
+// 500 to 8000 keys (28 and 4 heads) 65 / 71 and 97 / 104 us, of 2 / 4 rows (32 and 8 heads) 108 / 122 and 170 / 192.
+// A long chunk among them is read again for each of its units: one of 64 rows beside 63 single tokens 70 and 79,
+// one of 300 rows beside 128 189 and 262, one of 100 rows behind 8000 keys beside 40 114 and 92, one of 600 behind
+// 4000 beside 255 417 and 311.  (A launch of each for the sequences that it suits was slower in most of these.)
 bool tokens8_fits(const Attn8Call& c) {
   const int G = c.heads_q / c.kv.heads_kv;
   return !c.n_nodes && G <= kRows && c.rows <= (int64_t)c.batch * (kRows / G);

@@ -37,6 +37,7 @@ constexpr uint32_t kColO = 256;  // O[m]: columns 256 + m*128
 
 struct PromptArgs {
   static constexpr bool kTree = false;  // rows see the keys up to their own
+  static constexpr int kUnitCost = 2 * BN;  // (below)
   cure_kv_desc kv;
   const int32_t* row_start;
   const int32_t* cache_len;
@@ -52,17 +53,16 @@ struct PromptArgs {
   int expire_warp, expire_wait;  // self-test: the wait of CTA 0 that runs out, by its warp and number from 1
 };
 
-// Positions.  Every unit takes kUnitCost positions (what starting and ending a
-// piece costs, in key times) and then one for each key of the last row that its
+// Positions.  Every unit takes Args::kUnitCost positions (what starting and ending a
+// piece costs, in a kernel's key times) and then one for each key of the last row that its
 // row group could have; tile t of it stands at the position of its first key.
-constexpr int kUnitCost = 2 * BN;
 // What joining the parts of units costs a call (7 to 8 us: a prompt of 200 or 1024 cut
 // needlessly), and the fewest positions worth a CTA.
 constexpr int kJoinCost = 8 * BN;
 constexpr int kMinShare = 3 * BN;
 // Units of fewer positions on average, and those of a batch of more than 32, are
 // dealt out in turn: the reckoning that evens them out would take longer than they do.
-constexpr int kShortUnit = kUnitCost + 5 * BN;
+constexpr int kShortUnit = 7 * BN;
 // A share's border that lies nearer to a unit's border than this moves there.
 constexpr int kSnap = 4 * BN;
 
@@ -149,7 +149,7 @@ struct Walk {
   }
   // the k-th row group's positions for a head: of the first, and what each adds
   // (a tree's row groups all see its last node)
-  __device__ __forceinline__ int base() const { return split ? kUnitCost + s.L + (Args::kTree ? groups * R : 0) : 1; }
+  __device__ __forceinline__ int base() const { return split ? Args::kUnitCost + s.L + (Args::kTree ? groups * R : 0) : 1; }
   __device__ __forceinline__ int step() const { return split && !Args::kTree ? R : 0; }
   __device__ __forceinline__ int64_t before(int k) const {  // a head's positions in front of the k-th row group
     return k * (int64_t)base() + (int64_t)step() * k * (k + 1) / 2;
@@ -220,7 +220,7 @@ struct Walk {
   // Where the border p of a share, which lies in this unit, is drawn: at one of the
   // unit's borders if that is near (or if one side would be left without a tile).
   __device__ __forceinline__ int64_t border(int64_t p) const {
-    const int64_t first = ustart + kUnitCost;
+    const int64_t first = ustart + Args::kUnitCost;
     if (p < first + near) return ustart;
     if (p > first + (int64_t)(tiles() - 1) * BN || ustart + cost - p < near) return ustart + cost;
     return p;
@@ -241,7 +241,7 @@ struct Walk {
     x.o0 = (int)blockIdx.x;
     x.parts = 1;
     if (split) {
-      const int64_t first = ustart + kUnitCost;  // tile 0's position
+      const int64_t first = ustart + Args::kUnitCost;  // tile 0's position
       if (g > first) x.t0 = (int)min((int64_t)x.T, (g - first + BN - 1) / BN);
       x.t1 = g_end <= first ? 0 : (int)min((int64_t)x.T, (g_end - first + BN - 1) / BN);
       if (x.t0 < x.t1 && x.t1 - x.t0 < x.T) {
@@ -356,7 +356,7 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
   };
   auto size_of = [&](const Seq& s) -> Size {  // a sequence's positions of both kinds
     const int64_t k = walk.groups_of(s.n);
-    return {walk.Hkv * k, walk.Hkv * (k * (kUnitCost + s.L) + walk.R * (Args::kTree ? k * k : k * (k + 1) / 2))};
+    return {walk.Hkv * k, walk.Hkv * (k * (Args::kUnitCost + s.L) + walk.R * (Args::kTree ? k * k : k * (k + 1) / 2))};
   };
   auto scan = [&](int64_t v) -> int64_t {  // sum over the lanes up to this one
 #pragma unroll
@@ -402,7 +402,7 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
   // The wrong side is taken by up to 7 %, within some 20 % of the border.
   const float share = __fdividef((float)cost, (float)walk.P);
   const float cut = 1.08f * share + kJoinCost;
-  float whole = (float)(longest + kUnitCost);
+  float whole = (float)(longest + Args::kUnitCost);
   walk.falling = walk.few && units > walk.P && cost >= units * kShortUnit && whole <= cut;
   walk.mine = own;
   walk.number_of_mine = lane;
@@ -431,7 +431,7 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
       if (local >= 0 && local < n) {
         const int rg = (n - 1 - local) / walk.Hkv;
         const int keys = walk.mine.L + min((rg + 1) * walk.R, walk.mine.n);
-        most = fmaxf(most, (float)(r + 1) * (float)(keys + kUnitCost));
+        most = fmaxf(most, (float)(r + 1) * (float)(keys + Args::kUnitCost));
       }
     }
     whole = 1.03f * __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
@@ -525,7 +525,7 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
   if (walk.split) {
     if (share < (float)kMinShare) walk.P = max(1, (int)((float)run * (1.f / kMinShare)));
     walk.share = (int64_t)(__fdividef((float)run, (float)walk.P) * 0.999999f);
-    walk.near = min((int64_t)kSnap, max((int64_t)1, (walk.share - kUnitCost) / 2));
+    walk.near = min((int64_t)kSnap, max((int64_t)1, (walk.share - Args::kUnitCost) / 2));
   }
   // A CTA of cut units finds its range's end first, then takes the units inside the range
   // and the range's first and last piece, which may be parts of units.
