@@ -53,6 +53,9 @@ struct TokenArgs : PromptArgs {
   // Its start and end cost a unit 5 us; a tile, 0.55 (64 sequences of 500 to 16000 keys: 111 us with 2, 106 with 4,
   // 99 with 6, 96 with 8 to 10, 99 with 16).
   static constexpr int kUnitCost = 9 * BN;
+  // 256 sequences of 100 to 3000 keys, 8 heads of K and V: 212 us cut, 234 in turn; what cuts those leaves whole the
+  // 208 us of 1500 keys each.
+  static constexpr float kSpread = 0.8f;
   const uint16_t* q;
   const float *k_scale, *v_scale;
 };

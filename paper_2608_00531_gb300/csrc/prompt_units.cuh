@@ -37,7 +37,8 @@ constexpr uint32_t kColO = 256;  // O[m]: columns 256 + m*128
 
 struct PromptArgs {
   static constexpr bool kTree = false;  // rows see the keys up to their own
-  static constexpr int kUnitCost = 2 * BN;  // (below)
+  static constexpr int kUnitCost = 2 * BN;  // what a unit's start and end cost (below)
+  static constexpr float kSpread = 0.f;     // what unlike lengths add to units dealt out in turn (schedule)
   cure_kv_desc kv;
   const int32_t* row_start;
   const int32_t* cache_len;
@@ -436,7 +437,11 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
     }
     whole = 1.03f * __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
   } else if (units > walk.P) {
+    // (unlike lengths add up to unlike sums of units / P of them)
+    const float over = whole - __fdividef((float)cost, (float)units);
     whole = share + 0.5f * whole;
+    if constexpr (Args::kSpread > 0)
+      whole += Args::kSpread * fmaxf(0.f, over) * sqrt_approx(__fdividef((float)units, (float)walk.P));
   }
   walk.split = whole > cut;
   if (walk.split) {
