@@ -10,8 +10,15 @@
 //     B registers of a step (the dims are numbered so), V's are paired by key;
 //   - q is exact in fp16 under a power of two a row, P' = 2^(s + log2 vs - M + 7) as in k_prompt8.cu.
 // The warps of a CTA take a piece's steps in turn, and add up their sums behind its last one, with the next
-// piece's first steps on their way.
+// piece's first steps on their way.  That costs a unit some 5 us; where there are many short units, each warp
+// takes units of its own instead, and nothing is added up.
+//
+// Bound: HBM for long sequences but for the units' starts and ends, the warps' instructions for 8 heads of K and
+// V (4 rows of 16 used).  64 tokens behind 500 to 16000 keys (28 heads, 4 of K and V) 96 us, 5.2 TB/s; 256 behind
+// 1500 (32 and 8) 167 us (208 by whole CTAs), 200 behind 20 to 300 29 us (83).
 // Units, pieces, the scheduler and joins: prompt_units.cuh.
+#include <type_traits>
+
 #include "prompt8.cuh"
 
 namespace cure {
@@ -27,17 +34,18 @@ constexpr int kThreads12 = 32 * (kWorkers + 1);
 constexpr int NS = 2;                   // steps of a warp in shared memory
 constexpr int kBlk = CURE_KV8_BLOCK;
 constexpr int kHalf = kStep * D;        // 4 KiB: K or V of a step
+constexpr int kQBytes = 8 * 32 * 16;    // a unit's Q
 constexpr int kBatch = 8;               // steps whose pages and scales are looked up together
 constexpr float kLift = 7.f;            // P' is 2^kLift times what it stands for
 
 struct Lay {
-  static constexpr int m_tiles = 1, threads = kThreads12;
+  static constexpr int m_tiles = 1, threads = kThreads12, alone = kWorkers;
   enum : int { B_FULL = 0, B_DONE = B_FULL + kWorkers * NS, B_FREE, B_JOIN, piece_bar, taken_bar = piece_bar + kPieces, num_bars = taken_bar + kPieces };
   static constexpr int ring = 0;                                   // [warp][stage][K, V][32 keys][128]
   static_assert(kRows * D * 4 == 2 * kHalf, "a warp's sums take a stage's place");
   static constexpr int lse = ring + kWorkers * NS * 2 * kHalf;     // float [warp][16 rows]
   static constexpr int q = lse + kWorkers * kRows * 4;             // uint [product][lane][4]: Q's fragments
-  static constexpr int q_scale = q + 8 * 32 * 16;                  // float [16 rows]
+  static constexpr int q_scale = q + kQBytes;                      // float [16 rows]
   static constexpr int place = q_scale + kRows * 4;                // int [warp]: where its sums are
   static constexpr int bars = (place + kWorkers * 4 + 7) / 8 * 8;
   static constexpr int abort = bars + 8 * num_bars;
@@ -45,10 +53,19 @@ struct Lay {
   static constexpr int pieces = (joins + 4 + 15) / 16 * 16;
   static constexpr int prefix = pieces + (kPieces + 2) * kPieceInts * 4;
   static constexpr int kept = (prefix + 8 * (kAttnMaxBatch + 1) + 15) / 16 * 16;  // the piece that is added up, a copy for each warp
-  static constexpr int bytes = kept + kWorkers * kPieceInts * 4;
-  static_assert(bytes <= 232448, "fits the 227 KiB opt-in");
+  static constexpr int mode = kept + kWorkers * kPieceInts * 4;    // int: whether the warps attend alone
+  static constexpr int bytes = mode + 16;
+  // .. and where they may: [slot][warp] their pieces, [warp] Q's fragments (of the first at q) and factors.  (What shared memory takes
+  // is lost to the L1 cache: where it is not used, this costs 3 %.)
+  static constexpr int own = bytes;
+  static constexpr int own_q = own + kPieces * kWorkers * kPieceInts * 4;
+  static constexpr int own_scale = own_q + (kWorkers - 1) * kQBytes;
+  static constexpr int bytes_alone = own_scale + kWorkers * kRows * 4;
+  static_assert(bytes_alone <= 232448, "fits the 227 KiB opt-in");
 };
 
+// ALONE: warps may attend to units of their own.
+template <bool ALONE>
 struct TokenArgs : PromptArgs {
   // Its start and end cost a unit 5 us; a tile, 0.55 (64 sequences of 500 to 16000 keys: 111 us with 2, 106 with 4,
   // 99 with 6, 96 with 8 to 10, 99 with 16).
@@ -56,6 +73,8 @@ struct TokenArgs : PromptArgs {
   // 256 sequences of 100 to 3000 keys, 8 heads of K and V: 212 us cut, 234 in turn; what cuts those leaves whole the
   // 208 us of 1500 keys each.
   static constexpr float kSpread = 0.8f;
+  // A warp alone takes as long for a key as the CTA does for 6.5.
+  static constexpr float kAloneTail = ALONE ? 6.5f : 0.f;
   const uint16_t* q;
   const float *k_scale, *v_scale;
 };
@@ -84,8 +103,10 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
+template <bool MAY_ALONE>
 __global__ void __launch_bounds__(kThreads12, 1)
-tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const TokenArgs A) {
+tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+               const TokenArgs<MAY_ALONE> A) {
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t sb = smem_u32(smem);
@@ -109,6 +130,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     }
     *abort_flag = 0;
     *n_joins = 0;
+    *reinterpret_cast<volatile int*>(smem + Lay::mode) = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
@@ -120,6 +142,9 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   if (warp == kWorkers) {
     schedule<Lay>(A, npb, await, bar, smem, aborted, lane);
   } else {
+    // The scheduler's first piece says whether each warp attends to units of its own.
+    auto attend = [&](auto tag) {
+      constexpr bool ALONE = decltype(tag)::value;
     const int g = lane >> 2, t4 = lane & 3;  // fragment row (and key, and dims), fragment columns
     const int ps = A.kv.page_size;
     const bool paged = A.kv.layout == 1;
@@ -132,7 +157,11 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     Pieces pieces{0};
     Piece x;
     uint32_t issued = 0, used = 0, done = 0, joins = 0;
-    // The piece's steps of this warp: warp, warp + 11, .. of those with keys of the unit.
+    // The piece's steps of this warp, of those with keys of the unit: warp, warp + 11, .., or all.
+    constexpr int S = ALONE ? 1 : kWorkers;
+    constexpr int kRaw = ALONE ? 4 : 2;  // rows of Q on their way
+    const uint32_t qs = ALONE && warp > 0 ? Lay::own_q + (warp - 1) * kQBytes : Lay::q;
+    float* q_scale = reinterpret_cast<float*>(smem + (ALONE ? Lay::own_scale + warp * kRows * 4 : Lay::q_scale));
     int s0, n;
     // Pages and scales are looked up kBatch steps at a time, two batches and one ahead.  Lane 4 k + 2 v + p:
     // where block p of the batch's step k lies in a paged cache (page * blocks + block; -1: nowhere, zeros), and
@@ -140,7 +169,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     int place0, place1, place2;
     float scale0, scale1;
     auto look_up = [&](int batch) -> int {
-      const int k = batch * kBatch + (lane >> 2), tok = (s0 + k * kWorkers) * kStep + (lane & 1) * kBlk;
+      const int k = batch * kBatch + (lane >> 2), tok = (s0 + k * S) * kStep + (lane & 1) * kBlk;
       if (k >= n || tok >= x.keys) return -1;
       if (!paged) return 0;
       const int page = A.kv.block_table[(int64_t)x.b * A.kv.max_len + tok / ps];
@@ -154,7 +183,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       if (place < 0) return 1.f;
       int64_t at = place;
       if (!paged)
-        at = (int64_t)x.b * ((A.kv.max_len + kBlk - 1) / kBlk) + (s0 + (batch * kBatch + (lane >> 2)) * kWorkers) * (kStep / kBlk) +
+        at = (int64_t)x.b * ((A.kv.max_len + kBlk - 1) / kBlk) + (s0 + (batch * kBatch + (lane >> 2)) * S) * (kStep / kBlk) +
              (lane & 1);
       return __ldg((lane & 2 ? A.v_scale : A.k_scale) + at * A.kv.heads_kv + x.h);
     };
@@ -168,17 +197,27 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         const uint32_t dst = ring + st * (2 * kHalf) + (lane >> 1) * kHalf + (lane & 1) * (box * D);
         const CUtensorMap* map = lane < 2 ? &tm_k : &tm_v;
         if (paged) tma_load_4d(dst, map, full, 0, x.h, place < 0 ? 0 : place % per * kBlk, place < 0 ? -1 : place / per);
-        else tma_load_4d(dst, map, full, 0, x.h, (s0 + k * kWorkers) * kStep, x.b);
+        else tma_load_4d(dst, map, full, 0, x.h, (s0 + k * S) * kStep, x.b);
       }
       __syncwarp();
       ++issued;
     };
     // The next piece, its look-ups, and its first step on the way.
     auto begin = [&]() -> bool {
-      if (!pieces.next<Lay>(await, bar, smem, aborted, x)) return false;
-      s0 = x.t0 * kSteps + warp;
+      if constexpr (ALONE) {
+        const uint32_t slot = pieces.k % kPieces;
+        if (!await(bar(Lay::piece_bar + slot), (pieces.k / kPieces) & 1u, aborted)) return false;
+        x = reinterpret_cast<const Piece*>(smem + Lay::own)[slot * kWorkers + warp];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(Lay::taken_bar + slot));
+        ++pieces.k;
+        if (x.t0 >= x.t1) return false;
+      } else {
+        if (!pieces.next<Lay>(await, bar, smem, aborted, x)) return false;
+      }
+      s0 = x.t0 * kSteps + (ALONE ? 0 : warp);
       const int s_end = min(x.t1 * kSteps, (x.keys + kStep - 1) / kStep);
-      n = s0 < s_end ? (s_end - s0 + kWorkers - 1) / kWorkers : 0;
+      n = s0 < s_end ? (s_end - s0 + S - 1) / S : 0;
       place0 = look_up(0);
       place1 = look_up(1);
       place2 = look_up(2);
@@ -187,12 +226,12 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       scale1 = scale_of(1, place1);
       return true;
     };
-    // Q: the warp's rows (warp, warp + 11), 4 dims a lane, on their way
-    uint2 raw[2];
-    auto load_q = [&]() {
+    // Q: rows first, first + each of the unit (the warp's: warp, warp + 11), 4 dims a lane, on their way
+    uint2 raw[kRaw];
+    auto load_q = [&](int first, int each) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int row = warp + kWorkers * r, i = x.rg * npb + row / G;
+      for (int r = 0; r < kRaw; ++r) {
+        const int row = first + each * r, i = x.rg * npb + row / G;
         raw[r] = make_uint2(0u, 0u);
         if (row < npb * G && i < x.n)
           raw[r] = __ldg(reinterpret_cast<const uint2*>(
@@ -201,10 +240,10 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     };
     // .. in fp16 under a power of two that brings a row below 448, as the products' fragments: dims 4 L ..
     // 4 L + 3 of row r are registers r / 8 and 2 + r / 8 of product L % 8 in lane 4 (r % 8) + L / 8
-    auto put_q = [&]() {
+    auto put_q = [&](int first, int each) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int row = warp + kWorkers * r;
+      for (int r = 0; r < kRaw; ++r) {
+        const int row = first + each * r;
         if (row >= kRows) break;
         const float v[4] = {__uint_as_float(raw[r].x << 16), __uint_as_float(raw[r].x & 0xffff0000u),
                             __uint_as_float(raw[r].y << 16), __uint_as_float(raw[r].y & 0xffff0000u)};
@@ -212,29 +251,37 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(mine));
         const int e = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u), -60), 120);
         const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-        uint32_t* to = reinterpret_cast<uint32_t*>(smem + Lay::q) + ((lane & 7) * 32 + 4 * (row & 7) + (lane >> 3)) * 4 + (row >> 3);
+        uint32_t* to = reinterpret_cast<uint32_t*>(smem + qs) + ((lane & 7) * 32 + 4 * (row & 7) + (lane >> 3)) * 4 + (row >> 3);
         to[0] = pack_f16(v[0] * inv, v[1] * inv);
         to[2] = pack_f16(v[2] * inv, v[3] * inv);
         if (lane == 0)
-          reinterpret_cast<float*>(smem + Lay::q_scale)[row] =
+          q_scale[row] =
               fminf(fmaxf(A.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23), 0x1p-80f), 0x1p80f);
       }
     };
     bool more = begin();
-    if (more) {
-      load_q();
-      put_q();
+    if (more && !ALONE) {
+      load_q(warp, kWorkers);
+      put_q(warp, kWorkers);
       mbar_arrive(bar(Lay::B_FREE));
     }
     while (more) {
-      // all have read this warp's sums, and Q is there
-      if (!await(bar(Lay::B_FREE), done & 1u, aborted)) break;
+      if constexpr (ALONE) {
+#pragma unroll 1
+        for (int row = 0; row < kRows; row += kRaw) {
+          load_q(row, 1);
+          put_q(row, 1);
+        }
+        __syncwarp();
+      } else {  // all have read this warp's sums, and Q is there
+        if (!await(bar(Lay::B_FREE), done & 1u, aborted)) break;
+      }
       if (n > 1) issue(1, false);
       float c[2];
       int sees[2];
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
-        c[r] = reinterpret_cast<const float*>(smem + Lay::q_scale)[g + 8 * r];
+        c[r] = q_scale[g + 8 * r];
         sees[r] = x.L + x.rg * npb + (g + 8 * r) / G + 1;
       }
       const int least = x.L + x.rg * npb + 1;  // keys that all rows see
@@ -257,7 +304,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         if (!await(bar(Lay::B_FULL + warp * NS + st), (used / NS) & 1u, aborted)) goto out;
         ++used;
         const uint32_t kb = ring + st * (2 * kHalf), vb = kb + kHalf;
-        const int key0 = (s0 + k * kWorkers) * kStep;
+        const int key0 = (s0 + k * S) * kStep;
         // ---- S: key 8 nt + g of the step; codes 4 w .. + 3 of 16 are a lane's B registers of one product
         float s[4][4];
 #pragma unroll
@@ -271,7 +318,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           for (int nt = 0; nt < 4; ++nt) w[nt] = ld_shared_v4(kb + (8 * nt + g) * D + (((2 * t4 + j) ^ g) << 4));
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
-            const uint4 q = ld_shared_v4(sb + Lay::q + ((4 * j + z) * 32 + lane) * 16);
+            const uint4 q = ld_shared_v4(sb + qs + ((4 * j + z) * 32 + lane) * 16);
 #pragma unroll
             for (int nt = 0; nt < 4; ++nt) {
               uint32_t b0, b1;
@@ -371,6 +418,32 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       if (lane == 0) *kept = x;
       __syncwarp();
       more = begin();
+      if constexpr (ALONE) {
+        // a lane's 32 dims of rows g and g + 8
+        const Piece prev = *kept;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float l = l_run[r];
+          l += __shfl_xor_sync(0xffffffffu, l, 1);
+          l += __shfl_xor_sync(0xffffffffu, l, 2);
+          const float inv = l > 0.f ? 1.f / l : 0.f;
+          const int row = g + 8 * r, i = prev.rg * npb + row / G;
+          if (row >= npb * G || i >= prev.n) continue;
+          uint16_t* orow = A.out + ((int64_t)(prev.r0 + i) * A.heads_q + prev.h * G + row % G) * D + 32 * t4;
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int d = 0; d < 16; d += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int z = 0; z < 4; ++z)
+                w[z] = pack_bf16(o[d + 2 * z][2 * r + e] * inv, o[d + 2 * z + 1][2 * r + e] * inv);
+              *reinterpret_cast<uint4*>(orow + 16 * e + d) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+        __syncwarp();  // (all lanes have read the piece)
+        continue;
+      }
       const uint32_t st = issued % NS;
       float* mine = reinterpret_cast<float*>(smem + Lay::ring + warp * (NS * 2 * kHalf) + st * (2 * kHalf));
 #pragma unroll
@@ -389,7 +462,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
                             o[i + 3][2 * r + e] * inv);
       }
       if (lane == 0) place_of_sums[warp] = (int)(warp * (NS * 2 * kHalf) + st * (2 * kHalf));
-      if (more) load_q();
+      if (more) load_q(warp, kWorkers);
       mbar_arrive(bar(Lay::B_DONE));
       if (!await(bar(Lay::B_DONE), done & 1u, aborted)) break;
       ++done;
@@ -428,7 +501,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           if ((tid & 15) == 0) __stcg(A.ws_lse + slot * (2 * BM) + row, top + log2f(total));
         }
       }
-      if (more) put_q();
+      if (more) put_q(warp, kWorkers);
       fence_proxy_async_smem();  // (the sums' places get copies next)
       mbar_arrive(bar(Lay::B_FREE));
       if (whole) continue;
@@ -446,6 +519,15 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     if (*abort_flag)  // let copies in flight land before the CTA's smem goes away
       for (; used < issued; ++used)
         wait_bounded(bar(Lay::B_FULL + warp * NS + used % NS), (used / NS) & 1u, abort_flag, A.err, false);
+    };
+    if constexpr (MAY_ALONE) {
+      if (await(bar(Lay::piece_bar), 0, aborted)) {
+        if (*reinterpret_cast<volatile int*>(smem + Lay::mode)) attend(std::true_type{});
+        else attend(std::false_type{});
+      }
+    } else {
+      attend(std::false_type{});
+    }
   }
   __syncthreads();
   if (*abort_flag) {
@@ -467,14 +549,16 @@ bool tokens8_fits(const Attn8Call& c) {
   return !c.n_nodes && G <= kRows && c.rows <= (int64_t)c.batch * (kRows / G);
 }
 
-cudaError_t launch_tokens8(const Attn8Call& c, cudaStream_t s) {
+template <bool ALONE>
+static cudaError_t launch(const Attn8Call& c, cudaStream_t s) {
+  constexpr int bytes = ALONE ? Lay::bytes_alone : Lay::bytes;
   static std::atomic<uint64_t> ready;  // devices on which it has its shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(ready.load() & bit)) {
-    e = cudaFuncSetAttribute(tokens8_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::bytes);
+    e = cudaFuncSetAttribute(tokens8_kernel<ALONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit);
   }
@@ -482,12 +566,19 @@ cudaError_t launch_tokens8(const Attn8Call& c, cudaStream_t s) {
   const int box = c.kv.layout == 1 ? std::min(c.kv.page_size, kStep) : kStep;
   if (!make_codes_map(&mk, c.k_cache, c.kv, c.batch, box) || !make_codes_map(&mv, c.v_cache, c.kv, c.batch, box))
     return cudaErrorInvalidValue;
-  TokenArgs A = {};
+  TokenArgs<ALONE> A = {};
   fill_args8(c, &A);
   A.q = c.q;
   A.k_scale = c.k_scale;
   A.v_scale = c.v_scale;
-  return launch_pdl(tokens8_kernel, dim3((unsigned)num_sms()), dim3(kThreads12), (size_t)Lay::bytes, s, mk, mv, A);
+  return launch_pdl(tokens8_kernel<ALONE>, dim3((unsigned)num_sms()), dim3(kThreads12), (size_t)bytes, s, mk, mv, A);
+}
+
+// Fewer units than two to an SM are never a warp's each; the kernel that asks is 2 to 3 % slower where the answer is
+// no (64 sequences of 500 to 16000 keys, 4 heads of K and V: 98 us, not 96).
+cudaError_t launch_tokens8(const Attn8Call& c, cudaStream_t s) {
+  return c.batch > 32 && (int64_t)c.rows * c.kv.heads_kv >= (int64_t)2 * num_sms() ? launch<true>(c, s)
+                                                                                  : launch<false>(c, s);
 }
 
 }  // namespace cure

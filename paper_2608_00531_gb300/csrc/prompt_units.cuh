@@ -38,6 +38,7 @@ constexpr uint32_t kColO = 256;  // O[m]: columns 256 + m*128
 struct PromptArgs {
   static constexpr bool kTree = false;  // rows see the keys up to their own
   static constexpr int kUnitCost = 2 * BN;  // what a unit's start and end cost (below)
+  static constexpr float kAloneTail = 0.f;  // > 0: warps may take units of their own, and how much slower (schedule)
   static constexpr float kSpread = 0.f;     // what unlike lengths add to units dealt out in turn (schedule)
   cure_kv_desc kv;
   const int32_t* row_start;
@@ -444,6 +445,15 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
       whole += Args::kSpread * fmaxf(0.f, over) * sqrt_approx(__fdividef((float)units, (float)walk.P));
   }
   walk.split = whole > cut;
+  // Units of a warp each, where that is faster: they start and end under each other's copies, and at the call's
+  // end the last ones go on at a warp's pace.
+  bool alone = false;
+  if constexpr (Args::kAloneTail > 0)
+    if (!walk.few) {
+      const float keys = (float)(cost - units * (Args::kUnitCost - BN));
+      alone = __fdividef(keys, (float)walk.P) + Args::kAloneTail * (float)longest < fminf(whole, cut);
+      if (alone) walk.split = false;
+    }
   if (walk.split) {
     walk.falling = false;
     walk.mine = own;
@@ -485,6 +495,28 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
     __syncwarp();
     return true;
   };
+  if constexpr (Args::kAloneTail > 0)
+    if (alone) {
+      if (lane == 0) *reinterpret_cast<volatile int*>(smem + LAY::mode) = 1;
+      // the units of LAY::alone warps, a unit a lane
+      bool some = true;
+      for (int64_t base = 0; some; base += (int64_t)LAY::alone * walk.P) {
+        const int64_t u = base + (int64_t)lane * walk.P + blockIdx.x;
+        some = base + blockIdx.x < units;  // (behind the last: the end)
+        Piece own_piece = Piece{};
+        if (lane < LAY::alone && u < units) {
+          walk.seek(A, u);
+          own_piece = walk.within(0, units);
+        }
+        const uint32_t slot = k % kPieces;
+        if (!await(bar(LAY::taken_bar + slot), ((k / kPieces) & 1u) ^ 1u, aborted)) return;
+        ++k;
+        if (lane < LAY::alone) *(reinterpret_cast<Piece*>(smem + LAY::own) + slot * LAY::alone + lane) = own_piece;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(LAY::piece_bar + slot));
+      }
+      return;
+    }
   // Whole units, every P-th; or longest first, the first ones by number and then in
   // chunks of `team` units for a team of neighbouring CTAs, each chunk to the team that
   // has the least to do by then: every CTA follows the same reckoning.  Neighbours take

@@ -449,6 +449,37 @@ def test_few_rows_on_average(cure):
     assert cure.cure_device_error() == 0
 
 
+@pytest.mark.parametrize("ps", [0, 16, 64])
+@pytest.mark.parametrize("batch,Hq,Hkv,L", [(90, 28, 4, 300), (256, 32, 8, 120), (200, 32, 2, 40), (256, 5, 5, 700),
+                                            (256, 32, 32, 33), (256, 64, 8, 1)])
+def test_many_short_sequences(cure, ps, batch, Hq, Hkv, L):
+    """More units than there are warps, or fewer, of sequences of a few keys; none to a few rows each."""
+    rng = np.random.default_rng(batch + ps)
+    most = 16 // (Hq // Hkv)
+    n = [int(v) for v in np.minimum(rng.choice([0, 1, 1, 1, 2, 3], batch), most)]
+    n[0], n[-1] = 1, 0
+    x = _prompt(cure, [int(v) for v in rng.integers(0, L + 1, batch)], n, Hq, Hkv, ps, batch + L, std=2.0, pad=2,
+                pow2=bool(L % 2))
+    got = _run(cure, x).clone()
+    _check(x, got)
+    assert cure.cure_device_error() == 0
+    size = cure.cure_prompt_attn8_workspace_size(x["q"].shape[0], batch, Hq, x["cache"].kv)
+    ws, out, graph = torch.empty(size, dtype=torch.uint8, device=DEV), torch.full_like(x["q"], 3.5), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _run(cure, x, out=out, workspace=ws)
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[x["start"][0]:x["start"][-1]], got[x["start"][0]:x["start"][-1]])
+    if ps:  # a sequence without its first page
+        old = int(x["cache"].table[0, 0])
+        x["cache"].kv._keep[0, 0] = -1
+        bad = _run(cure, x)
+        assert cure.cure_device_error() == cure.DEVERR_PAGE
+        x["cache"].kv._keep[0, 0] = old
+        assert torch.equal(bad[x["start"][1]:], got[x["start"][1]:]) and torch.isfinite(bad[x["start"][0]:x["start"][1]]).all()
+
+
 def test_outputs_aligned_to_16_bytes(cure):
     """Outputs that begin 16 bytes behind a 32-byte boundary, in each form of the attention."""
     for lens, n, Hq in (([300, 0], [200, 70], 8), ([300, 1000, 50], [1, 1, 1], 8), ([1000, 30], [9, 12], 8)):
