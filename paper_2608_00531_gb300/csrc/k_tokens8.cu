@@ -542,7 +542,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 // Sequences whose rows fit one unit on average.  Against k_prompt8.cu: 64 sequences of 1 / 2 rows behind
 // 500 to 8000 keys (28 and 4 heads) 65 / 71 and 97 / 104 us, of 2 / 4 rows (32 and 8 heads) 108 / 122 and 170 / 192.
 // A long chunk among them is read again for each of its units: one of 64 rows beside 63 single tokens 70 and 79,
-// one of 300 rows beside 128 189 and 262, one of 100 rows behind 8000 keys beside 40 114 and 92, one of 600 behind
+// one of 300 rows beside 128 169 and 262, one of 100 rows behind 8000 keys beside 40 114 and 92, one of 600 behind
 // 4000 beside 255 417 and 311.  (A launch of each for the sequences that it suits was slower in most of these.)
 bool tokens8_fits(const Attn8Call& c) {
   const int G = c.heads_q / c.kv.heads_kv;
