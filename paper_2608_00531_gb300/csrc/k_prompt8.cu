@@ -34,7 +34,7 @@
 //
 // Bound: the softmax warps' chain.  A tile of 128 keys and two M tiles takes 1.5 us of their exponentials,
 // sums and conversions (the products' own time is 1.1), and a unit about 5 us on top until its first scores
-// are there and its last rows out.  One document of 16384 tokens, 64 heads and 8 of K and V: 2.9 ms, 1.52
+// are there and its last rows out.  One document of 16384 tokens, 64 heads and 8 of K and V: 2.83 ms, 1.55
 // PFLOP/s of the attention's operations; 32 prompts of 33 to 4096 tokens, 28 heads and 4: 247 us.  The blocks'
 // largest scores come with the scores from TMEM (tcgen05.ld.red): found in registers, 260 us and 3.06 ms.  Q taken
 // apart by warps 12-15 in front of the piece's V tiles cost 25 us of the prompts, Q asked for behind the first
@@ -53,7 +53,7 @@ constexpr int kTile = BN * D;           // 16 KiB of codes
 constexpr int kTileW = kTile * 2;
 constexpr int kQuad = 4;                // tiles whose pages and scales are looked up together
 constexpr int kScaleSlots = 8;          // quads whose scales lie in shared memory
-constexpr int kScaleFloats = 3 * kBlocks * 2;  // of a tile, each twice (pairs for packed arithmetic)
+constexpr int kScaleFloats = 7 * kBlocks;  // of a tile: ks and log2 vs of each block twice, and ks, log2 vs, 1 / vs once
 
 // Shared memory and barriers of the kernel for units of MT M tiles.  With one, Q takes half
 // the place, and two more tiles are on their way (which gains nothing where units are cut).
@@ -79,7 +79,7 @@ struct Layout {
   static constexpr int joins = abort + 4;                      // units that this CTA joins at its end
   static constexpr int pieces = (joins + 4 + 15) / 16 * 16;    // int [kPieces][kPieceInts], then [2] to join
   static constexpr int prefix = pieces + (kPieces + 2) * kPieceInts * 4;  // int64 first position of each sequence [B+1]
-  static constexpr int scales = (prefix + 8 * (kAttnMaxBatch + 1) + 15) / 16 * 16;  // float [slot][tile][ks, log2 vs, 1 / vs][8][2]
+  static constexpr int scales = (prefix + 8 * (kAttnMaxBatch + 1) + 15) / 16 * 16;  // float [slot][tile][kScaleFloats]
   static constexpr int q_scale = scales + kScaleSlots * kQuad * kScaleFloats * 4;   // float [piece % 2][m][row]
   static constexpr int inv = q_scale + 4 * BM * 4;             // float [group][row]: reciprocal row sums
   static constexpr int lse = inv + 2 * BM * 4;                 // float [group][row]: base-2 log-sum-exps
@@ -124,11 +124,6 @@ __device__ __forceinline__ uint32_t narrow(uint32_t lo, uint32_t hi) {
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
 __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
@@ -448,11 +443,14 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
         }
         const float nbase = m_run == -INFINITY ? 0.f : kLift - m_run;
         uint64_t sum = f2_pack(0.f, 0.f);
-        const uint64_t cc = f2_pack(c, c), nn = f2_pack(nbase, nbase);
         auto exponentials = [&](int q) {  // of 32 keys
-          const float4 ks = scales[q], lv = scales[kBlocks / 2 + q], iv = scales[kBlocks + q];
-          const uint64_t c2[2] = {f2_mul(cc, f2_pack(ks.x, ks.y)), f2_mul(cc, f2_pack(ks.z, ks.w))};
-          const uint64_t nb2[2] = {f2_add(nn, f2_pack(lv.x, lv.y)), f2_add(nn, f2_pack(lv.z, lv.w))};
+          // (a block's once each here, twice in the maximum's loads: twice here too takes a document 1.5 % longer, once
+          // there too 32 trees 3 %)
+          const float2 ks = reinterpret_cast<const float2*>(scales)[2 * kBlocks + q];
+          const float2 lv = reinterpret_cast<const float2*>(scales)[2 * kBlocks + kBlocks / 2 + q];
+          const float2 iv = reinterpret_cast<const float2*>(scales)[3 * kBlocks + q];
+          const float e0 = c * ks.x, e1 = c * ks.y, n0 = nbase + lv.x, n1 = nbase + lv.y;
+          const uint64_t c2[2] = {f2_pack(e0, e0), f2_pack(e1, e1)}, nb2[2] = {f2_pack(n0, n0), f2_pack(n1, n1)};
           uint32_t pk[16];
           uint64_t part[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
 #pragma unroll
@@ -464,7 +462,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
             part[u] = f2_add(part[u], f2_pack(p0, p1));
             pk[k] = pack_f16(p0, p1);
           }
-          sum = f2_fma(part[0], f2_pack(iv.x, iv.y), f2_fma(part[1], f2_pack(iv.z, iv.w), sum));
+          sum = f2_fma(part[0], f2_pack(iv.x, iv.x), f2_fma(part[1], f2_pack(iv.y, iv.y), sum));
           tmem_st16(tP + 16 * q, pk);
         };
         exponentials(0);
@@ -701,7 +699,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           const float lv = log2f(vs), rv = 1.f / vs;
           to[0] = make_float2(ks, ks);
           to[kBlocks] = make_float2(lv, lv);
-          to[2 * kBlocks] = make_float2(rv, rv);
+          float* once = reinterpret_cast<float*>(to - (lane & 7) + 2 * kBlocks) + (lane & 7);
+          once[0] = ks;
+          once[kBlocks] = lv;
+          once[2 * kBlocks] = rv;
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(Lay::B_SCALES + quads % kScaleSlots));
           ++quads;
