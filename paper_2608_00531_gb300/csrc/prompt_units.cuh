@@ -449,7 +449,7 @@ __device__ __forceinline__ void schedule(const Args& A, int npb, Wait& await, co
   // end the last ones go on at a warp's pace.
   bool alone = false;
   if constexpr (Args::kAloneTail > 0)
-    if (!walk.few) {
+    if (!walk.few && longest <= 1 << 22) {  // (a warp's unit of so many keys stays well within the waits' limit)
       const float keys = (float)(cost - units * (Args::kUnitCost - BN));
       alone = __fdividef(keys, (float)walk.P) + Args::kAloneTail * (float)longest < fminf(whole, cut);
       if (alone) walk.split = false;
