@@ -290,11 +290,11 @@ append8_kernel(const __grid_constant__ Append8Args G) {
       continue;
     }
     const int blk = (int)(slot / kBlk), t0 = (int)(slot % kBlk);
-    if (i > 0 && t0 > 0) {  // the block begins before this row: its CTA takes it
-      row += min(kBlk - t0, stop - row);
+    const int m = (int)min((int64_t)min(kBlk - t0, stop - row), cap - slot);  // the block's rows from here on
+    if (i > 0 && t0 > 0) {  // it begins before this row: its CTA takes it (but not what lies past the capacity)
+      row += m;
       continue;
     }
-    const int m = (int)min((int64_t)min(kBlk - t0, stop - row), cap - slot);  // the block's rows
     const int row0 = row;
     row += m;
     int64_t crow = 0, place = 0;
