@@ -515,8 +515,10 @@ cure_status cure_append_kv_axes(const void* q, const void* k, const void* v, int
  * to x / s (ties to even; values beyond 448 s saturate, a NaN stays one, and counts for
  * nothing in s).  What a block held before, its slots below cache_len[b], is
  * expressed anew where s changes: exactly, but for values below 2^-6 s, which are
- * rounded to steps of 2^-9 s.  Slots of the block that hold nothing may change their
- * meaning with its scale.
+ * rounded to steps of 2^-9 s (beside an infinity, s = 2^40, they are lost).  That
+ * stays when s falls again: around rows that may not stay, as a tree's, what is held
+ * is kept by cure_save_kv8 and cure_restore_kv8.  Slots of the block that hold nothing
+ * may change their meaning with its scale.
  */
 #define CURE_KV8_BLOCK 16
 
@@ -573,6 +575,28 @@ cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_ca
 
 /* Bytes of workspace cure_tree_attn8 needs for this shape on the current device (0 on a bad argument). */
 size_t cure_tree_attn8_workspace_size(int32_t batch, int32_t n_max, int32_t heads_q, const cure_kv_desc* kv);
+
+/*
+ * Rows that may not stay (a tree's in place) behind the tokens that caches in 8 bits
+ * hold: of every layer, cure_save_kv8 copies what sequence b holds of the block that
+ * slot cache_len[b] lies in (nothing where that is a multiple of 16, or not from 1 up to
+ * the capacity) and the block's scales to `saved`; cure_restore_kv8, at the same lengths
+ * and with the same pages, puts them back, to the bit.  The slots from cache_len[b] on hold
+ * nothing then.  In between only rows at or behind cache_len[b] may have been
+ * written.  Before a tree's cure_append_kv8, and behind the last attention that reads its
+ * rows, in front of cure_resync_kv8.  k_caches .. v_scales: HOST arrays of `layers`
+ * device pointers (0 .. 128 layers); saved: device memory of at least
+ * cure_save_kv8_size() bytes, 16-byte aligned.
+ */
+cure_status cure_save_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                          float* const* v_scales, const cure_kv_desc* kv, int32_t batch, const int32_t* cache_len,
+                          void* saved, size_t saved_bytes, void* stream);
+cure_status cure_restore_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                             float* const* v_scales, const cure_kv_desc* kv, int32_t batch, const int32_t* cache_len,
+                             const void* saved, size_t saved_bytes, void* stream);
+
+/* Bytes that cure_save_kv8 needs for this shape (0 on a bad argument). */
+size_t cure_save_kv8_size(int32_t layers, int32_t batch, const cure_kv_desc* kv);
 
 /*
  * cure_resync_kv for caches in 8 bits: the path's rows are taken from tree_k/tree_v (bf16

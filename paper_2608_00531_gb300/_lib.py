@@ -25,7 +25,7 @@ EXPORTS = ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_tree_a
            "cure_append_kv", "cure_prompt_attn", "cure_prompt_attn_workspace_size", "cure_device_error",
            "cure_rope_qkv_axes", "cure_append_kv_axes", "cure_append_kv8", "cure_prompt_attn8",
            "cure_prompt_attn8_workspace_size", "cure_tree_attn8", "cure_tree_attn8_workspace_size", "cure_resync_kv8",
-           "cure_status_string", "cure_abi_version")
+           "cure_save_kv8", "cure_save_kv8_size", "cure_restore_kv8", "cure_status_string", "cure_abi_version")
 
 
 class TreeParams(C.Structure):
@@ -125,6 +125,11 @@ def load() -> C.CDLL:
     lib.cure_resync_kv8.argtypes = [I32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
                                     C.POINTER(C.c_void_p), C.POINTER(KVDesc), P, P, I32, I32, I32, P, P, P, P, P, P, P, P,
                                     P, P]
+    lib.cure_save_kv8.argtypes = [I32, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.POINTER(C.c_void_p),
+                                  C.POINTER(C.c_void_p), C.POINTER(KVDesc), I32, P, P, C.c_size_t, P]
+    lib.cure_restore_kv8.argtypes = lib.cure_save_kv8.argtypes
+    lib.cure_save_kv8_size.argtypes = [I32, I32, C.POINTER(KVDesc)]
+    lib.cure_save_kv8_size.restype = C.c_size_t
     lib.cure_device_error.argtypes = [P, C.POINTER(I32)]
     lib.cure_status_string.argtypes = [C.c_int]
     lib.cure_status_string.restype = C.c_char_p
@@ -133,7 +138,7 @@ def load() -> C.CDLL:
                  "cure_resync_kv", "cure_device_error", "cure_sample_target", "cure_lm_head_argmax",
                  "cure_rope_init", "cure_rope_init_freqs", "cure_rope_qkv", "cure_append_kv", "cure_prompt_attn",
                  "cure_rope_qkv_axes", "cure_append_kv_axes", "cure_append_kv8", "cure_prompt_attn8", "cure_tree_attn8",
-                 "cure_resync_kv8"):
+                 "cure_resync_kv8", "cure_save_kv8", "cure_restore_kv8"):
         getattr(lib, name).restype = C.c_int
     _lib = lib
     return lib

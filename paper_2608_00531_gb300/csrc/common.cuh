@@ -141,6 +141,10 @@ struct LayerScales {
   float* k[kMaxLayers];
   float* v[kMaxLayers];
 };
+// What sequences hold of the blocks that the rows behind them would share, saved or put back.
+size_t held8_bytes(int layers, int batch, const cure_kv_desc& kv);
+cudaError_t launch_held8(bool save, int layers, const LayerPtrs& caches, const LayerScales& scales, const cure_kv_desc& kv,
+                         int batch, const int32_t* cache_len, void* saved, cudaStream_t s);
 cudaError_t launch_paths8(int layers, const LayerPtrs& caches, const LayerScales& scales, const cure_kv_desc& kv,
                           const uint16_t* tree_k, const uint16_t* tree_v, int batch, int n_max, int block,
                           const int32_t* path_nodes, const int32_t* accept_len, const int32_t* cache_len, int* err,

@@ -746,6 +746,60 @@ cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_ca
   return attn8(c, kv, workspace_bytes, stream);
 }
 
+// The layers' caches in 8 bits and their scales, checked.
+static bool layers8_ok(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                       float* const* v_scales, LayerPtrs* lp, LayerScales* ls) {
+  if (!k_caches || !v_caches || !k_scales || !v_scales) return false;
+  for (int l = 0; l < layers; ++l) {
+    if (!k_caches[l] || !v_caches[l] || !aligned(k_caches[l], 16) || !aligned(v_caches[l], 16) || !k_scales[l] ||
+        !v_scales[l] || !aligned(k_scales[l], 4) || !aligned(v_scales[l], 4))
+      return false;
+    lp->k[l] = k_caches[l];
+    lp->v[l] = v_caches[l];
+    ls->k[l] = k_scales[l];
+    ls->v[l] = v_scales[l];
+  }
+  return true;
+}
+
+size_t cure_save_kv8_size(int32_t layers, int32_t batch, const cure_kv_desc* kv) {
+  cure_status why;
+  if (!kv_ok(kv, &why) || !kv8_ok(kv) || layers < 0 || layers > kMaxLayers || batch < 0) return 0;
+  return held8_bytes(layers, batch, *kv);
+}
+
+static cure_status held8(bool save, int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                         float* const* v_scales, const cure_kv_desc* kv, int32_t batch, const int32_t* cache_len,
+                         void* saved, size_t saved_bytes, void* stream) {
+  cure_status why;
+  if (!kv_ok(kv, &why)) return why;
+  if (!kv8_ok(kv)) return CURE_ERR_UNSUPPORTED;
+  if (layers < 0 || layers > kMaxLayers || batch < 0) return CURE_ERR_INVALID_ARG;
+  if (layers == 0 || batch == 0) return CURE_OK;
+  LayerPtrs lp = {};
+  LayerScales ls = {};
+  if (!layers8_ok(layers, k_caches, v_caches, k_scales, v_scales, &lp, &ls) || !cache_len || !aligned(cache_len, 4) ||
+      !saved || !aligned(saved, 16))
+    return CURE_ERR_INVALID_ARG;
+  if (saved_bytes < held8_bytes(layers, batch, *kv)) return CURE_ERR_CAPACITY;
+  return from_cuda(launch_held8(save, layers, lp, ls, *kv, batch, cache_len, saved, static_cast<cudaStream_t>(stream)));
+}
+
+cure_status cure_save_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                          float* const* v_scales, const cure_kv_desc* kv, int32_t batch, const int32_t* cache_len,
+                          void* saved, size_t saved_bytes, void* stream) {
+  ApiRange range("cure_save_kv8");
+  return held8(true, layers, k_caches, v_caches, k_scales, v_scales, kv, batch, cache_len, saved, saved_bytes, stream);
+}
+
+cure_status cure_restore_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
+                             float* const* v_scales, const cure_kv_desc* kv, int32_t batch, const int32_t* cache_len,
+                             const void* saved, size_t saved_bytes, void* stream) {
+  ApiRange range("cure_restore_kv8");
+  return held8(false, layers, k_caches, v_caches, k_scales, v_scales, kv, batch, cache_len, const_cast<void*>(saved),
+               saved_bytes, stream);
+}
+
 cure_status cure_resync_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
                             float* const* v_scales, const cure_kv_desc* kv, const void* tree_k, const void* tree_v,
                             int32_t batch, int32_t n_max, int32_t block, const int32_t* path_nodes,
@@ -765,18 +819,9 @@ cure_status cure_resync_kv8(int32_t layers, void* const* k_caches, void* const* 
   LayerPtrs lp = {};
   LayerScales ls = {};
   if (layers > 0) {
-    if (!k_caches || !v_caches || !k_scales || !v_scales || !tree_k || !tree_v || !aligned(tree_k, 16) ||
-        !aligned(tree_v, 16))
+    if (!tree_k || !tree_v || !aligned(tree_k, 16) || !aligned(tree_v, 16) ||
+        !layers8_ok(layers, k_caches, v_caches, k_scales, v_scales, &lp, &ls))
       return CURE_ERR_INVALID_ARG;
-    for (int l = 0; l < layers; ++l) {
-      if (!k_caches[l] || !v_caches[l] || !aligned(k_caches[l], 16) || !aligned(v_caches[l], 16) || !k_scales[l] ||
-          !v_scales[l] || !aligned(k_scales[l], 4) || !aligned(v_scales[l], 4))
-        return CURE_ERR_INVALID_ARG;
-      lp.k[l] = k_caches[l];
-      lp.v[l] = v_caches[l];
-      ls.k[l] = k_scales[l];
-      ls.v[l] = v_scales[l];
-    }
   }
   int* err = device_error_word();
   const cudaStream_t s = static_cast<cudaStream_t>(stream);

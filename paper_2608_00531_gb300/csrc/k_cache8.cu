@@ -504,7 +504,60 @@ paths8_kernel(const __grid_constant__ Paths8Args A) {
   }
 }
 
+struct HeldArgs {
+  LayerPtrs caches;
+  LayerScales scales;
+  cure_kv_desc kv;
+  const int32_t* cache_len;
+  uint8_t* saved;  // codes [layer][K, V][sequence][16 slots][heads][128], then scales [layer][K, V][sequence][heads]
+  int layers, batch;
+};
+
+// What sequence blockIdx.x holds of the block that the next row behind it would share (none where its length is a
+// multiple of 16), with the block's scales: of every layer's K and V out of the caches, or back.  A block's slots lie
+// end to end in either layout.  28 layers of 32 sequences, 4 heads: 7 MB each way, 5 us.
+template <bool SAVE>
+__global__ void __launch_bounds__(kThreads)
+held8_kernel(const __grid_constant__ HeldArgs A) {
+  pdl_begin();
+  const int b = blockIdx.x, L = A.cache_len[b], Hkv = A.kv.heads_kv;
+  const int64_t cap = A.kv.layout == 0 ? A.kv.max_len : (int64_t)A.kv.max_len * A.kv.page_size;
+  if (L <= 0 || L % kBlk == 0 || L > cap) return;
+  int64_t row, place;
+  if (!place_of(A.kv, b, L / kBlk, &row, &place)) return;  // (nothing can be appended there either)
+  const int n = L % kBlk * Hkv * (kD / 16);  // 16 codes each
+  const int64_t all = (int64_t)2 * A.layers * A.batch;
+  for (int item = blockIdx.y; item < 2 * A.layers; item += gridDim.y) {
+    const int l = item >> 1, v = item & 1;
+    const int64_t at = (int64_t)item * A.batch + b;
+    uint4* codes = reinterpret_cast<uint4*>(static_cast<uint8_t*>(v ? A.caches.v[l] : A.caches.k[l]) + row * Hkv * kD);
+    uint4* kept = reinterpret_cast<uint4*>(A.saved + at * kBlk * Hkv * kD);
+    float* scales = (v ? A.scales.v[l] : A.scales.k[l]) + place * Hkv;
+    float* kept_scales = reinterpret_cast<float*>(A.saved + all * kBlk * Hkv * kD) + at * Hkv;
+    for (int i = threadIdx.x; i < n; i += kThreads) (SAVE ? kept : codes)[i] = (SAVE ? codes : kept)[i];
+    for (int i = threadIdx.x; i < Hkv; i += kThreads) (SAVE ? kept_scales : scales)[i] = (SAVE ? scales : kept_scales)[i];
+  }
+}
+
 }  // namespace
+
+size_t held8_bytes(int layers, int batch, const cure_kv_desc& kv) {
+  return (size_t)2 * layers * batch * kv.heads_kv * (kBlk * kD + sizeof(float));
+}
+
+cudaError_t launch_held8(bool save, int layers, const LayerPtrs& caches, const LayerScales& scales, const cure_kv_desc& kv,
+                         int batch, const int32_t* cache_len, void* saved, cudaStream_t s) {
+  HeldArgs a;
+  a.caches = caches;
+  a.scales = scales;
+  a.kv = kv;
+  a.cache_len = cache_len;
+  a.saved = static_cast<uint8_t*>(saved);
+  a.layers = layers;
+  a.batch = batch;
+  return launch_pdl(save ? held8_kernel<true> : held8_kernel<false>, dim3((unsigned)batch, (unsigned)(2 * layers)),
+                    dim3(kThreads), 0, s, a);
+}
 
 cudaError_t launch_append8(const RopeArgs& args, float* k_scale, float* v_scale, cudaStream_t s) {
   Append8Args a;

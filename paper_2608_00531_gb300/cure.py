@@ -713,12 +713,7 @@ def cure_resync_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.T
     if out is None:
         out = dict(draft_valid_len=_new((B,), _I32, stream), replay_tokens=_new((B, P), _I32, stream),
                    n_replay=_new((B,), _I32, stream))
-    size = (B * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size) * kv.heads_kv * kv.head_dim
-    a, b, c = kv8_scale_shape(kv, B)
-    array = C.c_void_p * max(1, layers)
-    kp, vp, ksp, vsp = (array(*_pointers(t, nm, dtype, n, dev)) for t, nm, dtype, n in (
-        (k_caches, "a k_cache", _E4M3, size), (v_caches, "a v_cache", _E4M3, size),
-        (k_scales, "a k_scale", _F32, a * b * c), (v_scales, "a v_scale", _F32, a * b * c)))
+    _, kp, vp, ksp, vsp = _layers8(k_caches, v_caches, k_scales, v_scales, kv, B, dev)
     check("cure_resync_kv8", _lib.load().cure_resync_kv8(
         layers, kp, vp, ksp, vsp, C.byref(kv), _here(tree_k, "tree_k", _BF16, dev), _here(tree_v, "tree_v", _BF16, dev), B,
         n_max, block, i32(acc["path_nodes"], "path_nodes", B * P), i32(acc["accept_len"], "accept_len", B),
@@ -728,6 +723,55 @@ def cure_resync_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.T
         i32(out["n_replay"], "n_replay", B), s))
     out["cache_len"] = cache_len_out
     return out
+
+
+def cure_save_kv8_size(layers: int, batch: int, kv: KVDesc) -> int:
+    return int(_lib.load().cure_save_kv8_size(layers, batch, C.byref(kv)))
+
+
+def cure_save_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor], k_scales: Sequence[torch.Tensor],
+                  v_scales: Sequence[torch.Tensor], kv: KVDesc, cache_len: torch.Tensor, *,
+                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """What the sequences hold of the blocks that rows appended behind them would share, of every layer's cache in
+    8 bits, for cure_restore_kv8 (uint8, cure_save_kv8_size bytes): before rows are appended that may not stay."""
+    dev, s = _current(stream)
+    of = _layers8(k_caches, v_caches, k_scales, v_scales, kv, cache_len.numel(), dev)
+    if out is None:
+        out = _new((cure_save_kv8_size(of[0], cache_len.numel(), kv),), torch.uint8, stream)
+    _held8("cure_save_kv8", of, kv, cache_len, out, dev, s)
+    return out
+
+
+def cure_restore_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor],
+                     k_scales: Sequence[torch.Tensor], v_scales: Sequence[torch.Tensor], kv: KVDesc,
+                     cache_len: torch.Tensor, saved: torch.Tensor, *, stream=None) -> None:
+    """Puts back what cure_save_kv8 saved at the same lengths: the tokens' codes and scales, to the bit.  The slots behind
+    them hold nothing then."""
+    dev, s = _current(stream)
+    of = _layers8(k_caches, v_caches, k_scales, v_scales, kv, cache_len.numel(), dev)
+    _held8("cure_restore_kv8", of, kv, cache_len, saved, dev, s)
+
+
+def _layers8(k_caches, v_caches, k_scales, v_scales, kv: KVDesc, batch: int, dev: int) -> tuple:
+    """The number of layers, and the arrays of their caches' and scales' addresses, checked."""
+    layers = len(k_caches)
+    if not layers == len(v_caches) == len(k_scales) == len(v_scales):
+        raise ValueError("one k_cache, v_cache, k_scale and v_scale per layer")
+    size = (batch * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size) * kv.heads_kv * kv.head_dim
+    a, b, c = kv8_scale_shape(kv, batch)
+    array = C.c_void_p * max(1, layers)
+    return (layers, *(array(*_pointers(t, nm, dtype, n, dev)) for t, nm, dtype, n in (
+        (k_caches, "a k_cache", _E4M3, size), (v_caches, "a v_cache", _E4M3, size),
+        (k_scales, "a k_scale", _F32, a * b * c), (v_scales, "a v_scale", _F32, a * b * c))))
+
+
+def _held8(name: str, of: tuple, kv: KVDesc, cache_len: torch.Tensor, saved: torch.Tensor, dev: int, s: int) -> None:
+    """cure_save_kv8 or cure_restore_kv8 of layers that _layers8 has checked."""
+    table = getattr(kv, "_keep", None)
+    if table is not None and table.numel() < cache_len.numel() * kv.max_len:
+        raise ValueError("block_table has fewer rows than the batch has sequences")
+    check(name, getattr(_lib.load(), name)(*of, C.byref(kv), cache_len.numel(), _here(cache_len, "cache_len", _I32, dev),
+                                           _here(saved, "saved", torch.uint8, dev), saved.numel(), s))
 
 
 def _pointers(tensors, name: str, dtype, n: int, dev: int) -> list:

@@ -168,7 +168,8 @@ class RepairVerifyStep:
         # for inputs that come as projections: the rotation, norm weights per layer, and the rows made of them
         self.rope, self.q_norm, self.k_norm, self.eps = rope, q_norm, k_norm, eps
         self._rows = None
-        self._starts = self._workspace8 = None  # for caches in 8 bits: the trees' rows in a packed batch, the workspace
+        # for caches in 8 bits: the trees' rows in a packed batch, the workspace, what the sequences' last blocks hold
+        self._starts = self._workspace8 = self._held = None
         self._dev_inputs = None
         self._copy_stream = None
         self._n_host = None
@@ -177,7 +178,9 @@ class RepairVerifyStep:
     def run(self, x: StepInputs, k_caches: List[torch.Tensor], v_caches: List[torch.Tensor],
             stream=None, scales=None) -> dict:
         """One step.  scales: (k_scales, v_scales), a tensor for each cache, where the caches are held in 8 bits; the
-        tree's rows then go into the caches, behind the sequences' tokens, and are attended to there."""
+        tree's rows then go into the caches, behind the sequences' tokens, and are attended to there.  They leave
+        the caches again before the accepted path's rows are written: what a sequence holds keeps its codes and scales
+        whatever the rejected rows are."""
         ids, vals, margin, logp1 = cure.cure_score_draft(x.draft_logits, self.k, out=self.score,
                                                          stream=stream)
         tree = cure.cure_build_tree(ids, margin, x.root_tok, x.cache_len, self.tau, self.R,
@@ -210,7 +213,9 @@ class RepairVerifyStep:
         return dict(score=self.score, tree=tree, attn=self.attn_out, acc=acc, resync=rs)
 
     def _attend8(self, x: StepInputs, kl, vl, ksl, vsl, tree: dict, stream) -> None:
-        """The layers' tree attention over caches in 8 bits, each layer's tree rows appended in place before it."""
+        """The layers' tree attention over caches in 8 bits, each layer's tree rows appended in place before it.  A
+        tree's first rows share a block, and its scale, with a sequence's last tokens: those are saved before, and put
+        back behind the attention, also where a call of it is refused."""
         if self._starts is None:
             with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
                 if torch.cuda.is_current_stream_capturing():
@@ -219,12 +224,20 @@ class RepairVerifyStep:
                 self._starts = torch.arange(0, (self.B + 1) * self.n_max, self.n_max, dtype=torch.int32, device=dev)
                 size = cure.cure_tree_attn8_workspace_size(self.B, self.n_max, self.Hq, self.kv)
                 self._workspace8 = torch.empty(max(size, 256), dtype=torch.uint8, device=dev)
-        for l in range(self.layers):
-            caches = (kl[l], vl[l], ksl[l], vsl[l])
-            cure.cure_append_kv8(x.tree_k[l], x.tree_v[l], *caches, self.kv, self._starts, x.cache_len, None,
-                                 pos=tree["pos"], stream=stream)
-            cure.cure_tree_attn8(x.q[l], *caches, self.kv, x.cache_len, tree["n_nodes"], tree["anc"], self.scale,
-                                 out=self.attn_out[l], workspace=self._workspace8, stream=stream)
+                self._held = torch.empty(max(cure.cure_save_kv8_size(self.layers, self.B, self.kv), 256),
+                                         dtype=torch.uint8, device=dev)
+        dev, s = cure._current(stream)
+        of = cure._layers8(kl, vl, ksl, vsl, self.kv, self.B, dev)
+        cure._held8("cure_save_kv8", of, self.kv, x.cache_len, self._held, dev, s)
+        try:
+            for l in range(self.layers):
+                caches = (kl[l], vl[l], ksl[l], vsl[l])
+                cure.cure_append_kv8(x.tree_k[l], x.tree_v[l], *caches, self.kv, self._starts, x.cache_len, None,
+                                     pos=tree["pos"], stream=stream)
+                cure.cure_tree_attn8(x.q[l], *caches, self.kv, x.cache_len, tree["n_nodes"], tree["anc"], self.scale,
+                                     out=self.attn_out[l], workspace=self._workspace8, stream=stream)
+        finally:
+            cure._held8("cure_restore_kv8", of, self.kv, x.cache_len, self._held, dev, s)
 
     def _rotate(self, x: StepInputs, pos: torch.Tensor, stream) -> StepInputs:
         """The step's Q/K/V from the layers' projections at the tree's positions (rows past a sequence's nodes
