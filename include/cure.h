@@ -585,7 +585,7 @@ size_t cure_tree_attn8_workspace_size(int32_t batch, int32_t n_max, int32_t head
  * nothing then.  In between only rows at or behind cache_len[b] may have been
  * written.  Before a tree's cure_append_kv8, and behind the last attention that reads its
  * rows, in front of cure_resync_kv8.  k_caches .. v_scales: HOST arrays of `layers`
- * device pointers (0 .. 128 layers); saved: device memory of at least
+ * device pointers (0 .. 128 layers), none twice; saved: device memory of at least
  * cure_save_kv8_size() bytes, 16-byte aligned.
  */
 cure_status cure_save_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
@@ -603,7 +603,9 @@ size_t cure_save_kv8_size(int32_t layers, int32_t batch, const cure_kv_desc* kv)
  * [layers][B][n_max][Hkv][D], not NULL: what the cache holds of the tree has been rounded
  * with other rows' scales) and written as cure_append_kv8 writes rows behind the
  * cache_len_in[b] tokens that a sequence holds.  k_scales, v_scales: HOST arrays of `layers`
- * device pointers, as the caches.  Lengths and replay lists as in cure_resync_kv.
+ * device pointers, as the caches; no cache and no scales twice (CURE_ERR_INVALID_ARG: two
+ * layers that share a block would give it two scales).  Lengths and replay lists as in
+ * cure_resync_kv.
  */
 cure_status cure_resync_kv8(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
                             float* const* v_scales, const cure_kv_desc* kv, const void* tree_k, const void* tree_v,

@@ -5,6 +5,8 @@
 #include <math.h>
 #include <nvtx3/nvToolsExt.h>
 
+#include <algorithm>
+#include <array>
 #include <atomic>
 #include <chrono>
 #include <mutex>
@@ -746,7 +748,16 @@ cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_ca
   return attn8(c, kv, workspace_bytes, stream);
 }
 
-// The layers' caches in 8 bits and their scales, checked.
+// Whether no two of n addresses are the same.
+static bool all_apart(const void* const* p, int n) {
+  std::array<uintptr_t, 2 * kMaxLayers> a;
+  for (int i = 0; i < n; ++i) a[i] = reinterpret_cast<uintptr_t>(p[i]);
+  std::sort(a.begin(), a.begin() + n);
+  return std::adjacent_find(a.begin(), a.begin() + n) == a.begin() + n;
+}
+
+// The layers' caches in 8 bits and their scales, checked.  A block that two of them share would be expressed anew by
+// both at once, under two scales.
 static bool layers8_ok(int32_t layers, void* const* k_caches, void* const* v_caches, float* const* k_scales,
                        float* const* v_scales, LayerPtrs* lp, LayerScales* ls) {
   if (!k_caches || !v_caches || !k_scales || !v_scales) return false;
@@ -759,7 +770,14 @@ static bool layers8_ok(int32_t layers, void* const* k_caches, void* const* v_cac
     ls->k[l] = k_scales[l];
     ls->v[l] = v_scales[l];
   }
-  return true;
+  const void *caches[2 * kMaxLayers], *scales[2 * kMaxLayers];
+  for (int l = 0; l < layers; ++l) {
+    caches[2 * l] = k_caches[l];
+    caches[2 * l + 1] = v_caches[l];
+    scales[2 * l] = k_scales[l];
+    scales[2 * l + 1] = v_scales[l];
+  }
+  return all_apart(caches, 2 * layers) && all_apart(scales, 2 * layers);
 }
 
 size_t cure_save_kv8_size(int32_t layers, int32_t batch, const cure_kv_desc* kv) {

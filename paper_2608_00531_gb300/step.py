@@ -180,7 +180,9 @@ class RepairVerifyStep:
         """One step.  scales: (k_scales, v_scales), a tensor for each cache, where the caches are held in 8 bits; the
         tree's rows then go into the caches, behind the sequences' tokens, and are attended to there.  They leave
         the caches again before the accepted path's rows are written: what a sequence holds keeps its codes and scales
-        whatever the rejected rows are."""
+        whatever the rejected rows are.  Layers that share a cache (layer_map) cannot be held in 8 bits."""
+        if scales is not None and len(set(self.layer_map[:self.layers])) < self.layers:
+            raise ValueError("layers that share a cache cannot be held in 8 bits")
         ids, vals, margin, logp1 = cure.cure_score_draft(x.draft_logits, self.k, out=self.score,
                                                          stream=stream)
         tree = cure.cure_build_tree(ids, margin, x.root_tok, x.cache_len, self.tau, self.R,

@@ -16,9 +16,9 @@ def test_size(lib):  # noqa: F811
 
 @pytest.mark.parametrize("name", ["cure_save_kv8", "cure_restore_kv8"])
 def test_refusals(lib, name):  # noqa: F811
-    array = (C.c_void_p * 2)(1 << 20, 2 << 20)
+    kc, vc, ks, vs = ((C.c_void_p * 2)(i << 20, (i + 1) << 20) for i in (1, 3, 5, 7))
     need = lib.cure_save_kv8_size(2, 3, _kv())
-    ok = dict(layers=2, kc=array, vc=array, ks=array, vs=array, kv=_kv(), batch=3, cl=DEV, saved=DEV, bytes=need)
+    ok = dict(layers=2, kc=kc, vc=vc, ks=ks, vs=vs, kv=_kv(), batch=3, cl=DEV, saved=DEV, bytes=need)
 
     def call(**kw):
         return getattr(lib, name)(*dict(ok, **kw).values(), None)
