@@ -48,6 +48,10 @@ class StepInputs:
     # bf16 [layers][B][n_max][(Hq + 2 Hkv) D]: Q, K and V as the projections give them, before the head norms and the
     # rotation; q, tree_k and tree_v are then None
     qkv: Optional[torch.Tensor] = None
+    # int32 [B]: the position of each sequence's root token where that is not its slot cache_len[b], as behind a prompt
+    # whose images' tokens stand at fewer positions than they are (the `pos` and `axes` of PromptPass.layer); not negative.
+    # The tree's tokens are text: they count on from there, the same on every axis, and so do the accepted ones.
+    next_pos: Optional[torch.Tensor] = None
 
 
 def _parts(qkv: torch.Tensor, heads_q: int, heads_kv: int, head_dim: int):
@@ -94,7 +98,8 @@ class PromptPass:
 
         scales: (k_scale, v_scale) of a cache held in 8 bits.  pos, axes: the rows' positions, where they are not their
         places in their sequences (cure_append_kv); rows see the keys up to their own place whatever their positions,
-        so none may be negative."""
+        so none may be negative.  Steps behind such rows take the position that the text goes on from as
+        StepInputs.next_pos."""
         n = qkv.shape[0]
         if n > self.rows:
             raise ValueError(f"PromptPass was made for {self.rows} rows, got {n}")
@@ -183,9 +188,12 @@ class RepairVerifyStep:
         whatever the rejected rows are.  Layers that share a cache (layer_map) cannot be held in 8 bits."""
         if scales is not None and len(set(self.layer_map[:self.layers])) < self.layers:
             raise ValueError("layers that share a cache cannot be held in 8 bits")
+        root_pos = x.cache_len if x.next_pos is None else x.next_pos
+        if x.next_pos is not None:
+            cure._sized(x.next_pos, "next_pos", self.B, cure._current(stream)[0])
         ids, vals, margin, logp1 = cure.cure_score_draft(x.draft_logits, self.k, out=self.score,
                                                          stream=stream)
-        tree = cure.cure_build_tree(ids, margin, x.root_tok, x.cache_len, self.tau, self.R,
+        tree = cure.cure_build_tree(ids, margin, x.root_tok, root_pos, self.tau, self.R,
                                     self.branches, self.depth, x.redraft, self.max_ufp,
                                     out=self.tree, stream=stream)
         kl = [k_caches[self.layer_map[l]] for l in range(self.layers)]
@@ -242,8 +250,8 @@ class RepairVerifyStep:
             cure._held8("cure_restore_kv8", of, self.kv, x.cache_len, self._held, dev, s)
 
     def _rotate(self, x: StepInputs, pos: torch.Tensor, stream) -> StepInputs:
-        """The step's Q/K/V from the layers' projections at the tree's positions (rows past a sequence's nodes
-        keep what they held)."""
+        """The step's Q/K/V from the layers' projections at the tree's positions (``StepInputs.next_pos`` where those
+        are not slots; rows past a sequence's nodes keep what they held)."""
         if x.qkv.shape[:3] != (self.layers, self.B, self.n_max):
             raise ValueError("qkv must be [layers][batch][n_max][..]")
         if self._rows is None:
@@ -273,6 +281,8 @@ class RepairVerifyStep:
         Results stay on the device, as in run()."""
         if xh.qkv is not None:
             raise ValueError("run_from_host takes q, tree_k and tree_v, not the layers' projections")
+        if xh.next_pos is not None and (xh.next_pos.dtype is not torch.int32 or xh.next_pos.numel() != self.B):
+            raise ValueError(f"next_pos must hold {self.B} int32 positions")
         fields = ("draft_logits", "root_tok", "cache_len", "q", "tree_k", "tree_v", "target_logits")
         dev = self.attn_out.device
         if self._dev_inputs is None or any(self._dev_inputs[f].shape != getattr(xh, f).shape for f in fields):
@@ -308,9 +318,13 @@ class RepairVerifyStep:
                        d["tree_v"], d["target_logits"])
         with torch.cuda.stream(main):
             main.wait_event(ev_first)
+            root_pos = x.cache_len
+            if xh.next_pos is not None:
+                root_pos = xh.next_pos.to(dev, non_blocking=True)
+                h2d += xh.next_pos.numel() * 4
             ids, vals, margin, logp1 = cure.cure_score_draft(x.draft_logits, self.k, out=self.score,
                                                              stream=main)
-            tree = cure.cure_build_tree(ids, margin, x.root_tok, x.cache_len, self.tau, self.R,
+            tree = cure.cure_build_tree(ids, margin, x.root_tok, root_pos, self.tau, self.R,
                                         self.branches, self.depth, x.redraft, self.max_ufp,
                                         out=self.tree, stream=main)
             node_rows = xh.target_logits.numel() * xh.target_logits.element_size() >= self.NODE_ROWS_MIN_BYTES
