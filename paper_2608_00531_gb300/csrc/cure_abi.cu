@@ -831,9 +831,10 @@ cure_status cure_resync_kv8(int32_t layers, void* const* k_caches, void* const* 
   if (layers < 0 || layers > kMaxLayers || batch < 0 || n_max < 1 || block < 1 || block > 32 || n_max < block + 1)
     return CURE_ERR_INVALID_ARG;
   if (batch == 0) return CURE_OK;
-  if (!path_nodes || !accept_len || !diverge_depth || !out_tokens || !cache_len_in || !cache_len_out ||
-      !draft_valid_len || !replay_tokens || !n_replay)
-    return CURE_ERR_INVALID_ARG;
+  for (const int32_t* p : {path_nodes, accept_len, diverge_depth, out_tokens, cache_len_in,
+                           static_cast<const int32_t*>(cache_len_out), static_cast<const int32_t*>(draft_valid_len),
+                           static_cast<const int32_t*>(replay_tokens), static_cast<const int32_t*>(n_replay)})
+    if (!p || !aligned(p, 4)) return CURE_ERR_INVALID_ARG;
   LayerPtrs lp = {};
   LayerScales ls = {};
   if (layers > 0) {
