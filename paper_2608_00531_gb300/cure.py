@@ -734,11 +734,11 @@ def cure_save_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Ten
                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """What the sequences hold of the blocks that rows appended behind them would share, of every layer's cache in
     8 bits, for cure_restore_kv8 (uint8, cure_save_kv8_size bytes): before rows are appended that may not stay."""
-    dev, s = _current(stream)
-    of = _layers8(k_caches, v_caches, k_scales, v_scales, kv, cache_len.numel(), dev)
+    (dev, s), B = _current(stream), cache_len.numel()
+    of = _layers8(k_caches, v_caches, k_scales, v_scales, kv, B, dev)
     if out is None:
-        out = _new((cure_save_kv8_size(of[0], cache_len.numel(), kv),), torch.uint8, stream)
-    _held8("cure_save_kv8", of, kv, cache_len, out, dev, s)
+        out = _new((cure_save_kv8_size(of[0], B, kv),), torch.uint8, stream)
+    _held8("cure_save_kv8", of, kv, B, cache_len, out, dev, s)
     return out
 
 
@@ -747,9 +747,9 @@ def cure_restore_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.
                      cache_len: torch.Tensor, saved: torch.Tensor, *, stream=None) -> None:
     """Puts back what cure_save_kv8 saved at the same lengths: the tokens' codes and scales, to the bit.  The slots behind
     them hold nothing then."""
-    dev, s = _current(stream)
-    of = _layers8(k_caches, v_caches, k_scales, v_scales, kv, cache_len.numel(), dev)
-    _held8("cure_restore_kv8", of, kv, cache_len, saved, dev, s)
+    (dev, s), B = _current(stream), cache_len.numel()
+    of = _layers8(k_caches, v_caches, k_scales, v_scales, kv, B, dev)
+    _held8("cure_restore_kv8", of, kv, B, cache_len, saved, dev, s)
 
 
 def _layers8(k_caches, v_caches, k_scales, v_scales, kv: KVDesc, batch: int, dev: int) -> tuple:
@@ -757,6 +757,9 @@ def _layers8(k_caches, v_caches, k_scales, v_scales, kv: KVDesc, batch: int, dev
     layers = len(k_caches)
     if not layers == len(v_caches) == len(k_scales) == len(v_scales):
         raise ValueError("one k_cache, v_cache, k_scale and v_scale per layer")
+    table = getattr(kv, "_keep", None)
+    if table is not None and table.numel() < batch * kv.max_len:
+        raise ValueError("block_table has fewer rows than the batch has sequences")
     size = (batch * kv.max_len if kv.layout == 0 else kv.num_pages * kv.page_size) * kv.heads_kv * kv.head_dim
     a, b, c = kv8_scale_shape(kv, batch)
     array = C.c_void_p * max(1, layers)
@@ -765,12 +768,10 @@ def _layers8(k_caches, v_caches, k_scales, v_scales, kv: KVDesc, batch: int, dev
         (k_scales, "a k_scale", _F32, a * b * c), (v_scales, "a v_scale", _F32, a * b * c))))
 
 
-def _held8(name: str, of: tuple, kv: KVDesc, cache_len: torch.Tensor, saved: torch.Tensor, dev: int, s: int) -> None:
-    """cure_save_kv8 or cure_restore_kv8 of layers that _layers8 has checked."""
-    table = getattr(kv, "_keep", None)
-    if table is not None and table.numel() < cache_len.numel() * kv.max_len:
-        raise ValueError("block_table has fewer rows than the batch has sequences")
-    check(name, getattr(_lib.load(), name)(*of, C.byref(kv), cache_len.numel(), _here(cache_len, "cache_len", _I32, dev),
+def _held8(name: str, of: tuple, kv: KVDesc, batch: int, cache_len: torch.Tensor, saved: torch.Tensor, dev: int,
+           s: int) -> None:
+    """cure_save_kv8 or cure_restore_kv8 of layers that _layers8 has checked for `batch` sequences."""
+    check(name, getattr(_lib.load(), name)(*of, C.byref(kv), batch, _sized(cache_len, "cache_len", batch, dev),
                                            _here(saved, "saved", torch.uint8, dev), saved.numel(), s))
 
 

@@ -238,7 +238,7 @@ class RepairVerifyStep:
                                          dtype=torch.uint8, device=dev)
         dev, s = cure._current(stream)
         of = cure._layers8(kl, vl, ksl, vsl, self.kv, self.B, dev)
-        cure._held8("cure_save_kv8", of, self.kv, x.cache_len, self._held, dev, s)
+        cure._held8("cure_save_kv8", of, self.kv, self.B, x.cache_len, self._held, dev, s)
         try:
             for l in range(self.layers):
                 caches = (kl[l], vl[l], ksl[l], vsl[l])
@@ -247,7 +247,7 @@ class RepairVerifyStep:
                 cure.cure_tree_attn8(x.q[l], *caches, self.kv, x.cache_len, tree["n_nodes"], tree["anc"], self.scale,
                                      out=self.attn_out[l], workspace=self._workspace8, stream=stream)
         finally:
-            cure._held8("cure_restore_kv8", of, self.kv, x.cache_len, self._held, dev, s)
+            cure._held8("cure_restore_kv8", of, self.kv, self.B, x.cache_len, self._held, dev, s)
 
     def _rotate(self, x: StepInputs, pos: torch.Tensor, stream) -> StepInputs:
         """The step's Q/K/V from the layers' projections at the tree's positions (``StepInputs.next_pos`` where those
