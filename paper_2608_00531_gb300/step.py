@@ -175,6 +175,7 @@ class RepairVerifyStep:
         self._rows = None
         # for caches in 8 bits: the trees' rows in a packed batch, the workspace, what the sequences' last blocks hold
         self._starts = self._workspace8 = self._held = None
+        self._more_launches = 0  # of the last step
         self._dev_inputs = None
         self._copy_stream = None
         self._n_host = None
@@ -198,6 +199,7 @@ class RepairVerifyStep:
                                     out=self.tree, stream=stream)
         kl = [k_caches[self.layer_map[l]] for l in range(self.layers)]
         vl = [v_caches[self.layer_map[l]] for l in range(self.layers)]
+        self._more_launches = (0 if x.qkv is None else self.layers) + (0 if scales is None else self.layers + 3)
         if x.qkv is not None:
             x = self._rotate(x, tree["pos"], stream)
         if scales is not None:
@@ -360,13 +362,14 @@ class RepairVerifyStep:
             rs = cure.cure_resync_kv(kl, vl, self.kv, x.tree_k, x.tree_v, acc, x.cache_len, self.K,
                                      cache_len_out=self.cache_len_out, out=self.rs, stream=main)
         self.last_h2d_bytes = h2d
+        self._more_launches = 0
         return dict(score=self.score, tree=tree, attn=self.attn_out, acc=acc, resync=rs)
 
     @property
     def launches_per_step(self) -> int:
-        """Library kernels one step launches: scan, tree, one attention kernel per
-        layer, target argmax + walk, and the resync gather (its finalize runs in
+        """Library kernels that a step like the last one launches (before the first: one over bf16 caches, from Q, K and V):
+        scan, tree, one attention kernel per layer, target argmax + walk, and the resync gather (its finalize runs in
         the gather's grid, since the step's new lengths do not alias the old).
-        Inputs that come as projections take one more per layer; caches in 8 bits one more per
-        layer, and one more in all."""
-        return 1 + 1 + self.layers + 2 + 1
+        Inputs that come as projections take one more per layer; caches in 8 bits one more per layer, and three in all
+        (what the last blocks hold saved and put back, the lengths)."""
+        return 1 + 1 + self.layers + 2 + 1 + self._more_launches
