@@ -654,6 +654,20 @@ cure_status cure_selftest_prompt_timeout(const void* q, const void* k_cache, con
                                          void* stream);
 
 /*
+ * The same of cure_prompt_attn8 (of few rows a sequence on average: warps 0 .. 11; else 0 .. 15) and cure_tree_attn8.
+ */
+cure_status cure_selftest_prompt8_timeout(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                          const float* v_scale, const cure_kv_desc* kv, const int32_t* row_start,
+                                          const int32_t* cache_len, int32_t rows, int32_t batch, int32_t heads_q,
+                                          float scale, void* out, void* workspace, size_t workspace_bytes, int32_t warp,
+                                          int32_t wait, void* stream);
+cure_status cure_selftest_tree8_timeout(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                        const float* v_scale, const cure_kv_desc* kv, const int32_t* cache_len,
+                                        const int32_t* n_nodes, const uint64_t* anc, int32_t batch, int32_t n_max,
+                                        int32_t heads_q, float scale, void* out, void* workspace,
+                                        size_t workspace_bytes, int32_t warp, int32_t wait, void* stream);
+
+/*
  * Self-test: the form a cure_tree_attn call of this shape takes (`kv` and
  * `route` are HOST pointers; in_place != 0: the in-place layout).  route[0] is
  * the number of CTAs in each unit's cluster (0: the persistent form), route[1]

@@ -25,7 +25,7 @@ EXPORTS = ("cure_score_draft", "cure_build_tree", "cure_tree_attn", "cure_tree_a
            "cure_append_kv", "cure_prompt_attn", "cure_prompt_attn_workspace_size", "cure_device_error",
            "cure_rope_qkv_axes", "cure_append_kv_axes", "cure_append_kv8", "cure_prompt_attn8",
            "cure_prompt_attn8_workspace_size", "cure_tree_attn8", "cure_tree_attn8_workspace_size", "cure_resync_kv8",
-           "cure_save_kv8", "cure_save_kv8_size", "cure_restore_kv8", "cure_status_string", "cure_abi_version")
+           "cure_selftest_prompt8_timeout", "cure_selftest_tree8_timeout", "cure_save_kv8", "cure_save_kv8_size", "cure_restore_kv8", "cure_status_string", "cure_abi_version")
 
 
 class TreeParams(C.Structure):
@@ -130,6 +130,8 @@ def load() -> C.CDLL:
     lib.cure_restore_kv8.argtypes = lib.cure_save_kv8.argtypes
     lib.cure_save_kv8_size.argtypes = [I32, I32, C.POINTER(KVDesc)]
     lib.cure_save_kv8_size.restype = C.c_size_t
+    lib.cure_selftest_prompt8_timeout.argtypes = [*lib.cure_prompt_attn8.argtypes[:-1], I32, I32, P]
+    lib.cure_selftest_tree8_timeout.argtypes = [*lib.cure_tree_attn8.argtypes[:-1], I32, I32, P]
     lib.cure_device_error.argtypes = [P, C.POINTER(I32)]
     lib.cure_status_string.argtypes = [C.c_int]
     lib.cure_status_string.restype = C.c_char_p

@@ -171,6 +171,7 @@ struct Attn8Call {
   uint16_t* out;
   void* workspace;
   int* err;
+  int expire_warp, expire_wait;  // self-test: > 0 waits, that warp's expire_wait-th in CTA 0 is on a barrier that nothing completes
 };
 size_t attn8_workspace();
 cudaError_t launch_attn8(const Attn8Call& c, cudaStream_t s);

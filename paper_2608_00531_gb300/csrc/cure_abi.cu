@@ -690,16 +690,16 @@ static cure_status attn8(Attn8Call& c, const cure_kv_desc* kv, size_t workspace_
       !aligned(c.workspace, 256) || !aligned(c.k_scale, 4) || !aligned(c.v_scale, 4) || !aligned(c.cache_len, 4))
     return CURE_ERR_INVALID_ARG;
   if (workspace_bytes < attn8_workspace()) return CURE_ERR_CAPACITY;
+  if (c.expire_wait < 0 || c.expire_warp < 0 || c.expire_warp > 15) return CURE_ERR_INVALID_ARG;
   c.kv = *kv;
   c.err = device_error_word();
   return from_cuda(launch_attn8(c, static_cast<cudaStream_t>(stream)));
 }
 
-cure_status cure_prompt_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
-                              const float* v_scale, const cure_kv_desc* kv, const int32_t* row_start,
-                              const int32_t* cache_len, int32_t rows, int32_t batch, int32_t heads_q, float scale,
-                              void* out, void* workspace, size_t workspace_bytes, void* stream) {
-  ApiRange range("cure_prompt_attn8");
+static cure_status prompt_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                const float* v_scale, const cure_kv_desc* kv, const int32_t* row_start,
+                                const int32_t* cache_len, int32_t rows, int32_t batch, int32_t heads_q, float scale,
+                                void* out, void* workspace, size_t workspace_bytes, void* stream, int warp, int wait) {
   const cure_status st = prompt_shape_ok(rows, batch, heads_q, kv);
   if (st != CURE_OK) return st;
   if (rows > 0 && batch > 0 && (!row_start || !aligned(row_start, 4))) return CURE_ERR_INVALID_ARG;
@@ -717,15 +717,36 @@ cure_status cure_prompt_attn8(const void* q, const void* k_cache, const void* v_
   c.scale = scale;
   c.out = static_cast<uint16_t*>(out);
   c.workspace = workspace;
+  c.expire_warp = warp;
+  c.expire_wait = wait;
   return attn8(c, kv, workspace_bytes, stream);
 }
 
-cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
-                            const float* v_scale, const cure_kv_desc* kv, const int32_t* cache_len,
-                            const int32_t* n_nodes, const uint64_t* anc, int32_t batch, int32_t n_max,
-                            int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
-                            void* stream) {
-  ApiRange range("cure_tree_attn8");
+cure_status cure_prompt_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                              const float* v_scale, const cure_kv_desc* kv, const int32_t* row_start,
+                              const int32_t* cache_len, int32_t rows, int32_t batch, int32_t heads_q, float scale,
+                              void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  ApiRange range("cure_prompt_attn8");
+  return prompt_attn8(q, k_cache, v_cache, k_scale, v_scale, kv, row_start, cache_len, rows, batch, heads_q, scale, out,
+                      workspace, workspace_bytes, stream, 0, 0);
+}
+
+cure_status cure_selftest_prompt8_timeout(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                          const float* v_scale, const cure_kv_desc* kv, const int32_t* row_start,
+                                          const int32_t* cache_len, int32_t rows, int32_t batch, int32_t heads_q,
+                                          float scale, void* out, void* workspace, size_t workspace_bytes, int32_t warp,
+                                          int32_t wait, void* stream) {
+  ApiRange range("cure_selftest_prompt8_timeout");
+  if (wait < 1) return CURE_ERR_INVALID_ARG;
+  return prompt_attn8(q, k_cache, v_cache, k_scale, v_scale, kv, row_start, cache_len, rows, batch, heads_q, scale, out,
+                      workspace, workspace_bytes, stream, warp, wait);
+}
+
+static cure_status tree_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                              const float* v_scale, const cure_kv_desc* kv, const int32_t* cache_len,
+                              const int32_t* n_nodes, const uint64_t* anc, int32_t batch, int32_t n_max,
+                              int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
+                              void* stream, int warp, int wait) {
   const cure_status st = tree8_shape_ok(batch, n_max, heads_q, kv);
   if (st != CURE_OK) return st;
   if (batch > 0 && (!n_nodes || !anc || !aligned(n_nodes, 4) || !aligned(anc, 8))) return CURE_ERR_INVALID_ARG;
@@ -745,7 +766,30 @@ cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_ca
   c.scale = scale;
   c.out = static_cast<uint16_t*>(out);
   c.workspace = workspace;
+  c.expire_warp = warp;
+  c.expire_wait = wait;
   return attn8(c, kv, workspace_bytes, stream);
+}
+
+cure_status cure_tree_attn8(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                            const float* v_scale, const cure_kv_desc* kv, const int32_t* cache_len,
+                            const int32_t* n_nodes, const uint64_t* anc, int32_t batch, int32_t n_max,
+                            int32_t heads_q, float scale, void* out, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  ApiRange range("cure_tree_attn8");
+  return tree_attn8(q, k_cache, v_cache, k_scale, v_scale, kv, cache_len, n_nodes, anc, batch, n_max, heads_q, scale, out,
+                    workspace, workspace_bytes, stream, 0, 0);
+}
+
+cure_status cure_selftest_tree8_timeout(const void* q, const void* k_cache, const void* v_cache, const float* k_scale,
+                                        const float* v_scale, const cure_kv_desc* kv, const int32_t* cache_len,
+                                        const int32_t* n_nodes, const uint64_t* anc, int32_t batch, int32_t n_max,
+                                        int32_t heads_q, float scale, void* out, void* workspace,
+                                        size_t workspace_bytes, int32_t warp, int32_t wait, void* stream) {
+  ApiRange range("cure_selftest_tree8_timeout");
+  if (wait < 1) return CURE_ERR_INVALID_ARG;
+  return tree_attn8(q, k_cache, v_cache, k_scale, v_scale, kv, cache_len, n_nodes, anc, batch, n_max, heads_q, scale, out,
+                    workspace, workspace_bytes, stream, warp, wait);
 }
 
 // Whether no two of n addresses are the same.

@@ -67,7 +67,7 @@ struct Layout {
     B_WFULL = B_VEMPTY + NV, B_WEMPTY = B_WFULL + NW, B_SFULL = B_WEMPTY + NW, B_PFULL = B_SFULL + 2,
     B_PVDONE = B_PFULL + 2, B_STAT = B_PVDONE + 2, B_OFREE = B_STAT + 2, B_DRAIN = B_OFREE + 2, B_JOIN = B_DRAIN + 2,
     B_SCALES = B_JOIN + 1, piece_bar = B_SCALES + kScaleSlots, taken_bar = piece_bar + kPieces,
-    num_bars = taken_bar + kPieces
+    B_NEVER = taken_bar + kPieces, num_bars
   };
   static constexpr int q = 0;                        // Q[m][part]
   static constexpr int k = q + MT * 2 * kQHalf;      // K[stage]
@@ -177,6 +177,7 @@ __host__ __device__ constexpr uint32_t idesc_0(int M, int N, bool b_mn_major) {
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
+constexpr uint32_t kGaveUp = 0x7fc0dead;  // a NaN that no arithmetic gives: the log-sum-exps of a CTA that gave up
 constexpr float kLift = 7.f;  // P' is 2^kLift times what it stands for: at most 2^15 with the lag of 2^8
 
 // ---- clusters: barrier, a peer's address of a shared-memory variable, loads from it
@@ -211,8 +212,9 @@ __device__ __forceinline__ void tmem_ld16_max(uint32_t taddr, uint32_t* r, float
 }
 
 // Units of two M tiles; or with CLUSTER (a tree's rows) of one, each with a cluster of A.cluster CTAs to
-// itself, which take an equal part of its tiles each and join them through distributed shared memory.
-template <class Args, bool CLUSTER>
+// itself, which take an equal part of its tiles each and join them through distributed shared memory.  EXPIRE
+// (self-test): one wait of one warp runs out.
+template <class Args, bool CLUSTER, bool EXPIRE>
 __global__ void __launch_bounds__(kThreads, 1)
 attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
              const __grid_constant__ CUtensorMap tm_q, const Args A) {
@@ -271,6 +273,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       mbar_init(bar(Lay::piece_bar + i), 1);
       mbar_init(bar(Lay::taken_bar + i), kTakers);
     }
+    if constexpr (EXPIRE) mbar_init(bar(Lay::B_NEVER), 1);
     *abort_flag = 0;
     *n_joins = 0;
     fence_mbar_init();
@@ -286,7 +289,11 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + Lay::tmem_slot);
-  Await<false> await;
+  Await<EXPIRE> await;
+  if constexpr (EXPIRE) {
+    await.never = bar(Lay::B_NEVER);
+    await.left = blockIdx.x == 0 && warp == A.expire_warp ? (uint32_t)A.expire_wait : 0u;
+  }
   Pieces pieces{0};
   Piece x;
   // Whether a piece has rows in both M tiles; else both softmax groups take M tile 0's, a tile each in turn.
@@ -879,8 +886,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
     // Each CTA of the cluster joins some of the unit's rows, a float4 a thread:
     //   O = sum_p 2^(lse_p) O_p / sum_p 2^(lse_p) over the parts that saw a key
     const Piece& p = *reinterpret_cast<const Piece*>(smem + Lay::pieces);
-    if (p.t0 >= p.t1 || *abort_flag)  // this CTA's part has none
-      for (int i = tid; i < BM; i += kThreads) lse_of[i] = -FLT_MAX;
+    // this CTA has given up (the unit's rows are then left unwritten), or its part has no keys
+    const float none = *abort_flag ? __uint_as_float(kGaveUp) : -FLT_MAX;
+    if (p.t0 >= p.t1 || *abort_flag)
+      for (int i = tid; i < BM; i += kThreads) lse_of[i] = none;
     cluster_sync();
     const int rank = (int)blockIdx.x % A.cluster;
     const int rows = min(npb, p.n - p.rg * npb) * G, each = (max(rows, 0) + A.cluster - 1) / A.cluster;
@@ -889,6 +898,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
       const int r = first + i % mine, c = i / mine;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       float top = -FLT_MAX, total = 0.f;
+      bool gave_up = false;
       const uint32_t l_at = sb + Lay::lse + r * 4, o_at = sb + Lay::w + (c * BM + r) * 16;
       for (int q0 = 0; q0 < A.cluster; q0 += 4) {
         float w[4], best = top;
@@ -899,6 +909,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
           w[q] = ld_cluster(map_rank(l_at, from));
           o[q] = ld_cluster_v4(map_rank(o_at, from));
           if (q0 + q >= A.cluster) w[q] = -FLT_MAX;
+          gave_up |= __float_as_uint(w[q]) == kGaveUp;
           best = fmaxf(best, w[q]);
         }
         const float a = ex2(top - best);
@@ -914,6 +925,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
                             fmaf(wq, o[q].w, acc.w));
         }
       }
+      if (gave_up) continue;
       const float inv = total > 0.f ? 1.f / total : 0.f;
       uint16_t* orow = A.out + ((int64_t)(p.r0 + p.rg * npb + r / G) * A.heads_q + p.h * G + r % G) * D;
       *reinterpret_cast<uint2*>(orow + 4 * c) =
@@ -930,7 +942,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
 }
 
 // Dynamic shared memory (and clusters above the portable size), once per device.
-template <class Args, bool CLUSTER>
+template <class Args, bool CLUSTER, bool EXPIRE = false>
 cudaError_t set_up() {
   static std::atomic<uint64_t> ready;
   int dev = 0;
@@ -938,7 +950,7 @@ cudaError_t set_up() {
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (ready.load() & bit) return cudaSuccess;
-  const auto kernel = attn8_kernel<Args, CLUSTER>;
+  const auto kernel = attn8_kernel<Args, CLUSTER, EXPIRE>;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<CLUSTER ? 1 : 2>::bytes);
   if (e == cudaSuccess && CLUSTER) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) ready.fetch_or(bit);
@@ -963,7 +975,7 @@ int max_clusters(int size) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, attn8_kernel<Tree8, true>, &cfg) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveClusters(&n, attn8_kernel<Tree8, true, false>, &cfg) != cudaSuccess) {
       cudaGetLastError();
       n = 0;
     }
@@ -981,9 +993,9 @@ int cluster_size(int64_t units) {
   return 0;
 }
 
-template <bool CLUSTER, class Args>
+template <bool CLUSTER, bool EXPIRE, class Args>
 cudaError_t launch(const Attn8Call& c, Args& A, int grid, cudaStream_t s) {
-  const cudaError_t e = set_up<Args, CLUSTER>();
+  const cudaError_t e = set_up<Args, CLUSTER, EXPIRE>();
   if (e != cudaSuccess) return e;
   CUtensorMap mk, mv, mq;
   const int box = c.kv.layout == 1 ? c.kv.page_size : BN;
@@ -1014,7 +1026,11 @@ cudaError_t launch(const Attn8Call& c, Args& A, int grid, cudaStream_t s) {
     attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
   }
-  return cudaLaunchKernelEx(&cfg, attn8_kernel<Args, CLUSTER>, mk, mv, mq, A);
+  return cudaLaunchKernelEx(&cfg, attn8_kernel<Args, CLUSTER, EXPIRE>, mk, mv, mq, A);
+}
+template <bool CLUSTER, class Args>
+cudaError_t launch(const Attn8Call& c, Args& A, int grid, cudaStream_t s) {
+  return c.expire_wait > 0 ? launch<CLUSTER, true>(c, A, grid, s) : launch<CLUSTER, false>(c, A, grid, s);
 }
 
 }  // namespace

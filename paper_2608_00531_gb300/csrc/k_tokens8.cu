@@ -40,7 +40,7 @@ constexpr float kLift = 7.f;            // P' is 2^kLift times what it stands fo
 
 struct Lay {
   static constexpr int m_tiles = 1, threads = kThreads12, alone = kWorkers;
-  enum : int { B_FULL = 0, B_DONE = B_FULL + kWorkers * NS, B_FREE, B_JOIN, piece_bar, taken_bar = piece_bar + kPieces, num_bars = taken_bar + kPieces };
+  enum : int { B_FULL = 0, B_DONE = B_FULL + kWorkers * NS, B_FREE, B_JOIN, piece_bar, taken_bar = piece_bar + kPieces, B_NEVER = taken_bar + kPieces, num_bars };
   static constexpr int ring = 0;                                   // [warp][stage][K, V][32 keys][128]
   static_assert(kRows * D * 4 == 2 * kHalf, "a warp's sums take a stage's place");
   static constexpr int lse = ring + kWorkers * NS * 2 * kHalf;     // float [warp][16 rows]
@@ -103,7 +103,8 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-template <bool MAY_ALONE>
+// EXPIRE (self-test): one wait of one warp runs out.
+template <bool MAY_ALONE, bool EXPIRE>
 __global__ void __launch_bounds__(kThreads12, 1)
 tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                const TokenArgs<MAY_ALONE> A) {
@@ -128,6 +129,7 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       mbar_init(bar(Lay::piece_bar + i), 1);
       mbar_init(bar(Lay::taken_bar + i), kWorkers);
     }
+    if constexpr (EXPIRE) mbar_init(bar(Lay::B_NEVER), 1);
     *abort_flag = 0;
     *n_joins = 0;
     *reinterpret_cast<volatile int*>(smem + Lay::mode) = 0;
@@ -137,7 +139,11 @@ tokens8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   }
   pdl_begin();
   __syncthreads();
-  Await<false> await;
+  Await<EXPIRE> await;
+  if constexpr (EXPIRE) {
+    await.never = bar(Lay::B_NEVER);
+    await.left = blockIdx.x == 0 && warp == A.expire_warp ? (uint32_t)A.expire_wait : 0u;
+  }
 
   if (warp == kWorkers) {
     schedule<Lay>(A, npb, await, bar, smem, aborted, lane);
@@ -549,7 +555,7 @@ bool tokens8_fits(const Attn8Call& c) {
   return !c.n_nodes && G <= kRows && c.rows <= (int64_t)c.batch * (kRows / G);
 }
 
-template <bool ALONE>
+template <bool ALONE, bool EXPIRE>
 static cudaError_t launch(const Attn8Call& c, cudaStream_t s) {
   constexpr int bytes = ALONE ? Lay::bytes_alone : Lay::bytes;
   static std::atomic<uint64_t> ready;  // devices on which it has its shared memory
@@ -558,7 +564,7 @@ static cudaError_t launch(const Attn8Call& c, cudaStream_t s) {
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(ready.load() & bit)) {
-    e = cudaFuncSetAttribute(tokens8_kernel<ALONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    e = cudaFuncSetAttribute(tokens8_kernel<ALONE, EXPIRE>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit);
   }
@@ -571,14 +577,15 @@ static cudaError_t launch(const Attn8Call& c, cudaStream_t s) {
   A.q = c.q;
   A.k_scale = c.k_scale;
   A.v_scale = c.v_scale;
-  return launch_pdl(tokens8_kernel<ALONE>, dim3((unsigned)num_sms()), dim3(kThreads12), (size_t)bytes, s, mk, mv, A);
+  return launch_pdl(tokens8_kernel<ALONE, EXPIRE>, dim3((unsigned)num_sms()), dim3(kThreads12), (size_t)bytes, s, mk, mv, A);
 }
 
 // Fewer units than two to an SM are never a warp's each; the kernel that asks is 2 to 3 % slower where the answer is
 // no (64 sequences of 500 to 16000 keys, 4 heads of K and V: 98 us, not 96).
 cudaError_t launch_tokens8(const Attn8Call& c, cudaStream_t s) {
-  return c.batch > 32 && (int64_t)c.rows * c.kv.heads_kv >= (int64_t)2 * num_sms() ? launch<true>(c, s)
-                                                                                  : launch<false>(c, s);
+  const bool alone = c.batch > 32 && (int64_t)c.rows * c.kv.heads_kv >= (int64_t)2 * num_sms();
+  if (c.expire_wait > 0) return alone ? launch<true, true>(c, s) : launch<false, true>(c, s);
+  return alone ? launch<true, false>(c, s) : launch<false, false>(c, s);
 }
 
 }  // namespace cure

@@ -62,6 +62,8 @@ inline void fill_args8(const Attn8Call& c, PromptArgs* A) {
   A->scale_log2 = c.scale * 1.4426950408889634f;
   A->out = c.out;
   A->err = c.err;
+  A->expire_warp = c.expire_warp;
+  A->expire_wait = c.expire_wait;
   A->tag = next_launch_tag();  // whatever the workspace's counters hold counts as zero
   const int ctas = num_sms();
   char* ws = static_cast<char*>(c.workspace);

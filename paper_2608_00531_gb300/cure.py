@@ -668,7 +668,17 @@ def cure_tree_attn8(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                     anc: torch.Tensor, scale: float, *, out: Optional[torch.Tensor] = None,
                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """cure_tree_attn over a cache held in 8 bits, in the in-place layout: q bf16 [B][n_max][heads_q][D], node j's K/V
-    rows at slot cache_len[b] + j (cure_append_kv8 with row_start = 0, n_max, 2 n_max, .. and the tree's ``pos``)."""
+    rows at slot cache_len[b] + j (cure_append_kv8 with row_start = 0, n_max, 2 n_max, .. and the tree's ``pos``; around
+    rows that may not stay, cure_save_kv8 and cure_restore_kv8)."""
+    out, held, args = _tree_attn8_args(q, k_cache, v_cache, k_scale, v_scale, kv, cache_len, n_nodes, anc, scale, out,
+                                       workspace, stream)
+    check("cure_tree_attn8", _lib.load().cure_tree_attn8(*args))
+    return out
+
+
+def _tree_attn8_args(q, k_cache, v_cache, k_scale, v_scale, kv: KVDesc, cache_len, n_nodes, anc, scale, out, workspace,
+                     stream):
+    """As _prompt_attn_args, of cure_tree_attn8."""
     dev, s = _current(stream)
     shape = q.shape
     if len(shape) != 4 or shape[3] != kv.head_dim:
@@ -687,11 +697,10 @@ def cure_tree_attn8(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
         workspace = _new((max(cure_tree_attn8_workspace_size(B, n_max, Hq, kv), 256),), torch.uint8, stream)
     kc, vc = _caches(k_cache, v_cache, kv, B, dev, _E4M3)
     ks, vs = _scales(k_scale, v_scale, kv, B, dev)
-    check("cure_tree_attn8", _lib.load().cure_tree_attn8(
+    return out, workspace, (
         _here(q, "q", _BF16, dev), kc, vc, ks, vs, C.byref(kv), _here(cache_len, "cache_len", _I32, dev),
         _here(n_nodes, "n_nodes", _I32, dev), _here(anc, "anc", torch.int64, dev), B, n_max, Hq, scale,
-        _here(out, "out", _BF16, dev), _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s))
-    return out
+        _here(out, "out", _BF16, dev), _here(workspace, "workspace", torch.uint8, dev), workspace.numel(), s)
 
 
 def cure_resync_kv8(k_caches: Sequence[torch.Tensor], v_caches: Sequence[torch.Tensor],
@@ -829,6 +838,31 @@ def cure_selftest_prompt_timeout(q: torch.Tensor, k_cache: torch.Tensor, v_cache
     out, held, args = _prompt_attn_args(q, k_cache, v_cache, kv, row_start, cache_len, scale, out, workspace, stream)
     check("cure_selftest_prompt_timeout",
           _lib.load().cure_selftest_prompt_timeout(*args[:-1], int(warp), int(wait), args[-1]))
+    return out
+
+
+def cure_selftest_prompt8_timeout(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor,
+                                  v_scale: torch.Tensor, kv: KVDesc, row_start: torch.Tensor, cache_len: torch.Tensor,
+                                  scale: float, warp: int, wait: int, *, out: Optional[torch.Tensor] = None,
+                                  workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """cure_prompt_attn8 with a wait that runs out, as cure_selftest_prompt_timeout."""
+    out, held, args = _prompt_attn8_args(q, k_cache, v_cache, k_scale, v_scale, kv, row_start, cache_len, scale, out,
+                                         workspace, stream)
+    check("cure_selftest_prompt8_timeout",
+          _lib.load().cure_selftest_prompt8_timeout(*args[:-1], int(warp), int(wait), args[-1]))
+    return out
+
+
+def cure_selftest_tree8_timeout(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor,
+                                v_scale: torch.Tensor, kv: KVDesc, cache_len: torch.Tensor, n_nodes: torch.Tensor,
+                                anc: torch.Tensor, scale: float, warp: int, wait: int, *,
+                                out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                stream=None) -> torch.Tensor:
+    """cure_tree_attn8 with a wait that runs out, as cure_selftest_prompt_timeout."""
+    out, held, args = _tree_attn8_args(q, k_cache, v_cache, k_scale, v_scale, kv, cache_len, n_nodes, anc, scale, out,
+                                       workspace, stream)
+    check("cure_selftest_tree8_timeout",
+          _lib.load().cure_selftest_tree8_timeout(*args[:-1], int(warp), int(wait), args[-1]))
     return out
 
 
