@@ -182,6 +182,7 @@ constexpr float kLift = 7.f;  // P' is 2^kLift times what it stands for: at most
 
 // ---- clusters: barrier, a peer's address of a shared-memory variable, loads from it
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();  // (what stands before may have left the warp's lanes apart, which an aligned barrier must not meet)
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t map_rank(uint32_t addr, int rank) {
@@ -935,6 +936,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ C
   } else if (!*abort_flag) {
     join_units<Lay>(A, npb, smem, *n_joins, warp, lane);
   }
+  __syncwarp();
   if (warp == 0) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);

@@ -667,6 +667,7 @@ __device__ __forceinline__ void join_units(const Args& A, int npb, const uint8_t
     if (rows8 >= 8) join(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
     else join(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
   }
+  __syncwarp();  // (what comes next is aligned: TMEM is given back)
 }
 
 }  // namespace prompt
