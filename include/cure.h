@@ -25,7 +25,8 @@
  *   cure_append_kv    Alg. 1 (input)        the same for prompt rows, K and V into the cache
  *   cure_prompt_attn  Alg. 1 (input)        causal attention of prompt rows over the cache
  * Each with several positions a token (cure_rope_qkv_axes, cure_append_kv_axes), and over a cache
- * held in 8 bits (cure_append_kv8, cure_prompt_attn8, cure_tree_attn8, cure_resync_kv8).
+ * held in 8 bits (cure_append_kv8, cure_prompt_attn8, cure_tree_attn8, cure_save_kv8,
+ * cure_restore_kv8, cure_resync_kv8).
  *
  * Conventions shared by every call
  *  - Every pointer argument is a DEVICE pointer unless stated otherwise; the
@@ -542,8 +543,10 @@ cure_status cure_append_kv8(const void* q, const void* k, const void* v, int64_t
  * cure_prompt_attn over a cache in 8 bits: the same formula with k = code * scale, and
  * the same rows, limits, errors and workspace rules.  Any scales from 2^-40 to 2^40
  * will do, not only powers of two; others (NaN, too) count as the nearer of those two.
- * Scores: q in two e4m3 parts, which hold it but for 2^-18 of its row's largest value;
- * products of e4m3 in float32.  A probability times its block's scale is
+ * Scores: q in two e4m3 parts, which hold it but for 2^-17 of its row's largest value
+ * (2^-10 / 224 in the parts' units), products of e4m3 in float32; of single tokens and
+ * the like (up to 16 / (heads_q / heads_kv) rows a sequence on average) q in fp16 under a
+ * power of two a row, but for 2^-32 of the row's largest value, products in float32.  A probability times its block's scale is
  * rounded to fp16, by up to 2^-11 of itself, or 2^-32 of the row's largest such term.
  * q must be finite, and V's codes in a sequence's own slots must not be NaN (K's may be
  * where a row does not see them).

@@ -9,8 +9,8 @@
 // Scores.  K goes from memory to the tensor cores as it is.  q (8 significant bits) is two
 // e4m3 values (4 bits each): with its row scaled by a power of two to at most 448,
 //   q = q1 + q2,  q1 = e4m3(q),  q2 = e4m3(q - q1)
-// is exact down to 2^-9 of steps, 2^-18 of the row's largest value.  S = q1 K + q2 K are 8
-// products of 32 dims where bf16 has 8 of 16, at twice the rate.
+// is exact but for q2's smallest step, 2^-9: at most 2^-10 where the row's largest value is above 224, 2^-17 of that.
+// S = q1 K + q2 K are 8 products of 32 dims where bf16 has 8 of 16, at twice the rate.
 //
 // Weights.  V's codes are widened to fp16 (exact), and P is fp16 with the block's scale in it:
 //   P'_j = 2^(s_j + log2 vs_j - M + 7),  M the running maximum of s_j + log2 vs_j
@@ -987,8 +987,9 @@ int max_clusters(int size) {
 }
 
 // CTAs of each unit's cluster for `units` units of one M tile; 0: units cut among all CTAs instead (the
-// faster form where a cluster would have two: 8 trees of up to 33 nodes, 28/4 heads, 50.5 us so, 53.7 in
-// clusters of 2; 4 of them 51.1 and, in clusters of 4, 36.9; one of 25 nodes, 32/8 heads, 30.7 and 18.5).
+// faster form where a cluster would have two).  us cut and in clusters, trees of 17 to 33 nodes behind 1024 to 8192
+// tokens, 28/4 heads: 8 of them 45.6 and, in clusters of 2, 47.6; 6 41.6 and 51.6; 5 42.3 and, of 3, 39.3; 4 45.2 and,
+// of 4, 31.2; 2 43.7 and 24.1.  One of 25 nodes behind 4096, 32/8 heads: 26.5 and 14.7.
 int cluster_size(int64_t units) {
   for (int c = kAttnMaxCluster; c >= 3; --c)
     if (units <= max_clusters(c)) return c;

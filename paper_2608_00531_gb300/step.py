@@ -184,7 +184,8 @@ class RepairVerifyStep:
     def run(self, x: StepInputs, k_caches: List[torch.Tensor], v_caches: List[torch.Tensor],
             stream=None, scales=None) -> dict:
         """One step.  scales: (k_scales, v_scales), a tensor for each cache, where the caches are held in 8 bits; the
-        tree's rows then go into the caches, behind the sequences' tokens, and are attended to there.  They leave
+        tree's rows then go into the caches, behind the sequences' tokens (where there must be room for all of a
+        sequence's nodes), and are attended to there.  They leave
         the caches again before the accepted path's rows are written: what a sequence holds keeps its codes and scales
         whatever the rejected rows are.  Layers that share a cache (layer_map) cannot be held in 8 bits."""
         if scales is not None and len(set(self.layer_map[:self.layers])) < self.layers:
