@@ -100,14 +100,18 @@ def test_next_pos_is_checked(cure, chain):  # noqa: F811
 
 
 def test_from_host(cure, chain):  # noqa: F811
-    """run_from_host takes rows that are rotated already; its tree has the positions that it is given."""
-    if chain["caches"][0][0].dtype is not torch.bfloat16:
-        pytest.skip("steps from the host are over bf16 caches")
+    """run_from_host takes rows that are rotated already; its tree has the positions that it is given.  It refuses caches in
+    8 bits."""
     from paper_2608_00531_gb300.step import StepInputs
     x, rnd = chain["x"], chain["rnd"]
     xh = StepInputs(*(t.cpu() for t in (x.draft_logits, x.root_tok, x.cache_len)), None,
                     *(rnd(LAYERS, B, N_MAX, h, 128).cpu() for h in (HQ, HKV, HKV)), x.target_logits.cpu(),
                     next_pos=torch.tensor(chain["at"], dtype=torch.int32))
+    if chain["caches"][0][0].dtype is not torch.bfloat16:
+        with pytest.raises(TypeError):
+            chain["step"].run_from_host(xh, *chain["caches"])
+        torch.cuda.synchronize()
+        return
     for want, xh in ((chain["at"], xh), (chain["n"], dataclasses.replace(xh, next_pos=None))):
         r = chain["step"].run_from_host(xh, *chain["caches"])
         tree = r["tree"]
