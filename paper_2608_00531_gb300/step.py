@@ -187,7 +187,8 @@ class RepairVerifyStep:
         tree's rows then go into the caches, behind the sequences' tokens (where there must be room for all of a
         sequence's nodes), and are attended to there.  They leave
         the caches again before the accepted path's rows are written: what a sequence holds keeps its codes and scales
-        whatever the rejected rows are.  Layers that share a cache (layer_map) cannot be held in 8 bits."""
+        whatever the rejected rows are.  (The step's own attention reads a sequence's last, shared block under the scale
+        that all of its rows give it.)  Layers that share a cache (layer_map) cannot be held in 8 bits."""
         if scales is not None and len(set(self.layer_map[:self.layers])) < self.layers:
             raise ValueError("layers that share a cache cannot be held in 8 bits")
         root_pos = x.cache_len if x.next_pos is None else x.next_pos
